@@ -33,6 +33,18 @@
  *                            and top-K KL from one sweep with both heads
  *   olive_token_logprob_fwd_noalloc  the forward without a workspace
  *
+ * The hidden rows come out of a decoder layer and the gradients go into an
+ * optimiser.  The parts of that way which meet the packed batch have calls too
+ * (the paper trains such students, Appendix A, and prints none of them):
+ *
+ *   olive_packed_positions   position of every packed token in its sequence
+ *   olive_qk_norm_rope_fwd, olive_qk_norm_rope_bwd
+ *                            RMS norm of each query and key head and rotation
+ *                            by position, in one pass
+ *   olive_gated_mlp_fwd, olive_gated_mlp_bwd
+ *                            gated feed-forward block with its residual
+ *   olive_grad_clip          global norm of a list of gradients, and clipping
+ *
  * Conventions shared by every call
  *   - Every pointer argument is a DEVICE pointer unless stated otherwise.  The
  *     caller owns every buffer; no call allocates device memory.  Scratch
@@ -101,10 +113,12 @@ typedef enum {
 enum { OLIVE_REDUCE_SUM = 0, OLIVE_REDUCE_MEAN = 1 };
 enum { OLIVE_KL_REVERSE = 0, OLIVE_KL_FORWARD = 1 };
 enum { OLIVE_DTYPE_BF16 = 0, OLIVE_DTYPE_F32 = 1 };
+enum { OLIVE_ACT_SILU = 0, OLIVE_ACT_GELU_TANH = 1 };
 enum { OLIVE_OP_LOGPROB_FWD = 0, OLIVE_OP_LOSS_BWD = 1, OLIVE_OP_DIVERGENCE = 2,
        OLIVE_OP_TOPK_FWD = 3, OLIVE_OP_SPLICE_MASKED = 4, OLIVE_OP_TOPK_KL_BWD = 5,
        OLIVE_OP_LOSS_FWD_BWD = 6, OLIVE_OP_OPD_STATS = 7, OLIVE_OP_TOPK_KL_FWD_BWD = 8,
-       OLIVE_OP_LOSS_FWD_BWD_SLAB = 9 };
+       OLIVE_OP_LOSS_FWD_BWD_SLAB = 9, OLIVE_OP_GATED_MLP_FWD = 10,
+       OLIVE_OP_GATED_MLP_BWD = 11, OLIVE_OP_QK_NORM_ROPE_BWD = 12, OLIVE_OP_GRAD_CLIP = 13 };
 
 /*
  * Rows of the G slab that the slab forms (olive_token_loss_fwd_bwd_slab,
@@ -136,6 +150,10 @@ OLIVE_API olive_status olive_status_clear(int32_t* dev_status, void* stream);
  *   op  OLIVE_OP_TOPK_KL_BWD, OLIVE_OP_LOSS_FWD_BWD,
  *       OLIVE_OP_TOPK_KL_FWD_BWD: d = (student) hidden width, grad_dtype as
  *       for OLIVE_OP_LOSS_BWD, d_t ignored.
+ *   op  OLIVE_OP_GATED_MLP_FWD / OLIVE_OP_GATED_MLP_BWD: d = hidden width,
+ *       V = inner width f, d_t ignored.
+ *   op  OLIVE_OP_QK_NORM_ROPE_BWD: d = head width; the rest ignored.
+ *   op  OLIVE_OP_GRAD_CLIP: T = number of tensors; the rest ignored.
  *   `grad` (bwd / divergence): non-zero when gradients are requested
  *   (OLIVE_OP_LOSS_BWD always computes them); `grad_dtype` is the dtype of
  *   d_W for OLIVE_OP_LOSS_BWD (bf16 output needs an fp32 accumulator).
@@ -520,6 +538,130 @@ OLIVE_API olive_status olive_token_logprob_fwd_noalloc(const void* hidden, const
                                                        int32_t V, float inv_tau, int reduction,
                                                        float* logp, float* lse, float* loss,
                                                        int32_t* dev_status, void* stream);
+
+/*
+ * olive_packed_positions -- position of every packed token inside its own
+ * sequence, from olive_splice_pack's cu_seqlens [S+1]:
+ *   positions[t] = t - cu_seqlens[s]  for cu_seqlens[s] <= t < cu_seqlens[s+1]
+ * and 0 for cu_seqlens[S] <= t < T_cap.  positions int32 [T_cap], T_cap >= 1,
+ * S >= 1.
+ */
+OLIVE_API olive_status olive_packed_positions(const int32_t* cu_seqlens, int32_t S, int32_t T_cap,
+                                              int32_t* positions, void* stream);
+
+/*
+ * olive_qk_norm_rope_fwd -- for every token t and every head of q (Hq heads)
+ * and of k (Hk heads), x the head's D values, w = w_q or w_k [D]:
+ *   n = w x / sqrt(mean(x^2) + eps)                                  (fp32)
+ *   (out[i], out[i']) = (n[i] c - n[i'] s, n[i'] c + n[i] s)
+ *     with c = cos_table[p, j], s = sin_table[p, j], p = positions[t], for the
+ *     pairs j < R/2: (i, i') = (j, j + R/2), or (2 j, 2 j + 1) if `interleaved`
+ *   out[i] = n[i] for R <= i < D
+ * rounded once to `dtype` (OLIVE_DTYPE_BF16 or OLIVE_DTYPE_F32), the type of
+ * q, k, w_q, w_k and the outputs.  Any scaling of the angles for long contexts
+ * is in the tables: cos_table, sin_table fp32 [P, R/2].
+ *   Head h of token t starts at q + t q_token_stride + h q_head_stride
+ *   (elements), so q and k can be views of one fused projection; its D values
+ *   are contiguous.  The outputs have strides of their own; an output may be
+ *   its own input (same pointer and strides).
+ *   D a multiple of 8, 8 <= D <= 256; R a multiple of 8, 0 <= R <= D; Hq, Hk
+ *   >= 0, not both 0 (the pointers of a side without heads are ignored); T >= 0;
+ *   strides multiples of 8, base pointers 16-byte aligned; eps >= 0.
+ * A position outside [0, P) gives NaN for its token and OLIVE_ERR_TOKEN_RANGE;
+ * dev_status may be NULL (nothing is reported then).
+ */
+OLIVE_API olive_status olive_qk_norm_rope_fwd(
+    const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k,
+    int64_t k_token_stride, int64_t k_head_stride, int32_t Hq, int32_t Hk, const void* w_q,
+    const void* w_k, float eps, const float* cos_table, const float* sin_table,
+    const int32_t* positions, int32_t P, int32_t T, int32_t D, int32_t R, int interleaved,
+    void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
+    int64_t k_out_token_stride, int64_t k_out_head_stride, int dtype, int32_t* dev_status,
+    void* stream);
+
+/*
+ * olive_qk_norm_rope_bwd -- gradients of olive_qk_norm_rope_fwd for its inputs
+ * q, k (as they went in) and the gradients g_q, g_k of its outputs: with dn the
+ * rotation of g by the opposite angle and r = 1 / sqrt(mean(x^2) + eps),
+ *   dx = r (dn w - x r^2 mean(dn w x)),     dw = sum over tokens and heads of dn x r
+ * d_q, d_k have the type of q and strides of their own (d_q may be g_q, with its
+ * strides); dw_q, dw_k fp32 [D] are both written (0 for a side without heads)
+ * and summed in a fixed order, in fp32 per thread and fp64 across threads.
+ * workspace: olive_workspace_size(OLIVE_OP_QK_NORM_ROPE_BWD, 1, D, 0, 1, 0, 0) bytes.
+ */
+OLIVE_API olive_status olive_qk_norm_rope_bwd(
+    const void* g_q, int64_t g_q_token_stride, int64_t g_q_head_stride, const void* g_k,
+    int64_t g_k_token_stride, int64_t g_k_head_stride, const void* q, int64_t q_token_stride,
+    int64_t q_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+    int32_t Hq, int32_t Hk, const void* w_q, const void* w_k, float eps, const float* cos_table,
+    const float* sin_table, const int32_t* positions, int32_t P, int32_t T, int32_t D, int32_t R,
+    int interleaved, void* d_q, int64_t d_q_token_stride, int64_t d_q_head_stride, void* d_k,
+    int64_t d_k_token_stride, int64_t d_k_head_stride, float* dw_q, float* dw_k, int dtype,
+    void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * olive_gated_mlp_fwd -- the gated feed-forward block on T rows:
+ *   g = x W_gate^T, u = x W_up^T           [T, f], fp32 accumulation
+ *   h = act(g) u                           bf16 (the operand of the next product)
+ *   y = h W_down^T (+ residual)            [T, d], rounded once to bf16
+ * act: OLIVE_ACT_SILU, g / (1 + exp(-g)), or OLIVE_ACT_GELU_TANH,
+ * g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).  bf16: x [T, d], W_gate and
+ * W_up [f, d], W_down [d, f], residual [T, d] or NULL (y may be residual), y
+ * [T, d].  `saved`, if not NULL, takes g and u for olive_gated_mlp_bwd: 4 T f
+ * bytes, 16-byte aligned, to be passed on as they are.  (16 bits each: a sign,
+ * 6 exponent and 9 fraction bits, 2^-10 relative.  bf16's 2^-8 would put as
+ * large an error on the gradients as rounding them to bf16 operands does.
+ * Magnitudes below 2^-30 lose accuracy and vanish below 2^-39; those above
+ * 2^33 are held as 2^33, infinities and NaN become NaN.)
+ * T >= 0 (0: nothing happens), d and f multiples of 8.  dev_status may be NULL.
+ * workspace: olive_workspace_size(OLIVE_OP_GATED_MLP_FWD, T, d, 0, f, 0, 0) bytes.
+ */
+OLIVE_API olive_status olive_gated_mlp_fwd(const void* x, const void* W_gate, const void* W_up,
+                                           const void* W_down, const void* residual, int32_t T,
+                                           int32_t d, int32_t f, int activation, void* y,
+                                           void* saved, void* workspace, size_t ws_bytes,
+                                           int32_t* dev_status, void* stream);
+
+/*
+ * olive_gated_mlp_bwd -- gradients of olive_gated_mlp_fwd (the residual's is dy
+ * itself), with g, u from `saved`:
+ *   dh = dy W_down,  dg = dh u act'(g),  du = dh act(g)     (dg, du bf16 operands)
+ *   dx = dg W_gate + du W_up
+ *   dW_gate = dg^T x,  dW_up = du^T x,  dW_down = dy^T h    (h formed again)
+ * dy, x bf16 [T, d]; dx [T, d] and the weights' gradients (shaped as the
+ * weights) of grad_dtype.  dx may be NULL, and so may the three weights'
+ * gradients together: what is NULL is not computed (not everything may be).
+ * T >= 0 (0: the weights' gradients are zeroed).  workspace:
+ * olive_workspace_size(OLIVE_OP_GATED_MLP_BWD, T, d, 0, f, 1, grad_dtype) bytes.
+ */
+OLIVE_API olive_status olive_gated_mlp_bwd(const void* dy, const void* x, const void* W_gate,
+                                           const void* W_up, const void* W_down, const void* saved,
+                                           int32_t T, int32_t d, int32_t f, int activation,
+                                           void* dx, void* dW_gate, void* dW_up, void* dW_down,
+                                           int grad_dtype, void* workspace, size_t ws_bytes,
+                                           int32_t* dev_status, void* stream);
+
+/*
+ * olive_grad_clip -- the 2-norm over all elements of n tensors together, and
+ * the tensors scaled so that it is at most max_norm:
+ *   norm[0] = sqrt(sum over all tensors of g^2)
+ *   dst[i]  = src[i] min(1, max_norm / (norm + 1e-6))
+ * src, dst, numel and dtype are HOST arrays of n entries (read before the call
+ * returns): device pointers, element counts (0 allowed: the pointers are then
+ * ignored) and OLIVE_DTYPE_BF16 or OLIVE_DTYPE_F32, tensor by tensor.  dst[i]
+ * may be src[i] (a factor of exactly 1 then writes nothing) but must not overlap
+ * it otherwise, nor another tensor; dst NULL: only the norm.  Any alignment of
+ * whole elements; 16-byte aligned pointers are read and written in 16-byte
+ * pieces.  The squares are summed in fp32 by 32s, in fp64 beyond (and in fp64
+ * throughout where fp32 squares would leave its range), in a fixed order.
+ * A norm that is infinite or NaN goes into the factor as it is (0 or NaN).
+ * norm fp32 [1] (device); n >= 0 (0: the norm is 0); max_norm > 0.
+ * workspace: olive_workspace_size(OLIVE_OP_GRAD_CLIP, max(n, 1), 0, 0, 1, 0, 0) bytes.
+ */
+OLIVE_API olive_status olive_grad_clip(const void* const* src, void* const* dst,
+                                       const int64_t* numel, const int32_t* dtype, int32_t n,
+                                       float max_norm, float* norm, void* workspace,
+                                       size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -30,7 +30,9 @@ DIRECTION = {"reverse": 0, "forward": 1}
 DTYPE = {torch.bfloat16: 0, torch.float32: 1}
 OP = {"logprob_fwd": 0, "loss_bwd": 1, "divergence": 2, "topk_fwd": 3, "splice_masked": 4,
       "topk_kl_bwd": 5, "loss_fwd_bwd": 6, "opd_stats": 7, "topk_kl_fwd_bwd": 8,
-      "loss_fwd_bwd_slab": 9}
+      "loss_fwd_bwd_slab": 9, "gated_mlp_fwd": 10, "gated_mlp_bwd": 11, "qk_norm_rope_bwd": 12,
+      "grad_clip": 13}
+ACT = {"silu": 0, "gelu_tanh": 1}
 
 
 class OliveError(RuntimeError):
@@ -44,6 +46,7 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _F = ctypes.c_float
 _S = ctypes.c_size_t
+_L = ctypes.c_int64
 
 
 def lib() -> ctypes.CDLL:
@@ -118,6 +121,23 @@ def _configure(L: ctypes.CDLL) -> ctypes.CDLL:
     L.olive_token_logprob_fwd_noalloc.restype = ctypes.c_int
     L.olive_token_logprob_fwd_noalloc.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, _F, ctypes.c_int,
                                                   _P, _P, _P, _P, _P]
+    view = [_P, _L, _L]
+    heads = [_I, _I, _P, _P, _F, _P, _P, _P, _I, _I, _I, _I, ctypes.c_int]
+    L.olive_packed_positions.restype = ctypes.c_int
+    L.olive_packed_positions.argtypes = [_P, _I, _I, _P, _P]
+    L.olive_qk_norm_rope_fwd.restype = ctypes.c_int
+    L.olive_qk_norm_rope_fwd.argtypes = view * 2 + heads + view * 2 + [ctypes.c_int, _P, _P]
+    L.olive_qk_norm_rope_bwd.restype = ctypes.c_int
+    L.olive_qk_norm_rope_bwd.argtypes = (view * 4 + heads + view * 2 +
+                                         [_P, _P, ctypes.c_int, _P, _S, _P, _P])
+    L.olive_gated_mlp_fwd.restype = ctypes.c_int
+    L.olive_gated_mlp_fwd.argtypes = [_P, _P, _P, _P, _P, _I, _I, _I, ctypes.c_int, _P, _P, _P, _S,
+                                      _P, _P]
+    L.olive_gated_mlp_bwd.restype = ctypes.c_int
+    L.olive_gated_mlp_bwd.argtypes = [_P, _P, _P, _P, _P, _P, _I, _I, _I, ctypes.c_int, _P, _P, _P,
+                                      _P, ctypes.c_int, _P, _S, _P, _P]
+    L.olive_grad_clip.restype = ctypes.c_int
+    L.olive_grad_clip.argtypes = [_P, _P, _P, _P, _I, _F, _P, _P, _S, _P]
     return L
 
 
@@ -568,6 +588,218 @@ def olive_scale(x, scale, out=None):
     return out
 
 
+def olive_packed_positions(cu_seqlens, T_cap: int, out=None):
+    """Position of every packed token inside its sequence (int32 [T_cap], 0
+    behind the last one) from olive_splice_pack's cu_seqlens."""
+    _need(cu_seqlens, torch.int32, "cu_seqlens")
+    if out is None:
+        out = torch.empty(T_cap, dtype=torch.int32, device=cu_seqlens.device)
+    _need(out, torch.int32, "out")
+    if out.numel() != T_cap:
+        raise ValueError("out holds T_cap positions")
+    st = lib().olive_packed_positions(_ptr(cu_seqlens), cu_seqlens.numel() - 1, T_cap, _ptr(out),
+                                      _stream())
+    _check(st, "olive_packed_positions")
+    return out
+
+
+def _heads(t, T, D, dtype, name, device):
+    """(pointer, token stride, head stride) of a [T, H, D] view with contiguous heads."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+        raise TypeError(f"{name} must be a CUDA {dtype} tensor on {device}")
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D:
+        raise ValueError(f"{name} must have the shape [{T}, heads, {D}]")
+    a, b, c = t.stride()
+    if c != 1 and D > 1:
+        raise TypeError(f"{name}: the {D} values of a head must be contiguous")
+    # (the stride of a dimension of one entry means nothing)
+    return t.data_ptr(), a if T > 1 else 0, b if t.shape[1] > 1 else 0
+
+
+def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
+    """Checks what the heads' forward and backward share; (views of q and k, the
+    shared C arguments, T, D, dtype)."""
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dtype not in DTYPE or q.dim() != 3:
+        raise TypeError("q must be a CUDA bf16 or fp32 tensor [T, heads, D]")
+    T, Hq, D = q.shape
+    dtype, dev = q.dtype, q.device
+    vq, vk = _heads(q, T, D, dtype, "q", dev), _heads(k, T, D, dtype, "k", dev)
+    for t, n in ((w_q, "w_q"), (w_k, "w_k")):
+        _need(t, dtype, n)
+        if t.numel() != D:
+            raise ValueError(f"{n} must hold {D} values")
+    _need(cos, torch.float32, "cos")
+    _need(sin, torch.float32, "sin")
+    _need(positions, torch.int32, "positions")
+    if cos.dim() != 2 or cos.shape != sin.shape:
+        raise ValueError("cos and sin must have the same shape [P, R/2]")
+    if positions.numel() != T:
+        raise ValueError(f"positions must hold {T} values")
+    P, half = cos.shape
+    common = (Hq, k.shape[1], w_q.data_ptr(), w_k.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(),
+              positions.data_ptr(), P, T, D, 2 * half, 1 if interleaved else 0)
+    return vq, vk, common, T, D, dtype
+
+
+def olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps: float = 1e-6,
+                           interleaved: bool = False, dev_status=None, out=None):
+    """RMS norm of every head of q [T, Hq, D] and k [T, Hk, D] (weights w_q, w_k
+    [D]) and rotation by positions [T] with the tables cos, sin (fp32 [P, R/2];
+    R <= D).  q and k may be views of one projection.  Returns (q_out, k_out),
+    contiguous unless given as `out` (views, or q and k themselves)."""
+    vq, vk, common, T, D, dtype = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    if out is None:
+        out = (torch.empty(q.shape, dtype=dtype, device=q.device),
+               torch.empty(k.shape, dtype=dtype, device=q.device))
+    yq, yk = out
+    if yq.shape != q.shape or yk.shape != k.shape:
+        raise ValueError("outputs must have the shapes of q and k")
+    st = lib().olive_qk_norm_rope_fwd(*vq, *vk, *common,
+                                      *_heads(yq, T, D, dtype, "q_out", q.device),
+                                      *_heads(yk, T, D, dtype, "k_out", q.device), DTYPE[dtype],
+                                      _ptr(dev_status), _stream())
+    _check(st, "olive_qk_norm_rope_fwd")
+    return yq, yk
+
+
+def olive_qk_norm_rope_bwd(g_q, g_k, q, k, w_q, w_k, cos, sin, positions, eps: float = 1e-6,
+                           interleaved: bool = False, ws=None, dev_status=None, out=None):
+    """Gradients of olive_qk_norm_rope_fwd for its inputs q, k and the gradients
+    g_q, g_k of its outputs.  Returns (d_q, d_k, dw_q, dw_k), the weights' in fp32;
+    `out` takes (d_q, d_k), e.g. views of one projection's gradient."""
+    vq, vk, common, T, D, dtype = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    dev = q.device
+    if g_q.shape != q.shape or g_k.shape != k.shape:
+        raise ValueError("g_q and g_k must have the shapes of q and k")
+    if out is None:
+        out = (torch.empty(q.shape, dtype=dtype, device=dev), torch.empty(k.shape, dtype=dtype, device=dev))
+    dq, dk = out
+    if dq.shape != q.shape or dk.shape != k.shape:
+        raise ValueError("outputs must have the shapes of q and k")
+    dw = torch.empty(2, D, dtype=torch.float32, device=dev)
+    if ws is None:
+        ws = workspace(lib().olive_workspace_size(OP["qk_norm_rope_bwd"], 1, D, 0, 1, 0, 0), dev)
+    dwq, dwk = dw[0], dw[1]
+    st = lib().olive_qk_norm_rope_bwd(*_heads(g_q, T, D, dtype, "g_q", dev),
+                                      *_heads(g_k, T, D, dtype, "g_k", dev), *vq, *vk, *common,
+                                      *_heads(dq, T, D, dtype, "d_q", dev),
+                                      *_heads(dk, T, D, dtype, "d_k", dev), dwq.data_ptr(),
+                                      dwk.data_ptr(), DTYPE[dtype], _ptr(ws), ws.numel(),
+                                      _ptr(dev_status), _stream())
+    _check(st, "olive_qk_norm_rope_bwd")
+    return dq, dk, dwq, dwk
+
+
+def _mlp_args(x, W_gate, W_up, W_down):
+    for t, n in ((x, "x"), (W_gate, "W_gate"), (W_up, "W_up"), (W_down, "W_down")):
+        _need(t, torch.bfloat16, n)
+    if x.dim() != 2:
+        raise ValueError("x must have the shape [T, d]")
+    T, d = x.shape
+    f = W_gate.shape[0]
+    if W_gate.shape != (f, d) or W_up.shape != (f, d) or W_down.shape != (d, f):
+        raise ValueError("W_gate and W_up must have the shape [f, d], W_down [d, f]")
+    return T, d, f
+
+
+def olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual=None, act: str = "silu",
+                        save: bool = False, ws=None, dev_status=None, out=None):
+    """Gated feed-forward block on the rows of x [T, d] (bf16):
+    (act(x W_gate^T) * (x W_up^T)) W_down^T (+ residual), act "silu" or
+    "gelu_tanh".  Returns (y, saved): saved, with save=True, is what
+    olive_gated_mlp_bwd takes (the pre-activations in 16 bits, 4 T f bytes), else
+    None."""
+    T, d, f = _mlp_args(x, W_gate, W_up, W_down)
+    dev = x.device
+    if residual is not None:
+        _need(residual, torch.bfloat16, "residual")
+        if residual.shape != x.shape:
+            raise ValueError("residual must have the shape of x")
+    if out is None:
+        out = torch.empty(T, d, dtype=torch.bfloat16, device=dev)
+    else:
+        _need(out, torch.bfloat16, "out")
+        if out.shape != x.shape:
+            raise ValueError("out must have the shape of x")
+    saved = torch.empty(2, T, f, dtype=torch.int16, device=dev) if save else None
+    if ws is None and T > 0:
+        ws = workspace(lib().olive_workspace_size(OP["gated_mlp_fwd"], T, d, 0, f, 0, 0), dev)
+    st = lib().olive_gated_mlp_fwd(_ptr(x), _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(residual),
+                                   T, d, f, ACT[act], _ptr(out), _ptr(saved), _ptr(ws),
+                                   0 if ws is None else ws.numel(), _ptr(dev_status), _stream())
+    _check(st, "olive_gated_mlp_fwd")
+    return out, saved
+
+
+def olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, act: str = "silu",
+                        grad_dtype=torch.bfloat16, need_dx: bool = True, need_dW: bool = True,
+                        ws=None, dev_status=None, out=None):
+    """Gradients of olive_gated_mlp_fwd (that of its residual is dy).  Returns
+    (dx, dW_gate, dW_up, dW_down) of grad_dtype, None for what is not needed."""
+    T, d, f = _mlp_args(x, W_gate, W_up, W_down)
+    dev = x.device
+    _need(dy, torch.bfloat16, "dy")
+    _need(saved, torch.int16, "saved")
+    if dy.shape != x.shape or saved.shape != (2, T, f):
+        raise ValueError("dy must have the shape of x, saved that of the forward")
+    if out is None:
+        e = lambda *shape: torch.empty(*shape, dtype=grad_dtype, device=dev)
+        out = ((e(T, d) if need_dx else None,) +
+               ((e(f, d), e(f, d), e(d, f)) if need_dW else (None, None, None)))
+    else:
+        for t, shape in zip(out, ((T, d), (f, d), (f, d), (d, f))):
+            if t is not None:
+                _need(t, grad_dtype, "out")
+                if t.shape != shape:
+                    raise ValueError("out must have the shapes of x and the weights")
+    if ws is None and T > 0:
+        ws = workspace(lib().olive_workspace_size(OP["gated_mlp_bwd"], T, d, 0, f, 1, DTYPE[grad_dtype]), dev)
+    st = lib().olive_gated_mlp_bwd(_ptr(dy), _ptr(x), _ptr(W_gate), _ptr(W_up), _ptr(W_down),
+                                   _ptr(saved), T, d, f, ACT[act], *[_ptr(t) for t in out],
+                                   DTYPE[grad_dtype], _ptr(ws), 0 if ws is None else ws.numel(),
+                                   _ptr(dev_status), _stream())
+    _check(st, "olive_gated_mlp_bwd")
+    return tuple(out)
+
+
+def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
+    """The 2-norm over all elements of `grads` (bf16 or fp32 CUDA tensors,
+    contiguous) as a 1-element fp32 tensor, and the gradients scaled by
+    min(1, max_norm / (norm + 1e-6)): in place, into the list `out`, or not at
+    all (out=None: only the norm)."""
+    n = len(grads)
+    cur = torch.cuda.current_device()
+    src = (_P * n)()
+    dst = (_P * n)() if out is not None else None
+    num = (_L * n)()
+    kind = (_I * n)()
+    inplace = isinstance(out, str)
+    if inplace and out != "inplace" or not inplace and out is not None and len(out) != n:
+        raise ValueError('out must be "inplace", None or a list of as many tensors as grads')
+    for i, g in enumerate(grads):
+        dt = DTYPE.get(g.dtype)
+        if dt is None or g.get_device() != cur or not g.is_contiguous():
+            raise TypeError(f"gradient {i} must be a contiguous bf16 or fp32 CUDA tensor on the "
+                            "current device")
+        src[i] = g.data_ptr()
+        num[i] = g.numel()
+        kind[i] = dt
+        if out is not None:
+            o = g if inplace else out[i]
+            if not inplace and (o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous() or
+                                o.get_device() != cur):
+                raise TypeError(f"out {i} must be like its gradient")
+            dst[i] = o.data_ptr()
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device="cuda")
+    if ws is None:
+        ws = workspace(lib().olive_workspace_size(OP["grad_clip"], max(n, 1), 0, 0, 1, 0, 0))
+    st = lib().olive_grad_clip(src, dst, num, kind, n, float(max_norm), norm.data_ptr(),
+                               ws.data_ptr(), ws.numel(), _stream())
+    _check(st, "olive_grad_clip")
+    return norm
+
+
 class FusedLMHeadCE(torch.autograd.Function):
     """Eq. (osd-ce) loss over the masked rows as an autograd op (gradients in
     the dtype of hidden).
@@ -609,3 +841,61 @@ class FusedLMHeadCE(torch.autograd.Function):
 def fused_lmhead_ce(hidden, W, targets, rows, n_rows, inv_tau=1.0, reduction="sum",
                     single_pass=True):
     return FusedLMHeadCE.apply(hidden, W, targets, rows, n_rows, inv_tau, reduction, single_pass)
+
+
+class QKNormRope(torch.autograd.Function):
+    """Heads' norm and rotation as an autograd op (weights' gradients in the
+    weights' type)."""
+
+    @staticmethod
+    def forward(ctx, q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=False):
+        ctx.save_for_backward(q, k, w_q, w_k, cos, sin, positions)
+        ctx.eps, ctx.interleaved = eps, interleaved
+        return olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+
+    @staticmethod
+    def backward(ctx, g_q, g_k):
+        q, k, w_q, w_k, cos, sin, positions = ctx.saved_tensors
+        last = lambda g: g if g.stride(-1) == 1 else g.contiguous()
+        dq, dk, dwq, dwk = olive_qk_norm_rope_bwd(last(g_q), last(g_k), q, k, w_q, w_k, cos, sin,
+                                                  positions, ctx.eps, ctx.interleaved)
+        return dq, dk, dwq.to(w_q.dtype), dwk.to(w_k.dtype), None, None, None, None, None
+
+
+def qk_norm_rope(q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=False):
+    return QKNormRope.apply(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+
+
+class GatedMLP(torch.autograd.Function):
+    """Gated feed-forward block as an autograd op (gradients in bf16).  The
+    pre-activations are saved only where a gradient is needed."""
+
+    @staticmethod
+    def forward(ctx, x, W_gate, W_up, W_down, residual=None, act="silu"):
+        needs = ctx.needs_input_grad
+        ctx.act, ctx.need_dx, ctx.need_dW = act, needs[0], any(needs[1:4])
+        y, saved = olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual, act,
+                                       save=ctx.need_dx or ctx.need_dW)
+        if saved is not None:
+            ctx.save_for_backward(x, W_gate, W_up, W_down, saved)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        dy = dy.contiguous()
+        res = dy if ctx.needs_input_grad[4] else None
+        if not (ctx.need_dx or ctx.need_dW):
+            return None, None, None, None, res, None
+        x, W_gate, W_up, W_down, saved = ctx.saved_tensors
+        got = olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, ctx.act, need_dx=ctx.need_dx,
+                                  need_dW=ctx.need_dW)
+        return (*got, res, None)
+
+
+def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu"):
+    return GatedMLP.apply(x, W_gate, W_up, W_down, residual, act)
+
+
+def clip_grad_norm_(parameters, max_norm):
+    """olive_grad_clip in place on the gradients that the parameters hold."""
+    return olive_grad_clip([p.grad for p in parameters if p.grad is not None], max_norm)

@@ -1,0 +1,781 @@
+// gated_mlp.cu -- the gated feed-forward block of a decoder layer on many rows,
+// forward and backward (olive_gated_mlp_fwd, olive_gated_mlp_bwd):
+//   g = x Wg^T, u = x Wu^T, h = act(g) u, y = h Wd^T (+ residual)
+//   dh = dy Wd, dg = dh u act'(g), du = dh act(g)
+//   dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x, dWd = dy^T h
+// as four kinds of one persistent tcgen05 kernel:
+//   MM_UP     g and u of 128 columns side by side in one 256-column
+//             accumulator; h (and, for a backward, g and u) in the epilogue
+//   MM_DOWN   h Wd^T, the residual added in the epilogue
+//   MM_DH     dy Wd; the epilogue reads g and u and writes dg, du and h
+//   MM_GRADS  the four products that are left, in one launch
+//
+// CTA pairs (clusters of two, tcgen05.mma.cta_group::2, M = 256): each CTA
+// stages its 128 rows of A and its half of the 256-wide B, 32 KB per 64-deep K
+// step, and receives its 128 x 256 fp32 accumulator in its own TMEM, twice, so
+// that the epilogue of a tile runs under the next tile's MMAs.  An operand is
+// read K-major or MN-major as it lies in memory; nothing is transposed or
+// copied.  Output tiles leave through shared memory by TMA, which also cuts the
+// ragged edges off.
+//
+// What bounds it: the tensor pipe (a K step of a pair is 512 cycles of MMAs
+// for 64 KB from L2).  Rounding: g and u are used from the fp32 accumulators;
+// h, dg and du are rounded to bf16 once, as operands of the next product; g and
+// u are saved with 10 significant bits (pack_saved below).
+#include <algorithm>
+#include <atomic>
+
+#include "gated_mlp.cuh"
+#include "sm103.cuh"
+
+namespace olive {
+namespace {
+
+constexpr int kBM = 128;             // rows of a CTA's tile
+constexpr int kBN = 256;             // columns of a tile (128 of g and 128 of u in MM_UP)
+constexpr int kBK = 64;
+constexpr int kStages = 5;
+constexpr int kSA = kBM * kBK * 2;   // this CTA's 128 rows of A, or its half of B
+constexpr int kStageBytes = 2 * kSA;
+constexpr int kEpiWarps = 8;
+constexpr int kProducerWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 32 * 10;
+constexpr int kOutBuf = 32 * 128;    // a warp's 32 rows of 128 bytes
+constexpr int kOutBufs = 2;
+constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kOutBufs * kOutBuf + 8 * (2 * kStages + 5) + 64;
+static_assert(kSmem <= 227 * 1024, "shared memory budget");
+constexpr int kRaster = 8;           // row tiles of a raster group (L2 reuse)
+constexpr int kMaxProbs = 4;
+constexpr int kStatusTimeout = 1 << OLIVE_ERR_TIMEOUT;
+
+enum { MM_UP = 0, MM_DOWN = 1, MM_DH = 2, MM_GRADS = 3 };
+
+// One product out[M, N] = A . B of a launch; maps are indices into MlpMaps.
+struct MlpProb {
+  int16_t a0, a1, b0, b1;  // operands before and from K step ks_half on (MM_UP: b0, b1 by CTA)
+  int16_t out;
+  int16_t a_mn, b_mn;      // MN-major operands
+  int16_t pad;
+  int M, N;
+  int mt, nt;              // pair tiles (256 rows), column tiles
+  int ks_half, ks;         // K steps
+  int tile0;               // its first tile in the launch's list
+};
+
+// The tiles of all products form one list.  The first n_whole of it are dealt
+// to the pairs in turn; the K steps of the others (fewer than there are pairs)
+// are laid end to end and cut into runs of `run` steps, one a pair.
+struct MlpSplit {
+  int n_whole;
+  int steps;               // K steps of the tiles that are cut
+  int run;
+  int first[kMaxProbs];    // the cut tiles of each product, and their offset in steps
+  int off[kMaxProbs];
+};
+
+struct MlpMaps {
+  CUtensorMap m[13];
+};
+
+struct MlpParams {
+  MlpProb pr[kMaxProbs];
+  int n_prob;
+  MlpSplit cut;
+  float* part;             // [pairs][2 CTAs][8 warps][128 columns][32 rows] partial accumulators
+  uint32_t* flag;          // [pairs][2 CTAs] warps that have stored theirs
+  uint32_t* clear;         // words the next launch of the call wants zero
+  int n_clear;
+  const __nv_bfloat16* residual;  // MM_DOWN
+  const uint16_t* saved_g;        // MM_DH: [T, f]
+  const uint16_t* saved_u;
+  int save, act, out_f32;
+  int16_t map_g, map_u;    // MM_UP: saved g, u; MM_DH: dg, du
+  int32_t* dev_status;
+  uint64_t wait_limit_ns;
+};
+
+struct Unit {
+  int prob, m0, n0;        // the pair's first row, first column (MM_UP: of h)
+  int k0, k1;              // K steps
+  int ks;                  // of the whole tile
+  int from;                // first pair that holds a part of the tile (k1 == ks: it is this pair's to finish)
+};
+
+// The units of one pair, in order: its whole tiles, then its run from the end
+// to the beginning.  So a run's piece that another pair finishes comes first,
+// and a pair that waits for pieces waits for runs whose first unit they are:
+// no chain of waits.
+struct UnitWalk {
+  int t, pos, lo, pairs, pair;
+  __device__ UnitWalk(const MlpParams& p, int pair_, int pairs_) {
+    pair = pair_;
+    pairs = pairs_;
+    t = pair;
+    lo = min(pair * p.cut.run, p.cut.steps);
+    pos = min(lo + p.cut.run, p.cut.steps);
+  }
+  __device__ void place(const MlpParams& p, int i, int tile, Unit& u) const {
+    const MlpProb& q = p.pr[i];
+    Raster ra{q.mt, q.nt, kRaster};
+    int mi, nj;
+    ra.tile(tile - q.tile0, mi, nj);
+    u.prob = i;
+    u.m0 = mi * 2 * kBM;
+    u.n0 = nj;
+    u.ks = q.ks;
+  }
+  __device__ bool next(const MlpParams& p, Unit& u) {
+    if (t < p.cut.n_whole) {
+      int i = 0;
+      while (i + 1 < p.n_prob && t >= p.pr[i + 1].tile0) ++i;
+      place(p, i, t, u);
+      u.k0 = 0;
+      u.k1 = u.ks;
+      u.from = pair;
+      t += pairs;
+      return true;
+    }
+    if (pos <= lo) return false;
+    int i = 0;
+    while (i + 1 < p.n_prob && pos - 1 >= p.cut.off[i + 1]) ++i;
+    const int ks = p.pr[i].ks;
+    const int w = (pos - 1 - p.cut.off[i]) / ks;
+    const int start = p.cut.off[i] + w * ks;
+    place(p, i, p.cut.first[i] + w, u);
+    u.k1 = pos - start;
+    u.k0 = max(lo - start, 0);
+    u.from = u.k0 > 0 ? start / p.cut.run : pair;
+    pos = start + u.k0;
+    return true;
+  }
+};
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(src), "r"(x), "r"(y)
+               : "memory");
+}
+// All but this thread's latest bulk group have read their source.
+__device__ __forceinline__ void bulk_wait_read_but_one() {
+  asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+}
+
+template <int kMode>
+__global__ void __launch_bounds__(kThreads, 1)
+    mlp_gemm_kernel(const __grid_constant__ MlpMaps maps, const __grid_constant__ MlpParams p) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  const uint32_t stages = base;
+  const uint32_t out_bufs = base + kStages * kStageBytes;
+  const uint32_t bar0 = out_bufs + kEpiWarps * kOutBufs * kOutBuf;
+  auto full_bar = [&](int st) { return bar0 + 8u * st; };
+  auto empty_bar = [&](int st) { return bar0 + 8u * (kStages + st); };
+  auto tfull = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
+  auto tempty = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
+  const uint32_t drain = bar0 + 8u * (2 * kStages + 4);
+  uint8_t* misc = smem_raw + kStages * kStageBytes + kEpiWarps * kOutBufs * kOutBuf + 8 * (2 * kStages + 5);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
+
+  const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5));
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = warp_uniform(cluster_rank());
+  const int pair = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
+
+  if (threadIdx.x == 0) {
+    for (int st = 0; st < kStages; ++st) {
+      mbar_init(full_bar(st), 1);   // the even CTA's producer (both CTAs' bytes)
+      mbar_init(empty_bar(st), 1);  // the even CTA's MMA commit (multicast)
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(tfull(b), 1);
+      mbar_init(tempty(b), 2 * kEpiWarps);  // the epilogue warps of both CTAs
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc_pair(smem_u32(tmem_slot), 512);
+    tmem_relinquish_pair();
+  }
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < p.n_clear; i += kThreads) p.clear[i] = 0;
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const WaitCtl ctl{abort_flag, p.wait_limit_ns};
+  UnitWalk walk(p, pair, pairs);
+  Unit u;
+
+  if (warp == kProducerWarp) {
+    const bool leader = elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    while (ok && walk.next(p, u)) {
+      const MlpProb& q = p.pr[u.prob];
+      const int mrow = u.m0 + static_cast<int>(rank) * kBM;
+      // MM_UP: the even CTA holds the tile's rows of Wg, the odd one those of Wu
+      const int nrow = kMode == MM_UP ? u.n0 * kBM : u.n0 * kBN + static_cast<int>(rank) * kBM;
+      for (int ks = u.k0; ks < u.k1; ++ks) {
+        if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, ctl)) { ok = false; break; }
+        const uint32_t sA = stages + stage * kStageBytes;
+        const uint32_t fb = map_shared(full_bar(stage), 0);
+        const bool second = kMode != MM_UP && ks >= q.ks_half;
+        const int k = (second ? ks - q.ks_half : ks) * kBK;
+        const CUtensorMap* ma = &maps.m[second ? q.a1 : q.a0];
+        const CUtensorMap* mb = &maps.m[(kMode == MM_UP ? rank != 0 : second) ? q.b1 : q.b0];
+        if (leader) {
+          if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), 2 * kStageBytes);
+          if (kMode == MM_GRADS && q.a_mn) {
+            tma_load_2d_pair(sA, ma, fb, mrow, k);
+            tma_load_2d_pair(sA + kSA / 2, ma, fb, mrow + 64, k);
+          } else {
+            tma_load_2d_pair(sA, ma, fb, k, mrow);
+          }
+          if (kMode == MM_GRADS || kMode == MM_DH) {
+            tma_load_2d_pair(sA + kSA, mb, fb, nrow, k);
+            tma_load_2d_pair(sA + kSA + kSA / 2, mb, fb, nrow + 64, k);
+          } else {
+            tma_load_2d_pair(sA + kSA, mb, fb, k, nrow);
+          }
+        }
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok && lane == 0) {
+      // let copies already issued land before the CTA retires
+      const uint64_t t0 = global_timer_ns();
+      while (global_timer_ns() - t0 < 50000) nanosleep_ns(1000);
+    }
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    if (rank == 0) {
+      const bool leader = elect_one();
+      int stage = 0, n = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      while (ok && walk.next(p, u)) {
+        const MlpProb& q = p.pr[u.prob];
+        const bool a_mn = kMode == MM_GRADS && q.a_mn;
+        constexpr bool b_mn = kMode == MM_GRADS || kMode == MM_DH;
+        const uint32_t id = idesc_bf16(2 * kBM, kBN, a_mn, b_mn);
+        // K-major: 16 K elements are 32 bytes along the swizzled row; MN-major:
+        // 16 rows of 128 bytes, 64-element blocks 8 KB apart
+        const uint64_t dA = sdesc_sw128(stages, a_mn ? kSA / 2 : 16, 1024);
+        const uint64_t dB = sdesc_sw128(stages + kSA, b_mn ? kSA / 2 : 16, 1024);
+        const uint32_t stepA = a_mn ? 128 : 2, stepB = b_mn ? 128 : 2;
+        const int b = n & 1;
+        if (!mbar_wait_warp(tempty(b), ((n >> 1) & 1) ^ 1, ctl)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t acc = warp_uniform(tmem_base) + b * kBN;
+        for (int ks = u.k0; ks < u.k1; ++ks) {
+          if (!mbar_wait_warp(full_bar(stage), phase, ctl)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t so = static_cast<uint32_t>(stage) * (kStageBytes >> 4);
+          if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < kBK / 16; ++kk)
+              umma_bf16_pair(acc, dA + (so + kk * stepA), dB + (so + kk * stepB), id, kk > 0 || ks > u.k0 ? 1u : 0u);
+            umma_commit_pair(empty_bar(stage));
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        if (leader) umma_commit_pair(tfull(b));
+        ++n;
+      }
+      // every MMA issued above has completed before TMEM is freed (a bounded
+      // wait that ignores the abort flag: it is for work already in flight)
+      if (leader) umma_commit_pair(drain);
+      volatile int keep_waiting = 0;
+      const uint64_t floor_ns = 200ull * 1000 * 1000;
+      const WaitCtl own{&keep_waiting, p.wait_limit_ns > floor_ns ? p.wait_limit_ns : floor_ns};
+      mbar_wait_warp(drain, 0, own);
+    }
+    __syncwarp();
+  } else {
+    // epilogue warp w: rows 32 (w % 4).. of the CTA's tile (TMEM lanes, one row
+    // a thread) and half w / 4 of its columns, in four 32-column chunks
+    const int half = warp >> 2;
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t buf0 = out_bufs + warp * kOutBufs * kOutBuf;
+    int sb = 0, n = 0;
+    bool ok = true;
+
+    // 32 rows of 128 bytes through shared memory (128-byte swizzle) to (x, y)
+    auto emit = [&](const CUtensorMap* map, int x, int y, const uint32_t (&w)[32]) {
+      if (lane == 0) bulk_wait_read_but_one();
+      __syncwarp();
+      const uint32_t buf = buf0 + sb * kOutBuf;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        st_shared_v4(buf + lane * 128 + ((c ^ (lane & 7)) << 4),
+                     make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
+      fence_proxy_async_shared();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_2d(map, buf, x, y);
+        bulk_commit();
+      }
+      sb ^= 1;
+    };
+
+    while (ok && walk.next(p, u)) {
+      const MlpProb& q = p.pr[u.prob];
+      const int b = n & 1;
+      if (!mbar_wait_warp(tfull(b), (n >> 1) & 1, ctl)) break;
+      tc_fence_after();
+      ++n;
+      const uint32_t acc = lane_addr + b * kBN;
+      // TMEM column of this warp's 32-column chunk j (MM_UP: chunks 0, 1 of g, 2, 3 of u)
+      auto col_of = [&](int j) {
+        return kMode == MM_UP ? (j >> 1) * 128 + half * 64 + (j & 1) * 32 : half * 128 + j * 32;
+      };
+      auto my_part = [&](int pr) {
+        return p.part + (static_cast<size_t>(pr * 2 + static_cast<int>(rank)) * kEpiWarps + warp) * (128 * 32) + lane;
+      };
+      auto release = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_shared(tempty(b), 0));
+      };
+
+      if (u.k1 < u.ks) {
+        // a piece of a tile that another pair finishes
+        float* to = my_part(pair);
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+          uint32_t r[32];
+          tmem_ld_32x32b_x32(acc + col_of(j), r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) __stcg(to + (j * 32 + i) * 32, __uint_as_float(r[i]));
+        }
+        release();
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) red_release_add(p.flag + pair * 2 + rank, 1u);
+        continue;
+      }
+      if (u.from < pair) {
+        for (int o = u.from; ok && o < pair; ++o) ok = wait_counter(p.flag + o * 2 + rank, kEpiWarps, ctl);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+      }
+      auto load = [&](int j, uint32_t(&r)[32]) {
+        tmem_ld_32x32b_x32(acc + col_of(j), r);
+        tmem_ld_wait();
+        for (int o = u.from; o < pair; ++o) {
+          const float* s = my_part(o) + j * 32 * 32;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __ldcg(s + i * 32));
+        }
+      };
+
+      const int y = u.m0 + static_cast<int>(rank) * kBM + (warp & 3) * 32;  // the warp's first row
+      const int t = y + lane;
+      if constexpr (kMode == MM_UP) {
+        const int x = u.n0 * kBM + half * 64;
+        uint32_t hw[32], gw[32], uw[32];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint32_t g[32], v[32];
+          load(j, g);
+          load(2 + j, v);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float g0 = __uint_as_float(g[i]), g1 = __uint_as_float(g[i + 1]);
+            const float u0 = __uint_as_float(v[i]), u1 = __uint_as_float(v[i + 1]);
+            hw[j * 16 + i / 2] = pack_bf16x2(activate(g0, p.act) * u0, activate(g1, p.act) * u1);
+            if (p.save) {
+              gw[j * 16 + i / 2] = pack_saved(g0, g1);
+              uw[j * 16 + i / 2] = pack_saved(u0, u1);
+            }
+          }
+        }
+        release();
+        if (y < q.M && x < q.N) {
+          emit(&maps.m[q.out], x, y, hw);
+          if (p.save) {
+            emit(&maps.m[p.map_g], x, y, gw);
+            emit(&maps.m[p.map_u], x, y, uw);
+          }
+        }
+      } else if constexpr (kMode == MM_DOWN) {
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          const int x = u.n0 * kBN + half * 128 + c * 64;
+          uint32_t w[32];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t r[32];
+            load(2 * c + j, r);
+            if (p.residual && t < q.M) {
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                const int xv = x + j * 32 + v * 8;
+                if (xv < q.N) {
+                  const uint4 e = *reinterpret_cast<const uint4*>(p.residual + static_cast<size_t>(t) * q.N + xv);
+                  const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    r[v * 8 + 2 * i] = __float_as_uint(__uint_as_float(r[v * 8 + 2 * i]) + __uint_as_float(ew[i] << 16));
+                    r[v * 8 + 2 * i + 1] =
+                        __float_as_uint(__uint_as_float(r[v * 8 + 2 * i + 1]) + __uint_as_float(ew[i] & 0xffff0000u));
+                  }
+                }
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) w[j * 16 + i / 2] = pack_bf16x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+          }
+          if (c == 1) release();
+          if (y < q.M && x < q.N) emit(&maps.m[q.out], x, y, w);
+        }
+      } else if constexpr (kMode == MM_DH) {
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          const int x = u.n0 * kBN + half * 128 + c * 64;
+          uint32_t gw[32], uw[32], hw[32];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint4 sg[4], su[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int xv = x + j * 32 + v * 8;
+              const bool in = t < q.M && xv < q.N;
+              const size_t at = static_cast<size_t>(t) * q.N + xv;
+              sg[v] = in ? *reinterpret_cast<const uint4*>(p.saved_g + at) : make_uint4(0, 0, 0, 0);
+              su[v] = in ? *reinterpret_cast<const uint4*>(p.saved_u + at) : make_uint4(0, 0, 0, 0);
+            }
+            uint32_t r[32];
+            load(2 * c + j, r);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const uint32_t gs[4] = {sg[v].x, sg[v].y, sg[v].z, sg[v].w};
+              const uint32_t us[4] = {su[v].x, su[v].y, su[v].z, su[v].w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float a[2], ds[2], uu[2];
+                const float dh[2] = {__uint_as_float(r[v * 8 + 2 * i]), __uint_as_float(r[v * 8 + 2 * i + 1])};
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  activate_both(unpack_saved(gs[i], e), p.act, a[e], ds[e]);
+                  uu[e] = unpack_saved(us[i], e);
+                }
+                const int o = j * 16 + v * 4 + i;
+                gw[o] = pack_bf16x2(dh[0] * uu[0] * ds[0], dh[1] * uu[1] * ds[1]);
+                uw[o] = pack_bf16x2(dh[0] * a[0], dh[1] * a[1]);
+                hw[o] = pack_bf16x2(a[0] * uu[0], a[1] * uu[1]);
+              }
+            }
+          }
+          if (c == 1) release();
+          if (y < q.M && x < q.N) {
+            emit(&maps.m[p.map_g], x, y, gw);
+            emit(&maps.m[p.map_u], x, y, uw);
+            emit(&maps.m[q.out], x, y, hw);
+          }
+        }
+      } else {
+        if (p.out_f32) {
+#pragma unroll 1
+          for (int j = 0; j < 4; ++j) {
+            const int x = u.n0 * kBN + half * 128 + j * 32;
+            uint32_t r[32];
+            load(j, r);
+            if (j == 3) release();
+            if (y < q.M && x < q.N) emit(&maps.m[q.out], x, y, r);
+          }
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < 2; ++c) {
+            const int x = u.n0 * kBN + half * 128 + c * 64;
+            uint32_t w[32];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              uint32_t r[32];
+              load(2 * c + j, r);
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) w[j * 16 + i / 2] = pack_bf16x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+            }
+            if (c == 1) release();
+            if (y < q.M && x < q.N) emit(&maps.m[q.out], x, y, w);
+          }
+        }
+      }
+    }
+    if (lane == 0) bulk_wait();
+    __syncwarp();
+  }
+
+  tc_fence_before();
+  // the pair's MMAs are complete and every access to the peer's barriers is
+  // over before either CTA frees its TMEM
+  cluster_sync_all();
+  if (threadIdx.x == 0 && *abort_flag && p.dev_status) atomicOr(p.dev_status, kStatusTimeout);
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+// ------------------------------------------------------------------- host ---
+
+// Pairs of CTAs the device holds at once (at most one for two SMs): runs of cut
+// tiles wait for one another, so the grid is never larger.
+template <int kMode>
+int resident_pairs(const Ctx& c) {
+  static std::atomic<int> held[kMaxDevices];
+  const bool cached = c.device >= 0 && c.device < kMaxDevices;
+  int n = cached ? held[c.device].load(std::memory_order_acquire) - 1 : -1;
+  if (n >= 0) return n;
+  static std::atomic<int> done[kMaxDevices];
+  if (!set_smem_once(reinterpret_cast<const void*>(mlp_gemm_kernel<kMode>), kSmem, c.device, done)) return 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (c.num_sms / 2));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, mlp_gemm_kernel<kMode>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  n = std::min({n, c.num_sms / 2, kMlpMaxPairs});
+  if (cached) held[c.device].store(n + 1, std::memory_order_release);
+  return n;
+}
+
+// Deals the tiles: whole ones while every pair gets one, the rest (fewer than
+// there are pairs) cut into equal runs of K steps where that is the shorter way.
+// A cut costs each pair the store of one partial accumulator, and its finisher
+// the wait for the others and their loads: about kCutCost K steps.
+constexpr int kCutCost = 14;
+constexpr int kMinRun = 4;
+// Returns the pairs to launch.
+int plan(MlpParams& p, int pairs) {
+  int tiles = 0;
+  for (int i = 0; i < p.n_prob; ++i) {
+    p.pr[i].tile0 = tiles;
+    tiles += p.pr[i].mt * p.pr[i].nt;
+  }
+  MlpSplit& s = p.cut;
+  s = MlpSplit{};
+  s.n_whole = tiles;
+  s.run = 1;
+  const int first = tiles - tiles % pairs;
+  int steps = 0, longest = 0;
+  for (int i = 0; i < p.n_prob; ++i) {
+    const int end = p.pr[i].tile0 + p.pr[i].mt * p.pr[i].nt;
+    s.first[i] = std::max(first, p.pr[i].tile0);
+    s.off[i] = steps;
+    const int count = std::max(0, end - s.first[i]);
+    if (count > 0) longest = std::max(longest, p.pr[i].ks);
+    steps += count * p.pr[i].ks;
+  }
+  const int run = std::max(kMinRun, static_cast<int>(ceil_div(steps, pairs)));
+  if (steps > 0 && run + kCutCost < longest) {
+    s.n_whole = first;
+    s.steps = steps;
+    s.run = run;
+    return first > 0 ? pairs : static_cast<int>(ceil_div(steps, run));
+  }
+  return std::min(pairs, tiles);
+}
+
+// `zeroed`: an earlier launch of the call clears this one's flags.
+template <int kMode>
+olive_status launch(const Ctx& c, const MlpMaps& maps, MlpParams& p, bool zeroed) {
+  int pairs = resident_pairs<kMode>(c);
+  if (pairs < 1) return OLIVE_ERR_UNSUPPORTED_DEVICE;
+  pairs = plan(p, pairs);
+  if (p.cut.steps > 0 && !zeroed &&
+      cudaMemsetAsync(p.flag, 0, 4 * mlp_flag_words(), c.stream) != cudaSuccess) {
+    cudaGetLastError();
+    return OLIVE_ERR_CUDA;
+  }
+  p.wait_limit_ns = c.wait_limit_ns;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * pairs);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, mlp_gemm_kernel<kMode>, maps, p) != cudaSuccess) {
+    cudaGetLastError();
+    return OLIVE_ERR_CUDA;
+  }
+  return OLIVE_OK;
+}
+
+// Collects a launch's tensor maps.
+struct MapSet {
+  MlpMaps maps;
+  int n = 0;
+  bool ok = true;
+  int16_t add(bool good) {
+    ok = ok && good;
+    return static_cast<int16_t>(n++);
+  }
+  // operand [rows, cols] bf16 with K along the columns: boxes of 128 rows x 64
+  int16_t k_major(const void* a, int64_t rows, int64_t cols) {
+    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, kBK, kBM));
+  }
+  // operand [rows, cols] bf16 with K along the rows: boxes of 64 rows x 64
+  int16_t mn_major(const void* a, int64_t rows, int64_t cols) {
+    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, 64, kBK));
+  }
+  // output [rows, cols]: boxes of 32 rows x 128 bytes
+  int16_t output(void* a, int64_t rows, int64_t cols, bool f32) {
+    return add(f32 ? encode_f32_2d(&maps.m[n], a, cols, rows, 4 * cols, 32, 32)
+                   : encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, 64, 32));
+  }
+};
+
+MlpProb problem(int M, int N, int n_tile, int K, int halves) {
+  MlpProb q = {};
+  q.M = M;
+  q.N = N;
+  q.mt = static_cast<int>(ceil_div(M, 2 * kBM));
+  q.nt = static_cast<int>(ceil_div(N, n_tile));
+  q.ks_half = static_cast<int>(ceil_div(K, kBK));
+  q.ks = halves * q.ks_half;
+  return q;
+}
+
+}  // namespace
+
+size_t mlp_part_bytes() { return 4ull * kMlpMaxPairs * 2 * kEpiWarps * 128 * 32; }
+size_t mlp_flag_words() { return 2ull * kMlpMaxPairs; }
+
+olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, const void* W_up,
+                            const void* W_down, const void* residual, int32_t T, int32_t d,
+                            int32_t f, int act, void* y, void* saved, void* ws,
+                            int32_t* dev_status) {
+  const MlpWs w = carve_mlp(ws, T, f, false);
+  uint16_t* sg = static_cast<uint16_t*>(saved);
+  uint16_t* su = saved ? sg + static_cast<size_t>(T) * f : nullptr;
+  {
+    MapSet s;
+    MlpParams p = {};
+    MlpProb q = problem(T, f, kBM, d, 1);
+    q.a0 = q.a1 = s.k_major(x, T, d);
+    q.b0 = s.k_major(W_gate, f, d);
+    q.b1 = s.k_major(W_up, f, d);
+    q.out = s.output(w.h, T, f, false);
+    if (saved) {
+      p.map_g = s.output(sg, T, f, false);
+      p.map_u = s.output(su, T, f, false);
+    }
+    if (!s.ok) return OLIVE_ERR_CUDA;
+    p.pr[0] = q;
+    p.n_prob = 1;
+    p.save = saved != nullptr;
+    p.act = act;
+    p.part = w.part;
+    p.flag = w.flag;
+    p.clear = w.flag + mlp_flag_words();
+    p.n_clear = static_cast<int>(mlp_flag_words());
+    p.dev_status = dev_status;
+    const olive_status st = launch<MM_UP>(c, s.maps, p, false);
+    if (st != OLIVE_OK) return st;
+  }
+  MapSet s;
+  MlpParams p = {};
+  MlpProb q = problem(T, d, kBN, f, 1);
+  q.a0 = q.a1 = s.k_major(w.h, T, f);
+  q.b0 = q.b1 = s.k_major(W_down, d, f);
+  q.out = s.output(y, T, d, false);
+  if (!s.ok) return OLIVE_ERR_CUDA;
+  p.pr[0] = q;
+  p.n_prob = 1;
+  p.residual = static_cast<const __nv_bfloat16*>(residual);
+  p.part = w.part;
+  p.flag = w.flag + mlp_flag_words();
+  p.dev_status = dev_status;
+  return launch<MM_DOWN>(c, s.maps, p, true);
+}
+
+olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const void* W_gate,
+                            const void* W_up, const void* W_down, const void* saved, int32_t T,
+                            int32_t d, int32_t f, int act, void* dx, void* dW_gate, void* dW_up,
+                            void* dW_down, int grad_dtype, void* ws, int32_t* dev_status) {
+  const MlpWs w = carve_mlp(ws, T, f, true);
+  const bool f32 = grad_dtype == OLIVE_DTYPE_F32;
+  {
+    MapSet s;
+    MlpParams p = {};
+    MlpProb q = problem(T, f, kBN, d, 1);
+    q.a0 = q.a1 = s.k_major(dy, T, d);
+    q.b0 = q.b1 = s.mn_major(W_down, d, f);
+    q.out = s.output(w.h, T, f, false);
+    p.map_g = s.output(w.dg, T, f, false);
+    p.map_u = s.output(w.du, T, f, false);
+    if (!s.ok) return OLIVE_ERR_CUDA;
+    p.pr[0] = q;
+    p.n_prob = 1;
+    p.act = act;
+    p.saved_g = static_cast<const uint16_t*>(saved);
+    p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
+    p.part = w.part;
+    p.flag = w.flag;
+    p.clear = w.flag + mlp_flag_words();
+    p.n_clear = static_cast<int>(mlp_flag_words());
+    p.dev_status = dev_status;
+    const olive_status st = launch<MM_DH>(c, s.maps, p, false);
+    if (st != OLIVE_OK) return st;
+  }
+  MapSet s;
+  MlpParams p = {};
+  if (dx) {
+    MlpProb q = problem(T, d, kBN, f, 2);
+    q.a0 = s.k_major(w.dg, T, f);
+    q.a1 = s.k_major(w.du, T, f);
+    q.b0 = s.mn_major(W_gate, f, d);
+    q.b1 = s.mn_major(W_up, f, d);
+    q.out = s.output(dx, T, d, f32);
+    p.pr[p.n_prob++] = q;
+  }
+  if (dW_gate) {
+    const int16_t xm = s.mn_major(x, T, d);
+    for (int i = 0; i < 2; ++i) {
+      MlpProb q = problem(f, d, kBN, T, 1);
+      q.a0 = q.a1 = s.mn_major(i ? w.du : w.dg, T, f);
+      q.b0 = q.b1 = xm;
+      q.a_mn = 1;
+      q.out = s.output(i ? dW_up : dW_gate, f, d, f32);
+      p.pr[p.n_prob++] = q;
+    }
+    MlpProb q = problem(d, f, kBN, T, 1);
+    q.a0 = q.a1 = s.mn_major(dy, T, d);
+    q.b0 = q.b1 = s.mn_major(w.h, T, f);
+    q.a_mn = 1;
+    q.out = s.output(dW_down, d, f, f32);
+    p.pr[p.n_prob++] = q;
+  }
+  if (!s.ok) return OLIVE_ERR_CUDA;
+  p.out_f32 = f32;
+  p.part = w.part;
+  p.flag = w.flag + mlp_flag_words();
+  p.dev_status = dev_status;
+  return launch<MM_GRADS>(c, s.maps, p, true);
+}
+
+}  // namespace olive

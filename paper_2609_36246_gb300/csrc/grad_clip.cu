@@ -1,0 +1,269 @@
+// grad_clip.cu -- the 2-norm over all elements of a list of gradients, and the
+// gradients scaled so that it is at most a limit (olive_grad_clip).
+//
+// The tensors are cut into units of 16 KB, numbered through; block b takes units
+// b, b + blocks, ...  A thread squares 64 bytes of a unit at a time (32 bf16 or 16
+// fp32 values) into one fp32 sum and adds that to an fp64 sum.  Where that fp32
+// sum is not finite, large or nearly zero the same values, still in registers,
+// are squared again in fp64: squares leave fp32's range long before the values
+// do.  Every block's total goes to the workspace.
+//
+// The second launch adds the blocks' totals (each block by itself: a few KB from
+// L2), and scales, from the last unit to the first: what the first launch read
+// last is still in the L2.
+//
+// What bounds it: HBM, each gradient read twice and written once (read once where
+// all of them fit the L2).
+#include <algorithm>
+#include <cmath>
+
+#include "internal.h"
+
+#include <cuda_bf16.h>
+
+namespace olive {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kVecs = 4;                               // 16-byte vectors of a thread's part of a unit
+constexpr int kUnitBytes = kThreads * kVecs * 16;
+constexpr int kBlocksPerSm = 6;
+constexpr int kMaxBlocks = 192 * kBlocksPerSm;
+constexpr int kMaxList = 512;                          // tensors of a launch
+
+struct Entry {
+  const void* src;
+  void* dst;
+  long long n;
+  uint32_t unit0;  // its first unit
+  uint32_t f32;
+};
+template <int N>
+struct List {
+  int count;
+  uint32_t units;
+  Entry e[N];
+};
+
+__device__ __forceinline__ bool aligned16_dev(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Values of a 16-byte vector.
+__device__ __forceinline__ void widen(const uint4& v, bool f32, float (&x)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (f32) {
+      x[i] = __uint_as_float(w[i]);
+      x[4 + i] = 0.f;
+    } else {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+
+// Sum of squares of a thread's vectors.
+__device__ __forceinline__ double squares(const uint4 (&v)[kVecs], bool f32) {
+  float q = 0.f;
+  uint32_t any = 0;
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    float x[8];
+    widen(v[k], f32, x);
+    any |= v[k].x | v[k].y | v[k].z | v[k].w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q = fmaf(x[i], x[i], q);
+  }
+  if (q < 1e36f && q > 1e-28f) return q;
+  if ((any & 0x7fff7fffu) == 0) return 0.0;
+  double d = 0.0;
+#pragma unroll 1
+  for (int k = 0; k < kVecs; ++k) {
+    float x[8];
+    widen(v[k], f32, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), d);
+  }
+  return d;
+}
+
+__device__ __forceinline__ float value_at(const void* p, bool f32, long long i) {
+  return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+__device__ __forceinline__ void store_at(void* p, bool f32, long long i, float v) {
+  if (f32)
+    static_cast<float*>(p)[i] = v;
+  else
+    static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// Sum over the block, in a fixed order, in every thread.
+__device__ double block_sum(double v, double* sums) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = v;
+  __syncthreads();
+  v = 0.0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) v += sums[i];
+  return v;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+    grad_norm_kernel(const __grid_constant__ List<N> list, double* part) {
+  __shared__ double sums[kThreads / 32];
+  double acc = 0.0;
+  int e = 0;
+  for (uint32_t u = blockIdx.x; u < list.units; u += gridDim.x) {
+    while (e + 1 < list.count && u >= list.e[e + 1].unit0) ++e;
+    const Entry& t = list.e[e];
+    const bool f32 = t.f32 != 0;
+    const int per = f32 ? 4 : 8;  // values of a vector
+    const long long first = static_cast<long long>(u - t.unit0) * (kThreads * kVecs * per);
+    const long long left = t.n - first;
+    if (aligned16_dev(t.src)) {
+      const uint4* v = reinterpret_cast<const uint4*>(static_cast<const char*>(t.src) + first * (f32 ? 4 : 2));
+      uint4 x[kVecs];
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int at = k * kThreads + threadIdx.x;
+        x[k] = static_cast<long long>(at + 1) * per <= left ? __ldg(v + at) : make_uint4(0, 0, 0, 0);
+      }
+      acc += squares(x, f32);
+      if (left < kThreads * kVecs * per) {  // values behind the last whole vector
+        const int tail = static_cast<int>(left % per);
+        if (static_cast<int>(threadIdx.x) < tail) {
+          const double y = value_at(t.src, f32, t.n - tail + threadIdx.x);
+          acc = fma(y, y, acc);
+        }
+      }
+    } else {
+      const int n = static_cast<int>(min(left, static_cast<long long>(kThreads * kVecs * per)));
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const double y = value_at(t.src, f32, first + i);
+        acc = fma(y, y, acc);
+      }
+    }
+  }
+  const double s = block_sum(acc, sums);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+    grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int parts, float max_norm,
+                      float* norm) {
+  __shared__ double sums[kThreads / 32];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
+  s = sqrt(block_sum(s, sums));
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(s);
+  const double ratio = static_cast<double>(max_norm) / (s + 1e-6);
+  const float f = ratio >= 1.0 ? 1.f : static_cast<float>(ratio);  // (NaN stays NaN)
+
+  int e = list.count - 1;
+  for (long long w = static_cast<long long>(list.units) - 1 - blockIdx.x; w >= 0; w -= gridDim.x) {
+    const uint32_t u = static_cast<uint32_t>(w);
+    while (u < list.e[e].unit0) --e;
+    const Entry& t = list.e[e];
+    if (f == 1.f && t.src == t.dst) continue;
+    const bool f32 = t.f32 != 0;
+    const int per = f32 ? 4 : 8;
+    const long long first = static_cast<long long>(u - t.unit0) * (kThreads * kVecs * per);
+    const long long left = t.n - first;
+    if (aligned16_dev(t.src) && aligned16_dev(t.dst)) {
+      const long long at0 = first * (f32 ? 4 : 2);
+      const uint4* v = reinterpret_cast<const uint4*>(static_cast<const char*>(t.src) + at0);
+      uint4* o = reinterpret_cast<uint4*>(static_cast<char*>(t.dst) + at0);
+      uint4 x[kVecs];
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int at = k * kThreads + threadIdx.x;
+        if (static_cast<long long>(at + 1) * per <= left) x[k] = v[at];
+      }
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int at = k * kThreads + threadIdx.x;
+        if (static_cast<long long>(at + 1) * per > left) continue;
+        uint32_t* q = reinterpret_cast<uint32_t*>(&x[k]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (f32) {
+            q[i] = __float_as_uint(__uint_as_float(q[i]) * f);
+          } else {
+            const __nv_bfloat162 h =
+                __floats2bfloat162_rn(__uint_as_float(q[i] << 16) * f, __uint_as_float(q[i] & 0xffff0000u) * f);
+            q[i] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+        }
+        o[at] = x[k];
+      }
+      if (left < kThreads * kVecs * per) {
+        const int tail = static_cast<int>(left % per);
+        if (static_cast<int>(threadIdx.x) < tail) {
+          const long long i = t.n - tail + threadIdx.x;
+          store_at(t.dst, f32, i, value_at(t.src, f32, i) * f);
+        }
+      }
+    } else {
+      const int n = static_cast<int>(min(left, static_cast<long long>(kThreads * kVecs * per)));
+      for (int i = threadIdx.x; i < n; i += kThreads)
+        store_at(t.dst, f32, first + i, value_at(t.src, f32, first + i) * f);
+    }
+  }
+}
+
+// Tensors [i0, i1) of the caller's list.
+template <int N>
+List<N> make_list(const void* const* src, void* const* dst, const int64_t* numel, const int32_t* dtype, int i0,
+                  int i1) {
+  List<N> l;
+  l.count = 0;
+  l.units = 0;
+  for (int i = i0; i < i1; ++i) {
+    if (numel[i] == 0) continue;
+    Entry& e = l.e[l.count++];
+    e.src = src[i];
+    e.dst = dst ? dst[i] : nullptr;
+    e.n = numel[i];
+    e.unit0 = l.units;
+    e.f32 = dtype[i] == OLIVE_DTYPE_F32;
+    l.units += static_cast<uint32_t>(ceil_div(numel[i] * (e.f32 ? 4 : 2), kUnitBytes));
+  }
+  return l;
+}
+
+template <int N>
+olive_status run(const Ctx& c, const void* const* src, void* const* dst, const int64_t* numel, const int32_t* dtype,
+                 int32_t n, float max_norm, float* norm, double* part) {
+  const int most = std::min(c.num_sms * kBlocksPerSm, kMaxBlocks);
+  int parts = 0;
+  for (int i = 0; i < n; i += N) {
+    const List<N> l = make_list<N>(src, dst, numel, dtype, i, std::min(n, i + N));
+    const int blocks = static_cast<int>(std::min<int64_t>(l.units, most));
+    if (blocks > 0) grad_norm_kernel<N><<<blocks, kThreads, 0, c.stream>>>(l, part + parts);
+    parts += blocks;
+  }
+  for (int i = 0; i < std::max(n, 1); i += N) {
+    List<N> l = make_list<N>(src, dst, numel, dtype, i, dst ? std::min(n, i + N) : i);
+    const int blocks = static_cast<int>(std::min<int64_t>(l.units, most));
+    grad_scale_kernel<N><<<std::max(blocks, 1), kThreads, 0, c.stream>>>(l, part, parts, max_norm, norm);
+    if (!dst) break;
+  }
+  return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t grad_clip_ws_bytes(int64_t n) { return align_up(8ull * kMaxBlocks * ceil_div(n, kMaxList), kWsAlign); }
+
+olive_status launch_grad_clip(const Ctx& c, const void* const* src, void* const* dst, const int64_t* numel,
+                              const int32_t* dtype, int32_t n, float max_norm, float* norm, void* ws) {
+  double* part = static_cast<double*>(ws);
+  // (the list travels in the launch's parameters: the short one costs less to launch)
+  return n <= 48 ? run<48>(c, src, dst, numel, dtype, n, max_norm, norm, part)
+                 : run<kMaxList>(c, src, dst, numel, dtype, n, max_norm, norm, part);
+}
+
+}  // namespace olive

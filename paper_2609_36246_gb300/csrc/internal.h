@@ -55,6 +55,10 @@ bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t
 bool encode_bf16_2d_plain(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                           uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer);
 
+// The same for fp32 with 128-byte swizzle.
+bool encode_f32_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
+                   uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer);
+
 // Rows of the G slab used by the backward passes for vocabulary size V.
 int64_t slab_rows(int64_t Tpad, int64_t V);
 inline int64_t vpad(int64_t V) { return align_up(static_cast<size_t>(V), 8); }
@@ -356,5 +360,59 @@ olive_status launch_topk_kl_fwd_bwd(const Ctx& c, const void* h_s, const void* W
                                     int32_t* s_ids, float* s_logp, float* t_logp_s,
                                     float* kl_topk, float* overlap, void* d_h_s, void* d_W_s,
                                     int grad_dtype, void* ws, int32_t* dev_status);
+
+// ---- gated feed-forward block (gated_mlp.cu) ----
+constexpr int kMlpMaxPairs = 96;  // CTA pairs the partials and flags are sized for
+struct MlpWs {
+  void* h;         // bf16 [T, f]
+  void* dg;        // bf16 [T, f] (backward)
+  void* du;        // bf16 [T, f] (backward)
+  float* part;     // mlp_part_bytes(): partial accumulators of cut tiles
+  uint32_t* flag;  // 2 x mlp_flag_words(): pieces stored, for each launch of a call
+};
+size_t mlp_part_bytes();
+size_t mlp_flag_words();
+size_t mlp_ws_bytes(int64_t T, int64_t f, bool bwd);
+MlpWs carve_mlp(void* ws, int64_t T, int64_t f, bool bwd);
+olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, const void* W_up,
+                            const void* W_down, const void* residual, int32_t T, int32_t d,
+                            int32_t f, int act, void* y, void* saved, void* ws,
+                            int32_t* dev_status);
+olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const void* W_gate,
+                            const void* W_up, const void* W_down, const void* saved, int32_t T,
+                            int32_t d, int32_t f, int act, void* dx, void* dW_gate, void* dW_up,
+                            void* dW_down, int grad_dtype, void* ws, int32_t* dev_status);
+
+// ---- heads' norm and rotation (qk_norm_rope.cu) ----
+struct HeadsView {
+  const void* x;
+  int64_t token_stride, head_stride;  // elements
+};
+struct QkArgs {
+  HeadsView in[2];    // q, k
+  HeadsView grad[2];  // gradients of the outputs (backward)
+  HeadsView out[2];   // outputs, or gradients of the inputs (written)
+  int32_t heads[2];
+  const void* w[2];
+  float eps;
+  const float *cos, *sin;
+  const int32_t* positions;
+  int32_t P, T, D, R;
+  int interleaved, dtype;
+  float* dw[2];
+  void* ws;
+  int32_t* dev_status;
+};
+size_t qk_bwd_ws_bytes(int64_t D);
+olive_status launch_qk_fwd(const Ctx& c, const QkArgs& a);
+olive_status launch_qk_bwd(const Ctx& c, const QkArgs& a);
+olive_status launch_packed_positions(const Ctx& c, const int32_t* cu_seqlens, int32_t S,
+                                     int32_t T_cap, int32_t* positions);
+
+// ---- global gradient norm and clipping (grad_clip.cu) ----
+size_t grad_clip_ws_bytes(int64_t n);
+olive_status launch_grad_clip(const Ctx& c, const void* const* src, void* const* dst,
+                              const int64_t* numel, const int32_t* dtype, int32_t n, float max_norm,
+                              float* norm, void* ws);
 
 }  // namespace olive

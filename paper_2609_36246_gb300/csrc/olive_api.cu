@@ -82,16 +82,16 @@ bool set_smem_once(const void* func, int smem, int device, std::atomic<int>* don
   return true;
 }
 
-static bool encode_bf16_2d_swz(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
-                               uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer,
-                               CUtensorMapSwizzle swz) {
+static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t inner,
+                      uint64_t outer, uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer,
+                      CUtensorMapSwizzle swz) {
   auto fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[2] = {inner, outer};
   cuuint64_t strides[1] = {row_bytes};
   cuuint32_t box[2] = {box_inner, box_outer};
   cuuint32_t estr[2] = {1, 1};
-  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+  const CUresult r = fn(map, type, 2, const_cast<void*>(base), dims,
                         strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
@@ -99,14 +99,20 @@ static bool encode_bf16_2d_swz(CUtensorMap* map, const void* base, uint64_t inne
 
 bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                     uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer) {
-  return encode_bf16_2d_swz(map, base, inner, outer, row_bytes, box_inner, box_outer,
-                            CU_TENSOR_MAP_SWIZZLE_128B);
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, row_bytes, box_inner,
+                   box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+bool encode_f32_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
+                   uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer) {
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, base, inner, outer, row_bytes, box_inner,
+                   box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 bool encode_bf16_2d_plain(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                           uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer) {
-  return encode_bf16_2d_swz(map, base, inner, outer, row_bytes, box_inner, box_outer,
-                            CU_TENSOR_MAP_SWIZZLE_NONE);
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, row_bytes, box_inner,
+                   box_outer, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 int64_t slab_rows(int64_t Tpad, int64_t V) {
@@ -340,6 +346,28 @@ KlWs carve_kl(void* ws, int64_t T, int64_t ds, int64_t dt, int64_t V, int grad) 
   return carve_kl_impl(ws, T, ds, dt, V, grad, nullptr);
 }
 
+static MlpWs carve_mlp_impl(void* ws, int64_t T, int64_t f, bool bwd, size_t* total) {
+  Carver c{static_cast<char*>(ws)};
+  MlpWs w = {};
+  w.h = c.take(2ull * T * f);
+  if (bwd) {
+    w.dg = c.take(2ull * T * f);
+    w.du = c.take(2ull * T * f);
+  }
+  w.part = static_cast<float*>(c.take(mlp_part_bytes()));
+  w.flag = static_cast<uint32_t*>(c.take(2 * 4 * mlp_flag_words()));
+  if (total) *total = c.off;
+  return w;
+}
+size_t mlp_ws_bytes(int64_t T, int64_t f, bool bwd) {
+  size_t n = 0;
+  carve_mlp_impl(nullptr, T, f, bwd, &n);
+  return n;
+}
+MlpWs carve_mlp(void* ws, int64_t T, int64_t f, bool bwd) {
+  return carve_mlp_impl(ws, T, f, bwd, nullptr);
+}
+
 }  // namespace olive
 
 using namespace olive;
@@ -354,6 +382,8 @@ olive_status check_ws(void* ws, size_t have, size_t need) {
     return OLIVE_ERR_WORKSPACE;
   return OLIVE_OK;
 }
+
+constexpr int32_t kMaxHeadDim = 256;
 
 bool width_ok(int32_t d) { return d >= 8 && d <= kMaxDim && (d % 8) == 0; }
 
@@ -395,8 +425,14 @@ olive_status olive_status_clear(int32_t* dev_status, void* stream) {
 size_t olive_workspace_size(int op, int32_t T, int32_t d, int32_t d_t, int32_t V, int grad,
                             int grad_dtype) {
   if (op == OLIVE_OP_SPLICE_MASKED) return T < 1 ? 0 : splice_masked_ws_bytes(T);
+  if (op == OLIVE_OP_QK_NORM_ROPE_BWD) return width_ok(d) && d <= kMaxHeadDim ? qk_bwd_ws_bytes(d) : 0;
+  if (op == OLIVE_OP_GRAD_CLIP) return T < 1 ? 0 : grad_clip_ws_bytes(T);
   if (T < 1 || V < 1 || !width_ok(d)) return 0;
   switch (op) {
+    case OLIVE_OP_GATED_MLP_FWD:
+    case OLIVE_OP_GATED_MLP_BWD:
+      if (!width_ok(V)) return 0;
+      return mlp_ws_bytes(T, V, op == OLIVE_OP_GATED_MLP_BWD);
     case OLIVE_OP_LOGPROB_FWD: return fwd_ws_bytes(T, d);
     case OLIVE_OP_LOSS_BWD:
       if (grad_dtype != OLIVE_DTYPE_BF16 && grad_dtype != OLIVE_DTYPE_F32) return 0;
@@ -722,6 +758,208 @@ olive_status olive_token_divergence(const void* h_s, const void* W_s, int32_t d_
   if (st != OLIVE_OK) return st;
   return launch_divergence(c, h_s, W_s, d_s, h_t, W_t, d_t, rows, n_rows, T, V, inv_tau, direction,
                            kl, grad_kl, d_h_s, grad_dtype, workspace, dev_status);
+}
+
+olive_status olive_packed_positions(const int32_t* cu_seqlens, int32_t S, int32_t T_cap,
+                                    int32_t* positions, void* stream) {
+  if (!cu_seqlens || !positions) return OLIVE_ERR_INVALID_ARG;
+  if (S < 1 || T_cap < 1) return OLIVE_ERR_SHAPE;
+  Ctx c;
+  olive_status st = make_ctx(stream, &c);
+  if (st != OLIVE_OK) return st;
+  return launch_packed_positions(c, cu_seqlens, S, T_cap, positions);
+}
+
+// The checks that the heads' forward and backward share.
+static olive_status check_qk(const QkArgs& a, bool bwd) {
+  if (a.dtype != OLIVE_DTYPE_BF16 && a.dtype != OLIVE_DTYPE_F32) return OLIVE_ERR_INVALID_ARG;
+  if (a.interleaved != 0 && a.interleaved != 1) return OLIVE_ERR_INVALID_ARG;
+  if (!(a.eps >= 0.f) || !std::isfinite(a.eps)) return OLIVE_ERR_INVALID_ARG;
+  if (a.T < 0 || a.D < 8 || a.D > kMaxHeadDim || a.R < 0 || a.R > a.D || a.P < 1 || a.heads[0] < 0 ||
+      a.heads[1] < 0 || a.heads[0] > kMaxDim || a.heads[1] > kMaxDim || a.heads[0] + a.heads[1] < 1)
+    return OLIVE_ERR_SHAPE;
+  if (a.D % 8 != 0 || a.R % 8 != 0) return OLIVE_ERR_ALIGNMENT;
+  if (a.T > 0 && (!a.positions || (a.R > 0 && (!a.cos || !a.sin)))) return OLIVE_ERR_INVALID_ARG;
+  if (!aligned16(a.cos) || !aligned16(a.sin)) return OLIVE_ERR_ALIGNMENT;
+  for (int s = 0; s < 2; ++s) {
+    if (a.heads[s] == 0 || a.T == 0) continue;
+    if (!a.w[s] || !a.in[s].x || !a.out[s].x || (bwd && !a.grad[s].x)) return OLIVE_ERR_INVALID_ARG;
+    if (!aligned16(a.w[s])) return OLIVE_ERR_ALIGNMENT;
+    for (const HeadsView* v : {&a.in[s], &a.out[s], &a.grad[s]}) {
+      if (v == &a.grad[s] && !bwd) continue;
+      if (!aligned16(v->x) || v->token_stride % 8 != 0 || v->head_stride % 8 != 0)
+        return OLIVE_ERR_ALIGNMENT;
+      if (v->token_stride < 0 || v->head_stride < 0) return OLIVE_ERR_SHAPE;
+    }
+  }
+  return OLIVE_OK;
+}
+
+olive_status olive_qk_norm_rope_fwd(
+    const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k,
+    int64_t k_token_stride, int64_t k_head_stride, int32_t Hq, int32_t Hk, const void* w_q,
+    const void* w_k, float eps, const float* cos_table, const float* sin_table,
+    const int32_t* positions, int32_t P, int32_t T, int32_t D, int32_t R, int interleaved,
+    void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
+    int64_t k_out_token_stride, int64_t k_out_head_stride, int dtype, int32_t* dev_status,
+    void* stream) {
+  QkArgs a = {};
+  a.in[0] = {q, q_token_stride, q_head_stride};
+  a.in[1] = {k, k_token_stride, k_head_stride};
+  a.out[0] = {q_out, q_out_token_stride, q_out_head_stride};
+  a.out[1] = {k_out, k_out_token_stride, k_out_head_stride};
+  a.heads[0] = Hq;
+  a.heads[1] = Hk;
+  a.w[0] = w_q;
+  a.w[1] = w_k;
+  a.eps = eps;
+  a.cos = cos_table;
+  a.sin = sin_table;
+  a.positions = positions;
+  a.P = P;
+  a.T = T;
+  a.D = D;
+  a.R = R;
+  a.interleaved = interleaved;
+  a.dtype = dtype;
+  a.dev_status = dev_status;
+  olive_status st = check_qk(a, false);
+  if (st != OLIVE_OK) return st;
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK) return st;
+  return T == 0 ? OLIVE_OK : launch_qk_fwd(c, a);
+}
+
+olive_status olive_qk_norm_rope_bwd(
+    const void* g_q, int64_t g_q_token_stride, int64_t g_q_head_stride, const void* g_k,
+    int64_t g_k_token_stride, int64_t g_k_head_stride, const void* q, int64_t q_token_stride,
+    int64_t q_head_stride, const void* k, int64_t k_token_stride, int64_t k_head_stride,
+    int32_t Hq, int32_t Hk, const void* w_q, const void* w_k, float eps, const float* cos_table,
+    const float* sin_table, const int32_t* positions, int32_t P, int32_t T, int32_t D, int32_t R,
+    int interleaved, void* d_q, int64_t d_q_token_stride, int64_t d_q_head_stride, void* d_k,
+    int64_t d_k_token_stride, int64_t d_k_head_stride, float* dw_q, float* dw_k, int dtype,
+    void* workspace, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  QkArgs a = {};
+  a.grad[0] = {g_q, g_q_token_stride, g_q_head_stride};
+  a.grad[1] = {g_k, g_k_token_stride, g_k_head_stride};
+  a.in[0] = {q, q_token_stride, q_head_stride};
+  a.in[1] = {k, k_token_stride, k_head_stride};
+  a.out[0] = {d_q, d_q_token_stride, d_q_head_stride};
+  a.out[1] = {d_k, d_k_token_stride, d_k_head_stride};
+  a.heads[0] = Hq;
+  a.heads[1] = Hk;
+  a.w[0] = w_q;
+  a.w[1] = w_k;
+  a.eps = eps;
+  a.cos = cos_table;
+  a.sin = sin_table;
+  a.positions = positions;
+  a.P = P;
+  a.T = T;
+  a.D = D;
+  a.R = R;
+  a.interleaved = interleaved;
+  a.dtype = dtype;
+  a.dw[0] = dw_q;
+  a.dw[1] = dw_k;
+  a.ws = workspace;
+  a.dev_status = dev_status;
+  olive_status st = check_qk(a, true);
+  if (st != OLIVE_OK) return st;
+  if (!dw_q || !dw_k) return OLIVE_ERR_INVALID_ARG;
+  st = check_ws(workspace, ws_bytes, qk_bwd_ws_bytes(D));
+  if (st != OLIVE_OK) return st;
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK) return st;
+  return launch_qk_bwd(c, a);
+}
+
+olive_status olive_gated_mlp_fwd(const void* x, const void* W_gate, const void* W_up,
+                                 const void* W_down, const void* residual, int32_t T, int32_t d,
+                                 int32_t f, int activation, void* y, void* saved, void* workspace,
+                                 size_t ws_bytes, int32_t* dev_status, void* stream) {
+  if (!W_gate || !W_up || !W_down) return OLIVE_ERR_INVALID_ARG;
+  if (activation != OLIVE_ACT_SILU && activation != OLIVE_ACT_GELU_TANH) return OLIVE_ERR_INVALID_ARG;
+  if (T < 0 || d < 1 || d > kMaxDim || f < 1 || f > kMaxDim) return OLIVE_ERR_SHAPE;
+  if (d % 8 != 0 || f % 8 != 0 || !aligned16(W_gate) || !aligned16(W_up) || !aligned16(W_down))
+    return OLIVE_ERR_ALIGNMENT;
+  olive_status st = OLIVE_OK;
+  if (T > 0) {
+    if (!x || !y) return OLIVE_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(y) || !aligned16(residual) || !aligned16(saved))
+      return OLIVE_ERR_ALIGNMENT;
+    st = check_ws(workspace, ws_bytes, mlp_ws_bytes(T, f, false));
+    if (st != OLIVE_OK) return st;
+  }
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK || T == 0) return st;
+  return launch_mlp_fwd(c, x, W_gate, W_up, W_down, residual, T, d, f, activation, y, saved,
+                        workspace, dev_status);
+}
+
+olive_status olive_gated_mlp_bwd(const void* dy, const void* x, const void* W_gate,
+                                 const void* W_up, const void* W_down, const void* saved, int32_t T,
+                                 int32_t d, int32_t f, int activation, void* dx, void* dW_gate,
+                                 void* dW_up, void* dW_down, int grad_dtype, void* workspace,
+                                 size_t ws_bytes, int32_t* dev_status, void* stream) {
+  if (!W_gate || !W_up || !W_down) return OLIVE_ERR_INVALID_ARG;
+  if (activation != OLIVE_ACT_SILU && activation != OLIVE_ACT_GELU_TANH) return OLIVE_ERR_INVALID_ARG;
+  if (grad_dtype != OLIVE_DTYPE_BF16 && grad_dtype != OLIVE_DTYPE_F32) return OLIVE_ERR_INVALID_ARG;
+  if ((dW_gate == nullptr) != (dW_up == nullptr) || (dW_gate == nullptr) != (dW_down == nullptr) ||
+      (!dx && !dW_gate && T > 0))
+    return OLIVE_ERR_INVALID_ARG;
+  if (T < 0 || d < 1 || d > kMaxDim || f < 1 || f > kMaxDim) return OLIVE_ERR_SHAPE;
+  if (d % 8 != 0 || f % 8 != 0 || !aligned16(W_gate) || !aligned16(W_up) || !aligned16(W_down) ||
+      !aligned16(dW_gate) || !aligned16(dW_up) || !aligned16(dW_down))
+    return OLIVE_ERR_ALIGNMENT;
+  olive_status st = OLIVE_OK;
+  if (T > 0) {
+    if (!dy || !x || !saved) return OLIVE_ERR_INVALID_ARG;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(saved) || !aligned16(dx)) return OLIVE_ERR_ALIGNMENT;
+    st = check_ws(workspace, ws_bytes, mlp_ws_bytes(T, f, true));
+    if (st != OLIVE_OK) return st;
+  }
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK) return st;
+  if (T == 0) {
+    const size_t n = static_cast<size_t>(d) * f * (grad_dtype == OLIVE_DTYPE_BF16 ? 2 : 4);
+    for (void* g : {dW_gate, dW_up, dW_down})
+      if (g && cudaMemsetAsync(g, 0, n, c.stream) != cudaSuccess) {
+        cudaGetLastError();
+        return OLIVE_ERR_CUDA;
+      }
+    return OLIVE_OK;
+  }
+  return launch_mlp_bwd(c, dy, x, W_gate, W_up, W_down, saved, T, d, f, activation, dx, dW_gate,
+                        dW_up, dW_down, grad_dtype, workspace, dev_status);
+}
+
+olive_status olive_grad_clip(const void* const* src, void* const* dst, const int64_t* numel,
+                             const int32_t* dtype, int32_t n, float max_norm, float* norm,
+                             void* workspace, size_t ws_bytes, void* stream) {
+  if (n < 0) return OLIVE_ERR_SHAPE;
+  if ((n > 0 && (!src || !numel || !dtype)) || !norm) return OLIVE_ERR_INVALID_ARG;
+  if (!(max_norm > 0.f)) return OLIVE_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n; ++i) {
+    if (dtype[i] != OLIVE_DTYPE_BF16 && dtype[i] != OLIVE_DTYPE_F32) return OLIVE_ERR_INVALID_ARG;
+    if (numel[i] < 0) return OLIVE_ERR_SHAPE;
+    if (numel[i] == 0) continue;
+    const uintptr_t whole = dtype[i] == OLIVE_DTYPE_BF16 ? 1 : 3;
+    if (!src[i] || (dst && !dst[i])) return OLIVE_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(src[i]) & whole) != 0 ||
+        (dst && (reinterpret_cast<uintptr_t>(dst[i]) & whole) != 0))
+      return OLIVE_ERR_ALIGNMENT;
+  }
+  olive_status st = check_ws(workspace, ws_bytes, grad_clip_ws_bytes(n > 0 ? n : 1));
+  if (st != OLIVE_OK) return st;
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK) return st;
+  return launch_grad_clip(c, src, dst, numel, dtype, n, max_norm, norm, workspace);
 }
 
 }  // extern "C"

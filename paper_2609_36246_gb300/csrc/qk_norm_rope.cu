@@ -1,0 +1,434 @@
+// qk_norm_rope.cu -- RMS norm of each query and key head and the rotation by the
+// token's position in one pass, forward and backward, and the packed tokens'
+// positions.
+//
+// A head's D values are held by the lanes of a group (8, 16 or 32 lanes for D up
+// to 64, 128 or 256), eight values each as two runs of four: in the half layout
+// j .. and j + R/2 .., so that both members of a pair are in one thread and a
+// rotation needs no exchange; the mean square is a butterfly over the group.  A
+// group takes several heads of one token and reads its cosines and sines once.
+//
+// What bounds it: HBM, 2 reads or writes of every value forward and 3 backward.
+#include <algorithm>
+
+#include "internal.h"
+
+#include <cuda_bf16.h>
+
+namespace olive {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxBwdBlocks = 1024;  // blocks whose partial weight gradients the workspace holds
+constexpr int kStatusToken = 1 << OLIVE_ERR_TOKEN_RANGE;
+
+template <typename T>
+struct Four;
+template <>
+struct Four<float> {
+  using Raw = float4;
+  static __device__ __forceinline__ void get(const Raw& r, float (&v)[4]) {
+    v[0] = r.x;
+    v[1] = r.y;
+    v[2] = r.z;
+    v[3] = r.w;
+  }
+  static __device__ __forceinline__ Raw put(const float (&v)[4]) { return make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <>
+struct Four<__nv_bfloat16> {
+  using Raw = uint2;
+  static __device__ __forceinline__ void get(const Raw& r, float (&v)[4]) {
+    v[0] = __uint_as_float(r.x << 16);
+    v[1] = __uint_as_float(r.x & 0xffff0000u);
+    v[2] = __uint_as_float(r.y << 16);
+    v[3] = __uint_as_float(r.y & 0xffff0000u);
+  }
+  static __device__ __forceinline__ Raw put(const float (&v)[4]) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  }
+};
+
+// What a lane holds of a head: two runs of four values.
+struct Place {
+  int a, b;       // their first elements
+  bool in, turn;  // the lane has a part of the head; a rotated one
+  int j;          // its first pair
+};
+template <bool kInter>
+__device__ __forceinline__ Place place(int lane, int D, int R) {
+  Place q;
+  q.in = lane < D / 8;
+  q.turn = lane < R / 8;
+  q.j = 4 * lane;
+  if (kInter || !q.turn) {
+    q.a = 8 * lane;
+    q.b = q.a + 4;
+  } else {
+    q.a = 4 * lane;
+    q.b = R / 2 + 4 * lane;
+  }
+  return q;
+}
+
+// The pairs of (a, b) turned by the angles (c, s).
+template <bool kInter>
+__device__ __forceinline__ void rotate(float (&a)[4], float (&b)[4], const float (&c)[4], const float (&s)[4]) {
+  if (kInter) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float x = a[2 * i], y = a[2 * i + 1], z = b[2 * i], w = b[2 * i + 1];
+      a[2 * i] = x * c[i] - y * s[i];
+      a[2 * i + 1] = y * c[i] + x * s[i];
+      b[2 * i] = z * c[2 + i] - w * s[2 + i];
+      b[2 * i + 1] = w * c[2 + i] + z * s[2 + i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = a[i], y = b[i];
+      a[i] = x * c[i] - y * s[i];
+      b[i] = y * c[i] + x * s[i];
+    }
+  }
+}
+
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// Item i of a launch: `per` heads of one token, all queries or all keys.
+struct Item {
+  int t, side, h0, h1;
+};
+__device__ __forceinline__ Item item_of(const QkArgs& p, long long i, int per, int nq, int nch) {
+  Item m;
+  m.t = static_cast<int>(i / nch);
+  int c = static_cast<int>(i - static_cast<long long>(m.t) * nch);
+  m.side = c >= nq;
+  if (m.side) c -= nq;
+  m.h0 = c * per;
+  m.h1 = min(m.h0 + per, p.heads[m.side]);
+  return m;
+}
+
+// Cosines and sines of a lane's pairs; `fine`: the position is inside the tables.
+__device__ __forceinline__ bool angles(const QkArgs& p, int t, const Place& q, bool report, float (&c)[4], float (&s)[4]) {
+  const int pos = p.positions[t];
+  const bool fine = pos >= 0 && pos < p.P;
+  if (!fine && report && p.dev_status) atomicOr(p.dev_status, kStatusToken);
+  if (q.turn) {
+    const size_t at = static_cast<size_t>(fine ? pos : 0) * (p.R / 2) + q.j;
+    Four<float>::get(*reinterpret_cast<const float4*>(p.cos + at), c);
+    Four<float>::get(*reinterpret_cast<const float4*>(p.sin + at), s);
+  }
+  return fine;
+}
+
+template <typename T, bool kInter, int L>
+__global__ void __launch_bounds__(kThreads) qk_fwd_kernel(const QkArgs p, int per, int nq, int nch) {
+  using V = Four<T>;
+  constexpr int kAtOnce = 4;  // heads whose loads are in flight together
+  const int lane = threadIdx.x % L;
+  const long long i = static_cast<long long>(blockIdx.x) * (kThreads / L) + threadIdx.x / L;
+  const bool live = i < static_cast<long long>(p.T) * nch;
+  const Item m = item_of(p, live ? i : 0, per, nq, nch);
+  const Place q = place<kInter>(lane, p.D, p.R);
+  const HeadsView src = p.in[m.side], dst = p.out[m.side];
+  const T* x = static_cast<const T*>(src.x) + static_cast<int64_t>(m.t) * src.token_stride;
+  T* y = static_cast<T*>(const_cast<void*>(dst.x)) + static_cast<int64_t>(m.t) * dst.token_stride;
+  const T* w = static_cast<const T*>(p.w[m.side]);
+  const float inv_d = 1.f / p.D;
+
+  float wa[4] = {}, wb[4] = {}, c[4] = {}, s[4] = {};
+  bool fine = true;
+  for (int h = m.h0; __any_sync(0xffffffffu, live && h < m.h1); h += kAtOnce) {
+    typename V::Raw ra[kAtOnce], rb[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (live && q.in && h + k < m.h1) {
+        const T* row = x + static_cast<int64_t>(h + k) * src.head_stride;
+        ra[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
+        rb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
+      } else {
+        ra[k] = rb[k] = typename V::Raw{};
+      }
+    }
+    if (h == m.h0 && live) {
+      fine = angles(p, m.t, q, lane == 0, c, s);
+      if (q.in) {
+        V::get(*reinterpret_cast<const typename V::Raw*>(w + q.a), wa);
+        V::get(*reinterpret_cast<const typename V::Raw*>(w + q.b), wb);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      float a[4], b[4];
+      V::get(ra[k], a);
+      V::get(rb[k], b);
+      float ss = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+      ss = group_sum<L>(ss);
+      if (!(live && q.in && h + k < m.h1)) continue;
+      float r = rsqrtf(fmaf(ss, inv_d, p.eps));
+      if (!fine) r = __uint_as_float(0x7fffffffu);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        a[e] = a[e] * r * wa[e];
+        b[e] = b[e] * r * wb[e];
+      }
+      if (q.turn) rotate<kInter>(a, b, c, s);
+      T* row = y + static_cast<int64_t>(h + k) * dst.head_stride;
+      *reinterpret_cast<typename V::Raw*>(row + q.a) = V::put(a);
+      *reinterpret_cast<typename V::Raw*>(row + q.b) = V::put(b);
+    }
+  }
+}
+
+// Backward.  With n = x r (r the reciprocal root mean square) and dn the
+// gradient turned back, dx = r (dn w - n mean(dn w n)) and dw = sum of dn n over
+// all tokens and heads: sum(x^2) and sum(dn w x) come from one butterfly.  A
+// thread keeps the weight gradients of its eight columns over all its heads; the
+// block adds its threads' up and stores them, and a second launch adds the blocks'.
+template <typename T, bool kInter, int L>
+__global__ void __launch_bounds__(kThreads) qk_bwd_kernel(const QkArgs p, int per, int nq, int nch) {
+  using V = Four<T>;
+  constexpr int kAtOnce = 2;
+  __shared__ float sums[kThreads / 32][2][8 * L];
+  const int lane = threadIdx.x % L;
+  const Place q = place<kInter>(lane, p.D, p.R);
+  const float inv_d = 1.f / p.D;
+  const long long items = static_cast<long long>(p.T) * nch;
+  const long long step = static_cast<long long>(gridDim.x) * (kThreads / L);
+  float w[2][8] = {}, dw[2][8] = {};
+  if (q.in) {
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      if (p.heads[side] == 0) continue;
+      const T* v = static_cast<const T*>(p.w[side]);
+      float a[4], b[4];
+      V::get(*reinterpret_cast<const typename V::Raw*>(v + q.a), a);
+      V::get(*reinterpret_cast<const typename V::Raw*>(v + q.b), b);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[side][e] = a[e];
+        w[side][4 + e] = b[e];
+      }
+    }
+  }
+
+  long long i = static_cast<long long>(blockIdx.x) * (kThreads / L) + threadIdx.x / L;
+  for (; __any_sync(0xffffffffu, i < items); i += step) {
+    const bool live = i < items;
+    const Item m = item_of(p, live ? i : 0, per, nq, nch);
+    const HeadsView src = p.in[m.side], grd = p.grad[m.side], dst = p.out[m.side];
+    const T* x = static_cast<const T*>(src.x) + static_cast<int64_t>(m.t) * src.token_stride;
+    const T* g = static_cast<const T*>(grd.x) + static_cast<int64_t>(m.t) * grd.token_stride;
+    T* y = static_cast<T*>(const_cast<void*>(dst.x)) + static_cast<int64_t>(m.t) * dst.token_stride;
+    float c[4] = {}, s[4] = {}, acc[8] = {}, wm[8];
+    bool fine = true;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) wm[e] = m.side ? w[1][e] : w[0][e];
+    for (int h = m.h0; __any_sync(0xffffffffu, live && h < m.h1); h += kAtOnce) {
+      typename V::Raw xa[kAtOnce], xb[kAtOnce], ga[kAtOnce], gb[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (live && q.in && h + k < m.h1) {
+          const T* row = x + static_cast<int64_t>(h + k) * src.head_stride;
+          xa[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
+          xb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
+          row = g + static_cast<int64_t>(h + k) * grd.head_stride;
+          ga[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
+          gb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
+        } else {
+          xa[k] = xb[k] = ga[k] = gb[k] = typename V::Raw{};
+        }
+      }
+      if (h == m.h0 && live) {
+        fine = angles(p, m.t, q, lane == 0, c, s);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = -s[e];
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        float v[8], d[8];
+        {
+          float a[4], b[4];
+          V::get(xa[k], a);
+          V::get(xb[k], b);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = a[e];
+            v[4 + e] = b[e];
+          }
+          V::get(ga[k], a);
+          V::get(gb[k], b);
+          if (q.turn) rotate<kInter>(a, b, c, s);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            d[e] = a[e];
+            d[4 + e] = b[e];
+          }
+        }
+        float ss = 0.f, dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          ss = fmaf(v[e], v[e], ss);
+          dot = fmaf(d[e] * wm[e], v[e], dot);
+        }
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) {
+          ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        }
+        if (!(live && q.in && h + k < m.h1)) continue;
+        float r = rsqrtf(fmaf(ss, inv_d, p.eps));
+        if (!fine) r = __uint_as_float(0x7fffffffu);
+        const float mean = dot * r * inv_d;  // mean(dn w n)
+        float a[4], b[4];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float n = v[e] * r;
+          acc[e] = fmaf(d[e], n, acc[e]);
+          const float o = r * fmaf(-n, mean, d[e] * wm[e]);
+          if (e < 4)
+            a[e] = o;
+          else
+            b[e - 4] = o;
+        }
+        T* row = y + static_cast<int64_t>(h + k) * dst.head_stride;
+        *reinterpret_cast<typename V::Raw*>(row + q.a) = V::put(a);
+        *reinterpret_cast<typename V::Raw*>(row + q.b) = V::put(b);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dw[0][e] += m.side ? 0.f : acc[e];
+      dw[1][e] += m.side ? acc[e] : 0.f;
+    }
+  }
+
+  // the warp's groups, then the block's warps
+#pragma unroll
+  for (int side = 0; side < 2; ++side)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float v = dw[side][e];
+#pragma unroll
+      for (int o = 16; o >= L; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (threadIdx.x % 32 < L && q.in) sums[threadIdx.x / 32][side][(e < 4 ? q.a : q.b - 4) + e] = v;
+    }
+  __syncthreads();
+  float* part = static_cast<float*>(p.ws) + static_cast<size_t>(blockIdx.x) * 2 * p.D;
+  for (int k = threadIdx.x; k < 2 * p.D; k += kThreads) {
+    const int side = k >= p.D, col = k - side * p.D;
+    float v = 0.f;
+#pragma unroll
+    for (int wp = 0; wp < kThreads / 32; ++wp) v += sums[wp][side][col];
+    part[k] = v;
+  }
+}
+
+// dw[side][col] = sum over the blocks, 32 columns a block, in a fixed order.
+__global__ void __launch_bounds__(256) qk_dw_kernel(const float* part, int blocks, int D, float* dw_q, float* dw_k) {
+  __shared__ double sums[8][32];
+  const int col = blockIdx.x * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
+  double v = 0.0;
+  if (col < 2 * D)
+    for (int b = g; b < blocks; b += 8) v += static_cast<double>(part[static_cast<size_t>(b) * 2 * D + col]);
+  sums[g][threadIdx.x % 32] = v;
+  __syncthreads();
+  if (g == 0 && col < 2 * D) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += sums[i][threadIdx.x];
+    (col < D ? dw_q[col] : dw_k[col - D]) = static_cast<float>(v);
+  }
+}
+
+__global__ void positions_kernel(const int32_t* cu, int S, int T_cap, int32_t* positions) {
+  const int t = blockIdx.x * blockDim.x + threadIdx.x;
+  if (t >= T_cap) return;
+  int lo = 0, hi = S;  // the last s with cu[s] <= t
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (cu[mid] <= t)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  positions[t] = lo < S ? t - cu[lo] : 0;
+}
+
+template <typename T, bool kInter, int L>
+void run_fwd(const Ctx& c, const QkArgs& a) {
+  // several heads an item where there are enough of them to fill the GPU
+  // anyway: their loads are in flight together and the angles are read once
+  const int64_t heads = static_cast<int64_t>(a.T) * (a.heads[0] + a.heads[1]);
+  const int64_t room = static_cast<int64_t>(c.num_sms) * 2048 / L;
+  const int per = heads >= 8 * room ? 8 : heads >= 4 * room ? 4 : 1;
+  const int nq = static_cast<int>(ceil_div(a.heads[0], per));
+  const int nch = nq + static_cast<int>(ceil_div(a.heads[1], per));
+  const int64_t blocks = ceil_div(static_cast<int64_t>(a.T) * nch, kThreads / L);
+  qk_fwd_kernel<T, kInter, L><<<static_cast<unsigned>(blocks), kThreads, 0, c.stream>>>(a, per, nq, nch);
+}
+
+template <typename T, bool kInter, int L>
+void run_bwd(const Ctx& c, const QkArgs& a) {
+  const int64_t heads = static_cast<int64_t>(a.T) * (a.heads[0] + a.heads[1]);
+  const int64_t room = static_cast<int64_t>(c.num_sms) * 1024 / L;
+  const int per = heads >= 8 * room ? 8 : heads >= 2 * room ? 2 : 1;
+  const int nq = static_cast<int>(ceil_div(a.heads[0], per));
+  const int nch = nq + static_cast<int>(ceil_div(a.heads[1], per));
+  const int64_t want = ceil_div(static_cast<int64_t>(a.T) * nch, kThreads / L);
+  const int blocks = static_cast<int>(std::min<int64_t>(want, std::min(4 * c.num_sms, kMaxBwdBlocks)));
+  if (blocks > 0) qk_bwd_kernel<T, kInter, L><<<blocks, kThreads, 0, c.stream>>>(a, per, nq, nch);
+  qk_dw_kernel<<<static_cast<int>(ceil_div(2 * a.D, 32)), 256, 0, c.stream>>>(
+      static_cast<const float*>(a.ws), blocks, a.D, a.dw[0], a.dw[1]);
+}
+
+template <bool kBwd, typename T, bool kInter>
+void by_width(const Ctx& c, const QkArgs& a) {
+  auto go = [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    if constexpr (kBwd)
+      run_bwd<T, kInter, L>(c, a);
+    else
+      run_fwd<T, kInter, L>(c, a);
+  };
+  if (a.D <= 64)
+    go(std::integral_constant<int, 8>{});
+  else if (a.D <= 128)
+    go(std::integral_constant<int, 16>{});
+  else
+    go(std::integral_constant<int, 32>{});
+}
+
+template <bool kBwd>
+olive_status by_type(const Ctx& c, const QkArgs& a) {
+  if (a.dtype == OLIVE_DTYPE_BF16)
+    a.interleaved ? by_width<kBwd, __nv_bfloat16, true>(c, a) : by_width<kBwd, __nv_bfloat16, false>(c, a);
+  else
+    a.interleaved ? by_width<kBwd, float, true>(c, a) : by_width<kBwd, float, false>(c, a);
+  return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t qk_bwd_ws_bytes(int64_t D) { return align_up(4ull * kMaxBwdBlocks * 2 * D, kWsAlign); }
+
+olive_status launch_qk_fwd(const Ctx& c, const QkArgs& a) { return by_type<false>(c, a); }
+
+olive_status launch_qk_bwd(const Ctx& c, const QkArgs& a) { return by_type<true>(c, a); }
+
+olive_status launch_packed_positions(const Ctx& c, const int32_t* cu_seqlens, int32_t S,
+                                     int32_t T_cap, int32_t* positions) {
+  positions_kernel<<<static_cast<unsigned>(ceil_div(T_cap, 256)), 256, 0, c.stream>>>(cu_seqlens, S, T_cap, positions);
+  return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
+}
+
+}  // namespace olive
