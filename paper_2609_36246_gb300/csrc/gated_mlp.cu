@@ -34,21 +34,28 @@ namespace {
 constexpr int kBM = 128;             // rows of a CTA's tile
 constexpr int kBN = 256;             // columns of a tile (128 of g and 128 of u in MM_UP)
 constexpr int kBK = 64;
-constexpr int kStages = 5;
 constexpr int kSA = kBM * kBK * 2;   // this CTA's 128 rows of A, or its half of B
 constexpr int kStageBytes = 2 * kSA;
 constexpr int kEpiWarps = 8;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 32 * 10;
-constexpr int kOutBuf = 32 * 128;    // a warp's 32 rows of 128 bytes
-constexpr int kOutBufs = 2;
-constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kOutBufs * kOutBuf + 8 * (2 * kStages + 5) + 64;
-static_assert(kSmem <= 227 * 1024, "shared memory budget");
+constexpr int kOutBuf = 32 * 64;     // a warp's 32 rows of 64 bytes
+enum { MM_UP = 0, MM_DOWN = 1, MM_DH = 2, MM_GRADS = 3 };
+// Three output buffers a warp where a tile gives three results, else two in turn.
+template <int kMode>
+struct Layout {
+  static constexpr bool kThree = kMode == MM_UP || kMode == MM_DH;
+  static constexpr int kOutBufs = kThree ? 3 : 2;
+  static constexpr int kStages = kThree ? 5 : 6;
+  static constexpr int kOut = kStages * kStageBytes;
+  static constexpr int kBars = kOut + kEpiWarps * kOutBufs * kOutBuf;
+  static constexpr int kMisc = kBars + 8 * (2 * kStages + 5);
+  static constexpr int kSmem = kMisc + 64;
+  static_assert(kSmem <= 227 * 1024, "shared memory budget");
+};
 constexpr int kRaster = 8;           // row tiles of a raster group (L2 reuse)
 constexpr int kMaxProbs = 4;
 constexpr int kStatusTimeout = 1 << OLIVE_ERR_TIMEOUT;
-
-enum { MM_UP = 0, MM_DOWN = 1, MM_DH = 2, MM_GRADS = 3 };
 
 // One product out[M, N] = A . B of a launch; maps are indices into MlpMaps.
 struct MlpProb {
@@ -59,18 +66,17 @@ struct MlpProb {
   int M, N;
   int mt, nt;              // pair tiles (256 rows), column tiles
   int ks_half, ks;         // K steps
-  int tile0;               // its first tile in the launch's list
 };
 
-// The tiles of all products form one list.  The first n_whole of it are dealt
-// to the pairs in turn; the K steps of the others (fewer than there are pairs)
-// are laid end to end and cut into runs of `run` steps, one a pair.
+// The first whole[i] tiles of each product are dealt to the pairs in turn; the K
+// steps of the others (fewer than there are pairs, of each product) are laid end
+// to end and cut into runs of `run` steps, one a pair.
 struct MlpSplit {
-  int n_whole;
+  int n_whole;             // sum of whole
+  int whole[kMaxProbs];
   int steps;               // K steps of the tiles that are cut
   int run;
-  int first[kMaxProbs];    // the cut tiles of each product, and their offset in steps
-  int off[kMaxProbs];
+  int off[kMaxProbs];      // offset in steps of each product's cut tiles
 };
 
 struct MlpMaps {
@@ -80,6 +86,7 @@ struct MlpMaps {
 struct MlpParams {
   MlpProb pr[kMaxProbs];
   int n_prob;
+  int n_maps;
   MlpSplit cut;
   float* part;             // [pairs][2 CTAs][8 warps][128 columns][32 rows] partial accumulators
   uint32_t* flag;          // [pairs][2 CTAs] warps that have stored theirs
@@ -88,7 +95,7 @@ struct MlpParams {
   const __nv_bfloat16* residual;  // MM_DOWN
   const uint16_t* saved_g;        // MM_DH: [T, f]
   const uint16_t* saved_u;
-  int save, act, out_f32;
+  int save, out_f32;
   int16_t map_g, map_u;    // MM_UP: saved g, u; MM_DH: dg, du
   int32_t* dev_status;
   uint64_t wait_limit_ns;
@@ -118,7 +125,7 @@ struct UnitWalk {
     const MlpProb& q = p.pr[i];
     Raster ra{q.mt, q.nt, kRaster};
     int mi, nj;
-    ra.tile(tile - q.tile0, mi, nj);
+    ra.tile(tile, mi, nj);
     u.prob = i;
     u.m0 = mi * 2 * kBM;
     u.n0 = nj;
@@ -126,9 +133,9 @@ struct UnitWalk {
   }
   __device__ bool next(const MlpParams& p, Unit& u) {
     if (t < p.cut.n_whole) {
-      int i = 0;
-      while (i + 1 < p.n_prob && t >= p.pr[i + 1].tile0) ++i;
-      place(p, i, t, u);
+      int i = 0, at = t;
+      while (i + 1 < p.n_prob && at >= p.cut.whole[i]) at -= p.cut.whole[i++];
+      place(p, i, at, u);
       u.k0 = 0;
       u.k1 = u.ks;
       u.from = pair;
@@ -141,7 +148,7 @@ struct UnitWalk {
     const int ks = p.pr[i].ks;
     const int w = (pos - 1 - p.cut.off[i]) / ks;
     const int start = p.cut.off[i] + w * ks;
-    place(p, i, p.cut.first[i] + w, u);
+    place(p, i, p.cut.whole[i] + w, u);
     u.k1 = pos - start;
     u.k0 = max(lo - start, 0);
     u.from = u.k0 > 0 ? start / p.cut.run : pair;
@@ -161,22 +168,28 @@ __device__ __forceinline__ void bulk_wait_read_but_one() {
   asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
 }
 
-template <int kMode>
+// Stores to a warp's output buffer: 16-byte piece `c` of row `lane`, 64-byte
+// swizzle (as the tensor maps of the outputs), and the buffer to (x, y).
+__device__ __forceinline__ uint32_t out_piece(uint32_t buf, int lane, int c) {
+  return buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4);
+}
+
+template <int kMode, int kAct>
 __global__ void __launch_bounds__(kThreads, 1)
     mlp_gemm_kernel(const __grid_constant__ MlpMaps maps, const __grid_constant__ MlpParams p) {
+  using L = Layout<kMode>;
+  constexpr int kStages = L::kStages;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
   const uint32_t stages = base;
-  const uint32_t out_bufs = base + kStages * kStageBytes;
-  const uint32_t bar0 = out_bufs + kEpiWarps * kOutBufs * kOutBuf;
+  const uint32_t bar0 = base + L::kBars;
   auto full_bar = [&](int st) { return bar0 + 8u * st; };
   auto empty_bar = [&](int st) { return bar0 + 8u * (kStages + st); };
   auto tfull = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
   auto tempty = [&](int b) { return bar0 + 8u * (2 * kStages + 2 + b); };
   const uint32_t drain = bar0 + 8u * (2 * kStages + 4);
-  uint8_t* misc = smem_raw + kStages * kStageBytes + kEpiWarps * kOutBufs * kOutBuf + 8 * (2 * kStages + 5);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_raw + L::kMisc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + L::kMisc + 4);
 
   const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5));
   const int lane = threadIdx.x & 31;
@@ -196,6 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     *abort_flag = 0;
     fence_mbar_init();
   }
+  if (warp == kProducerWarp && lane < p.n_maps) tma_prefetch_desc(&maps.m[lane]);
   if (warp == kMmaWarp) {
     tmem_alloc_pair(smem_u32(tmem_slot), 512);
     tmem_relinquish_pair();
@@ -299,44 +313,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else {
     // epilogue warp w: rows 32 (w % 4).. of the CTA's tile (TMEM lanes, one row
-    // a thread) and half w / 4 of its columns, in four 32-column chunks
+    // a thread) and half w / 4 of its columns, 16 columns at a time.  The loops
+    // are rolled: a tile's epilogue runs once in several microseconds, and code
+    // that is unrolled over the columns is fetched from the L2 each time.
     const int half = warp >> 2;
-    const int row = (warp & 3) * 32 + lane;
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    const uint32_t buf0 = out_bufs + warp * kOutBufs * kOutBuf;
-    int sb = 0, n = 0;
+    const uint32_t out0 = base + L::kOut + warp * L::kOutBufs * kOutBuf;
+    int n = 0, turn = 0;
     bool ok = true;
-
-    // 32 rows of 128 bytes through shared memory (128-byte swizzle) to (x, y)
-    auto emit = [&](const CUtensorMap* map, int x, int y, const uint32_t (&w)[32]) {
-      if (lane == 0) bulk_wait_read_but_one();
-      __syncwarp();
-      const uint32_t buf = buf0 + sb * kOutBuf;
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        st_shared_v4(buf + lane * 128 + ((c ^ (lane & 7)) << 4),
-                     make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
-      fence_proxy_async_shared();
-      __syncwarp();
-      if (lane == 0) {
-        tma_store_2d(map, buf, x, y);
-        bulk_commit();
-      }
-      sb ^= 1;
-    };
 
     while (ok && walk.next(p, u)) {
       const MlpProb& q = p.pr[u.prob];
       const int b = n & 1;
-      if (!mbar_wait_warp(tfull(b), (n >> 1) & 1, ctl)) break;
-      tc_fence_after();
-      ++n;
       const uint32_t acc = lane_addr + b * kBN;
-      // TMEM column of this warp's 32-column chunk j (MM_UP: chunks 0, 1 of g, 2, 3 of u)
-      auto col_of = [&](int j) {
-        return kMode == MM_UP ? (j >> 1) * 128 + half * 64 + (j & 1) * 32 : half * 128 + j * 32;
-      };
-      auto my_part = [&](int pr) {
+      const int y = u.m0 + static_cast<int>(rank) * kBM + (warp & 3) * 32;  // the warp's first row
+      const int t = y + lane;
+      const int x0 = kMode == MM_UP ? u.n0 * kBM + half * 64 : u.n0 * kBN + half * 128;
+      constexpr int kSteps = kMode == MM_UP ? 4 : 8;  // of 16 result columns
+      // TMEM column of step s (MM_UP: g; u is 128 columns on)
+      auto col = [&](int s) { return half * (kMode == MM_UP ? 64 : 128) + s * 16; };
+      auto part_of = [&](int pr) {
         return p.part + (static_cast<size_t>(pr * 2 + static_cast<int>(rank)) * kEpiWarps + warp) * (128 * 32) + lane;
       };
       auto release = [&] {
@@ -344,17 +340,38 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(map_shared(tempty(b), 0));
       };
+      // what the epilogue reads from memory, one step ahead of its use
+      const bool whole = u.k1 == u.ks;
+      uint4 e0[2] = {}, e1[2] = {};
+      auto fetch = [&](int s) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int x = x0 + s * 16 + v * 8;
+          const bool in = whole && s < kSteps && t < q.M && x < q.N;
+          const size_t at = static_cast<size_t>(t) * q.N + x;
+          if (kMode == MM_DOWN)
+            e0[v] = in && p.residual ? *reinterpret_cast<const uint4*>(p.residual + at) : make_uint4(0, 0, 0, 0);
+          if (kMode == MM_DH) {
+            e0[v] = in ? __ldg(reinterpret_cast<const uint4*>(p.saved_g + at)) : make_uint4(0, 0, 0, 0);
+            e1[v] = in ? __ldg(reinterpret_cast<const uint4*>(p.saved_u + at)) : make_uint4(0, 0, 0, 0);
+          }
+        }
+      };
+      fetch(0);
+      if (!mbar_wait_warp(tfull(b), (n >> 1) & 1, ctl)) break;
+      tc_fence_after();
+      ++n;
 
-      if (u.k1 < u.ks) {
+      if (!whole) {
         // a piece of a tile that another pair finishes
-        float* to = my_part(pair);
+        float* to = part_of(pair);
 #pragma unroll 1
-        for (int j = 0; j < 4; ++j) {
-          uint32_t r[32];
-          tmem_ld_32x32b_x32(acc + col_of(j), r);
+        for (int s = 0; s < 8; ++s) {
+          uint32_t r[16];
+          tmem_ld_32x32b_x16(acc + (kMode == MM_UP ? (s >> 2) * 128 + col(s & 3) : col(s)), r);
           tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) __stcg(to + (j * 32 + i) * 32, __uint_as_float(r[i]));
+          for (int i = 0; i < 16; ++i) __stcg(to + (s * 16 + i) * 32, __uint_as_float(r[i]));
         }
         release();
         __threadfence();
@@ -367,146 +384,140 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
       }
-      auto load = [&](int j, uint32_t(&r)[32]) {
-        tmem_ld_32x32b_x32(acc + col_of(j), r);
+      // step s of the finished accumulator: the pair's own sum and the pieces'
+      auto load = [&](int tcol, int s, uint32_t(&r)[16]) {
+        tmem_ld_32x32b_x16(acc + tcol, r);
         tmem_ld_wait();
         for (int o = u.from; o < pair; ++o) {
-          const float* s = my_part(o) + j * 32 * 32;
+          const float* f = part_of(o) + s * 16 * 32;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __ldcg(s + i * 32));
+          for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __ldcg(f + i * 32));
         }
       };
+      const bool inside = y < q.M;
 
-      const int y = u.m0 + static_cast<int>(rank) * kBM + (warp & 3) * 32;  // the warp's first row
-      const int t = y + lane;
-      if constexpr (kMode == MM_UP) {
-        const int x = u.n0 * kBM + half * 64;
-        uint32_t hw[32], gw[32], uw[32];
+#pragma unroll 1
+      for (int s = 0; s < kSteps; ++s) {
+        const int x = x0 + (s & ~1) * 16;  // first column of the 64-byte output rows
+        // (fp32 results fill a buffer in one step)
+        const bool f32 = kMode == MM_GRADS && p.out_f32;
+        const bool opens = f32 || (s & 1) == 0, closes = f32 || (s & 1) == 1;
+        uint32_t r[16], v[16];
+        load(col(s), s, r);
+        if constexpr (kMode == MM_UP) load(128 + col(s), 4 + s, v);
+        if (s == kSteps - 1) release();
+        uint32_t buf = out0;
+        if (opens) {
+          // the buffers about to be written have been read by their last store
+          if (lane == 0) {
+            if (L::kThree)
+              bulk_wait_read();
+            else
+              bulk_wait_read_but_one();
+          }
+          __syncwarp();
+        }
+        if constexpr (!L::kThree) buf += turn * kOutBuf;
+        const int c0 = f32 ? 0 : (s & 1) * 2;  // 16-byte pieces of the row
+
+        if constexpr (kMode == MM_UP) {
+          uint32_t hw[8], gw[8], uw[8], wide = 0;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          uint32_t g[32], v[32];
-          load(j, g);
-          load(2 + j, v);
+          for (int i = 0; i < 8; ++i) {
+            const float g0 = __uint_as_float(r[2 * i]), g1 = __uint_as_float(r[2 * i + 1]);
+            const float u0 = __uint_as_float(v[2 * i]), u1 = __uint_as_float(v[2 * i + 1]);
+            hw[i] = pack_bf16x2(activate<kAct>(g0) * u0, activate<kAct>(g1) * u1);
+            gw[i] = pack_saved(g0, g1, wide);
+            uw[i] = pack_saved(u0, u1, wide);
+          }
+          if (wide & kSavedWide) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float g0 = __uint_as_float(g[i]), g1 = __uint_as_float(g[i + 1]);
-            const float u0 = __uint_as_float(v[i]), u1 = __uint_as_float(v[i + 1]);
-            hw[j * 16 + i / 2] = pack_bf16x2(activate(g0, p.act) * u0, activate(g1, p.act) * u1);
-            if (p.save) {
-              gw[j * 16 + i / 2] = pack_saved(g0, g1);
-              uw[j * 16 + i / 2] = pack_saved(u0, u1);
+            for (int i = 0; i < 8; ++i) {
+              gw[i] = saved_bits(__uint_as_float(r[2 * i])) | saved_bits(__uint_as_float(r[2 * i + 1])) << 16;
+              uw[i] = saved_bits(__uint_as_float(v[2 * i])) | saved_bits(__uint_as_float(v[2 * i + 1])) << 16;
             }
           }
-        }
-        release();
-        if (y < q.M && x < q.N) {
-          emit(&maps.m[q.out], x, y, hw);
-          if (p.save) {
-            emit(&maps.m[p.map_g], x, y, gw);
-            emit(&maps.m[p.map_u], x, y, uw);
-          }
-        }
-      } else if constexpr (kMode == MM_DOWN) {
-#pragma unroll 1
-        for (int c = 0; c < 2; ++c) {
-          const int x = u.n0 * kBN + half * 128 + c * 64;
-          uint32_t w[32];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint32_t r[32];
-            load(2 * c + j, r);
-            if (p.residual && t < q.M) {
-#pragma unroll
-              for (int v = 0; v < 4; ++v) {
-                const int xv = x + j * 32 + v * 8;
-                if (xv < q.N) {
-                  const uint4 e = *reinterpret_cast<const uint4*>(p.residual + static_cast<size_t>(t) * q.N + xv);
-                  const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    r[v * 8 + 2 * i] = __float_as_uint(__uint_as_float(r[v * 8 + 2 * i]) + __uint_as_float(ew[i] << 16));
-                    r[v * 8 + 2 * i + 1] =
-                        __float_as_uint(__uint_as_float(r[v * 8 + 2 * i + 1]) + __uint_as_float(ew[i] & 0xffff0000u));
-                  }
-                }
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) w[j * 16 + i / 2] = pack_bf16x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-          }
-          if (c == 1) release();
-          if (y < q.M && x < q.N) emit(&maps.m[q.out], x, y, w);
-        }
-      } else if constexpr (kMode == MM_DH) {
-#pragma unroll 1
-        for (int c = 0; c < 2; ++c) {
-          const int x = u.n0 * kBN + half * 128 + c * 64;
-          uint32_t gw[32], uw[32], hw[32];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint4 sg[4], su[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const int xv = x + j * 32 + v * 8;
-              const bool in = t < q.M && xv < q.N;
-              const size_t at = static_cast<size_t>(t) * q.N + xv;
-              sg[v] = in ? *reinterpret_cast<const uint4*>(p.saved_g + at) : make_uint4(0, 0, 0, 0);
-              su[v] = in ? *reinterpret_cast<const uint4*>(p.saved_u + at) : make_uint4(0, 0, 0, 0);
-            }
-            uint32_t r[32];
-            load(2 * c + j, r);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const uint32_t gs[4] = {sg[v].x, sg[v].y, sg[v].z, sg[v].w};
-              const uint32_t us[4] = {su[v].x, su[v].y, su[v].z, su[v].w};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                float a[2], ds[2], uu[2];
-                const float dh[2] = {__uint_as_float(r[v * 8 + 2 * i]), __uint_as_float(r[v * 8 + 2 * i + 1])};
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  activate_both(unpack_saved(gs[i], e), p.act, a[e], ds[e]);
-                  uu[e] = unpack_saved(us[i], e);
-                }
-                const int o = j * 16 + v * 4 + i;
-                gw[o] = pack_bf16x2(dh[0] * uu[0] * ds[0], dh[1] * uu[1] * ds[1]);
-                uw[o] = pack_bf16x2(dh[0] * a[0], dh[1] * a[1]);
-                hw[o] = pack_bf16x2(a[0] * uu[0], a[1] * uu[1]);
-              }
-            }
-          }
-          if (c == 1) release();
-          if (y < q.M && x < q.N) {
-            emit(&maps.m[p.map_g], x, y, gw);
-            emit(&maps.m[p.map_u], x, y, uw);
-            emit(&maps.m[q.out], x, y, hw);
-          }
-        }
-      } else {
-        if (p.out_f32) {
-#pragma unroll 1
-          for (int j = 0; j < 4; ++j) {
-            const int x = u.n0 * kBN + half * 128 + j * 32;
-            uint32_t r[32];
-            load(j, r);
-            if (j == 3) release();
-            if (y < q.M && x < q.N) emit(&maps.m[q.out], x, y, r);
-          }
-        } else {
-#pragma unroll 1
           for (int c = 0; c < 2; ++c) {
-            const int x = u.n0 * kBN + half * 128 + c * 64;
-            uint32_t w[32];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              uint32_t r[32];
-              load(2 * c + j, r);
-#pragma unroll
-              for (int i = 0; i < 32; i += 2) w[j * 16 + i / 2] = pack_bf16x2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-            }
-            if (c == 1) release();
-            if (y < q.M && x < q.N) emit(&maps.m[q.out], x, y, w);
+            st_shared_v4(out_piece(buf, lane, c0 + c), make_uint4(hw[4 * c], hw[4 * c + 1], hw[4 * c + 2], hw[4 * c + 3]));
+            st_shared_v4(out_piece(buf + kOutBuf, lane, c0 + c),
+                         make_uint4(gw[4 * c], gw[4 * c + 1], gw[4 * c + 2], gw[4 * c + 3]));
+            st_shared_v4(out_piece(buf + 2 * kOutBuf, lane, c0 + c),
+                         make_uint4(uw[4 * c], uw[4 * c + 1], uw[4 * c + 2], uw[4 * c + 3]));
           }
+        } else if constexpr (kMode == MM_DH) {
+          const uint32_t gs[8] = {e0[0].x, e0[0].y, e0[0].z, e0[0].w, e0[1].x, e0[1].y, e0[1].z, e0[1].w};
+          const uint32_t us[8] = {e1[0].x, e1[0].y, e1[0].z, e1[0].w, e1[1].x, e1[1].y, e1[1].z, e1[1].w};
+          fetch(s + 1);
+          uint32_t hw[8], gw[8], uw[8], bad = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float a0, a1, d0, d1;
+            activate_both<kAct>(saved_lo(gs[i]), a0, d0);
+            activate_both<kAct>(saved_hi(gs[i]), a1, d1);
+            const float u0 = saved_lo(us[i]), u1 = saved_hi(us[i]);
+            const float h0 = __uint_as_float(r[2 * i]), h1 = __uint_as_float(r[2 * i + 1]);
+            gw[i] = pack_bf16x2(h0 * u0 * d0, h1 * u1 * d1);
+            uw[i] = pack_bf16x2(h0 * a0, h1 * a1);
+            hw[i] = pack_bf16x2(a0 * u0, a1 * u1);
+            bad |= saved_nan(gs[i]) | saved_nan(us[i]);
+          }
+          if (bad) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              // (0x7fff is NaN in bf16 as well)
+              const uint32_t m = saved_nan(gs[i]) | saved_nan(us[i]);
+              const uint32_t nan = (m >> 15) * 0x7fffu;
+              gw[i] |= nan;
+              uw[i] |= nan;
+              hw[i] |= nan;
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            st_shared_v4(out_piece(buf, lane, c0 + c), make_uint4(hw[4 * c], hw[4 * c + 1], hw[4 * c + 2], hw[4 * c + 3]));
+            st_shared_v4(out_piece(buf + kOutBuf, lane, c0 + c),
+                         make_uint4(gw[4 * c], gw[4 * c + 1], gw[4 * c + 2], gw[4 * c + 3]));
+            st_shared_v4(out_piece(buf + 2 * kOutBuf, lane, c0 + c),
+                         make_uint4(uw[4 * c], uw[4 * c + 1], uw[4 * c + 2], uw[4 * c + 3]));
+          }
+        } else if (f32) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            st_shared_v4(out_piece(buf, lane, c), make_uint4(r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]));
+        } else {
+          if constexpr (kMode == MM_DOWN) {
+            const uint32_t rs[8] = {e0[0].x, e0[0].y, e0[0].z, e0[0].w, e0[1].x, e0[1].y, e0[1].z, e0[1].w};
+            fetch(s + 1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              r[2 * i] = __float_as_uint(__uint_as_float(r[2 * i]) + __uint_as_float(rs[i] << 16));
+              r[2 * i + 1] = __float_as_uint(__uint_as_float(r[2 * i + 1]) + __uint_as_float(rs[i] & 0xffff0000u));
+            }
+          }
+          uint32_t w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = pack_bf16x2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            st_shared_v4(out_piece(buf, lane, c0 + c), make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]));
+        }
+
+        if (closes) {
+          fence_proxy_async_shared();
+          __syncwarp();
+          const int xo = f32 ? x0 + s * 16 : x;
+          if (lane == 0) {
+            if (inside && xo < q.N) {
+              tma_store_2d(&maps.m[q.out], buf, xo, y);
+              if (kMode == MM_DH || (kMode == MM_UP && p.save)) {
+                tma_store_2d(&maps.m[p.map_g], buf + kOutBuf, xo, y);
+                tma_store_2d(&maps.m[p.map_u], buf + 2 * kOutBuf, xo, y);
+              }
+            }
+            bulk_commit();
+          }
+          turn ^= 1;
         }
       }
     }
@@ -529,18 +540,18 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Pairs of CTAs the device holds at once (at most one for two SMs): runs of cut
 // tiles wait for one another, so the grid is never larger.
-template <int kMode>
+template <int kMode, int kAct>
 int resident_pairs(const Ctx& c) {
   static std::atomic<int> held[kMaxDevices];
   const bool cached = c.device >= 0 && c.device < kMaxDevices;
   int n = cached ? held[c.device].load(std::memory_order_acquire) - 1 : -1;
   if (n >= 0) return n;
   static std::atomic<int> done[kMaxDevices];
-  if (!set_smem_once(reinterpret_cast<const void*>(mlp_gemm_kernel<kMode>), kSmem, c.device, done)) return 0;
+  if (!set_smem_once(reinterpret_cast<const void*>(mlp_gemm_kernel<kMode, kAct>), Layout<kMode>::kSmem, c.device, done)) return 0;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * (c.num_sms / 2));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
+  cfg.dynamicSmemBytes = Layout<kMode>::kSmem;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2;
@@ -548,7 +559,7 @@ int resident_pairs(const Ctx& c) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, mlp_gemm_kernel<kMode>, &cfg) != cudaSuccess) {
+  if (cudaOccupancyMaxActiveClusters(&n, mlp_gemm_kernel<kMode, kAct>, &cfg) != cudaSuccess) {
     cudaGetLastError();
     return 0;
   }
@@ -557,47 +568,58 @@ int resident_pairs(const Ctx& c) {
   return n;
 }
 
-// Deals the tiles: whole ones while every pair gets one, the rest (fewer than
-// there are pairs) cut into equal runs of K steps where that is the shorter way.
-// A cut costs each pair the store of one partial accumulator, and its finisher
-// the wait for the others and their loads: about kCutCost K steps.
+// Deals the tiles to `pairs` pairs, whole ones or cut, whichever ends sooner; a
+// cut costs each pair the store of one partial accumulator, and its finisher the
+// wait for the others and their loads: about kCutCost K steps.  Returns the
+// pairs to launch.
 constexpr int kCutCost = 14;
 constexpr int kMinRun = 4;
-// Returns the pairs to launch.
 int plan(MlpParams& p, int pairs) {
-  int tiles = 0;
-  for (int i = 0; i < p.n_prob; ++i) {
-    p.pr[i].tile0 = tiles;
-    tiles += p.pr[i].mt * p.pr[i].nt;
-  }
   MlpSplit& s = p.cut;
   s = MlpSplit{};
-  s.n_whole = tiles;
   s.run = 1;
-  const int first = tiles - tiles % pairs;
-  int steps = 0, longest = 0;
+  // whole tiles, in turn: the pair with the most steps
+  int tiles[kMaxProbs], all = 0;
+  int64_t whole_end = 0;
   for (int i = 0; i < p.n_prob; ++i) {
-    const int end = p.pr[i].tile0 + p.pr[i].mt * p.pr[i].nt;
-    s.first[i] = std::max(first, p.pr[i].tile0);
+    tiles[i] = p.pr[i].mt * p.pr[i].nt;
+    all += tiles[i];
+  }
+  for (int r = 0; r < std::min(pairs, all); ++r) {
+    int64_t load = 0;
+    int first = 0;
+    for (int i = 0; i < p.n_prob; first += tiles[i++]) {
+      const int skip = ((r - first) % pairs + pairs) % pairs;  // to this pair's first tile of the product
+      if (skip < tiles[i]) load += static_cast<int64_t>(ceil_div(tiles[i] - skip, pairs)) * p.pr[i].ks;
+    }
+    whole_end = std::max(whole_end, load);
+  }
+  // every product's last tiles cut
+  int64_t cut_end = 0;
+  int steps = 0;
+  for (int i = 0; i < p.n_prob; ++i) {
+    const int rest = tiles[i] % pairs;
+    s.whole[i] = tiles[i] - rest;
     s.off[i] = steps;
-    const int count = std::max(0, end - s.first[i]);
-    if (count > 0) longest = std::max(longest, p.pr[i].ks);
-    steps += count * p.pr[i].ks;
+    steps += rest * p.pr[i].ks;
+    cut_end += static_cast<int64_t>(s.whole[i] / pairs) * p.pr[i].ks;
   }
   const int run = std::max(kMinRun, static_cast<int>(ceil_div(steps, pairs)));
-  if (steps > 0 && run + kCutCost < longest) {
-    s.n_whole = first;
+  if (steps > 0 && cut_end + run + kCutCost < whole_end) {
+    for (int i = 0; i < p.n_prob; ++i) s.n_whole += s.whole[i];
     s.steps = steps;
     s.run = run;
-    return first > 0 ? pairs : static_cast<int>(ceil_div(steps, run));
+    return s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, run));
   }
-  return std::min(pairs, tiles);
+  for (int i = 0; i < p.n_prob; ++i) s.whole[i] = tiles[i];
+  s.n_whole = all;
+  return std::min(pairs, all);
 }
 
 // `zeroed`: an earlier launch of the call clears this one's flags.
-template <int kMode>
+template <int kMode, int kAct = 0>
 olive_status launch(const Ctx& c, const MlpMaps& maps, MlpParams& p, bool zeroed) {
-  int pairs = resident_pairs<kMode>(c);
+  int pairs = resident_pairs<kMode, kAct>(c);
   if (pairs < 1) return OLIVE_ERR_UNSUPPORTED_DEVICE;
   pairs = plan(p, pairs);
   if (p.cut.steps > 0 && !zeroed &&
@@ -609,7 +631,7 @@ olive_status launch(const Ctx& c, const MlpMaps& maps, MlpParams& p, bool zeroed
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * pairs);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
+  cfg.dynamicSmemBytes = Layout<kMode>::kSmem;
   cfg.stream = c.stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -618,7 +640,7 @@ olive_status launch(const Ctx& c, const MlpMaps& maps, MlpParams& p, bool zeroed
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, mlp_gemm_kernel<kMode>, maps, p) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, mlp_gemm_kernel<kMode, kAct>, maps, p) != cudaSuccess) {
     cudaGetLastError();
     return OLIVE_ERR_CUDA;
   }
@@ -642,10 +664,9 @@ struct MapSet {
   int16_t mn_major(const void* a, int64_t rows, int64_t cols) {
     return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, 64, kBK));
   }
-  // output [rows, cols]: boxes of 32 rows x 128 bytes
+  // output [rows, cols]: boxes of 32 rows x 64 bytes
   int16_t output(void* a, int64_t rows, int64_t cols, bool f32) {
-    return add(f32 ? encode_f32_2d(&maps.m[n], a, cols, rows, 4 * cols, 32, 32)
-                   : encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, 64, 32));
+    return add(encode_out_2d(&maps.m[n], a, cols, rows, f32, 32));
   }
 };
 
@@ -670,6 +691,8 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
                             int32_t f, int act, void* y, void* saved, void* ws,
                             int32_t* dev_status) {
   const MlpWs w = carve_mlp(ws, T, f, false);
+  if (T <= kMlpFewRows)
+    return launch_mlp_few(c, x, W_gate, W_up, W_down, residual, T, d, f, act, y, saved, w.h, dev_status);
   uint16_t* sg = static_cast<uint16_t*>(saved);
   uint16_t* su = saved ? sg + static_cast<size_t>(T) * f : nullptr;
   {
@@ -687,14 +710,15 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
     if (!s.ok) return OLIVE_ERR_CUDA;
     p.pr[0] = q;
     p.n_prob = 1;
+  p.n_maps = s.n;
     p.save = saved != nullptr;
-    p.act = act;
     p.part = w.part;
     p.flag = w.flag;
     p.clear = w.flag + mlp_flag_words();
     p.n_clear = static_cast<int>(mlp_flag_words());
     p.dev_status = dev_status;
-    const olive_status st = launch<MM_UP>(c, s.maps, p, false);
+    const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_UP, OLIVE_ACT_SILU>(c, s.maps, p, false)
+                                                  : launch<MM_UP, OLIVE_ACT_GELU_TANH>(c, s.maps, p, false);
     if (st != OLIVE_OK) return st;
   }
   MapSet s;
@@ -706,6 +730,7 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
   if (!s.ok) return OLIVE_ERR_CUDA;
   p.pr[0] = q;
   p.n_prob = 1;
+  p.n_maps = s.n;
   p.residual = static_cast<const __nv_bfloat16*>(residual);
   p.part = w.part;
   p.flag = w.flag + mlp_flag_words();
@@ -731,7 +756,7 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
     if (!s.ok) return OLIVE_ERR_CUDA;
     p.pr[0] = q;
     p.n_prob = 1;
-    p.act = act;
+  p.n_maps = s.n;
     p.saved_g = static_cast<const uint16_t*>(saved);
     p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
     p.part = w.part;
@@ -739,7 +764,8 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
     p.clear = w.flag + mlp_flag_words();
     p.n_clear = static_cast<int>(mlp_flag_words());
     p.dev_status = dev_status;
-    const olive_status st = launch<MM_DH>(c, s.maps, p, false);
+    const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_DH, OLIVE_ACT_SILU>(c, s.maps, p, false)
+                                                  : launch<MM_DH, OLIVE_ACT_GELU_TANH>(c, s.maps, p, false);
     if (st != OLIVE_OK) return st;
   }
   MapSet s;
@@ -771,6 +797,7 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
     p.pr[p.n_prob++] = q;
   }
   if (!s.ok) return OLIVE_ERR_CUDA;
+  p.n_maps = s.n;
   p.out_f32 = f32;
   p.part = w.part;
   p.flag = w.flag + mlp_flag_words();

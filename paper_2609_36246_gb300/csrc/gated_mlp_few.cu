@@ -1,0 +1,362 @@
+// gated_mlp_few.cu -- the gated feed-forward block on few rows (single tokens, a
+// batch's next tokens), forward: two launches that read the weights once.
+//
+// Few rows make the weights the wide operand: they are A (M = 128 weight rows in
+// the lanes), the tokens B (N = 16 to 128 columns), so one MMA shape serves any
+// count of tokens and the accumulator's columns are the tokens.
+//   launch 1  a CTA takes `rows` rows of W_gate and the same of W_up, into two
+//             accumulators, so that a thread has g and u of its row; h = act(g) u
+//   launch 2  a CTA takes `rows` rows of W_down; y = h W_down^T (+ residual)
+// MMAs always cover 128 lanes: where a CTA has fewer rows the others read what
+// lies behind the tile in shared memory and their lanes are not read back.
+//
+// What bounds it: HBM, the weights' 6 d f bytes; so the CTAs are made small and
+// many (two to an SM, up to 108 KB each in flight).  Where there are too few
+// rows for that, the CTAs of a cluster share a tile's K steps and add their
+// accumulators up through distributed shared memory, every CTA for a part of the
+// tokens, in the cluster's order.  The second launch starts while the first runs
+// (programmatic dependent launch) and fills its stages with W_down before it waits
+// for h.
+#include <algorithm>
+#include <atomic>
+
+#include "gated_mlp.cuh"
+#include "sm103.cuh"
+
+namespace olive {
+namespace {
+
+constexpr int kBK = 64;
+constexpr int kMaxStages = 24;
+constexpr int kEpiWarps = 4, kProducerWarp = 4, kMmaWarp = 5;
+constexpr int kThreads = 32 * 6;
+constexpr int kTile = 128 * 128;      // bytes the MMA reads of an A tile
+// shared memory of a CTA: two to an SM, or one where the tokens' tile is large
+constexpr int budget(int n) { return (n <= 64 ? 108 : 210) * 1024; }
+constexpr int kBarBytes = 8 * (2 * kMaxStages + 1) + 16;
+
+struct FewMaps {
+  CUtensorMap a0, a1, b;  // W_gate, W_up (or W_down), tokens
+};
+struct FewParams {
+  int T, rows_all, K;     // tokens, weight rows, inner width
+  int rows, stages;
+  void* out;              // h or y, [T, rows_all]
+  const __nv_bfloat16* residual;
+  uint16_t *saved_g, *saved_u;
+  int32_t* dev_status;
+  uint64_t wait_limit_ns;
+};
+
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+  return r;
+}
+
+template <bool kUp, int kN, int kAct>
+__global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ FewMaps maps, const FewParams p) {
+  constexpr int kAcc = kUp ? 2 : 1;
+  constexpr uint32_t kCols = kAcc * kN < 32 ? 32 : kAcc * kN;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  const int a_bytes = p.rows * 128;
+  const int stage_bytes = kAcc * a_bytes + kN * 128;
+  // barriers first (1 KB), then the stages, then what the last one's MMAs read past it
+  auto full_bar = [&](int s) { return base + 8u * s; };
+  auto empty_bar = [&](int s) { return base + 8u * (kMaxStages + s); };
+  const uint32_t done_bar = base + 8u * (2 * kMaxStages);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_raw + 8 * (2 * kMaxStages + 1));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_raw + 8 * (2 * kMaxStages + 1) + 4);
+  const uint32_t ring = base + 1024;
+  float* recv = reinterpret_cast<float*>(smem_raw + 1024);
+
+  const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5));
+  const int lane = threadIdx.x & 31;
+  const int c = static_cast<int>(cluster_size()), rank = static_cast<int>(cluster_rank());
+  const int row0 = static_cast<int>(blockIdx.x) / c * p.rows;
+  const int t0 = static_cast<int>(blockIdx.y) * kN;
+  const int nt = min(kN, p.T - t0);
+  const int ks_all = (p.K + kBK - 1) / kBK;
+  const int ks0 = ks_all * rank / c, ks1 = ks_all * (rank + 1) / c;
+
+  if (kUp) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    mbar_init(done_bar, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == kProducerWarp && lane == 0) {
+    tma_prefetch_desc(&maps.a0);
+    if (kUp) tma_prefetch_desc(&maps.a1);
+    tma_prefetch_desc(&maps.b);
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(tmem_slot), kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const WaitCtl ctl{abort_flag, p.wait_limit_ns};
+  bool ok = true;
+
+  if (warp == kProducerWarp) {
+    const bool leader = elect_one();
+    auto weights = [&](int s, int ks) {
+      const uint32_t at = ring + s * stage_bytes;
+      mbar_arrive_expect_tx(full_bar(s), stage_bytes);
+      tma_load_2d(at, &maps.a0, full_bar(s), ks * kBK, row0);
+      if (kUp) tma_load_2d(at + a_bytes, &maps.a1, full_bar(s), ks * kBK, row0);
+    };
+    auto tokens = [&](int s, int ks) {
+      tma_load_2d(ring + s * stage_bytes + kAcc * a_bytes, &maps.b, full_bar(s), ks * kBK, t0);
+    };
+    const int first = min(p.stages, ks1 - ks0);
+    if (leader) {
+      for (int s = 0; s < first; ++s) weights(s, ks0 + s);
+      // W_down does not depend on the launch before this one; h does
+      if (!kUp) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        fence_proxy_async_global();
+      }
+      for (int s = 0; s < first; ++s) tokens(s, ks0 + s);
+    }
+    __syncwarp();
+    int s = 0;
+    uint32_t phase = 0;
+    for (int ks = ks0 + first; ks < ks1; ++ks) {
+      if (!mbar_wait_warp(empty_bar(s), phase, ctl)) { ok = false; break; }
+      if (leader) {
+        weights(s, ks);
+        tokens(s, ks);
+      }
+      if (++s == p.stages) { s = 0; phase ^= 1u; }
+    }
+    if (!ok && lane == 0) {
+      // let copies already issued land before the CTA retires
+      const uint64_t w = global_timer_ns();
+      while (global_timer_ns() - w < 50000) nanosleep_ns(1000);
+    }
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    const bool leader = elect_one();
+    const uint32_t acc = warp_uniform(tmem_base);
+    const uint32_t id = idesc_bf16(128, kN, false, false);
+    int s = 0;
+    uint32_t phase = 0;
+    for (int ks = ks0; ks < ks1; ++ks) {
+      if (!mbar_wait_warp(full_bar(s), phase, ctl)) { ok = false; break; }
+      tc_fence_after();
+      const uint64_t da = sdesc_sw128(ring + s * stage_bytes, 16, 1024);
+      const uint64_t db = sdesc_sw128(ring + s * stage_bytes + kAcc * a_bytes, 16, 1024);
+      if (leader) {
+#pragma unroll
+        for (int kk = 0; kk < kBK / 16; ++kk) {
+          const uint32_t go = ks > ks0 || kk > 0 ? 1u : 0u;
+          umma_bf16(acc, da + 2 * kk, db + 2 * kk, id, go);
+          if (kUp) umma_bf16(acc + kN, da + (a_bytes >> 4) + 2 * kk, db + 2 * kk, id, go);
+        }
+        umma_commit(empty_bar(s));
+      }
+      if (++s == p.stages) { s = 0; phase ^= 1u; }
+    }
+    // every MMA issued above has completed before the accumulators are read or
+    // freed (a bounded wait that ignores the abort flag: it is for work in flight)
+    if (leader) umma_commit(done_bar);
+    volatile int keep_waiting = 0;
+    const uint64_t floor_ns = 200ull * 1000 * 1000;
+    const WaitCtl own{&keep_waiting, p.wait_limit_ns > floor_ns ? p.wait_limit_ns : floor_ns};
+    mbar_wait_warp(done_bar, 0, own);
+  } else {
+    // (the MMA warp commits to it in any case; its own waits are bounded)
+    ok = mbar_wait_warp(done_bar, 0, ctl);
+    tc_fence_after();
+  }
+
+  const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+  const int row = (warp & 3) * 32 + lane;
+  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
+  // one result from its sums
+  auto store = [&](float a, float b, int t, int n) {
+    const size_t at = static_cast<size_t>(t0 + t) * p.rows_all + n;
+    if (kUp) {
+      out[at] = __float2bfloat16_rn(activate<kAct>(a) * b);
+      if (p.saved_g) {
+        p.saved_g[at] = static_cast<uint16_t>(saved_bits(a));
+        p.saved_u[at] = static_cast<uint16_t>(saved_bits(b));
+      }
+    } else {
+      out[at] = __float2bfloat16_rn(p.residual ? a + __bfloat162float(p.residual[at]) : a);
+    }
+  };
+  if (c == 1) {
+    if (warp < kEpiWarps && ok && (warp & 3) * 32 < p.rows) {
+      const int n = row0 + row;
+      const bool mine = row < p.rows && n < p.rows_all;
+#pragma unroll 1
+      for (int t = 0; t < nt; t += 16) {
+        uint32_t a[16], b[16];
+        tmem_ld_32x32b_x16(lane_addr + t, a);
+        if (kUp) tmem_ld_32x32b_x16(lane_addr + kN + t, b);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (mine && t + i < nt) store(__uint_as_float(a[i]), kUp ? __uint_as_float(b[i]) : 0.f, t + i, n);
+      }
+    }
+  } else {
+    // CTA q of the cluster finishes tokens [q per, (q + 1) per): every CTA sends
+    // it its sums of them, recv[sender][token][accumulator][row]
+    const int per = (nt + c - 1) / c;
+    cluster_sync_all();  // all MMAs of the cluster are done: the stages are free
+    if (warp < kEpiWarps && ok && (warp & 3) * 32 < p.rows) {
+#pragma unroll 1
+      for (int t = 0; t < nt; t += 16) {
+        uint32_t a[16], b[16];
+        tmem_ld_32x32b_x16(lane_addr + t, a);
+        if (kUp) tmem_ld_32x32b_x16(lane_addr + kN + t, b);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if (t + i >= nt || row >= p.rows) continue;
+          const int q = (t + i) / per, j = t + i - q * per;
+          const uint32_t at = ring + 4u * (((rank * per + j) * kAcc) * p.rows + row);
+          st_shared_cluster(map_shared(at, q), a[i]);
+          if (kUp) st_shared_cluster(map_shared(at + 4u * p.rows, q), b[i]);
+        }
+      }
+    }
+    cluster_sync_all();
+    const int my = max(0, min(per, nt - rank * per));
+    for (int i = threadIdx.x; i < my * p.rows; i += kThreads) {
+      const int j = i / p.rows, r = i - j * p.rows;
+      if (row0 + r >= p.rows_all) continue;
+      float a = 0.f, b = 0.f;
+      for (int q = 0; q < c; ++q) {
+        const float* f = recv + ((q * per + j) * kAcc) * p.rows + r;
+        a += f[0];
+        if (kUp) b += f[p.rows];
+      }
+      store(a, b, rank * per + j, row0 + r);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag && p.dev_status) atomicOr(p.dev_status, 1 << OLIVE_ERR_TIMEOUT);
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, kCols);
+  }
+}
+
+// Weight rows of a CTA and CTAs of a cluster for `rows_all` rows, `ks` K steps
+// and `tiles` tiles of n tokens.
+struct FewShape {
+  int rows, c;
+};
+FewShape few_shape(int rows_all, int ks, int tiles, int n, int sms, bool up) {
+  const int slots = n <= 64 ? 2 * sms : sms;  // CTAs that run at once
+  const int most = up && n <= 64 ? 64 : 128;
+  // as many rows as leave one CTA for every slot, at least 32 (8 KB of TMA a step)
+  FewShape s{static_cast<int>(align_up(std::max<int64_t>(1, ceil_div(static_cast<int64_t>(rows_all) * tiles, slots)), 8)), 1};
+  s.rows = std::min(most, std::max(s.rows, 32));
+  const auto ctas = [&] { return ceil_div(rows_all, s.rows) * s.c * tiles; };
+  // shared K steps where that leaves slots empty: wider tiles, several CTAs each
+  while (s.c < 8 && 2 * ctas() <= slots && ks >= 8 * s.c) s.c *= 2;
+  return s;
+}
+
+template <bool kUp, int kN, int kAct>
+olive_status launch_few(const Ctx& c, const FewMaps& maps, FewParams p, const FewShape& s) {
+  constexpr int kAcc = kUp ? 2 : 1;
+  const int stage = kAcc * p.rows * 128 + kN * 128;
+  // the MMAs read 128 rows from the last stage's last A
+  const int past = std::max(0, (kAcc - 1) * p.rows * 128 + kTile - stage);
+  const int ks = static_cast<int>(ceil_div(ceil_div(p.K, kBK), s.c));
+  p.stages = std::min({(budget(kN) - 1024 - past) / stage, kMaxStages, ks});
+  const int exchange = s.c > 1 ? 4 * kAcc * p.rows * s.c * static_cast<int>(ceil_div(kN, s.c)) : 0;
+  const int smem = 1024 + std::max(p.stages * stage + past, exchange);
+  p.wait_limit_ns = c.wait_limit_ns;
+  static std::atomic<int> done[kMaxDevices];
+  if (!set_smem_once(reinterpret_cast<const void*>(few_kernel<kUp, kN, kAct>), 227 * 1024, c.device, done))
+    return OLIVE_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(ceil_div(p.rows_all, p.rows) * s.c), static_cast<unsigned>(ceil_div(p.T, kN)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = s.c;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = kUp ? 1 : 2;  // (only the second launch may start before the one ahead of it ends)
+  if (cudaLaunchKernelEx(&cfg, few_kernel<kUp, kN, kAct>, maps, p) != cudaSuccess) {
+    cudaGetLastError();
+    return OLIVE_ERR_CUDA;
+  }
+  return OLIVE_OK;
+}
+
+template <bool kUp, int kAct>
+olive_status by_tokens(const Ctx& c, const FewMaps& maps, const FewParams& p, int n, const FewShape& s) {
+  switch (n) {
+    case 16: return launch_few<kUp, 16, kAct>(c, maps, p, s);
+    case 32: return launch_few<kUp, 32, kAct>(c, maps, p, s);
+    case 64: return launch_few<kUp, 64, kAct>(c, maps, p, s);
+    default: return launch_few<kUp, 128, kAct>(c, maps, p, s);
+  }
+}
+
+}  // namespace
+
+olive_status launch_mlp_few(const Ctx& c, const void* x, const void* W_gate, const void* W_up,
+                            const void* W_down, const void* residual, int32_t T, int32_t d,
+                            int32_t f, int act, void* y, void* saved, void* h,
+                            int32_t* dev_status) {
+  const int n = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
+  const int tiles = static_cast<int>(ceil_div(T, n));
+  FewMaps m = {};
+  FewParams p = {};
+  p.T = T;
+  p.dev_status = dev_status;
+
+  FewShape s = few_shape(f, static_cast<int>(ceil_div(d, kBK)), tiles, n, c.num_sms, true);
+  p.rows_all = f;
+  p.K = d;
+  p.rows = s.rows;
+  p.out = h;
+  p.saved_g = static_cast<uint16_t*>(saved);
+  p.saved_u = saved ? p.saved_g + static_cast<size_t>(T) * f : nullptr;
+  if (!encode_bf16_2d(&m.a0, W_gate, d, f, 2ull * d, kBK, s.rows) ||
+      !encode_bf16_2d(&m.a1, W_up, d, f, 2ull * d, kBK, s.rows) ||
+      !encode_bf16_2d(&m.b, x, d, T, 2ull * d, kBK, n))
+    return OLIVE_ERR_CUDA;
+  const olive_status st = act == OLIVE_ACT_SILU ? by_tokens<true, OLIVE_ACT_SILU>(c, m, p, n, s)
+                                                : by_tokens<true, OLIVE_ACT_GELU_TANH>(c, m, p, n, s);
+  if (st != OLIVE_OK) return st;
+
+  s = few_shape(d, static_cast<int>(ceil_div(f, kBK)), tiles, n, c.num_sms, false);
+  p.rows_all = d;
+  p.K = f;
+  p.rows = s.rows;
+  p.out = y;
+  p.residual = static_cast<const __nv_bfloat16*>(residual);
+  p.saved_g = p.saved_u = nullptr;
+  if (!encode_bf16_2d(&m.a0, W_down, f, d, 2ull * f, kBK, s.rows) ||
+      !encode_bf16_2d(&m.b, h, f, T, 2ull * f, kBK, n))
+    return OLIVE_ERR_CUDA;
+  return by_tokens<false, 0>(c, m, p, n, s);
+}
+
+}  // namespace olive

@@ -55,9 +55,9 @@ bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t
 bool encode_bf16_2d_plain(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                           uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer);
 
-// The same for fp32 with 128-byte swizzle.
-bool encode_f32_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
-                   uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer);
+// A dense bf16 or fp32 result: boxes of 64 bytes x box_outer rows, 64-byte swizzle.
+bool encode_out_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, bool f32,
+                   uint32_t box_outer);
 
 // Rows of the G slab used by the backward passes for vocabulary size V.
 int64_t slab_rows(int64_t Tpad, int64_t V);
@@ -377,6 +377,12 @@ MlpWs carve_mlp(void* ws, int64_t T, int64_t f, bool bwd);
 olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, const void* W_up,
                             const void* W_down, const void* residual, int32_t T, int32_t d,
                             int32_t f, int act, void* y, void* saved, void* ws,
+                            int32_t* dev_status);
+// The forward on few rows (gated_mlp_few.cu); h: workspace [T, f].
+constexpr int kMlpFewRows = 128;
+olive_status launch_mlp_few(const Ctx& c, const void* x, const void* W_gate, const void* W_up,
+                            const void* W_down, const void* residual, int32_t T, int32_t d,
+                            int32_t f, int act, void* y, void* saved, void* h,
                             int32_t* dev_status);
 olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const void* W_gate,
                             const void* W_up, const void* W_down, const void* saved, int32_t T,

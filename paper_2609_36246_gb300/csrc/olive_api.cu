@@ -103,10 +103,11 @@ bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t
                    box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-bool encode_f32_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
-                   uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer) {
-  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, base, inner, outer, row_bytes, box_inner,
-                   box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
+bool encode_out_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, bool f32,
+                   uint32_t box_outer) {
+  const uint32_t elt = f32 ? 4 : 2;
+  return encode_2d(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base,
+                   inner, outer, elt * inner, 64 / elt, box_outer, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 bool encode_bf16_2d_plain(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
