@@ -11,9 +11,9 @@
 //   MM_GRADS  the four products that are left, in one launch
 //
 // CTA pairs (clusters of two, tcgen05.mma.cta_group::2, M = 256): each CTA
-// stages its 128 rows of A and its half of the 256-wide B, 32 KB per 64-deep K
-// step, and receives its 128 x 256 fp32 accumulator in its own TMEM, twice, so
-// that the epilogue of a tile runs under the next tile's MMAs.  An operand is
+// stages its 128 rows of A and its half of the B rows (256 or 128 wide tiles), and
+// receives its 128 rows of the fp32 accumulator in its own TMEM, twice, so that
+// the epilogue of a tile runs under the next tile's MMAs.  An operand is
 // read K-major or MN-major as it lies in memory; nothing is transposed or
 // copied.  Output tiles leave through shared memory by TMA, which also cuts the
 // ragged edges off.
@@ -32,26 +32,31 @@ namespace olive {
 namespace {
 
 constexpr int kBM = 128;             // rows of a CTA's tile
-constexpr int kBN = 256;             // columns of a tile (128 of g and 128 of u in MM_UP)
+constexpr int kWide = 256, kNarrow = 128;  // columns of a tile (half of them g, half u in MM_UP)
 constexpr int kBK = 64;
-constexpr int kSA = kBM * kBK * 2;   // this CTA's 128 rows of A, or its half of B
-constexpr int kStageBytes = 2 * kSA;
+constexpr int kSA = kBM * kBK * 2;   // this CTA's 128 rows of A
 constexpr int kEpiWarps = 8;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 32 * 10;
 constexpr int kOutBuf = 32 * 64;     // a warp's 32 rows of 64 bytes
+constexpr int kSlots = 8;            // a finisher warp's pieces in flight
+constexpr int kSlotBytes = 16 * 32 * 4;
 enum { MM_UP = 0, MM_DOWN = 1, MM_DH = 2, MM_GRADS = 3 };
 // Three output buffers a warp where a tile gives three results, else two in turn.
-template <int kMode>
+template <int kMode, int kBN>
 struct Layout {
   static constexpr bool kThree = kMode == MM_UP || kMode == MM_DH;
   static constexpr int kOutBufs = kThree ? 3 : 2;
-  static constexpr int kStages = kThree ? 5 : 6;
+  static constexpr int kSB = kBN / 2 * kBK * 2;  // this CTA's half of B
+  static constexpr int kStageBytes = kSA + kSB;
+  static constexpr int kStages = kBN == kNarrow ? 7 : kThree ? 5 : 6;
   static constexpr int kOut = kStages * kStageBytes;
   static constexpr int kBars = kOut + kEpiWarps * kOutBufs * kOutBuf;
-  static constexpr int kMisc = kBars + 8 * (2 * kStages + 5);
+  static constexpr int kBarCount = 2 * kStages + 5 + kEpiWarps * kSlots;
+  static constexpr int kMisc = kBars + 8 * kBarCount;
   static constexpr int kSmem = kMisc + 64;
   static_assert(kSmem <= 227 * 1024, "shared memory budget");
+  static_assert(kEpiWarps * kSlots * kSlotBytes <= kStages * kStageBytes, "pieces pass through the stages");
 };
 constexpr int kRaster = 8;           // row tiles of a raster group (L2 reuse)
 constexpr int kMaxProbs = 4;
@@ -88,7 +93,7 @@ struct MlpParams {
   int n_prob;
   int n_maps;
   MlpSplit cut;
-  float* part;             // [pairs][2 CTAs][8 warps][128 columns][32 rows] partial accumulators
+  float* part;             // [pairs][2 CTAs][8 warps][kBN / 2 columns][32 rows] partial accumulators
   uint32_t* flag;          // [pairs][2 CTAs] warps that have stored theirs
   uint32_t* clear;         // words the next launch of the call wants zero
   int n_clear;
@@ -174,11 +179,19 @@ __device__ __forceinline__ uint32_t out_piece(uint32_t buf, int lane, int c) {
   return buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4);
 }
 
-template <int kMode, int kAct>
+// Untiled bulk copy global -> shared, completion counted on the mbarrier.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+      : "memory");
+}
+
+template <int kMode, int kAct, int kBN>
 __global__ void __launch_bounds__(kThreads, 1)
     mlp_gemm_kernel(const __grid_constant__ MlpMaps maps, const __grid_constant__ MlpParams p) {
-  using L = Layout<kMode>;
-  constexpr int kStages = L::kStages;
+  using L = Layout<kMode, kBN>;
+  constexpr int kStages = L::kStages, kStageBytes = L::kStageBytes;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
   const uint32_t stages = base;
@@ -206,12 +219,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(tempty(b), 2 * kEpiWarps);  // the epilogue warps of both CTAs
     }
     mbar_init(drain, 1);
+    for (int i = 0; i < kEpiWarps * kSlots; ++i) mbar_init(drain + 8u * (1 + i), 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
   if (warp == kProducerWarp && lane < p.n_maps) tma_prefetch_desc(&maps.m[lane]);
   if (warp == kMmaWarp) {
-    tmem_alloc_pair(smem_u32(tmem_slot), 512);
+    tmem_alloc_pair(smem_u32(tmem_slot), 2 * kBN);
     tmem_relinquish_pair();
   }
   if (blockIdx.x == 0)
@@ -233,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const MlpProb& q = p.pr[u.prob];
       const int mrow = u.m0 + static_cast<int>(rank) * kBM;
       // MM_UP: the even CTA holds the tile's rows of Wg, the odd one those of Wu
-      const int nrow = kMode == MM_UP ? u.n0 * kBM : u.n0 * kBN + static_cast<int>(rank) * kBM;
+      const int nrow = kMode == MM_UP ? u.n0 * (kBN / 2) : u.n0 * kBN + static_cast<int>(rank) * (kBN / 2);
       for (int ks = u.k0; ks < u.k1; ++ks) {
         if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, ctl)) { ok = false; break; }
         const uint32_t sA = stages + stage * kStageBytes;
@@ -252,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (kMode == MM_GRADS || kMode == MM_DH) {
             tma_load_2d_pair(sA + kSA, mb, fb, nrow, k);
-            tma_load_2d_pair(sA + kSA + kSA / 2, mb, fb, nrow + 64, k);
+            if (kBN == kWide) tma_load_2d_pair(sA + kSA + L::kSB / 2, mb, fb, nrow + 64, k);
           } else {
             tma_load_2d_pair(sA + kSA, mb, fb, k, nrow);
           }
@@ -279,8 +293,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t id = idesc_bf16(2 * kBM, kBN, a_mn, b_mn);
         // K-major: 16 K elements are 32 bytes along the swizzled row; MN-major:
         // 16 rows of 128 bytes, 64-element blocks 8 KB apart
-        const uint64_t dA = sdesc_sw128(stages, a_mn ? kSA / 2 : 16, 1024);
-        const uint64_t dB = sdesc_sw128(stages + kSA, b_mn ? kSA / 2 : 16, 1024);
+        const uint64_t dA = sdesc_sw128(stages, a_mn ? 64 * kBK * 2 : 16, 1024);
+        const uint64_t dB = sdesc_sw128(stages + kSA, b_mn ? 64 * kBK * 2 : 16, 1024);
         const uint32_t stepA = a_mn ? 128 : 2, stepB = b_mn ? 128 : 2;
         const int b = n & 1;
         if (!mbar_wait_warp(tempty(b), ((n >> 1) & 1) ^ 1, ctl)) { ok = false; break; }
@@ -328,12 +342,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t acc = lane_addr + b * kBN;
       const int y = u.m0 + static_cast<int>(rank) * kBM + (warp & 3) * 32;  // the warp's first row
       const int t = y + lane;
-      const int x0 = kMode == MM_UP ? u.n0 * kBM + half * 64 : u.n0 * kBN + half * 128;
-      constexpr int kSteps = kMode == MM_UP ? 4 : 8;  // of 16 result columns
-      // TMEM column of step s (MM_UP: g; u is 128 columns on)
-      auto col = [&](int s) { return half * (kMode == MM_UP ? 64 : 128) + s * 16; };
+      constexpr int kCols = kMode == MM_UP ? kBN / 2 : kBN;  // result columns of a tile
+      constexpr int kSteps = kCols / 32;                     // of 16 columns, this warp's half
+      const int x0 = u.n0 * kCols + half * (kCols / 2);
+      // TMEM column of step s (MM_UP: g; u is kBN / 2 columns on)
+      auto col = [&](int s) { return half * (kCols / 2) + s * 16; };
+      // this warp's part of a pair's partial accumulator: [kBN / 32 steps][16 columns][32 rows]
       auto part_of = [&](int pr) {
-        return p.part + (static_cast<size_t>(pr * 2 + static_cast<int>(rank)) * kEpiWarps + warp) * (128 * 32) + lane;
+        return p.part + (static_cast<size_t>(pr * 2 + static_cast<int>(rank)) * kEpiWarps + warp) * (kBN / 2 * 32);
       };
       auto release = [&] {
         tc_fence_before();
@@ -364,11 +380,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 
       if (!whole) {
         // a piece of a tile that another pair finishes
-        float* to = part_of(pair);
+        float* to = part_of(pair) + lane;
 #pragma unroll 1
-        for (int s = 0; s < 8; ++s) {
+        for (int s = 0; s < kBN / 32; ++s) {
           uint32_t r[16];
-          tmem_ld_32x32b_x16(acc + (kMode == MM_UP ? (s >> 2) * 128 + col(s & 3) : col(s)), r);
+          tmem_ld_32x32b_x16(acc + (kMode == MM_UP ? s / kSteps * (kBN / 2) + col(s % kSteps) : col(s)), r);
           tmem_ld_wait();
 #pragma unroll
           for (int i = 0; i < 16; ++i) __stcg(to + (s * 16 + i) * 32, __uint_as_float(r[i]));
@@ -379,19 +395,48 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) red_release_add(p.flag + pair * 2 + rank, 1u);
         continue;
       }
-      if (u.from < pair) {
+      // A tile that is finished from pieces is the pair's last unit: its MMAs are
+      // done, so the pieces pass through the stages, kSlots steps of them in flight
+      // (plain loads held 16 KB in flight and took 8 us a 128 KB piece).  Step i of
+      // the sequence is columns step_of(i / pieces) of pair u.from + i % pieces.
+      const int pieces = pair - u.from;
+      constexpr int kAll = kBN / 32;
+      auto step_of = [&](int k) { return kMode == MM_UP ? (k & 1) * kSteps + (k >> 1) : k; };
+      const uint32_t slot0 = stages + warp * (kSlots * kSlotBytes);
+      const uint32_t slot_bar = drain + 8u * (1 + warp * kSlots);
+      auto request = [&](int i) {
+        if (lane == 0 && i < kAll * pieces) {
+          const uint32_t bar = slot_bar + 8u * (i % kSlots);
+          mbar_arrive_expect_tx(bar, kSlotBytes);
+          bulk_load(slot0 + i % kSlots * kSlotBytes,
+                    part_of(u.from + i % pieces) + step_of(i / pieces) * (16 * 32), kSlotBytes, bar);
+        }
+      };
+      int taken = 0;
+      if (pieces > 0) {
         for (int o = u.from; ok && o < pair; ++o) ok = wait_counter(p.flag + o * 2 + rank, kEpiWarps, ctl);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
+        fence_proxy_async_global();
+        for (int i = 0; i < kSlots; ++i) request(i);
       }
-      // step s of the finished accumulator: the pair's own sum and the pieces'
-      auto load = [&](int tcol, int s, uint32_t(&r)[16]) {
+      // the next 16 columns of the finished accumulator: the pair's own sum and the pieces'
+      auto load = [&](int tcol, uint32_t(&r)[16]) {
         tmem_ld_32x32b_x16(acc + tcol, r);
         tmem_ld_wait();
-        for (int o = u.from; o < pair; ++o) {
-          const float* f = part_of(o) + s * 16 * 32;
+        for (int o = 0; o < pieces; ++o, ++taken) {
+          const int slot = taken % kSlots;
+          ok = ok && mbar_wait_warp(slot_bar + 8u * slot, (taken / kSlots) & 1, ctl);
+          if (!ok) return;
+          const uint32_t f = slot0 + slot * kSlotBytes + 4 * lane;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __ldcg(f + i * 32));
+          for (int i = 0; i < 16; ++i) {
+            float v;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(f + i * 128) : "memory");
+            r[i] = __float_as_uint(__uint_as_float(r[i]) + v);
+          }
+          __syncwarp();
+          request(taken + kSlots);
         }
       };
       const bool inside = y < q.M;
@@ -403,8 +448,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool f32 = kMode == MM_GRADS && p.out_f32;
         const bool opens = f32 || (s & 1) == 0, closes = f32 || (s & 1) == 1;
         uint32_t r[16], v[16];
-        load(col(s), s, r);
-        if constexpr (kMode == MM_UP) load(128 + col(s), 4 + s, v);
+        load(col(s), r);
+        if constexpr (kMode == MM_UP) load(kBN / 2 + col(s), v);
+        if (!ok) break;
         if (s == kSteps - 1) release();
         uint32_t buf = out0;
         if (opens) {
@@ -522,6 +568,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     if (lane == 0) bulk_wait();
+    if (!ok && lane == 0) {
+      const uint64_t t0 = global_timer_ns();  // pieces in flight land
+      while (global_timer_ns() - t0 < 50000) nanosleep_ns(1000);
+    }
     __syncwarp();
   }
 
@@ -532,120 +582,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0 && *abort_flag && p.dev_status) atomicOr(p.dev_status, kStatusTimeout);
   if (warp == kMmaWarp) {
     tc_fence_after();
-    tmem_dealloc_pair(tmem_base, 512);
+    tmem_dealloc_pair(tmem_base, 2 * kBN);
   }
 }
 
 // ------------------------------------------------------------------- host ---
-
-// Pairs of CTAs the device holds at once (at most one for two SMs): runs of cut
-// tiles wait for one another, so the grid is never larger.
-template <int kMode, int kAct>
-int resident_pairs(const Ctx& c) {
-  static std::atomic<int> held[kMaxDevices];
-  const bool cached = c.device >= 0 && c.device < kMaxDevices;
-  int n = cached ? held[c.device].load(std::memory_order_acquire) - 1 : -1;
-  if (n >= 0) return n;
-  static std::atomic<int> done[kMaxDevices];
-  if (!set_smem_once(reinterpret_cast<const void*>(mlp_gemm_kernel<kMode, kAct>), Layout<kMode>::kSmem, c.device, done)) return 0;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * (c.num_sms / 2));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Layout<kMode>::kSmem;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, mlp_gemm_kernel<kMode, kAct>, &cfg) != cudaSuccess) {
-    cudaGetLastError();
-    return 0;
-  }
-  n = std::min({n, c.num_sms / 2, kMlpMaxPairs});
-  if (cached) held[c.device].store(n + 1, std::memory_order_release);
-  return n;
-}
-
-// Deals the tiles to `pairs` pairs, whole ones or cut, whichever ends sooner; a
-// cut costs each pair the store of one partial accumulator, and its finisher the
-// wait for the others and their loads: about kCutCost K steps.  Returns the
-// pairs to launch.
-constexpr int kCutCost = 14;
-constexpr int kMinRun = 4;
-int plan(MlpParams& p, int pairs) {
-  MlpSplit& s = p.cut;
-  s = MlpSplit{};
-  s.run = 1;
-  // whole tiles, in turn: the pair with the most steps
-  int tiles[kMaxProbs], all = 0;
-  int64_t whole_end = 0;
-  for (int i = 0; i < p.n_prob; ++i) {
-    tiles[i] = p.pr[i].mt * p.pr[i].nt;
-    all += tiles[i];
-  }
-  for (int r = 0; r < std::min(pairs, all); ++r) {
-    int64_t load = 0;
-    int first = 0;
-    for (int i = 0; i < p.n_prob; first += tiles[i++]) {
-      const int skip = ((r - first) % pairs + pairs) % pairs;  // to this pair's first tile of the product
-      if (skip < tiles[i]) load += static_cast<int64_t>(ceil_div(tiles[i] - skip, pairs)) * p.pr[i].ks;
-    }
-    whole_end = std::max(whole_end, load);
-  }
-  // every product's last tiles cut
-  int64_t cut_end = 0;
-  int steps = 0;
-  for (int i = 0; i < p.n_prob; ++i) {
-    const int rest = tiles[i] % pairs;
-    s.whole[i] = tiles[i] - rest;
-    s.off[i] = steps;
-    steps += rest * p.pr[i].ks;
-    cut_end += static_cast<int64_t>(s.whole[i] / pairs) * p.pr[i].ks;
-  }
-  const int run = std::max(kMinRun, static_cast<int>(ceil_div(steps, pairs)));
-  if (steps > 0 && cut_end + run + kCutCost < whole_end) {
-    for (int i = 0; i < p.n_prob; ++i) s.n_whole += s.whole[i];
-    s.steps = steps;
-    s.run = run;
-    return s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, run));
-  }
-  for (int i = 0; i < p.n_prob; ++i) s.whole[i] = tiles[i];
-  s.n_whole = all;
-  return std::min(pairs, all);
-}
-
-// `zeroed`: an earlier launch of the call clears this one's flags.
-template <int kMode, int kAct = 0>
-olive_status launch(const Ctx& c, const MlpMaps& maps, MlpParams& p, bool zeroed) {
-  int pairs = resident_pairs<kMode, kAct>(c);
-  if (pairs < 1) return OLIVE_ERR_UNSUPPORTED_DEVICE;
-  pairs = plan(p, pairs);
-  if (p.cut.steps > 0 && !zeroed &&
-      cudaMemsetAsync(p.flag, 0, 4 * mlp_flag_words(), c.stream) != cudaSuccess) {
-    cudaGetLastError();
-    return OLIVE_ERR_CUDA;
-  }
-  p.wait_limit_ns = c.wait_limit_ns;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(2 * pairs);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Layout<kMode>::kSmem;
-  cfg.stream = c.stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, mlp_gemm_kernel<kMode, kAct>, maps, p) != cudaSuccess) {
-    cudaGetLastError();
-    return OLIVE_ERR_CUDA;
-  }
-  return OLIVE_OK;
-}
 
 // Collects a launch's tensor maps.
 struct MapSet {
@@ -656,9 +597,9 @@ struct MapSet {
     ok = ok && good;
     return static_cast<int16_t>(n++);
   }
-  // operand [rows, cols] bf16 with K along the columns: boxes of 128 rows x 64
-  int16_t k_major(const void* a, int64_t rows, int64_t cols) {
-    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, kBK, kBM));
+  // operand [rows, cols] bf16 with K along the columns: boxes of `box` rows x 64
+  int16_t k_major(const void* a, int64_t rows, int64_t cols, int box) {
+    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, kBK, box));
   }
   // operand [rows, cols] bf16 with K along the rows: boxes of 64 rows x 64
   int16_t mn_major(const void* a, int64_t rows, int64_t cols) {
@@ -670,12 +611,153 @@ struct MapSet {
   }
 };
 
-MlpProb problem(int M, int N, int n_tile, int K, int halves) {
+// Pairs of CTAs the device holds at once (at most one for two SMs): runs of cut
+// tiles wait for one another, so the grid is never larger.
+template <int kMode, int kAct, int kBN>
+int resident_pairs(const Ctx& c) {
+  static std::atomic<int> held[kMaxDevices];
+  const bool cached = c.device >= 0 && c.device < kMaxDevices;
+  int n = cached ? held[c.device].load(std::memory_order_acquire) - 1 : -1;
+  if (n >= 0) return n;
+  static std::atomic<int> done[kMaxDevices];
+  constexpr int kSmem = Layout<kMode, kBN>::kSmem;
+  if (!set_smem_once(reinterpret_cast<const void*>(mlp_gemm_kernel<kMode, kAct, kBN>), kSmem, c.device, done)) return 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (c.num_sms / 2));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, mlp_gemm_kernel<kMode, kAct, kBN>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  n = std::min({n, c.num_sms / 2, kMlpMaxPairs});
+  if (cached) held[c.device].store(n + 1, std::memory_order_release);
+  return n;
+}
+
+// How a launch is cut up: tile width, tiles dealt whole or cut, pairs.
+struct Plan {
+  int bn, pairs;
+  MlpSplit cut;
+  double ns;  // estimate
+};
+
+// The estimate's terms, ns, by tile width: a K step of a pair, a tile's epilogue
+// (seen once, at the end), the store of a piece and the wait for it, and each
+// piece that a finisher adds.
+struct Cost {
+  double step, tail, cut, piece;
+};
+constexpr Cost kCostWide{290, 4500, 2500, 1800}, kCostNarrow{165, 2600, 2000, 1000};
+
+// Deals the tiles to the pairs, whole ones or every product's last ones cut, by
+// what is estimated to end first.
+Plan plan_tiles(const MlpParams& p, bool up, int bn, int pairs) {
+  const Cost& k = bn == kWide ? kCostWide : kCostNarrow;
+  const int cols = up ? bn / 2 : bn;
+  int tiles[kMaxProbs], all = 0, longest = 0;
+  for (int i = 0; i < p.n_prob; ++i) {
+    tiles[i] = p.pr[i].mt * static_cast<int>(ceil_div(p.pr[i].N, cols));
+    all += tiles[i];
+    longest = std::max(longest, p.pr[i].ks);
+  }
+  Plan w{bn, std::min(pairs, all), {}, 0};
+  w.cut.run = 1;
+  // whole, in turn: the pair with the most steps
+  int64_t most = 0;
+  for (int r = 0; r < w.pairs; ++r) {
+    int64_t load = 0;
+    int first = 0;
+    for (int i = 0; i < p.n_prob; first += tiles[i++]) {
+      const int skip = ((r - first) % pairs + pairs) % pairs;  // to this pair's first tile of the product
+      if (skip < tiles[i]) load += ceil_div(tiles[i] - skip, pairs) * p.pr[i].ks;
+    }
+    most = std::max(most, load);
+  }
+  for (int i = 0; i < p.n_prob; ++i) w.cut.whole[i] = tiles[i];
+  w.cut.n_whole = all;
+  w.ns = most * k.step + k.tail;
+  // every product's last tiles cut
+  MlpSplit s = {};
+  int64_t before = 0, steps = 0;
+  for (int i = 0; i < p.n_prob; ++i) {
+    const int rest = tiles[i] % pairs;
+    s.whole[i] = tiles[i] - rest;
+    s.n_whole += s.whole[i];
+    s.off[i] = static_cast<int>(steps);
+    steps += static_cast<int64_t>(rest) * p.pr[i].ks;
+    before += static_cast<int64_t>(s.whole[i] / pairs) * p.pr[i].ks;
+  }
+  if (steps == 0 || steps > (1 << 30)) return w;
+  s.steps = static_cast<int>(steps);
+  for (int m = 1; m <= 8; ++m) {  // longer runs on fewer pairs: fewer pieces
+    s.run = static_cast<int>(ceil_div(steps * m, pairs));
+    const double pieces = static_cast<double>(longest) / s.run;
+    const double ns = (before + s.run) * k.step + k.tail + k.cut + k.piece * pieces;
+    if (ns < w.ns) w = Plan{bn, s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, s.run)), s, ns};
+  }
+  return w;
+}
+
+// `zeroed`: an earlier launch of the call clears this one's flags.
+template <int kMode, int kAct, int kBN>
+olive_status launch_tiles(const Ctx& c, const MlpMaps& maps, MlpParams& p, const Plan& plan, bool zeroed) {
+  p.cut = plan.cut;
+  for (int i = 0; i < p.n_prob; ++i)
+    p.pr[i].nt = static_cast<int>(ceil_div(p.pr[i].N, kMode == MM_UP ? kBN / 2 : kBN));
+  if (p.cut.steps > 0 && !zeroed &&
+      cudaMemsetAsync(p.flag, 0, 4 * mlp_flag_words(), c.stream) != cudaSuccess) {
+    cudaGetLastError();
+    return OLIVE_ERR_CUDA;
+  }
+  p.wait_limit_ns = c.wait_limit_ns;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * plan.pairs);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Layout<kMode, kBN>::kSmem;
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, mlp_gemm_kernel<kMode, kAct, kBN>, maps, p) != cudaSuccess) {
+    cudaGetLastError();
+    return OLIVE_ERR_CUDA;
+  }
+  return OLIVE_OK;
+}
+
+// `fill(bn)` sets the launch's tensor maps for tiles of bn columns.
+template <int kMode, int kAct = 0, class Fill>
+olive_status launch(const Ctx& c, MlpParams& p, bool zeroed, Fill&& fill) {
+  const int pairs = std::min(resident_pairs<kMode, kAct, kWide>(c), resident_pairs<kMode, kAct, kNarrow>(c));
+  if (pairs < 1) return OLIVE_ERR_UNSUPPORTED_DEVICE;
+  const Plan wide = plan_tiles(p, kMode == MM_UP, kWide, pairs);
+  const Plan narrow = plan_tiles(p, kMode == MM_UP, kNarrow, pairs);
+  const bool w = wide.ns <= narrow.ns;
+  MapSet s;
+  fill(s, w ? kWide : kNarrow);
+  if (!s.ok) return OLIVE_ERR_CUDA;
+  p.n_maps = s.n;
+  return w ? launch_tiles<kMode, kAct, kWide>(c, s.maps, p, wide, zeroed)
+           : launch_tiles<kMode, kAct, kNarrow>(c, s.maps, p, narrow, zeroed);
+}
+
+MlpProb problem(int M, int N, int K, int halves) {
   MlpProb q = {};
   q.M = M;
   q.N = N;
   q.mt = static_cast<int>(ceil_div(M, 2 * kBM));
-  q.nt = static_cast<int>(ceil_div(N, n_tile));
   q.ks_half = static_cast<int>(ceil_div(K, kBK));
   q.ks = halves * q.ks_half;
   return q;
@@ -683,7 +765,7 @@ MlpProb problem(int M, int N, int n_tile, int K, int halves) {
 
 }  // namespace
 
-size_t mlp_part_bytes() { return 4ull * kMlpMaxPairs * 2 * kEpiWarps * 128 * 32; }
+size_t mlp_part_bytes() { return 4ull * kMlpMaxPairs * 2 * kEpiWarps * (kWide / 2 * 32); }
 size_t mlp_flag_words() { return 2ull * kMlpMaxPairs; }
 
 olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, const void* W_up,
@@ -693,49 +775,41 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
   const MlpWs w = carve_mlp(ws, T, f, false);
   if (T <= kMlpFewRows)
     return launch_mlp_few(c, x, W_gate, W_up, W_down, residual, T, d, f, act, y, saved, w.h, dev_status);
-  uint16_t* sg = static_cast<uint16_t*>(saved);
-  uint16_t* su = saved ? sg + static_cast<size_t>(T) * f : nullptr;
-  {
-    MapSet s;
-    MlpParams p = {};
-    MlpProb q = problem(T, f, kBM, d, 1);
-    q.a0 = q.a1 = s.k_major(x, T, d);
-    q.b0 = s.k_major(W_gate, f, d);
-    q.b1 = s.k_major(W_up, f, d);
+  MlpParams p = {};
+  p.n_prob = 1;
+  p.part = w.part;
+  p.dev_status = dev_status;
+
+  p.pr[0] = problem(T, f, d, 1);
+  p.flag = w.flag;
+  p.clear = w.flag + mlp_flag_words();
+  p.n_clear = static_cast<int>(mlp_flag_words());
+  p.save = saved != nullptr;
+  auto up = [&](MapSet& s, int bn) {
+    MlpProb& q = p.pr[0];
+    q.a0 = q.a1 = s.k_major(x, T, d, kBM);
+    q.b0 = s.k_major(W_gate, f, d, bn / 2);
+    q.b1 = s.k_major(W_up, f, d, bn / 2);
     q.out = s.output(w.h, T, f, false);
     if (saved) {
-      p.map_g = s.output(sg, T, f, false);
-      p.map_u = s.output(su, T, f, false);
+      p.map_g = s.output(saved, T, f, false);
+      p.map_u = s.output(static_cast<uint16_t*>(saved) + static_cast<size_t>(T) * f, T, f, false);
     }
-    if (!s.ok) return OLIVE_ERR_CUDA;
-    p.pr[0] = q;
-    p.n_prob = 1;
-  p.n_maps = s.n;
-    p.save = saved != nullptr;
-    p.part = w.part;
-    p.flag = w.flag;
-    p.clear = w.flag + mlp_flag_words();
-    p.n_clear = static_cast<int>(mlp_flag_words());
-    p.dev_status = dev_status;
-    const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_UP, OLIVE_ACT_SILU>(c, s.maps, p, false)
-                                                  : launch<MM_UP, OLIVE_ACT_GELU_TANH>(c, s.maps, p, false);
-    if (st != OLIVE_OK) return st;
-  }
-  MapSet s;
-  MlpParams p = {};
-  MlpProb q = problem(T, d, kBN, f, 1);
-  q.a0 = q.a1 = s.k_major(w.h, T, f);
-  q.b0 = q.b1 = s.k_major(W_down, d, f);
-  q.out = s.output(y, T, d, false);
-  if (!s.ok) return OLIVE_ERR_CUDA;
-  p.pr[0] = q;
-  p.n_prob = 1;
-  p.n_maps = s.n;
-  p.residual = static_cast<const __nv_bfloat16*>(residual);
-  p.part = w.part;
+  };
+  const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_UP, OLIVE_ACT_SILU>(c, p, false, up)
+                                                : launch<MM_UP, OLIVE_ACT_GELU_TANH>(c, p, false, up);
+  if (st != OLIVE_OK) return st;
+
+  p.pr[0] = problem(T, d, f, 1);
   p.flag = w.flag + mlp_flag_words();
-  p.dev_status = dev_status;
-  return launch<MM_DOWN>(c, s.maps, p, true);
+  p.n_clear = 0;
+  p.residual = static_cast<const __nv_bfloat16*>(residual);
+  return launch<MM_DOWN>(c, p, true, [&](MapSet& s, int bn) {
+    MlpProb& q = p.pr[0];
+    q.a0 = q.a1 = s.k_major(w.h, T, f, kBM);
+    q.b0 = q.b1 = s.k_major(W_down, d, f, bn / 2);
+    q.out = s.output(y, T, d, false);
+  });
 }
 
 olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const void* W_gate,
@@ -744,65 +818,65 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
                             void* dW_down, int grad_dtype, void* ws, int32_t* dev_status) {
   const MlpWs w = carve_mlp(ws, T, f, true);
   const bool f32 = grad_dtype == OLIVE_DTYPE_F32;
-  {
-    MapSet s;
-    MlpParams p = {};
-    MlpProb q = problem(T, f, kBN, d, 1);
-    q.a0 = q.a1 = s.k_major(dy, T, d);
+  MlpParams p = {};
+  p.part = w.part;
+  p.dev_status = dev_status;
+
+  p.n_prob = 1;
+  p.pr[0] = problem(T, f, d, 1);
+  p.flag = w.flag;
+  p.clear = w.flag + mlp_flag_words();
+  p.n_clear = static_cast<int>(mlp_flag_words());
+  p.saved_g = static_cast<const uint16_t*>(saved);
+  p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
+  auto dh = [&](MapSet& s, int) {
+    MlpProb& q = p.pr[0];
+    q.a0 = q.a1 = s.k_major(dy, T, d, kBM);
     q.b0 = q.b1 = s.mn_major(W_down, d, f);
     q.out = s.output(w.h, T, f, false);
     p.map_g = s.output(w.dg, T, f, false);
     p.map_u = s.output(w.du, T, f, false);
-    if (!s.ok) return OLIVE_ERR_CUDA;
-    p.pr[0] = q;
-    p.n_prob = 1;
-  p.n_maps = s.n;
-    p.saved_g = static_cast<const uint16_t*>(saved);
-    p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
-    p.part = w.part;
-    p.flag = w.flag;
-    p.clear = w.flag + mlp_flag_words();
-    p.n_clear = static_cast<int>(mlp_flag_words());
-    p.dev_status = dev_status;
-    const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_DH, OLIVE_ACT_SILU>(c, s.maps, p, false)
-                                                  : launch<MM_DH, OLIVE_ACT_GELU_TANH>(c, s.maps, p, false);
-    if (st != OLIVE_OK) return st;
-  }
-  MapSet s;
-  MlpParams p = {};
-  if (dx) {
-    MlpProb q = problem(T, d, kBN, f, 2);
-    q.a0 = s.k_major(w.dg, T, f);
-    q.a1 = s.k_major(w.du, T, f);
-    q.b0 = s.mn_major(W_gate, f, d);
-    q.b1 = s.mn_major(W_up, f, d);
-    q.out = s.output(dx, T, d, f32);
-    p.pr[p.n_prob++] = q;
-  }
-  if (dW_gate) {
-    const int16_t xm = s.mn_major(x, T, d);
-    for (int i = 0; i < 2; ++i) {
-      MlpProb q = problem(f, d, kBN, T, 1);
-      q.a0 = q.a1 = s.mn_major(i ? w.du : w.dg, T, f);
-      q.b0 = q.b1 = xm;
-      q.a_mn = 1;
-      q.out = s.output(i ? dW_up : dW_gate, f, d, f32);
-      p.pr[p.n_prob++] = q;
-    }
-    MlpProb q = problem(d, f, kBN, T, 1);
-    q.a0 = q.a1 = s.mn_major(dy, T, d);
-    q.b0 = q.b1 = s.mn_major(w.h, T, f);
-    q.a_mn = 1;
-    q.out = s.output(dW_down, d, f, f32);
-    p.pr[p.n_prob++] = q;
-  }
-  if (!s.ok) return OLIVE_ERR_CUDA;
-  p.n_maps = s.n;
-  p.out_f32 = f32;
-  p.part = w.part;
+  };
+  const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_DH, OLIVE_ACT_SILU>(c, p, false, dh)
+                                                : launch<MM_DH, OLIVE_ACT_GELU_TANH>(c, p, false, dh);
+  if (st != OLIVE_OK) return st;
+
+  p.n_prob = 0;
   p.flag = w.flag + mlp_flag_words();
-  p.dev_status = dev_status;
-  return launch<MM_GRADS>(c, s.maps, p, true);
+  p.n_clear = 0;
+  p.out_f32 = f32;
+  if (dx) p.pr[p.n_prob++] = problem(T, d, f, 2);
+  const int first = p.n_prob;
+  if (dW_gate) {
+    p.pr[p.n_prob++] = problem(f, d, T, 1);
+    p.pr[p.n_prob++] = problem(f, d, T, 1);
+    p.pr[p.n_prob++] = problem(d, f, T, 1);
+  }
+  return launch<MM_GRADS>(c, p, true, [&](MapSet& s, int) {
+    if (dx) {
+      MlpProb& q = p.pr[0];
+      q.a0 = s.k_major(w.dg, T, f, kBM);
+      q.a1 = s.k_major(w.du, T, f, kBM);
+      q.b0 = s.mn_major(W_gate, f, d);
+      q.b1 = s.mn_major(W_up, f, d);
+      q.out = s.output(dx, T, d, f32);
+    }
+    if (dW_gate) {
+      const int16_t xm = s.mn_major(x, T, d);
+      for (int i = 0; i < 2; ++i) {
+        MlpProb& q = p.pr[first + i];
+        q.a0 = q.a1 = s.mn_major(i ? w.du : w.dg, T, f);
+        q.b0 = q.b1 = xm;
+        q.a_mn = 1;
+        q.out = s.output(i ? dW_up : dW_gate, f, d, f32);
+      }
+      MlpProb& q = p.pr[first + 2];
+      q.a0 = q.a1 = s.mn_major(dy, T, d);
+      q.b0 = q.b1 = s.mn_major(w.h, T, f);
+      q.a_mn = 1;
+      q.out = s.output(dW_down, d, f, f32);
+    }
+  });
 }
 
 }  // namespace olive

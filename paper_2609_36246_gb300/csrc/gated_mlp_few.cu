@@ -28,12 +28,11 @@ namespace {
 
 constexpr int kBK = 64;
 constexpr int kMaxStages = 24;
-constexpr int kEpiWarps = 4, kProducerWarp = 4, kMmaWarp = 5;
-constexpr int kThreads = 32 * 6;
+constexpr int kEpiWarps = 8, kProducerWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 32 * 10;
 constexpr int kTile = 128 * 128;      // bytes the MMA reads of an A tile
 // shared memory of a CTA: two to an SM, or one where the tokens' tile is large
 constexpr int budget(int n) { return (n <= 64 ? 108 : 210) * 1024; }
-constexpr int kBarBytes = 8 * (2 * kMaxStages + 1) + 16;
 
 struct FewMaps {
   CUtensorMap a0, a1, b;  // W_gate, W_up (or W_down), tokens
@@ -52,6 +51,14 @@ __device__ __forceinline__ uint32_t cluster_size() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
   return r;
+}
+
+__device__ __forceinline__ void st_cluster_v2(uint32_t addr, uint32_t x, uint32_t y) {
+  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
 }
 
 template <bool kUp, int kN, int kAct>
@@ -179,12 +186,15 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
     tc_fence_after();
   }
 
+  // epilogue warp w: weight rows 32 (w % 4).. of the accumulators and half w / 4
+  // of the tokens, 8 at a time
   const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
   const int row = (warp & 3) * 32 + lane;
+  const int tb = (warp >> 2) * (kN / 2), te = min(tb + kN / 2, nt);
+  const bool epi = warp < kEpiWarps && ok && (warp & 3) * 32 < p.rows;
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
   // one result from its sums
-  auto store = [&](float a, float b, int t, int n) {
-    const size_t at = static_cast<size_t>(t0 + t) * p.rows_all + n;
+  auto store = [&](float a, float b, size_t at) {
     if (kUp) {
       out[at] = __float2bfloat16_rn(activate<kAct>(a) * b);
       if (p.saved_g) {
@@ -196,54 +206,64 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
     }
   };
   if (c == 1) {
-    if (warp < kEpiWarps && ok && (warp & 3) * 32 < p.rows) {
-      const int n = row0 + row;
-      const bool mine = row < p.rows && n < p.rows_all;
+    const bool mine = epi && row < p.rows && row0 + row < p.rows_all;
+    size_t at = static_cast<size_t>(t0 + tb) * p.rows_all + row0 + row;
 #pragma unroll 1
-      for (int t = 0; t < nt; t += 16) {
-        uint32_t a[16], b[16];
-        tmem_ld_32x32b_x16(lane_addr + t, a);
-        if (kUp) tmem_ld_32x32b_x16(lane_addr + kN + t, b);
-        tmem_ld_wait();
+    for (int t = tb; epi && t < te; t += 8) {
+      uint32_t a[8], b[8];
+      tmem_ld_32x32b_x8(lane_addr + t, a);
+      if (kUp) tmem_ld_32x32b_x8(lane_addr + kN + t, b);
+      tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (mine && t + i < nt) store(__uint_as_float(a[i]), kUp ? __uint_as_float(b[i]) : 0.f, t + i, n);
-      }
+      for (int i = 0; i < 8; ++i, at += p.rows_all)
+        if (mine && t + i < te) store(__uint_as_float(a[i]), kUp ? __uint_as_float(b[i]) : 0.f, at);
     }
   } else {
     // CTA q of the cluster finishes tokens [q per, (q + 1) per): every CTA sends
-    // it its sums of them, recv[sender][token][accumulator][row]
-    const int per = (nt + c - 1) / c;
+    // it its sums of them, recv[sender][accumulator][row][token]
+    const int per = kN / c;
     cluster_sync_all();  // all MMAs of the cluster are done: the stages are free
-    if (warp < kEpiWarps && ok && (warp & 3) * 32 < p.rows) {
 #pragma unroll 1
-      for (int t = 0; t < nt; t += 16) {
-        uint32_t a[16], b[16];
-        tmem_ld_32x32b_x16(lane_addr + t, a);
-        if (kUp) tmem_ld_32x32b_x16(lane_addr + kN + t, b);
-        tmem_ld_wait();
+    for (int t = tb; epi && t < te; t += 8) {
+      uint32_t a[8], b[8];
+      tmem_ld_32x32b_x8(lane_addr + t, a);
+      if (kUp) tmem_ld_32x32b_x8(lane_addr + kN + t, b);
+      tmem_ld_wait();
+      if (row >= p.rows) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (t + i >= nt || row >= p.rows) continue;
-          const int q = (t + i) / per, j = t + i - q * per;
-          const uint32_t at = ring + 4u * (((rank * per + j) * kAcc) * p.rows + row);
-          st_shared_cluster(map_shared(at, q), a[i]);
-          if (kUp) st_shared_cluster(map_shared(at + 4u * p.rows, q), b[i]);
+      for (int v = 0; v < 4; ++v) {
+        const int q = (t + 2 * v) / per, j = t + 2 * v - q * per;
+        const uint32_t at = ring + 4u * ((rank * kAcc * p.rows + row) * per + j);
+        const uint32_t au = at + 4u * p.rows * per;
+        if (per == 2) {
+          st_cluster_v2(map_shared(at, q), a[2 * v], a[2 * v + 1]);
+          if (kUp) st_cluster_v2(map_shared(au, q), b[2 * v], b[2 * v + 1]);
+        } else if (v % 2 == 0) {
+          st_cluster_v4(map_shared(at, q), a[2 * v], a[2 * v + 1], a[2 * v + 2], a[2 * v + 3]);
+          if (kUp) st_cluster_v4(map_shared(au, q), b[2 * v], b[2 * v + 1], b[2 * v + 2], b[2 * v + 3]);
         }
       }
     }
     cluster_sync_all();
-    const int my = max(0, min(per, nt - rank * per));
-    for (int i = threadIdx.x; i < my * p.rows; i += kThreads) {
-      const int j = i / p.rows, r = i - j * p.rows;
+    const int my = min(per, nt - rank * per);
+    for (int i = threadIdx.x; i < (my + 1) / 2 * p.rows; i += kThreads) {
+      const int j = i / p.rows * 2, r = i - j / 2 * p.rows;
       if (row0 + r >= p.rows_all) continue;
-      float a = 0.f, b = 0.f;
+      float2 a = {0.f, 0.f}, b = {0.f, 0.f};
       for (int q = 0; q < c; ++q) {
-        const float* f = recv + ((q * per + j) * kAcc) * p.rows + r;
-        a += f[0];
-        if (kUp) b += f[p.rows];
+        const float* f = recv + (q * kAcc * p.rows + r) * per + j;
+        const float2 x = *reinterpret_cast<const float2*>(f);
+        a.x += x.x;
+        a.y += x.y;
+        if (kUp) {
+          const float2 y = *reinterpret_cast<const float2*>(f + p.rows * per);
+          b.x += y.x;
+          b.y += y.y;
+        }
       }
-      store(a, b, rank * per + j, row0 + r);
+      const size_t at = static_cast<size_t>(t0 + rank * per + j) * p.rows_all + row0 + r;
+      store(a.x, b.x, at);
+      if (j + 1 < my) store(a.y, b.y, at + p.rows_all);
     }
   }
 
@@ -258,18 +278,32 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
 
 // Weight rows of a CTA and CTAs of a cluster for `rows_all` rows, `ks` K steps
 // and `tiles` tiles of n tokens.
+//
+// Long tiles (many rows, K steps shared by a cluster) read each token's values
+// fewer times; the exchange of accumulators, 4 rows n bytes each, is what they
+// cost.  So: as many rows as keep a CTA's exchange within 16 KB (32 KB from n =
+// 128 on), and clusters that fill the slots.  Measured, us a call: d = 2048,
+// f = 6144 at n = 16 15.2 with 128 rows by 4 and 8 CTAs, 20.5 with 48 rows by 1
+// and 2; at n = 64 in the second launch 23.2 with 64 rows by 4, 25.6 with 128 rows
+// by 8.  The first launch has two accumulators to exchange and from n = 64 on is
+// quicker with whole K steps (23.2 us with 64 rows by 1, 27.5 by 2; n = 128, d =
+// 4096, f = 12288: 73.6 with 88 rows by 1, 93.0 by 2).
 struct FewShape {
   int rows, c;
 };
 FewShape few_shape(int rows_all, int ks, int tiles, int n, int sms, bool up) {
   const int slots = n <= 64 ? 2 * sms : sms;  // CTAs that run at once
-  const int most = up && n <= 64 ? 64 : 128;
-  // as many rows as leave one CTA for every slot, at least 32 (8 KB of TMA a step)
-  FewShape s{static_cast<int>(align_up(std::max<int64_t>(1, ceil_div(static_cast<int64_t>(rows_all) * tiles, slots)), 8)), 1};
-  s.rows = std::min(most, std::max(s.rows, 32));
+  const int most = (n < 128 ? 16 : 32) * 1024 / (4 * n * (up ? 2 : 1));
+  FewShape s{std::min(128, std::max(64, most)), 1};
   const auto ctas = [&] { return ceil_div(rows_all, s.rows) * s.c * tiles; };
-  // shared K steps where that leaves slots empty: wider tiles, several CTAs each
-  while (s.c < 8 && 2 * ctas() <= slots && ks >= 8 * s.c) s.c *= 2;
+  if (up && n >= 128) {
+    // one CTA a slot where that is one wave
+    const int64_t even = align_up(ceil_div(static_cast<int64_t>(rows_all) * tiles, slots), 8);
+    s.rows = static_cast<int>(std::min<int64_t>(128, std::max<int64_t>(64, even)));
+  }
+  while (s.rows > 32 && 8 * ctas() < sms) s.rows = s.rows > 64 ? 64 : 32;
+  const int c_most = up && n >= 64 && 2 * ctas() >= sms ? 1 : 8;
+  while (s.c < c_most && 2 * ctas() <= slots && ks >= 8 * s.c) s.c *= 2;
   return s;
 }
 
@@ -281,7 +315,7 @@ olive_status launch_few(const Ctx& c, const FewMaps& maps, FewParams p, const Fe
   const int past = std::max(0, (kAcc - 1) * p.rows * 128 + kTile - stage);
   const int ks = static_cast<int>(ceil_div(ceil_div(p.K, kBK), s.c));
   p.stages = std::min({(budget(kN) - 1024 - past) / stage, kMaxStages, ks});
-  const int exchange = s.c > 1 ? 4 * kAcc * p.rows * s.c * static_cast<int>(ceil_div(kN, s.c)) : 0;
+  const int exchange = s.c > 1 ? 4 * kAcc * p.rows * kN : 0;
   const int smem = 1024 + std::max(p.stages * stage + past, exchange);
   p.wait_limit_ns = c.wait_limit_ns;
   static std::atomic<int> done[kMaxDevices];
