@@ -15,8 +15,9 @@
 // receives its 128 rows of the fp32 accumulator in its own TMEM, twice, so that
 // the epilogue of a tile runs under the next tile's MMAs.  An operand is
 // read K-major or MN-major as it lies in memory; nothing is transposed or
-// copied.  Output tiles leave through shared memory by TMA, which also cuts the
-// ragged edges off.
+// copied.  Results are turned in shared memory so that a warp's store covers whole
+// 64-byte rows (TMA stores of the same rows took 7 cycles a row, 7.5 us for a tile
+// of 256 columns of a weight gradient whose products take 1 us).
 //
 // What bounds it: the tensor pipe (a K step of a pair is 512 cycles of MMAs
 // for 64 KB from L2).  Rounding: g and u are used from the fp32 accumulators;
@@ -38,15 +39,15 @@ constexpr int kSA = kBM * kBK * 2;   // this CTA's 128 rows of A
 constexpr int kEpiWarps = 8;
 constexpr int kProducerWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 32 * 10;
-constexpr int kOutBuf = 32 * 64;     // a warp's 32 rows of 64 bytes
+constexpr int kOutBuf = 32 * 64;     // a warp's 32 rows of 64 bytes of a result
 constexpr int kSlots = 8;            // a finisher warp's pieces in flight
 constexpr int kSlotBytes = 16 * 32 * 4;
 enum { MM_UP = 0, MM_DOWN = 1, MM_DH = 2, MM_GRADS = 3 };
-// Three output buffers a warp where a tile gives three results, else two in turn.
+// An output buffer a warp for each result of a tile.
 template <int kMode, int kBN>
 struct Layout {
   static constexpr bool kThree = kMode == MM_UP || kMode == MM_DH;
-  static constexpr int kOutBufs = kThree ? 3 : 2;
+  static constexpr int kOutBufs = kThree ? 3 : 1;
   static constexpr int kSB = kBN / 2 * kBK * 2;  // this CTA's half of B
   static constexpr int kStageBytes = kSA + kSB;
   static constexpr int kStages = kBN == kNarrow ? 7 : kThree ? 5 : 6;
@@ -65,10 +66,9 @@ constexpr int kStatusTimeout = 1 << OLIVE_ERR_TIMEOUT;
 // One product out[M, N] = A . B of a launch; maps are indices into MlpMaps.
 struct MlpProb {
   int16_t a0, a1, b0, b1;  // operands before and from K step ks_half on (MM_UP: b0, b1 by CTA)
-  int16_t out;
-  int16_t a_mn, b_mn;      // MN-major operands
-  int16_t pad;
-  int M, N;
+  int a_mn;                // MN-major A
+  void* out;               // row-major, pitch ld
+  int M, N, ld;
   int mt, nt;              // pair tiles (256 rows), column tiles
   int ks_half, ks;         // K steps
 };
@@ -85,7 +85,7 @@ struct MlpSplit {
 };
 
 struct MlpMaps {
-  CUtensorMap m[13];
+  CUtensorMap m[10];
 };
 
 struct MlpParams {
@@ -101,7 +101,7 @@ struct MlpParams {
   const uint16_t* saved_g;        // MM_DH: [T, f]
   const uint16_t* saved_u;
   int save, out_f32;
-  int16_t map_g, map_u;    // MM_UP: saved g, u; MM_DH: dg, du
+  void *out_g, *out_u;     // MM_UP: saved g, u (pitch N); MM_DH: dg, du (pitch ld)
   int32_t* dev_status;
   uint64_t wait_limit_ns;
 };
@@ -162,21 +162,22 @@ struct UnitWalk {
   }
 };
 
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
-                   reinterpret_cast<uint64_t>(map)),
-               "r"(src), "r"(x), "r"(y)
-               : "memory");
+// 16-byte piece `c` of row `row` of a warp's output buffer: written by rows and
+// read by pieces without bank conflicts.
+__device__ __forceinline__ uint32_t out_piece(uint32_t buf, int row, int c) {
+  return buf + row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
 }
-// All but this thread's latest bulk group have read their source.
-__device__ __forceinline__ void bulk_wait_read_but_one() {
-  asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-}
-
-// Stores to a warp's output buffer: 16-byte piece `c` of row `lane`, 64-byte
-// swizzle (as the tensor maps of the outputs), and the buffer to (x, y).
-__device__ __forceinline__ uint32_t out_piece(uint32_t buf, int lane, int c) {
-  return buf + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4);
+// The buffer to rows y.. and the columns of 64 bytes from x on of an [M, N] array
+// of elt-byte values, pitch ld.
+__device__ __forceinline__ void put_rows(void* out, uint32_t buf, int lane, int x, int y, int M, int N, int ld, int elt) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 8 + (lane >> 2), c = lane & 3;
+    const int col = x + c * (16 / elt);
+    if (y + row < M && col < N)
+      *reinterpret_cast<uint4*>(static_cast<char*>(out) + (static_cast<size_t>(y + row) * ld + col) * elt) =
+          ld_shared_v4(out_piece(buf, row, c));
+  }
 }
 
 // Untiled bulk copy global -> shared, completion counted on the mbarrier.
@@ -228,22 +229,31 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_alloc_pair(smem_u32(tmem_slot), 2 * kBN);
     tmem_relinquish_pair();
   }
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < p.n_clear; i += kThreads) p.clear[i] = 0;
   tc_fence_before();
   cluster_sync_all();
   tc_fence_after();
+  // The launch ahead may still be running (programmatic dependent launch): up to
+  // here nothing of it was needed, and this launch's successor may do the same.
+  grid_launch_dependents();
+  grid_wait();
+  fence_proxy_async_global();
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < p.n_clear; i += kThreads) p.clear[i] = 0;
   const uint32_t tmem_base = *tmem_slot;
   const WaitCtl ctl{abort_flag, p.wait_limit_ns};
+  // Every role walks the pair's units by itself, and finds the next one while it
+  // has work in flight: the walk's divisions take about 1000 cycles, a short tile's
+  // MMAs 2000.
   UnitWalk walk(p, pair, pairs);
-  Unit u;
+  Unit u, ahead;
+  bool more = walk.next(p, u);
 
   if (warp == kProducerWarp) {
     const bool leader = elect_one();
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    while (ok && walk.next(p, u)) {
+    for (; ok && more; u = ahead) {
       const MlpProb& q = p.pr[u.prob];
       const int mrow = u.m0 + static_cast<int>(rank) * kBM;
       // MM_UP: the even CTA holds the tile's rows of Wg, the odd one those of Wu
@@ -271,6 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tma_load_2d_pair(sA + kSA, mb, fb, k, nrow);
           }
         }
+        if (ks == u.k0) more = walk.next(p, ahead);
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
     }
@@ -286,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int stage = 0, n = 0;
       uint32_t phase = 0;
       bool ok = true;
-      while (ok && walk.next(p, u)) {
+      for (; ok && more; u = ahead) {
         const MlpProb& q = p.pr[u.prob];
         const bool a_mn = kMode == MM_GRADS && q.a_mn;
         constexpr bool b_mn = kMode == MM_GRADS || kMode == MM_DH;
@@ -310,6 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               umma_bf16_pair(acc, dA + (so + kk * stepA), dB + (so + kk * stepB), id, kk > 0 || ks > u.k0 ? 1u : 0u);
             umma_commit_pair(empty_bar(stage));
           }
+          if (ks == u.k0) more = walk.next(p, ahead);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
         if (!ok) break;
@@ -333,10 +345,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int half = warp >> 2;
     const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t out0 = base + L::kOut + warp * L::kOutBufs * kOutBuf;
-    int n = 0, turn = 0;
+    int n = 0;
     bool ok = true;
 
-    while (ok && walk.next(p, u)) {
+    for (; ok && more; u = ahead) {
       const MlpProb& q = p.pr[u.prob];
       const int b = n & 1;
       const uint32_t acc = lane_addr + b * kBN;
@@ -374,6 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       };
       fetch(0);
+      more = walk.next(p, ahead);
       if (!mbar_wait_warp(tfull(b), (n >> 1) & 1, ctl)) break;
       tc_fence_after();
       ++n;
@@ -439,8 +452,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           request(taken + kSlots);
         }
       };
-      const bool inside = y < q.M;
-
 #pragma unroll 1
       for (int s = 0; s < kSteps; ++s) {
         const int x = x0 + (s & ~1) * 16;  // first column of the 64-byte output rows
@@ -452,18 +463,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if constexpr (kMode == MM_UP) load(kBN / 2 + col(s), v);
         if (!ok) break;
         if (s == kSteps - 1) release();
-        uint32_t buf = out0;
-        if (opens) {
-          // the buffers about to be written have been read by their last store
-          if (lane == 0) {
-            if (L::kThree)
-              bulk_wait_read();
-            else
-              bulk_wait_read_but_one();
-          }
-          __syncwarp();
-        }
-        if constexpr (!L::kThree) buf += turn * kOutBuf;
+        const uint32_t buf = out0;
+        if (opens) __syncwarp();  // the buffers' last contents have been read
         const int c0 = f32 ? 0 : (s & 1) * 2;  // 16-byte pieces of the row
 
         if constexpr (kMode == MM_UP) {
@@ -550,24 +551,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
 
         if (closes) {
-          fence_proxy_async_shared();
           __syncwarp();
+          const int elt = f32 ? 4 : 2;
           const int xo = f32 ? x0 + s * 16 : x;
-          if (lane == 0) {
-            if (inside && xo < q.N) {
-              tma_store_2d(&maps.m[q.out], buf, xo, y);
-              if (kMode == MM_DH || (kMode == MM_UP && p.save)) {
-                tma_store_2d(&maps.m[p.map_g], buf + kOutBuf, xo, y);
-                tma_store_2d(&maps.m[p.map_u], buf + 2 * kOutBuf, xo, y);
-              }
-            }
-            bulk_commit();
+          put_rows(q.out, buf, lane, xo, y, q.M, q.N, q.ld, elt);
+          if (kMode == MM_DH || (kMode == MM_UP && p.save)) {
+            const int ld = kMode == MM_UP ? q.N : q.ld;
+            put_rows(p.out_g, buf + kOutBuf, lane, xo, y, q.M, q.N, ld, 2);
+            put_rows(p.out_u, buf + 2 * kOutBuf, lane, xo, y, q.M, q.N, ld, 2);
           }
-          turn ^= 1;
         }
       }
     }
-    if (lane == 0) bulk_wait();
     if (!ok && lane == 0) {
       const uint64_t t0 = global_timer_ns();  // pieces in flight land
       while (global_timer_ns() - t0 < 50000) nanosleep_ns(1000);
@@ -598,16 +593,12 @@ struct MapSet {
     return static_cast<int16_t>(n++);
   }
   // operand [rows, cols] bf16 with K along the columns: boxes of `box` rows x 64
-  int16_t k_major(const void* a, int64_t rows, int64_t cols, int box) {
-    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, kBK, box));
+  int16_t k_major(const void* a, int64_t rows, int64_t cols, int64_t pitch, int box) {
+    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * pitch, kBK, box));
   }
   // operand [rows, cols] bf16 with K along the rows: boxes of 64 rows x 64
-  int16_t mn_major(const void* a, int64_t rows, int64_t cols) {
-    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * cols, 64, kBK));
-  }
-  // output [rows, cols]: boxes of 32 rows x 64 bytes
-  int16_t output(void* a, int64_t rows, int64_t cols, bool f32) {
-    return add(encode_out_2d(&maps.m[n], a, cols, rows, f32, 32));
+  int16_t mn_major(const void* a, int64_t rows, int64_t cols, int64_t pitch) {
+    return add(encode_bf16_2d(&maps.m[n], a, cols, rows, 2 * pitch, 64, kBK));
   }
 };
 
@@ -650,58 +641,64 @@ struct Plan {
 };
 
 // The estimate's terms, ns, by tile width: a K step of a pair, a tile's epilogue
-// (seen once, at the end), the store of a piece and the wait for it, and each
-// piece that a finisher adds.
+// (by mode: the least that a tile takes, and seen in full at the end), the store
+// of a piece and the wait for it, and each piece that a finisher adds.
 struct Cost {
-  double step, tail, cut, piece;
+  double step, tile[4], cut, piece;
 };
-constexpr Cost kCostWide{290, 4500, 2500, 1800}, kCostNarrow{165, 2600, 2000, 1000};
+constexpr double kClear = 3500;  // zeroing the flags, where no launch of the call has
+constexpr Cost kCostWide{290, {4500, 3300, 6500, 3300}, 2500, 1800};
+constexpr Cost kCostNarrow{165, {2500, 1900, 3500, 1900}, 2000, 1000};
 
 // Deals the tiles to the pairs, whole ones or every product's last ones cut, by
 // what is estimated to end first.
-Plan plan_tiles(const MlpParams& p, bool up, int bn, int pairs) {
+Plan plan_tiles(const MlpParams& p, int mode, int bn, int pairs) {
   const Cost& k = bn == kWide ? kCostWide : kCostNarrow;
-  const int cols = up ? bn / 2 : bn;
+  const int cols = mode == MM_UP ? bn / 2 : bn;
   int tiles[kMaxProbs], all = 0, longest = 0;
+  double ns[kMaxProbs];  // of a whole tile
   for (int i = 0; i < p.n_prob; ++i) {
     tiles[i] = p.pr[i].mt * static_cast<int>(ceil_div(p.pr[i].N, cols));
+    ns[i] = std::max(p.pr[i].ks * k.step, k.tile[mode]);
     all += tiles[i];
     longest = std::max(longest, p.pr[i].ks);
   }
   Plan w{bn, std::min(pairs, all), {}, 0};
   w.cut.run = 1;
-  // whole, in turn: the pair with the most steps
-  int64_t most = 0;
+  // whole, in turn: the pair with the most to do
   for (int r = 0; r < w.pairs; ++r) {
-    int64_t load = 0;
+    double load = 0;
     int first = 0;
     for (int i = 0; i < p.n_prob; first += tiles[i++]) {
       const int skip = ((r - first) % pairs + pairs) % pairs;  // to this pair's first tile of the product
-      if (skip < tiles[i]) load += ceil_div(tiles[i] - skip, pairs) * p.pr[i].ks;
+      if (skip < tiles[i]) load += static_cast<double>(ceil_div(tiles[i] - skip, pairs)) * ns[i];
     }
-    most = std::max(most, load);
+    w.ns = std::max(w.ns, load);
   }
   for (int i = 0; i < p.n_prob; ++i) w.cut.whole[i] = tiles[i];
   w.cut.n_whole = all;
-  w.ns = most * k.step + k.tail;
+  w.ns += k.tile[mode];
   // every product's last tiles cut
   MlpSplit s = {};
-  int64_t before = 0, steps = 0;
+  int64_t steps = 0;
+  double before = 0;
   for (int i = 0; i < p.n_prob; ++i) {
     const int rest = tiles[i] % pairs;
     s.whole[i] = tiles[i] - rest;
     s.n_whole += s.whole[i];
     s.off[i] = static_cast<int>(steps);
     steps += static_cast<int64_t>(rest) * p.pr[i].ks;
-    before += static_cast<int64_t>(s.whole[i] / pairs) * p.pr[i].ks;
+    before += s.whole[i] / pairs * ns[i];
+    if (steps > (1 << 30)) return w;
   }
-  if (steps == 0 || steps > (1 << 30)) return w;
+  if (steps == 0) return w;
   s.steps = static_cast<int>(steps);
   for (int m = 1; m <= 8; ++m) {  // longer runs on fewer pairs: fewer pieces
     s.run = static_cast<int>(ceil_div(steps * m, pairs));
     const double pieces = static_cast<double>(longest) / s.run;
-    const double ns = (before + s.run) * k.step + k.tail + k.cut + k.piece * pieces;
-    if (ns < w.ns) w = Plan{bn, s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, s.run)), s, ns};
+    double t = before + s.run * k.step + k.tile[mode] + k.cut + k.piece * pieces;
+    if (mode == MM_UP || mode == MM_DH) t += kClear;
+    if (t < w.ns) w = Plan{bn, s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, s.run)), s, t};
   }
   return w;
 }
@@ -723,13 +720,15 @@ olive_status launch_tiles(const Ctx& c, const MlpMaps& maps, MlpParams& p, const
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = Layout<kMode, kBN>::kSmem;
   cfg.stream = c.stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   if (cudaLaunchKernelEx(&cfg, mlp_gemm_kernel<kMode, kAct, kBN>, maps, p) != cudaSuccess) {
     cudaGetLastError();
     return OLIVE_ERR_CUDA;
@@ -742,8 +741,8 @@ template <int kMode, int kAct = 0, class Fill>
 olive_status launch(const Ctx& c, MlpParams& p, bool zeroed, Fill&& fill) {
   const int pairs = std::min(resident_pairs<kMode, kAct, kWide>(c), resident_pairs<kMode, kAct, kNarrow>(c));
   if (pairs < 1) return OLIVE_ERR_UNSUPPORTED_DEVICE;
-  const Plan wide = plan_tiles(p, kMode == MM_UP, kWide, pairs);
-  const Plan narrow = plan_tiles(p, kMode == MM_UP, kNarrow, pairs);
+  const Plan wide = plan_tiles(p, kMode, kWide, pairs);
+  const Plan narrow = plan_tiles(p, kMode, kNarrow, pairs);
   const bool w = wide.ns <= narrow.ns;
   MapSet s;
   fill(s, w ? kWide : kNarrow);
@@ -753,10 +752,12 @@ olive_status launch(const Ctx& c, MlpParams& p, bool zeroed, Fill&& fill) {
            : launch_tiles<kMode, kAct, kNarrow>(c, s.maps, p, narrow, zeroed);
 }
 
-MlpProb problem(int M, int N, int K, int halves) {
+MlpProb problem(int M, int N, int K, int halves, void* out, int ld) {
   MlpProb q = {};
+  q.out = out;
   q.M = M;
   q.N = N;
+  q.ld = ld;
   q.mt = static_cast<int>(ceil_div(M, 2 * kBM));
   q.ks_half = static_cast<int>(ceil_div(K, kBK));
   q.ks = halves * q.ks_half;
@@ -775,40 +776,37 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
   const MlpWs w = carve_mlp(ws, T, f, false);
   if (T <= kMlpFewRows)
     return launch_mlp_few(c, x, W_gate, W_up, W_down, residual, T, d, f, act, y, saved, w.h, dev_status);
+  const int fp = static_cast<int>(mlp_pitch(f));
   MlpParams p = {};
   p.n_prob = 1;
   p.part = w.part;
   p.dev_status = dev_status;
 
-  p.pr[0] = problem(T, f, d, 1);
+  p.pr[0] = problem(T, f, d, 1, w.h, fp);
   p.flag = w.flag;
   p.clear = w.flag + mlp_flag_words();
   p.n_clear = static_cast<int>(mlp_flag_words());
   p.save = saved != nullptr;
+  p.out_g = saved;
+  p.out_u = saved ? static_cast<uint16_t*>(saved) + static_cast<size_t>(T) * f : nullptr;
   auto up = [&](MapSet& s, int bn) {
     MlpProb& q = p.pr[0];
-    q.a0 = q.a1 = s.k_major(x, T, d, kBM);
-    q.b0 = s.k_major(W_gate, f, d, bn / 2);
-    q.b1 = s.k_major(W_up, f, d, bn / 2);
-    q.out = s.output(w.h, T, f, false);
-    if (saved) {
-      p.map_g = s.output(saved, T, f, false);
-      p.map_u = s.output(static_cast<uint16_t*>(saved) + static_cast<size_t>(T) * f, T, f, false);
-    }
+    q.a0 = q.a1 = s.k_major(x, T, d, d, kBM);
+    q.b0 = s.k_major(W_gate, f, d, d, bn / 2);
+    q.b1 = s.k_major(W_up, f, d, d, bn / 2);
   };
   const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_UP, OLIVE_ACT_SILU>(c, p, false, up)
                                                 : launch<MM_UP, OLIVE_ACT_GELU_TANH>(c, p, false, up);
   if (st != OLIVE_OK) return st;
 
-  p.pr[0] = problem(T, d, f, 1);
+  p.pr[0] = problem(T, d, f, 1, y, d);
   p.flag = w.flag + mlp_flag_words();
   p.n_clear = 0;
   p.residual = static_cast<const __nv_bfloat16*>(residual);
   return launch<MM_DOWN>(c, p, true, [&](MapSet& s, int bn) {
     MlpProb& q = p.pr[0];
-    q.a0 = q.a1 = s.k_major(w.h, T, f, kBM);
-    q.b0 = q.b1 = s.k_major(W_down, d, f, bn / 2);
-    q.out = s.output(y, T, d, false);
+    q.a0 = q.a1 = s.k_major(w.h, T, f, fp, kBM);
+    q.b0 = q.b1 = s.k_major(W_down, d, f, f, bn / 2);
   });
 }
 
@@ -817,25 +815,24 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
                             int32_t d, int32_t f, int act, void* dx, void* dW_gate, void* dW_up,
                             void* dW_down, int grad_dtype, void* ws, int32_t* dev_status) {
   const MlpWs w = carve_mlp(ws, T, f, true);
-  const bool f32 = grad_dtype == OLIVE_DTYPE_F32;
+  const int fp = static_cast<int>(mlp_pitch(f));
   MlpParams p = {};
   p.part = w.part;
   p.dev_status = dev_status;
 
   p.n_prob = 1;
-  p.pr[0] = problem(T, f, d, 1);
+  p.pr[0] = problem(T, f, d, 1, w.h, fp);
   p.flag = w.flag;
   p.clear = w.flag + mlp_flag_words();
   p.n_clear = static_cast<int>(mlp_flag_words());
   p.saved_g = static_cast<const uint16_t*>(saved);
   p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
+  p.out_g = w.dg;
+  p.out_u = w.du;
   auto dh = [&](MapSet& s, int) {
     MlpProb& q = p.pr[0];
-    q.a0 = q.a1 = s.k_major(dy, T, d, kBM);
-    q.b0 = q.b1 = s.mn_major(W_down, d, f);
-    q.out = s.output(w.h, T, f, false);
-    p.map_g = s.output(w.dg, T, f, false);
-    p.map_u = s.output(w.du, T, f, false);
+    q.a0 = q.a1 = s.k_major(dy, T, d, d, kBM);
+    q.b0 = q.b1 = s.mn_major(W_down, d, f, f);
   };
   const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_DH, OLIVE_ACT_SILU>(c, p, false, dh)
                                                 : launch<MM_DH, OLIVE_ACT_GELU_TANH>(c, p, false, dh);
@@ -844,37 +841,34 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
   p.n_prob = 0;
   p.flag = w.flag + mlp_flag_words();
   p.n_clear = 0;
-  p.out_f32 = f32;
-  if (dx) p.pr[p.n_prob++] = problem(T, d, f, 2);
+  p.out_f32 = grad_dtype == OLIVE_DTYPE_F32;
+  if (dx) p.pr[p.n_prob++] = problem(T, d, f, 2, dx, d);
   const int first = p.n_prob;
   if (dW_gate) {
-    p.pr[p.n_prob++] = problem(f, d, T, 1);
-    p.pr[p.n_prob++] = problem(f, d, T, 1);
-    p.pr[p.n_prob++] = problem(d, f, T, 1);
+    p.pr[p.n_prob++] = problem(f, d, T, 1, dW_gate, d);
+    p.pr[p.n_prob++] = problem(f, d, T, 1, dW_up, d);
+    p.pr[p.n_prob++] = problem(d, f, T, 1, dW_down, f);
   }
   return launch<MM_GRADS>(c, p, true, [&](MapSet& s, int) {
     if (dx) {
       MlpProb& q = p.pr[0];
-      q.a0 = s.k_major(w.dg, T, f, kBM);
-      q.a1 = s.k_major(w.du, T, f, kBM);
-      q.b0 = s.mn_major(W_gate, f, d);
-      q.b1 = s.mn_major(W_up, f, d);
-      q.out = s.output(dx, T, d, f32);
+      q.a0 = s.k_major(w.dg, T, f, fp, kBM);
+      q.a1 = s.k_major(w.du, T, f, fp, kBM);
+      q.b0 = s.mn_major(W_gate, f, d, d);
+      q.b1 = s.mn_major(W_up, f, d, d);
     }
     if (dW_gate) {
-      const int16_t xm = s.mn_major(x, T, d);
+      const int16_t xm = s.mn_major(x, T, d, d);
       for (int i = 0; i < 2; ++i) {
         MlpProb& q = p.pr[first + i];
-        q.a0 = q.a1 = s.mn_major(i ? w.du : w.dg, T, f);
+        q.a0 = q.a1 = s.mn_major(i ? w.du : w.dg, T, f, fp);
         q.b0 = q.b1 = xm;
         q.a_mn = 1;
-        q.out = s.output(i ? dW_up : dW_gate, f, d, f32);
       }
       MlpProb& q = p.pr[first + 2];
-      q.a0 = q.a1 = s.mn_major(dy, T, d);
-      q.b0 = q.b1 = s.mn_major(w.h, T, f);
+      q.a0 = q.a1 = s.mn_major(dy, T, d, d);
+      q.b0 = q.b1 = s.mn_major(w.h, T, f, fp);
       q.a_mn = 1;
-      q.out = s.output(dW_down, d, f, f32);
     }
   });
 }

@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
   const int ks_all = (p.K + kBK - 1) / kBK;
   const int ks0 = ks_all * rank / c, ks1 = ks_all * (rank + 1) / c;
 
-  if (kUp) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  grid_launch_dependents();
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full_bar(s), 1);
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
       for (int s = 0; s < first; ++s) weights(s, ks0 + s);
       // W_down does not depend on the launch before this one; h does
       if (!kUp) {
-        asm volatile("griddepcontrol.wait;" ::: "memory");
+        grid_wait();
         fence_proxy_async_global();
       }
       for (int s = 0; s < first; ++s) tokens(s, ks0 + s);

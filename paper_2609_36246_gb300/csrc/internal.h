@@ -55,10 +55,6 @@ bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t
 bool encode_bf16_2d_plain(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                           uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer);
 
-// A dense bf16 or fp32 result: boxes of 64 bytes x box_outer rows, 64-byte swizzle.
-bool encode_out_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, bool f32,
-                   uint32_t box_outer);
-
 // Rows of the G slab used by the backward passes for vocabulary size V.
 int64_t slab_rows(int64_t Tpad, int64_t V);
 inline int64_t vpad(int64_t V) { return align_up(static_cast<size_t>(V), 8); }
@@ -363,10 +359,13 @@ olive_status launch_topk_kl_fwd_bwd(const Ctx& c, const void* h_s, const void* W
 
 // ---- gated feed-forward block (gated_mlp.cu) ----
 constexpr int kMlpMaxPairs = 96;  // CTA pairs the partials and flags are sized for
+// Pitch of the block's own [T, f] arrays: whole 128-byte rows, which TMA reads a
+// fifth faster than rows that straddle them.
+inline int64_t mlp_pitch(int64_t f) { return static_cast<int64_t>(align_up(static_cast<size_t>(f), 64)); }
 struct MlpWs {
-  void* h;         // bf16 [T, f]
-  void* dg;        // bf16 [T, f] (backward)
-  void* du;        // bf16 [T, f] (backward)
+  void* h;         // bf16 [T, mlp_pitch(f)]
+  void* dg;        // bf16 [T, mlp_pitch(f)] (backward)
+  void* du;        // bf16 [T, mlp_pitch(f)] (backward)
   float* part;     // mlp_part_bytes(): partial accumulators of cut tiles
   uint32_t* flag;  // 2 x mlp_flag_words(): pieces stored, for each launch of a call
 };

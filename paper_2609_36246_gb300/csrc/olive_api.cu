@@ -82,16 +82,16 @@ bool set_smem_once(const void* func, int smem, int device, std::atomic<int>* don
   return true;
 }
 
-static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t inner,
-                      uint64_t outer, uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer,
-                      CUtensorMapSwizzle swz) {
+static bool encode_bf16_2d_swz(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
+                               uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer,
+                               CUtensorMapSwizzle swz) {
   auto fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[2] = {inner, outer};
   cuuint64_t strides[1] = {row_bytes};
   cuuint32_t box[2] = {box_inner, box_outer};
   cuuint32_t estr[2] = {1, 1};
-  const CUresult r = fn(map, type, 2, const_cast<void*>(base), dims,
+  const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
                         strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz,
                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
@@ -99,21 +99,14 @@ static bool encode_2d(CUtensorMap* map, CUtensorMapDataType type, const void* ba
 
 bool encode_bf16_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                     uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer) {
-  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, row_bytes, box_inner,
-                   box_outer, CU_TENSOR_MAP_SWIZZLE_128B);
-}
-
-bool encode_out_2d(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, bool f32,
-                   uint32_t box_outer) {
-  const uint32_t elt = f32 ? 4 : 2;
-  return encode_2d(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base,
-                   inner, outer, elt * inner, 64 / elt, box_outer, CU_TENSOR_MAP_SWIZZLE_64B);
+  return encode_bf16_2d_swz(map, base, inner, outer, row_bytes, box_inner, box_outer,
+                            CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 bool encode_bf16_2d_plain(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer,
                           uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer) {
-  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, inner, outer, row_bytes, box_inner,
-                   box_outer, CU_TENSOR_MAP_SWIZZLE_NONE);
+  return encode_bf16_2d_swz(map, base, inner, outer, row_bytes, box_inner, box_outer,
+                            CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 int64_t slab_rows(int64_t Tpad, int64_t V) {
@@ -350,10 +343,11 @@ KlWs carve_kl(void* ws, int64_t T, int64_t ds, int64_t dt, int64_t V, int grad) 
 static MlpWs carve_mlp_impl(void* ws, int64_t T, int64_t f, bool bwd, size_t* total) {
   Carver c{static_cast<char*>(ws)};
   MlpWs w = {};
-  w.h = c.take(2ull * T * f);
+  const size_t rows = 2ull * T * mlp_pitch(f);
+  w.h = c.take(rows);
   if (bwd) {
-    w.dg = c.take(2ull * T * f);
-    w.du = c.take(2ull * T * f);
+    w.dg = c.take(rows);
+    w.du = c.take(rows);
   }
   w.part = static_cast<float*>(c.take(mlp_part_bytes()));
   w.flag = static_cast<uint32_t*>(c.take(2 * 4 * mlp_flag_words()));

@@ -140,6 +140,15 @@ __device__ __forceinline__ T warp_uniform_copy(const T* src) {
   return r;
 }
 
+// ------------------------------------------- programmatic dependent launch ---
+// Lets the stream's next kernel start (if it was launched to) before this one
+// ends; and, in such a kernel, waits until the kernels ahead have ended and their
+// memory operations are visible.
+__device__ __forceinline__ void grid_launch_dependents() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ------------------------------------------------------------------- TMA ---
 // 2-D tiled bulk tensor load global -> shared, completion counted in bytes on
 // the mbarrier.  x is the innermost (contiguous) coordinate in elements.
