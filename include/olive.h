@@ -564,9 +564,9 @@ OLIVE_API olive_status olive_packed_positions(const int32_t* cu_seqlens, int32_t
  *   (elements), so q and k can be views of one fused projection; its D values
  *   are contiguous.  The outputs have strides of their own; an output may be
  *   its own input (same pointer and strides).
- *   D a multiple of 8, 8 <= D <= 256; R a multiple of 8, 0 <= R <= D; Hq, Hk
- *   >= 0, not both 0 (the pointers of a side without heads are ignored); T >= 0;
- *   strides multiples of 8, base pointers 16-byte aligned; eps >= 0.
+ *   D a multiple of 8, 8 <= D <= 256; R a multiple of 8, 0 <= R <= D; 0 <=
+ *   Hq, Hk <= 4096, not both 0 (the pointers of a side without heads are ignored);
+ *   T >= 0; strides multiples of 8, base pointers 16-byte aligned; eps >= 0.
  * A position outside [0, P) gives NaN for its token and OLIVE_ERR_TOKEN_RANGE;
  * dev_status may be NULL (nothing is reported then).
  */
@@ -586,7 +586,7 @@ OLIVE_API olive_status olive_qk_norm_rope_fwd(
  *   dx = r (dn w - x r^2 mean(dn w x)),     dw = sum over tokens and heads of dn x r
  * d_q, d_k have the type of q and strides of their own (d_q may be g_q, with its
  * strides); dw_q, dw_k fp32 [D] are both written (0 for a side without heads)
- * and summed in a fixed order, in fp32 per thread and fp64 across threads.
+ * and summed in a fixed order, in fp32 within a block of threads and fp64 across.
  * workspace: olive_workspace_size(OLIVE_OP_QK_NORM_ROPE_BWD, 1, D, 0, 1, 0, 0) bytes.
  */
 OLIVE_API olive_status olive_qk_norm_rope_bwd(

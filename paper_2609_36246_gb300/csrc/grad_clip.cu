@@ -18,8 +18,7 @@
 #include <cmath>
 
 #include "internal.h"
-
-#include <cuda_bf16.h>
+#include "sm103.cuh"
 
 namespace olive {
 namespace {
@@ -48,13 +47,13 @@ struct List {
 __device__ __forceinline__ bool aligned16_dev(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Values of a 16-byte vector.
-__device__ __forceinline__ void widen(const uint4& v, bool f32, float (&x)[8]) {
+template <bool kF32>
+__device__ __forceinline__ void widen(const uint4& v, float (&x)[kF32 ? 4 : 8]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (f32) {
+    if constexpr (kF32) {
       x[i] = __uint_as_float(w[i]);
-      x[4 + i] = 0.f;
     } else {
       x[2 * i] = __uint_as_float(w[i] << 16);
       x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
@@ -63,34 +62,53 @@ __device__ __forceinline__ void widen(const uint4& v, bool f32, float (&x)[8]) {
 }
 
 // Sum of squares of a thread's vectors.
-__device__ __forceinline__ double squares(const uint4 (&v)[kVecs], bool f32) {
+template <bool kF32>
+__device__ __forceinline__ double squares(const uint4 (&v)[kVecs]) {
+  constexpr int kPer = kF32 ? 4 : 8;
   float q = 0.f;
   uint32_t any = 0;
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
-    float x[8];
-    widen(v[k], f32, x);
+    float x[kPer];
+    widen<kF32>(v[k], x);
     any |= v[k].x | v[k].y | v[k].z | v[k].w;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q = fmaf(x[i], x[i], q);
+    for (int i = 0; i < kPer; ++i) q = fmaf(x[i], x[i], q);
   }
   if (q < 1e36f && q > 1e-28f) return q;
-  if ((any & 0x7fff7fffu) == 0) return 0.0;
+  if ((any & (kF32 ? 0x7fffffffu : 0x7fff7fffu)) == 0) return 0.0;
   double d = 0.0;
-#pragma unroll 1
-  for (int k = 0; k < kVecs; ++k) {
-    float x[8];
-    widen(v[k], f32, x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) d = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), d);
+  for (int k = 0; k < kVecs; ++k) {
+    float x[kPer];
+    widen<kF32>(v[k], x);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) d = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), d);
   }
   return d;
 }
 
-__device__ __forceinline__ float value_at(const void* p, bool f32, long long i) {
+// A vector scaled by f.
+template <bool kF32>
+__device__ __forceinline__ uint4 scaled(const uint4& v, float f) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (kF32) {
+      w[i] = __float_as_uint(__uint_as_float(w[i]) * f);
+    } else {
+      const __nv_bfloat162 h =
+          __floats2bfloat162_rn(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ float value_at(const void* p, bool f32, int i) {
   return f32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
 }
-__device__ __forceinline__ void store_at(void* p, bool f32, long long i, float v) {
+__device__ __forceinline__ void store_at(void* p, bool f32, int i, float v) {
   if (f32)
     static_cast<float*>(p)[i] = v;
   else
@@ -109,6 +127,29 @@ __device__ double block_sum(double v, double* sums) {
   return v;
 }
 
+// Unit u's place in the list, whose entry is at e or behind it (before it, in
+// descending order).
+struct Span {
+  const char* src;
+  char* dst;
+  int n;      // values
+  bool f32, whole;
+};
+template <int N>
+__device__ __forceinline__ Span span(const List<N>& list, int e, uint32_t u) {
+  const Entry& t = list.e[e];
+  Span s;
+  s.f32 = t.f32 != 0;
+  const int per = kUnitBytes / (s.f32 ? 4 : 2);
+  const long long at = static_cast<long long>(u - t.unit0);
+  const long long left = t.n - at * per;
+  s.n = static_cast<int>(min(left, static_cast<long long>(per)));
+  s.whole = left >= per;
+  s.src = static_cast<const char*>(t.src) + at * kUnitBytes;
+  s.dst = static_cast<char*>(t.dst) + at * kUnitBytes;
+  return s;
+}
+
 template <int N>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
     grad_norm_kernel(const __grid_constant__ List<N> list, double* part) {
@@ -117,35 +158,32 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
   int e = 0;
   for (uint32_t u = blockIdx.x; u < list.units; u += gridDim.x) {
     while (e + 1 < list.count && u >= list.e[e + 1].unit0) ++e;
-    const Entry& t = list.e[e];
-    const bool f32 = t.f32 != 0;
-    const int per = f32 ? 4 : 8;  // values of a vector
-    const long long first = static_cast<long long>(u - t.unit0) * (kThreads * kVecs * per);
-    const long long left = t.n - first;
-    if (aligned16_dev(t.src)) {
-      const uint4* v = reinterpret_cast<const uint4*>(static_cast<const char*>(t.src) + first * (f32 ? 4 : 2));
+    const Span s = span(list, e, u);
+    if (aligned16_dev(s.src)) {
+      const uint4* v = reinterpret_cast<const uint4*>(s.src) + threadIdx.x;
       uint4 x[kVecs];
+      if (s.whole) {
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        const int at = k * kThreads + threadIdx.x;
-        x[k] = static_cast<long long>(at + 1) * per <= left ? __ldg(v + at) : make_uint4(0, 0, 0, 0);
-      }
-      acc += squares(x, f32);
-      if (left < kThreads * kVecs * per) {  // values behind the last whole vector
-        const int tail = static_cast<int>(left % per);
-        if (static_cast<int>(threadIdx.x) < tail) {
-          const double y = value_at(t.src, f32, t.n - tail + threadIdx.x);
+        for (int k = 0; k < kVecs; ++k) x[k] = __ldg(v + k * kThreads);
+      } else {
+        const int per = s.f32 ? 4 : 8, vecs = s.n / per, tail = s.n % per;
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k)
+          x[k] = k * kThreads + static_cast<int>(threadIdx.x) < vecs ? __ldg(v + k * kThreads) : make_uint4(0, 0, 0, 0);
+        if (static_cast<int>(threadIdx.x) < tail) {  // values behind the last whole vector
+          const double y = value_at(s.src, s.f32, s.n - tail + threadIdx.x);
           acc = fma(y, y, acc);
         }
       }
+      acc += s.f32 ? squares<true>(x) : squares<false>(x);
     } else {
-      const int n = static_cast<int>(min(left, static_cast<long long>(kThreads * kVecs * per)));
-      for (int i = threadIdx.x; i < n; i += kThreads) {
-        const double y = value_at(t.src, f32, first + i);
+      for (int i = threadIdx.x; i < s.n; i += kThreads) {
+        const double y = value_at(s.src, s.f32, i);
         acc = fma(y, y, acc);
       }
     }
   }
+  grid_launch_dependents();
   const double s = block_sum(acc, sums);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
@@ -155,61 +193,45 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm)
     grad_scale_kernel(const __grid_constant__ List<N> list, const double* part, int parts, float max_norm,
                       float* norm) {
   __shared__ double sums[kThreads / 32];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
-  s = sqrt(block_sum(s, sums));
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(s);
-  const double ratio = static_cast<double>(max_norm) / (s + 1e-6);
+  grid_wait();
+  double total = 0.0;
+  for (int i = threadIdx.x; i < parts; i += kThreads) total += part[i];
+  total = sqrt(block_sum(total, sums));
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(total);
+  const double ratio = static_cast<double>(max_norm) / (total + 1e-6);
   const float f = ratio >= 1.0 ? 1.f : static_cast<float>(ratio);  // (NaN stays NaN)
 
   int e = list.count - 1;
   for (long long w = static_cast<long long>(list.units) - 1 - blockIdx.x; w >= 0; w -= gridDim.x) {
     const uint32_t u = static_cast<uint32_t>(w);
     while (u < list.e[e].unit0) --e;
-    const Entry& t = list.e[e];
-    if (f == 1.f && t.src == t.dst) continue;
-    const bool f32 = t.f32 != 0;
-    const int per = f32 ? 4 : 8;
-    const long long first = static_cast<long long>(u - t.unit0) * (kThreads * kVecs * per);
-    const long long left = t.n - first;
-    if (aligned16_dev(t.src) && aligned16_dev(t.dst)) {
-      const long long at0 = first * (f32 ? 4 : 2);
-      const uint4* v = reinterpret_cast<const uint4*>(static_cast<const char*>(t.src) + at0);
-      uint4* o = reinterpret_cast<uint4*>(static_cast<char*>(t.dst) + at0);
+    const Span s = span(list, e, u);
+    if (f == 1.f && s.src == s.dst) continue;
+    if (aligned16_dev(s.src) && aligned16_dev(s.dst)) {
+      const uint4* v = reinterpret_cast<const uint4*>(s.src) + threadIdx.x;
+      uint4* o = reinterpret_cast<uint4*>(s.dst) + threadIdx.x;
+      const int per = s.f32 ? 4 : 8, vecs = s.n / per, tail = s.n % per;
       uint4 x[kVecs];
+      if (s.whole) {
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        const int at = k * kThreads + threadIdx.x;
-        if (static_cast<long long>(at + 1) * per <= left) x[k] = v[at];
-      }
+        for (int k = 0; k < kVecs; ++k) x[k] = v[k * kThreads];
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        const int at = k * kThreads + threadIdx.x;
-        if (static_cast<long long>(at + 1) * per > left) continue;
-        uint32_t* q = reinterpret_cast<uint32_t*>(&x[k]);
+        for (int k = 0; k < kVecs; ++k) o[k * kThreads] = s.f32 ? scaled<true>(x[k], f) : scaled<false>(x[k], f);
+      } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (f32) {
-            q[i] = __float_as_uint(__uint_as_float(q[i]) * f);
-          } else {
-            const __nv_bfloat162 h =
-                __floats2bfloat162_rn(__uint_as_float(q[i] << 16) * f, __uint_as_float(q[i] & 0xffff0000u) * f);
-            q[i] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-        }
-        o[at] = x[k];
-      }
-      if (left < kThreads * kVecs * per) {
-        const int tail = static_cast<int>(left % per);
+        for (int k = 0; k < kVecs; ++k)
+          if (k * kThreads + static_cast<int>(threadIdx.x) < vecs) x[k] = v[k * kThreads];
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k)
+          if (k * kThreads + static_cast<int>(threadIdx.x) < vecs)
+            o[k * kThreads] = s.f32 ? scaled<true>(x[k], f) : scaled<false>(x[k], f);
         if (static_cast<int>(threadIdx.x) < tail) {
-          const long long i = t.n - tail + threadIdx.x;
-          store_at(t.dst, f32, i, value_at(t.src, f32, i) * f);
+          const int i = s.n - tail + threadIdx.x;
+          store_at(s.dst, s.f32, i, value_at(s.src, s.f32, i) * f);
         }
       }
     } else {
-      const int n = static_cast<int>(min(left, static_cast<long long>(kThreads * kVecs * per)));
-      for (int i = threadIdx.x; i < n; i += kThreads)
-        store_at(t.dst, f32, first + i, value_at(t.src, f32, first + i) * f);
+      for (int i = threadIdx.x; i < s.n; i += kThreads) store_at(s.dst, s.f32, i, value_at(s.src, s.f32, i) * f);
     }
   }
 }
@@ -248,7 +270,17 @@ olive_status run(const Ctx& c, const void* const* src, void* const* dst, const i
   for (int i = 0; i < std::max(n, 1); i += N) {
     List<N> l = make_list<N>(src, dst, numel, dtype, i, dst ? std::min(n, i + N) : i);
     const int blocks = static_cast<int>(std::min<int64_t>(l.units, most));
-    grad_scale_kernel<N><<<std::max(blocks, 1), kThreads, 0, c.stream>>>(l, part, parts, max_norm, norm);
+    // starts while the launch ahead ends, and waits for it by itself
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(std::max(blocks, 1)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = c.stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, grad_scale_kernel<N>, l, static_cast<const double*>(part), parts, max_norm, norm);
     if (!dst) break;
   }
   return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;

@@ -379,6 +379,7 @@ olive_status check_ws(void* ws, size_t have, size_t need) {
 }
 
 constexpr int32_t kMaxHeadDim = 256;
+constexpr int32_t kMaxHeads = 4096;
 
 bool width_ok(int32_t d) { return d >= 8 && d <= kMaxDim && (d % 8) == 0; }
 
@@ -771,7 +772,7 @@ static olive_status check_qk(const QkArgs& a, bool bwd) {
   if (a.interleaved != 0 && a.interleaved != 1) return OLIVE_ERR_INVALID_ARG;
   if (!(a.eps >= 0.f) || !std::isfinite(a.eps)) return OLIVE_ERR_INVALID_ARG;
   if (a.T < 0 || a.D < 8 || a.D > kMaxHeadDim || a.R < 0 || a.R > a.D || a.P < 1 || a.heads[0] < 0 ||
-      a.heads[1] < 0 || a.heads[0] > kMaxDim || a.heads[1] > kMaxDim || a.heads[0] + a.heads[1] < 1)
+      a.heads[1] < 0 || a.heads[0] > kMaxHeads || a.heads[1] > kMaxHeads || a.heads[0] + a.heads[1] < 1)
     return OLIVE_ERR_SHAPE;
   if (a.D % 8 != 0 || a.R % 8 != 0) return OLIVE_ERR_ALIGNMENT;
   if (a.T > 0 && (!a.positions || (a.R > 0 && (!a.cos || !a.sin)))) return OLIVE_ERR_INVALID_ARG;

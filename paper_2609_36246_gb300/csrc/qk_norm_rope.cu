@@ -12,14 +12,16 @@
 #include <algorithm>
 
 #include "internal.h"
-
-#include <cuda_bf16.h>
+#include "sm103.cuh"
 
 namespace olive {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxBwdBlocks = 1024;  // blocks whose partial weight gradients the workspace holds
+constexpr int kFwdBlocks = 4, kBwdBlocks = 2;  // blocks an SM
+// blocks whose partial weight gradients the workspace holds (a side of many heads
+// may need more than run at once, for one token's chunks)
+constexpr int kMaxBwdBlocks = 1024;
 constexpr int kStatusToken = 1 << OLIVE_ERR_TOKEN_RANGE;
 
 template <typename T>
@@ -101,21 +103,6 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// Item i of a launch: `per` heads of one token, all queries or all keys.
-struct Item {
-  int t, side, h0, h1;
-};
-__device__ __forceinline__ Item item_of(const QkArgs& p, long long i, int per, int nq, int nch) {
-  Item m;
-  m.t = static_cast<int>(i / nch);
-  int c = static_cast<int>(i - static_cast<long long>(m.t) * nch);
-  m.side = c >= nq;
-  if (m.side) c -= nq;
-  m.h0 = c * per;
-  m.h1 = min(m.h0 + per, p.heads[m.side]);
-  return m;
-}
-
 // Cosines and sines of a lane's pairs; `fine`: the position is inside the tables.
 __device__ __forceinline__ bool angles(const QkArgs& p, int t, const Place& q, bool report, float (&c)[4], float (&s)[4]) {
   const int pos = p.positions[t];
@@ -129,37 +116,53 @@ __device__ __forceinline__ bool angles(const QkArgs& p, int t, const Place& q, b
   return fine;
 }
 
+// Heads whose loads a thread has in flight together: 64 bytes of each operand.
+// Measured, us on 32768 tokens of 32 + 8 heads of 128, bf16: forward, 4 blocks an
+// SM, 117 with four heads, 130 with two; 128 with four and 3 blocks; backward 186
+// with four heads and 2 blocks, 201 with two and 3, 212 with one and 4.
+template <typename T>
+constexpr int at_once() {
+  return sizeof(T) == 2 ? 4 : 2;
+}
+
+// A group's heads: `per` of one token, all queries or all keys; chunk c of a
+// token's nch, the first nq of them queries.
 template <typename T, bool kInter, int L>
-__global__ void __launch_bounds__(kThreads) qk_fwd_kernel(const QkArgs p, int per, int nq, int nch) {
+__global__ void __launch_bounds__(kThreads, kFwdBlocks) qk_fwd_kernel(const QkArgs p, int per, int nq, int nch) {
   using V = Four<T>;
-  constexpr int kAtOnce = 4;  // heads whose loads are in flight together
+  constexpr int kAtOnce = at_once<T>();
   const int lane = threadIdx.x % L;
   const long long i = static_cast<long long>(blockIdx.x) * (kThreads / L) + threadIdx.x / L;
   const bool live = i < static_cast<long long>(p.T) * nch;
-  const Item m = item_of(p, live ? i : 0, per, nq, nch);
+  // (32-bit division where it is enough: the 64-bit one is a hundred instructions)
+  const int t = !live ? 0 : i >> 32 ? static_cast<int>(i / nch) : static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(nch));
+  int c0 = live ? static_cast<int>(i - static_cast<long long>(t) * nch) : 0;
+  const int side = c0 >= nq;
+  if (side) c0 -= nq;
+  const int h0 = c0 * per, h1 = live ? min(h0 + per, p.heads[side]) : h0;
   const Place q = place<kInter>(lane, p.D, p.R);
-  const HeadsView src = p.in[m.side], dst = p.out[m.side];
-  const T* x = static_cast<const T*>(src.x) + static_cast<int64_t>(m.t) * src.token_stride;
-  T* y = static_cast<T*>(const_cast<void*>(dst.x)) + static_cast<int64_t>(m.t) * dst.token_stride;
-  const T* w = static_cast<const T*>(p.w[m.side]);
+  const HeadsView src = p.in[side], dst = p.out[side];
+  const T* x = static_cast<const T*>(src.x) + t * src.token_stride;
+  T* y = static_cast<T*>(const_cast<void*>(dst.x)) + t * dst.token_stride;
+  const T* w = static_cast<const T*>(p.w[side]);
   const float inv_d = 1.f / p.D;
 
   float wa[4] = {}, wb[4] = {}, c[4] = {}, s[4] = {};
   bool fine = true;
-  for (int h = m.h0; __any_sync(0xffffffffu, live && h < m.h1); h += kAtOnce) {
+  for (int h = h0; __any_sync(0xffffffffu, h < h1); h += kAtOnce) {
     typename V::Raw ra[kAtOnce], rb[kAtOnce];
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      if (live && q.in && h + k < m.h1) {
-        const T* row = x + static_cast<int64_t>(h + k) * src.head_stride;
+      if (q.in && h + k < h1) {
+        const T* row = x + (h + k) * src.head_stride;
         ra[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
         rb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
       } else {
         ra[k] = rb[k] = typename V::Raw{};
       }
     }
-    if (h == m.h0 && live) {
-      fine = angles(p, m.t, q, lane == 0, c, s);
+    if (h == h0 && live) {
+      fine = angles(p, t, q, lane == 0, c, s);
       if (q.in) {
         V::get(*reinterpret_cast<const typename V::Raw*>(w + q.a), wa);
         V::get(*reinterpret_cast<const typename V::Raw*>(w + q.b), wb);
@@ -174,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) qk_fwd_kernel(const QkArgs p, int pe
 #pragma unroll
       for (int e = 0; e < 4; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
       ss = group_sum<L>(ss);
-      if (!(live && q.in && h + k < m.h1)) continue;
+      if (!(q.in && h + k < h1)) continue;
       float r = rsqrtf(fmaf(ss, inv_d, p.eps));
       if (!fine) r = __uint_as_float(0x7fffffffu);
 #pragma unroll
@@ -183,7 +186,7 @@ __global__ void __launch_bounds__(kThreads) qk_fwd_kernel(const QkArgs p, int pe
         b[e] = b[e] * r * wb[e];
       }
       if (q.turn) rotate<kInter>(a, b, c, s);
-      T* row = y + static_cast<int64_t>(h + k) * dst.head_stride;
+      T* row = y + (h + k) * dst.head_stride;
       *reinterpret_cast<typename V::Raw*>(row + q.a) = V::put(a);
       *reinterpret_cast<typename V::Raw*>(row + q.b) = V::put(b);
     }
@@ -192,65 +195,68 @@ __global__ void __launch_bounds__(kThreads) qk_fwd_kernel(const QkArgs p, int pe
 
 // Backward.  With n = x r (r the reciprocal root mean square) and dn the
 // gradient turned back, dx = r (dn w - n mean(dn w n)) and dw = sum of dn n over
-// all tokens and heads: sum(x^2) and sum(dn w x) come from one butterfly.  A
-// thread keeps the weight gradients of its eight columns over all its heads; the
-// block adds its threads' up and stores them, and a second launch adds the blocks'.
+// all tokens and heads: sum(x^2) and sum(dn w x) come from one butterfly.
+// A block works on queries (the first `bq` blocks) or keys alone, a group on one
+// chunk of the heads of every so-manieth token, so that a thread keeps the weight
+// gradients of its eight columns in registers from beginning to end; the block
+// adds its threads' up and stores them, and a second launch adds the blocks'.
 template <typename T, bool kInter, int L>
-__global__ void __launch_bounds__(kThreads) qk_bwd_kernel(const QkArgs p, int per, int nq, int nch) {
+__global__ void __launch_bounds__(kThreads, kBwdBlocks) qk_bwd_kernel(const QkArgs p, int per, int bq) {
   using V = Four<T>;
-  constexpr int kAtOnce = 2;
-  __shared__ float sums[kThreads / 32][2][8 * L];
+  constexpr int kAtOnce = at_once<T>();
+  __shared__ float sums[kThreads / 32][8 * L];
   const int lane = threadIdx.x % L;
   const Place q = place<kInter>(lane, p.D, p.R);
   const float inv_d = 1.f / p.D;
-  const long long items = static_cast<long long>(p.T) * nch;
-  const long long step = static_cast<long long>(gridDim.x) * (kThreads / L);
-  float w[2][8] = {}, dw[2][8] = {};
+  const int side = static_cast<int>(blockIdx.x) >= bq;
+  const int block = static_cast<int>(blockIdx.x) - (side ? bq : 0);
+  const int blocks = side ? static_cast<int>(gridDim.x) - bq : bq;
+  const int nch = (p.heads[side] + per - 1) / per;
+  const int group = block * (kThreads / L) + static_cast<int>(threadIdx.x) / L;
+  const int step = blocks * (kThreads / L) / nch;  // tokens worked on at once
+  const int chunk = group % nch;
+  const int h0 = chunk * per, h1 = min(h0 + per, p.heads[side]);
+  const HeadsView src = p.in[side], grd = p.grad[side], dst = p.out[side];
+
+  float w[8] = {}, dw[8] = {};
   if (q.in) {
+    const T* v = static_cast<const T*>(p.w[side]);
+    float a[4], b[4];
+    V::get(*reinterpret_cast<const typename V::Raw*>(v + q.a), a);
+    V::get(*reinterpret_cast<const typename V::Raw*>(v + q.b), b);
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      if (p.heads[side] == 0) continue;
-      const T* v = static_cast<const T*>(p.w[side]);
-      float a[4], b[4];
-      V::get(*reinterpret_cast<const typename V::Raw*>(v + q.a), a);
-      V::get(*reinterpret_cast<const typename V::Raw*>(v + q.b), b);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        w[side][e] = a[e];
-        w[side][4 + e] = b[e];
-      }
+    for (int e = 0; e < 4; ++e) {
+      w[e] = a[e];
+      w[4 + e] = b[e];
     }
   }
 
-  long long i = static_cast<long long>(blockIdx.x) * (kThreads / L) + threadIdx.x / L;
-  for (; __any_sync(0xffffffffu, i < items); i += step) {
-    const bool live = i < items;
-    const Item m = item_of(p, live ? i : 0, per, nq, nch);
-    const HeadsView src = p.in[m.side], grd = p.grad[m.side], dst = p.out[m.side];
-    const T* x = static_cast<const T*>(src.x) + static_cast<int64_t>(m.t) * src.token_stride;
-    const T* g = static_cast<const T*>(grd.x) + static_cast<int64_t>(m.t) * grd.token_stride;
-    T* y = static_cast<T*>(const_cast<void*>(dst.x)) + static_cast<int64_t>(m.t) * dst.token_stride;
-    float c[4] = {}, s[4] = {}, acc[8] = {}, wm[8];
+  // (groups beyond the last whole set of chunks have no token)
+  for (int t = group / nch < step ? group / nch : p.T; __any_sync(0xffffffffu, t < p.T); t = t < p.T - step ? t + step : p.T) {
+    const bool live = t < p.T;
+    const int tt = live ? t : 0, he = live ? h1 : h0;
+    const T* x = static_cast<const T*>(src.x) + tt * src.token_stride;
+    const T* g = static_cast<const T*>(grd.x) + tt * grd.token_stride;
+    T* y = static_cast<T*>(const_cast<void*>(dst.x)) + tt * dst.token_stride;
+    float c[4] = {}, s[4] = {};
     bool fine = true;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) wm[e] = m.side ? w[1][e] : w[0][e];
-    for (int h = m.h0; __any_sync(0xffffffffu, live && h < m.h1); h += kAtOnce) {
+    for (int h = h0; __any_sync(0xffffffffu, h < he); h += kAtOnce) {
       typename V::Raw xa[kAtOnce], xb[kAtOnce], ga[kAtOnce], gb[kAtOnce];
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
-        if (live && q.in && h + k < m.h1) {
-          const T* row = x + static_cast<int64_t>(h + k) * src.head_stride;
+        if (q.in && h + k < he) {
+          const T* row = x + (h + k) * src.head_stride;
           xa[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
           xb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
-          row = g + static_cast<int64_t>(h + k) * grd.head_stride;
+          row = g + (h + k) * grd.head_stride;
           ga[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
           gb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
         } else {
           xa[k] = xb[k] = ga[k] = gb[k] = typename V::Raw{};
         }
       }
-      if (h == m.h0 && live) {
-        fine = angles(p, m.t, q, lane == 0, c, s);
+      if (h == h0 && live) {
+        fine = angles(p, t, q, lane == 0, c, s);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] = -s[e];
       }
@@ -279,14 +285,14 @@ __global__ void __launch_bounds__(kThreads) qk_bwd_kernel(const QkArgs p, int pe
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           ss = fmaf(v[e], v[e], ss);
-          dot = fmaf(d[e] * wm[e], v[e], dot);
+          dot = fmaf(d[e] * w[e], v[e], dot);
         }
 #pragma unroll
         for (int o = L / 2; o > 0; o >>= 1) {
           ss += __shfl_xor_sync(0xffffffffu, ss, o);
           dot += __shfl_xor_sync(0xffffffffu, dot, o);
         }
-        if (!(live && q.in && h + k < m.h1)) continue;
+        if (!(q.in && h + k < he)) continue;
         float r = rsqrtf(fmaf(ss, inv_d, p.eps));
         if (!fine) r = __uint_as_float(0x7fffffffu);
         const float mean = dot * r * inv_d;  // mean(dn w n)
@@ -294,59 +300,57 @@ __global__ void __launch_bounds__(kThreads) qk_bwd_kernel(const QkArgs p, int pe
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float n = v[e] * r;
-          acc[e] = fmaf(d[e], n, acc[e]);
-          const float o = r * fmaf(-n, mean, d[e] * wm[e]);
+          dw[e] = fmaf(d[e], n, dw[e]);
+          const float o = r * fmaf(-n, mean, d[e] * w[e]);
           if (e < 4)
             a[e] = o;
           else
             b[e - 4] = o;
         }
-        T* row = y + static_cast<int64_t>(h + k) * dst.head_stride;
+        T* row = y + (h + k) * dst.head_stride;
         *reinterpret_cast<typename V::Raw*>(row + q.a) = V::put(a);
         *reinterpret_cast<typename V::Raw*>(row + q.b) = V::put(b);
       }
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      dw[0][e] += m.side ? 0.f : acc[e];
-      dw[1][e] += m.side ? acc[e] : 0.f;
-    }
   }
+  grid_launch_dependents();
 
   // the warp's groups, then the block's warps
 #pragma unroll
-  for (int side = 0; side < 2; ++side)
+  for (int e = 0; e < 8; ++e) {
+    float v = dw[e];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float v = dw[side][e];
-#pragma unroll
-      for (int o = 16; o >= L; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (threadIdx.x % 32 < L && q.in) sums[threadIdx.x / 32][side][(e < 4 ? q.a : q.b - 4) + e] = v;
-    }
+    for (int o = 16; o >= L; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (threadIdx.x % 32 < L && q.in) sums[threadIdx.x / 32][(e < 4 ? q.a : q.b - 4) + e] = v;
+  }
   __syncthreads();
-  float* part = static_cast<float*>(p.ws) + static_cast<size_t>(blockIdx.x) * 2 * p.D;
-  for (int k = threadIdx.x; k < 2 * p.D; k += kThreads) {
-    const int side = k >= p.D, col = k - side * p.D;
+  float* part = static_cast<float*>(p.ws) + static_cast<size_t>(blockIdx.x) * p.D;
+  for (int col = threadIdx.x; col < p.D; col += kThreads) {
     float v = 0.f;
 #pragma unroll
-    for (int wp = 0; wp < kThreads / 32; ++wp) v += sums[wp][side][col];
-    part[k] = v;
+    for (int wp = 0; wp < kThreads / 32; ++wp) v += sums[wp][col];
+    part[col] = v;
   }
 }
 
-// dw[side][col] = sum over the blocks, 32 columns a block, in a fixed order.
-__global__ void __launch_bounds__(256) qk_dw_kernel(const float* part, int blocks, int D, float* dw_q, float* dw_k) {
-  __shared__ double sums[8][32];
-  const int col = blockIdx.x * 32 + threadIdx.x % 32, g = threadIdx.x / 32;
+// dw of a side (blockIdx.y) = sum over its blocks, 32 columns a block, in a fixed
+// order.
+__global__ void __launch_bounds__(1024) qk_dw_kernel(const float* part, int bq, int blocks, int D, float* dw_q, float* dw_k) {
+  __shared__ double sums[32][32];
+  grid_wait();
+  const int lane = threadIdx.x % 32, g = threadIdx.x / 32, col = blockIdx.x * 32 + lane;
+  const int b0 = blockIdx.y ? bq : 0, b1 = blockIdx.y ? blocks : bq;
   double v = 0.0;
-  if (col < 2 * D)
-    for (int b = g; b < blocks; b += 8) v += static_cast<double>(part[static_cast<size_t>(b) * 2 * D + col]);
-  sums[g][threadIdx.x % 32] = v;
+  if (col < D) {
+#pragma unroll 4
+    for (int b = b0 + g; b < b1; b += 32) v += static_cast<double>(part[static_cast<size_t>(b) * D + col]);
+  }
+  sums[g][lane] = v;
   __syncthreads();
-  if (g == 0 && col < 2 * D) {
+  if (g == 0 && col < D) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += sums[i][threadIdx.x];
-    (col < D ? dw_q[col] : dw_k[col - D]) = static_cast<float>(v);
+    for (int i = 1; i < 32; ++i) v += sums[i][lane];
+    (blockIdx.y ? dw_k : dw_q)[col] = static_cast<float>(v);
   }
 }
 
@@ -379,16 +383,34 @@ void run_fwd(const Ctx& c, const QkArgs& a) {
 
 template <typename T, bool kInter, int L>
 void run_bwd(const Ctx& c, const QkArgs& a) {
+  const int groups = kThreads / L;
   const int64_t heads = static_cast<int64_t>(a.T) * (a.heads[0] + a.heads[1]);
-  const int64_t room = static_cast<int64_t>(c.num_sms) * 1024 / L;
-  const int per = heads >= 8 * room ? 8 : heads >= 2 * room ? 2 : 1;
-  const int nq = static_cast<int>(ceil_div(a.heads[0], per));
-  const int nch = nq + static_cast<int>(ceil_div(a.heads[1], per));
-  const int64_t want = ceil_div(static_cast<int64_t>(a.T) * nch, kThreads / L);
-  const int blocks = static_cast<int>(std::min<int64_t>(want, std::min(4 * c.num_sms, kMaxBwdBlocks)));
-  if (blocks > 0) qk_bwd_kernel<T, kInter, L><<<blocks, kThreads, 0, c.stream>>>(a, per, nq, nch);
-  qk_dw_kernel<<<static_cast<int>(ceil_div(2 * a.D, 32)), 256, 0, c.stream>>>(
-      static_cast<const float*>(a.ws), blocks, a.D, a.dw[0], a.dw[1]);
+  // several heads a group where there are enough of them to fill the GPU anyway
+  const int64_t room = static_cast<int64_t>(c.num_sms) * kBwdBlocks * groups;
+  const int per = heads >= 16 * room ? 8 : heads >= 4 * room ? 4 : heads >= 2 * room ? 2 : 1;
+  const int most = std::min(kBwdBlocks * c.num_sms, kMaxBwdBlocks);  // as many as run at once
+  // blocks of a side: its share, at least one token's chunks
+  int blocks[2] = {0, 0};
+  for (int s = 0; s < 2 && a.T > 0; ++s) {
+    if (a.heads[s] == 0) continue;
+    const int64_t nch = ceil_div(a.heads[s], per);
+    const int64_t share = std::max<int64_t>(1, static_cast<int64_t>(most) * a.heads[s] / (a.heads[0] + a.heads[1]));
+    const int64_t least = ceil_div(nch, groups);
+    blocks[s] = static_cast<int>(std::max(least, std::min(share, ceil_div(a.T * nch, groups))));
+  }
+  const int all = blocks[0] + blocks[1];
+  if (all > 0) qk_bwd_kernel<T, kInter, L><<<all, kThreads, 0, c.stream>>>(a, per, blocks[0]);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(ceil_div(a.D, 32)), 2);
+  cfg.blockDim = dim3(1024);
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaLaunchKernelEx(&cfg, qk_dw_kernel, static_cast<const float*>(a.ws), blocks[0], all, static_cast<int>(a.D),
+                     a.dw[0], a.dw[1]);
 }
 
 template <bool kBwd, typename T, bool kInter>
@@ -419,7 +441,7 @@ olive_status by_type(const Ctx& c, const QkArgs& a) {
 
 }  // namespace
 
-size_t qk_bwd_ws_bytes(int64_t D) { return align_up(4ull * kMaxBwdBlocks * 2 * D, kWsAlign); }
+size_t qk_bwd_ws_bytes(int64_t D) { return align_up(4ull * kMaxBwdBlocks * D, kWsAlign); }
 
 olive_status launch_qk_fwd(const Ctx& c, const QkArgs& a) { return by_type<false>(c, a); }
 
