@@ -8,7 +8,9 @@ or fails to load, every call raises.
 
 from __future__ import annotations
 
+import array
 import ctypes
+import functools
 import os
 import re
 
@@ -603,42 +605,77 @@ def olive_packed_positions(cu_seqlens, T_cap: int, out=None):
     return out
 
 
-def _heads(t, T, D, dtype, name, device):
-    """(pointer, token stride, head stride) of a [T, H, D] view with contiguous heads."""
+# Small calls are bound by the host (a launch is 2.5 us on the GB300's, an attribute
+# of a tensor 0.07): the calls below look at each tensor once, in one expression, and
+# name what is wrong only when something is.
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+@functools.lru_cache(maxsize=4096)
+def _ws_bytes(op, T, d, V, grad, grad_dtype):
+    return int(lib().olive_workspace_size(op, T, d, 0, V, grad, grad_dtype))
+
+
+def _bytes(n, dev):
+    return torch.empty(n, dtype=torch.uint8, device=dev)
+
+
+def _refuse_heads(t, T, H, D, dtype, name, device):
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
         raise TypeError(f"{name} must be a CUDA {dtype} tensor on {device}")
-    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D:
-        raise ValueError(f"{name} must have the shape [{T}, heads, {D}]")
-    a, b, c = t.stride()
-    if c != 1 and D > 1:
-        raise TypeError(f"{name}: the {D} values of a head must be contiguous")
+    if t.shape != (T, H, D):
+        raise ValueError(f"{name} must have the shape [{T}, {H}, {D}]")
+    raise TypeError(f"{name}: the {D} values of a head must be contiguous")
+
+
+def _heads(t, shape, dtype, name, device):
+    """Pointer, token stride and head stride of a view [T, H, D] with contiguous heads."""
+    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or
+            t.stride(2) != 1 or t.device != device):
+        _refuse_heads(t, *shape, dtype, name, device)
+    T, H, _ = shape
     # (the stride of a dimension of one entry means nothing)
-    return t.data_ptr(), a if T > 1 else 0, b if t.shape[1] > 1 else 0
+    return t.data_ptr(), t.stride(0) if T > 1 else 0, t.stride(1) if H > 1 else 0
 
 
 def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
     """Checks what the heads' forward and backward share; (views of q and k, the
-    shared C arguments, T, D, dtype)."""
-    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dtype not in DTYPE or q.dim() != 3:
-        raise TypeError("q must be a CUDA bf16 or fp32 tensor [T, heads, D]")
-    T, Hq, D = q.shape
-    dtype, dev = q.dtype, q.device
-    vq, vk = _heads(q, T, D, dtype, "q", dev), _heads(k, T, D, dtype, "k", dev)
+    shared C arguments, their shapes, dtype, device)."""
+    if (not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or not q.is_cuda or
+            q.dtype not in DTYPE or q.dim() != 3 or k.dim() != 3):
+        raise TypeError("q and k must be CUDA bf16 or fp32 tensors [T, heads, D]")
+    sq, sk, dtype, dev = q.shape, k.shape, q.dtype, q.device
+    T, Hq, D = sq
+    if sk[0] != T or sk[2] != D:
+        raise ValueError(f"k must have the shape [{T}, heads, {D}]")
+    vq, vk = _heads(q, sq, dtype, "q", dev), _heads(k, sk, dtype, "k", dev)
     for t, n in ((w_q, "w_q"), (w_k, "w_k")):
         _need(t, dtype, n)
         if t.numel() != D:
             raise ValueError(f"{n} must hold {D} values")
-    _need(cos, torch.float32, "cos")
-    _need(sin, torch.float32, "sin")
-    _need(positions, torch.int32, "positions")
+    _need(cos, _F32, "cos")
+    _need(sin, _F32, "sin")
+    _need(positions, _I32, "positions")
     if cos.dim() != 2 or cos.shape != sin.shape:
         raise ValueError("cos and sin must have the same shape [P, R/2]")
     if positions.numel() != T:
         raise ValueError(f"positions must hold {T} values")
     P, half = cos.shape
-    common = (Hq, k.shape[1], w_q.data_ptr(), w_k.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(),
+    common = (Hq, sk[1], w_q.data_ptr(), w_k.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(),
               positions.data_ptr(), P, T, D, 2 * half, 1 if interleaved else 0)
-    return vq, vk, common, T, D, dtype
+    return vq, vk, common, sq, sk, dtype, dev
+
+
+def _qk_out(out, sq, sk, dtype, dev):
+    """The outputs and their views: contiguous ones where none are given."""
+    if out is None:
+        yq = torch.empty(sq, dtype=dtype, device=dev)
+        yk = torch.empty(sk, dtype=dtype, device=dev)
+        _, Hq, D = sq
+        Hk = sk[1]
+        return yq, yk, (yq.data_ptr(), Hq * D, D), (yk.data_ptr(), Hk * D, D)
+    yq, yk = out
+    return yq, yk, _heads(yq, sq, dtype, "q's output", dev), _heads(yk, sk, dtype, "k's output", dev)
 
 
 def olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps: float = 1e-6,
@@ -647,18 +684,12 @@ def olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps: float = 1e-
     [D]) and rotation by positions [T] with the tables cos, sin (fp32 [P, R/2];
     R <= D).  q and k may be views of one projection.  Returns (q_out, k_out),
     contiguous unless given as `out` (views, or q and k themselves)."""
-    vq, vk, common, T, D, dtype = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
-    if out is None:
-        out = (torch.empty(q.shape, dtype=dtype, device=q.device),
-               torch.empty(k.shape, dtype=dtype, device=q.device))
-    yq, yk = out
-    if yq.shape != q.shape or yk.shape != k.shape:
-        raise ValueError("outputs must have the shapes of q and k")
-    st = lib().olive_qk_norm_rope_fwd(*vq, *vk, *common,
-                                      *_heads(yq, T, D, dtype, "q_out", q.device),
-                                      *_heads(yk, T, D, dtype, "k_out", q.device), DTYPE[dtype],
-                                      _ptr(dev_status), _stream())
-    _check(st, "olive_qk_norm_rope_fwd")
+    vq, vk, common, sq, sk, dtype, dev = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    yq, yk, oq, ok = _qk_out(out, sq, sk, dtype, dev)
+    st = lib().olive_qk_norm_rope_fwd(*vq, *vk, *common, *oq, *ok, DTYPE[dtype], _ptr(dev_status),
+                                      _stream())
+    if st:
+        _check(st, "olive_qk_norm_rope_fwd")
     return yq, yk
 
 
@@ -667,32 +698,24 @@ def olive_qk_norm_rope_bwd(g_q, g_k, q, k, w_q, w_k, cos, sin, positions, eps: f
     """Gradients of olive_qk_norm_rope_fwd for its inputs q, k and the gradients
     g_q, g_k of its outputs.  Returns (d_q, d_k, dw_q, dw_k), the weights' in fp32;
     `out` takes (d_q, d_k), e.g. views of one projection's gradient."""
-    vq, vk, common, T, D, dtype = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
-    dev = q.device
-    if g_q.shape != q.shape or g_k.shape != k.shape:
-        raise ValueError("g_q and g_k must have the shapes of q and k")
-    if out is None:
-        out = (torch.empty(q.shape, dtype=dtype, device=dev), torch.empty(k.shape, dtype=dtype, device=dev))
-    dq, dk = out
-    if dq.shape != q.shape or dk.shape != k.shape:
-        raise ValueError("outputs must have the shapes of q and k")
-    dw = torch.empty(2, D, dtype=torch.float32, device=dev)
+    vq, vk, common, sq, sk, dtype, dev = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    gq, gk = _heads(g_q, sq, dtype, "g_q", dev), _heads(g_k, sk, dtype, "g_k", dev)
+    dq, dk, oq, ok = _qk_out(out, sq, sk, dtype, dev)
+    D = sq[2]
+    dwq, dwk = torch.empty(D, dtype=_F32, device=dev), torch.empty(D, dtype=_F32, device=dev)
     if ws is None:
-        ws = workspace(lib().olive_workspace_size(OP["qk_norm_rope_bwd"], 1, D, 0, 1, 0, 0), dev)
-    dwq, dwk = dw[0], dw[1]
-    st = lib().olive_qk_norm_rope_bwd(*_heads(g_q, T, D, dtype, "g_q", dev),
-                                      *_heads(g_k, T, D, dtype, "g_k", dev), *vq, *vk, *common,
-                                      *_heads(dq, T, D, dtype, "d_q", dev),
-                                      *_heads(dk, T, D, dtype, "d_k", dev), dwq.data_ptr(),
-                                      dwk.data_ptr(), DTYPE[dtype], _ptr(ws), ws.numel(),
+        ws = _bytes(_ws_bytes(12, 1, D, 1, 0, 0), dev)
+    st = lib().olive_qk_norm_rope_bwd(*gq, *gk, *vq, *vk, *common, *oq, *ok, dwq.data_ptr(),
+                                      dwk.data_ptr(), DTYPE[dtype], ws.data_ptr(), ws.numel(),
                                       _ptr(dev_status), _stream())
-    _check(st, "olive_qk_norm_rope_bwd")
+    if st:
+        _check(st, "olive_qk_norm_rope_bwd")
     return dq, dk, dwq, dwk
 
 
 def _mlp_args(x, W_gate, W_up, W_down):
     for t, n in ((x, "x"), (W_gate, "W_gate"), (W_up, "W_up"), (W_down, "W_down")):
-        _need(t, torch.bfloat16, n)
+        _need(t, _BF16, n)
     if x.dim() != 2:
         raise ValueError("x must have the shape [T, d]")
     T, d = x.shape
@@ -712,22 +735,23 @@ def olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual=None, act: str = "silu
     T, d, f = _mlp_args(x, W_gate, W_up, W_down)
     dev = x.device
     if residual is not None:
-        _need(residual, torch.bfloat16, "residual")
+        _need(residual, _BF16, "residual")
         if residual.shape != x.shape:
             raise ValueError("residual must have the shape of x")
     if out is None:
-        out = torch.empty(T, d, dtype=torch.bfloat16, device=dev)
+        out = torch.empty((T, d), dtype=_BF16, device=dev)
     else:
-        _need(out, torch.bfloat16, "out")
+        _need(out, _BF16, "out")
         if out.shape != x.shape:
             raise ValueError("out must have the shape of x")
-    saved = torch.empty(2, T, f, dtype=torch.int16, device=dev) if save else None
-    if ws is None and T > 0:
-        ws = workspace(lib().olive_workspace_size(OP["gated_mlp_fwd"], T, d, 0, f, 0, 0), dev)
-    st = lib().olive_gated_mlp_fwd(_ptr(x), _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(residual),
-                                   T, d, f, ACT[act], _ptr(out), _ptr(saved), _ptr(ws),
-                                   0 if ws is None else ws.numel(), _ptr(dev_status), _stream())
-    _check(st, "olive_gated_mlp_fwd")
+    saved = torch.empty((2, T, f), dtype=torch.int16, device=dev) if save else None
+    if ws is None:
+        ws = _bytes(_ws_bytes(10, T, d, f, 0, 0), dev)
+    st = lib().olive_gated_mlp_fwd(x.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(),
+                                   _ptr(residual), T, d, f, ACT[act], out.data_ptr(), _ptr(saved),
+                                   ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream())
+    if st:
+        _check(st, "olive_gated_mlp_fwd")
     return out, saved
 
 
@@ -738,28 +762,46 @@ def olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, act: str = "silu",
     (dx, dW_gate, dW_up, dW_down) of grad_dtype, None for what is not needed."""
     T, d, f = _mlp_args(x, W_gate, W_up, W_down)
     dev = x.device
-    _need(dy, torch.bfloat16, "dy")
+    _need(dy, _BF16, "dy")
     _need(saved, torch.int16, "saved")
     if dy.shape != x.shape or saved.shape != (2, T, f):
         raise ValueError("dy must have the shape of x, saved that of the forward")
     if out is None:
-        e = lambda *shape: torch.empty(*shape, dtype=grad_dtype, device=dev)
-        out = ((e(T, d) if need_dx else None,) +
-               ((e(f, d), e(f, d), e(d, f)) if need_dW else (None, None, None)))
+        dx = torch.empty((T, d), dtype=grad_dtype, device=dev) if need_dx else None
+        dg = du = dd = None
+        if need_dW:
+            dg = torch.empty((f, d), dtype=grad_dtype, device=dev)
+            du = torch.empty((f, d), dtype=grad_dtype, device=dev)
+            dd = torch.empty((d, f), dtype=grad_dtype, device=dev)
     else:
-        for t, shape in zip(out, ((T, d), (f, d), (f, d), (d, f))):
+        dx, dg, du, dd = out
+        for t, shape in ((dx, (T, d)), (dg, (f, d)), (du, (f, d)), (dd, (d, f))):
             if t is not None:
                 _need(t, grad_dtype, "out")
                 if t.shape != shape:
                     raise ValueError("out must have the shapes of x and the weights")
-    if ws is None and T > 0:
-        ws = workspace(lib().olive_workspace_size(OP["gated_mlp_bwd"], T, d, 0, f, 1, DTYPE[grad_dtype]), dev)
-    st = lib().olive_gated_mlp_bwd(_ptr(dy), _ptr(x), _ptr(W_gate), _ptr(W_up), _ptr(W_down),
-                                   _ptr(saved), T, d, f, ACT[act], *[_ptr(t) for t in out],
-                                   DTYPE[grad_dtype], _ptr(ws), 0 if ws is None else ws.numel(),
+    kind = DTYPE[grad_dtype]
+    if ws is None:
+        ws = _bytes(_ws_bytes(11, T, d, f, 1, kind), dev)
+    st = lib().olive_gated_mlp_bwd(dy.data_ptr(), x.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(),
+                                   W_down.data_ptr(), saved.data_ptr(), T, d, f, ACT[act], _ptr(dx),
+                                   _ptr(dg), _ptr(du), _ptr(dd), kind, ws.data_ptr(), ws.numel(),
                                    _ptr(dev_status), _stream())
-    _check(st, "olive_gated_mlp_bwd")
-    return tuple(out)
+    if st:
+        _check(st, "olive_gated_mlp_bwd")
+    return dx, dg, du, dd
+
+
+def _grad_list(tensors, cur, what):
+    """Pointers, element counts and dtypes of contiguous tensors on device `cur`."""
+    try:
+        kinds = [DTYPE[t.dtype] for t in tensors]
+    except (KeyError, AttributeError):
+        raise TypeError(f"{what} must be bf16 or fp32 tensors") from None
+    for i, t in enumerate(tensors):
+        if not t.is_contiguous() or t.get_device() != cur:
+            raise TypeError(f"{what} {i} must be contiguous and on the current CUDA device")
+    return [t.data_ptr() for t in tensors], [t.numel() for t in tensors], kinds
 
 
 def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
@@ -769,34 +811,36 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     all (out=None: only the norm)."""
     n = len(grads)
     cur = torch.cuda.current_device()
-    src = (_P * n)()
-    dst = (_P * n)() if out is not None else None
-    num = (_L * n)()
-    kind = (_I * n)()
-    inplace = isinstance(out, str)
-    if inplace and out != "inplace" or not inplace and out is not None and len(out) != n:
-        raise ValueError('out must be "inplace", None or a list of as many tensors as grads')
-    for i, g in enumerate(grads):
-        dt = DTYPE.get(g.dtype)
-        if dt is None or g.get_device() != cur or not g.is_contiguous():
-            raise TypeError(f"gradient {i} must be a contiguous bf16 or fp32 CUDA tensor on the "
-                            "current device")
-        src[i] = g.data_ptr()
-        num[i] = g.numel()
-        kind[i] = dt
-        if out is not None:
-            o = g if inplace else out[i]
-            if not inplace and (o.dtype != g.dtype or o.shape != g.shape or not o.is_contiguous() or
-                                o.get_device() != cur):
-                raise TypeError(f"out {i} must be like its gradient")
-            dst[i] = o.data_ptr()
+    src, num, kinds = _grad_list(grads, cur, "gradients")
+    dst = None
+    if out is not None:
+        if isinstance(out, str):
+            if out != "inplace":
+                raise ValueError('out must be "inplace", None or a list of as many tensors as grads')
+            dst = src
+        else:
+            if len(out) != n:
+                raise ValueError('out must be "inplace", None or a list of as many tensors as grads')
+            dst, sizes, types = _grad_list(out, cur, "out")
+            if sizes != num or types != kinds:
+                raise TypeError("out must be like the gradients")
     if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device="cuda")
+        norm = torch.empty(1, dtype=_F32, device="cuda")
+    else:
+        _need(norm, _F32, "norm")
     if ws is None:
-        ws = workspace(lib().olive_workspace_size(OP["grad_clip"], max(n, 1), 0, 0, 1, 0, 0))
-    st = lib().olive_grad_clip(src, dst, num, kind, n, float(max_norm), norm.data_ptr(),
-                               ws.data_ptr(), ws.numel(), _stream())
-    _check(st, "olive_grad_clip")
+        ws = _bytes(_ws_bytes(13, max(n, 1), 0, 1, 0, 0), "cuda")
+    # the four host arrays behind one another
+    table = array.array("Q", src)
+    table.extend(dst or ())
+    table.extend(num)
+    at, count = table.buffer_info()
+    kind = array.array("i", kinds)
+    st = lib().olive_grad_clip(at, at + 8 * n if dst is not None else None, at + 8 * (count - n),
+                               kind.buffer_info()[0], n, max_norm, norm.data_ptr(), ws.data_ptr(),
+                               ws.numel(), _stream())
+    if st:
+        _check(st, "olive_grad_clip")
     return norm
 
 
