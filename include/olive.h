@@ -613,7 +613,7 @@ OLIVE_API olive_status olive_qk_norm_rope_bwd(
  * large an error on the gradients as rounding them to bf16 operands does.
  * Magnitudes below 2^-30 lose accuracy and vanish below 2^-39; those above
  * 2^33 are held as 2^33, infinities and NaN become NaN.)
- * T >= 0 (0: nothing happens), d and f multiples of 8.  dev_status may be NULL.
+ * 0 <= T <= 2^30 (0: nothing happens), d and f multiples of 8.  dev_status may be NULL.
  * workspace: olive_workspace_size(OLIVE_OP_GATED_MLP_FWD, T, d, 0, f, 0, 0) bytes.
  */
 OLIVE_API olive_status olive_gated_mlp_fwd(const void* x, const void* W_gate, const void* W_up,
@@ -631,7 +631,7 @@ OLIVE_API olive_status olive_gated_mlp_fwd(const void* x, const void* W_gate, co
  * dy, x bf16 [T, d]; dx [T, d] and the weights' gradients (shaped as the
  * weights) of grad_dtype.  dx may be NULL, and so may the three weights'
  * gradients together: what is NULL is not computed (not everything may be).
- * T >= 0 (0: the weights' gradients are zeroed).  workspace:
+ * 0 <= T <= 2^30 (0: the weights' gradients are zeroed).  workspace:
  * olive_workspace_size(OLIVE_OP_GATED_MLP_BWD, T, d, 0, f, 1, grad_dtype) bytes.
  */
 OLIVE_API olive_status olive_gated_mlp_bwd(const void* dy, const void* x, const void* W_gate,

@@ -285,11 +285,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
     }
-    if (!ok && lane == 0) {
-      // let copies already issued land before the CTA retires
-      const uint64_t t0 = global_timer_ns();
-      while (global_timer_ns() - t0 < 50000) nanosleep_ns(1000);
-    }
     __syncwarp();
   } else if (warp == kMmaWarp) {
     if (rank == 0) {
@@ -563,14 +558,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (!ok && lane == 0) {
-      const uint64_t t0 = global_timer_ns();  // pieces in flight land
-      while (global_timer_ns() - t0 < 50000) nanosleep_ns(1000);
-    }
     __syncwarp();
   }
 
   tc_fence_before();
+  __syncthreads();
+  // a wait ran out: copies in flight, to this CTA or counted on its peer's
+  // barriers, land before either retires
+  if (*abort_flag) let_copies_land();
   // the pair's MMAs are complete and every access to the peer's barriers is
   // over before either CTA frees its TMEM
   cluster_sync_all();
@@ -665,13 +660,14 @@ Plan plan_tiles(const MlpParams& p, int mode, int bn, int pairs) {
   }
   Plan w{bn, std::min(pairs, all), {}, 0};
   w.cut.run = 1;
-  // whole, in turn: the pair with the most to do
-  for (int r = 0; r < w.pairs; ++r) {
+  // whole, in turn: the pair with the most to do.  A product's last tiles go to
+  // neighbouring pairs, one each, from the pair on that its first tile went to; so
+  // the most is found at one of those pairs.
+  for (int j = 0, from = 0; j < p.n_prob; from = (from + tiles[j++]) % pairs) {
     double load = 0;
-    int first = 0;
-    for (int i = 0; i < p.n_prob; first += tiles[i++]) {
-      const int skip = ((r - first) % pairs + pairs) % pairs;  // to this pair's first tile of the product
-      if (skip < tiles[i]) load += static_cast<double>(ceil_div(tiles[i] - skip, pairs)) * ns[i];
+    for (int i = 0, first = 0; i < p.n_prob; first = (first + tiles[i++]) % pairs) {
+      const int skip = from >= first ? from - first : from - first + pairs;
+      load += (tiles[i] / pairs + (skip < tiles[i] % pairs ? 1 : 0)) * ns[i];
     }
     w.ns = std::max(w.ns, load);
   }

@@ -145,11 +145,6 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
       }
       if (++s == p.stages) { s = 0; phase ^= 1u; }
     }
-    if (!ok && lane == 0) {
-      // let copies already issued land before the CTA retires
-      const uint64_t w = global_timer_ns();
-      while (global_timer_ns() - w < 50000) nanosleep_ns(1000);
-    }
     __syncwarp();
   } else if (warp == kMmaWarp) {
     const bool leader = elect_one();
@@ -186,6 +181,8 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
     tc_fence_after();
   }
 
+  __syncthreads();
+  if (*abort_flag) let_copies_land();  // a wait ran out: the stages may still be written
   // epilogue warp w: weight rows 32 (w % 4).. of the accumulators and half w / 4
   // of the tokens, 8 at a time
   const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);

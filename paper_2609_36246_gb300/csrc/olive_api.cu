@@ -349,8 +349,10 @@ static MlpWs carve_mlp_impl(void* ws, int64_t T, int64_t f, bool bwd, size_t* to
     w.dg = c.take(rows);
     w.du = c.take(rows);
   }
-  w.part = static_cast<float*>(c.take(mlp_part_bytes()));
-  w.flag = static_cast<uint32_t*>(c.take(2 * 4 * mlp_flag_words()));
+  if (bwd || T > kMlpFewRows) {
+    w.part = static_cast<float*>(c.take(mlp_part_bytes()));
+    w.flag = static_cast<uint32_t*>(c.take(2 * 4 * mlp_flag_words()));
+  }
   if (total) *total = c.off;
   return w;
 }
@@ -380,6 +382,7 @@ olive_status check_ws(void* ws, size_t have, size_t need) {
 
 constexpr int32_t kMaxHeadDim = 256;
 constexpr int32_t kMaxHeads = 4096;
+constexpr int32_t kMaxMlpRows = 1 << 30;  // row indices of its last tile stay in 31 bits
 
 bool width_ok(int32_t d) { return d >= 8 && d <= kMaxDim && (d % 8) == 0; }
 
@@ -427,7 +430,7 @@ size_t olive_workspace_size(int op, int32_t T, int32_t d, int32_t d_t, int32_t V
   switch (op) {
     case OLIVE_OP_GATED_MLP_FWD:
     case OLIVE_OP_GATED_MLP_BWD:
-      if (!width_ok(V)) return 0;
+      if (!width_ok(V) || T > kMaxMlpRows) return 0;
       return mlp_ws_bytes(T, V, op == OLIVE_OP_GATED_MLP_BWD);
     case OLIVE_OP_LOGPROB_FWD: return fwd_ws_bytes(T, d);
     case OLIVE_OP_LOSS_BWD:
@@ -878,7 +881,7 @@ olive_status olive_gated_mlp_fwd(const void* x, const void* W_gate, const void* 
                                  size_t ws_bytes, int32_t* dev_status, void* stream) {
   if (!W_gate || !W_up || !W_down) return OLIVE_ERR_INVALID_ARG;
   if (activation != OLIVE_ACT_SILU && activation != OLIVE_ACT_GELU_TANH) return OLIVE_ERR_INVALID_ARG;
-  if (T < 0 || d < 1 || d > kMaxDim || f < 1 || f > kMaxDim) return OLIVE_ERR_SHAPE;
+  if (T < 0 || T > kMaxMlpRows || d < 1 || d > kMaxDim || f < 1 || f > kMaxDim) return OLIVE_ERR_SHAPE;
   if (d % 8 != 0 || f % 8 != 0 || !aligned16(W_gate) || !aligned16(W_up) || !aligned16(W_down))
     return OLIVE_ERR_ALIGNMENT;
   olive_status st = OLIVE_OK;
@@ -907,7 +910,7 @@ olive_status olive_gated_mlp_bwd(const void* dy, const void* x, const void* W_ga
   if ((dW_gate == nullptr) != (dW_up == nullptr) || (dW_gate == nullptr) != (dW_down == nullptr) ||
       (!dx && !dW_gate && T > 0))
     return OLIVE_ERR_INVALID_ARG;
-  if (T < 0 || d < 1 || d > kMaxDim || f < 1 || f > kMaxDim) return OLIVE_ERR_SHAPE;
+  if (T < 0 || T > kMaxMlpRows || d < 1 || d > kMaxDim || f < 1 || f > kMaxDim) return OLIVE_ERR_SHAPE;
   if (d % 8 != 0 || f % 8 != 0 || !aligned16(W_gate) || !aligned16(W_up) || !aligned16(W_down) ||
       !aligned16(dW_gate) || !aligned16(dW_up) || !aligned16(dW_down))
     return OLIVE_ERR_ALIGNMENT;

@@ -355,8 +355,9 @@ __global__ void __launch_bounds__(1024) qk_dw_kernel(const float* part, int bq, 
 }
 
 __global__ void positions_kernel(const int32_t* cu, int S, int T_cap, int32_t* positions) {
-  const int t = blockIdx.x * blockDim.x + threadIdx.x;
-  if (t >= T_cap) return;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (at >= T_cap) return;
+  const int t = static_cast<int>(at);
   int lo = 0, hi = S;  // the last s with cu[s] <= t
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
@@ -370,11 +371,12 @@ __global__ void positions_kernel(const int32_t* cu, int S, int T_cap, int32_t* p
 
 template <typename T, bool kInter, int L>
 void run_fwd(const Ctx& c, const QkArgs& a) {
-  // several heads an item where there are enough of them to fill the GPU
-  // anyway: their loads are in flight together and the angles are read once
+  // as many heads a group as bring all of them into one wave, at most 8: their
+  // loads are in flight together and the angles are read once
   const int64_t heads = static_cast<int64_t>(a.T) * (a.heads[0] + a.heads[1]);
-  const int64_t room = static_cast<int64_t>(c.num_sms) * 2048 / L;
-  const int per = heads >= 8 * room ? 8 : heads >= 4 * room ? 4 : 1;
+  const int64_t room = static_cast<int64_t>(c.num_sms) * kFwdBlocks * (kThreads / L);
+  int per = 1;
+  while (per < 8 && heads > per * room) per *= 2;
   const int nq = static_cast<int>(ceil_div(a.heads[0], per));
   const int nch = nq + static_cast<int>(ceil_div(a.heads[1], per));
   const int64_t blocks = ceil_div(static_cast<int64_t>(a.T) * nch, kThreads / L);

@@ -46,6 +46,13 @@ struct WaitCtl {
   uint64_t limit_ns;     // per-wait wall-clock limit
 };
 
+// After a wait that ran out: time for asynchronous copies in flight (a few
+// microseconds each) to land before the CTA retires.
+__device__ __forceinline__ void let_copies_land() {
+  const uint64_t t0 = global_timer_ns();
+  while (global_timer_ns() - t0 < 50000) nanosleep_ns(1000);
+}
+
 // -------------------------------------------------------------- mbarrier ---
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");

@@ -269,3 +269,55 @@ def test_refusals():
     with pytest.raises(B.OliveError) as e:
         B.olive_gated_mlp_fwd(s["x"], *w, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 9
+
+
+# shapes by the path they take: few rows with each count of tokens, by whole K steps and by clusters
+# that share them (one token's tiles fill the GPU or do not); many rows in tiles of 128 and of 256
+# columns, with every product whole, and with tiles cut in two and in many pieces
+@pytest.mark.parametrize("T,d,f", [
+    (5, 64, 20000), (5, 1000, 24), (20, 2048, 4096), (33, 512, 12288), (64, 4096, 512), (100, 136, 16384),
+    (128, 2048, 2056), (128, 8, 4096), (3, 8, 8),
+    (200, 1024, 2816), (512, 2048, 6144), (256, 4096, 1032), (130, 256, 8200), (1500, 4096, 264), (2000, 512, 4000),
+    (9000, 64, 72), (4100, 1288, 1544)])
+def test_paths(T, d, f):
+    _check(T, d, f, act="gelu_tanh" if T % 2 else "silu", residual=T % 3 != 0,
+           grad_dtype=torch.float32 if d % 16 else torch.bfloat16)
+
+
+@pytest.mark.parametrize("T,d,f", [(7, 131072, 512), (900, 32768, 1024)])
+def test_waits_that_run_out_are_reported(T, d, f, monkeypatch):
+    """With no time to wait the calls give up, say so and leave the context usable (the widths make
+    the epilogues wait long enough for the limit to be looked at)."""
+    s = _case(T, d, f)
+    w = (s["W_gate"], s["W_up"], s["W_down"])
+    y, saved = B.olive_gated_mlp_fwd(s["x"], *w, save=True)
+    want = B.olive_gated_mlp_bwd(s["dy"], s["x"], *w, saved)
+    monkeypatch.setenv("OLIVE_WAIT_LIMIT_MS", "0")
+    for bwd in (False, True):
+        st = B.new_status()
+        if bwd:
+            B.olive_gated_mlp_bwd(s["dy"], s["x"], *w, saved, dev_status=st)
+        else:
+            B.olive_gated_mlp_fwd(s["x"], *w, dev_status=st)
+        torch.cuda.synchronize()
+        assert B.status_bits(st) == ["OLIVE_ERR_TIMEOUT"]
+    monkeypatch.delenv("OLIVE_WAIT_LIMIT_MS")
+    st = B.new_status()
+    again, saved2 = B.olive_gated_mlp_fwd(s["x"], *w, save=True, dev_status=st)
+    got = B.olive_gated_mlp_bwd(s["dy"], s["x"], *w, saved2, dev_status=st)
+    assert B.status_bits(st) == [] and torch.equal(again, y) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_workspace_of_another_call_and_sticky_contents():
+    """What an earlier call left in a workspace does not matter."""
+    for T, d, f in ((30, 256, 512), (700, 512, 1544)):
+        s = _case(T, d, f)
+        w = (s["W_gate"], s["W_up"], s["W_down"])
+        want, saved = B.olive_gated_mlp_fwd(s["x"], *w, save=True)
+        grads = B.olive_gated_mlp_bwd(s["dy"], s["x"], *w, saved)
+        for byte in (0x00, 0xff, 0x7f):
+            ws = torch.full((B.olive_workspace_size("gated_mlp_bwd", T, d, f),), byte, dtype=torch.uint8, device="cuda")
+            assert torch.equal(B.olive_gated_mlp_fwd(s["x"], *w, ws=ws)[0], want)
+            ws.fill_(byte)
+            got = B.olive_gated_mlp_bwd(s["dy"], s["x"], *w, saved, ws=ws)
+            assert all(torch.equal(a, b) for a, b in zip(got, grads))
