@@ -118,8 +118,8 @@ __device__ __forceinline__ bool angles(const QkArgs& p, int t, const Place& q, b
 
 // Heads whose loads a thread has in flight together: 64 bytes of each operand.
 // Measured, us on 32768 tokens of 32 + 8 heads of 128, bf16: forward, 4 blocks an
-// SM, 117 with four heads, 130 with two; 128 with four and 3 blocks; backward 186
-// with four heads and 2 blocks, 201 with two and 3, 212 with one and 4.
+// SM, 106 with four heads (6.3 TB/s), 121 with two; 118 with four and 3 blocks;
+// backward 180 with four heads and 2 blocks (5.6 TB/s), 184 with two and 3.
 template <typename T>
 constexpr int at_once() {
   return sizeof(T) == 2 ? 4 : 2;
@@ -142,34 +142,47 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) qk_fwd_kernel(const QkAr
   const int h0 = c0 * per, h1 = live ? min(h0 + per, p.heads[side]) : h0;
   const Place q = place<kInter>(lane, p.D, p.R);
   const HeadsView src = p.in[side], dst = p.out[side];
-  const T* x = static_cast<const T*>(src.x) + t * src.token_stride;
-  T* y = static_cast<T*>(const_cast<void*>(dst.x)) + t * dst.token_stride;
   const T* w = static_cast<const T*>(p.w[side]);
   const float inv_d = 1.f / p.D;
+  // the lane's first run of a head; the second is `other` values on
+  const int other = q.b - q.a;
+  const T* x = static_cast<const T*>(src.x) + t * src.token_stride + h0 * src.head_stride + q.a;
+  T* y = static_cast<T*>(const_cast<void*>(dst.x)) + t * dst.token_stride + h0 * dst.head_stride + q.a;
 
-  float wa[4] = {}, wb[4] = {}, c[4] = {}, s[4] = {};
+  // The rotation with the weights in it: out = r (a ca - b sb, b cb + a sa) with
+  // ca = w_a cos, sa = w_a sin, cb = w_b cos, sb = w_b sin, formed once a token
+  float ca[4], sa[4], cb[4], sb[4];
   bool fine = true;
   for (int h = h0; __any_sync(0xffffffffu, h < h1); h += kAtOnce) {
     typename V::Raw ra[kAtOnce], rb[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
+    for (int k = 0; k < kAtOnce; ++k, x += src.head_stride) {
       if (q.in && h + k < h1) {
-        const T* row = x + (h + k) * src.head_stride;
-        ra[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
-        rb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
+        ra[k] = *reinterpret_cast<const typename V::Raw*>(x);
+        rb[k] = *reinterpret_cast<const typename V::Raw*>(x + other);
       } else {
         ra[k] = rb[k] = typename V::Raw{};
       }
     }
-    if (h == h0 && live) {
-      fine = angles(p, t, q, lane == 0, c, s);
-      if (q.in) {
+    if (h == h0) {
+      float wa[4] = {}, wb[4] = {}, c[4] = {}, s[4] = {};
+      if (live) fine = angles(p, t, q, lane == 0, c, s);
+      if (live && q.in) {
         V::get(*reinterpret_cast<const typename V::Raw*>(w + q.a), wa);
         V::get(*reinterpret_cast<const typename V::Raw*>(w + q.b), wb);
       }
+      const auto fold = [&](float& cc, float& ss, float ww, int pair) {
+        cc = q.turn ? ww * c[pair] : ww;
+        ss = ww * s[pair];
+      };
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        fold(ca[e], sa[e], wa[e], kInter ? e / 2 : e);
+        fold(cb[e], sb[e], wb[e], kInter ? 2 + e / 2 : e);
+      }
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
+    for (int k = 0; k < kAtOnce; ++k, y += dst.head_stride) {
       float a[4], b[4];
       V::get(ra[k], a);
       V::get(rb[k], b);
@@ -180,15 +193,23 @@ __global__ void __launch_bounds__(kThreads, kFwdBlocks) qk_fwd_kernel(const QkAr
       if (!(q.in && h + k < h1)) continue;
       float r = rsqrtf(fmaf(ss, inv_d, p.eps));
       if (!fine) r = __uint_as_float(0x7fffffffu);
+      float oa[4], ob[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        a[e] = a[e] * r * wa[e];
-        b[e] = b[e] * r * wb[e];
+        if (!q.turn) {  // (not a turn by 0: an infinite partner would make it NaN)
+          oa[e] = r * (a[e] * ca[e]);
+          ob[e] = r * (b[e] * cb[e]);
+        } else if (kInter) {  // pairs inside a run: even members -, odd ones +
+          const int m = e ^ 1;
+          oa[e] = r * fmaf(a[e], ca[e], e & 1 ? a[m] * sa[m] : -(a[m] * sa[m]));
+          ob[e] = r * fmaf(b[e], cb[e], e & 1 ? b[m] * sb[m] : -(b[m] * sb[m]));
+        } else {
+          oa[e] = r * fmaf(a[e], ca[e], -(b[e] * sb[e]));
+          ob[e] = r * fmaf(b[e], cb[e], a[e] * sa[e]);
+        }
       }
-      if (q.turn) rotate<kInter>(a, b, c, s);
-      T* row = y + (h + k) * dst.head_stride;
-      *reinterpret_cast<typename V::Raw*>(row + q.a) = V::put(a);
-      *reinterpret_cast<typename V::Raw*>(row + q.b) = V::put(b);
+      *reinterpret_cast<typename V::Raw*>(y) = V::put(oa);
+      *reinterpret_cast<typename V::Raw*>(y + other) = V::put(ob);
     }
   }
 }
@@ -216,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) qk_bwd_kernel(const QkAr
   const int step = blocks * (kThreads / L) / nch;  // tokens worked on at once
   const int chunk = group % nch;
   const int h0 = chunk * per, h1 = min(h0 + per, p.heads[side]);
+  const int other = q.b - q.a;  // from the lane's first run of a head to its second
   const HeadsView src = p.in[side], grd = p.grad[side], dst = p.out[side];
 
   float w[8] = {}, dw[8] = {};
@@ -235,22 +257,20 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) qk_bwd_kernel(const QkAr
   for (int t = group / nch < step ? group / nch : p.T; __any_sync(0xffffffffu, t < p.T); t = t < p.T - step ? t + step : p.T) {
     const bool live = t < p.T;
     const int tt = live ? t : 0, he = live ? h1 : h0;
-    const T* x = static_cast<const T*>(src.x) + tt * src.token_stride;
-    const T* g = static_cast<const T*>(grd.x) + tt * grd.token_stride;
-    T* y = static_cast<T*>(const_cast<void*>(dst.x)) + tt * dst.token_stride;
+    const T* x = static_cast<const T*>(src.x) + tt * src.token_stride + h0 * src.head_stride + q.a;
+    const T* g = static_cast<const T*>(grd.x) + tt * grd.token_stride + h0 * grd.head_stride + q.a;
+    T* y = static_cast<T*>(const_cast<void*>(dst.x)) + tt * dst.token_stride + h0 * dst.head_stride + q.a;
     float c[4] = {}, s[4] = {};
     bool fine = true;
     for (int h = h0; __any_sync(0xffffffffu, h < he); h += kAtOnce) {
       typename V::Raw xa[kAtOnce], xb[kAtOnce], ga[kAtOnce], gb[kAtOnce];
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
+      for (int k = 0; k < kAtOnce; ++k, x += src.head_stride, g += grd.head_stride) {
         if (q.in && h + k < he) {
-          const T* row = x + (h + k) * src.head_stride;
-          xa[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
-          xb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
-          row = g + (h + k) * grd.head_stride;
-          ga[k] = *reinterpret_cast<const typename V::Raw*>(row + q.a);
-          gb[k] = *reinterpret_cast<const typename V::Raw*>(row + q.b);
+          xa[k] = *reinterpret_cast<const typename V::Raw*>(x);
+          xb[k] = *reinterpret_cast<const typename V::Raw*>(x + other);
+          ga[k] = *reinterpret_cast<const typename V::Raw*>(g);
+          gb[k] = *reinterpret_cast<const typename V::Raw*>(g + other);
         } else {
           xa[k] = xb[k] = ga[k] = gb[k] = typename V::Raw{};
         }
@@ -261,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) qk_bwd_kernel(const QkAr
         for (int e = 0; e < 4; ++e) s[e] = -s[e];
       }
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
+      for (int k = 0; k < kAtOnce; ++k, y += dst.head_stride) {
         float v[8], d[8];
         {
           float a[4], b[4];
@@ -307,9 +327,8 @@ __global__ void __launch_bounds__(kThreads, kBwdBlocks) qk_bwd_kernel(const QkAr
           else
             b[e - 4] = o;
         }
-        T* row = y + (h + k) * dst.head_stride;
-        *reinterpret_cast<typename V::Raw*>(row + q.a) = V::put(a);
-        *reinterpret_cast<typename V::Raw*>(row + q.b) = V::put(b);
+        *reinterpret_cast<typename V::Raw*>(y) = V::put(a);
+        *reinterpret_cast<typename V::Raw*>(y + other) = V::put(b);
       }
     }
   }

@@ -269,3 +269,23 @@ def test_refusals():
     with pytest.raises(B.OliveError) as e:
         f(*args(q=wide[..., 4:]))
     assert e.value.status == 3
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_values_that_are_not_finite_stay_where_the_formula_has_them(value, inter):
+    """An infinite value makes its row's scale 0 and itself (and its pair's partner) NaN; a NaN takes
+    the row.  Other rows do not change."""
+    s = _case(6, 3, 1, 64, 32, torch.float32, fused=False)
+    more = (s["w_q"], s["w_k"], s["cos"], s["sin"], s["positions"], EPS, inter)
+    want, _ = B.olive_qk_norm_rope_fwd(s["q"], s["k"], *more)
+    s["q"][2, 1, 40] = value
+    got, _ = B.olive_qk_norm_rope_fwd(s["q"], s["k"], *more)
+    keep = torch.ones(6, 3, dtype=torch.bool, device="cuda")
+    keep[2, 1] = False
+    assert torch.equal(got[keep], want[keep])
+    bad = torch.isnan(got[2, 1])
+    if value != value:
+        assert bad.all()
+    else:
+        assert bad[40] and int(bad.sum()) == 1 and float(got[2, 1][~bad].abs().max()) == 0
