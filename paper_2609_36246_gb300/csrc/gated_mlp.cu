@@ -342,14 +342,39 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t out0 = base + L::kOut + warp * L::kOutBufs * kOutBuf;
     int n = 0;
     bool ok = true;
+    constexpr int kCols = kMode == MM_UP ? kBN / 2 : kBN;  // result columns of a tile
+    // What the epilogue reads from memory (MM_DH: g and u, MM_DOWN: the residual), a
+    // chunk of 32 columns ahead of its use, in whole 64-byte rows as put_rows stores
+    // them; the chunk goes through the results' buffers.  (Each thread reading its
+    // own row from memory, 32 rows an instruction, cost the dh launch 20 us of 75 at
+    // 2816 rows, d = 2048, f = 5632.)
+    constexpr bool kReads = kMode == MM_DH || kMode == MM_DOWN;
+    const bool reads = kMode == MM_DH || (kMode == MM_DOWN && p.residual);
+    uint4 e0[4], e1[4];
+    auto fetch = [&](const Unit& w, int chunk, bool valid) {
+      const MlpProb& q = p.pr[0];
+      const int y = w.m0 + static_cast<int>(rank) * kBM + (warp & 3) * 32 + (lane >> 2);
+      const int x = w.n0 * kCols + half * (kCols / 2) + chunk * 32 + (lane & 3) * 8;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = valid && reads && y + 8 * i < q.M && x < q.N;
+        const size_t at = static_cast<size_t>(y + 8 * i) * q.N + x;
+        e0[i] = e1[i] = make_uint4(0, 0, 0, 0);
+        if (in && kMode == MM_DH) {
+          e0[i] = __ldg(reinterpret_cast<const uint4*>(p.saved_g + at));
+          e1[i] = __ldg(reinterpret_cast<const uint4*>(p.saved_u + at));
+        } else if (in) {
+          e0[i] = *reinterpret_cast<const uint4*>(p.residual + at);
+        }
+      }
+    };
+    if (kReads && more) fetch(u, 0, u.k1 == u.ks);
 
     for (; ok && more; u = ahead) {
       const MlpProb& q = p.pr[u.prob];
       const int b = n & 1;
       const uint32_t acc = lane_addr + b * kBN;
       const int y = u.m0 + static_cast<int>(rank) * kBM + (warp & 3) * 32;  // the warp's first row
-      const int t = y + lane;
-      constexpr int kCols = kMode == MM_UP ? kBN / 2 : kBN;  // result columns of a tile
       constexpr int kSteps = kCols / 32;                     // of 16 columns, this warp's half
       const int x0 = u.n0 * kCols + half * (kCols / 2);
       // TMEM column of step s (MM_UP: g; u is kBN / 2 columns on)
@@ -363,24 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(map_shared(tempty(b), 0));
       };
-      // what the epilogue reads from memory, one step ahead of its use
       const bool whole = u.k1 == u.ks;
-      uint4 e0[2] = {}, e1[2] = {};
-      auto fetch = [&](int s) {
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int x = x0 + s * 16 + v * 8;
-          const bool in = whole && s < kSteps && t < q.M && x < q.N;
-          const size_t at = static_cast<size_t>(t) * q.N + x;
-          if (kMode == MM_DOWN)
-            e0[v] = in && p.residual ? *reinterpret_cast<const uint4*>(p.residual + at) : make_uint4(0, 0, 0, 0);
-          if (kMode == MM_DH) {
-            e0[v] = in ? __ldg(reinterpret_cast<const uint4*>(p.saved_g + at)) : make_uint4(0, 0, 0, 0);
-            e1[v] = in ? __ldg(reinterpret_cast<const uint4*>(p.saved_u + at)) : make_uint4(0, 0, 0, 0);
-          }
-        }
-      };
-      fetch(0);
       more = walk.next(p, ahead);
       if (!mbar_wait_warp(tfull(b), (n >> 1) & 1, ctl)) break;
       tc_fence_after();
@@ -401,6 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __threadfence();
         __syncwarp();
         if (lane == 0) red_release_add(p.flag + pair * 2 + rank, 1u);
+        if (kReads) fetch(ahead, 0, more && ahead.k1 == ahead.ks);
         continue;
       }
       // A tile that is finished from pieces is the pair's last unit: its MMAs are
@@ -459,7 +468,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         if (s == kSteps - 1) release();
         const uint32_t buf = out0;
-        if (opens) __syncwarp();  // the buffers' last contents have been read
+        if (opens) {
+          __syncwarp();  // the buffers' last contents have been read
+          if (kReads && reads) {
+            // MM_DH: g where dg will be, u where du will be; MM_DOWN: the residual
+            // where y will be, each thread's row by the thread that replaces it
+            constexpr int kFirst = kMode == MM_DH ? kOutBuf : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              st_shared_v4(out_piece(buf + kFirst, i * 8 + (lane >> 2), lane & 3), e0[i]);
+              if (kMode == MM_DH) st_shared_v4(out_piece(buf + 2 * kOutBuf, i * 8 + (lane >> 2), lane & 3), e1[i]);
+            }
+            if (s + 2 < kSteps)
+              fetch(u, (s >> 1) + 1, true);
+            else
+              fetch(ahead, 0, more && ahead.k1 == ahead.ks);
+            __syncwarp();
+          }
+        }
         const int c0 = f32 ? 0 : (s & 1) * 2;  // 16-byte pieces of the row
 
         if constexpr (kMode == MM_UP) {
@@ -488,9 +514,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                          make_uint4(uw[4 * c], uw[4 * c + 1], uw[4 * c + 2], uw[4 * c + 3]));
           }
         } else if constexpr (kMode == MM_DH) {
-          const uint32_t gs[8] = {e0[0].x, e0[0].y, e0[0].z, e0[0].w, e0[1].x, e0[1].y, e0[1].z, e0[1].w};
-          const uint32_t us[8] = {e1[0].x, e1[0].y, e1[0].z, e1[0].w, e1[1].x, e1[1].y, e1[1].z, e1[1].w};
-          fetch(s + 1);
+          const uint4 ga = ld_shared_v4(out_piece(buf + kOutBuf, lane, c0)), gb = ld_shared_v4(out_piece(buf + kOutBuf, lane, c0 + 1));
+          const uint4 ua = ld_shared_v4(out_piece(buf + 2 * kOutBuf, lane, c0)),
+                      ub = ld_shared_v4(out_piece(buf + 2 * kOutBuf, lane, c0 + 1));
+          const uint32_t gs[8] = {ga.x, ga.y, ga.z, ga.w, gb.x, gb.y, gb.z, gb.w};
+          const uint32_t us[8] = {ua.x, ua.y, ua.z, ua.w, ub.x, ub.y, ub.z, ub.w};
           uint32_t hw[8], gw[8], uw[8], bad = 0;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -528,9 +556,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int c = 0; c < 4; ++c)
             st_shared_v4(out_piece(buf, lane, c), make_uint4(r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]));
         } else {
-          if constexpr (kMode == MM_DOWN) {
-            const uint32_t rs[8] = {e0[0].x, e0[0].y, e0[0].z, e0[0].w, e0[1].x, e0[1].y, e0[1].z, e0[1].w};
-            fetch(s + 1);
+          if (kMode == MM_DOWN && reads) {
+            const uint4 ra = ld_shared_v4(out_piece(buf, lane, c0)), rb = ld_shared_v4(out_piece(buf, lane, c0 + 1));
+            const uint32_t rs[8] = {ra.x, ra.y, ra.z, ra.w, rb.x, rb.y, rb.z, rb.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               r[2 * i] = __float_as_uint(__uint_as_float(r[2 * i]) + __uint_as_float(rs[i] << 16));
@@ -635,15 +663,16 @@ struct Plan {
   double ns;  // estimate
 };
 
-// The estimate's terms, ns, by tile width: a K step of a pair, a tile's epilogue
-// (by mode: the least that a tile takes, and seen in full at the end), the store
-// of a piece and the wait for it, and each piece that a finisher adds.
+// The estimate's terms, ns, by tile width: a K step of a pair; by mode, the least
+// that a tile takes while all pairs' epilogues load and store, and the last tile's
+// epilogue; the store of a piece and the wait for it, and each piece that a
+// finisher adds.
 struct Cost {
-  double step, tile[4], cut, piece;
+  double step, tile[4], tail[4], cut, piece;
 };
+constexpr Cost kCostWide{290, {7000, 3300, 13000, 3300}, {4500, 3300, 6500, 3300}, 2500, 1800};
+constexpr Cost kCostNarrow{165, {4000, 1900, 7000, 1900}, {2500, 1900, 3500, 1900}, 2000, 1000};
 constexpr double kClear = 3500;  // zeroing the flags, where no launch of the call has
-constexpr Cost kCostWide{290, {4500, 3300, 6500, 3300}, 2500, 1800};
-constexpr Cost kCostNarrow{165, {2500, 1900, 3500, 1900}, 2000, 1000};
 
 // Deals the tiles to the pairs, whole ones or every product's last ones cut, by
 // what is estimated to end first.
@@ -673,7 +702,7 @@ Plan plan_tiles(const MlpParams& p, int mode, int bn, int pairs) {
   }
   for (int i = 0; i < p.n_prob; ++i) w.cut.whole[i] = tiles[i];
   w.cut.n_whole = all;
-  w.ns += k.tile[mode];
+  w.ns += k.tail[mode];
   // every product's last tiles cut
   MlpSplit s = {};
   int64_t steps = 0;
@@ -692,7 +721,7 @@ Plan plan_tiles(const MlpParams& p, int mode, int bn, int pairs) {
   for (int m = 1; m <= 8; ++m) {  // longer runs on fewer pairs: fewer pieces
     s.run = static_cast<int>(ceil_div(steps * m, pairs));
     const double pieces = static_cast<double>(longest) / s.run;
-    double t = before + s.run * k.step + k.tile[mode] + k.cut + k.piece * pieces;
+    double t = before + s.run * k.step + k.tail[mode] + k.cut + k.piece * pieces;
     if (mode == MM_UP || mode == MM_DH) t += kClear;
     if (t < w.ns) w = Plan{bn, s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, s.run)), s, t};
   }
