@@ -365,12 +365,12 @@ __global__ void __launch_bounds__(1024) qk_dw_kernel(const float* part, int bq, 
     for (int b = b0 + g; b < b1; b += 32) v += static_cast<double>(part[static_cast<size_t>(b) * D + col]);
   }
   sums[g][lane] = v;
-  __syncthreads();
-  if (g == 0 && col < D) {
 #pragma unroll
-    for (int i = 1; i < 32; ++i) v += sums[i][lane];
-    (blockIdx.y ? dw_k : dw_q)[col] = static_cast<float>(v);
+  for (int o = 16; o > 0; o >>= 1) {
+    __syncthreads();
+    if (g < o) sums[g][lane] += sums[g + o][lane];
   }
+  if (g == 0 && col < D) (blockIdx.y ? dw_k : dw_q)[col] = static_cast<float>(sums[0][lane]);
 }
 
 __global__ void positions_kernel(const int32_t* cu, int S, int T_cap, int32_t* positions) {
