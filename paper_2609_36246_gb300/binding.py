@@ -11,6 +11,7 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
+import operator
 import os
 import re
 
@@ -609,6 +610,23 @@ def olive_packed_positions(cu_seqlens, T_cap: int, out=None):
 # of a tensor 0.07): the calls below look at each tensor once, in one expression, and
 # name what is wrong only when something is.
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_ptr_of, _numel_of, _device_of = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device
+_is_dense, _dtype_of = torch.Tensor.is_contiguous, operator.attrgetter("dtype")
+
+
+def _need_all(tensors, dtype, names):
+    """_need for several tensors of one dtype at once."""
+    try:
+        for t in tensors:
+            if t.dtype is not dtype:
+                break
+        else:
+            if min(map(_device_of, tensors)) >= 0 and all(map(_is_dense, tensors)):
+                return
+    except (TypeError, AttributeError):
+        pass
+    for t, n in zip(tensors, names):
+        _need(t, dtype, n)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -630,12 +648,14 @@ def _refuse_heads(t, T, H, D, dtype, name, device):
 
 def _heads(t, shape, dtype, name, device):
     """Pointer, token stride and head stride of a view [T, H, D] with contiguous heads."""
-    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or
-            t.stride(2) != 1 or t.device != device):
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != device:
+        _refuse_heads(t, *shape, dtype, name, device)
+    a, b, c = t.stride()
+    if c != 1:
         _refuse_heads(t, *shape, dtype, name, device)
     T, H, _ = shape
     # (the stride of a dimension of one entry means nothing)
-    return t.data_ptr(), t.stride(0) if T > 1 else 0, t.stride(1) if H > 1 else 0
+    return t.data_ptr(), a if T > 1 else 0, b if H > 1 else 0
 
 
 def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
@@ -649,18 +669,17 @@ def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
     if sk[0] != T or sk[2] != D:
         raise ValueError(f"k must have the shape [{T}, heads, {D}]")
     vq, vk = _heads(q, sq, dtype, "q", dev), _heads(k, sk, dtype, "k", dev)
-    for t, n in ((w_q, "w_q"), (w_k, "w_k")):
-        _need(t, dtype, n)
-        if t.numel() != D:
-            raise ValueError(f"{n} must hold {D} values")
-    _need(cos, _F32, "cos")
-    _need(sin, _F32, "sin")
+    _need_all((w_q, w_k), dtype, ("w_q", "w_k"))
+    _need_all((cos, sin), _F32, ("cos", "sin"))
     _need(positions, _I32, "positions")
-    if cos.dim() != 2 or cos.shape != sin.shape:
+    if w_q.numel() != D or w_k.numel() != D:
+        raise ValueError(f"w_q and w_k must hold {D} values")
+    table = cos.shape
+    if len(table) != 2 or table != sin.shape:
         raise ValueError("cos and sin must have the same shape [P, R/2]")
     if positions.numel() != T:
         raise ValueError(f"positions must hold {T} values")
-    P, half = cos.shape
+    P, half = table
     common = (Hq, sk[1], w_q.data_ptr(), w_k.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(),
               positions.data_ptr(), P, T, D, 2 * half, 1 if interleaved else 0)
     return vq, vk, common, sq, sk, dtype, dev
@@ -714,13 +733,13 @@ def olive_qk_norm_rope_bwd(g_q, g_k, q, k, w_q, w_k, cos, sin, positions, eps: f
 
 
 def _mlp_args(x, W_gate, W_up, W_down):
-    for t, n in ((x, "x"), (W_gate, "W_gate"), (W_up, "W_up"), (W_down, "W_down")):
-        _need(t, _BF16, n)
-    if x.dim() != 2:
+    _need_all((x, W_gate, W_up, W_down), _BF16, ("x", "W_gate", "W_up", "W_down"))
+    rows, wide = x.shape, W_gate.shape
+    if len(rows) != 2:
         raise ValueError("x must have the shape [T, d]")
-    T, d = x.shape
-    f = W_gate.shape[0]
-    if W_gate.shape != (f, d) or W_up.shape != (f, d) or W_down.shape != (d, f):
+    T, d = rows
+    f = wide[0]
+    if wide != (f, d) or W_up.shape != wide or W_down.shape != (d, f):
         raise ValueError("W_gate and W_up must have the shape [f, d], W_down [d, f]")
     return T, d, f
 
@@ -795,13 +814,13 @@ def olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, act: str = "silu",
 def _grad_list(tensors, cur, what):
     """Pointers, element counts and dtypes of contiguous tensors on device `cur`."""
     try:
-        kinds = [DTYPE[t.dtype] for t in tensors]
-    except (KeyError, AttributeError):
+        kinds = list(map(DTYPE.__getitem__, map(_dtype_of, tensors)))
+        fine = all(map(_is_dense, tensors)) and set(map(_device_of, tensors)) <= {cur}
+    except (KeyError, AttributeError, TypeError):
         raise TypeError(f"{what} must be bf16 or fp32 tensors") from None
-    for i, t in enumerate(tensors):
-        if not t.is_contiguous() or t.get_device() != cur:
-            raise TypeError(f"{what} {i} must be contiguous and on the current CUDA device")
-    return [t.data_ptr() for t in tensors], [t.numel() for t in tensors], kinds
+    if not fine:
+        raise TypeError(f"{what} must be contiguous and on the current CUDA device")
+    return list(map(_ptr_of, tensors)), list(map(_numel_of, tensors)), kinds
 
 
 def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
