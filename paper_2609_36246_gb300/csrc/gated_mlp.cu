@@ -4,8 +4,8 @@
 //   dh = dy Wd, dg = dh u act'(g), du = dh act(g)
 //   dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x, dWd = dy^T h
 // as four kinds of one persistent tcgen05 kernel:
-//   MM_UP     g and u of 128 columns side by side in one 256-column
-//             accumulator; h (and, for a backward, g and u) in the epilogue
+//   MM_UP     g and u of the same columns side by side in one accumulator; h
+//             (and, for a backward, g and u) in the epilogue
 //   MM_DOWN   h Wd^T, the residual added in the epilogue
 //   MM_DH     dy Wd; the epilogue reads g and u and writes dg, du and h
 //   MM_GRADS  the four products that are left, in one launch
@@ -16,13 +16,23 @@
 // the epilogue of a tile runs under the next tile's MMAs.  An operand is
 // read K-major or MN-major as it lies in memory; nothing is transposed or
 // copied.  Results are turned in shared memory so that a warp's store covers whole
-// 64-byte rows (TMA stores of the same rows took 7 cycles a row, 7.5 us for a tile
-// of 256 columns of a weight gradient whose products take 1 us).
+// 64-byte rows.  Wide tiles read each operand less often (64 KB a K step of 512 MMA
+// cycles); narrow ones are for small problems, whose epilogues and last waves are
+// then shorter (512 rows, d = 256, f = 704, us: forward 13.4, backward 18.5; 19.3 and
+// 35.3 with wide tiles; 2777 rows, 2048, 5504: 150 and 314; 137 and 260 with wide
+// ones); plan_tiles below chooses.
 //
-// What bounds it: the tensor pipe (a K step of a pair is 512 cycles of MMAs
-// for 64 KB from L2).  Rounding: g and u are used from the fp32 accumulators;
-// h, dg and du are rounded to bf16 once, as operands of the next product; g and
-// u are saved with 10 significant bits (pack_saved below).
+// What bounds it: the tensor pipe in the products with long K steps and light
+// epilogues, the epilogue's loads and stores in MM_UP and MM_DH at small d.
+// Measured: 8192 rows, d = 4096, f = 12288, forward and backward 4.48 ms, 1.66
+// PFLOP/s, under the power cap; 2777 rows, d = 2048, f = 5504, launch by launch from
+// empty caches, us: up 83, down 52, dh 68, gradients 175 (1.8 PFLOP/s; 91 % of the
+// tensor pipe's cycles on 2816 rows); d = 2040, f = 5464, whose rows are not whole
+// 128-byte lines: 109, 53, 91, 187.
+//
+// Rounding: g and u are used from the fp32 accumulators; h, dg and du are rounded
+// to bf16 once, as operands of the next product; g and u are saved with 10
+// significant bits (pack_saved).
 #include <algorithm>
 #include <atomic>
 
@@ -346,8 +356,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // What the epilogue reads from memory (MM_DH: g and u, MM_DOWN: the residual), a
     // chunk of 32 columns ahead of its use, in whole 64-byte rows as put_rows stores
     // them; the chunk goes through the results' buffers.  (Each thread reading its
-    // own row from memory, 32 rows an instruction, cost the dh launch 20 us of 75 at
-    // 2816 rows, d = 2048, f = 5632.)
+    // own row from memory, 32 rows an instruction, took the dh launch 75 us in place
+    // of 68 at 2816 rows, d = 2048, f = 5632, and 66 in place of 54 at d = 512.)
     constexpr bool kReads = kMode == MM_DH || kMode == MM_DOWN;
     const bool reads = kMode == MM_DH || (kMode == MM_DOWN && p.residual);
     uint4 e0[4], e1[4];
@@ -799,7 +809,7 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
                             int32_t f, int act, void* y, void* saved, void* ws,
                             int32_t* dev_status) {
   const MlpWs w = carve_mlp(ws, T, f, false);
-  if (T <= kMlpFewRows)
+  if (mlp_few(T, f))
     return launch_mlp_few(c, x, W_gate, W_up, W_down, residual, T, d, f, act, y, saved, w.h, dev_status);
   const int fp = static_cast<int>(mlp_pitch(f));
   MlpParams p = {};

@@ -17,6 +17,10 @@
 // tokens, in the cluster's order.  The second launch starts while the first runs
 // (programmatic dependent launch) and fills its stages with W_down before it waits
 // for h.
+//
+// Measured, us, the weights in HBM: one token 54 at d = 4096, f = 12288 (5.6 TB/s
+// over 302 MB), 21 at 2048, 6144; 64 tokens 64 and 28; 128 tokens 75 and 36.  (In
+// gated_mlp.cu's form: one 138 and 49, 64 77 and 37, 128 79 and 38.)
 #include <algorithm>
 #include <atomic>
 

@@ -359,8 +359,8 @@ olive_status launch_topk_kl_fwd_bwd(const Ctx& c, const void* h_s, const void* W
 
 // ---- gated feed-forward block (gated_mlp.cu) ----
 constexpr int kMlpMaxPairs = 96;  // CTA pairs the partials and flags are sized for
-// Pitch of the block's own [T, f] arrays: whole 128-byte rows, which TMA reads a
-// fifth faster than rows that straddle them.
+// Pitch of the block's own [T, f] arrays: whole 128-byte rows, as rows
+// that straddle 128-byte lines take TMA longer.
 inline int64_t mlp_pitch(int64_t f) { return static_cast<int64_t>(align_up(static_cast<size_t>(f), 64)); }
 struct MlpWs {
   void* h;         // bf16 [T, mlp_pitch(f)]
@@ -378,7 +378,16 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
                             int32_t f, int act, void* y, void* saved, void* ws,
                             int32_t* dev_status);
 // The forward on few rows (gated_mlp_few.cu); h: workspace [T, f].
-constexpr int kMlpFewRows = 128;
+// It is taken up to 64 rows, and up to 128 where the first launch's tiles of 64
+// weight rows are more than half of the SMs.  Measured, us, this form and the other:
+// 64 rows (2048, 6144) 28 and 37, (1024, 2816) 17 and 21, (4096, 2816) 35 and 30;
+// 80 rows (4096, 11008) 69 and 75, (2040, 5464) 35 and 40, (2560, 8192) 48 and 44,
+// but (2560, 5120) 42 and 39, (2048, 4096) 33 and 28, (512, 1536) 19 and 16 and (256,
+// 704) 18 and 13, of which the rule lets the first of the four through.
+constexpr int kMlpFewRows = 64, kMlpFewRowsWide = 128, kMlpWide = 64 * 77;
+inline bool mlp_few(int64_t T, int64_t f) {
+  return T <= kMlpFewRows || (T <= kMlpFewRowsWide && f >= kMlpWide);
+}
 olive_status launch_mlp_few(const Ctx& c, const void* x, const void* W_gate, const void* W_up,
                             const void* W_down, const void* residual, int32_t T, int32_t d,
                             int32_t f, int act, void* y, void* saved, void* h,

@@ -349,7 +349,7 @@ static MlpWs carve_mlp_impl(void* ws, int64_t T, int64_t f, bool bwd, size_t* to
     w.dg = c.take(rows);
     w.du = c.take(rows);
   }
-  if (bwd || T > kMlpFewRows) {
+  if (bwd || !mlp_few(T, f)) {
     w.part = static_cast<float*>(c.take(mlp_part_bytes()));
     w.flag = static_cast<uint32_t*>(c.take(2 * 4 * mlp_flag_words()));
   }

@@ -8,7 +8,9 @@
 // rotation needs no exchange; the mean square is a butterfly over the group.  A
 // group takes several heads of one token and reads its cosines and sines once.
 //
-// What bounds it: HBM, 2 reads or writes of every value forward and 3 backward.
+// What bounds it: HBM, 2 reads or writes of every value forward and 3 backward (6.3
+// and 5.6 TB/s at 32768 tokens of 32 + 8 heads of 128, 107 and 180 us; at_once
+// below), and the launch for a token or a few (2.8 us).
 #include <algorithm>
 
 #include "internal.h"

@@ -284,6 +284,15 @@ def test_paths(T, d, f):
            grad_dtype=torch.float32 if d % 16 else torch.bfloat16)
 
 
+# both sides of the widths from which 65 to 128 rows take the weights as the wide operand, with the
+# second product's K steps whole and shared by clusters
+@pytest.mark.parametrize("T", [64, 65, 100, 128, 129])
+@pytest.mark.parametrize("d,f", [(136, 4920), (136, 4928), (8, 4936), (1032, 5000), (2048, 4928)])
+def test_wide_blocks(T, d, f):
+    _check(T, d, f, act="gelu_tanh" if T % 2 else "silu", residual=T != 100,
+           grad_dtype=torch.float32 if d == 136 else torch.bfloat16)
+
+
 @pytest.mark.parametrize("T,d,f", [(7, 131072, 512), (900, 32768, 1024)])
 def test_waits_that_run_out_are_reported(T, d, f, monkeypatch):
     """With no time to wait the calls give up, say so and leave the context usable (the widths make
