@@ -673,67 +673,81 @@ struct Plan {
   double ns;  // estimate
 };
 
-// The estimate's terms, ns, by tile width: a K step of a pair; by mode, the least
+// The estimate's terms, ns, by tile width: by mode, a K step of a pair, the least
 // that a tile takes while all pairs' epilogues load and store, and the last tile's
 // epilogue; the store of a piece and the wait for it, and each piece that a
 // finisher adds.
 struct Cost {
-  double step, tile[4], tail[4], cut, piece;
+  double step[4], tile[4], tail[4], cut, piece;
 };
-constexpr Cost kCostWide{290, {7000, 3300, 13000, 3300}, {4500, 3300, 6500, 3300}, 2500, 1800};
-constexpr Cost kCostNarrow{165, {4000, 1900, 7000, 1900}, {2500, 1900, 3500, 1900}, 2000, 1000};
+constexpr Cost kCostWide{{290, 290, 290, 290}, {7000, 3300, 13000, 3300}, {4500, 3300, 6500, 3300}, 2500, 1800};
+constexpr Cost kCostNarrow{{165, 165, 165, 185}, {4000, 1900, 7000, 2100}, {2500, 1900, 3500, 1900}, 2000, 1000};
 constexpr double kClear = 3500;  // zeroing the flags, where no launch of the call has
 
-// Deals the tiles to the pairs, whole ones or every product's last ones cut, by
-// what is estimated to end first.
+// Deals the tiles to the pairs, whole ones, every product's last ones cut, or those
+// of the products with long K steps only, by what is estimated to end first.  A run
+// of short tiles takes as many epilogues (the backward of 7 rows, d = 1376, f = 3864,
+// whose weight gradients have one K step a tile: 101 us where the estimate counted
+// a run's K steps alone, 45 with the epilogues).
 Plan plan_tiles(const MlpParams& p, int mode, int bn, int pairs) {
   const Cost& k = bn == kWide ? kCostWide : kCostNarrow;
+  const double step = k.step[mode];
   const int cols = mode == MM_UP ? bn / 2 : bn;
-  int tiles[kMaxProbs], all = 0, longest = 0;
+  int tiles[kMaxProbs], all = 0;
   double ns[kMaxProbs];  // of a whole tile
   for (int i = 0; i < p.n_prob; ++i) {
     tiles[i] = p.pr[i].mt * static_cast<int>(ceil_div(p.pr[i].N, cols));
-    ns[i] = std::max(p.pr[i].ks * k.step, k.tile[mode]);
+    ns[i] = std::max(p.pr[i].ks * step, k.tile[mode]);
     all += tiles[i];
-    longest = std::max(longest, p.pr[i].ks);
   }
-  Plan w{bn, std::min(pairs, all), {}, 0};
-  w.cut.run = 1;
-  // whole, in turn: the pair with the most to do.  A product's last tiles go to
-  // neighbouring pairs, one each, from the pair on that its first tile went to; so
-  // the most is found at one of those pairs.
-  for (int j = 0, from = 0; j < p.n_prob; from = (from + tiles[j++]) % pairs) {
-    double load = 0;
-    for (int i = 0, first = 0; i < p.n_prob; first = (first + tiles[i++]) % pairs) {
-      const int skip = from >= first ? from - first : from - first + pairs;
-      load += (tiles[i] / pairs + (skip < tiles[i] % pairs ? 1 : 0)) * ns[i];
+  // The time of whole tiles dealt in turn: of the pair with the most to do.  A
+  // product's last tiles go to neighbouring pairs, one each, from the pair on that
+  // its first tile went to; so the most is found at one of those pairs.
+  const auto in_turn = [&](const int* whole) {
+    double most = 0;
+    for (int j = 0, from = 0; j < p.n_prob; from = (from + whole[j++]) % pairs) {
+      double load = 0;
+      for (int i = 0, first = 0; i < p.n_prob; first = (first + whole[i++]) % pairs) {
+        const int skip = from >= first ? from - first : from - first + pairs;
+        load += (whole[i] / pairs + (skip < whole[i] % pairs ? 1 : 0)) * ns[i];
+      }
+      most = std::max(most, load);
     }
-    w.ns = std::max(w.ns, load);
-  }
+    return most;
+  };
+  Plan w{bn, std::min(pairs, all), {}, in_turn(tiles) + k.tail[mode]};
+  w.cut.run = 1;
   for (int i = 0; i < p.n_prob; ++i) w.cut.whole[i] = tiles[i];
   w.cut.n_whole = all;
-  w.ns += k.tail[mode];
-  // every product's last tiles cut
-  MlpSplit s = {};
-  int64_t steps = 0;
-  double before = 0;
-  for (int i = 0; i < p.n_prob; ++i) {
-    const int rest = tiles[i] % pairs;
-    s.whole[i] = tiles[i] - rest;
-    s.n_whole += s.whole[i];
-    s.off[i] = static_cast<int>(steps);
-    steps += static_cast<int64_t>(rest) * p.pr[i].ks;
-    before += s.whole[i] / pairs * ns[i];
-    if (steps > (1 << 30)) return w;
-  }
-  if (steps == 0) return w;
-  s.steps = static_cast<int>(steps);
-  for (int m = 1; m <= 8; ++m) {  // longer runs on fewer pairs: fewer pieces
-    s.run = static_cast<int>(ceil_div(steps * m, pairs));
-    const double pieces = static_cast<double>(longest) / s.run;
-    double t = before + s.run * k.step + k.tail[mode] + k.cut + k.piece * pieces;
-    if (mode == MM_UP || mode == MM_DH) t += kClear;
-    if (t < w.ns) w = Plan{bn, s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, s.run)), s, t};
+  // the last tiles cut: of every product, of those that are not bound by epilogues
+  for (int some = 0; some < 2; ++some) {
+    MlpSplit s = {};
+    int64_t steps = 0;
+    int longest = 0;
+    double slow = step;  // a step of the shortest tiles
+    for (int i = 0; i < p.n_prob; ++i) {
+      const int rest = some && p.pr[i].ks * step <= k.tile[mode] ? 0 : tiles[i] % pairs;
+      s.whole[i] = tiles[i] - rest;
+      s.n_whole += s.whole[i];
+      s.off[i] = static_cast<int>(steps);
+      steps += static_cast<int64_t>(rest) * p.pr[i].ks;
+      if (steps > (1 << 30)) return w;
+      if (rest > 0) {
+        longest = std::max(longest, p.pr[i].ks);
+        slow = std::max(slow, ns[i] / p.pr[i].ks);
+      }
+    }
+    if (steps == 0) continue;
+    s.steps = static_cast<int>(steps);
+    const double before = in_turn(s.whole);
+    for (int m = 1; m <= 8; ++m) {  // longer runs on fewer pairs: fewer pieces
+      s.run = static_cast<int>(ceil_div(steps * m, pairs));
+      const double pieces = static_cast<double>(longest) / s.run;
+      // the run that adds another tile's pieces, or the one of short tiles
+      double t = before + k.tail[mode] + std::max(s.run * step + k.cut + k.piece * pieces, s.run * slow);
+      if (mode == MM_UP || mode == MM_DH) t += kClear;
+      if (t < w.ns) w = Plan{bn, s.n_whole > 0 ? pairs : static_cast<int>(ceil_div(steps, s.run)), s, t};
+    }
   }
   return w;
 }
