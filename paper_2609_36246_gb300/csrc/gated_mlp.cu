@@ -9,6 +9,7 @@
 //   MM_DOWN   h Wd^T, the residual added in the epilogue
 //   MM_DH     dy Wd; the epilogue reads g and u and writes dg, du and h
 //   MM_GRADS  the four products that are left, in one launch
+// Few rows take gated_mlp_few.cu's form, except for the weights' gradients.
 //
 // CTA pairs (clusters of two, tcgen05.mma.cta_group::2, M = 256): each CTA
 // stages its 128 rows of A and its half of the B rows (256 or 128 wide tiles), and
@@ -688,7 +689,7 @@ constexpr double kClear = 3500;  // zeroing the flags, where no launch of the ca
 // of the products with long K steps only, by what is estimated to end first.  A run
 // of short tiles takes as many epilogues (the backward of 7 rows, d = 1376, f = 3864,
 // whose weight gradients have one K step a tile: 101 us where the estimate counted
-// a run's K steps alone, 45 with the epilogues).
+// a run's K steps alone, 45 with the epilogues, both with dx in the launch).
 Plan plan_tiles(const MlpParams& p, int mode, int bn, int pairs) {
   const Cost& k = bn == kWide ? kCostWide : kCostNarrow;
   const double step = k.step[mode];
@@ -869,22 +870,30 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
   p.part = w.part;
   p.dev_status = dev_status;
 
-  p.n_prob = 1;
-  p.pr[0] = problem(T, f, d, 1, w.h, fp);
-  p.flag = w.flag;
-  p.clear = w.flag + mlp_flag_words();
-  p.n_clear = static_cast<int>(mlp_flag_words());
-  p.saved_g = static_cast<const uint16_t*>(saved);
-  p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
-  p.out_g = w.dg;
-  p.out_u = w.du;
-  auto dh = [&](MapSet& s, int) {
-    MlpProb& q = p.pr[0];
-    q.a0 = q.a1 = s.k_major(dy, T, d, d, kBM);
-    q.b0 = q.b1 = s.mn_major(W_down, d, f, f);
-  };
-  const olive_status st = act == OLIVE_ACT_SILU ? launch<MM_DH, OLIVE_ACT_SILU>(c, p, false, dh)
-                                                : launch<MM_DH, OLIVE_ACT_GELU_TANH>(c, p, false, dh);
+  const bool few = T <= kMlpFewRows;
+  olive_status st;
+  if (few) {
+    st = launch_mlp_few_bwd(c, dy, W_gate, W_up, W_down, saved, T, d, f, act, w, dx, grad_dtype, dev_status);
+    dx = nullptr;  // (done)
+    if (!dW_gate) return st;
+  } else {
+    p.n_prob = 1;
+    p.pr[0] = problem(T, f, d, 1, w.h, fp);
+    p.flag = w.flag;
+    p.clear = w.flag + mlp_flag_words();
+    p.n_clear = static_cast<int>(mlp_flag_words());
+    p.saved_g = static_cast<const uint16_t*>(saved);
+    p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
+    p.out_g = w.dg;
+    p.out_u = w.du;
+    auto dh = [&](MapSet& s, int) {
+      MlpProb& q = p.pr[0];
+      q.a0 = q.a1 = s.k_major(dy, T, d, d, kBM);
+      q.b0 = q.b1 = s.mn_major(W_down, d, f, f);
+    };
+    st = act == OLIVE_ACT_SILU ? launch<MM_DH, OLIVE_ACT_SILU>(c, p, false, dh)
+                               : launch<MM_DH, OLIVE_ACT_GELU_TANH>(c, p, false, dh);
+  }
   if (st != OLIVE_OK) return st;
 
   p.n_prob = 0;
@@ -898,7 +907,7 @@ olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const v
     p.pr[p.n_prob++] = problem(f, d, T, 1, dW_up, d);
     p.pr[p.n_prob++] = problem(d, f, T, 1, dW_down, f);
   }
-  return launch<MM_GRADS>(c, p, true, [&](MapSet& s, int) {
+  return launch<MM_GRADS>(c, p, !few, [&](MapSet& s, int) {
     if (dx) {
       MlpProb& q = p.pr[0];
       q.a0 = s.k_major(w.dg, T, f, fp, kBM);

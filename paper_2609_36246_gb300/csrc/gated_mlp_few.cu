@@ -1,12 +1,17 @@
 // gated_mlp_few.cu -- the gated feed-forward block on few rows (single tokens, a
-// batch's next tokens), forward: two launches that read the weights once.
+// batch's next tokens): the forward in two launches that read the weights once, and
+// the backward's products of the same shape, dh and dx, in two more.
 //
-// Few rows make the weights the wide operand: they are A (M = 128 weight rows in
-// the lanes), the tokens B (N = 16 to 128 columns), so one MMA shape serves any
-// count of tokens and the accumulator's columns are the tokens.
-//   launch 1  a CTA takes `rows` rows of W_gate and the same of W_up, into two
+// Few rows make the weights the wide operand: they are A (M = 128 of their rows or
+// columns in the lanes), the tokens B (N = 16 to 128 columns), so one MMA shape
+// serves any count of tokens and the accumulator's columns are the tokens.
+//   FEW_UP    a CTA takes `rows` rows of W_gate and the same of W_up, into two
 //             accumulators, so that a thread has g and u of its row; h = act(g) u
-//   launch 2  a CTA takes `rows` rows of W_down; y = h W_down^T (+ residual)
+//   FEW_DOWN  a CTA takes `rows` rows of W_down; y = h W_down^T (+ residual)
+//   FEW_DH    a CTA takes `rows` columns of W_down, read MN-major as they lie;
+//             dh = dy W_down, and from g and u dg, du and h
+//   FEW_DX    a CTA takes `rows` columns of W_gate, then the same of W_up, into one
+//             accumulator; dx = dg W_gate + du W_up
 // MMAs always cover 128 lanes: where a CTA has fewer rows the others read what
 // lies behind the tile in shared memory and their lanes are not read back.
 //
@@ -15,12 +20,14 @@
 // rows for that, the CTAs of a cluster share a tile's K steps and add their
 // accumulators up through distributed shared memory, every CTA for a part of the
 // tokens, in the cluster's order.  The second launch starts while the first runs
-// (programmatic dependent launch) and fills its stages with W_down before it waits
-// for h.
+// (programmatic dependent launch) and fills its stages with weights before it waits
+// for the first one's results.
 //
 // Measured, us, the weights in HBM: one token 54 at d = 4096, f = 12288 (5.6 TB/s
 // over 302 MB), 21 at 2048, 6144; 64 tokens 64 and 28; 128 tokens 75 and 36.  (In
-// gated_mlp.cu's form: one 138 and 49, 64 77 and 37, 128 79 and 38.)
+// gated_mlp.cu's form: one 138 and 49, 64 77 and 37, 128 79 and 38.)  Backward, with
+// the weights' gradients: one row 152 at 4096, 12288, 52 of them dh and dx (5.8 TB/s);
+// 16 rows 50 and 64 rows 56 at 2048, 6144 (200, 70 and 69 in gated_mlp.cu's form).
 #include <algorithm>
 #include <atomic>
 
@@ -38,15 +45,20 @@ constexpr int kTile = 128 * 128;      // bytes the MMA reads of an A tile
 // shared memory of a CTA: two to an SM, or one where the tokens' tile is large
 constexpr int budget(int n) { return (n <= 64 ? 108 : 210) * 1024; }
 
+enum { FEW_UP = 0, FEW_DOWN = 1, FEW_DH = 2, FEW_DX = 3 };
+
 struct FewMaps {
-  CUtensorMap a0, a1, b;  // W_gate, W_up (or W_down), tokens
+  CUtensorMap a0, a1;  // W_gate and W_up, or W_down
+  CUtensorMap b0, b1;  // tokens (FEW_DX: dg, du)
 };
 struct FewParams {
-  int T, rows_all, K;     // tokens, weight rows, inner width
+  int T, rows_all, K;     // tokens, weight rows (columns of the result), inner width
   int rows, stages;
-  void* out;              // h or y, [T, rows_all]
+  int ld, out_f32;        // FEW_DH: pitch of its results; FEW_DX: type of dx
+  void* out;              // h, y, h again or dx
   const __nv_bfloat16* residual;
-  uint16_t *saved_g, *saved_u;
+  uint16_t *saved_g, *saved_u;  // [T, rows_all], written by FEW_UP, read by FEW_DH
+  __nv_bfloat16 *out_g, *out_u; // FEW_DH: dg, du
   int32_t* dev_status;
   uint64_t wait_limit_ns;
 };
@@ -65,8 +77,11 @@ __device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t x, uint32_
                : "memory");
 }
 
-template <bool kUp, int kN, int kAct>
+template <int kMode, int kN, int kAct>
 __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ FewMaps maps, const FewParams p) {
+  constexpr bool kUp = kMode == FEW_UP;
+  constexpr bool kFirst = kMode == FEW_UP || kMode == FEW_DH;  // of its call
+  constexpr bool kMn = kMode == FEW_DH || kMode == FEW_DX;     // A is MN-major
   constexpr int kAcc = kUp ? 2 : 1;
   constexpr uint32_t kCols = kAcc * kN < 32 ? 32 : kAcc * kN;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -88,10 +103,9 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
   const int row0 = static_cast<int>(blockIdx.x) / c * p.rows;
   const int t0 = static_cast<int>(blockIdx.y) * kN;
   const int nt = min(kN, p.T - t0);
-  const int ks_all = (p.K + kBK - 1) / kBK;
+  const int ks_half = (p.K + kBK - 1) / kBK, ks_all = kMode == FEW_DX ? 2 * ks_half : ks_half;
   const int ks0 = ks_all * rank / c, ks1 = ks_all * (rank + 1) / c;
 
-  grid_launch_dependents();
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full_bar(s), 1);
@@ -103,12 +117,16 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
   }
   if (warp == kProducerWarp && lane == 0) {
     tma_prefetch_desc(&maps.a0);
-    if (kUp) tma_prefetch_desc(&maps.a1);
-    tma_prefetch_desc(&maps.b);
+    if (kUp || kMode == FEW_DX) tma_prefetch_desc(&maps.a1);
+    tma_prefetch_desc(&maps.b0);
+    if (kMode == FEW_DX) tma_prefetch_desc(&maps.b1);
   }
   if (warp == kMmaWarp) {
     tmem_alloc(smem_u32(tmem_slot), kCols);
     tmem_relinquish();
+    // (not before this CTA has its tensor memory: the next launch's CTAs take theirs
+    // and keep it while they wait for this grid)
+    grid_launch_dependents();
   }
   tc_fence_before();
   __syncthreads();
@@ -122,17 +140,25 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
     auto weights = [&](int s, int ks) {
       const uint32_t at = ring + s * stage_bytes;
       mbar_arrive_expect_tx(full_bar(s), stage_bytes);
-      tma_load_2d(at, &maps.a0, full_bar(s), ks * kBK, row0);
-      if (kUp) tma_load_2d(at + a_bytes, &maps.a1, full_bar(s), ks * kBK, row0);
+      if constexpr (kMn) {
+        const bool second = kMode == FEW_DX && ks >= ks_half;
+        for (int i = 0; i < p.rows; i += 64)
+          tma_load_2d(at + i * 128, second ? &maps.a1 : &maps.a0, full_bar(s), row0 + i, (second ? ks - ks_half : ks) * kBK);
+      } else {
+        tma_load_2d(at, &maps.a0, full_bar(s), ks * kBK, row0);
+        if (kUp) tma_load_2d(at + a_bytes, &maps.a1, full_bar(s), ks * kBK, row0);
+      }
     };
     auto tokens = [&](int s, int ks) {
-      tma_load_2d(ring + s * stage_bytes + kAcc * a_bytes, &maps.b, full_bar(s), ks * kBK, t0);
+      const bool second = kMode == FEW_DX && ks >= ks_half;
+      tma_load_2d(ring + s * stage_bytes + kAcc * a_bytes, second ? &maps.b1 : &maps.b0, full_bar(s),
+                  (second ? ks - ks_half : ks) * kBK, t0);
     };
     const int first = min(p.stages, ks1 - ks0);
     if (leader) {
       for (int s = 0; s < first; ++s) weights(s, ks0 + s);
-      // W_down does not depend on the launch before this one; h does
-      if (!kUp) {
+      // the weights do not depend on the launch before this one; h, dg and du do
+      if (!kFirst) {
         grid_wait();
         fence_proxy_async_global();
       }
@@ -153,19 +179,21 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
   } else if (warp == kMmaWarp) {
     const bool leader = elect_one();
     const uint32_t acc = warp_uniform(tmem_base);
-    const uint32_t id = idesc_bf16(128, kN, false, false);
+    const uint32_t id = idesc_bf16(128, kN, kMn, false);
     int s = 0;
     uint32_t phase = 0;
     for (int ks = ks0; ks < ks1; ++ks) {
       if (!mbar_wait_warp(full_bar(s), phase, ctl)) { ok = false; break; }
       tc_fence_after();
-      const uint64_t da = sdesc_sw128(ring + s * stage_bytes, 16, 1024);
+      // (MN-major: 16 K elements are 16 rows of 128 bytes, 64-element blocks 8 KB apart)
+      const uint64_t da = sdesc_sw128(ring + s * stage_bytes, kMn ? 64 * kBK * 2 : 16, 1024);
+      constexpr int kStepA = kMn ? 128 : 2;
       const uint64_t db = sdesc_sw128(ring + s * stage_bytes + kAcc * a_bytes, 16, 1024);
       if (leader) {
 #pragma unroll
         for (int kk = 0; kk < kBK / 16; ++kk) {
           const uint32_t go = ks > ks0 || kk > 0 ? 1u : 0u;
-          umma_bf16(acc, da + 2 * kk, db + 2 * kk, id, go);
+          umma_bf16(acc, da + kStepA * kk, db + 2 * kk, id, go);
           if (kUp) umma_bf16(acc + kN, da + (a_bytes >> 4) + 2 * kk, db + 2 * kk, id, go);
         }
         umma_commit(empty_bar(s));
@@ -180,8 +208,10 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
     const WaitCtl own{&keep_waiting, p.wait_limit_ns > floor_ns ? p.wait_limit_ns : floor_ns};
     mbar_wait_warp(done_bar, 0, own);
   } else {
-    // (the MMA warp commits to it in any case; its own waits are bounded)
-    ok = mbar_wait_warp(done_bar, 0, ctl);
+    // (the MMA warp commits to it in any case; its own waits are bounded.  This one
+    // lasts as long as the products, so looking at the limit each time costs nothing,
+    // and a limit that is shorter than they take is noticed)
+    ok = mbar_wait_warp<1>(done_bar, 0, ctl);
     tc_fence_after();
   }
 
@@ -194,30 +224,55 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
   const int tb = (warp >> 2) * (kN / 2), te = min(tb + kN / 2, nt);
   const bool epi = warp < kEpiWarps && ok && (warp & 3) * 32 < p.rows;
   __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out);
-  // one result from its sums
-  auto store = [&](float a, float b, size_t at) {
-    if (kUp) {
+  const int ld = kMode == FEW_DH ? p.ld : p.rows_all;  // pitch of the results
+  // g and u of FEW_DH, read ahead of a group's stores
+  auto before = [&](size_t at, uint32_t& g, uint32_t& u) {
+    if (kMode == FEW_DH) {
+      g = p.saved_g[at];
+      u = p.saved_u[at];
+    }
+  };
+  // one result from its sums; at: in the results, in: in what is saved
+  auto store = [&](float a, float b, uint32_t g, uint32_t u, size_t at, size_t in) {
+    if constexpr (kUp) {
       out[at] = __float2bfloat16_rn(activate<kAct>(a) * b);
       if (p.saved_g) {
-        p.saved_g[at] = static_cast<uint16_t>(saved_bits(a));
-        p.saved_u[at] = static_cast<uint16_t>(saved_bits(b));
+        p.saved_g[in] = static_cast<uint16_t>(saved_bits(a));
+        p.saved_u[in] = static_cast<uint16_t>(saved_bits(b));
       }
+    } else if constexpr (kMode == FEW_DH) {
+      float ag, slope;
+      activate_both<kAct>(saved_lo(g), ag, slope);
+      float uf = saved_lo(u);
+      if ((saved_nan(g) | saved_nan(u)) & 0x8000u) ag = slope = uf = __uint_as_float(0x7fffffffu);
+      p.out_g[at] = __float2bfloat16_rn(a * uf * slope);
+      p.out_u[at] = __float2bfloat16_rn(a * ag);
+      out[at] = __float2bfloat16_rn(ag * uf);
+    } else if constexpr (kMode == FEW_DX) {
+      if (p.out_f32)
+        static_cast<float*>(p.out)[at] = a;
+      else
+        out[at] = __float2bfloat16_rn(a);
     } else {
       out[at] = __float2bfloat16_rn(p.residual ? a + __bfloat162float(p.residual[at]) : a);
     }
   };
   if (c == 1) {
     const bool mine = epi && row < p.rows && row0 + row < p.rows_all;
-    size_t at = static_cast<size_t>(t0 + tb) * p.rows_all + row0 + row;
+    size_t at = static_cast<size_t>(t0 + tb) * ld + row0 + row;
+    size_t in = kMode == FEW_DH ? static_cast<size_t>(t0 + tb) * p.rows_all + row0 + row : 0;
 #pragma unroll 1
     for (int t = tb; epi && t < te; t += 8) {
-      uint32_t a[8], b[8];
+      uint32_t a[8], b[8], g[8] = {}, u[8] = {};
+#pragma unroll
+      for (int i = 0; kMode == FEW_DH && i < 8; ++i)
+        if (mine && t + i < te) before(in + static_cast<size_t>(i) * p.rows_all, g[i], u[i]);
       tmem_ld_32x32b_x8(lane_addr + t, a);
       if (kUp) tmem_ld_32x32b_x8(lane_addr + kN + t, b);
       tmem_ld_wait();
 #pragma unroll
-      for (int i = 0; i < 8; ++i, at += p.rows_all)
-        if (mine && t + i < te) store(__uint_as_float(a[i]), kUp ? __uint_as_float(b[i]) : 0.f, at);
+      for (int i = 0; i < 8; ++i, at += ld, in += p.rows_all)
+        if (mine && t + i < te) store(__uint_as_float(a[i]), kUp ? __uint_as_float(b[i]) : 0.f, g[i], u[i], at, kMode == FEW_DH ? in : at);
     }
   } else {
     // CTA q of the cluster finishes tokens [q per, (q + 1) per): every CTA sends
@@ -251,6 +306,11 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
       const int j = i / p.rows * 2, r = i - j / 2 * p.rows;
       if (row0 + r >= p.rows_all) continue;
       float2 a = {0.f, 0.f}, b = {0.f, 0.f};
+      const size_t t = t0 + rank * per + j;
+      const size_t at = t * ld + row0 + r, in = kMode == FEW_DH ? t * p.rows_all + row0 + r : at;
+      uint32_t g0 = 0, u0 = 0, g1 = 0, u1 = 0;
+      before(in, g0, u0);
+      if (j + 1 < my) before(in + p.rows_all, g1, u1);
       for (int q = 0; q < c; ++q) {
         const float* f = recv + (q * kAcc * p.rows + r) * per + j;
         const float2 x = *reinterpret_cast<const float2*>(f);
@@ -262,9 +322,8 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
           b.y += y.y;
         }
       }
-      const size_t at = static_cast<size_t>(t0 + rank * per + j) * p.rows_all + row0 + r;
-      store(a.x, b.x, at);
-      if (j + 1 < my) store(a.y, b.y, at + p.rows_all);
+      store(a.x, b.x, g0, u0, at, in);
+      if (j + 1 < my) store(a.y, b.y, g1, u1, at + ld, in + p.rows_all);
     }
   }
 
@@ -289,10 +348,11 @@ __global__ void __launch_bounds__(kThreads) few_kernel(const __grid_constant__ F
 // by 8.  The first launch has two accumulators to exchange and from n = 64 on is
 // quicker with whole K steps (23.2 us with 64 rows by 1, 27.5 by 2; n = 128, d =
 // 4096, f = 12288: 73.6 with 88 rows by 1, 93.0 by 2).
+// MN-major weights come in blocks of 64 (`least`).
 struct FewShape {
   int rows, c;
 };
-FewShape few_shape(int rows_all, int ks, int tiles, int n, int sms, bool up) {
+FewShape few_shape(int rows_all, int ks, int tiles, int n, int sms, bool up, int least) {
   const int slots = n <= 64 ? 2 * sms : sms;  // CTAs that run at once
   const int most = (n < 128 ? 16 : 32) * 1024 / (4 * n * (up ? 2 : 1));
   FewShape s{std::min(128, std::max(64, most)), 1};
@@ -306,25 +366,26 @@ FewShape few_shape(int rows_all, int ks, int tiles, int n, int sms, bool up) {
   // than a larger cluster (64 tokens, d = 1024, f = 2816: 17.2 us with 32 rows by 1,
   // 18.6 with 64 by 2)
   const int enough = up && n >= 64 ? sms / 2 : sms / 8;
-  while (s.rows > 32 && ctas() < enough) s.rows = s.rows > 64 ? 64 : 32;
+  while (s.rows > least && ctas() < enough) s.rows = s.rows > 64 ? 64 : 32;
   const int c_most = up && n >= 64 && 2 * ctas() >= sms ? 1 : 8;
   while (s.c < c_most && 2 * ctas() <= slots && ks >= 8 * s.c) s.c *= 2;
   return s;
 }
 
-template <bool kUp, int kN, int kAct>
+template <int kMode, int kN, int kAct>
 olive_status launch_few(const Ctx& c, const FewMaps& maps, FewParams p, const FewShape& s) {
+  constexpr bool kUp = kMode == FEW_UP, kFirst = kUp || kMode == FEW_DH;
   constexpr int kAcc = kUp ? 2 : 1;
   const int stage = kAcc * p.rows * 128 + kN * 128;
   // the MMAs read 128 rows from the last stage's last A
   const int past = std::max(0, (kAcc - 1) * p.rows * 128 + kTile - stage);
-  const int ks = static_cast<int>(ceil_div(ceil_div(p.K, kBK), s.c));
+  const int ks = static_cast<int>(ceil_div((kMode == FEW_DX ? 2 : 1) * ceil_div(p.K, kBK), s.c));
   p.stages = std::min({(budget(kN) - 1024 - past) / stage, kMaxStages, ks});
   const int exchange = s.c > 1 ? 4 * kAcc * p.rows * kN : 0;
   const int smem = 1024 + std::max(p.stages * stage + past, exchange);
   p.wait_limit_ns = c.wait_limit_ns;
   static std::atomic<int> done[kMaxDevices];
-  if (!set_smem_once(reinterpret_cast<const void*>(few_kernel<kUp, kN, kAct>), 227 * 1024, c.device, done))
+  if (!set_smem_once(reinterpret_cast<const void*>(few_kernel<kMode, kN, kAct>), 227 * 1024, c.device, done))
     return OLIVE_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(ceil_div(p.rows_all, p.rows) * s.c), static_cast<unsigned>(ceil_div(p.T, kN)));
@@ -339,22 +400,24 @@ olive_status launch_few(const Ctx& c, const FewMaps& maps, FewParams p, const Fe
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = kUp ? 1 : 2;  // (only the second launch may start before the one ahead of it ends)
-  if (cudaLaunchKernelEx(&cfg, few_kernel<kUp, kN, kAct>, maps, p) != cudaSuccess) {
+  cfg.numAttrs = kFirst ? 1 : 2;  // (only the second launch may start before the one ahead of it ends)
+  if (cudaLaunchKernelEx(&cfg, few_kernel<kMode, kN, kAct>, maps, p) != cudaSuccess) {
     cudaGetLastError();
     return OLIVE_ERR_CUDA;
   }
   return OLIVE_OK;
 }
 
-template <bool kUp, int kAct>
+template <int kMode, int kAct>
 olive_status by_tokens(const Ctx& c, const FewMaps& maps, const FewParams& p, int n, const FewShape& s) {
   switch (n) {
-    case 16: return launch_few<kUp, 16, kAct>(c, maps, p, s);
-    case 32: return launch_few<kUp, 32, kAct>(c, maps, p, s);
-    case 64: return launch_few<kUp, 64, kAct>(c, maps, p, s);
-    default: return launch_few<kUp, 128, kAct>(c, maps, p, s);
+    case 16: return launch_few<kMode, 16, kAct>(c, maps, p, s);
+    case 32: return launch_few<kMode, 32, kAct>(c, maps, p, s);
+    case 64: return launch_few<kMode, 64, kAct>(c, maps, p, s);
+    default: break;
   }
+  if constexpr (kMode == FEW_UP || kMode == FEW_DOWN) return launch_few<kMode, 128, kAct>(c, maps, p, s);
+  return OLIVE_ERR_SHAPE;
 }
 
 }  // namespace
@@ -370,7 +433,7 @@ olive_status launch_mlp_few(const Ctx& c, const void* x, const void* W_gate, con
   p.T = T;
   p.dev_status = dev_status;
 
-  FewShape s = few_shape(f, static_cast<int>(ceil_div(d, kBK)), tiles, n, c.num_sms, true);
+  FewShape s = few_shape(f, static_cast<int>(ceil_div(d, kBK)), tiles, n, c.num_sms, true, 32);
   p.rows_all = f;
   p.K = d;
   p.rows = s.rows;
@@ -379,13 +442,13 @@ olive_status launch_mlp_few(const Ctx& c, const void* x, const void* W_gate, con
   p.saved_u = saved ? p.saved_g + static_cast<size_t>(T) * f : nullptr;
   if (!encode_bf16_2d(&m.a0, W_gate, d, f, 2ull * d, kBK, s.rows) ||
       !encode_bf16_2d(&m.a1, W_up, d, f, 2ull * d, kBK, s.rows) ||
-      !encode_bf16_2d(&m.b, x, d, T, 2ull * d, kBK, n))
+      !encode_bf16_2d(&m.b0, x, d, T, 2ull * d, kBK, n))
     return OLIVE_ERR_CUDA;
-  const olive_status st = act == OLIVE_ACT_SILU ? by_tokens<true, OLIVE_ACT_SILU>(c, m, p, n, s)
-                                                : by_tokens<true, OLIVE_ACT_GELU_TANH>(c, m, p, n, s);
+  const olive_status st = act == OLIVE_ACT_SILU ? by_tokens<FEW_UP, OLIVE_ACT_SILU>(c, m, p, n, s)
+                                                : by_tokens<FEW_UP, OLIVE_ACT_GELU_TANH>(c, m, p, n, s);
   if (st != OLIVE_OK) return st;
 
-  s = few_shape(d, static_cast<int>(ceil_div(f, kBK)), tiles, n, c.num_sms, false);
+  s = few_shape(d, static_cast<int>(ceil_div(f, kBK)), tiles, n, c.num_sms, false, 32);
   p.rows_all = d;
   p.K = f;
   p.rows = s.rows;
@@ -393,9 +456,49 @@ olive_status launch_mlp_few(const Ctx& c, const void* x, const void* W_gate, con
   p.residual = static_cast<const __nv_bfloat16*>(residual);
   p.saved_g = p.saved_u = nullptr;
   if (!encode_bf16_2d(&m.a0, W_down, f, d, 2ull * f, kBK, s.rows) ||
-      !encode_bf16_2d(&m.b, h, f, T, 2ull * f, kBK, n))
+      !encode_bf16_2d(&m.b0, h, f, T, 2ull * f, kBK, n))
     return OLIVE_ERR_CUDA;
-  return by_tokens<false, 0>(c, m, p, n, s);
+  return by_tokens<FEW_DOWN, 0>(c, m, p, n, s);
+}
+
+olive_status launch_mlp_few_bwd(const Ctx& c, const void* dy, const void* W_gate, const void* W_up,
+                                const void* W_down, const void* saved, int32_t T, int32_t d,
+                                int32_t f, int act, const MlpWs& w, void* dx, int grad_dtype,
+                                int32_t* dev_status) {
+  const int n = T <= 16 ? 16 : T <= 32 ? 32 : 64;
+  const int fp = static_cast<int>(mlp_pitch(f));
+  FewMaps m = {};
+  FewParams p = {};
+  p.T = T;
+  p.dev_status = dev_status;
+
+  FewShape s = few_shape(f, static_cast<int>(ceil_div(d, kBK)), 1, n, c.num_sms, false, 64);
+  p.rows_all = f;
+  p.K = d;
+  p.rows = s.rows;
+  p.out = w.h;
+  p.out_g = static_cast<__nv_bfloat16*>(w.dg);
+  p.out_u = static_cast<__nv_bfloat16*>(w.du);
+  p.ld = fp;
+  p.saved_g = static_cast<uint16_t*>(const_cast<void*>(saved));
+  p.saved_u = p.saved_g + static_cast<size_t>(T) * f;
+  if (!encode_bf16_2d(&m.a0, W_down, f, d, 2ull * f, 64, kBK) || !encode_bf16_2d(&m.b0, dy, d, T, 2ull * d, kBK, n))
+    return OLIVE_ERR_CUDA;
+  const olive_status st = act == OLIVE_ACT_SILU ? by_tokens<FEW_DH, OLIVE_ACT_SILU>(c, m, p, n, s)
+                                                : by_tokens<FEW_DH, OLIVE_ACT_GELU_TANH>(c, m, p, n, s);
+  if (st != OLIVE_OK || !dx) return st;
+
+  s = few_shape(d, 2 * static_cast<int>(ceil_div(f, kBK)), 1, n, c.num_sms, false, 64);
+  p.rows_all = d;
+  p.K = f;
+  p.rows = s.rows;
+  p.out = dx;
+  p.out_f32 = grad_dtype == OLIVE_DTYPE_F32;
+  if (!encode_bf16_2d(&m.a0, W_gate, d, f, 2ull * d, 64, kBK) ||
+      !encode_bf16_2d(&m.a1, W_up, d, f, 2ull * d, 64, kBK) ||
+      !encode_bf16_2d(&m.b0, w.dg, f, T, 2ull * fp, kBK, n) || !encode_bf16_2d(&m.b1, w.du, f, T, 2ull * fp, kBK, n))
+    return OLIVE_ERR_CUDA;
+  return by_tokens<FEW_DX, 0>(c, m, p, n, s);
 }
 
 }  // namespace olive

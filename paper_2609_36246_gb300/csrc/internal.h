@@ -392,6 +392,12 @@ olive_status launch_mlp_few(const Ctx& c, const void* x, const void* W_gate, con
                             const void* W_down, const void* residual, int32_t T, int32_t d,
                             int32_t f, int act, void* y, void* saved, void* h,
                             int32_t* dev_status);
+// The backward's dh (with dg, du and h, to the workspace w) and, where asked for,
+// dx on up to kMlpFewRows rows.
+olive_status launch_mlp_few_bwd(const Ctx& c, const void* dy, const void* W_gate, const void* W_up,
+                                const void* W_down, const void* saved, int32_t T, int32_t d,
+                                int32_t f, int act, const MlpWs& w, void* dx, int grad_dtype,
+                                int32_t* dev_status);
 olive_status launch_mlp_bwd(const Ctx& c, const void* dy, const void* x, const void* W_gate,
                             const void* W_up, const void* W_down, const void* saved, int32_t T,
                             int32_t d, int32_t f, int act, void* dx, void* dW_gate, void* dW_up,

@@ -110,13 +110,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
 // every operand moves over from a thread's registers at each instruction: a K
 // step of two copies or four MMAs took 370 to 480 cycles to issue, of the
 // 480 to 540 its MMAs run.
+//
+// The limit is looked at every kEvery tries (a power of two).
+template <uint32_t kEvery = 16>
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const WaitCtl& ctl) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   const uint64_t t0 = global_timer_ns();
   uint32_t it = 0;
   while (true) {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    if ((++it & 15u) == 0) {
+    if ((++it & (kEvery - 1)) == 0) {
       const bool late = global_timer_ns() - t0 > ctl.limit_ns;
       if (late) *ctl.abort = 1;
       if (__any_sync(0xffffffffu, late || *ctl.abort != 0)) return false;

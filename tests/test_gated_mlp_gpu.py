@@ -293,6 +293,56 @@ def test_wide_blocks(T, d, f):
            grad_dtype=torch.float32 if d == 136 else torch.bfloat16)
 
 
+# the backward of few rows: each count of tokens, widths that end inside a block of 64 columns or
+# just behind one, K steps whole and shared by clusters
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 32, 33, 63, 64, 65])
+@pytest.mark.parametrize("d,f", [(8, 8), (56, 72), (64, 128), (136, 192), (200, 4104), (4104, 200), (1376, 3864)])
+def test_few_rows_backward(T, d, f):
+    _check(T, d, f, act="silu" if T % 2 else "gelu_tanh", grad_dtype=torch.float32 if T in (15, 33, 64) else torch.bfloat16)
+
+
+@pytest.mark.parametrize("T", [1, 20, 64, 65])
+@pytest.mark.parametrize("grad_dtype", [torch.bfloat16, torch.float32])
+def test_parts_of_the_backward(T, grad_dtype):
+    """dx alone and the weights' gradients alone, again and again: the same bits each time, on few rows
+    those of the call for all (with more rows the products' sums are cut by what else is asked for),
+    and right."""
+    s = _case(T, 520, 1416)
+    w = (s["W_gate"], s["W_up"], s["W_down"])
+    y, saved = B.olive_gated_mlp_fwd(s["x"], *w, save=True)
+    back = lambda **k: B.olive_gated_mlp_bwd(s["dy"], s["x"], *w, saved, grad_dtype=grad_dtype, **k)
+    whole, dx, dw = back(), back(need_dW=False), back(need_dx=False)
+    assert dx[1:] == (None, None, None) and dw[0] is None
+    same = lambda a, b: all(torch.equal(g, h) for g, h in zip(a, b) if g is not None)
+    for _ in range(5):
+        assert same(back(need_dW=False), dx) and same(back(need_dx=False), dw) and same(back(), whole)
+    if T <= 64:
+        assert same(dx, whole) and same(dw, whole)
+    _, ref = _reference(s, "silu")
+    _, bounds = _bounds(s, "silu")
+    tol = ROWS_RTOL if grad_dtype == torch.bfloat16 else F32_RTOL
+    for g, r, e in zip((dx[0],) + dw[1:], ref, bounds):
+        _close(g, r, tol, "part", e)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_few_rows_backward_keeps_a_bad_row_to_itself(bad):
+    """A row of x or dy that is not finite leaves the other rows' dx as they were; its own is NaN."""
+    T, d, f, at = 37, 136, 328, 18
+    s = _case(T, d, f)
+    w = (s["W_gate"], s["W_up"], s["W_down"])
+    y, saved = B.olive_gated_mlp_fwd(s["x"], *w, save=True)
+    want = B.olive_gated_mlp_bwd(s["dy"], s["x"], *w, saved, need_dW=False)[0]
+    rest = [i for i in range(T) if i != at]
+    for name in ("x", "dy"):
+        t = {k: s[k].clone() for k in ("x", "dy")}
+        t[name][at, 3] = bad
+        y, saved = B.olive_gated_mlp_fwd(t["x"], *w, save=True)
+        dx = B.olive_gated_mlp_bwd(t["dy"], t["x"], *w, saved, need_dW=False)[0]
+        assert torch.equal(dx[rest], want[rest])
+        assert not torch.isfinite(dx[at]).any()
+
+
 @pytest.mark.parametrize("T,d,f", [(7, 131072, 512), (900, 32768, 1024)])
 def test_waits_that_run_out_are_reported(T, d, f, monkeypatch):
     """With no time to wait the calls give up, say so and leave the context usable (the widths make
