@@ -23,8 +23,8 @@
 // (programmatic dependent launch) and fills its stages with weights before it waits
 // for the first one's results.
 //
-// Measured, us, the weights in HBM: one token 54 at d = 4096, f = 12288 (5.6 TB/s
-// over 302 MB), 21 at 2048, 6144; 64 tokens 64 and 28; 128 tokens 75 and 36.  (In
+// Measured, us, the weights in HBM: one token 53 at d = 4096, f = 12288 (5.7 TB/s
+// over 302 MB), 21 at 2048, 6144; 64 tokens 63 and 29; 128 tokens 75 and 37.  (In
 // gated_mlp.cu's form: one 138 and 49, 64 77 and 37, 128 79 and 38.)  Backward, with
 // the weights' gradients: one row 152 at 4096, 12288, 52 of them dh and dx (5.8 TB/s);
 // 16 rows 50 and 64 rows 56 at 2048, 6144 (200, 70 and 69 in gated_mlp.cu's form).

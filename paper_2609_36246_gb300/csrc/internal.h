@@ -380,7 +380,7 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
 // The forward on few rows (gated_mlp_few.cu); h: workspace [T, f].
 // It is taken up to 64 rows, and up to 128 where the first launch's tiles of 64
 // weight rows are more than half of the SMs.  Measured, us, this form and the other:
-// 64 rows (2048, 6144) 28 and 37, (1024, 2816) 17 and 21, (4096, 2816) 35 and 30;
+// 64 rows (2048, 6144) 29 and 37, (1024, 2816) 17 and 21, (4096, 2816) 35 and 30;
 // 80 rows (4096, 11008) 69 and 75, (2040, 5464) 35 and 40, (2560, 8192) 48 and 44,
 // but (2560, 5120) 42 and 39, (2048, 4096) 33 and 28, (512, 1536) 19 and 16 and (256,
 // 704) 18 and 13, of which the rule lets the first of the four through.
