@@ -5,8 +5,8 @@
 // b, b + blocks, ...  A thread squares 64 bytes of a unit at a time (32 bf16 or 16
 // fp32 values) into one fp32 sum and adds that to an fp64 sum.  Where that fp32
 // sum is not finite, large or nearly zero the same values, still in registers,
-// are squared again in fp64: squares leave fp32's range long before the values
-// do.  Every block's total goes to the workspace.
+// are squared again scaled by a power of two: squares leave fp32's range long
+// before the values do.  Every block's total goes to the workspace.
 //
 // The second launch adds the blocks' totals (each block by itself: a few KB from
 // L2), and scales, from the last unit to the first: what the first launch read
@@ -76,16 +76,24 @@ __device__ __forceinline__ double squares(const uint4 (&v)[kVecs]) {
     for (int i = 0; i < kPer; ++i) q = fmaf(x[i], x[i], q);
   }
   if (q < 1e36f && q > 1e-28f) return q;
+  if (q != q) return q;  // a NaN among them: so it is in any width
   if ((any & (kF32 ? 0x7fffffffu : 0x7fff7fffu)) == 0) return 0.0;
-  double d = 0.0;
+  // The squares again, of values scaled by a power of two.  Small: none is above 1e-14,
+  // so that 2^100 of it is at most 1.3e16, and the least fp32 value becomes 1.8e-15.
+  // Large: 2^-70 of the largest fp32 value is 2.9e17; what it flushes is nothing beside
+  // a value of 1.7e17 or more.  (The norm of 1 GB of values like 1e-30 or 1e30 takes
+  // 168 us, 1902 with squares in fp64; in range 143.)
+  const bool small = q <= 1e-28f;
+  const float by = small ? 0x1p100f : 0x1p-70f;
+  q = 0.f;
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
     float x[kPer];
     widen<kF32>(v[k], x);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) d = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), d);
+    for (int i = 0; i < kPer; ++i) q = fmaf(x[i] * by, x[i] * by, q);
   }
-  return d;
+  return static_cast<double>(q) * (small ? 0x1p-200 : 0x1p140);
 }
 
 // A vector scaled by f.

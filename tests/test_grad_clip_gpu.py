@@ -78,6 +78,26 @@ def test_squares_outside_fp32(scale, dtype):
     _check(_grads([(5000,), (77, 33)], [dtype], scale), 1e-3, "inplace")
 
 
+# the ends of the types' ranges, and both sides of the sums at which the squares are scaled (1e-28
+# and 1e36); the norm of the largest ones stays within
+# fp32, and 1 / norm, subnormal there, keeps 21 bits
+@pytest.mark.parametrize("value,count", [
+    (1e-45, 5000), (9.2e-41, 5000), (1.2e-38, 5000), (1.7e-15, 4097), (1.8e-15, 4097), (2.5e-15, 4097), (1e-14, 1), (1.1e-14, 1),
+    (1.7e17, 4097), (1.8e17, 4097), (2.5e17, 4097), (9.9e17, 1), (1.01e18, 1), (3.3e38, 1), (1e37, 900)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_ends_of_the_range(value, count, dtype):
+    g = [torch.full((count,), value, device="cuda").to(dtype)]
+    g[0][::3] *= -1
+    _check(g, 1.0, "inplace")
+
+
+@pytest.mark.parametrize("big,small", [(1e-15, 1e-45), (1e-15, 1e-30), (1e-12, 1e-40), (1.5e38, 1e-45), (1e18, 1e-3), (1e18, 1e17)])
+def test_ends_of_the_range_within_a_vector(big, small):
+    g = torch.full((4000,), small, device="cuda")
+    g[5::1000] = big
+    _check([g], 1.0, "inplace")
+
+
 def test_large_beside_small():
     g = _grads([(9000,), (9000,)], [torch.float32])
     g[0] *= 1e25
