@@ -169,6 +169,9 @@ def _check(st: int, where: str):
 def _need(t, dtype, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous CUDA {dtype} tensor")
+    # the call goes to the current device's stream, where another device's address is a stray one
+    if t.get_device() != torch.cuda.current_device():
+        raise TypeError(f"{name} must be on the current CUDA device, {torch.cuda.current_device()}")
 
 
 def new_status(device=None) -> torch.Tensor:
@@ -621,12 +624,20 @@ def _need_all(tensors, dtype, names):
             if t.dtype is not dtype:
                 break
         else:
-            if min(map(_device_of, tensors)) >= 0 and all(map(_is_dense, tensors)):
+            if set(map(_device_of, tensors)) == {torch.cuda.current_device()} and all(map(_is_dense, tensors)):
                 return
     except (TypeError, AttributeError):
         pass
     for t, n in zip(tensors, names):
         _need(t, dtype, n)
+
+
+def _need_given(ws, dev_status):
+    """The checks of a workspace and a status word that the caller brings."""
+    if ws is not None:
+        _need(ws, ws.dtype, "ws")
+    if dev_status is not None:
+        _need(dev_status, _I32, "dev_status")
 
 
 @functools.lru_cache(maxsize=4096)
@@ -661,9 +672,10 @@ def _heads(t, shape, dtype, name, device):
 def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
     """Checks what the heads' forward and backward share; (views of q and k, the
     shared C arguments, their shapes, dtype, device)."""
-    if (not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or not q.is_cuda or
+    if (not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or
+            _device_of(q) != torch.cuda.current_device() or
             q.dtype not in DTYPE or q.dim() != 3 or k.dim() != 3):
-        raise TypeError("q and k must be CUDA bf16 or fp32 tensors [T, heads, D]")
+        raise TypeError("q and k must be bf16 or fp32 tensors [T, heads, D] on the current CUDA device")
     sq, sk, dtype, dev = q.shape, k.shape, q.dtype, q.device
     T, Hq, D = sq
     if sk[0] != T or sk[2] != D:
@@ -705,6 +717,7 @@ def olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps: float = 1e-
     contiguous unless given as `out` (views, or q and k themselves)."""
     vq, vk, common, sq, sk, dtype, dev = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
     yq, yk, oq, ok = _qk_out(out, sq, sk, dtype, dev)
+    _need_given(None, dev_status)
     st = lib().olive_qk_norm_rope_fwd(*vq, *vk, *common, *oq, *ok, DTYPE[dtype], _ptr(dev_status),
                                       _stream())
     if st:
@@ -720,6 +733,7 @@ def olive_qk_norm_rope_bwd(g_q, g_k, q, k, w_q, w_k, cos, sin, positions, eps: f
     vq, vk, common, sq, sk, dtype, dev = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
     gq, gk = _heads(g_q, sq, dtype, "g_q", dev), _heads(g_k, sk, dtype, "g_k", dev)
     dq, dk, oq, ok = _qk_out(out, sq, sk, dtype, dev)
+    _need_given(ws, dev_status)
     D = sq[2]
     dwq, dwk = torch.empty(D, dtype=_F32, device=dev), torch.empty(D, dtype=_F32, device=dev)
     if ws is None:
@@ -763,6 +777,7 @@ def olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual=None, act: str = "silu
         _need(out, _BF16, "out")
         if out.shape != x.shape:
             raise ValueError("out must have the shape of x")
+    _need_given(ws, dev_status)
     saved = torch.empty((2, T, f), dtype=torch.int16, device=dev) if save else None
     if ws is None:
         ws = _bytes(_ws_bytes(10, T, d, f, 0, 0), dev)
@@ -800,6 +815,7 @@ def olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, act: str = "silu",
                 if t.shape != shape:
                     raise ValueError("out must have the shapes of x and the weights")
     kind = DTYPE[grad_dtype]
+    _need_given(ws, dev_status)
     if ws is None:
         ws = _bytes(_ws_bytes(11, T, d, f, 1, kind), dev)
     st = lib().olive_gated_mlp_bwd(dy.data_ptr(), x.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(),
@@ -847,6 +863,7 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
         norm = torch.empty(1, dtype=_F32, device="cuda")
     else:
         _need(norm, _F32, "norm")
+    _need_given(ws, None)
     if ws is None:
         ws = _bytes(_ws_bytes(13, max(n, 1), 0, 1, 0, 0), "cuda")
     # the four host arrays behind one another

@@ -1,0 +1,92 @@
+"""What the Python entry points of the layer's calls decide by themselves, on the host (host_calls.py):
+nothing here launches a kernel."""
+
+import pytest
+import torch
+
+from paper_2609_36246_gb300 import binding as B
+from tests import host_calls
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture
+def rec(monkeypatch):
+    return host_calls.recorded(monkeypatch)
+
+
+def _mlp(T=4, d=64, f=72):
+    r = lambda *s: torch.randn(*s).to(BF16)
+    return dict(x=r(T, d), W_gate=r(f, d), W_up=r(f, d), W_down=r(d, f), residual=r(T, d), dy=r(T, d),
+                saved=torch.zeros(2, T, f, dtype=torch.int16))
+
+
+def _qk(T=5, hq=3, hk=2, D=64, R=64, dtype=BF16):
+    r = lambda *s: torch.randn(*s).to(dtype)
+    return dict(q=r(T, hq, D), k=r(T, hk, D), w_q=r(D), w_k=r(D), cos=torch.ones(9, R // 2), sin=torch.zeros(9, R // 2),
+                positions=torch.arange(T, dtype=torch.int32), g_q=r(T, hq, D), g_k=r(T, hk, D))
+
+
+def _extra():
+    """A workspace and a status word of the caller's."""
+    return dict(ws=torch.zeros(4096, dtype=torch.uint8), dev_status=torch.zeros(1, dtype=torch.int32))
+
+
+def _like_outputs(s, *names):
+    return {"out%d" % i: torch.empty_like(s[n]) for i, n in enumerate(names)}
+
+
+# each call as (its tensors, the call of them): every tensor of it in turn is on another device
+def _calls():
+    s, e = _mlp(), _extra()
+    yield {**{k: s[k] for k in ("x", "W_gate", "W_up", "W_down", "residual")}, **_like_outputs(s, "x"), **e}, lambda t: \
+        B.olive_gated_mlp_fwd(t["x"], t["W_gate"], t["W_up"], t["W_down"], t["residual"], ws=t["ws"],
+                              dev_status=t["dev_status"], out=t["out0"])
+    s, e = _mlp(), _extra()
+    weights = ("W_gate", "W_up", "W_down")
+    yield {**{k: v for k, v in s.items() if k != "residual"}, **_like_outputs(s, "x", *weights), **e}, lambda t: \
+        B.olive_gated_mlp_bwd(t["dy"], t["x"], *(t[n] for n in weights), t["saved"], ws=t["ws"],
+                              dev_status=t["dev_status"], out=[t["out%d" % i] for i in range(4)])
+    names = ("q", "k", "w_q", "w_k", "cos", "sin", "positions")
+    s, e = _qk(), _extra()
+    yield {**{k: s[k] for k in names}, **_like_outputs(s, "q", "k"), "dev_status": e["dev_status"]}, lambda t: \
+        B.olive_qk_norm_rope_fwd(*(t[n] for n in names), dev_status=t["dev_status"], out=(t["out0"], t["out1"]))
+    s, e = _qk(), _extra()
+    yield {**s, **_like_outputs(s, "q", "k"), **e}, lambda t: \
+        B.olive_qk_norm_rope_bwd(t["g_q"], t["g_k"], *(t[n] for n in names), ws=t["ws"], dev_status=t["dev_status"],
+                                 out=(t["out0"], t["out1"]))
+    yield dict(cu=torch.zeros(3, dtype=torch.int32), out=torch.zeros(7, dtype=torch.int32)), lambda t: \
+        B.olive_packed_positions(t["cu"], 7, out=t["out"])
+    yield dict(g=torch.ones(5), h=torch.ones(6), a=torch.ones(5), b=torch.ones(6), norm=torch.ones(1), ws=_extra()["ws"]), \
+        lambda t: B.olive_grad_clip([t["g"], t["h"]], 1.0, out=[t["a"], t["b"]], norm=t["norm"], ws=t["ws"])
+
+
+def test_tensors_of_another_device_are_refused(rec):
+    for tensors, call in _calls():
+        call(tensors)
+        made = len(rec.calls)
+        for name, t in tensors.items():
+            rec.place(t, 1)
+            with pytest.raises(TypeError):
+                call(tensors)
+            rec.place(t, 0)
+        # (all of them elsewhere: the launch would still go to the current device)
+        for t in tensors.values():
+            rec.place(t, 1)
+        with pytest.raises(TypeError):
+            call(tensors)
+        assert len(rec.calls) == made
+
+
+def test_calls_before_them_refuse_it_too(rec):
+    h, W = torch.zeros(4, 64, dtype=BF16), torch.zeros(50, 64, dtype=BF16)
+    ids = [torch.zeros(4, dtype=torch.int32) for _ in range(3)]
+    run = lambda: B.olive_token_logprob_fwd(h, W, *ids)
+    run()
+    made = len(rec.calls)
+    for t in (h, W, *ids):
+        rec.place(t, 1)
+        with pytest.raises(TypeError):
+            run()
+        rec.place(t, 0)
+    assert len(rec.named("olive_token_logprob_fwd")) == 1 and len(rec.calls) == made
