@@ -839,11 +839,33 @@ def _grad_list(tensors, cur, what):
     return list(map(_ptr_of, tensors)), list(map(_numel_of, tensors)), kinds
 
 
+def _apart(starts, ends):
+    """Whether no two spans of addresses share a byte: as many end as begin before the
+    next one does (so an empty one may lie anywhere)."""
+    return all(map(operator.le, sorted(ends), sorted(starts)[1:]))
+
+
+def _need_apart(src, dst, counts, kinds):
+    """Refuses outputs that share memory with one another or with another gradient: the
+    blocks of one tensor would write what those of the other read or write."""
+    sizes = [n << 1 + k for n, k in zip(counts, kinds)]  # (kind 0 is bf16, 1 fp32)
+    ends = list(map(operator.add, dst, sizes))
+    fine = _apart(dst, ends)
+    if fine and src is not dst:
+        # gradients that are only read may share memory with one another
+        read = [(a, a + n) for a, d, n in zip(src, dst, sizes) if a != d]
+        fine = (_apart(dst + [a for a, _ in read], ends + [b for _, b in read]) or
+                all(_apart(dst + [a], ends + [b]) for a, b in read))
+    if not fine:
+        raise ValueError("a gradient that is scaled must not share memory with another (a tied one is listed once)")
+
+
 def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     """The 2-norm over all elements of `grads` (bf16 or fp32 CUDA tensors,
     contiguous) as a 1-element fp32 tensor, and the gradients scaled by
     min(1, max_norm / (norm + 1e-6)): in place, into the list `out`, or not at
-    all (out=None: only the norm)."""
+    all (out=None: only the norm).  What is written must not share memory with
+    another gradient or output."""
     n = len(grads)
     cur = torch.cuda.current_device()
     src, num, kinds = _grad_list(grads, cur, "gradients")
@@ -859,6 +881,7 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
             dst, sizes, types = _grad_list(out, cur, "out")
             if sizes != num or types != kinds:
                 raise TypeError("out must be like the gradients")
+        _need_apart(src, dst, num, kinds)
     if norm is None:
         norm = torch.empty(1, dtype=_F32, device="cuda")
     else:

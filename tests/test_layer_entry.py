@@ -90,3 +90,41 @@ def test_calls_before_them_refuse_it_too(rec):
             run()
         rec.place(t, 0)
     assert len(rec.named("olive_token_logprob_fwd")) == 1 and len(rec.calls) == made
+
+
+def _pieces(flat, *spans):
+    return [flat[a:b] for a, b in spans]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gradients_that_share_memory_are_not_scaled(rec, dtype):
+    flat, other = torch.ones(100, dtype=dtype), torch.ones(100, dtype=dtype)
+    clip = lambda g, **k: B.olive_grad_clip(g, 1.0, **k)
+    same = [flat, other, flat]
+    for g in (same, [flat[:10], flat[9:20]], [flat[50:60], other, flat[:100]], [flat, other[:5], flat[99:]]):
+        with pytest.raises(ValueError):
+            clip(g)
+        with pytest.raises(ValueError):  # the outputs
+            clip([torch.ones(t.numel(), dtype=dtype) for t in g], out=g)
+        fresh = [torch.empty_like(t) for t in g]
+        clip(g, out=fresh)  # read only: nothing is written twice
+        clip(g, out=None)
+    # an output over another gradient, and over its own but for an element
+    with pytest.raises(ValueError):
+        clip([flat, other], out=[other, flat])
+    with pytest.raises(ValueError):
+        clip([flat[:50]], out=[flat[1:51]])
+    with pytest.raises(ValueError):
+        clip([flat, flat, other], out=[torch.empty_like(flat), torch.empty_like(flat), flat])
+    assert len(rec.named("olive_grad_clip")) == 8
+
+
+def test_gradients_that_only_touch_are_scaled(rec):
+    flat, other = torch.ones(100), torch.ones(100, dtype=BF16)
+    g = _pieces(flat, (50, 100), (0, 25), (25, 50)) + _pieces(other, (1, 3), (0, 1), (3, 100))
+    empty = [flat[10:10], other[:0], flat[100:], torch.ones(0)]
+    for some in (g, g + empty, empty, [flat, other] + empty, []):
+        B.olive_grad_clip(some, 1.0)
+        B.olive_grad_clip(some, 1.0, out=[t.clone() for t in some])
+        B.olive_grad_clip(some, 1.0, out=[t if i % 2 else t.clone() for i, t in enumerate(some)])
+    assert len(rec.named("olive_grad_clip")) == 15
