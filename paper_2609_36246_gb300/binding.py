@@ -1000,5 +1000,8 @@ def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu"):
 
 
 def clip_grad_norm_(parameters, max_norm):
-    """olive_grad_clip in place on the gradients that the parameters hold."""
+    """olive_grad_clip in place on the gradients that the parameters (or the one
+    parameter) hold."""
+    if isinstance(parameters, torch.Tensor):
+        parameters = (parameters,)
     return olive_grad_clip([p.grad for p in parameters if p.grad is not None], max_norm)

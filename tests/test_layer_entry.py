@@ -128,3 +128,16 @@ def test_gradients_that_only_touch_are_scaled(rec):
         B.olive_grad_clip(some, 1.0, out=[t.clone() for t in some])
         B.olive_grad_clip(some, 1.0, out=[t if i % 2 else t.clone() for i, t in enumerate(some)])
     assert len(rec.named("olive_grad_clip")) == 15
+
+
+def test_one_parameter_is_clipped(rec):
+    """Not its rows, which hold no gradient."""
+    p = torch.nn.Parameter(torch.zeros(4, 3))
+    p.grad = torch.ones(4, 3)
+    B.clip_grad_norm_(p, 1.0)
+    B.clip_grad_norm_([p], 1.0)
+    one, listed = rec.named("olive_grad_clip")
+    assert one[4] == listed[4] == 1
+    p.grad = None
+    B.clip_grad_norm_(p, 1.0)
+    assert rec.named("olive_grad_clip")[-1][4] == 0
