@@ -1004,4 +1004,6 @@ def clip_grad_norm_(parameters, max_norm):
     parameter) hold."""
     if isinstance(parameters, torch.Tensor):
         parameters = (parameters,)
-    return olive_grad_clip([p.grad for p in parameters if p.grad is not None], max_norm)
+    # (a gradient that several entries hold is one: a tied parameter's counts and is scaled once)
+    grads = {id(g): g for g in (p.grad for p in parameters) if g is not None}
+    return olive_grad_clip(list(grads.values()), max_norm)

@@ -141,3 +141,14 @@ def test_one_parameter_is_clipped(rec):
     p.grad = None
     B.clip_grad_norm_(p, 1.0)
     assert rec.named("olive_grad_clip")[-1][4] == 0
+
+
+def test_a_tied_parameter_is_clipped_once(rec):
+    p, q = (torch.nn.Parameter(torch.zeros(5)) for _ in range(2))
+    p.grad, q.grad = torch.ones(5), torch.ones(5)
+    for listed in ([p, q, p], [p, p], [q, p]):
+        B.clip_grad_norm_(listed, 1.0)
+    assert [a[4] for a in rec.named("olive_grad_clip")] == [2, 1, 2]
+    q.grad = p.grad  # one gradient held by two parameters
+    B.clip_grad_norm_([p, q], 1.0)
+    assert rec.named("olive_grad_clip")[-1][4] == 1
