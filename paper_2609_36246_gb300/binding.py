@@ -999,6 +999,14 @@ def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu"):
     return GatedMLP.apply(x, W_gate, W_up, W_down, residual, act)
 
 
+def _in_memory_order(g):
+    """The same values with the dimensions in the order of their strides: contiguous,
+    unless there are gaps.  (The values' order does not matter to clipping.)"""
+    if g.is_contiguous():
+        return g
+    return g.permute(sorted(range(g.dim()), key=g.stride, reverse=True))
+
+
 def clip_grad_norm_(parameters, max_norm):
     """olive_grad_clip in place on the gradients that the parameters (or the one
     parameter) hold."""
@@ -1006,4 +1014,10 @@ def clip_grad_norm_(parameters, max_norm):
         parameters = (parameters,)
     # (a gradient that several entries hold is one: a tied parameter's counts and is scaled once)
     grads = {id(g): g for g in (p.grad for p in parameters) if g is not None}
-    return olive_grad_clip(list(grads.values()), max_norm)
+    grads = [_in_memory_order(g) for g in grads.values()]
+    flat = [g.contiguous() for g in grads]  # (itself, but for one with gaps: a copy, which goes back)
+    norm = olive_grad_clip(flat, max_norm)
+    for g, f in zip(grads, flat):
+        if f is not g:
+            g.copy_(f)
+    return norm

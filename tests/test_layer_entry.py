@@ -152,3 +152,19 @@ def test_a_tied_parameter_is_clipped_once(rec):
     q.grad = p.grad  # one gradient held by two parameters
     B.clip_grad_norm_([p, q], 1.0)
     assert rec.named("olive_grad_clip")[-1][4] == 1
+
+
+def test_gradients_in_other_orders_are_clipped(rec, monkeypatch):
+    """A transposed gradient is taken as it lies; one with gaps through a copy that goes back."""
+    p = [torch.nn.Parameter(torch.zeros(6, 4)) for _ in range(3)]
+    p[0].grad = torch.arange(24.0).view(4, 6).t()
+    wide = torch.arange(48.0).view(6, 8)
+    p[1].grad = wide[:, ::2]
+    p[2].grad = torch.ones(6, 4)
+    seen = []
+    monkeypatch.setattr(B, "olive_grad_clip", lambda g, limit: seen.extend(g) or [t.mul_(0.5) for t in g] and "norm")
+    assert B.clip_grad_norm_(p, 1.0) == "norm"
+    assert all(t.is_contiguous() for t in seen) and seen[0].data_ptr() == p[0].grad.data_ptr() and seen[2] is p[2].grad
+    assert torch.equal(p[0].grad, torch.arange(24.0).view(4, 6).t() / 2)
+    assert torch.equal(p[1].grad, torch.arange(48.0).view(6, 8)[:, ::2] / 2)
+    assert torch.equal(wide[:, 1::2], torch.arange(48.0).view(6, 8)[:, 1::2])
