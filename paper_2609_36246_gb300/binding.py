@@ -16,6 +16,7 @@ import os
 import re
 
 import torch
+from torch.autograd.function import once_differentiable
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libolive.so")
@@ -948,7 +949,7 @@ def fused_lmhead_ce(hidden, W, targets, rows, n_rows, inv_tau=1.0, reduction="su
 
 class QKNormRope(torch.autograd.Function):
     """Heads' norm and rotation as an autograd op (weights' gradients in the
-    weights' type)."""
+    weights' type).  It has first derivatives only."""
 
     @staticmethod
     def forward(ctx, q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=False):
@@ -957,6 +958,7 @@ class QKNormRope(torch.autograd.Function):
         return olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_q, g_k):
         q, k, w_q, w_k, cos, sin, positions = ctx.saved_tensors
         last = lambda g: g if g.stride(-1) == 1 else g.contiguous()
@@ -970,8 +972,8 @@ def qk_norm_rope(q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=Fals
 
 
 class GatedMLP(torch.autograd.Function):
-    """Gated feed-forward block as an autograd op (gradients in bf16).  The
-    pre-activations are saved only where a gradient is needed."""
+    """Gated feed-forward block as an autograd op (gradients in bf16; first
+    derivatives only, but for the residual's).  The pre-activations are saved only where a gradient is needed."""
 
     @staticmethod
     def forward(ctx, x, W_gate, W_up, W_down, residual=None, act="silu"):
@@ -985,14 +987,18 @@ class GatedMLP(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        dy = dy.contiguous()
         res = dy if ctx.needs_input_grad[4] else None
         if not (ctx.need_dx or ctx.need_dW):
             return None, None, None, None, res, None
+        return (*GatedMLP._gradients(ctx, dy), res, None)
+
+    @staticmethod
+    @once_differentiable
+    def _gradients(ctx, dy):
+        dy = dy.contiguous()
         x, W_gate, W_up, W_down, saved = ctx.saved_tensors
-        got = olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, ctx.act, need_dx=ctx.need_dx,
-                                  need_dW=ctx.need_dW)
-        return (*got, res, None)
+        return olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, ctx.act, need_dx=ctx.need_dx,
+                                   need_dW=ctx.need_dW)
 
 
 def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu"):

@@ -12,7 +12,8 @@ from paper_2609_36246_gb300 import binding as B
 
 
 class Recorder:
-    """A library whose entry points do nothing, say OLIVE_OK and keep their arguments.
+    """A library whose entry points do nothing, say OLIVE_OK and keep their arguments; what
+    they would have written reads 1.
 
     Tensors are on device 0, the current one, except those that place() put elsewhere."""
 
@@ -51,8 +52,7 @@ def recorded(monkeypatch):
     monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
     monkeypatch.setattr(torch.Tensor, "get_device", lambda t: rec.device_index(t))
     monkeypatch.setattr(torch.Tensor, "device", property(lambda t: torch.device("cuda", rec.device_index(t))))
-    for name in ("empty", "zeros", "ones"):
-        real = getattr(torch, name)
-        # (what is allocated on a CUDA device lies on the host)
+    # (what is allocated on a CUDA device lies on the host)
+    for name, real in (("empty", torch.ones), ("ones", torch.ones), ("zeros", torch.zeros)):
         monkeypatch.setattr(torch, name, lambda *a, _real=real, device=None, **k: _real(*a, **k))
     return rec

@@ -168,3 +168,31 @@ def test_gradients_in_other_orders_are_clipped(rec, monkeypatch):
     assert torch.equal(p[0].grad, torch.arange(24.0).view(4, 6).t() / 2)
     assert torch.equal(p[1].grad, torch.arange(48.0).view(6, 8)[:, ::2] / 2)
     assert torch.equal(wide[:, 1::2], torch.arange(48.0).view(6, 8)[:, 1::2])
+
+
+def _second_order(out, leaf):
+    """Differentiates a gradient: what a penalty on it does."""
+    g, = torch.autograd.grad(out.float().square().sum(), [leaf], create_graph=True)
+    (out.float().sum() + g.float().square().sum()).backward()
+
+
+def test_second_derivatives_of_the_layer_are_refused(rec):
+    """They are not formed; leaving them out unsaid would give a wrong gradient."""
+    s = _mlp()
+    for leaf in ("x", "W_gate"):
+        t = {k: v.clone().requires_grad_(k == leaf) for k, v in s.items() if k not in ("dy", "saved")}
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            _second_order(B.gated_mlp(*t.values()), t[leaf])
+    s = _qk()
+    for leaf in ("q", "w_k"):
+        t = {k: v.clone().requires_grad_(k == leaf) for k, v in s.items() if not k.startswith("g_")}
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            _second_order(sum(y.float().sum() for y in B.qk_norm_rope(*t.values())), t[leaf])
+
+
+@pytest.mark.parametrize("others", [(), ("x", "W_down")])
+def test_second_derivatives_of_the_residual(rec, others):
+    """Its gradient is the output's: (sum y + sum (2 y)^2) differentiates to 1 + 8 y, with y = 1."""
+    t = {k: v.clone().requires_grad_(k == "residual" or k in others) for k, v in _mlp().items() if k not in ("dy", "saved")}
+    _second_order(B.gated_mlp(*t.values()), t["residual"])
+    assert torch.equal(t["residual"].grad, torch.full_like(t["residual"], 9.0))
