@@ -906,7 +906,7 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
 
 class FusedLMHeadCE(torch.autograd.Function):
     """Eq. (osd-ce) loss over the masked rows as an autograd op (gradients in
-    the dtype of hidden).
+    the dtype of hidden; first derivatives only).
 
     With a gradient needed, the forward runs olive_token_loss_fwd_bwd with a
     unit loss gradient (each logit tile computed once) and the backward scales
@@ -931,6 +931,7 @@ class FusedLMHeadCE(torch.autograd.Function):
         return loss[0]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g):
         gl = g.reshape(1).to(torch.float32).contiguous()
         if ctx.single:

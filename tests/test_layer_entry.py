@@ -196,3 +196,11 @@ def test_second_derivatives_of_the_residual(rec, others):
     t = {k: v.clone().requires_grad_(k == "residual" or k in others) for k, v in _mlp().items() if k not in ("dy", "saved")}
     _second_order(B.gated_mlp(*t.values()), t["residual"])
     assert torch.equal(t["residual"].grad, torch.full_like(t["residual"], 9.0))
+
+
+@pytest.mark.parametrize("single_pass", [True, False])
+def test_second_derivatives_of_the_loss_are_refused(rec, single_pass):
+    ids = [torch.zeros(4, dtype=torch.int32) for _ in range(3)]
+    h, W = torch.zeros(4, 64, dtype=BF16, requires_grad=True), torch.zeros(50, 64, dtype=BF16, requires_grad=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        _second_order(B.fused_lmhead_ce(h, W, *ids, single_pass=single_pass), h)
