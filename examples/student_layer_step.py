@@ -14,6 +14,7 @@ steps on drawn ids.
 
 from __future__ import annotations
 
+import functools
 import os
 import sys
 
@@ -66,14 +67,17 @@ def layer(p, ids, positions, sequence, tables, heads, kv_heads, qk_norm_rope=B.q
     return _rows_norm(x, p["w_out"]).contiguous()
 
 
-def step(p, batch, V, T, heads, kv_heads, tables, lr=0.0, max_norm=1.0):
+def step(p, batch, V, T, heads, kv_heads, tables, lr=0.0, max_norm=1.0, dev_status=None):
     """One training step on (prefix_ids, prefix_off, cont_ids, cont_off), all on the device: the mean
-    loss of the continuation tokens and the gradients' norm before clipping, as device tensors."""
-    pk = B.olive_splice_pack(*batch, V, T)
+    loss of the continuation tokens and the gradients' norm before clipping, as device tensors.  What
+    any call of the step, forward or backward, finds wrong on the device is in dev_status."""
+    st = B.new_status() if dev_status is None else dev_status
+    pk = B.olive_splice_pack(*batch, V, T, dev_status=st)
     positions = B.olive_packed_positions(pk["cu_seqlens"], T)
     sequence = (torch.arange(T, device="cuda")[:, None] >= pk["cu_seqlens"][None, 1:]).sum(1)
-    hidden = layer(p, pk["ids"], positions, sequence, tables, heads, kv_heads)
-    loss = B.fused_lmhead_ce(hidden, p["W"], pk["targets"], pk["rows"], pk["n_rows"], reduction="mean")
+    hidden = layer(p, pk["ids"], positions, sequence, tables, heads, kv_heads,
+                   functools.partial(B.qk_norm_rope, dev_status=st), functools.partial(B.gated_mlp, dev_status=st))
+    loss = B.fused_lmhead_ce(hidden, p["W"], pk["targets"], pk["rows"], pk["n_rows"], reduction="mean", dev_status=st)
     loss.backward()
     norm = B.clip_grad_norm_(p.values(), max_norm)
     with torch.no_grad():
@@ -98,9 +102,12 @@ def main(steps=10):
     batch, T = draw_batch(V, [(40, 88), (100, 28), (16, 112), (64, 64)])
     p = init(V, d, heads, kv_heads, D, f)
     tables = rope_tables(256, D)
+    st = B.new_status()
     for i in range(steps):
-        loss, norm = step(p, batch, V, T, heads, kv_heads, tables, lr=0.5)
+        loss, norm = step(p, batch, V, T, heads, kv_heads, tables, lr=0.5, dev_status=st)
         print(f"step {i}: loss {float(loss):.4f}  gradient norm {float(norm):.4f}")
+        if B.status_bits(st):
+            raise SystemExit(f"step {i}: {', '.join(B.status_bits(st))}")
 
 
 if __name__ == "__main__":

@@ -906,7 +906,8 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
 
 class FusedLMHeadCE(torch.autograd.Function):
     """Eq. (osd-ce) loss over the masked rows as an autograd op (gradients in
-    the dtype of hidden; first derivatives only).
+    the dtype of hidden; first derivatives only).  A status word given is the
+    forward's and the backward's.
 
     With a gradient needed, the forward runs olive_token_loss_fwd_bwd with a
     unit loss gradient (each logit tile computed once) and the backward scales
@@ -916,17 +917,18 @@ class FusedLMHeadCE(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, hidden, W, targets, rows, n_rows, inv_tau=1.0, reduction="sum",
-                single_pass=True):
-        ctx.inv_tau, ctx.reduction = inv_tau, reduction
+                single_pass=True, dev_status=None):
+        ctx.inv_tau, ctx.reduction, ctx.dev_status = inv_tau, reduction, dev_status
         ctx.single = bool(single_pass and (hidden.requires_grad or W.requires_grad))
         if ctx.single:
             one = torch.ones(1, dtype=torch.float32, device=hidden.device)
             _, _, loss, dh, dw = olive_token_loss_fwd_bwd(hidden, W, targets, rows, n_rows, one,
-                                                          inv_tau, reduction, grad_dtype=hidden.dtype)
+                                                          inv_tau, reduction, grad_dtype=hidden.dtype,
+                                                          dev_status=dev_status)
             ctx.save_for_backward(dh, dw)
         else:
             _, lse, loss = olive_token_logprob_fwd(hidden, W, targets, rows, n_rows, inv_tau,
-                                                   reduction)
+                                                   reduction, dev_status=dev_status)
             ctx.save_for_backward(hidden, W, targets, rows, n_rows, lse)
         return loss[0]
 
@@ -936,27 +938,32 @@ class FusedLMHeadCE(torch.autograd.Function):
         gl = g.reshape(1).to(torch.float32).contiguous()
         if ctx.single:
             dh1, dw1 = ctx.saved_tensors
-            return (olive_scale(dh1, gl), olive_scale(dw1, gl), None, None, None, None, None, None)
+            return (olive_scale(dh1, gl), olive_scale(dw1, gl), *[None] * 7)
         hidden, W, targets, rows, n_rows, lse = ctx.saved_tensors
         dh, dw = olive_token_loss_bwd(hidden, W, targets, rows, n_rows, lse, gl, ctx.inv_tau,
-                                      ctx.reduction, grad_dtype=hidden.dtype)
-        return dh, dw, None, None, None, None, None, None
+                                      ctx.reduction, grad_dtype=hidden.dtype,
+                                      dev_status=ctx.dev_status)
+        return (dh, dw, *[None] * 7)
 
 
 def fused_lmhead_ce(hidden, W, targets, rows, n_rows, inv_tau=1.0, reduction="sum",
-                    single_pass=True):
-    return FusedLMHeadCE.apply(hidden, W, targets, rows, n_rows, inv_tau, reduction, single_pass)
+                    single_pass=True, dev_status=None):
+    return FusedLMHeadCE.apply(hidden, W, targets, rows, n_rows, inv_tau, reduction, single_pass,
+                               dev_status)
 
 
 class QKNormRope(torch.autograd.Function):
     """Heads' norm and rotation as an autograd op (weights' gradients in the
-    weights' type).  It has first derivatives only."""
+    weights' type).  It has first derivatives only.  A status word given is the
+    forward's and the backward's."""
 
     @staticmethod
-    def forward(ctx, q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=False):
+    def forward(ctx, q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=False,
+                dev_status=None):
         ctx.save_for_backward(q, k, w_q, w_k, cos, sin, positions)
-        ctx.eps, ctx.interleaved = eps, interleaved
-        return olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+        ctx.eps, ctx.interleaved, ctx.dev_status = eps, interleaved, dev_status
+        return olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps, interleaved,
+                                      dev_status)
 
     @staticmethod
     @once_differentiable
@@ -964,24 +971,29 @@ class QKNormRope(torch.autograd.Function):
         q, k, w_q, w_k, cos, sin, positions = ctx.saved_tensors
         last = lambda g: g if g.stride(-1) == 1 else g.contiguous()
         dq, dk, dwq, dwk = olive_qk_norm_rope_bwd(last(g_q), last(g_k), q, k, w_q, w_k, cos, sin,
-                                                  positions, ctx.eps, ctx.interleaved)
-        return dq, dk, dwq.to(w_q.dtype), dwk.to(w_k.dtype), None, None, None, None, None
+                                                  positions, ctx.eps, ctx.interleaved,
+                                                  dev_status=ctx.dev_status)
+        return (dq, dk, dwq.to(w_q.dtype), dwk.to(w_k.dtype), *[None] * 6)
 
 
-def qk_norm_rope(q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=False):
-    return QKNormRope.apply(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+def qk_norm_rope(q, k, w_q, w_k, cos, sin, positions, eps=1e-6, interleaved=False,
+                 dev_status=None):
+    return QKNormRope.apply(q, k, w_q, w_k, cos, sin, positions, eps, interleaved, dev_status)
 
 
 class GatedMLP(torch.autograd.Function):
     """Gated feed-forward block as an autograd op (gradients in bf16; first
-    derivatives only, but for the residual's).  The pre-activations are saved only where a gradient is needed."""
+    derivatives only, but for the residual's).  The pre-activations are saved only
+    where a gradient is needed.  A status word given is the forward's and the
+    backward's."""
 
     @staticmethod
-    def forward(ctx, x, W_gate, W_up, W_down, residual=None, act="silu"):
+    def forward(ctx, x, W_gate, W_up, W_down, residual=None, act="silu", dev_status=None):
         needs = ctx.needs_input_grad
         ctx.act, ctx.need_dx, ctx.need_dW = act, needs[0], any(needs[1:4])
+        ctx.dev_status = dev_status
         y, saved = olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual, act,
-                                       save=ctx.need_dx or ctx.need_dW)
+                                       save=ctx.need_dx or ctx.need_dW, dev_status=dev_status)
         if saved is not None:
             ctx.save_for_backward(x, W_gate, W_up, W_down, saved)
         return y
@@ -990,8 +1002,8 @@ class GatedMLP(torch.autograd.Function):
     def backward(ctx, dy):
         res = dy if ctx.needs_input_grad[4] else None
         if not (ctx.need_dx or ctx.need_dW):
-            return None, None, None, None, res, None
-        return (*GatedMLP._gradients(ctx, dy), res, None)
+            return None, None, None, None, res, None, None
+        return (*GatedMLP._gradients(ctx, dy), res, None, None)
 
     @staticmethod
     @once_differentiable
@@ -999,11 +1011,11 @@ class GatedMLP(torch.autograd.Function):
         dy = dy.contiguous()
         x, W_gate, W_up, W_down, saved = ctx.saved_tensors
         return olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, ctx.act, need_dx=ctx.need_dx,
-                                   need_dW=ctx.need_dW)
+                                   need_dW=ctx.need_dW, dev_status=ctx.dev_status)
 
 
-def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu"):
-    return GatedMLP.apply(x, W_gate, W_up, W_down, residual, act)
+def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu", dev_status=None):
+    return GatedMLP.apply(x, W_gate, W_up, W_down, residual, act, dev_status)
 
 
 def _in_memory_order(g):

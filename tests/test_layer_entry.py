@@ -204,3 +204,25 @@ def test_second_derivatives_of_the_loss_are_refused(rec, single_pass):
     h, W = torch.zeros(4, 64, dtype=BF16, requires_grad=True), torch.zeros(50, 64, dtype=BF16, requires_grad=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         _second_order(B.fused_lmhead_ce(h, W, *ids, single_pass=single_pass), h)
+
+
+def test_autograd_forms_pass_the_status_word_on(rec):
+    """To the forward's call and to the backward's."""
+    st = torch.zeros(1, dtype=torch.int32)
+    s = _mlp()
+    B.gated_mlp(*(s[k].requires_grad_() for k in ("x", "W_gate", "W_up", "W_down", "residual")), dev_status=st).sum().backward()
+    s = _qk()
+    leaf = [s[k].requires_grad_(s[k].dtype == BF16) for k in ("q", "k", "w_q", "w_k", "cos", "sin", "positions")]
+    sum(y.sum() for y in B.qk_norm_rope(*leaf, dev_status=st)).backward()
+    for single_pass in (True, False):
+        h, W = torch.zeros(4, 64, dtype=BF16, requires_grad=True), torch.zeros(50, 64, dtype=BF16, requires_grad=True)
+        ids = [torch.zeros(4, dtype=torch.int32) for _ in range(3)]
+        B.fused_lmhead_ce(h, W, *ids, single_pass=single_pass, dev_status=st).backward()
+    with torch.no_grad():
+        B.gated_mlp(*list(_mlp().values())[:4], dev_status=st)
+    names = [c.name for c in rec.calls]
+    for name, times in (("olive_gated_mlp_fwd", 2), ("olive_gated_mlp_bwd", 1), ("olive_qk_norm_rope_fwd", 1),
+                        ("olive_qk_norm_rope_bwd", 1), ("olive_token_loss_fwd_bwd", 1), ("olive_token_logprob_fwd", 1),
+                        ("olive_token_loss_bwd", 1)):
+        assert names.count(name) == times, name
+        assert all(args[-2] == st.data_ptr() for args in rec.named(name)), name  # (the stream is last)

@@ -30,3 +30,43 @@ def test_gradients_of_any_layout_are_clipped(dtype, limit):
         assert p.grad is g and ((g.double() - b * f).abs() <= tol * (b * f).abs() + 1e-40).all()
         if limit == 1e6:
             assert torch.equal(g.double(), b)
+
+
+def test_autograd_forms_report_what_the_device_found(monkeypatch):
+    """A wait that ran out (there is no time to wait) and a position outside the tables."""
+    draw = lambda *s: torch.randn(*s, device="cuda").to(torch.bfloat16)
+    mlp = [t.requires_grad_() for t in (draw(900, 32768), *(draw(1024, 32768) * 0.005 for _ in range(2)), draw(32768, 1024))]
+    before, after = B.new_status(), B.new_status()
+    monkeypatch.setenv("OLIVE_WAIT_LIMIT_MS", "0")
+    B.gated_mlp(*mlp, dev_status=before)
+    monkeypatch.delenv("OLIVE_WAIT_LIMIT_MS")
+    y = B.gated_mlp(*mlp, dev_status=after)
+    assert B.status_bits(before) == ["OLIVE_ERR_TIMEOUT"] and B.status_bits(after) == []
+    monkeypatch.setenv("OLIVE_WAIT_LIMIT_MS", "0")
+    y.backward(torch.ones_like(y))
+    torch.cuda.synchronize()
+    monkeypatch.delenv("OLIVE_WAIT_LIMIT_MS")
+    assert B.status_bits(after) == ["OLIVE_ERR_TIMEOUT"]
+
+    q, k, w = draw(5, 3, 64).requires_grad_(), draw(5, 2, 64), draw(64)
+    table = torch.ones(4, 32, device="cuda")
+    for wrong in (False, True):
+        pos = torch.tensor([0, 1, 2, 3, 4 if wrong else 0], dtype=torch.int32, device="cuda")
+        st = B.new_status()
+        yq, _ = B.qk_norm_rope(q, k, w, w, table, table, pos, dev_status=st)
+        bits = ["OLIVE_ERR_TOKEN_RANGE"] if wrong else []
+        assert B.status_bits(st) == bits
+        st.zero_()
+        yq.backward(torch.ones_like(yq))
+        assert B.status_bits(st) == bits
+
+
+def test_a_step_of_the_example_reports_too(monkeypatch):
+    from examples import student_layer_step as E
+
+    batch, T = E.draw_batch(512, [(20, 40), (9, 60)])
+    p = E.init(512, 64, 2, 1, 32, 136)
+    for rows, bits in ((128, []), (64, ["OLIVE_ERR_TOKEN_RANGE"])):  # the second sequence has 69 tokens
+        st = B.new_status()
+        E.step(p, batch, 512, T, 2, 1, E.rope_tables(rows, 32), dev_status=st)
+        assert B.status_bits(st) == bits
