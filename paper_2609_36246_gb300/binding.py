@@ -1015,6 +1015,10 @@ class GatedMLP(torch.autograd.Function):
 
 
 def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu", dev_status=None):
+    # (asked here: inside a Function autograd is off anyway, and a Parameter "needs" its
+    # gradient under no_grad too; what is saved is 4 T f bytes)
+    if not torch.is_grad_enabled():
+        return olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual, act, dev_status=dev_status)[0]
     return GatedMLP.apply(x, W_gate, W_up, W_down, residual, act, dev_status)
 
 

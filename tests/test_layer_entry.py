@@ -226,3 +226,20 @@ def test_autograd_forms_pass_the_status_word_on(rec):
                         ("olive_token_loss_bwd", 1)):
         assert names.count(name) == times, name
         assert all(args[-2] == st.data_ptr() for args in rec.named(name)), name  # (the stream is last)
+
+
+def test_nothing_is_saved_without_gradients(rec):
+    """Parameters ask for gradients also where autograd is off."""
+    s = _mlp()
+    leaf = [torch.nn.Parameter(s[k]) for k in ("W_gate", "W_up", "W_down")]
+    saved = lambda: rec.named("olive_gated_mlp_fwd")[-1][10]
+    B.gated_mlp(s["x"], *leaf)
+    assert saved() is not None
+    for off in (torch.no_grad, torch.inference_mode):
+        with off():
+            y = B.gated_mlp(s["x"], *leaf, s["residual"], "gelu_tanh")
+        assert saved() is None and not y.requires_grad
+        assert rec.named("olive_gated_mlp_fwd")[-1][4] == s["residual"].data_ptr()
+        assert rec.named("olive_gated_mlp_fwd")[-1][8] == B.ACT["gelu_tanh"]
+    B.gated_mlp(*(s[k] for k in ("x", "W_gate", "W_up", "W_down")), s["residual"].requires_grad_())
+    assert saved() is None

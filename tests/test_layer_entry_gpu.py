@@ -70,3 +70,23 @@ def test_a_step_of_the_example_reports_too(monkeypatch):
         st = B.new_status()
         E.step(p, batch, 512, T, 2, 1, E.rope_tables(rows, 32), dev_status=st)
         assert B.status_bits(st) == bits
+
+
+@pytest.mark.parametrize("T", [16, 700])
+def test_scoring_with_parameters_saves_nothing(T):
+    """Under no_grad a call holds what olive_gated_mlp_fwd holds without saving, and gives its bits."""
+    draw = lambda *s: torch.randn(*s, device="cuda").to(torch.bfloat16)
+    x, w = draw(T, 256), [torch.nn.Parameter(t) for t in (draw(4096, 256), draw(4096, 256), draw(256, 4096))]
+
+    def peak(f):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        start = torch.cuda.memory_allocated()
+        y = f()
+        return torch.cuda.max_memory_allocated() - start, y
+
+    want, y = peak(lambda: B.olive_gated_mlp_fwd(x, *w)[0])
+    with torch.no_grad():
+        got, z = peak(lambda: B.gated_mlp(x, *w))
+    assert got <= want and torch.equal(y, z)
+    assert peak(lambda: B.gated_mlp(x, *w))[0] >= want + 4 * T * 4096
