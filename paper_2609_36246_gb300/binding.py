@@ -952,6 +952,16 @@ def fused_lmhead_ce(hidden, W, targets, rows, n_rows, inv_tau=1.0, reduction="su
                                dev_status)
 
 
+def _heads_gradient(g):
+    """A gradient [T, heads, D] as the backward can read it.  Autograd hands over whatever
+    view the next operation left (columns of a wider tensor, say), which need not start
+    on 16 bytes nor have strides of whole 16 bytes: then a copy."""
+    token, head, last = g.stride()
+    fits = (last == 1 and g.data_ptr() % 16 == 0 and (g.shape[0] < 2 or token % 8 == 0) and
+            (g.shape[1] < 2 or head % 8 == 0))
+    return g if fits else g.clone(memory_format=torch.contiguous_format)
+
+
 class QKNormRope(torch.autograd.Function):
     """Heads' norm and rotation as an autograd op (weights' gradients in the
     weights' type).  It has first derivatives only.  A status word given is the
@@ -969,8 +979,7 @@ class QKNormRope(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, g_q, g_k):
         q, k, w_q, w_k, cos, sin, positions = ctx.saved_tensors
-        last = lambda g: g if g.stride(-1) == 1 else g.contiguous()
-        dq, dk, dwq, dwk = olive_qk_norm_rope_bwd(last(g_q), last(g_k), q, k, w_q, w_k, cos, sin,
+        dq, dk, dwq, dwk = olive_qk_norm_rope_bwd(_heads_gradient(g_q), _heads_gradient(g_k), q, k, w_q, w_k, cos, sin,
                                                   positions, ctx.eps, ctx.interleaved,
                                                   dev_status=ctx.dev_status)
         return (dq, dk, dwq.to(w_q.dtype), dwk.to(w_k.dtype), *[None] * 6)
@@ -1008,7 +1017,8 @@ class GatedMLP(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def _gradients(ctx, dy):
-        dy = dy.contiguous()
+        if not dy.is_contiguous() or dy.data_ptr() % 16:
+            dy = dy.clone(memory_format=torch.contiguous_format)
         x, W_gate, W_up, W_down, saved = ctx.saved_tensors
         return olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, ctx.act, need_dx=ctx.need_dx,
                                    need_dW=ctx.need_dW, dev_status=ctx.dev_status)

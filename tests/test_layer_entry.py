@@ -243,3 +243,32 @@ def test_nothing_is_saved_without_gradients(rec):
         assert rec.named("olive_gated_mlp_fwd")[-1][8] == B.ACT["gelu_tanh"]
     B.gated_mlp(*(s[k] for k in ("x", "W_gate", "W_up", "W_down")), s["residual"].requires_grad_())
     assert saved() is None
+
+
+def _cat_loss(parts):
+    """Parts side by side and a sum that weighs them differently: their gradients are views."""
+    y = torch.cat(parts, -1).float()
+    return (y * torch.arange(1, y.numel() + 1).view(y.shape)).sum()
+
+
+@pytest.mark.parametrize("D", [8, 64])
+@pytest.mark.parametrize("before,after", [(0, 4), (4, 0), (3, 1), (8, 8), (0, 0)])
+def test_gradients_that_autograd_hands_over_as_views(rec, D, before, after):
+    """What lies off the 16-byte rule is copied, what fits is read where it is."""
+    s = _qk(D=D, R=8)
+    yq, yk = B.qk_norm_rope(*(s[k].requires_grad_(k in "qk") for k in ("q", "k", "w_q", "w_k", "cos", "sin", "positions")))
+    pad = lambda y, n: [torch.zeros(*y.shape[:2], n, dtype=y.dtype)] if n else []
+    (_cat_loss(pad(yq, before) + [yq] + pad(yq, after)) + _cat_loss(pad(yk, before) + [yk] + pad(yk, after))).backward()
+    gq, gq_t, gq_h, gk, gk_t, gk_h = rec.named("olive_qk_norm_rope_bwd")[0][:6]
+    assert gq % 16 == 0 and gk % 16 == 0 and not any(x % 8 for x in (gq_t, gq_h, gk_t, gk_h))
+    assert gq_h == (D if before % 8 or after % 8 else D + before + after)
+
+
+@pytest.mark.parametrize("T", [4, 1])
+def test_output_gradients_that_start_anywhere(rec, T):
+    s = _mlp(T=T)
+    y = B.gated_mlp(s["x"].requires_grad_(), *(s[k] for k in ("W_gate", "W_up", "W_down")))
+    off = torch.zeros(T * 64 + 3, dtype=BF16)[3:].view(T, 64)
+    assert off.is_contiguous() and off.data_ptr() % 16 == 6
+    y.backward(off)
+    assert rec.named("olive_gated_mlp_bwd")[0][0] % 16 == 0

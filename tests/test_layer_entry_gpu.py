@@ -90,3 +90,37 @@ def test_scoring_with_parameters_saves_nothing(T):
         got, z = peak(lambda: B.gated_mlp(x, *w))
     assert got <= want and torch.equal(y, z)
     assert peak(lambda: B.gated_mlp(x, *w))[0] >= want + 4 * T * 4096
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [8, 64])
+@pytest.mark.parametrize("before,after", [(0, 4), (4, 0), (3, 1), (8, 8)])
+def test_heads_inside_a_wider_tensor(dtype, D, before, after):
+    """The gradients of heads that go on beside other columns have the bits of contiguous ones."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    draw = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(dtype)
+    T, w = 21, [draw(D), draw(D)]
+    table = [draw(T, 4).float(), draw(T, 4).float()]
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    heads = [draw(T, 3, D), draw(T, 2, D)]
+    weigh = [draw(T, h.shape[1], before + D + after) for h in heads]
+    leaf = [h.clone().requires_grad_() for h in heads]
+    total = 0
+    for y, g in zip(B.qk_norm_rope(*leaf, *w, *table, pos), weigh):
+        wide = torch.cat([g[..., :before], y, g[..., before + D:]], -1)
+        total = total + (wide.float() * g.float()).sum()
+    total.backward()
+    own = [g[..., before:before + D].contiguous() for g in weigh]
+    want = B.olive_qk_norm_rope_bwd(*own, *heads, *w, *table, pos)
+    assert all(torch.equal(t.grad, d) for t, d in zip(leaf, want))
+
+
+def test_block_output_gradient_that_starts_anywhere():
+    draw = lambda *s: torch.randn(*s, device="cuda").to(torch.bfloat16)
+    x, w, flat = draw(70, 64), (draw(72, 64), draw(72, 64), draw(64, 72)), draw(70 * 64 + 3)
+    dy = flat[3:].view(70, 64)
+    leaf = x.clone().requires_grad_()
+    B.gated_mlp(leaf, *w).backward(dy)
+    _, saved = B.olive_gated_mlp_fwd(x, *w, save=True)
+    want = B.olive_gated_mlp_bwd(dy.clone(), x, *w, saved, need_dW=False)[0]
+    assert torch.equal(leaf.grad, want)
