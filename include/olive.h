@@ -563,7 +563,8 @@ OLIVE_API olive_status olive_packed_positions(const int32_t* cu_seqlens, int32_t
  *   Head h of token t starts at q + t q_token_stride + h q_head_stride
  *   (elements), so q and k can be views of one fused projection; its D values
  *   are contiguous.  The outputs have strides of their own; an output may be
- *   its own input (same pointer and strides).
+ *   its own input (same pointer and strides).  Heads of an output must not share
+ *   memory (OLIVE_ERR_SHAPE); those of an input may (a stride of 0).
  *   D a multiple of 8, 8 <= D <= 256; R a multiple of 8, 0 <= R <= D; 0 <=
  *   Hq, Hk <= 4096, not both 0 (the pointers of a side without heads are ignored);
  *   T >= 0; strides multiples of 8, base pointers 16-byte aligned; eps >= 0.

@@ -769,6 +769,22 @@ olive_status olive_packed_positions(const int32_t* cu_seqlens, int32_t S, int32_
   return launch_packed_positions(c, cu_seqlens, S, T_cap, positions);
 }
 
+// Whether two heads of a view share memory (strides checked before).
+static bool heads_overlap(const HeadsView& v, int64_t heads, int64_t T, int64_t D) {
+  const int64_t ts = v.token_stride, hs = v.head_stride;
+  if ((heads > 1 && hs < D) || (T > 1 && ts < D)) return true;
+  if (heads == 1 || T == 1) return false;
+  // one token's heads before the next token's, or one head's tokens before the next head's
+  if ((ts - D) / hs >= heads - 1 || (hs - D) / ts >= T - 1) return false;
+  // else the heads of two tokens lie between one another: a head `at` behind another of
+  // its token, and the tokens' own heads nearest to it
+  for (int64_t h = 1; h < heads; ++h) {
+    const int64_t at = h * hs, m = std::min(at / ts, T - 1);
+    if (at - m * ts < D || (m + 1 < T && (m + 1) * ts - at < D)) return true;
+  }
+  return false;
+}
+
 // The checks that the heads' forward and backward share.
 static olive_status check_qk(const QkArgs& a, bool bwd) {
   if (a.dtype != OLIVE_DTYPE_BF16 && a.dtype != OLIVE_DTYPE_F32) return OLIVE_ERR_INVALID_ARG;
@@ -790,6 +806,7 @@ static olive_status check_qk(const QkArgs& a, bool bwd) {
         return OLIVE_ERR_ALIGNMENT;
       if (v->token_stride < 0 || v->head_stride < 0) return OLIVE_ERR_SHAPE;
     }
+    if (heads_overlap(a.out[s], a.heads[s], a.T, a.D)) return OLIVE_ERR_SHAPE;
   }
   return OLIVE_OK;
 }
