@@ -612,8 +612,8 @@ OLIVE_API olive_status olive_qk_norm_rope_bwd(
  * bytes, 16-byte aligned, to be passed on as they are.  (16 bits each: a sign,
  * 6 exponent and 9 fraction bits, 2^-10 relative.  bf16's 2^-8 would put as
  * large an error on the gradients as rounding them to bf16 operands does.
- * Magnitudes below 2^-30 lose accuracy and vanish below 2^-39; those above
- * 2^33 are held as 2^33, infinities and NaN become NaN.)
+ * Magnitudes below 2^-30 are held in steps of 2^-39; what is larger than
+ * 2^33 - 2^24 is held as that, infinities and NaN become NaN.)
  * 0 <= T <= 2^30 (0: nothing happens), d and f multiples of 8.  dev_status may be NULL.
  * workspace: olive_workspace_size(OLIVE_OP_GATED_MLP_FWD, T, d, 0, f, 0, 0) bytes.
  */
