@@ -44,6 +44,7 @@
  *   olive_gated_mlp_fwd, olive_gated_mlp_bwd
  *                            gated feed-forward block with its residual
  *   olive_grad_clip          global norm of a list of gradients, and clipping
+ *   olive_grad_clip_apart    whether such a list may be scaled (a host check)
  *
  * Conventions shared by every call
  *   - Every pointer argument is a DEVICE pointer unless stated otherwise.  The
@@ -651,7 +652,8 @@ OLIVE_API olive_status olive_gated_mlp_bwd(const void* dy, const void* x, const 
  * returns): device pointers, element counts (0 allowed: the pointers are then
  * ignored) and OLIVE_DTYPE_BF16 or OLIVE_DTYPE_F32, tensor by tensor.  dst[i]
  * may be src[i] (a factor of exactly 1 then writes nothing) but must not overlap
- * it otherwise, nor another tensor; dst NULL: only the norm.  Any alignment of
+ * it otherwise, nor another tensor (olive_grad_clip_apart tells; this call does
+ * not look); dst NULL: only the norm.  Any alignment of
  * whole elements; 16-byte aligned pointers are read and written in 16-byte
  * pieces.  The squares are summed in fp32 by 32s, in fp64 beyond (of
  * values scaled by a power of two where their squares would leave fp32's
@@ -664,6 +666,18 @@ OLIVE_API olive_status olive_grad_clip(const void* const* src, void* const* dst,
                                        const int64_t* numel, const int32_t* dtype, int32_t n,
                                        float max_norm, float* norm, void* workspace,
                                        size_t ws_bytes, void* stream);
+
+/*
+ * olive_grad_clip_apart -- whether the tensors of a call to olive_grad_clip are
+ * apart as they must be: OLIVE_OK, or OLIVE_ERR_INVALID_ARG where what is written
+ * (dst) shares memory with another dst, with another tensor's src, or with its own
+ * src without being it.  Host arrays as there; nothing is launched and no device is
+ * needed.  (A list that names a tied parameter's gradient twice is such a case:
+ * two blocks would scale it at once.)  OLIVE_ERR_WORKSPACE: no host memory to sort in.
+ */
+OLIVE_API olive_status olive_grad_clip_apart(const void* const* src, void* const* dst,
+                                             const int64_t* numel, const int32_t* dtype,
+                                             int32_t n);
 
 #ifdef __cplusplus
 }

@@ -142,6 +142,8 @@ def _configure(L: ctypes.CDLL) -> ctypes.CDLL:
                                       _P, ctypes.c_int, _P, _S, _P, _P]
     L.olive_grad_clip.restype = ctypes.c_int
     L.olive_grad_clip.argtypes = [_P, _P, _P, _P, _I, _F, _P, _P, _S, _P]
+    L.olive_grad_clip_apart.restype = ctypes.c_int
+    L.olive_grad_clip_apart.argtypes = [_P, _P, _P, _P, _I]
     return L
 
 
@@ -840,27 +842,6 @@ def _grad_list(tensors, cur, what):
     return list(map(_ptr_of, tensors)), list(map(_numel_of, tensors)), kinds
 
 
-def _apart(starts, ends):
-    """Whether no two spans of addresses share a byte: as many end as begin before the
-    next one does (so an empty one may lie anywhere)."""
-    return all(map(operator.le, sorted(ends), sorted(starts)[1:]))
-
-
-def _need_apart(src, dst, counts, kinds):
-    """Refuses outputs that share memory with one another or with another gradient: the
-    blocks of one tensor would write what those of the other read or write."""
-    sizes = [n << 1 + k for n, k in zip(counts, kinds)]  # (kind 0 is bf16, 1 fp32)
-    ends = list(map(operator.add, dst, sizes))
-    fine = _apart(dst, ends)
-    if fine and src is not dst:
-        # gradients that are only read may share memory with one another
-        read = [(a, a + n) for a, d, n in zip(src, dst, sizes) if a != d]
-        fine = (_apart(dst + [a for a, _ in read], ends + [b for _, b in read]) or
-                all(_apart(dst + [a], ends + [b]) for a, b in read))
-    if not fine:
-        raise ValueError("a gradient that is scaled must not share memory with another (a tied one is listed once)")
-
-
 def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     """The 2-norm over all elements of `grads` (bf16 or fp32 CUDA tensors,
     contiguous) as a 1-element fp32 tensor, and the gradients scaled by
@@ -882,7 +863,6 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
             dst, sizes, types = _grad_list(out, cur, "out")
             if sizes != num or types != kinds:
                 raise TypeError("out must be like the gradients")
-        _need_apart(src, dst, num, kinds)
     if norm is None:
         norm = torch.empty(1, dtype=_F32, device="cuda")
     else:
@@ -896,9 +876,12 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     table.extend(num)
     at, count = table.buffer_info()
     kind = array.array("i", kinds)
-    st = lib().olive_grad_clip(at, at + 8 * n if dst is not None else None, at + 8 * (count - n),
-                               kind.buffer_info()[0], n, max_norm, norm.data_ptr(), ws.data_ptr(),
-                               ws.numel(), _stream())
+    lists = (at, at + 8 * n if dst is not None else None, at + 8 * (count - n), kind.buffer_info()[0], n)
+    L = lib()
+    # (blocks of one tensor would write what those of another read or write)
+    if L.olive_grad_clip_apart(*lists):
+        raise ValueError("a gradient that is scaled must not share memory with another (a tied one is listed once)")
+    st = L.olive_grad_clip(*lists, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
     if st:
         _check(st, "olive_grad_clip")
     return norm

@@ -954,6 +954,41 @@ olive_status olive_gated_mlp_bwd(const void* dy, const void* x, const void* W_ga
                         dW_up, dW_down, grad_dtype, workspace, dev_status);
 }
 
+olive_status olive_grad_clip_apart(const void* const* src, void* const* dst, const int64_t* numel,
+                                   const int32_t* dtype, int32_t n) {
+  if (n < 0) return OLIVE_ERR_SHAPE;
+  if (n > 0 && (!src || !numel || !dtype)) return OLIVE_ERR_INVALID_ARG;
+  if (!dst || n == 0) return OLIVE_OK;
+  struct Span {
+    uintptr_t begin, end;
+    bool written;
+  };
+  Span few[128];
+  Span* const spans = 2ll * n <= 128 ? few : static_cast<Span*>(std::malloc(2ull * n * sizeof(Span)));
+  if (!spans) return OLIVE_ERR_WORKSPACE;
+  int64_t m = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (numel[i] <= 0) continue;
+    const uintptr_t bytes = static_cast<uintptr_t>(numel[i]) * (dtype[i] == OLIVE_DTYPE_BF16 ? 2 : 4);
+    const uintptr_t w = reinterpret_cast<uintptr_t>(dst[i]), r = reinterpret_cast<uintptr_t>(src[i]);
+    spans[m++] = {w, w + bytes, true};
+    if (r != w) spans[m++] = {r, r + bytes, false};
+  }
+  std::sort(spans, spans + m, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  // in the order of their beginnings: one that is written must begin behind the ends of
+  // all before it, one that is read behind those that are written
+  uintptr_t end = 0, written = 0;
+  bool apart = true;
+  for (int64_t i = 0; i < m; ++i) {
+    const Span& s = spans[i];
+    apart = apart && s.begin >= (s.written ? end : written);
+    end = std::max(end, s.end);
+    if (s.written) written = std::max(written, s.end);
+  }
+  if (spans != few) std::free(spans);
+  return apart ? OLIVE_OK : OLIVE_ERR_INVALID_ARG;
+}
+
 olive_status olive_grad_clip(const void* const* src, void* const* dst, const int64_t* numel,
                              const int32_t* dtype, int32_t n, float max_norm, float* norm,
                              void* workspace, size_t ws_bytes, void* stream) {

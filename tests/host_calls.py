@@ -9,6 +9,7 @@ import types
 import torch
 
 from paper_2609_36246_gb300 import binding as B
+from paper_2609_36246_gb300 import build
 
 
 class Recorder:
@@ -18,8 +19,11 @@ class Recorder:
     Tensors are on device 0, the current one, except those that place() put elsewhere."""
 
     def __init__(self):
+        build.build()
         self.calls = []
         self._index = {}
+        # (host checks are the library's own)
+        self.olive_grad_clip_apart = B.lib().olive_grad_clip_apart
 
     def place(self, t, index):
         self._index[id(t)] = (index, t)  # (t is held, so that its id stays its own)

@@ -1,6 +1,9 @@
 """What the Python entry points of the layer's calls decide by themselves, on the host (host_calls.py):
 nothing here launches a kernel."""
 
+import array
+import random
+
 import pytest
 import torch
 
@@ -272,3 +275,35 @@ def test_output_gradients_that_start_anywhere(rec, T):
     assert off.is_contiguous() and off.data_ptr() % 16 == 6
     y.backward(off)
     assert rec.named("olive_gated_mlp_bwd")[0][0] % 16 == 0
+
+
+def test_drawn_lists_against_all_pairs(rec):
+    """olive_grad_clip_apart against every pair of spans, with and without shared sources."""
+    rng = random.Random(1)
+    share = lambda a, m, b, n: m > 0 and n > 0 and a < b + n and b < a + m
+    seen = [0, 0]
+    for trial in range(20000):
+        n = rng.randint(0, 5) if trial % 100 else 130 + trial // 200
+        room = 30 if n < 10 else 40 * n
+        num, kind = [rng.randint(0, 3) for _ in range(n)], [rng.randint(0, 1) for _ in range(n)]
+        dst = [64 + 4 * rng.randint(0, room) for _ in range(n)]
+        src = [d if rng.random() < 0.5 else 64 + 4 * rng.randint(0, room) for d in dst]
+        size = [c * (4 if k else 2) for c, k in zip(num, kind)]
+        apart = not any(share(dst[i], size[i], dst[j], size[j]) or share(src[j], size[j], dst[i], size[i])
+                        for i in range(n) for j in range(n) if i != j)
+        apart = apart and not any(s != d and share(s, m, d, m) for s, d, m in zip(src, dst, size))
+        table = array.array("Q", src + dst + num)
+        at, kinds = table.buffer_info()[0], array.array("i", kind)
+        got = rec.olive_grad_clip_apart(at, at + 8 * n, at + 16 * n, kinds.buffer_info()[0], n)
+        assert got == (0 if apart else 1), (src, dst, num, kind)
+        assert rec.olive_grad_clip_apart(at, None, at + 16 * n, kinds.buffer_info()[0], n) == 0
+        seen[apart] += 1
+    assert min(seen) > 2000
+
+
+def test_refusals_of_the_list_check(rec):
+    some = array.array("q", [0, 1 << 20, 4, 0])
+    at = some.buffer_info()[0]
+    check = rec.olive_grad_clip_apart
+    assert check(at, at, at, at, -1) == 2 and check(None, None, None, None, 0) == 0
+    assert check(None, at, at, at, 1) == 1 and check(at, at, None, at, 1) == 1 and check(at, at, at, None, 1) == 1
