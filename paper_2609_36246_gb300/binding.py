@@ -173,8 +173,8 @@ def _need(t, dtype, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous CUDA {dtype} tensor")
     # the call goes to the current device's stream, where another device's address is a stray one
-    if t.get_device() != torch.cuda.current_device():
-        raise TypeError(f"{name} must be on the current CUDA device, {torch.cuda.current_device()}")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise TypeError(f"{name} must be on the current CUDA device, {torch._C._cuda_getDevice()}")
 
 
 def new_status(device=None) -> torch.Tensor:
@@ -627,7 +627,8 @@ def _need_all(tensors, dtype, names):
             if t.dtype is not dtype:
                 break
         else:
-            if set(map(_device_of, tensors)) == {torch.cuda.current_device()} and all(map(_is_dense, tensors)):
+            where = set(map(_device_of, tensors))
+            if min(where) >= 0 and where == {torch._C._cuda_getDevice()} and all(map(_is_dense, tensors)):
                 return
     except (TypeError, AttributeError):
         pass
@@ -676,7 +677,7 @@ def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
     """Checks what the heads' forward and backward share; (views of q and k, the
     shared C arguments, their shapes, dtype, device)."""
     if (not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or
-            _device_of(q) != torch.cuda.current_device() or
+            not q.is_cuda or _device_of(q) != torch._C._cuda_getDevice() or
             q.dtype not in DTYPE or q.dim() != 3 or k.dim() != 3):
         raise TypeError("q and k must be bf16 or fp32 tensors [T, heads, D] on the current CUDA device")
     sq, sk, dtype, dev = q.shape, k.shape, q.dtype, q.device

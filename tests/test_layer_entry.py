@@ -307,3 +307,13 @@ def test_refusals_of_the_list_check(rec):
     check = rec.olive_grad_clip_apart
     assert check(at, at, at, at, -1) == 2 and check(None, None, None, None, 0) == 0
     assert check(None, at, at, at, 1) == 1 and check(at, at, None, at, 1) == 1 and check(at, at, at, None, 1) == 1
+
+
+def test_host_tensors_are_refused_with_a_name_also_without_a_gpu():
+    s, q = _mlp(), _qk()
+    with pytest.raises(TypeError, match="x must"):
+        B.olive_gated_mlp_fwd(*list(s.values())[:4])
+    with pytest.raises(TypeError, match="q and k must"):
+        B.olive_qk_norm_rope_fwd(*list(q.values())[:7])
+    with pytest.raises(TypeError, match="cu_seqlens must"):
+        B.olive_packed_positions(torch.zeros(3, dtype=torch.int32), 4)
