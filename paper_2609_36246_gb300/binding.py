@@ -158,10 +158,19 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# The current device's index.  (torch.cuda.current_device() without its look at whether
+# CUDA is initialised; what is asked for here follows a tensor that is on a device.)
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream():
     # the handle of torch.cuda.current_stream() without the Stream object (2.8 us
     # of a call on the GB300's host)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(_current())
+
+
+def _stream_of(device: int):
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _check(st: int, where: str):
@@ -173,8 +182,8 @@ def _need(t, dtype, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous CUDA {dtype} tensor")
     # the call goes to the current device's stream, where another device's address is a stray one
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise TypeError(f"{name} must be on the current CUDA device, {torch._C._cuda_getDevice()}")
+    if t.get_device() != _current():
+        raise TypeError(f"{name} must be on the current CUDA device, {_current()}")
 
 
 def new_status(device=None) -> torch.Tensor:
@@ -621,27 +630,34 @@ _is_dense, _dtype_of = torch.Tensor.is_contiguous, operator.attrgetter("dtype")
 
 
 def _need_all(tensors, dtype, names):
-    """_need for several tensors of one dtype at once."""
+    """_need for several tensors of one dtype at once; the current device's index."""
     try:
         for t in tensors:
             if t.dtype is not dtype:
                 break
         else:
-            where = set(map(_device_of, tensors))
-            if min(where) >= 0 and where == {torch._C._cuda_getDevice()} and all(map(_is_dense, tensors)):
-                return
+            cur, *more = set(map(_device_of, tensors))
+            if cur >= 0 and not more and cur == _current() and all(map(_is_dense, tensors)):
+                return cur
     except (TypeError, AttributeError):
         pass
     for t, n in zip(tensors, names):
         _need(t, dtype, n)
+    return _current()
 
 
-def _need_given(ws, dev_status):
+def _need_on(cur, t, dtype, name):
+    """_need, the current device's index being known."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != cur or not t.is_contiguous():
+        _need(t, dtype, name)
+
+
+def _need_given(cur, ws, dev_status):
     """The checks of a workspace and a status word that the caller brings."""
     if ws is not None:
-        _need(ws, ws.dtype, "ws")
+        _need_on(cur, ws, ws.dtype, "ws")
     if dev_status is not None:
-        _need(dev_status, _I32, "dev_status")
+        _need_on(cur, dev_status, _I32, "dev_status")
 
 
 @functools.lru_cache(maxsize=4096)
@@ -653,21 +669,21 @@ def _bytes(n, dev):
     return torch.empty(n, dtype=torch.uint8, device=dev)
 
 
-def _refuse_heads(t, T, H, D, dtype, name, device):
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
-        raise TypeError(f"{name} must be a CUDA {dtype} tensor on {device}")
+def _refuse_heads(t, T, H, D, dtype, name, cur):
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != cur:
+        raise TypeError(f"{name} must be a {dtype} tensor on the current CUDA device, {cur}")
     if t.shape != (T, H, D):
         raise ValueError(f"{name} must have the shape [{T}, {H}, {D}]")
     raise TypeError(f"{name}: the {D} values of a head must be contiguous")
 
 
-def _heads(t, shape, dtype, name, device):
+def _heads(t, shape, dtype, name, cur):
     """Pointer, token stride and head stride of a view [T, H, D] with contiguous heads."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != device:
-        _refuse_heads(t, *shape, dtype, name, device)
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.get_device() != cur:
+        _refuse_heads(t, *shape, dtype, name, cur)
     a, b, c = t.stride()
     if c != 1:
-        _refuse_heads(t, *shape, dtype, name, device)
+        _refuse_heads(t, *shape, dtype, name, cur)
     T, H, _ = shape
     # (the stride of a dimension of one entry means nothing)
     return t.data_ptr(), a if T > 1 else 0, b if H > 1 else 0
@@ -675,19 +691,19 @@ def _heads(t, shape, dtype, name, device):
 
 def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
     """Checks what the heads' forward and backward share; (views of q and k, the
-    shared C arguments, their shapes, dtype, device)."""
-    if (not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or
-            not q.is_cuda or _device_of(q) != torch._C._cuda_getDevice() or
+    shared C arguments, their shapes, dtype, device and its index)."""
+    if (not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or not q.is_cuda or
             q.dtype not in DTYPE or q.dim() != 3 or k.dim() != 3):
-        raise TypeError("q and k must be bf16 or fp32 tensors [T, heads, D] on the current CUDA device")
+        raise TypeError("q and k must be CUDA bf16 or fp32 tensors [T, heads, D]")
+    cur = _need_all((w_q, w_k), q.dtype, ("w_q", "w_k"))
     sq, sk, dtype, dev = q.shape, k.shape, q.dtype, q.device
     T, Hq, D = sq
     if sk[0] != T or sk[2] != D:
         raise ValueError(f"k must have the shape [{T}, heads, {D}]")
-    vq, vk = _heads(q, sq, dtype, "q", dev), _heads(k, sk, dtype, "k", dev)
-    _need_all((w_q, w_k), dtype, ("w_q", "w_k"))
-    _need_all((cos, sin), _F32, ("cos", "sin"))
-    _need(positions, _I32, "positions")
+    vq, vk = _heads(q, sq, dtype, "q", cur), _heads(k, sk, dtype, "k", cur)
+    _need_on(cur, cos, _F32, "cos")
+    _need_on(cur, sin, _F32, "sin")
+    _need_on(cur, positions, _I32, "positions")
     if w_q.numel() != D or w_k.numel() != D:
         raise ValueError(f"w_q and w_k must hold {D} values")
     table = cos.shape
@@ -698,10 +714,10 @@ def _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved):
     P, half = table
     common = (Hq, sk[1], w_q.data_ptr(), w_k.data_ptr(), eps, cos.data_ptr(), sin.data_ptr(),
               positions.data_ptr(), P, T, D, 2 * half, 1 if interleaved else 0)
-    return vq, vk, common, sq, sk, dtype, dev
+    return vq, vk, common, sq, sk, dtype, dev, cur
 
 
-def _qk_out(out, sq, sk, dtype, dev):
+def _qk_out(out, sq, sk, dtype, dev, cur):
     """The outputs and their views: contiguous ones where none are given."""
     if out is None:
         yq = torch.empty(sq, dtype=dtype, device=dev)
@@ -710,7 +726,7 @@ def _qk_out(out, sq, sk, dtype, dev):
         Hk = sk[1]
         return yq, yk, (yq.data_ptr(), Hq * D, D), (yk.data_ptr(), Hk * D, D)
     yq, yk = out
-    return yq, yk, _heads(yq, sq, dtype, "q's output", dev), _heads(yk, sk, dtype, "k's output", dev)
+    return yq, yk, _heads(yq, sq, dtype, "q's output", cur), _heads(yk, sk, dtype, "k's output", cur)
 
 
 def olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps: float = 1e-6,
@@ -719,11 +735,11 @@ def olive_qk_norm_rope_fwd(q, k, w_q, w_k, cos, sin, positions, eps: float = 1e-
     [D]) and rotation by positions [T] with the tables cos, sin (fp32 [P, R/2];
     R <= D).  q and k may be views of one projection.  Returns (q_out, k_out),
     contiguous unless given as `out` (views, or q and k themselves)."""
-    vq, vk, common, sq, sk, dtype, dev = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
-    yq, yk, oq, ok = _qk_out(out, sq, sk, dtype, dev)
-    _need_given(None, dev_status)
+    vq, vk, common, sq, sk, dtype, dev, cur = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    yq, yk, oq, ok = _qk_out(out, sq, sk, dtype, dev, cur)
+    _need_given(cur, None, dev_status)
     st = lib().olive_qk_norm_rope_fwd(*vq, *vk, *common, *oq, *ok, DTYPE[dtype], _ptr(dev_status),
-                                      _stream())
+                                      _stream_of(cur))
     if st:
         _check(st, "olive_qk_norm_rope_fwd")
     return yq, yk
@@ -734,24 +750,24 @@ def olive_qk_norm_rope_bwd(g_q, g_k, q, k, w_q, w_k, cos, sin, positions, eps: f
     """Gradients of olive_qk_norm_rope_fwd for its inputs q, k and the gradients
     g_q, g_k of its outputs.  Returns (d_q, d_k, dw_q, dw_k), the weights' in fp32;
     `out` takes (d_q, d_k), e.g. views of one projection's gradient."""
-    vq, vk, common, sq, sk, dtype, dev = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
-    gq, gk = _heads(g_q, sq, dtype, "g_q", dev), _heads(g_k, sk, dtype, "g_k", dev)
-    dq, dk, oq, ok = _qk_out(out, sq, sk, dtype, dev)
-    _need_given(ws, dev_status)
+    vq, vk, common, sq, sk, dtype, dev, cur = _qk_args(q, k, w_q, w_k, cos, sin, positions, eps, interleaved)
+    gq, gk = _heads(g_q, sq, dtype, "g_q", cur), _heads(g_k, sk, dtype, "g_k", cur)
+    dq, dk, oq, ok = _qk_out(out, sq, sk, dtype, dev, cur)
+    _need_given(cur, ws, dev_status)
     D = sq[2]
     dwq, dwk = torch.empty(D, dtype=_F32, device=dev), torch.empty(D, dtype=_F32, device=dev)
     if ws is None:
         ws = _bytes(_ws_bytes(12, 1, D, 1, 0, 0), dev)
     st = lib().olive_qk_norm_rope_bwd(*gq, *gk, *vq, *vk, *common, *oq, *ok, dwq.data_ptr(),
                                       dwk.data_ptr(), DTYPE[dtype], ws.data_ptr(), ws.numel(),
-                                      _ptr(dev_status), _stream())
+                                      _ptr(dev_status), _stream_of(cur))
     if st:
         _check(st, "olive_qk_norm_rope_bwd")
     return dq, dk, dwq, dwk
 
 
 def _mlp_args(x, W_gate, W_up, W_down):
-    _need_all((x, W_gate, W_up, W_down), _BF16, ("x", "W_gate", "W_up", "W_down"))
+    cur = _need_all((x, W_gate, W_up, W_down), _BF16, ("x", "W_gate", "W_up", "W_down"))
     rows, wide = x.shape, W_gate.shape
     if len(rows) != 2:
         raise ValueError("x must have the shape [T, d]")
@@ -759,7 +775,7 @@ def _mlp_args(x, W_gate, W_up, W_down):
     f = wide[0]
     if wide != (f, d) or W_up.shape != wide or W_down.shape != (d, f):
         raise ValueError("W_gate and W_up must have the shape [f, d], W_down [d, f]")
-    return T, d, f
+    return T, d, f, cur
 
 
 def olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual=None, act: str = "silu",
@@ -769,25 +785,25 @@ def olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual=None, act: str = "silu
     "gelu_tanh".  Returns (y, saved): saved, with save=True, is what
     olive_gated_mlp_bwd takes (the pre-activations in 16 bits, 4 T f bytes), else
     None."""
-    T, d, f = _mlp_args(x, W_gate, W_up, W_down)
+    T, d, f, cur = _mlp_args(x, W_gate, W_up, W_down)
     dev = x.device
     if residual is not None:
-        _need(residual, _BF16, "residual")
+        _need_on(cur, residual, _BF16, "residual")
         if residual.shape != x.shape:
             raise ValueError("residual must have the shape of x")
     if out is None:
         out = torch.empty((T, d), dtype=_BF16, device=dev)
     else:
-        _need(out, _BF16, "out")
+        _need_on(cur, out, _BF16, "out")
         if out.shape != x.shape:
             raise ValueError("out must have the shape of x")
-    _need_given(ws, dev_status)
+    _need_given(cur, ws, dev_status)
     saved = torch.empty((2, T, f), dtype=torch.int16, device=dev) if save else None
     if ws is None:
         ws = _bytes(_ws_bytes(10, T, d, f, 0, 0), dev)
     st = lib().olive_gated_mlp_fwd(x.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(),
                                    _ptr(residual), T, d, f, ACT[act], out.data_ptr(), _ptr(saved),
-                                   ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream())
+                                   ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream_of(cur))
     if st:
         _check(st, "olive_gated_mlp_fwd")
     return out, saved
@@ -798,10 +814,10 @@ def olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, act: str = "silu",
                         ws=None, dev_status=None, out=None):
     """Gradients of olive_gated_mlp_fwd (that of its residual is dy).  Returns
     (dx, dW_gate, dW_up, dW_down) of grad_dtype, None for what is not needed."""
-    T, d, f = _mlp_args(x, W_gate, W_up, W_down)
+    T, d, f, cur = _mlp_args(x, W_gate, W_up, W_down)
     dev = x.device
-    _need(dy, _BF16, "dy")
-    _need(saved, torch.int16, "saved")
+    _need_on(cur, dy, _BF16, "dy")
+    _need_on(cur, saved, torch.int16, "saved")
     if dy.shape != x.shape or saved.shape != (2, T, f):
         raise ValueError("dy must have the shape of x, saved that of the forward")
     if out is None:
@@ -815,17 +831,17 @@ def olive_gated_mlp_bwd(dy, x, W_gate, W_up, W_down, saved, act: str = "silu",
         dx, dg, du, dd = out
         for t, shape in ((dx, (T, d)), (dg, (f, d)), (du, (f, d)), (dd, (d, f))):
             if t is not None:
-                _need(t, grad_dtype, "out")
+                _need_on(cur, t, grad_dtype, "out")
                 if t.shape != shape:
                     raise ValueError("out must have the shapes of x and the weights")
     kind = DTYPE[grad_dtype]
-    _need_given(ws, dev_status)
+    _need_given(cur, ws, dev_status)
     if ws is None:
         ws = _bytes(_ws_bytes(11, T, d, f, 1, kind), dev)
     st = lib().olive_gated_mlp_bwd(dy.data_ptr(), x.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(),
                                    W_down.data_ptr(), saved.data_ptr(), T, d, f, ACT[act], _ptr(dx),
                                    _ptr(dg), _ptr(du), _ptr(dd), kind, ws.data_ptr(), ws.numel(),
-                                   _ptr(dev_status), _stream())
+                                   _ptr(dev_status), _stream_of(cur))
     if st:
         _check(st, "olive_gated_mlp_bwd")
     return dx, dg, du, dd
@@ -850,7 +866,7 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     all (out=None: only the norm).  What is written must not share memory with
     another gradient or output."""
     n = len(grads)
-    cur = torch.cuda.current_device()
+    cur = _current()
     src, num, kinds = _grad_list(grads, cur, "gradients")
     dst = None
     if out is not None:
@@ -867,8 +883,8 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     if norm is None:
         norm = torch.empty(1, dtype=_F32, device="cuda")
     else:
-        _need(norm, _F32, "norm")
-    _need_given(ws, None)
+        _need_on(cur, norm, _F32, "norm")
+    _need_given(cur, ws, None)
     if ws is None:
         ws = _bytes(_ws_bytes(13, max(n, 1), 0, 1, 0, 0), "cuda")
     # the four host arrays behind one another
@@ -882,7 +898,7 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     # (blocks of one tensor would write what those of another read or write)
     if L.olive_grad_clip_apart(*lists):
         raise ValueError("a gradient that is scaled must not share memory with another (a tied one is listed once)")
-    st = L.olive_grad_clip(*lists, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    st = L.olive_grad_clip(*lists, max_norm, norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(cur))
     if st:
         _check(st, "olive_grad_clip")
     return norm

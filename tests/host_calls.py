@@ -52,7 +52,7 @@ def recorded(monkeypatch):
     monkeypatch.setattr(B, "_ws_bytes", lambda *_: 256)
     monkeypatch.setattr(B, "_device_of", rec.device_index)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(B, "_current", lambda: 0)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
     monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
     monkeypatch.setattr(torch.Tensor, "get_device", lambda t: rec.device_index(t))
