@@ -655,9 +655,10 @@ OLIVE_API olive_status olive_gated_mlp_bwd(const void* dy, const void* x, const 
  * it otherwise, nor another tensor (olive_grad_clip_apart tells; this call does
  * not look); dst NULL: only the norm.  Any alignment of
  * whole elements; 16-byte aligned pointers are read and written in 16-byte
- * pieces.  The squares are summed in fp32 by 32s, in fp64 beyond (of
- * values scaled by a power of two where their squares would leave fp32's
- * range), in a fixed order.
+ * pieces, others one by one, which takes five to ten times as long.  The squares are
+ * summed in fp32 by 32s (fp32 tensors: by 16s; of values scaled by a power of two
+ * where their squares would leave fp32's range) and in fp64 beyond; values outside
+ * whole 16-byte pieces are squared and summed in fp64.  The order is fixed.
  * A norm that is infinite or NaN goes into the factor as it is (0 or NaN).
  * norm fp32 [1] (device); n >= 0 (0: the norm is 0); max_norm > 0.
  * workspace: olive_workspace_size(OLIVE_OP_GRAD_CLIP, max(n, 1), 0, 0, 1, 0, 0) bytes.

@@ -25,7 +25,7 @@
 //
 // What bounds it: the tensor pipe in the products with long K steps and light
 // epilogues, the epilogue's loads and stores in MM_UP and MM_DH at small d.
-// Measured: 8192 rows, d = 4096, f = 12288, forward and backward 4.5 ms, 1.65
+// Measured: 8192 rows, d = 4096, f = 12288, forward and backward 4.5 ms, 1.64
 // PFLOP/s, under the power cap; 2777 rows, d = 2048, f = 5504, launch by launch from
 // empty caches, us: up 83, down 52, dh 68, gradients 175 (1.8 PFLOP/s; 91 % of the
 // tensor pipe's cycles on 2816 rows); d = 2040, f = 5464, whose rows are not whole

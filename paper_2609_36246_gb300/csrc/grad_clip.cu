@@ -6,14 +6,19 @@
 // fp32 values) into one fp32 sum and adds that to an fp64 sum.  Where that fp32
 // sum is not finite, large or nearly zero the same values, still in registers,
 // are squared again scaled by a power of two: squares leave fp32's range long
-// before the values do.  Every block's total goes to the workspace.
+// before the values do.  Every block's total goes to the workspace.  Values that are
+// not in whole 16-byte pieces (a tensor's last few, all of one that starts off 16 bytes)
+// are read one by one and squared in fp64.
 //
 // The second launch adds the blocks' totals (each block by itself: a few KB from
 // L2), and scales, from the last unit to the first: what the first launch read
 // last is still in the L2.
 //
 // What bounds it: HBM, each gradient read twice and written once (read once where
-// all of them fit the L2): 2 GB in 915 us, of which the norm 282 (7.15 TB/s).
+// all of them fit the L2): 2 GB in 915 us, of which the norm 282 (7.15 TB/s).  Of a
+// tensor that starts off 16 bytes, the single loads and the fp64 squares: 1 GB of bf16
+// takes 1819 us for the norm and 2946 with the scaling (176 and 477 where it is aligned;
+// from empty caches).
 #include <algorithm>
 #include <cmath>
 

@@ -378,12 +378,14 @@ olive_status launch_mlp_fwd(const Ctx& c, const void* x, const void* W_gate, con
                             int32_t f, int act, void* y, void* saved, void* ws,
                             int32_t* dev_status);
 // The forward on few rows (gated_mlp_few.cu); h: workspace [T, f].
-// It is taken up to 64 rows, and up to 128 where the first launch's tiles of 64
-// weight rows are more than half of the SMs.  Measured, us, this form and the other:
-// 64 rows (2048, 6144) 29 and 37, (1024, 2816) 17 and 21, (4096, 2816) 35 and 30;
-// 80 rows (4096, 11008) 69 and 75, (2040, 5464) 35 and 40, (2560, 8192) 48 and 44,
-// but (2560, 5120) 42 and 39, (2048, 4096) 33 and 28, (512, 1536) 19 and 16 and (256,
-// 704) 18 and 13, of which the rule lets the first of the four through.
+// It is taken up to 64 rows, and up to 128 from f = 4928 on, where the first launch
+// has more tiles of 64 weight rows than half of 152 SMs.  The rule looks at T and f
+// alone, d decides as well, so it is not always the better form.  Measured, us, this
+// form and the other, where it is right: 64 rows (2048, 6144) 29 and 37, (1024, 2816) 17
+// and 21; 80 rows (4096, 11008) 69 and 75, (2040, 5464) 35 and 40; and left to the other,
+// 80 rows (2048, 4096) 33 and 28, (512, 1536) 19 and 16, (256, 704) 18 and 13.  Where it
+// is wrong: 64 rows (4096, 2816) 35 and 30, (2048, 2048) 22.1 and 21.4; 80 rows (2560,
+// 8192) 48 and 44, (2560, 5120) 42 and 39.
 constexpr int kMlpFewRows = 64, kMlpFewRowsWide = 128, kMlpWide = 64 * 77;
 inline bool mlp_few(int64_t T, int64_t f) {
   return T <= kMlpFewRows || (T <= kMlpFewRowsWide && f >= kMlpWide);
