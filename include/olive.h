@@ -45,6 +45,12 @@
  *                            gated feed-forward block with its residual
  *   olive_grad_clip          global norm of a list of gradients, and clipping
  *   olive_grad_clip_apart    whether such a list may be scaled (a host check)
+ *   olive_embedding_fwd, olive_embedding_bwd
+ *                            rows of the embedding by packed ids, and its
+ *                            gradient by sorted tokens
+ *   olive_row_norm_fwd, olive_row_norm_bwd
+ *                            layer norm or RMS norm of the rows, with the
+ *                            residual's sum on the way
  *
  * Conventions shared by every call
  *   - Every pointer argument is a DEVICE pointer unless stated otherwise.  The
@@ -115,11 +121,13 @@ enum { OLIVE_REDUCE_SUM = 0, OLIVE_REDUCE_MEAN = 1 };
 enum { OLIVE_KL_REVERSE = 0, OLIVE_KL_FORWARD = 1 };
 enum { OLIVE_DTYPE_BF16 = 0, OLIVE_DTYPE_F32 = 1 };
 enum { OLIVE_ACT_SILU = 0, OLIVE_ACT_GELU_TANH = 1 };
+enum { OLIVE_NORM_LAYER = 0, OLIVE_NORM_RMS = 1 };
 enum { OLIVE_OP_LOGPROB_FWD = 0, OLIVE_OP_LOSS_BWD = 1, OLIVE_OP_DIVERGENCE = 2,
        OLIVE_OP_TOPK_FWD = 3, OLIVE_OP_SPLICE_MASKED = 4, OLIVE_OP_TOPK_KL_BWD = 5,
        OLIVE_OP_LOSS_FWD_BWD = 6, OLIVE_OP_OPD_STATS = 7, OLIVE_OP_TOPK_KL_FWD_BWD = 8,
        OLIVE_OP_LOSS_FWD_BWD_SLAB = 9, OLIVE_OP_GATED_MLP_FWD = 10,
-       OLIVE_OP_GATED_MLP_BWD = 11, OLIVE_OP_QK_NORM_ROPE_BWD = 12, OLIVE_OP_GRAD_CLIP = 13 };
+       OLIVE_OP_GATED_MLP_BWD = 11, OLIVE_OP_QK_NORM_ROPE_BWD = 12, OLIVE_OP_GRAD_CLIP = 13,
+       OLIVE_OP_ROW_NORM_BWD = 14, OLIVE_OP_EMBEDDING_BWD = 15 };
 
 /*
  * Rows of the G slab that the slab forms (olive_token_loss_fwd_bwd_slab,
@@ -155,6 +163,8 @@ OLIVE_API olive_status olive_status_clear(int32_t* dev_status, void* stream);
  *       V = inner width f, d_t ignored.
  *   op  OLIVE_OP_QK_NORM_ROPE_BWD: d = head width; the rest ignored.
  *   op  OLIVE_OP_GRAD_CLIP: T = number of tensors; the rest ignored.
+ *   op  OLIVE_OP_ROW_NORM_BWD: d = width; the rest ignored.
+ *   op  OLIVE_OP_EMBEDDING_BWD: T, d = width, V; the rest ignored.
  *   `grad` (bwd / divergence): non-zero when gradients are requested
  *   (OLIVE_OP_LOSS_BWD always computes them); `grad_dtype` is the dtype of
  *   d_W for OLIVE_OP_LOSS_BWD (bf16 output needs an fp32 accumulator).
@@ -679,6 +689,72 @@ OLIVE_API olive_status olive_grad_clip(const void* const* src, void* const* dst,
 OLIVE_API olive_status olive_grad_clip_apart(const void* const* src, void* const* dst,
                                              const int64_t* numel, const int32_t* dtype,
                                              int32_t n);
+
+/*
+ * olive_embedding_fwd -- rows of the embedding W [V, d] for packed ids:
+ *   out[t] = scale W[ids[t]]   rounded once to `dtype` (OLIVE_DTYPE_BF16 or
+ * OLIVE_DTYPE_F32), the type of W and out [T, d].  n_ids (device, int32 [1]) may
+ * be NULL: all T rows are looked up; else rows t >= *n_ids are zeroed (what is
+ * below 0 or above T counts as 0 or T), e.g. cu_seqlens + S of olive_splice_pack.
+ * T >= 0, V >= 1, d a multiple of 8.  An id outside [0, V) gives NaN in its row and
+ * OLIVE_ERR_TOKEN_RANGE; dev_status may be NULL (nothing is reported then).
+ */
+OLIVE_API olive_status olive_embedding_fwd(const void* W, const int32_t* ids, const int32_t* n_ids,
+                                           int32_t T, int32_t V, int32_t d, float scale, void* out,
+                                           int dtype, int32_t* dev_status, void* stream);
+
+/*
+ * olive_embedding_bwd -- the gradient of olive_embedding_fwd's W for the
+ * gradient dy [T, d] (of `dtype`) of its output:
+ *   dW[v] = scale sum over t with ids[t] = v of dy[t]      (0 where there is none)
+ * or, with `accumulate` (1), dW[v] += that, for a W whose gradient holds the LM
+ * head's already: only rows that a token names are then read and written.  dW
+ * [V, d] of grad_dtype, rounded once (with what it held in the same sum).
+ * Tokens are sorted by id and summed in their order in fp32 (runs of more than 32
+ * tokens, beyond 65536 tokens 128, in pieces of that size, added in fp64), so
+ * results are the same bits from call to call.  Rows t >= *n_ids and ids outside
+ * [0, V) (OLIVE_ERR_TOKEN_RANGE) count nowhere.  T = 0: dW is zeroed, or left.
+ * workspace: olive_workspace_size(OLIVE_OP_EMBEDDING_BWD, T, d, 0, V, 0, 0) bytes.
+ */
+OLIVE_API olive_status olive_embedding_bwd(const void* dy, const int32_t* ids,
+                                           const int32_t* n_ids, int32_t T, int32_t V, int32_t d,
+                                           float scale, void* dW, int dtype, int grad_dtype,
+                                           int accumulate, void* workspace, size_t ws_bytes,
+                                           int32_t* dev_status, void* stream);
+
+/*
+ * olive_row_norm_fwd -- norm of every row of x [T, d], weights w [d], bias b [d] or
+ * NULL, all of `dtype` (OLIVE_DTYPE_BF16 or OLIVE_DTYPE_F32):
+ *   h = x, or with a residual [T, d]: h = x + residual, rounded, stored to `sum`
+ *   m = mean(h)  (OLIVE_NORM_LAYER; 0 for OLIVE_NORM_RMS)
+ *   r = 1 / sqrt(mean((h - m)^2) + eps)
+ *   y = (h - m) r w + b     in fp32, rounded once
+ * `stats` (fp32 [2, T], NULL: not kept) takes the rows' m, then their r, for
+ * olive_row_norm_bwd.  residual and sum are both given or both NULL; y may be x, sum
+ * may be x or residual (the same pointer), y and sum differ.  T >= 0, d a multiple of
+ * 8 up to 16384, eps >= 0, pointers 16-byte aligned.
+ */
+OLIVE_API olive_status olive_row_norm_fwd(const void* x, const void* residual, const void* w,
+                                          const void* b, int32_t T, int32_t d, float eps, int kind,
+                                          void* y, void* sum, float* stats, int dtype,
+                                          void* stream);
+
+/*
+ * olive_row_norm_bwd -- gradients of olive_row_norm_fwd for the rows h it normed
+ * (its x, or its sum), from the gradient dy of y, and g_sum, that of the sum by
+ * other ways (NULL: none): with n = (h - m) r and a = dy w,
+ *   dx = r (a - mean(a) - n mean(a n)) + g_sum   (mean(a): OLIVE_NORM_LAYER only)
+ *   dw = sum over rows of dy n,   db = sum over rows of dy    fp32 [d]
+ * dx is the gradient of x and of the residual; it may be dy or g_sum.  db may be
+ * NULL.  Sums over rows have a fixed order, in fp32 within a block of threads and
+ * fp64 across.  T = 0: dw and db are zeroed.
+ * workspace: olive_workspace_size(OLIVE_OP_ROW_NORM_BWD, 1, d, 0, 1, 0, 0) bytes.
+ */
+OLIVE_API olive_status olive_row_norm_bwd(const void* dy, const void* h, const void* w,
+                                          const float* stats, const void* g_sum, int32_t T,
+                                          int32_t d, int kind, void* dx, float* dw, float* db,
+                                          int dtype, void* workspace, size_t ws_bytes,
+                                          void* stream);
 
 #ifdef __cplusplus
 }

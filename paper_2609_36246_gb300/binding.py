@@ -35,8 +35,9 @@ DTYPE = {torch.bfloat16: 0, torch.float32: 1}
 OP = {"logprob_fwd": 0, "loss_bwd": 1, "divergence": 2, "topk_fwd": 3, "splice_masked": 4,
       "topk_kl_bwd": 5, "loss_fwd_bwd": 6, "opd_stats": 7, "topk_kl_fwd_bwd": 8,
       "loss_fwd_bwd_slab": 9, "gated_mlp_fwd": 10, "gated_mlp_bwd": 11, "qk_norm_rope_bwd": 12,
-      "grad_clip": 13}
+      "grad_clip": 13, "row_norm_bwd": 14, "embedding_bwd": 15}
 ACT = {"silu": 0, "gelu_tanh": 1}
+NORM = {"layer": 0, "rms": 1}
 
 
 class OliveError(RuntimeError):
@@ -144,6 +145,17 @@ def _configure(L: ctypes.CDLL) -> ctypes.CDLL:
     L.olive_grad_clip.argtypes = [_P, _P, _P, _P, _I, _F, _P, _P, _S, _P]
     L.olive_grad_clip_apart.restype = ctypes.c_int
     L.olive_grad_clip_apart.argtypes = [_P, _P, _P, _P, _I]
+    L.olive_embedding_fwd.restype = ctypes.c_int
+    L.olive_embedding_fwd.argtypes = [_P, _P, _P, _I, _I, _I, _F, _P, ctypes.c_int, _P, _P]
+    L.olive_embedding_bwd.restype = ctypes.c_int
+    L.olive_embedding_bwd.argtypes = [_P, _P, _P, _I, _I, _I, _F, _P, ctypes.c_int, ctypes.c_int,
+                                      ctypes.c_int, _P, _S, _P, _P]
+    L.olive_row_norm_fwd.restype = ctypes.c_int
+    L.olive_row_norm_fwd.argtypes = [_P, _P, _P, _P, _I, _I, _F, ctypes.c_int, _P, _P, _P,
+                                     ctypes.c_int, _P]
+    L.olive_row_norm_bwd.restype = ctypes.c_int
+    L.olive_row_norm_bwd.argtypes = [_P, _P, _P, _P, _P, _I, _I, ctypes.c_int, _P, _P, _P,
+                                     ctypes.c_int, _P, _S, _P]
     return L
 
 
@@ -904,6 +916,147 @@ def olive_grad_clip(grads, max_norm: float, out="inplace", norm=None, ws=None):
     return norm
 
 
+def _embedding_ids(cur, ids, n_ids, dev_status):
+    _need_on(cur, ids, _I32, "ids")
+    if n_ids is not None:
+        _need_on(cur, n_ids, _I32, "n_ids")
+        if n_ids.numel() != 1:
+            raise ValueError("n_ids must hold one value")
+    _need_given(cur, None, dev_status)
+
+
+def olive_embedding_fwd(W, ids, scale: float = 1.0, n_ids=None, dev_status=None, out=None):
+    """scale * W[ids] (W [V, d] bf16 or fp32, ids int32 [T]); rows from n_ids on
+    (a device int32, e.g. cu_seqlens[-1:]) are 0."""
+    if not isinstance(W, torch.Tensor) or W.dtype not in DTYPE or W.dim() != 2:
+        raise TypeError("W must be a bf16 or fp32 tensor [V, d]")
+    dtype = W.dtype
+    cur = _need_all((W,), dtype, ("W",))
+    _embedding_ids(cur, ids, n_ids, dev_status)
+    T = ids.numel()
+    V, d = W.shape
+    if out is None:
+        out = torch.empty((T, d), dtype=dtype, device=W.device)
+    else:
+        _need_on(cur, out, dtype, "out")
+        if out.shape != (T, d):
+            raise ValueError(f"out must have the shape [{T}, {d}]")
+    st = lib().olive_embedding_fwd(W.data_ptr(), ids.data_ptr(), _ptr(n_ids), T, V, d, scale,
+                                   out.data_ptr(), DTYPE[dtype], _ptr(dev_status), _stream_of(cur))
+    if st:
+        _check(st, "olive_embedding_fwd")
+    return out
+
+
+def olive_embedding_bwd(dy, ids, V: int, scale: float = 1.0, n_ids=None, grad_dtype=torch.bfloat16,
+                        out=None, accumulate: bool = False, ws=None, dev_status=None):
+    """Gradient [V, d] of olive_embedding_fwd's W for the gradient dy [T, d] of its
+    output, or with `accumulate` added to `out` (an LM head's gradient that is also
+    the embedding's).  Sums have a fixed order."""
+    if not isinstance(dy, torch.Tensor) or dy.dtype not in DTYPE or dy.dim() != 2:
+        raise TypeError("dy must be a bf16 or fp32 tensor [T, d]")
+    cur = _need_all((dy,), dy.dtype, ("dy",))
+    _embedding_ids(cur, ids, n_ids, dev_status)
+    _need_given(cur, ws, None)
+    T, d = dy.shape
+    if ids.numel() != T:
+        raise ValueError(f"ids must hold {T} values")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the gradient that is added to, out")
+        out = torch.empty((V, d), dtype=grad_dtype, device=dy.device)
+    else:
+        grad_dtype = out.dtype
+        if grad_dtype not in DTYPE:
+            raise TypeError("out must be bf16 or fp32")
+        _need_on(cur, out, grad_dtype, "out")
+        if out.shape != (V, d):
+            raise ValueError(f"out must have the shape [{V}, {d}]")
+    if ws is None:
+        ws = _bytes(_ws_bytes(15, T, d, V, 0, 0), dy.device)
+    st = lib().olive_embedding_bwd(dy.data_ptr(), ids.data_ptr(), _ptr(n_ids), T, V, d, scale,
+                                   out.data_ptr(), DTYPE[dy.dtype], DTYPE[grad_dtype],
+                                   1 if accumulate else 0, ws.data_ptr(), ws.numel(),
+                                   _ptr(dev_status), _stream_of(cur))
+    if st:
+        _check(st, "olive_embedding_bwd")
+    return out
+
+
+def _norm_args(x, w, name):
+    """What the rows' norm's forward and backward share: T, d, dtype and the device's index."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in DTYPE or x.dim() != 2:
+        raise TypeError(f"{name} must be a bf16 or fp32 tensor [T, d]")
+    dtype = x.dtype
+    cur = _need_all((x, w), dtype, (name, "w"))
+    T, d = x.shape
+    if w.shape != (d,):
+        raise ValueError(f"w must have the shape [{d}]")
+    return T, d, dtype, cur
+
+
+def _like(cur, t, x, name):
+    _need_on(cur, t, x.dtype, name)
+    if t.shape != x.shape:
+        raise ValueError(f"{name} must have the shape of the rows")
+    return t
+
+
+def olive_row_norm_fwd(x, w, b=None, residual=None, eps: float = 1e-6, kind: str = "layer",
+                       save: bool = False, out=None, sum_out=None):
+    """Norm of the rows of h = x (+ residual), [T, d] bf16 or fp32: kind "layer"
+    (centred) or "rms", weights w and bias b [d].  Returns (y, h, stats): h is x
+    itself where there is no residual, stats (save=True) what olive_row_norm_bwd
+    takes, else None."""
+    T, d, dtype, cur = _norm_args(x, w, "x")
+    dev = x.device
+    if b is not None:
+        _need_on(cur, b, dtype, "b")
+        if b.shape != (d,):
+            raise ValueError(f"b must have the shape [{d}]")
+    y = torch.empty((T, d), dtype=dtype, device=dev) if out is None else _like(cur, out, x, "out")
+    h = x
+    if residual is not None:
+        _like(cur, residual, x, "residual")
+        h = torch.empty((T, d), dtype=dtype, device=dev) if sum_out is None else _like(cur, sum_out, x, "sum_out")
+    elif sum_out is not None:
+        raise ValueError("sum_out is the sum with a residual")
+    stats = torch.empty((2, T), dtype=_F32, device=dev) if save else None
+    st = lib().olive_row_norm_fwd(x.data_ptr(), _ptr(residual), w.data_ptr(), _ptr(b), T, d, eps,
+                                  NORM[kind], y.data_ptr(), h.data_ptr() if residual is not None else None,
+                                  _ptr(stats), DTYPE[dtype], _stream_of(cur))
+    if st:
+        _check(st, "olive_row_norm_fwd")
+    return y, h, stats
+
+
+def olive_row_norm_bwd(dy, h, w, stats, g_h=None, kind: str = "layer", need_db: bool = True, ws=None,
+                       out=None):
+    """Gradients of olive_row_norm_fwd for the rows h that it normed: (dx, dw, db),
+    dx that of x and of the residual, dw and db fp32 [d] (db None where it is not
+    needed).  g_h, the gradient of h by other ways, is added to dx."""
+    T, d, dtype, cur = _norm_args(h, w, "h")
+    dev = h.device
+    _like(cur, dy, h, "dy")
+    if g_h is not None:
+        _like(cur, g_h, h, "g_h")
+    _need_on(cur, stats, _F32, "stats")
+    if stats.shape != (2, T):
+        raise ValueError("stats must be that of the forward")
+    _need_given(cur, ws, None)
+    dx = torch.empty((T, d), dtype=dtype, device=dev) if out is None else _like(cur, out, h, "out")
+    dw = torch.empty(d, dtype=_F32, device=dev)
+    db = torch.empty(d, dtype=_F32, device=dev) if need_db else None
+    if ws is None:
+        ws = _bytes(_ws_bytes(14, 1, d, 1, 0, 0), dev)
+    st = lib().olive_row_norm_bwd(dy.data_ptr(), h.data_ptr(), w.data_ptr(), stats.data_ptr(), _ptr(g_h),
+                                  T, d, NORM[kind], dx.data_ptr(), dw.data_ptr(), _ptr(db), DTYPE[dtype],
+                                  ws.data_ptr(), ws.numel(), _stream_of(cur))
+    if st:
+        _check(st, "olive_row_norm_bwd")
+    return dx, dw, db
+
+
 class FusedLMHeadCE(torch.autograd.Function):
     """Eq. (osd-ce) loss over the masked rows as an autograd op (gradients in
     the dtype of hidden; first derivatives only).  A status word given is the
@@ -1030,6 +1183,68 @@ def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu", dev_status=Non
     if not torch.is_grad_enabled():
         return olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual, act, dev_status=dev_status)[0]
     return GatedMLP.apply(x, W_gate, W_up, W_down, residual, act, dev_status)
+
+
+def _whole(g):
+    """A gradient as the calls read it: dense and on a 16-byte boundary, else a copy."""
+    return g if g.is_contiguous() and g.data_ptr() % 16 == 0 else g.clone(memory_format=torch.contiguous_format)
+
+
+class Embedding(torch.autograd.Function):
+    """Embedding rows as an autograd op (the gradient in W's type; first derivatives
+    only).  A status word given is the forward's and the backward's."""
+
+    @staticmethod
+    def forward(ctx, W, ids, scale=1.0, n_ids=None, dev_status=None):
+        ctx.save_for_backward(ids, *(() if n_ids is None else (n_ids,)))
+        ctx.V, ctx.scale, ctx.dtype, ctx.dev_status = W.shape[0], scale, W.dtype, dev_status
+        return olive_embedding_fwd(W, ids, scale, n_ids, dev_status)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        ids, *n_ids = ctx.saved_tensors
+        dW = olive_embedding_bwd(_whole(dy), ids, ctx.V, ctx.scale, n_ids[0] if n_ids else None, ctx.dtype,
+                                 dev_status=ctx.dev_status)
+        return dW, None, None, None, None
+
+
+def embedding(W, ids, scale=1.0, n_ids=None, dev_status=None):
+    return Embedding.apply(W, ids, scale, n_ids, dev_status)
+
+
+class RowNorm(torch.autograd.Function):
+    """Rows' norm as an autograd op (weights' gradients in the weights' type; first
+    derivatives only): y, or with a residual (y, h) with h the sum."""
+
+    @staticmethod
+    def forward(ctx, x, w, b=None, residual=None, eps=1e-6, kind="rms"):
+        y, h, stats = olive_row_norm_fwd(x, w, b, residual, eps, kind, save=True)
+        ctx.save_for_backward(h, w, stats)
+        ctx.kind, ctx.b_dtype, ctx.added = kind, None if b is None else b.dtype, residual is not None
+        ctx.set_materialize_grads(False)
+        return (y, h) if ctx.added else y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, g_h=None):
+        if dy is None and g_h is None:
+            return None, None, None, None, None, None
+        h, w, stats = ctx.saved_tensors
+        if dy is None:  # only the sum was used
+            return g_h, None, None, g_h, None, None
+        dx, dw, db = olive_row_norm_bwd(_whole(dy), h, w, stats, None if g_h is None else _whole(g_h), ctx.kind,
+                                        ctx.b_dtype is not None)
+        return (dx, dw.to(w.dtype), None if db is None else db.to(ctx.b_dtype), dx if ctx.added else None,
+                None, None)
+
+
+def row_norm(x, w, b=None, residual=None, eps=1e-6, kind="rms"):
+    # (nothing is kept for a backward where autograd is off)
+    if not torch.is_grad_enabled():
+        y, h, _ = olive_row_norm_fwd(x, w, b, residual, eps, kind)
+        return y if residual is None else (y, h)
+    return RowNorm.apply(x, w, b, residual, eps, kind)
 
 
 def _in_memory_order(g):

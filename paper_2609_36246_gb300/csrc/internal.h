@@ -437,4 +437,47 @@ olive_status launch_grad_clip(const Ctx& c, const void* const* src, void* const*
                               const int64_t* numel, const int32_t* dtype, int32_t n, float max_norm,
                               float* norm, void* ws);
 
+// ---- rows' norm (row_norm.cu) ----
+struct NormArgs {
+  const void *x, *residual, *w, *b;  // x: forward; backward: the rows that were normed
+  void *y, *sum;
+  float* stats;                      // [2, T]: means, reciprocal deviations
+  const void *dy, *g_sum;
+  void* dx;
+  float *dw, *db;
+  int32_t T, d;
+  float eps;
+  int kind, dtype;
+  void* ws;
+};
+constexpr int32_t kMaxNormDim = 16384;
+size_t norm_bwd_ws_bytes(int64_t d);
+olive_status launch_norm_fwd(const Ctx& c, const NormArgs& a);
+olive_status launch_norm_bwd(const Ctx& c, const NormArgs& a);
+
+// ---- embedding (embedding.cu) ----
+struct EmbArgs {
+  const void* W;
+  const int32_t *ids, *n_ids;
+  int32_t T, V, d;
+  float scale;
+  void* out;
+  const void* dy;
+  void* dW;
+  int dtype, grad_dtype, accumulate;
+  int32_t* dev_status;
+};
+struct EmbSort {
+  uint32_t* buf_keys[2];  // [T] ids of the tokens, V where a token has none
+  int32_t* buf_pos[2];    // [T] their tokens
+  uint32_t* table;        // [tiles, 512] digits of a pass
+  uint32_t* named;        // [ceil(V / 32)] bit v: a token names row v
+  float* part;            // [units, 2, d] parts of runs that cross units
+  const uint32_t* keys;   // the sorted ones
+  const int32_t* pos;
+};
+size_t emb_bwd_ws_bytes(int64_t T, int64_t d, int64_t V);
+olive_status launch_emb_fwd(const Ctx& c, const EmbArgs& a);
+olive_status launch_emb_bwd(const Ctx& c, const EmbArgs& a, void* ws);
+
 }  // namespace olive

@@ -424,6 +424,7 @@ olive_status olive_status_clear(int32_t* dev_status, void* stream) {
 size_t olive_workspace_size(int op, int32_t T, int32_t d, int32_t d_t, int32_t V, int grad,
                             int grad_dtype) {
   if (op == OLIVE_OP_SPLICE_MASKED) return T < 1 ? 0 : splice_masked_ws_bytes(T);
+  if (op == OLIVE_OP_ROW_NORM_BWD) return width_ok(d) && d <= kMaxNormDim ? norm_bwd_ws_bytes(d) : 0;
   if (op == OLIVE_OP_QK_NORM_ROPE_BWD) return width_ok(d) && d <= kMaxHeadDim ? qk_bwd_ws_bytes(d) : 0;
   if (op == OLIVE_OP_GRAD_CLIP) return T < 1 ? 0 : grad_clip_ws_bytes(T);
   if (T < 1 || V < 1 || !width_ok(d)) return 0;
@@ -432,6 +433,7 @@ size_t olive_workspace_size(int op, int32_t T, int32_t d, int32_t d_t, int32_t V
     case OLIVE_OP_GATED_MLP_BWD:
       if (!width_ok(V) || T > kMaxMlpRows) return 0;
       return mlp_ws_bytes(T, V, op == OLIVE_OP_GATED_MLP_BWD);
+    case OLIVE_OP_EMBEDDING_BWD: return emb_bwd_ws_bytes(T, d, V);
     case OLIVE_OP_LOGPROB_FWD: return fwd_ws_bytes(T, d);
     case OLIVE_OP_LOSS_BWD:
       if (grad_dtype != OLIVE_DTYPE_BF16 && grad_dtype != OLIVE_DTYPE_F32) return 0;
@@ -1011,6 +1013,140 @@ olive_status olive_grad_clip(const void* const* src, void* const* dst, const int
   st = make_ctx(stream, &c);
   if (st != OLIVE_OK) return st;
   return launch_grad_clip(c, src, dst, numel, dtype, n, max_norm, norm, workspace);
+}
+
+static bool dtype_ok(int dtype) { return dtype == OLIVE_DTYPE_BF16 || dtype == OLIVE_DTYPE_F32; }
+
+olive_status olive_embedding_fwd(const void* W, const int32_t* ids, const int32_t* n_ids, int32_t T,
+                                 int32_t V, int32_t d, float scale, void* out, int dtype,
+                                 int32_t* dev_status, void* stream) {
+  if (!W || !dtype_ok(dtype) || !std::isfinite(scale)) return OLIVE_ERR_INVALID_ARG;
+  if (T < 0 || V < 1 || d < 1 || d > kMaxDim) return OLIVE_ERR_SHAPE;
+  if (T > 0 && (!ids || !out)) return OLIVE_ERR_INVALID_ARG;
+  if (d % 8 != 0 || !aligned16(W) || (T > 0 && !aligned16(out))) return OLIVE_ERR_ALIGNMENT;
+  // (blocks of the look-up's grid)
+  if (ceil_div(static_cast<int64_t>(T) * (d / 8), 256) > INT32_MAX) return OLIVE_ERR_SHAPE;
+  Ctx c;
+  const olive_status st = make_ctx(stream, &c);
+  if (st != OLIVE_OK || T == 0) return st;
+  EmbArgs a = {};
+  a.W = W;
+  a.ids = ids;
+  a.n_ids = n_ids;
+  a.T = T;
+  a.V = V;
+  a.d = d;
+  a.scale = scale;
+  a.out = out;
+  a.dtype = dtype;
+  a.dev_status = dev_status;
+  return launch_emb_fwd(c, a);
+}
+
+olive_status olive_embedding_bwd(const void* dy, const int32_t* ids, const int32_t* n_ids,
+                                 int32_t T, int32_t V, int32_t d, float scale, void* dW, int dtype,
+                                 int grad_dtype, int accumulate, void* workspace, size_t ws_bytes,
+                                 int32_t* dev_status, void* stream) {
+  if (!dW || !dtype_ok(dtype) || !dtype_ok(grad_dtype) || !std::isfinite(scale) ||
+      (accumulate != 0 && accumulate != 1))
+    return OLIVE_ERR_INVALID_ARG;
+  if (T < 0 || V < 1 || d < 1 || d > kMaxDim) return OLIVE_ERR_SHAPE;
+  if (T > 0 && (!ids || !dy)) return OLIVE_ERR_INVALID_ARG;
+  if (d % 8 != 0 || !aligned16(dW) || (T > 0 && !aligned16(dy))) return OLIVE_ERR_ALIGNMENT;
+  olive_status st = OLIVE_OK;
+  if (T > 0) {
+    if (ceil_div(T, 32) * ceil_div(d, 1024) + ceil_div(V, 32) > INT32_MAX) return OLIVE_ERR_SHAPE;
+    st = check_ws(workspace, ws_bytes, emb_bwd_ws_bytes(T, d, V));
+    if (st != OLIVE_OK) return st;
+  }
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK) return st;
+  if (T == 0) {
+    const size_t n = static_cast<size_t>(V) * d * (grad_dtype == OLIVE_DTYPE_BF16 ? 2 : 4);
+    if (!accumulate && cudaMemsetAsync(dW, 0, n, c.stream) != cudaSuccess) {
+      cudaGetLastError();
+      return OLIVE_ERR_CUDA;
+    }
+    return OLIVE_OK;
+  }
+  EmbArgs a = {};
+  a.ids = ids;
+  a.n_ids = n_ids;
+  a.T = T;
+  a.V = V;
+  a.d = d;
+  a.scale = scale;
+  a.dy = dy;
+  a.dW = dW;
+  a.dtype = dtype;
+  a.grad_dtype = grad_dtype;
+  a.accumulate = accumulate;
+  a.dev_status = dev_status;
+  return launch_emb_bwd(c, a, workspace);
+}
+
+olive_status olive_row_norm_fwd(const void* x, const void* residual, const void* w, const void* b,
+                                int32_t T, int32_t d, float eps, int kind, void* y, void* sum,
+                                float* stats, int dtype, void* stream) {
+  if (!w || !dtype_ok(dtype) || (kind != OLIVE_NORM_LAYER && kind != OLIVE_NORM_RMS) ||
+      !(eps >= 0.f) || !std::isfinite(eps) || (residual == nullptr) != (sum == nullptr))
+    return OLIVE_ERR_INVALID_ARG;
+  if (T < 0 || d < 1 || d > kMaxNormDim) return OLIVE_ERR_SHAPE;
+  if (T > 0 && (!x || !y || y == sum)) return OLIVE_ERR_INVALID_ARG;
+  if (d % 8 != 0 || !aligned16(w) || !aligned16(b)) return OLIVE_ERR_ALIGNMENT;
+  if (T > 0 && (!aligned16(x) || !aligned16(residual) || !aligned16(y) || !aligned16(sum)))
+    return OLIVE_ERR_ALIGNMENT;
+  Ctx c;
+  const olive_status st = make_ctx(stream, &c);
+  if (st != OLIVE_OK || T == 0) return st;
+  NormArgs a = {};
+  a.x = x;
+  a.residual = residual;
+  a.w = w;
+  a.b = b;
+  a.y = y;
+  a.sum = sum;
+  a.stats = stats;
+  a.T = T;
+  a.d = d;
+  a.eps = eps;
+  a.kind = kind;
+  a.dtype = dtype;
+  return launch_norm_fwd(c, a);
+}
+
+olive_status olive_row_norm_bwd(const void* dy, const void* h, const void* w, const float* stats,
+                                const void* g_sum, int32_t T, int32_t d, int kind, void* dx,
+                                float* dw, float* db, int dtype, void* workspace, size_t ws_bytes,
+                                void* stream) {
+  if (!w || !dw || !dtype_ok(dtype) || (kind != OLIVE_NORM_LAYER && kind != OLIVE_NORM_RMS))
+    return OLIVE_ERR_INVALID_ARG;
+  if (T < 0 || d < 1 || d > kMaxNormDim) return OLIVE_ERR_SHAPE;
+  if (T > 0 && (!dy || !h || !stats || !dx)) return OLIVE_ERR_INVALID_ARG;
+  if (d % 8 != 0 || !aligned16(w)) return OLIVE_ERR_ALIGNMENT;
+  if (T > 0 && (!aligned16(dy) || !aligned16(h) || !aligned16(g_sum) || !aligned16(dx)))
+    return OLIVE_ERR_ALIGNMENT;
+  olive_status st = check_ws(workspace, ws_bytes, norm_bwd_ws_bytes(d));
+  if (st != OLIVE_OK) return st;
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK) return st;
+  NormArgs a = {};
+  a.x = h;
+  a.w = w;
+  a.stats = const_cast<float*>(stats);
+  a.dy = dy;
+  a.g_sum = g_sum;
+  a.dx = dx;
+  a.dw = dw;
+  a.db = db;
+  a.T = T;
+  a.d = d;
+  a.kind = kind;
+  a.dtype = dtype;
+  a.ws = workspace;
+  return launch_norm_bwd(c, a);
 }
 
 }  // extern "C"
