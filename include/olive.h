@@ -48,6 +48,8 @@
  *   olive_embedding_fwd, olive_embedding_bwd
  *                            rows of the embedding by packed ids, and its
  *                            gradient by sorted tokens
+ *   olive_packed_attention_fwd
+ *                            attention of packed tokens to their own sequence
  *   olive_row_norm_fwd, olive_row_norm_bwd
  *                            layer norm or RMS norm of the rows, with the
  *                            residual's sum on the way
@@ -755,6 +757,38 @@ OLIVE_API olive_status olive_row_norm_bwd(const void* dy, const void* h, const v
                                           int32_t d, int kind, void* dx, float* dw, float* db,
                                           int dtype, void* workspace, size_t ws_bytes,
                                           void* stream);
+
+/*
+ * olive_packed_attention_fwd -- attention of every packed token to tokens of its own
+ * sequence.  Token cu_seqlens[s] + i is row i of sequence s (n_s rows); query head h
+ * goes with key head h / (Hq / Hk).  Row i sees key j < n_s where not `causal` or
+ * j <= i or j < prefix_end[s] - cu_seqlens[s] (int32 [S], e.g. olive_splice_pack's
+ * cut_offsets: prompt and prefix are then seen by all rows; NULL: no such keys):
+ *   s_ij = z_ij, or cap tanh(z_ij / cap) if cap > 0,  with z_ij = scale <q_i, k_j>
+ *          - slopes[h] |i - j|                 (slopes fp32 [Hq], NULL: none)
+ *   lse_i = log sum over seen j of exp(s_ij)                      fp32 [Hq, T]
+ *   o_i = sum over seen j of exp(s_ij - lse_i) v_j                bf16 [T, Hq, D]
+ * Rows behind the last sequence (t >= cu_seqlens[S]) get o = 0, lse = -inf.  q, k, v, o
+ * bf16, D values of a head contiguous; token and head strides as in
+ * olive_qk_norm_rope_fwd, so q, k, v may be views of one projection (the token stride is
+ * not 0 where T > 1).  lse may be NULL.  Scores, maxima and sums are fp32; the weights
+ * exp(s - reference) are rounded to bf16 as operands of the second product (2^-9
+ * relative each).  A value that is not finite in a row of k or v reaches rows of its own
+ * sequence only (it may reach earlier ones of its 128-row tile).
+ *   D a multiple of 8, 8 <= D <= 128; Hq a multiple of Hk, 1 <= Hk <= Hq <= 4096;
+ *   S >= 1; 0 <= T <= 2^30; scale > 0; cap >= 0; strides multiples of 8, base pointers
+ *   16-byte aligned; the heads of o must not share memory, nor with q, k, v.
+ * Device errors (dev_status may be NULL): OFFSETS (cu_seqlens does not begin with 0,
+ * falls, or exceeds T: rows of the sequences concerned are then undefined, nothing
+ * outside the arrays is touched), TIMEOUT.
+ */
+OLIVE_API olive_status olive_packed_attention_fwd(
+    const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k,
+    int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+    int64_t v_head_stride, int32_t Hq, int32_t Hk, const int32_t* cu_seqlens, int32_t S, int32_t T,
+    int32_t D, float scale, int causal, const int32_t* prefix_end, float cap, const float* slopes,
+    void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse, int32_t* dev_status,
+    void* stream);
 
 #ifdef __cplusplus
 }

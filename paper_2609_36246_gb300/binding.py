@@ -150,6 +150,9 @@ def _configure(L: ctypes.CDLL) -> ctypes.CDLL:
     L.olive_embedding_bwd.restype = ctypes.c_int
     L.olive_embedding_bwd.argtypes = [_P, _P, _P, _I, _I, _I, _F, _P, ctypes.c_int, ctypes.c_int,
                                       ctypes.c_int, _P, _S, _P, _P]
+    att = [_I, _I, _P, _I, _I, _I, _F, ctypes.c_int, _P, _F, _P]
+    L.olive_packed_attention_fwd.restype = ctypes.c_int
+    L.olive_packed_attention_fwd.argtypes = view * 3 + att + view + [_P, _P, _P]
     L.olive_row_norm_fwd.restype = ctypes.c_int
     L.olive_row_norm_fwd.argtypes = [_P, _P, _P, _P, _I, _I, _F, ctypes.c_int, _P, _P, _P,
                                      ctypes.c_int, _P]
@@ -1055,6 +1058,61 @@ def olive_row_norm_bwd(dy, h, w, stats, g_h=None, kind: str = "layer", need_db: 
     if st:
         _check(st, "olive_row_norm_bwd")
     return dx, dw, db
+
+
+def _att_args(q, k, v, cu_seqlens, scale, causal, prefix_end, cap, slopes):
+    """Checks what the attention's forward and backward share; (views of q, k and v, the
+    shared C arguments, their shapes, device and its index)."""
+    if (not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or not q.is_cuda or
+            q.dtype is not _BF16 or q.dim() != 3 or k.dim() != 3):
+        raise TypeError("q and k must be CUDA bf16 tensors [T, heads, D]")
+    cur = _current()
+    sq, sk = q.shape, k.shape
+    T, Hq, D = sq
+    Hk = sk[1]
+    if sk[0] != T or sk[2] != D:
+        raise ValueError(f"k must have the shape [{T}, heads, {D}]")
+    vq, vk, vv = _heads(q, sq, _BF16, "q", cur), _heads(k, sk, _BF16, "k", cur), _heads(v, sk, _BF16, "v", cur)
+    _need_on(cur, cu_seqlens, _I32, "cu_seqlens")
+    S = cu_seqlens.numel() - 1
+    if prefix_end is not None:
+        _need_on(cur, prefix_end, _I32, "prefix_end")
+        if prefix_end.numel() != S:
+            raise ValueError(f"prefix_end must hold {S} values")
+    if slopes is not None:
+        _need_on(cur, slopes, _F32, "slopes")
+        if slopes.numel() != Hq:
+            raise ValueError(f"slopes must hold {Hq} values")
+    common = (Hq, Hk, cu_seqlens.data_ptr(), S, T, D, D ** -0.5 if scale is None else scale,
+              1 if causal else 0, _ptr(prefix_end), cap, _ptr(slopes))
+    return vq, vk, vv, common, sq, sk, q.device, cur
+
+
+def _att_out(out, shape, name, dev, cur):
+    """An output and its view: a contiguous one where none is given."""
+    if out is None:
+        out = torch.empty(shape, dtype=_BF16, device=dev)
+        return out, (out.data_ptr(), shape[1] * shape[2], shape[2])
+    return out, _heads(out, shape, _BF16, name, cur)
+
+
+def olive_packed_attention_fwd(q, k, v, cu_seqlens, scale=None, causal: bool = True, prefix_end=None,
+                               cap: float = 0.0, slopes=None, dev_status=None, out=None):
+    """Attention of packed tokens to their own sequence: q [T, Hq, D], k and v
+    [T, Hk, D] (bf16; views will do), cu_seqlens int32 [S + 1].  scale is
+    1 / sqrt(D) unless given; prefix_end (int32 [S], packed indices) ends what all
+    rows of a sequence see; cap > 0 bends the scores by a tanh, slopes (fp32 [Hq])
+    lower them with the distance.  Returns (o [T, Hq, D], lse fp32 [Hq, T]); rows
+    behind the last sequence get 0 and -inf."""
+    vq, vk, vv, common, sq, _, dev, cur = _att_args(q, k, v, cu_seqlens, scale, causal, prefix_end, cap, slopes)
+    o, vo = _att_out(out, sq, "out", dev, cur)
+    _need_given(cur, None, dev_status)
+    lse = torch.empty((sq[1], sq[0]), dtype=_F32, device=dev)
+    st = lib().olive_packed_attention_fwd(*vq, *vk, *vv, *common, *vo, lse.data_ptr(), _ptr(dev_status),
+                                          _stream_of(cur))
+    if st:
+        _check(st, "olive_packed_attention_fwd")
+    return o, lse
 
 
 class FusedLMHeadCE(torch.autograd.Function):

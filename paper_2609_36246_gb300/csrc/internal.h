@@ -480,4 +480,25 @@ size_t emb_bwd_ws_bytes(int64_t T, int64_t d, int64_t V);
 olive_status launch_emb_fwd(const Ctx& c, const EmbArgs& a);
 olive_status launch_emb_bwd(const Ctx& c, const EmbArgs& a, void* ws);
 
+// ---- attention inside packed sequences (packed_attention.cu, packed_attention_bwd.cu) ----
+struct AttArgs {
+  HeadsView q, k, v, o;            // o: written by the forward
+  HeadsView d_o, dq, dk, dv;       // backward
+  float* lse;                      // [Hq, T], NULL: not written
+  const int32_t *cu, *prefix_end;  // [S + 1]; [S] or NULL
+  const float* slopes;             // [Hq] or NULL
+  int32_t Hq, Hk, S, T, D;
+  float scale, cap;                // cap 0: none
+  int causal;
+  uint64_t wait_limit_ns;
+  int32_t* dev_status;
+  void* ws;
+};
+constexpr int kMaxAttDim = 128;
+size_t att_bwd_ws_bytes(int64_t T, int64_t Hq, int64_t S);
+olive_status launch_att_fwd(const Ctx& c, const AttArgs& a);
+olive_status launch_att_bwd(const Ctx& c, const AttArgs& a);
+// A 3-D bf16 tensor map of a view [T, heads, D] whose boxes are 128 tokens of one head's 64 values.
+bool encode_heads(CUtensorMap* map, const HeadsView& x, int32_t T, int32_t heads, int32_t D);
+
 }  // namespace olive

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cstdlib>
 #include <mutex>
+#include <tuple>
 
 #include "internal.h"
 
@@ -107,6 +108,22 @@ bool encode_bf16_2d_plain(CUtensorMap* map, const void* base, uint64_t inner, ui
                           uint64_t row_bytes, uint32_t box_inner, uint32_t box_outer) {
   return encode_bf16_2d_swz(map, base, inner, outer, row_bytes, box_inner, box_outer,
                             CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+bool encode_heads(CUtensorMap* map, const HeadsView& x, int32_t T, int32_t heads, int32_t D) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  // (heads that share memory are one; the stride of a dimension of one entry means nothing)
+  const bool one = heads == 1 || x.head_stride == 0;
+  const cuuint64_t head = one ? 2ull * kMaxAttDim : 2ull * x.head_stride;
+  const cuuint64_t token = T == 1 ? 2ull * kMaxAttDim : 2ull * x.token_stride;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), one ? 1ull : heads, static_cast<cuuint64_t>(T)};
+  cuuint64_t strides[2] = {head, token};
+  cuuint32_t box[3] = {64, 1, 128};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x.x), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 int64_t slab_rows(int64_t Tpad, int64_t V) {
@@ -383,6 +400,9 @@ olive_status check_ws(void* ws, size_t have, size_t need) {
 constexpr int32_t kMaxHeadDim = 256;
 constexpr int32_t kMaxHeads = 4096;
 constexpr int32_t kMaxMlpRows = 1 << 30;  // row indices of its last tile stay in 31 bits
+
+constexpr int32_t kMaxAttTokens = 1 << 30;
+constexpr int64_t kMaxAttStride = 1ll << 38;  // a tensor map's strides are below 2^40 bytes
 
 bool width_ok(int32_t d) { return d >= 8 && d <= kMaxDim && (d % 8) == 0; }
 
@@ -1147,6 +1167,66 @@ olive_status olive_row_norm_bwd(const void* dy, const void* h, const void* w, co
   a.dtype = dtype;
   a.ws = workspace;
   return launch_norm_bwd(c, a);
+}
+
+// The checks that the attention's forward and backward share.
+static olive_status check_att(const AttArgs& a) {
+  if (!a.cu || (a.causal != 0 && a.causal != 1) || !(a.scale > 0.f) || !std::isfinite(a.scale) || !(a.cap >= 0.f) ||
+      !std::isfinite(a.cap))
+    return OLIVE_ERR_INVALID_ARG;
+  if (a.T < 0 || a.T > kMaxAttTokens || a.S < 1 || a.S > kMaxAttTokens || a.D < 8 || a.D > kMaxAttDim || a.Hk < 1 ||
+      a.Hq < a.Hk || a.Hq > kMaxHeads || a.Hq % a.Hk != 0)
+    return OLIVE_ERR_SHAPE;
+  return a.D % 8 != 0 ? OLIVE_ERR_ALIGNMENT : OLIVE_OK;
+}
+// A view [T, heads, D] of the attention's; `written`: its heads must not share memory.
+static olive_status check_att_view(const HeadsView& v, int64_t heads, const AttArgs& a, bool written) {
+  if (!v.x) return OLIVE_ERR_INVALID_ARG;
+  if (!aligned16(v.x) || v.token_stride % 8 != 0 || v.head_stride % 8 != 0) return OLIVE_ERR_ALIGNMENT;
+  if (v.token_stride < 0 || v.head_stride < 0 || (a.T > 1 && v.token_stride == 0) || v.token_stride > kMaxAttStride ||
+      v.head_stride > kMaxAttStride || (written && heads_overlap(v, heads, a.T, a.D)))
+    return OLIVE_ERR_SHAPE;
+  return OLIVE_OK;
+}
+
+olive_status olive_packed_attention_fwd(
+    const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k,
+    int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+    int64_t v_head_stride, int32_t Hq, int32_t Hk, const int32_t* cu_seqlens, int32_t S, int32_t T,
+    int32_t D, float scale, int causal, const int32_t* prefix_end, float cap, const float* slopes,
+    void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse, int32_t* dev_status,
+    void* stream) {
+  AttArgs a = {};
+  a.q = {q, q_token_stride, q_head_stride};
+  a.k = {k, k_token_stride, k_head_stride};
+  a.v = {v, v_token_stride, v_head_stride};
+  a.o = {o, o_token_stride, o_head_stride};
+  a.lse = lse;
+  a.cu = cu_seqlens;
+  a.prefix_end = prefix_end;
+  a.slopes = slopes;
+  a.Hq = Hq;
+  a.Hk = Hk;
+  a.S = S;
+  a.T = T;
+  a.D = D;
+  a.scale = scale;
+  a.cap = cap;
+  a.causal = causal;
+  a.dev_status = dev_status;
+  olive_status st = check_att(a);
+  if (st != OLIVE_OK) return st;
+  if (T > 0)
+    for (const auto& [view, heads, written] : {std::tuple<const HeadsView&, int32_t, bool>{a.q, Hq, false},
+                                               {a.k, Hk, false}, {a.v, Hk, false}, {a.o, Hq, true}}) {
+      st = check_att_view(view, heads, a, written);
+      if (st != OLIVE_OK) return st;
+    }
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK || T == 0) return st;
+  a.wait_limit_ns = c.wait_limit_ns;
+  return launch_att_fwd(c, a);
 }
 
 }  // extern "C"

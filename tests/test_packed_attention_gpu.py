@@ -1,0 +1,233 @@
+"""Attention inside packed sequences against the definition in 64 bits.
+
+Tolerances.  A score is a sum of up to 128 exact products in fp32: off by at most 2^-16 of A, the
+largest sum of the magnitudes of a row's products (times the scale), whatever the order; the bias and
+the cap add 2^-22 of their size each, and an exponential is off by its argument's error.  The weights
+are rounded to bf16, 2^-8 of each, so an output is within (2^-8 + 2^-15 (A + B)) of the sum of its
+terms' magnitudes, and its own rounding, 2^-8 of it.
+"""
+
+import math
+
+import pytest
+import torch
+
+from paper_2609_36246_gb300 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+STEP = 2.0 ** -8 * 1.01
+
+
+def _case(lens, hq, hk, D, pad=0, prefix=None, cap=0.0, bias=False, causal=True, seed=0, sharp=1.0, scale=None):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    T = sum(lens) + pad
+    qkv = (r(T, hq + 2 * hk, D) * sharp).to(BF16)
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    s = dict(q=qkv[:, :hq], k=qkv[:, hq:hq + hk], v=qkv[:, hq + hk:], do=r(T, hq, D).to(BF16), lens=lens,
+             cu=torch.tensor(cu, dtype=torch.int32, device="cuda"),
+             more=dict(causal=causal, cap=cap, scale=scale, prefix_end=None, slopes=None))
+    if prefix is not None:
+        ends = [a + min(n, prefix) for a, n in zip(cu, lens)]
+        s["more"]["prefix_end"] = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    if bias:
+        s["more"]["slopes"] = 0.3 * 2.0 ** -torch.arange(hq, device="cuda", dtype=torch.float32)
+    return s
+
+
+def _seen(s, T):
+    """Which key each row sees [T, T], and the rows' distances."""
+    cu = s["cu"].long()
+    t = torch.arange(T, device="cuda")
+    seq = torch.bucketize(t, cu[1:], right=True)
+    live = t < cu[-1]
+    seen = (seq[:, None] == seq[None]) & live[:, None] & live[None]
+    if s["more"]["causal"]:
+        ok = t[None] <= t[:, None]
+        end = s["more"]["prefix_end"]
+        if end is not None:
+            ok = ok | (t[None] < end.long()[seq.clamp(max=end.numel() - 1)][:, None])
+        seen = seen & ok
+    return seen, (t[:, None] - t[None]).abs().double()
+
+
+def _reference(s, grads=False):
+    """o and lse, gradients, and what bounds the errors, head by head."""
+    q, k, v = s["q"], s["k"], s["v"]
+    T, hq, D = q.shape
+    per = hq // k.shape[1]
+    m = s["more"]
+    scale = m["scale"] or D ** -0.5
+    seen, far = _seen(s, T)
+    out = {n: torch.zeros(x.shape, dtype=torch.float64, device="cuda") for n, x in
+           (("o", q), ("tol_o", q), ("dq", q), ("dk", k), ("dv", v), ("tol_dq", q), ("tol_dk", k), ("tol_dv", v))}
+    out["lse"] = torch.full((hq, T), -math.inf, dtype=torch.float64, device="cuda")
+    out["tol_lse"] = torch.zeros((hq, T), dtype=torch.float64, device="cuda")
+    for h in range(hq):
+        Q, K, V = q[:, h].double(), k[:, h // per].double(), v[:, h // per].double()
+        z = scale * Q @ K.t()
+        size = scale * Q.abs() @ K.abs().t()
+        bend = torch.ones_like(z)
+        err = 2.0 ** -16 * size
+        if m["cap"]:
+            t = torch.tanh(z / m["cap"])
+            z, bend = m["cap"] * t, 1 - t * t
+            err = err + 2.0 ** -20 * m["cap"]
+        if m["slopes"] is not None:
+            z = z - m["slopes"][h].double() * far
+            err = err + 2.0 ** -22 * m["slopes"][h].double() * far
+        err = (err * seen).amax(-1, keepdim=True) + 2.0 ** -20
+        z = z.masked_fill(~seen, -math.inf)
+        lse = torch.logsumexp(z, -1)
+        p = torch.where(seen, (z - lse[:, None]).exp(), 0.0)
+        o = p @ V
+        out["o"][:, h], out["lse"][h] = o, lse
+        out["tol_o"][:, h] = (STEP + 2 * err) * (p @ V.abs()) + STEP * o.abs()
+        out["tol_lse"][h] = err[:, 0] + 2.0 ** -21 * (1 + torch.where(seen.any(-1), lse.abs(), 0.0))
+        if not grads:
+            continue
+        dO = s["do"][:, h].double()
+        dp = torch.where(seen, dO @ V.t(), 0.0)
+        delta = (p * dp).sum(-1, keepdim=True)
+        ds = p * (dp - delta) * bend
+        # errors: of p (err), of dp's fp32 sum, of delta (from o as it is stored, but for rows of few
+        # keys), of the operands' rounding to bf16
+        e_dp = 2.0 ** -16 * (dO.abs() @ V.abs().t())
+        e_delta = (STEP + 2 * err) * (dO.abs() * (p @ V.abs())).sum(-1, keepdim=True) + STEP * (dO.abs() * o.abs()).sum(-1, keepdim=True)
+        e_ds = p * (e_dp + e_delta) + (2 * err + STEP + 2.0 ** -20) * p * (dp.abs() + delta.abs()) + STEP * ds.abs()
+        e_p = (STEP + 2 * err) * p
+        out["dq"][:, h] = scale * ds @ K
+        out["tol_dq"][:, h] = scale * e_ds @ K.abs() + STEP * out["dq"][:, h].abs()
+        out["dk"][:, h // per] += scale * ds.t() @ Q
+        out["tol_dk"][:, h // per] += scale * e_ds.t() @ Q.abs()
+        out["dv"][:, h // per] += p.t() @ dO
+        out["tol_dv"][:, h // per] += e_p.t() @ dO.abs()
+    for n in ("dk", "dv"):
+        out["tol_" + n] += STEP * out[n].abs()
+    return out
+
+
+def _near(got, ref, name):
+    want, tol = ref[name], ref["tol_" + name]
+    fine = torch.isfinite(want)
+    assert got.shape == want.shape and torch.equal(torch.isfinite(got), fine), name
+    over = ((got.double() - want).abs() - tol)[fine]
+    assert not over.numel() or float(over.max()) <= 0, (name, float(over.max()), float((got.double() - want).abs()[fine].max()))
+
+
+def _forward(s):
+    st = B.new_status()
+    o, lse = B.olive_packed_attention_fwd(s["q"], s["k"], s["v"], s["cu"], **s["more"], dev_status=st)
+    assert B.status_bits(st) == []
+    return o, lse
+
+
+def _check(s):
+    ref = _reference(s)
+    o, lse = _forward(s)
+    _near(o, ref, "o")
+    _near(lse, ref, "lse")
+    behind = int(s["cu"][-1])
+    assert not o[behind:].any() and bool((lse[:, behind:] == -math.inf).all())
+    return o, lse
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 100, 127, 128, 129, 255, 256, 257, 300, 513, 1000])
+@pytest.mark.parametrize("hq,hk,D", [(2, 1, 128), (3, 1, 64)])
+def test_lengths(n, hq, hk, D):
+    _check(_case([n], hq, hk, D, seed=n))
+
+
+@pytest.mark.parametrize("D", [8, 16, 24, 32, 56, 64, 72, 80, 96, 104, 120, 128])
+@pytest.mark.parametrize("hq,hk", [(1, 1), (4, 2)])
+def test_widths(D, hq, hk):
+    _check(_case([77, 200], hq, hk, D, seed=D))
+
+
+@pytest.mark.parametrize("hq,hk", [(1, 1), (2, 2), (2, 1), (8, 2), (5, 1), (9, 3), (12, 12), (40, 8)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_heads(hq, hk, causal):
+    _check(_case([130, 7, 300], hq, hk, 64, causal=causal, seed=hq))
+
+
+FORMS = [dict(), dict(causal=False), dict(prefix=50), dict(prefix=0), dict(prefix=1), dict(prefix=200), dict(cap=5.0), dict(bias=True),
+         dict(cap=2.0, bias=True, prefix=140), dict(causal=False, bias=True), dict(scale=0.7), dict(sharp=4.0), dict(sharp=4.0, cap=30.0)]
+
+
+@pytest.mark.parametrize("form", FORMS, ids=str)
+@pytest.mark.parametrize("hq,hk,D", [(4, 2, 128), (3, 3, 40)])
+def test_forms(form, hq, hk, D):
+    _check(_case([1, 300, 129, 0, 17, 128, 2, 400], hq, hk, D, pad=33, **form))
+
+
+def test_many_sequences():
+    """More than a warp looks for at once, empty and single ones among them."""
+    gen = torch.Generator().manual_seed(0)
+    lens = torch.randint(0, 5, (1200,), generator=gen).tolist()
+    lens[700] = 150
+    _check(_case(lens, 2, 1, 32))
+    _check(_case(lens, 3, 1, 32, causal=False, pad=5))
+
+
+def test_largest_scores_late():
+    """Each tile's keys outweigh those before them: the reference has to follow."""
+    s = _case([700], 2, 1, 64)
+    by = torch.linspace(0.2, 12, 700, device="cuda")[:, None, None]
+    s["k"].copy_((s["q"][:, :1].float().mean(0, keepdim=True) * 0 + 1) * by.to(BF16))
+    s["q"].copy_(s["q"].abs())
+    _check(s)
+
+
+def test_what_is_not_finite():
+    """A bad token behind a sequence's end, or in another one, does not show; its own sequence's does."""
+    s = _case([100, 77, 60], 4, 2, 64, pad=20)
+    good, lse = _forward(s)
+    for n in ("q", "k", "v"):
+        s[n][100 + 77:] = float("nan")  # the last sequence, and nobody's rows
+    o, lse2 = _forward(s)
+    assert torch.equal(o[:177], good[:177]) and torch.equal(lse2[:, :177], lse[:, :177])
+    assert torch.isnan(o[177:237]).all() and not o[237:].any()
+
+
+def test_layouts():
+    """The same values in other layouts give the same bits."""
+    s = _case([200, 61], 4, 2, 80, pad=3)
+    want = _forward(s)
+    for lay in ("heads first", "wide"):
+        def relaid(t):
+            if lay == "heads first":
+                return t.transpose(0, 1).contiguous().transpose(0, 1)
+            wide = torch.full((t.shape[0], t.shape[1] + 3, t.shape[2] + 16), float("nan"), dtype=BF16, device="cuda")
+            wide[:, 1:-2, 8:-8] = t
+            return wide[:, 1:-2, 8:-8]
+        out = relaid(torch.zeros_like(want[0]))
+        o, lse = B.olive_packed_attention_fwd(*(relaid(s[n]) for n in "qkv"), s["cu"], **s["more"], out=out)
+        assert o is out and torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    # key heads that share memory
+    one = s["k"][:, :1].contiguous()
+    o, lse = B.olive_packed_attention_fwd(s["q"], one.expand(-1, 2, -1), one.expand(-1, 2, -1), s["cu"], **s["more"])
+    both = one.repeat(1, 2, 1)
+    o2, lse2 = B.olive_packed_attention_fwd(s["q"], both, both, s["cu"], **s["more"])
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("cu", [[0, 50, 40, 90], [0, 200], [5, 50], [-3, 60], [0, 2**31 - 1], [70, 20]])
+def test_offsets_that_do_not_describe_the_batch(cu):
+    s = _case([100], 2, 1, 64)
+    st = B.new_status()
+    bad = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    B.olive_packed_attention_fwd(s["q"], s["k"], s["v"], bad, dev_status=st)
+    B.olive_packed_attention_fwd(s["q"], s["k"], s["v"], bad)
+    assert B.status_bits(st) == ["OLIVE_ERR_OFFSETS"]
+
+
+def test_no_tokens():
+    s = _case([1], 2, 1, 64)
+    o, lse = B.olive_packed_attention_fwd(s["q"][:0], s["k"][:0], s["v"][:0], torch.zeros(2, dtype=torch.int32, device="cuda"))
+    assert o.shape == (0, 2, 64) and lse.shape == (2, 0)
+    s = _case([0, 0], 2, 1, 64, pad=10)
+    _check(s)
