@@ -48,7 +48,7 @@
  *   olive_embedding_fwd, olive_embedding_bwd
  *                            rows of the embedding by packed ids, and its
  *                            gradient by sorted tokens
- *   olive_packed_attention_fwd
+ *   olive_packed_attention_fwd, olive_packed_attention_bwd
  *                            attention of packed tokens to their own sequence
  *   olive_row_norm_fwd, olive_row_norm_bwd
  *                            layer norm or RMS norm of the rows, with the
@@ -129,7 +129,8 @@ enum { OLIVE_OP_LOGPROB_FWD = 0, OLIVE_OP_LOSS_BWD = 1, OLIVE_OP_DIVERGENCE = 2,
        OLIVE_OP_LOSS_FWD_BWD = 6, OLIVE_OP_OPD_STATS = 7, OLIVE_OP_TOPK_KL_FWD_BWD = 8,
        OLIVE_OP_LOSS_FWD_BWD_SLAB = 9, OLIVE_OP_GATED_MLP_FWD = 10,
        OLIVE_OP_GATED_MLP_BWD = 11, OLIVE_OP_QK_NORM_ROPE_BWD = 12, OLIVE_OP_GRAD_CLIP = 13,
-       OLIVE_OP_ROW_NORM_BWD = 14, OLIVE_OP_EMBEDDING_BWD = 15 };
+       OLIVE_OP_ROW_NORM_BWD = 14, OLIVE_OP_EMBEDDING_BWD = 15,
+       OLIVE_OP_PACKED_ATTENTION_BWD = 16 };
 
 /*
  * Rows of the G slab that the slab forms (olive_token_loss_fwd_bwd_slab,
@@ -167,6 +168,7 @@ OLIVE_API olive_status olive_status_clear(int32_t* dev_status, void* stream);
  *   op  OLIVE_OP_GRAD_CLIP: T = number of tensors; the rest ignored.
  *   op  OLIVE_OP_ROW_NORM_BWD: d = width; the rest ignored.
  *   op  OLIVE_OP_EMBEDDING_BWD: T, d = width, V; the rest ignored.
+ *   op  OLIVE_OP_PACKED_ATTENTION_BWD: T, V = query heads; the rest ignored.
  *   `grad` (bwd / divergence): non-zero when gradients are requested
  *   (OLIVE_OP_LOSS_BWD always computes them); `grad_dtype` is the dtype of
  *   d_W for OLIVE_OP_LOSS_BWD (bf16 output needs an fp32 accumulator).
@@ -789,6 +791,30 @@ OLIVE_API olive_status olive_packed_attention_fwd(
     int32_t D, float scale, int causal, const int32_t* prefix_end, float cap, const float* slopes,
     void* o, int64_t o_token_stride, int64_t o_head_stride, float* lse, int32_t* dev_status,
     void* stream);
+
+/*
+ * olive_packed_attention_bwd -- gradients of olive_packed_attention_fwd for its inputs,
+ * its outputs o and lse, and the gradient d_o of o (lse's is taken as 0): with p_ij =
+ * exp(s_ij - lse_i) and delta_i = <d_o_i, o_i> (for rows that see up to 16 keys the sum
+ * over them of p_ij <d_o_i, v_j>, which o's rounding does not enter),
+ *   dv_j = sum p_ij d_o_i,   dz_ij = p_ij (<d_o_i, v_j> - delta_i) (1 - (t_ij)^2),
+ *   dq_i = scale sum dz_ij k_j,   dk_j = scale sum dz_ij q_i
+ * t_ij = tanh(z_ij / cap), 0 without a cap; dk and dv summed over the query heads of a
+ * key head.  p and dz are rounded to bf16 as operands, sums are fp32 in a fixed order.
+ * Rows behind the last sequence get 0.  All views bf16 with strides of their own, as in
+ * the forward; the heads of dq, dk and dv must not share memory, nor those with the inputs.
+ * workspace: olive_workspace_size(OLIVE_OP_PACKED_ATTENTION_BWD, T, 0, 0, Hq, 0, 0) bytes.
+ */
+OLIVE_API olive_status olive_packed_attention_bwd(
+    const void* d_o, int64_t d_o_token_stride, int64_t d_o_head_stride, const void* q,
+    int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+    int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+    const void* o, int64_t o_token_stride, int64_t o_head_stride, const float* lse, int32_t Hq,
+    int32_t Hk, const int32_t* cu_seqlens, int32_t S, int32_t T, int32_t D, float scale, int causal,
+    const int32_t* prefix_end, float cap, const float* slopes, void* dq, int64_t dq_token_stride,
+    int64_t dq_head_stride, void* dk, int64_t dk_token_stride, int64_t dk_head_stride, void* dv,
+    int64_t dv_token_stride, int64_t dv_head_stride, void* workspace, size_t ws_bytes,
+    int32_t* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

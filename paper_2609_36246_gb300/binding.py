@@ -35,7 +35,8 @@ DTYPE = {torch.bfloat16: 0, torch.float32: 1}
 OP = {"logprob_fwd": 0, "loss_bwd": 1, "divergence": 2, "topk_fwd": 3, "splice_masked": 4,
       "topk_kl_bwd": 5, "loss_fwd_bwd": 6, "opd_stats": 7, "topk_kl_fwd_bwd": 8,
       "loss_fwd_bwd_slab": 9, "gated_mlp_fwd": 10, "gated_mlp_bwd": 11, "qk_norm_rope_bwd": 12,
-      "grad_clip": 13, "row_norm_bwd": 14, "embedding_bwd": 15}
+      "grad_clip": 13, "row_norm_bwd": 14, "embedding_bwd": 15,
+      "packed_attention_bwd": 16}
 ACT = {"silu": 0, "gelu_tanh": 1}
 NORM = {"layer": 0, "rms": 1}
 
@@ -153,6 +154,8 @@ def _configure(L: ctypes.CDLL) -> ctypes.CDLL:
     att = [_I, _I, _P, _I, _I, _I, _F, ctypes.c_int, _P, _F, _P]
     L.olive_packed_attention_fwd.restype = ctypes.c_int
     L.olive_packed_attention_fwd.argtypes = view * 3 + att + view + [_P, _P, _P]
+    L.olive_packed_attention_bwd.restype = ctypes.c_int
+    L.olive_packed_attention_bwd.argtypes = view * 5 + [_P] + att + view * 3 + [_P, _S, _P, _P]
     L.olive_row_norm_fwd.restype = ctypes.c_int
     L.olive_row_norm_fwd.argtypes = [_P, _P, _P, _P, _I, _I, _F, ctypes.c_int, _P, _P, _P,
                                      ctypes.c_int, _P]
@@ -1115,6 +1118,30 @@ def olive_packed_attention_fwd(q, k, v, cu_seqlens, scale=None, causal: bool = T
     return o, lse
 
 
+def olive_packed_attention_bwd(d_o, q, k, v, o, lse, cu_seqlens, scale=None, causal: bool = True,
+                               prefix_end=None, cap: float = 0.0, slopes=None, ws=None, dev_status=None,
+                               out=None):
+    """Gradients (dq, dk, dv) of olive_packed_attention_fwd for its outputs o and lse
+    and the gradient d_o of o; `out` takes them, e.g. views of one projection's
+    gradient."""
+    vq, vk, vv, common, sq, sk, dev, cur = _att_args(q, k, v, cu_seqlens, scale, causal, prefix_end, cap, slopes)
+    vg, vo = _heads(d_o, sq, _BF16, "d_o", cur), _heads(o, sq, _BF16, "o", cur)
+    _need_on(cur, lse, _F32, "lse")
+    if lse.shape != (sq[1], sq[0]):
+        raise ValueError(f"lse must have the shape [{sq[1]}, {sq[0]}]")
+    dq, dk, dv = (None, None, None) if out is None else out
+    (dq, oq), (dk, ok), (dv, ov) = (_att_out(t, s, n, dev, cur) for t, s, n in
+                                    ((dq, sq, "dq"), (dk, sk, "dk"), (dv, sk, "dv")))
+    _need_given(cur, ws, dev_status)
+    if ws is None:
+        ws = _bytes(_ws_bytes(16, sq[0], 0, sq[1], 0, 0), dev)
+    st = lib().olive_packed_attention_bwd(*vg, *vq, *vk, *vv, *vo, lse.data_ptr(), *common, *oq, *ok, *ov,
+                                          ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream_of(cur))
+    if st:
+        _check(st, "olive_packed_attention_bwd")
+    return dq, dk, dv
+
+
 class FusedLMHeadCE(torch.autograd.Function):
     """Eq. (osd-ce) loss over the masked rows as an autograd op (gradients in
     the dtype of hidden; first derivatives only).  A status word given is the
@@ -1303,6 +1330,38 @@ def row_norm(x, w, b=None, residual=None, eps=1e-6, kind="rms"):
         y, h, _ = olive_row_norm_fwd(x, w, b, residual, eps, kind)
         return y if residual is None else (y, h)
     return RowNorm.apply(x, w, b, residual, eps, kind)
+
+
+class PackedAttention(torch.autograd.Function):
+    """Attention inside packed sequences as an autograd op (first derivatives only; none
+    for the distance bias).  A status word given is the forward's and the backward's."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, cu_seqlens, scale=None, causal=True, prefix_end=None, cap=0.0, slopes=None,
+                dev_status=None):
+        o, lse = olive_packed_attention_fwd(q, k, v, cu_seqlens, scale, causal, prefix_end, cap, slopes, dev_status)
+        more = [t for t in (prefix_end, slopes) if t is not None]
+        ctx.save_for_backward(q, k, v, o, lse, cu_seqlens, *more)
+        ctx.given = (prefix_end is not None, slopes is not None)
+        ctx.form, ctx.dev_status = (scale, causal, cap), dev_status
+        return o
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_o):
+        q, k, v, o, lse, cu, *more = ctx.saved_tensors
+        scale, causal, cap = ctx.form
+        prefix_end, slopes = (more.pop(0) if there else None for there in ctx.given)
+        if d_o.shape[0] > 1 and d_o.stride(0) == 0:  # (one row for all tokens)
+            d_o = d_o.clone(memory_format=torch.contiguous_format)
+        dq, dk, dv = olive_packed_attention_bwd(_heads_gradient(d_o), q, k, v, o, lse, cu, scale, causal, prefix_end,
+                                                cap, slopes, dev_status=ctx.dev_status)
+        return (dq, dk, dv, *[None] * 7)
+
+
+def packed_attention(q, k, v, cu_seqlens, scale=None, causal=True, prefix_end=None, cap=0.0, slopes=None,
+                     dev_status=None):
+    return PackedAttention.apply(q, k, v, cu_seqlens, scale, causal, prefix_end, cap, slopes, dev_status)
 
 
 def _in_memory_order(g):

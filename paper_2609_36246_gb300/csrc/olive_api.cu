@@ -444,6 +444,8 @@ olive_status olive_status_clear(int32_t* dev_status, void* stream) {
 size_t olive_workspace_size(int op, int32_t T, int32_t d, int32_t d_t, int32_t V, int grad,
                             int grad_dtype) {
   if (op == OLIVE_OP_SPLICE_MASKED) return T < 1 ? 0 : splice_masked_ws_bytes(T);
+  if (op == OLIVE_OP_PACKED_ATTENTION_BWD)
+    return T < 1 || T > kMaxAttTokens || V < 1 || V > kMaxHeads ? 0 : att_bwd_ws_bytes(T, V);
   if (op == OLIVE_OP_ROW_NORM_BWD) return width_ok(d) && d <= kMaxNormDim ? norm_bwd_ws_bytes(d) : 0;
   if (op == OLIVE_OP_QK_NORM_ROPE_BWD) return width_ok(d) && d <= kMaxHeadDim ? qk_bwd_ws_bytes(d) : 0;
   if (op == OLIVE_OP_GRAD_CLIP) return T < 1 ? 0 : grad_clip_ws_bytes(T);
@@ -1177,6 +1179,8 @@ static olive_status check_att(const AttArgs& a) {
   if (a.T < 0 || a.T > kMaxAttTokens || a.S < 1 || a.S > kMaxAttTokens || a.D < 8 || a.D > kMaxAttDim || a.Hk < 1 ||
       a.Hq < a.Hk || a.Hq > kMaxHeads || a.Hq % a.Hk != 0)
     return OLIVE_ERR_SHAPE;
+  // (blocks of the backward's first launch)
+  if ((a.T / 128 + static_cast<int64_t>(a.S)) * a.Hq > INT32_MAX) return OLIVE_ERR_SHAPE;
   return a.D % 8 != 0 ? OLIVE_ERR_ALIGNMENT : OLIVE_OK;
 }
 // A view [T, heads, D] of the attention's; `written`: its heads must not share memory.
@@ -1227,6 +1231,59 @@ olive_status olive_packed_attention_fwd(
   if (st != OLIVE_OK || T == 0) return st;
   a.wait_limit_ns = c.wait_limit_ns;
   return launch_att_fwd(c, a);
+}
+
+olive_status olive_packed_attention_bwd(
+    const void* d_o, int64_t d_o_token_stride, int64_t d_o_head_stride, const void* q,
+    int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+    int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+    const void* o, int64_t o_token_stride, int64_t o_head_stride, const float* lse, int32_t Hq,
+    int32_t Hk, const int32_t* cu_seqlens, int32_t S, int32_t T, int32_t D, float scale, int causal,
+    const int32_t* prefix_end, float cap, const float* slopes, void* dq, int64_t dq_token_stride,
+    int64_t dq_head_stride, void* dk, int64_t dk_token_stride, int64_t dk_head_stride, void* dv,
+    int64_t dv_token_stride, int64_t dv_head_stride, void* workspace, size_t ws_bytes,
+    int32_t* dev_status, void* stream) {
+  AttArgs a = {};
+  a.d_o = {d_o, d_o_token_stride, d_o_head_stride};
+  a.q = {q, q_token_stride, q_head_stride};
+  a.k = {k, k_token_stride, k_head_stride};
+  a.v = {v, v_token_stride, v_head_stride};
+  a.o = {o, o_token_stride, o_head_stride};
+  a.dq = {dq, dq_token_stride, dq_head_stride};
+  a.dk = {dk, dk_token_stride, dk_head_stride};
+  a.dv = {dv, dv_token_stride, dv_head_stride};
+  a.lse = const_cast<float*>(lse);
+  a.cu = cu_seqlens;
+  a.prefix_end = prefix_end;
+  a.slopes = slopes;
+  a.Hq = Hq;
+  a.Hk = Hk;
+  a.S = S;
+  a.T = T;
+  a.D = D;
+  a.scale = scale;
+  a.cap = cap;
+  a.causal = causal;
+  a.ws = workspace;
+  a.dev_status = dev_status;
+  olive_status st = check_att(a);
+  if (st != OLIVE_OK) return st;
+  if (T > 0) {
+    if (!lse) return OLIVE_ERR_INVALID_ARG;
+    for (const auto& [view, heads, written] :
+         {std::tuple<const HeadsView&, int32_t, bool>{a.d_o, Hq, false}, {a.q, Hq, false}, {a.k, Hk, false},
+          {a.v, Hk, false}, {a.o, Hq, false}, {a.dq, Hq, true}, {a.dk, Hk, true}, {a.dv, Hk, true}}) {
+      st = check_att_view(view, heads, a, written);
+      if (st != OLIVE_OK) return st;
+    }
+    st = check_ws(workspace, ws_bytes, att_bwd_ws_bytes(T, Hq));
+    if (st != OLIVE_OK) return st;
+  }
+  Ctx c;
+  st = make_ctx(stream, &c);
+  if (st != OLIVE_OK || T == 0) return st;
+  a.wait_limit_ns = c.wait_limit_ns;
+  return launch_att_bwd(c, a);
 }
 
 }  // extern "C"

@@ -126,14 +126,25 @@ def _forward(s):
     return o, lse
 
 
+def _backward(s, o, lse, **kw):
+    st = B.new_status()
+    got = B.olive_packed_attention_bwd(s["do"], s["q"], s["k"], s["v"], o, lse, s["cu"], **s["more"], dev_status=st, **kw)
+    assert B.status_bits(st) == []
+    return got
+
+
 def _check(s):
-    ref = _reference(s)
+    ref = _reference(s, True)
     o, lse = _forward(s)
     _near(o, ref, "o")
     _near(lse, ref, "lse")
     behind = int(s["cu"][-1])
     assert not o[behind:].any() and bool((lse[:, behind:] == -math.inf).all())
-    return o, lse
+    grads = _backward(s, o, lse)
+    for name, g in zip(("dq", "dk", "dv"), grads):
+        _near(g, ref, name)
+        assert not g[behind:].any(), name
+    return (o, lse, *grads)
 
 
 @pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 100, 127, 128, 129, 255, 256, 257, 300, 513, 1000])
@@ -185,18 +196,19 @@ def test_largest_scores_late():
 def test_what_is_not_finite():
     """A bad token behind a sequence's end, or in another one, does not show; its own sequence's does."""
     s = _case([100, 77, 60], 4, 2, 64, pad=20)
-    good, lse = _forward(s)
-    for n in ("q", "k", "v"):
+    good = _check(s)
+    for n in ("q", "k", "v", "do"):
         s[n][100 + 77:] = float("nan")  # the last sequence, and nobody's rows
-    o, lse2 = _forward(s)
-    assert torch.equal(o[:177], good[:177]) and torch.equal(lse2[:, :177], lse[:, :177])
-    assert torch.isnan(o[177:237]).all() and not o[237:].any()
+    o, lse = _forward(s)
+    assert torch.equal(o[:177], good[0][:177]) and torch.equal(lse[:, :177], good[1][:, :177])
+    for g, want in zip((o, *_backward(s, o, lse)), (good[0], *good[2:])):
+        assert torch.equal(g[:177], want[:177]) and torch.isnan(g[177:237]).all() and not g[237:].any()
 
 
 def test_layouts():
     """The same values in other layouts give the same bits."""
     s = _case([200, 61], 4, 2, 80, pad=3)
-    want = _forward(s)
+    want = _check(s)
     for lay in ("heads first", "wide"):
         def relaid(t):
             if lay == "heads first":
@@ -204,15 +216,91 @@ def test_layouts():
             wide = torch.full((t.shape[0], t.shape[1] + 3, t.shape[2] + 16), float("nan"), dtype=BF16, device="cuda")
             wide[:, 1:-2, 8:-8] = t
             return wide[:, 1:-2, 8:-8]
+        q, k, v, do = (relaid(s[n]) for n in ("q", "k", "v", "do"))
         out = relaid(torch.zeros_like(want[0]))
-        o, lse = B.olive_packed_attention_fwd(*(relaid(s[n]) for n in "qkv"), s["cu"], **s["more"], out=out)
-        assert o is out and torch.equal(o, want[0]) and torch.equal(lse, want[1])
+        o, lse = B.olive_packed_attention_fwd(q, k, v, s["cu"], **s["more"], out=out)
+        outs = [relaid(torch.zeros_like(t)) for t in want[2:]]
+        grads = B.olive_packed_attention_bwd(do, q, k, v, o, lse, s["cu"], **s["more"], out=outs)
+        assert o is out and all(a is b for a, b in zip(grads, outs))
+        assert all(torch.equal(a, b) for a, b in zip((o, lse, *grads), want))
     # key heads that share memory
     one = s["k"][:, :1].contiguous()
-    o, lse = B.olive_packed_attention_fwd(s["q"], one.expand(-1, 2, -1), one.expand(-1, 2, -1), s["cu"], **s["more"])
-    both = one.repeat(1, 2, 1)
-    o2, lse2 = B.olive_packed_attention_fwd(s["q"], both, both, s["cu"], **s["more"])
-    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    res = []
+    for kv in (one.expand(-1, 2, -1), one.repeat(1, 2, 1)):
+        o, lse = B.olive_packed_attention_fwd(s["q"], kv, kv, s["cu"], **s["more"])
+        res.append((o, lse, *B.olive_packed_attention_bwd(s["do"], s["q"], kv, kv, o, lse, s["cu"], **s["more"])))
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+def test_rows_of_one_key_have_no_gradient_of_their_score():
+    """A softmax of one key is constant: exactly zero."""
+    for lens, kw in (([1] * 300, {}), ([1, 1, 1], dict(causal=False)), ([1] * 20, dict(cap=3.0, bias=True, prefix=1))):
+        s = _case(lens, 4, 2, 64, **kw)
+        _, _, dq, dk, dv = _check(s)
+        assert not dq.any() and not dk.any() and bool(dv.any())
+
+
+def test_gradient_against_differences():
+    """Along a random direction, against central differences of the 64-bit forward (their truncation
+    is below 1e-5 of the slope's terms; the gradients' operands are rounded to 2^-8)."""
+    s = _case([90, 40], 4, 2, 64, cap=8.0, bias=True, prefix=30)
+    o, lse = _forward(s)
+    grads = _backward(s, o, lse)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    dirs = [torch.randn(s[n].shape, generator=gen, device="cuda", dtype=torch.float64) for n in "qkv"]
+    e = 1e-3
+    values = []
+    for step in (e, -e):
+        moved = {**s, **{n: s[n].double() + step * u for n, u in zip("qkv", dirs)}}
+        values.append(float((_reference(moved)["o"] * s["do"].double()).sum()))
+    slope = (values[0] - values[1]) / (2 * e)
+    terms = [g.double() * u for g, u in zip(grads, dirs)]
+    got, size = sum(float(t.sum()) for t in terms), sum(float(t.abs().sum()) for t in terms)
+    assert abs(got - slope) <= 3 * STEP * size
+
+
+def test_autograd_form():
+    s = _case([90, 33], 4, 2, 64, pad=5, prefix=10, cap=9.0, bias=True)
+    leaves = [s[n].clone().requires_grad_() for n in "qkv"]
+    o = B.packed_attention(*leaves, s["cu"], **s["more"])
+    (torch.cat([o, o], 1)[:, 2:6].float() * s["do"].float()).sum().backward()
+    o2, lse = _forward(s)
+    s["do"] = torch.cat([s["do"][:, 2:], s["do"][:, :2]], 1)
+    assert torch.equal(o, o2) and all(torch.equal(t.grad, g) for t, g in zip(leaves, _backward(s, o2, lse)))
+    for loss in (lambda o: o.sum(), lambda o: (o * o.new_ones(1, 4, 64)).sum()):  # gradients that are one row for all
+        got = torch.autograd.grad(loss(B.packed_attention(*leaves, s["cu"], **s["more"])), leaves)
+        s["do"] = torch.ones_like(o2)
+        assert all(torch.equal(a, b) for a, b in zip(got, _backward(s, o2, lse)))
+    g, = torch.autograd.grad(B.packed_attention(*leaves, s["cu"]).square().sum(), leaves[0], create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(g.sum(), leaves[0])
+
+
+def test_captured_and_on_another_stream():
+    s = _case([700, 45, 300], 8, 2, 128, pad=9)
+
+    def run():
+        o, lse = B.olive_packed_attention_fwd(s["q"], s["k"], s["v"], s["cu"], **s["more"])
+        return (o, lse, *B.olive_packed_attention_bwd(s["do"], s["q"], s["k"], s["v"], o, lse, s["cu"], **s["more"]))
+
+    want = run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = run()
+    both = run()  # beside it
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) and torch.equal(c, b) for a, b, c in zip(got, want, both))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for seed, lens in ((5, [1, 1000, 44]), (6, [500, 545, 0])):  # (other sequences in the same arrays)
+        new = _case(lens, 8, 2, 128, pad=9, seed=seed)
+        for n in ("q", "k", "v", "do", "cu"):
+            s[n].copy_(new[n])
+        want = run()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 @pytest.mark.parametrize("cu", [[0, 50, 40, 90], [0, 200], [5, 50], [-3, 60], [0, 2**31 - 1], [70, 20]])
@@ -221,7 +309,10 @@ def test_offsets_that_do_not_describe_the_batch(cu):
     st = B.new_status()
     bad = torch.tensor(cu, dtype=torch.int32, device="cuda")
     B.olive_packed_attention_fwd(s["q"], s["k"], s["v"], bad, dev_status=st)
-    B.olive_packed_attention_fwd(s["q"], s["k"], s["v"], bad)
+    o, lse = B.olive_packed_attention_fwd(s["q"], s["k"], s["v"], bad)
+    assert B.status_bits(st) == ["OLIVE_ERR_OFFSETS"]
+    st = B.new_status()
+    B.olive_packed_attention_bwd(s["do"], s["q"], s["k"], s["v"], o, lse, bad, dev_status=st)
     assert B.status_bits(st) == ["OLIVE_ERR_OFFSETS"]
 
 
@@ -229,5 +320,7 @@ def test_no_tokens():
     s = _case([1], 2, 1, 64)
     o, lse = B.olive_packed_attention_fwd(s["q"][:0], s["k"][:0], s["v"][:0], torch.zeros(2, dtype=torch.int32, device="cuda"))
     assert o.shape == (0, 2, 64) and lse.shape == (2, 0)
+    got = B.olive_packed_attention_bwd(o, s["q"][:0], s["k"][:0], s["v"][:0], o, lse, torch.zeros(2, dtype=torch.int32, device="cuda"))
+    assert [tuple(t.shape) for t in got] == [(0, 2, 64), (0, 1, 64), (0, 1, 64)]
     s = _case([0, 0], 2, 1, 64, pad=10)
     _check(s)
