@@ -8,8 +8,11 @@
 //
 // A CTA works on two slots of 128 query rows with the same keys (two heads of a key
 // head, or two tiles of a head) and walks the key tiles:
-//   warp 8     TMA: query tiles, then key and value tiles into rings of two
-//   warp 9     MMA: S = Q K^T into tensor memory, O += P V with P read from there
+//   warp 8     TMA: query tiles, then key and value tiles into rings of three and two
+//   warp 9     MMA: S = Q K^T into tensor memory, O += P V with P read from there, the
+//              slots in turn (a warp for each: their products mix, both slots' rows then
+//              wait at once; 8 x 4096 tokens 922 us in place of 833)
+//   warp 11    hands out items
 //   warps 0-3, 4-7  the rows of slot 0 and 1, one a thread: the running maximum and
 //              sum, P = exp2(S - reference) in bf16 over S in tensor memory.
 // While one slot's rows are exponentiated the other's products run.  A row's reference
@@ -22,27 +25,31 @@
 namespace olive {
 namespace {
 
-constexpr int kThreads = 384;  // (the last two warps only give up their registers)
+constexpr int kThreads = 384;
 constexpr int kRegsLaunch = 168, kRegsSoft = 224, kRegsRest = 56;
 static_assert(2 * kRegsSoft + kRegsRest <= 3 * kRegsLaunch, "the block's registers");
-constexpr int kStages = 2;
-constexpr int kTmaWarp = 8, kMmaWarp = 9;
+constexpr int kK = 3, kV = 2;  // stages of key and value tiles
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kItemWarp = 11;
+constexpr int kReaders = 10;
 constexpr float kLag = 8.f;
-enum { B_QFULL = 0, B_QEMPTY = 2, B_KFULL = 4, B_KEMPTY = B_KFULL + kStages, B_VFULL = B_KEMPTY + kStages,
-       B_VEMPTY = B_VFULL + kStages, B_VFIX = B_VEMPTY + kStages, B_SFULL = B_VFIX + kStages, B_PREADY = B_SFULL + 2,
-       B_OFULL = B_PREADY + 2, B_OEMPTY = B_OFULL + 2, B_DRAIN = B_OEMPTY + 2, B_COUNT };
-
-constexpr int smem_bytes(int boxes) { return 1024 + (2 + 2 * kStages) * boxes * kBoxBytes + 8 * B_COUNT + 16; }
+enum { B_QFULL = 0, B_QEMPTY = 2, B_KFULL = 4, B_KEMPTY = B_KFULL + kK, B_VFULL = B_KEMPTY + kK, B_VEMPTY = B_VFULL + kV,
+       B_VFIX = B_VEMPTY + kV, B_SFULL = B_VFIX + kV, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 2, B_OEMPTY = B_OFULL + 2,
+       B_DRAIN = B_OEMPTY + 2, B_RING, B_COUNT = B_RING + kRingBars };
 
 // An item's slots: heads, first rows and key tiles.
 struct Item {
   Seq q;
   int kv_head, head[2], row0[2], tiles[2], seen[2];  // seen: keys that the slot's last row sees
+  int end;
 };
+constexpr int kMisc = 16 + static_cast<int>(sizeof(ItemRing<Item>));
+constexpr int smem_bytes(int boxes) {
+  return 1024 + (2 + kK + kV) * boxes * kBoxBytes + (8 * B_COUNT + 15) / 16 * 16 + kMisc;
+}
 // Two heads of a key head where their number is even, else two tiles of a head.
 template <bool kPairHeads>
-__device__ __forceinline__ bool item_at(const AttArgs& p, int64_t i, int units, Item& it) {
-  const int slot = static_cast<int>(i / units), u = static_cast<int>(i % units);
+__device__ __forceinline__ bool item_at(const AttArgs& p, int i, int units, Item& it) {
+  const int slot = i / units, u = i % units;
   it.q = seq_of_slot<kPairHeads ? 128 : 256>(p, slot);
   if (it.q.tile < 0) return false;
   constexpr int R = kPairHeads ? 128 : 256;
@@ -57,27 +64,33 @@ __device__ __forceinline__ bool item_at(const AttArgs& p, int64_t i, int units, 
     it.tiles[a] = (it.seen[a] + 127) / 128;
   }
   it.kv_head = it.head[0] / per;
+  it.end = 0;
   return true;
 }
 
-template <int kBoxes, bool kPairHeads, bool kExtra>
+template <int kBoxes, bool kPairHeads, int kForm>
 __global__ void __launch_bounds__(kThreads, 1)
     att_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                   const __grid_constant__ CUtensorMap map_v, const AttArgs p, int units, int64_t items) {
+                   const __grid_constant__ CUtensorMap map_v, const AttArgs p, int units, int ask) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   constexpr uint32_t kTileBytes = kBoxes * kBoxBytes;
-  const uint32_t sq = base, sk = sq + 2 * kTileBytes, sv = sk + kStages * kTileBytes;
-  const uint32_t bar0 = sv + kStages * kTileBytes;
-  uint8_t* misc = smem_raw + (bar0 - raw) + 8 * B_COUNT;
+  const uint32_t sq = base, sk = sq + 2 * kTileBytes, sv = sk + kK * kTileBytes;
+  const uint32_t bar0 = sv + kV * kTileBytes;
+  uint8_t* misc = smem_raw + (bar0 - raw) + (8 * B_COUNT + 15) / 16 * 16;
+  ItemRing<Item>& ring = *reinterpret_cast<ItemRing<Item>*>(misc + 16);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
   const auto bar = [&](int i) { return bar0 + 8u * i; };
+  const RingAt ring_at{bar(B_RING)};
   const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < B_COUNT; ++i)
-      mbar_init(bar(i), i >= B_PREADY && i < B_PREADY + 2 ? 4 : i >= B_OEMPTY && i < B_OEMPTY + 2 ? 4 : 1);
+    for (int i = 0; i < B_RING; ++i) {
+      const auto among = [&](int first, int n) { return i >= first && i < first + n; };
+      mbar_init(bar(i), among(B_PREADY, 2) || among(B_OEMPTY, 2) ? 4 : 1);
+    }
+    init_ring(ring_at, kReaders);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -89,14 +102,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_desc(&map_q);
     tma_prefetch_desc(&map_k);
     tma_prefetch_desc(&map_v);
-  }
-  check_offsets(p);
-  zero_behind(p, const_cast<void*>(p.o.x), p.o.token_stride, p.o.head_stride, p.Hq);
-  if (p.lse) {
-    const int first = cu_at(p, p.S), n = p.T - first;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < static_cast<int64_t>(n) * p.Hq;
-         i += static_cast<int64_t>(gridDim.x) * kThreads)
-      p.lse[i / n * p.T + first + i % n] = __uint_as_float(0xff800000u);
   }
   tc_fence_before();
   __syncthreads();
@@ -112,10 +117,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
-      uint32_t n_q[2] = {0, 0}, n_kv = 0;
+      uint32_t n_q[2] = {0, 0};
+      Turn k, v;
       bool ok = true;
-      for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-        if (!item_at<kPairHeads>(p, i, units, it)) continue;
+      for (uint32_t n = 0; ok && next_item(ring, ring_at, n, it, ctl, ok);) {
         const int tiles = max(it.tiles[0], it.tiles[1]), seen = max(it.seen[0], it.seen[1]);
         const auto query = [&](int a) {
           if (it.tiles[a] == 0) return true;
@@ -128,89 +133,109 @@ __global__ void __launch_bounds__(kThreads, 1)
           return true;
         };
         ok = query(0);
-        for (int j = 0; ok && j < tiles; ++j, ++n_kv) {
-          const int s = n_kv % kStages;
-          const uint32_t free = (n_kv / kStages & 1) ^ 1;
-          if (!(ok = mbar_wait_warp(bar(B_KEMPTY + s), free, ctl))) break;
+        for (int j = 0; ok && j < tiles; ++j, k.next(kK), v.next(kV)) {
+          if (!(ok = mbar_wait_warp(bar(B_KEMPTY + k.i), k.phase ^ 1, ctl))) break;
           if (leader) {
-            mbar_arrive_expect_tx(bar(B_KFULL + s), kTileBytes);
-            load_tile(sk + s * kTileBytes, &map_k, bar(B_KFULL + s), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + 128 * j);
+            mbar_arrive_expect_tx(bar(B_KFULL + k.i), kTileBytes);
+            load_tile(sk + k.i * kTileBytes, &map_k, bar(B_KFULL + k.i), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + 128 * j);
           }
           if (j == 0 && !(ok = query(1))) break;
-          if (!(ok = mbar_wait_warp(bar(B_VEMPTY + s), free, ctl))) break;
+          if (!(ok = mbar_wait_warp(bar(B_VEMPTY + v.i), v.phase ^ 1, ctl))) break;
           if (leader) {
-            mbar_arrive_expect_tx(bar(B_VFULL + s), kTileBytes);
-            load_tile(sv + s * kTileBytes, &map_v, bar(B_VFULL + s), kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + 128 * j);
+            mbar_arrive_expect_tx(bar(B_VFULL + v.i), kTileBytes);
+            load_tile(sv + v.i * kTileBytes, &map_v, bar(B_VFULL + v.i), kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + 128 * j);
           }
           // the sequence's last rows: what follows them up to whole K steps is zeroed
           const int rows = seen - 128 * j;
           if (rows < 128 && rows % 16 != 0) {
-            if (!(ok = mbar_wait_warp(bar(B_VFULL + s), n_kv / kStages & 1, ctl))) break;
-            if (it.q.n - 128 * j < 128) zero_rows(sv + s * kTileBytes, kBoxes, rows, up16(rows));
+            if (!(ok = mbar_wait_warp(bar(B_VFULL + v.i), v.phase, ctl))) break;
+            if (it.q.n - 128 * j < 128) zero_rows(sv + v.i * kTileBytes, kBoxes, rows, up16(rows));
             fence_proxy_async_shared();
             __syncwarp();
-            if (leader) mbar_arrive(bar(B_VFIX + s));
+            if (leader) mbar_arrive(bar(B_VFIX + v.i));
           }
         }
+        if (ok && leader) mbar_arrive(ring_at.issued());
       }
       if (!ok) let_copies_land();
       __syncwarp();
     } else if (warp == kMmaWarp) {
       const bool leader = elect_one();
       const int steps = (p.D + 15) / 16;
-      uint32_t n_q[2] = {0, 0}, n_kv = 0, fixed = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};
+      const uint32_t id_out = idesc_bf16(128, 16 * steps, false, true);
+      uint32_t n_q[2] = {0, 0}, n_p[2] = {0, 0}, n_o[2] = {0, 0}, fixed = 0;
+      Turn k, v;
       bool ok = true;
-      for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-        if (!item_at<kPairHeads>(p, i, units, it)) continue;
+      for (uint32_t n = 0; ok && next_item(ring, ring_at, n, it, ctl, ok);) {
         const int tiles = max(it.tiles[0], it.tiles[1]), seen = max(it.seen[0], it.seen[1]);
+        // Slot 0's products of a round, the waits for slot 1's and for the next round's
+        // tiles while those run, slot 1's.  (A wait takes some 130 cycles where nothing is
+        // waited for, and what is queued lasts little longer: all of them ahead of a
+        // round, its period is 3430 cycles.)
+        const auto fix_rows = [&](int j) {  // whether tile j's last rows are mended
+          const int rows = seen - 128 * j;
+          return rows < 128 && rows % 16 != 0;
+        };
+        if (!(ok = mbar_wait_warp(bar(B_KFULL + k.i), k.phase, ctl))) break;
         for (int j = 0; ok && j <= tiles; ++j) {
-          const uint32_t at = n_kv + j, before = at - 1;
-          if (j < tiles && !(ok = mbar_wait_warp(bar(B_KFULL + at % kStages), at / kStages & 1, ctl))) break;
-          if (j > 0) {
-            if (!(ok = mbar_wait_warp(bar(B_VFULL + before % kStages), before / kStages & 1, ctl))) break;
-            const int rows = seen - 128 * (j - 1), s = before % kStages;
-            if (rows < 128 && rows % 16 != 0) {
-              if (!(ok = mbar_wait_warp(bar(B_VFIX + s), fixed >> s & 1, ctl))) break;
-              fixed ^= 1u << s;
-            }
-          }
+          // v: the tile before, of this round's second products; k: this round's
+          Turn k2 = k;
+          if (j < tiles) k2.next(kK);
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
-            if (j > 0 && j - 1 < it.tiles[a]) {  // O += P V of the tile before
+            const bool add = j > 0 && j <= it.tiles[a];
+            if (add) {  // O += P V of the tile before
               if (j == 1 && !(ok = mbar_wait_warp(bar(B_OEMPTY + a), (n_o[a]++ & 1) ^ 1, ctl))) break;
               if (!(ok = mbar_wait_warp(bar(B_PREADY + a), n_p[a]++ & 1, ctl))) break;
               tc_fence_after();
               const int ks = up16(min(128, it.seen[a] - 128 * (j - 1))) / 16;
-              if (leader) {
-                mma_cols(t_o(a), t_s(a), 32, sv + before % kStages * kTileBytes, idesc_bf16(128, 16 * steps, false, true), ks, j > 1);
-                if (j == it.tiles[a]) umma_commit(bar(B_OFULL + a));
-              }
+              mma_cols(leader, t_o(a), t_s(a), 32, sv + v.i * kTileBytes, id_out, ks, j > 1);
+              if (leader && j == it.tiles[a]) umma_commit(bar(B_OFULL + a));
             }
             if (j < it.tiles[a]) {  // S of this one
               if (j == 0 && !(ok = mbar_wait_warp(bar(B_QFULL + a), n_q[a]++ & 1, ctl))) break;
               tc_fence_after();
-              const int cols = up16(min(128, it.seen[a] - 128 * j));
+              const uint32_t id = idesc_bf16(128, up16(min(128, it.seen[a] - 128 * j)), false, false);
+              mma_rows(leader, t_s(a), sq + a * kTileBytes, sk + k.i * kTileBytes, id, steps);
               if (leader) {
-                mma_rows(t_s(a), sq + a * kTileBytes, sk + at % kStages * kTileBytes, idesc_bf16(128, cols, false, false), steps);
                 umma_commit(bar(B_SFULL + a));
                 if (j == it.tiles[a] - 1) umma_commit(bar(B_QEMPTY + a));
               }
             }
+            if (a == 0 && j < tiles) {
+              // the next round's tiles: V of this one, K of the next
+              Turn v2 = v;
+              if (j > 0) v2.next(kV);
+              const Phase next[2] = {{bar(B_VFULL + v2.i), v2.phase},
+                                     {bar(B_KFULL + (j + 1 < tiles ? k2.i : k.i)), j + 1 < tiles ? k2.phase : k.phase}};
+              if (!(ok = mbar_wait_warp(next, ctl))) break;
+              if (fix_rows(j)) {
+                if (!(ok = mbar_wait_warp(bar(B_VFIX + v2.i), fixed >> v2.i & 1, ctl))) break;
+                fixed ^= 1u << v2.i;
+              }
+            }
           }
           if (ok && leader) {
-            if (j > 0) umma_commit(bar(B_VEMPTY + before % kStages));
-            if (j < tiles) umma_commit(bar(B_KEMPTY + at % kStages));
+            if (j > 0) umma_commit(bar(B_VEMPTY + v.i));
+            if (j < tiles) umma_commit(bar(B_KEMPTY + k.i));
           }
+          if (j > 0) v.next(kV);
+          k = k2;
         }
-        n_kv += tiles;
       }
-      // every MMA issued is complete before the CTA retires (they end by themselves)
-      if (leader) umma_commit(bar(B_DRAIN));
-      volatile int keep_waiting = 0;
-      const uint64_t floor_ns = 200ull * 1000 * 1000;
-      const WaitCtl own{&keep_waiting, p.wait_limit_ns > floor_ns ? p.wait_limit_ns : floor_ns};
-      mbar_wait_warp(bar(B_DRAIN), 0, own);
-      __syncwarp();
+      drain_mmas(bar(B_DRAIN), leader, p.wait_limit_ns);
+    } else if (warp == kItemWarp) {
+      hand_out(ring, ring_at, ask, ctl, [&](int i, Item& item) { return item_at<kPairHeads>(p, i, units, item); },
+               [&](int i) {
+                 if (i == 0) check_offsets(p);
+                 const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
+                 if (i >= parts) return;
+                 zero_behind(p, p.o, p.Hq, i, parts);
+                 const int first = cu_at(p, p.S), rows = p.T - first;
+                 if (p.lse)
+                   for (int64_t e = static_cast<int64_t>(i) * 32 + lane; e < static_cast<int64_t>(rows) * p.Hq; e += parts * 32)
+                     p.lse[e / rows * p.T + first + e % rows] = __uint_as_float(0xff800000u);
+               });
     }
   } else {
     regs_inc<kRegsSoft>();
@@ -218,18 +243,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const int row = (warp & 3) * 32 + lane;
     const uint32_t ts = t_s(a) + lanes, to = t_o(a) + lanes;
-    const float scale2 = p.scale * kAttLog2e;
+    const ScoreForm form(p);
     uint32_t n_s = 0, n_o = 0;
     bool ok = true;
-    for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-      if (!item_at<kPairHeads>(p, i, units, it)) continue;
+    for (uint32_t n = 0; ok && next_item(ring, ring_at, n, it, ctl, ok);) {
       const int tiles = a ? it.tiles[1] : it.tiles[0];
       if (tiles == 0) continue;
       const int head = a ? it.head[1] : it.head[0];
       const int pos = (a ? it.row0[1] : it.row0[0]) + row;
       const int lim = keys_seen(p, it.q, min(pos, it.q.n - 1));
-      const float slope2 = kExtra && p.slopes ? p.slopes[head] * kAttLog2e : 0.f;
-      const float to_cap = kExtra && p.cap > 0.f ? 2.f * scale2 / p.cap : 0.f, cap2 = p.cap * kAttLog2e;
+      const float slope2 = kForm != FORM_PLAIN && p.slopes ? p.slopes[head] * kAttLog2e : 0.f;
       float ref = 0.f, sum = 0.f;
       for (int j = 0; j < tiles; ++j) {
         if (!(ok = mbar_wait_warp(bar(B_SFULL + a), n_s++ & 1, ctl))) break;
@@ -238,16 +261,16 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(ts + 32 * c, s[c]);
         tmem_ld_wait();
-        float mul = scale2;
-        if constexpr (kExtra) {
+        float mul = form.scale2;
+        if constexpr (kForm != FORM_PLAIN) {
           mul = 1.f;
+          const float far = static_cast<float>(pos - 128 * j);
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              float x = __uint_as_float(s[c][e]);
-              x = to_cap != 0.f ? cap2 * tanh_of(x * to_cap) : x * scale2;
-              s[c][e] = __float_as_uint(fmaf(-slope2, fabsf(static_cast<float>(pos - (128 * j + 32 * c + e))), x));
+              float bend;
+              s[c][e] = __float_as_uint(form.at<kForm>(__uint_as_float(s[c][e]), slope2, fabsf(far - (32 * c + e)), bend));
             }
         }
         const int here = lim - 128 * j;
@@ -280,22 +303,28 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_st_32x32b_x32(to + c, o);
           }
         }
-        float part[4] = {};
+        uint64_t part[2] = {pair(sum, 0.f), pair(0.f, 0.f)};
+        const uint64_t mul2 = pair(mul, mul), off2 = pair(-ref, -ref);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t w[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
             const int c = 2 * h + (e >> 4), k = 2 * (e & 15);
-            const float x = fast_exp2(fmaf(__uint_as_float(s[c][k]), mul, -ref));
-            const float y = fast_exp2(fmaf(__uint_as_float(s[c][k + 1]), mul, -ref));
-            part[2 * (e & 1)] += x;
-            part[2 * (e & 1) + 1] += y;
+            float x, y;
+            unpair(fma_pair(pair(__uint_as_float(s[c][k]), __uint_as_float(s[c][k + 1])), mul2, off2), x, y);
+            x = fast_exp2(x);
+            y = fast_exp2(y);
+            part[e & 1] = add_pair(part[e & 1], pair(x, y));
             w[e] = pack_bf16x2(x, y);
           }
           tmem_st_32x32b_x32(ts + 32 * h, w);
         }
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
+        {
+          float x, y;
+          unpair(add_pair(part[0], part[1]), x, y);
+          sum = x + y;
+        }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -338,32 +367,37 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-template <int kBoxes, bool kPairHeads, bool kExtra>
+template <int kBoxes, bool kPairHeads, int kForm>
 olive_status run_fwd(const Ctx& c, const AttArgs& a) {
   CUtensorMap mq, mk, mv;
   if (!encode_heads(&mq, a.q, a.T, a.Hq, a.D) || !encode_heads(&mk, a.k, a.T, a.Hk, a.D) || !encode_heads(&mv, a.v, a.T, a.Hk, a.D))
     return OLIVE_ERR_CUDA;
   static std::atomic<int> done[kMaxDevices];
-  const auto kernel = att_fwd_kernel<kBoxes, kPairHeads, kExtra>;
+  const auto kernel = att_fwd_kernel<kBoxes, kPairHeads, kForm>;
   constexpr int kSmem = smem_bytes(kBoxes);
   if (!set_smem_once(reinterpret_cast<const void*>(kernel), kSmem, c.device, done)) return OLIVE_ERR_CUDA;
   const int units = kPairHeads ? a.Hq / 2 : a.Hq;
   const int64_t items = att_slots(a.T, a.S, kPairHeads ? 128 : 256) * units;
-  kernel<<<static_cast<unsigned>(std::min<int64_t>(items, c.num_sms)), kThreads, kSmem, c.stream>>>(mq, mk, mv, a, units, items);
+  kernel<<<static_cast<unsigned>(items), kThreads, kSmem, c.stream>>>(mq, mk, mv, a, units,
+                                                                     when_to_ask(items, c.num_sms, a.T, a.S));
   return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
 }
 
-template <int kBoxes>
+template <int kBoxes, bool kPairHeads>
 olive_status by_form(const Ctx& c, const AttArgs& a) {
-  const bool pair = a.Hq / a.Hk % 2 == 0, extra = a.cap > 0.f || a.slopes;
-  if (pair) return extra ? run_fwd<kBoxes, true, true>(c, a) : run_fwd<kBoxes, true, false>(c, a);
-  return extra ? run_fwd<kBoxes, false, true>(c, a) : run_fwd<kBoxes, false, false>(c, a);
+  if (a.cap > 0.f) return run_fwd<kBoxes, kPairHeads, FORM_CAP>(c, a);
+  return a.slopes ? run_fwd<kBoxes, kPairHeads, FORM_BIAS>(c, a) : run_fwd<kBoxes, kPairHeads, FORM_PLAIN>(c, a);
+}
+
+template <int kBoxes>
+olive_status by_heads(const Ctx& c, const AttArgs& a) {
+  return a.Hq / a.Hk % 2 == 0 ? by_form<kBoxes, true>(c, a) : by_form<kBoxes, false>(c, a);
 }
 
 }  // namespace
 
 olive_status launch_att_fwd(const Ctx& c, const AttArgs& a) {
-  return a.D <= 64 ? by_form<1>(c, a) : by_form<2>(c, a);
+  return a.D <= 64 ? by_heads<1>(c, a) : by_heads<2>(c, a);
 }
 
 }  // namespace olive

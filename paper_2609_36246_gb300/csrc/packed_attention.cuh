@@ -54,24 +54,113 @@ __device__ __forceinline__ int keys_seen(const AttArgs& p, const Seq& q, int i) 
   return p.causal ? min(max(i + 1, q.prefix), q.n) : q.n;
 }
 
-// Offsets that do not describe the batch, and outputs behind the last sequence.
+// Offsets that do not describe the batch (a warp).
 __device__ __forceinline__ void check_offsets(const AttArgs& p) {
-  if (blockIdx.x != 0) return;
-  bool bad = threadIdx.x == 0 && p.cu[0] != 0;
-  for (int s = threadIdx.x; s < p.S; s += blockDim.x) {
+  const int lane = threadIdx.x & 31;
+  bool bad = lane == 0 && p.cu[0] != 0;
+  for (int s = lane; s < p.S; s += 32) {
     const int a = p.cu[s], b = p.cu[s + 1];
     bad |= a < 0 || b < a || b > p.T;
   }
   if (bad && p.dev_status) atomicOr(p.dev_status, kStatusOffsets);
 }
-__device__ __forceinline__ void zero_behind(const AttArgs& p, void* x, int64_t token_stride, int64_t head_stride, int heads) {
+// Part `part` of `parts` of the rows behind the last sequence, zeroed (a warp).
+__device__ __forceinline__ void zero_behind(const AttArgs& p, const HeadsView& x, int heads, int64_t part, int64_t parts) {
   const int first = cu_at(p, p.S), vecs = p.D / 8;
   const int64_t n = static_cast<int64_t>(p.T - first) * heads * vecs;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+  for (int64_t i = part * 32 + (threadIdx.x & 31); i < n; i += parts * 32) {
     const int64_t row = i / vecs;
-    __nv_bfloat16* at = static_cast<__nv_bfloat16*>(x) + (first + row / heads) * token_stride + (row % heads) * head_stride;
+    __nv_bfloat16* at = static_cast<__nv_bfloat16*>(const_cast<void*>(x.x)) + (first + row / heads) * x.token_stride +
+                        (row % heads) * x.head_stride;
     reinterpret_cast<uint4*>(at)[i % vecs] = make_uint4(0, 0, 0, 0);
   }
+}
+
+// The items of a launch, one a block; a block that is done takes over blocks that have
+// not started.  One warp asks, finds the item's sequence and hands it to the others
+// through a ring in shared memory.  What is claimed early cannot be taken by blocks that
+// run dry, so a block asks when the copies of its last item are issued (two tiles before
+// its end); where items are so short that asking and searching would show, it asks while
+// the ring of kItems has room; and where there is an SM for every item it does not ask.
+enum { ASK_NEVER = 0, ASK_LATE = 2, ASK_EARLY = 4 };  // and the entries of the ring in use
+constexpr int kItems = 4;
+constexpr int64_t kParts = 1024;  // items that also zero a part of the rows behind the last sequence
+template <class Item>
+struct ItemRing {
+  alignas(16) uint32_t answer[4];
+  Item item[kItems];
+};
+// Barriers: `taken`, `issued` (an item's copies), full [kItems], empty [kItems].
+constexpr int kRingBars = 2 + 2 * kItems;
+struct RingAt {
+  uint32_t bars;
+  __device__ __forceinline__ uint32_t taken() const { return bars; }
+  __device__ __forceinline__ uint32_t issued() const { return bars + 8; }
+  __device__ __forceinline__ uint32_t full(uint32_t n) const { return bars + 16 + 8 * (n % kItems); }
+  __device__ __forceinline__ uint32_t empty(uint32_t n) const { return bars + 16 + 8 * kItems + 8 * (n % kItems); }
+};
+__device__ __forceinline__ void init_ring(const RingAt& r, int readers) {
+  mbar_init(r.taken(), 1);
+  mbar_init(r.issued(), 1);
+  for (int i = 0; i < kItems; ++i) {
+    mbar_init(r.full(i), 1);
+    mbar_init(r.empty(i), readers);
+  }
+}
+// The warp that hands out items.  find(i, item) says whether item i exists; rest(i) is
+// what else is done for every i, after the item is out.
+template <class Item, class Find, class Rest>
+__device__ __forceinline__ void hand_out(ItemRing<Item>& ring, const RingAt& at, int ask, const WaitCtl& ctl, Find find, Rest rest) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t answer = smem_u32(ring.answer);
+  uint32_t n = 0, asked = 0;
+  bool ok = true;
+  int i = blockIdx.x;
+  while (i >= 0) {
+    Item it;
+    const bool there = find(i, it);
+    if (there) {
+      if (lane == 0) ring.item[n % kItems] = it;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(at.full(n));
+      ++n;
+    }
+    rest(i);
+    // (room for the next entry, be it the last)
+    if (!(ok = mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, ctl))) break;
+    if (ask == ASK_NEVER) break;
+    if (there && ask == ASK_LATE && !(ok = mbar_wait_warp(at.issued(), (n - 1) & 1, ctl))) break;
+    if (lane == 0) {
+      fence_proxy_async_shared();
+      mbar_arrive_expect_tx(at.taken(), 16);
+      take_block(answer, at.taken());
+    }
+    __syncwarp();
+    if (!(ok = mbar_wait_warp(at.taken(), asked++ & 1, ctl))) {
+      let_copies_land();
+      break;
+    }
+    i = warp_uniform(taken_block(answer));
+  }
+  if (ok && lane == 0) {
+    ring.item[n % kItems].end = 1;
+    mbar_arrive(at.full(n));
+  }
+  __syncwarp();
+}
+// A reader's next item; false: there is none (or the block gives up, ok = false).
+template <class Item>
+__device__ __forceinline__ bool next_item(const ItemRing<Item>& ring, const RingAt& at, uint32_t& n, Item& it,
+                                          const WaitCtl& ctl, bool& ok) {
+  if (!(ok = mbar_wait_warp(at.full(n), n / kItems & 1, ctl))) return false;
+  it = warp_uniform_copy(&ring.item[n % kItems]);
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(at.empty(n));
+  ++n;
+  return it.end == 0;
+}
+inline int when_to_ask(int64_t items, int sms, int64_t T, int64_t S) {
+  return items <= sms ? ASK_NEVER : T / S <= 256 ? ASK_EARLY : ASK_LATE;
 }
 
 // tanh(x) = 1 - 2 / (1 + e^2x), x in units of ln 2 / 2: off by some 2^-23, which is
@@ -81,6 +170,25 @@ __device__ __forceinline__ float tanh_of(float x2) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + fast_exp2(x2)));
   return fmaf(-2.f, r, 1.f);
 }
+// How scores are formed from products: as they are, lowered with the distance, or
+// capped (and lowered, by a slope that may be 0).  In base 2.
+enum { FORM_PLAIN = 0, FORM_BIAS = 1, FORM_CAP = 2 };
+struct ScoreForm {
+  float scale2, to_cap, cap2;
+  __device__ __forceinline__ explicit ScoreForm(const AttArgs& p)
+      : scale2(p.scale * kAttLog2e), to_cap(p.cap > 0.f ? 2.f * kAttLog2e * p.scale / p.cap : 0.f), cap2(p.cap * kAttLog2e) {}
+  // The score of a product at a distance, and the derivative of its cap.
+  template <int kForm>
+  __device__ __forceinline__ float at(float s, float slope2, float dist, float& bend) const {
+    if constexpr (kForm == FORM_CAP) {
+      const float t = tanh_of(s * to_cap);
+      bend = fmaf(-t, t, 1.f);
+      return fmaf(-slope2, dist, cap2 * t);
+    }
+    bend = 1.f;
+    return fmaf(-slope2, dist, s * scale2);
+  }
+};
 
 // A tile of up to 128 columns into shared memory: boxes of 64 columns.
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int boxes, int head, int token) {
@@ -95,24 +203,53 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, int boxes, int from, in
     for (int i = from * 8 + lane; i < to * 8; i += 32) st_shared_v4(tile + b * kBoxBytes + i * 16, make_uint4(0, 0, 0, 0));
 }
 
+// A place in a ring of barriers and its phase.
+struct Turn {
+  int i = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int n) {
+    if (++i == n) {
+      i = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+// The end of an MMA warp: what it issued is complete before the CTA retires (a wait that
+// ignores the abort flag: MMAs in flight end by themselves).
+__device__ __forceinline__ void drain_mmas(uint32_t bar, bool leader, uint64_t limit_ns) {
+  if (leader) umma_commit(bar);
+  volatile int keep_waiting = 0;
+  const uint64_t floor_ns = 200ull * 1000 * 1000;
+  const WaitCtl own{&keep_waiting, limit_ns > floor_ns ? limit_ns : floor_ns};
+  mbar_wait_warp(bar, 0, own);
+  __syncwarp();
+}
+
 __device__ __forceinline__ int up16(int n) { return (n + 15) & ~15; }
 
+// The products of a whole warp, `leader` the lane that issues: with the loop and the
+// operands the warp's they stay in uniform registers (sm103.cuh, mbar_wait_warp).
 // S = A B^T over a head's width: both operands tiles of rows (K-major).
-__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
+__device__ __forceinline__ void mma_rows(bool leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
   const uint64_t da = sdesc_sw128(a, 16, 1024), db = sdesc_sw128(b, 16, 1024);
-#pragma unroll 1
-  for (int k = 0; k < steps; ++k) {
+#pragma unroll
+  for (int k = 0; k < kMaxAttDim / 16; ++k) {
+    if (k >= steps) break;
     const uint32_t at = (k >> 2) * (kBoxBytes >> 4) + (k & 3) * 2;
-    umma_bf16(d, da + at, db + at, idesc, k > 0 ? 1u : 0u);
+    if (leader) umma_bf16(d, da + at, db + at, idesc, k > 0 ? 1u : 0u);
   }
 }
 // D (+)= A B with A [128, rows of B] in tensor memory and B a tile of rows (MN-major);
 // A's second 64 columns lie `half` tensor memory columns behind its first.
-__device__ __forceinline__ void mma_cols(uint32_t d, uint32_t a, int half, uint32_t b, uint32_t idesc, int steps, bool more) {
+__device__ __forceinline__ void mma_cols(bool leader, uint32_t d, uint32_t a, int half, uint32_t b, uint32_t idesc, int steps, bool more) {
   const uint64_t db = sdesc_sw128(b, kBoxBytes, 1024);
-#pragma unroll 1
-  for (int k = 0; k < steps; ++k)
-    umma_bf16_ta(d, a + (k >> 2) * half + (k & 3) * 8, db + k * 128, idesc, more || k > 0 ? 1u : 0u);
+  const uint32_t first = more ? 1u : 0u;
+#pragma unroll
+  for (int k = 0; k < kAttTile / 16; ++k) {
+    if (k >= steps) break;
+    if (leader) umma_bf16_ta(d, a + (k >> 2) * half + (k & 3) * 8, db + k * 128, idesc, k > 0 ? 1u : first);
+  }
 }
 
 }  // namespace olive

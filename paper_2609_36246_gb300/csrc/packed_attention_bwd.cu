@@ -11,6 +11,7 @@
 // added up in memory, results are the same bits from call to call, and no fp32 copy of
 // dq exists.
 #include <algorithm>
+#include <type_traits>
 
 #include "packed_attention.cuh"
 
@@ -20,8 +21,8 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kRegsLaunch = 168, kRegsRows = 224, kRegsRest = 56;
 static_assert(2 * kRegsRows + kRegsRest <= 3 * kRegsLaunch, "the block's registers");
-constexpr int kStages = 2;
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kVecWarp = 10;
+constexpr int kTmaWarp = 8, kMmaWarp = 9, kItemWarp = 11;  // (two warps issue MMAs)
+constexpr int kReaders = 11;
 constexpr int kRowWarps = 8;
 
 // ------------------------------------------------------------------ delta ---
@@ -51,18 +52,6 @@ __device__ __forceinline__ float dot16(const float (&a)[8], const float (&b)[8])
 __device__ __forceinline__ const __nv_bfloat16* row_of(const HeadsView& x, int64_t t, int h) {
   return static_cast<const __nv_bfloat16*>(x.x) + t * x.token_stride + h * x.head_stride;
 }
-// A score in base 2 and the derivative of its cap.
-__device__ __forceinline__ float score2(const AttArgs& p, float s, float slope2, float dist, float& bend) {
-  bend = 1.f;
-  float x = s * (p.scale * kAttLog2e);
-  if (p.cap > 0.f) {
-    const float t = tanh_of(x * (2.f / p.cap));
-    bend = fmaf(-t, t, 1.f);
-    x = p.cap * kAttLog2e * t;
-  }
-  return fmaf(-slope2, dist, x);
-}
-
 // stats: [Hq, T] of (lse in base 2, delta); a block works on a tile's rows of one head,
 // 16 lanes a row.
 __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttArgs p, float2* stats) {
@@ -71,6 +60,7 @@ __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttArgs 
   if (q.tile < 0) return;
   const int lane = threadIdx.x % 16, group = threadIdx.x / 16, kv = head / (p.Hq / p.Hk);
   const bool in = 8 * lane < p.D;
+  const ScoreForm form(p);
   const float slope2 = p.slopes ? p.slopes[head] * kAttLog2e : 0.f;
 #pragma unroll 1
   for (int r = group; r < 128; r += kDeltaThreads / 16) {
@@ -91,7 +81,8 @@ __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttArgs 
         const int64_t tj = q.start + min(j, keys - 1);
         eight(row_of(p.k, tj, kv) + 8 * lane, in, b);
         float bend;
-        const float s = score2(p, dot16(qr, b), slope2, fabsf(static_cast<float>(t - tj)), bend);
+        const float d = dot16(qr, b), far = fabsf(static_cast<float>(t - tj));
+        const float s = p.cap > 0.f ? form.at<FORM_CAP>(d, slope2, far, bend) : form.at<FORM_BIAS>(d, slope2, far, bend);
         eight(row_of(p.v, tj, kv) + 8 * lane, in, b);
         const float dp = dot16(a, b);
         if (j < keys) sum = fmaf(fast_exp2(s - lse2), dp, sum);
@@ -123,69 +114,76 @@ __device__ __forceinline__ void store_cols(uint32_t taddr, __nv_bfloat16* row, b
   }
 }
 
-// The end of the MMA warp: what it issued is complete before the CTA retires.
-__device__ __forceinline__ void drain_mmas(uint32_t bar, bool leader, uint64_t limit_ns) {
-  if (leader) umma_commit(bar);
-  volatile int keep_waiting = 0;
-  const uint64_t floor_ns = 200ull * 1000 * 1000;
-  const WaitCtl own{&keep_waiting, limit_ns > floor_ns ? limit_ns : floor_ns};
-  mbar_wait_warp(bar, 0, own);
-  __syncwarp();
-}
-
 // ----------------------------------------------------------------- dk, dv ---
-// tensor memory: S^T (then P^T), dP^T (then dS^T), dV, dK.  The MMAs of step t run in
-// the order dP_t, dV_t, S_{t+1}, dK_t: P_t is formed while dP_t runs and dS_t while
-// dV_t and S_{t+1} do.
-enum { A_KVFULL = 0, A_KVEMPTY, A_QFULL, A_QEMPTY = A_QFULL + kStages, A_FIX = A_QEMPTY + kStages,
-       A_VECFULL = A_FIX + kStages, A_VECEMPTY = A_VECFULL + kStages, A_SFULL = A_VECEMPTY + kStages, A_PREADY,
-       A_DPFULL, A_DSREADY, A_OFULL, A_OEMPTY, A_DRAIN, A_COUNT };
-
-constexpr int kv_smem(int boxes) { return 1024 + (2 + 2 * kStages) * boxes * kBoxBytes + kStages * 1024 + 8 * A_COUNT + 16; }
+// tensor memory: S^T (then P^T), dP^T (then dS^T), dV, dK.  One warp issues S_t and dV_t,
+// another dP_t and dK_t: P_t is formed while dP_t runs, dS_t while dV_t and S_{t+1} do,
+// and no wait of one chain holds up the other.
+constexpr int kQ = 3, kO = 2;  // stages of q and of do (whose rows' lse and delta come along)
+enum { A_KVFULL = 0, A_KVEMPTY, A_QFULL, A_QEMPTY = A_QFULL + kQ, A_QFIX = A_QEMPTY + kQ, A_DOFULL = A_QFIX + kQ,
+       A_DOEMPTY = A_DOFULL + kO, A_DOFIX = A_DOEMPTY + kO, A_VECFULL = A_DOFIX + kO, A_VECEMPTY = A_VECFULL + kO,
+       A_SFULL = A_VECEMPTY + kO, A_PREADY, A_DPFULL, A_DSREADY, A_OFULL, A_OEMPTY, A_DRAIN, A_RING = A_DRAIN + 2,
+       A_COUNT = A_RING + kRingBars };
 
 struct KvItem {
   Seq q;
   int kv_head, k0, first, tiles, steps;  // first query tile, query tiles of a head, of all heads
+  int end;
 };
-__device__ __forceinline__ bool kv_item(const AttArgs& p, int64_t i, KvItem& it) {
-  it.q = seq_of_slot<128>(p, static_cast<int>(i / p.Hk));
+constexpr int kKvBars = (8 * A_COUNT + 15) / 16 * 16, kKvMisc = 16 + static_cast<int>(sizeof(ItemRing<KvItem>));
+constexpr int kv_smem(int boxes) { return (2 + kQ + kO) * boxes * kBoxBytes + kO * 1024 + kKvBars + kKvMisc; }
+__device__ __forceinline__ bool kv_item(const AttArgs& p, int i, KvItem& it) {
+  it.q = seq_of_slot<128>(p, i / p.Hk);
   if (it.q.tile < 0) return false;
-  it.kv_head = static_cast<int>(i % p.Hk);
+  it.end = 0;
+  it.kv_head = i % p.Hk;
   it.k0 = 128 * it.q.tile;
   it.first = p.causal && it.k0 >= it.q.prefix ? it.q.tile : 0;
   it.tiles = (it.q.n + 127) / 128 - it.first;
   it.steps = it.tiles * (p.Hq / p.Hk);
   return true;
 }
-// Step t of an item: a query head and the first row of a query tile.
-__device__ __forceinline__ void kv_step(const AttArgs& p, const KvItem& it, int t, int& head, int& q0) {
-  head = it.kv_head * (p.Hq / p.Hk) + t / it.tiles;
-  q0 = 128 * (it.first + t % it.tiles);
-}
+// An item's steps: a query head and the first row of a query tile.
+struct KvStep {
+  int head, q0, left;
+  __device__ __forceinline__ KvStep(const AttArgs& p, const KvItem& it)
+      : head(it.kv_head * (p.Hq / p.Hk)), q0(128 * it.first), left(it.tiles) {}
+  __device__ __forceinline__ void next(const KvItem& it) {
+    q0 += 128;
+    if (--left == 0) {
+      ++head;
+      q0 = 128 * it.first;
+      left = it.tiles;
+    }
+  }
+};
 
-template <int kBoxes, bool kExtra>
+template <int kBoxes, int kForm>
 __global__ void __launch_bounds__(kThreads, 1)
     att_dkdv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const AttArgs p,
-                    const float2* stats, int64_t items) {
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+                    const float2* stats, int ask) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);  // (of 1024 bytes' alignment: there is no room to move up)
   constexpr uint32_t kTileBytes = kBoxes * kBoxBytes;
-  const uint32_t sk = base, sv = sk + kTileBytes, sq = sv + kTileBytes, sdo = sq + kStages * kTileBytes;
-  const uint32_t vec0 = sdo + kStages * kTileBytes;  // a stage's [2][128]: lse, delta
+  const uint32_t sk = raw, sv = sk + kTileBytes, sq = sv + kTileBytes, sdo = sq + kQ * kTileBytes;
+  const uint32_t vec0 = sdo + kO * kTileBytes;  // a stage's [2][128]: -lse, -delta
   float* vec = reinterpret_cast<float*>(smem_raw + (vec0 - raw));
-  const uint32_t bar0 = vec0 + kStages * 1024;
-  uint8_t* misc = smem_raw + (bar0 - raw) + 8 * A_COUNT;
+  const uint32_t bar0 = vec0 + kO * 1024;
+  uint8_t* misc = smem_raw + (bar0 - raw) + kKvBars;
+  ItemRing<KvItem>& ring = *reinterpret_cast<ItemRing<KvItem>*>(misc + 16);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
   const auto bar = [&](int i) { return bar0 + 8u * i; };
+  const RingAt ring_at{bar(A_RING)};
   const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < A_COUNT; ++i) {
-      const bool rows = i == A_PREADY || i == A_DSREADY || i == A_OEMPTY || (i >= A_VECEMPTY && i < A_VECEMPTY + kStages);
-      mbar_init(bar(i), rows ? kRowWarps : 1);
+    for (int i = 0; i < A_RING; ++i) {
+      const bool rows = i == A_PREADY || i == A_DSREADY || i == A_OEMPTY || (i >= A_VECEMPTY && i < A_VECEMPTY + kO);
+      const bool both = i == A_KVEMPTY || i == A_OFULL || (i >= A_DOEMPTY && i < A_DOEMPTY + kO);
+      mbar_init(bar(i), rows ? kRowWarps : both ? 2 : 1);
     }
+    init_ring(ring_at, kReaders);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -199,8 +197,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_desc(&map_v);
     tma_prefetch_desc(&map_do);
   }
-  zero_behind(p, const_cast<void*>(p.dk.x), p.dk.token_stride, p.dk.head_stride, p.Hk);
-  zero_behind(p, const_cast<void*>(p.dv.x), p.dv.token_stride, p.dv.head_stride, p.Hk);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -208,211 +204,245 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 384;
   const WaitCtl ctl{abort_flag, p.wait_limit_ns};
   KvItem it;
-  int head, q0;
 
   if (warp >= kTmaWarp) {
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
-      uint32_t n_kv = 0, n_q = 0;
+      uint32_t n_kv = 0;
+      Turn q, o;
       bool ok = true;
-      for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-        if (!kv_item(p, i, it)) continue;
+      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
         if (!(ok = mbar_wait_warp(bar(A_KVEMPTY), (n_kv++ & 1) ^ 1, ctl))) break;
         if (leader) {
           mbar_arrive_expect_tx(bar(A_KVFULL), 2 * kTileBytes);
           load_tile(sk, &map_k, bar(A_KVFULL), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + it.k0);
           load_tile(sv, &map_v, bar(A_KVFULL), kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + it.k0);
         }
-        for (int t = 0; t < it.steps; ++t, ++n_q) {
-          const int s = n_q % kStages;
-          kv_step(p, it, t, head, q0);
-          if (!(ok = mbar_wait_warp(bar(A_QEMPTY + s), (n_q / kStages & 1) ^ 1, ctl))) break;
-          if (leader) {
-            mbar_arrive_expect_tx(bar(A_QFULL + s), 2 * kTileBytes);
-            load_tile(sq + s * kTileBytes, &map_q, bar(A_QFULL + s), kBoxes, p.q.head_stride ? head : 0, it.q.start + q0);
-            load_tile(sdo + s * kTileBytes, &map_do, bar(A_QFULL + s), kBoxes, p.d_o.head_stride ? head : 0, it.q.start + q0);
+        KvStep at(p, it);
+        for (int t = 0; t < it.steps; ++t, at.next(it), q.next(kQ), o.next(kO)) {
+          float2 got[4];  // the rows' lse and delta, on their way while the stages are waited for
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = min(at.q0 + lane + 32 * e, it.q.n - 1);
+            got[e] = stats[static_cast<int64_t>(at.head) * p.T + it.q.start + r];
           }
+          if (!(ok = mbar_wait_warp(bar(A_QEMPTY + q.i), q.phase ^ 1, ctl))) break;
+          if (leader) {
+            mbar_arrive_expect_tx(bar(A_QFULL + q.i), kTileBytes);
+            load_tile(sq + q.i * kTileBytes, &map_q, bar(A_QFULL + q.i), kBoxes, p.q.head_stride ? at.head : 0, it.q.start + at.q0);
+          }
+          if (!(ok = mbar_wait_warp(bar(A_DOEMPTY + o.i), o.phase ^ 1, ctl))) break;
+          if (leader) {
+            mbar_arrive_expect_tx(bar(A_DOFULL + o.i), kTileBytes);
+            load_tile(sdo + o.i * kTileBytes, &map_do, bar(A_DOFULL + o.i), kBoxes, p.d_o.head_stride ? at.head : 0,
+                      it.q.start + at.q0);
+          }
+          if (!(ok = mbar_wait_warp(bar(A_VECEMPTY + o.i), o.phase ^ 1, ctl))) break;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            vec[o.i * 256 + lane + 32 * e] = -got[e].x;
+            vec[o.i * 256 + 128 + lane + 32 * e] = -got[e].y;
+          }
+          __syncwarp();
+          if (leader) mbar_arrive(bar(A_VECFULL + o.i));
           // the sequence's last rows: what follows them up to whole K steps is zeroed
-          const int rows = it.q.n - q0;
+          const int rows = it.q.n - at.q0;
           if (rows < 128 && rows % 16 != 0) {
-            if (!(ok = mbar_wait_warp(bar(A_QFULL + s), n_q / kStages & 1, ctl))) break;
-            zero_rows(sq + s * kTileBytes, kBoxes, rows, up16(rows));
-            zero_rows(sdo + s * kTileBytes, kBoxes, rows, up16(rows));
+            if (!(ok = mbar_wait_warp(bar(A_QFULL + q.i), q.phase, ctl) && mbar_wait_warp(bar(A_DOFULL + o.i), o.phase, ctl))) break;
+            zero_rows(sq + q.i * kTileBytes, kBoxes, rows, up16(rows));
+            zero_rows(sdo + o.i * kTileBytes, kBoxes, rows, up16(rows));
             fence_proxy_async_shared();
             __syncwarp();
-            if (leader) mbar_arrive(bar(A_FIX + s));
+            if (leader) {
+              mbar_arrive(bar(A_QFIX + q.i));
+              mbar_arrive(bar(A_DOFIX + o.i));
+            }
           }
         }
+        if (ok && leader) mbar_arrive(ring_at.issued());
       }
       if (!ok) let_copies_land();
       __syncwarp();
-    } else if (warp == kMmaWarp) {
+    } else if (warp < kItemWarp) {
       const bool leader = elect_one();
+      const bool first = warp == kMmaWarp;  // S and dV; the other dP and dK
       const int steps = (p.D + 15) / 16;
       const uint32_t id_out = idesc_bf16(128, 16 * steps, false, true);
-      uint32_t n_kv = 0, n_q = 0, fixed = 0, n = 0;
+      uint32_t n_kv = 0, n = 0, fixed = 0;
+      Turn q, o;  // of the step whose second product is next
       bool ok = true;
-      for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-        if (!kv_item(p, i, it)) continue;
+      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok); ++n_kv) {
         if (!(ok = mbar_wait_warp(bar(A_KVFULL), n_kv & 1, ctl))) break;
-        // (the last rows' tile is shorter)
-        const auto rows_of = [&](int t) {
-          kv_step(p, it, t, head, q0);
-          return min(128, it.q.n - q0);
+        KvStep at(p, it);
+        // (a wait takes some 130 cycles where nothing is waited for: one a step, for its
+        // second product and the next step's first)
+        if (!(ok = mbar_wait_warp(first ? bar(A_QFULL + q.i) : bar(A_DOFULL + o.i), first ? q.phase : o.phase, ctl))) break;
+        tc_fence_after();
+        int rows = min(128, it.q.n - at.q0);  // (a tile of a sequence's last rows is shorter)
+        const auto scores = [&](const Turn& qs) {
+          mma_rows(leader, t_s, sk, sq + qs.i * kTileBytes, idesc_bf16(128, up16(rows), false, false), steps);
+          if (leader) umma_commit(bar(A_SFULL));
         };
-        const auto scores = [&](int t) {
-          const int s = (n_q + t) % kStages;
-          if (!mbar_wait_warp(bar(A_QFULL + s), (n_q + t) / kStages & 1, ctl)) return false;
-          tc_fence_after();
-          const uint32_t id = idesc_bf16(128, up16(rows_of(t)), false, false);
+        const auto slopes = [&](const Turn& os) {
+          mma_rows(leader, t_dp, sv, sdo + os.i * kTileBytes, idesc_bf16(128, up16(rows), false, false), steps);
           if (leader) {
-            mma_rows(t_s, sk, sq + s * kTileBytes, id, steps);
-            umma_commit(bar(A_SFULL));
-          }
-          return true;
-        };
-        if (!(ok = scores(0))) break;
-        for (int t = 0; t < it.steps; ++t, ++n) {
-          const int s = (n_q + t) % kStages, rows = rows_of(t);
-          if (leader) {
-            mma_rows(t_dp, sv, sdo + s * kTileBytes, idesc_bf16(128, up16(rows), false, false), steps);
             umma_commit(bar(A_DPFULL));
+            umma_commit(bar(A_DOEMPTY + os.i));
           }
-          if (rows % 16 != 0) {
-            if (!(ok = mbar_wait_warp(bar(A_FIX + s), fixed >> s & 1, ctl))) break;
-            fixed ^= 1u << s;
-          }
+        };
+        if (first)
+          scores(q);
+        else
+          slopes(o);
+        for (int t = 0; t < it.steps; ++t, ++n) {
+          const bool more = t + 1 < it.steps;
+          Turn q2 = q, o2 = o;
+          q2.next(kQ);
+          o2.next(kO);
           if (t == 0 && !(ok = mbar_wait_warp(bar(A_OEMPTY), (n_kv & 1) ^ 1, ctl))) break;
-          if (!(ok = mbar_wait_warp(bar(A_PREADY), n & 1, ctl))) break;
-          tc_fence_after();
-          if (leader) mma_cols(t_dv, t_s, 64, sdo + s * kTileBytes, id_out, up16(rows) / 16, t > 0);
-          if (t + 1 < it.steps && !(ok = scores(t + 1))) break;
-          if (!(ok = mbar_wait_warp(bar(A_DSREADY), n & 1, ctl))) break;
-          tc_fence_after();
-          if (leader) {
-            mma_cols(t_dk, t_dp, 64, sq + s * kTileBytes, id_out, up16(rows) / 16, t > 0);
-            umma_commit(bar(A_QEMPTY + s));
+          if (rows % 16 != 0) {
+            const int i = first ? o.i : q.i;
+            if (!(ok = mbar_wait_warp(bar((first ? A_DOFIX : A_QFIX) + i), fixed >> i & 1, ctl))) break;
+            fixed ^= 1u << i;
           }
+          const int ks = up16(rows) / 16;
+          at.next(it);
+          rows = min(128, it.q.n - at.q0);
+          if (first) {
+            const Phase last[2] = {{bar(A_PREADY), n & 1}, {bar(A_DOFULL + o.i), o.phase}};
+            const Phase both[3] = {last[0], last[1], {bar(A_QFULL + q2.i), q2.phase}};
+            if (!(ok = more ? mbar_wait_warp(both, ctl) : mbar_wait_warp(last, ctl))) break;
+            tc_fence_after();
+            mma_cols(leader, t_dv, t_s, 64, sdo + o.i * kTileBytes, id_out, ks, t > 0);
+            if (leader) umma_commit(bar(A_DOEMPTY + o.i));
+            if (more) scores(q2);
+          } else {
+            const Phase last[2] = {{bar(A_DSREADY), n & 1}, {bar(A_QFULL + q.i), q.phase}};
+            const Phase both[3] = {last[0], last[1], {bar(A_DOFULL + o2.i), o2.phase}};
+            if (!(ok = more ? mbar_wait_warp(both, ctl) : mbar_wait_warp(last, ctl))) break;
+            tc_fence_after();
+            mma_cols(leader, t_dk, t_dp, 64, sq + q.i * kTileBytes, id_out, ks, t > 0);
+            if (leader) umma_commit(bar(A_QEMPTY + q.i));
+            if (more) slopes(o2);
+          }
+          q = q2;
+          o = o2;
         }
         if (!ok) break;
-        n_q += it.steps;
-        ++n_kv;
         if (leader) {
           umma_commit(bar(A_OFULL));
           umma_commit(bar(A_KVEMPTY));
         }
       }
-      drain_mmas(bar(A_DRAIN), leader, p.wait_limit_ns);
-    } else if (warp == kVecWarp) {
-      uint32_t n_q = 0;
-      bool ok = true;
-      for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-        if (!kv_item(p, i, it)) continue;
-        for (int t = 0; t < it.steps; ++t, ++n_q) {
-          const int s = n_q % kStages;
-          kv_step(p, it, t, head, q0);
-          float2 got[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = min(q0 + lane + 32 * e, it.q.n - 1);
-            got[e] = stats[static_cast<int64_t>(head) * p.T + it.q.start + r];
-          }
-          if (!(ok = mbar_wait_warp(bar(A_VECEMPTY + s), (n_q / kStages & 1) ^ 1, ctl))) break;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            vec[s * 256 + lane + 32 * e] = got[e].x;
-            vec[s * 256 + 128 + lane + 32 * e] = got[e].y;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(A_VECFULL + s));
-        }
-      }
+      drain_mmas(bar(A_DRAIN + (first ? 0 : 1)), leader, p.wait_limit_ns);
+    } else if (warp == kItemWarp) {
+      hand_out(ring, ring_at, ask, ctl, [&](int i, KvItem& item) { return kv_item(p, i, item); },
+               [&](int i) {
+                 const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
+                 if (i >= parts) return;
+                 zero_behind(p, p.dk, p.Hk, i, parts);
+                 zero_behind(p, p.dv, p.Hk, i, parts);
+               });
     }
   } else {
     regs_inc<kRegsRows>();
     const int half = warp >> 2;  // of the tile's query columns
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const float scale2 = p.scale * kAttLog2e;
+    const ScoreForm form(p);
     uint32_t n_q = 0, n_o = 0;
+    Turn o;
     bool ok = true;
-    for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-      if (!kv_item(p, i, it)) continue;
+    for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
       const int key = it.k0 + (warp & 3) * 32 + lane;
       const bool alone = first_row_alone(p, it.q);
-      for (int t = 0; t < it.steps; ++t, ++n_q) {
-        const int s = n_q % kStages;
-        kv_step(p, it, t, head, q0);
+      KvStep step(p, it);
+      for (int t = 0; t < it.steps; ++t, ++n_q, step.next(it), o.next(kO)) {
+        const int s = o.i, q0 = step.q0;
         // columns [lo, hi) of this half see the key
         const int at = q0 + 64 * half;
         const int lo = key >= it.q.n ? 64 : p.causal && key >= it.q.prefix ? key - at : 0, hi = it.q.n - at;
         const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < 64);
-        const float slope2 = kExtra && p.slopes ? p.slopes[head] * kAttLog2e : 0.f;
-        if (!(ok = mbar_wait_warp(bar(A_VECFULL + s), n_q / kStages & 1, ctl))) break;
+        const float slope2 = kForm != FORM_PLAIN && p.slopes ? p.slopes[step.head] * kAttLog2e : 0.f;
+        if (!(ok = mbar_wait_warp(bar(A_VECFULL + s), o.phase, ctl))) break;
         if (!(ok = mbar_wait_warp(bar(A_SFULL), n_q & 1, ctl))) break;
         tc_fence_after();
-        float pr[64];
-        [[maybe_unused]] float bend[kExtra ? 64 : 1];
-        {
-          uint32_t a[2][32];
+        uint64_t pr[32];  // pairs of columns
+        [[maybe_unused]] float bend[kForm == FORM_CAP ? 64 : 1];
+        [[maybe_unused]] const float far = static_cast<float>(at - key);
+        // (two copies of the loops: as one, the masks' instructions are issued for every tile)
+        const auto weights = [&](auto is_masked) {
+          uint32_t a[2][32], w[32];
           tmem_ld_32x32b_x32(t_s + lanes + 64 * half, a[0]);
           tmem_ld_32x32b_x32(t_s + lanes + 64 * half + 32, a[1]);
           tmem_ld_wait();
-          const float4* lse = reinterpret_cast<const float4*>(vec + s * 256 + 64 * half);
+          const ulonglong2* lse = reinterpret_cast<const ulonglong2*>(vec + s * 256 + 64 * half);
 #pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const float4 l4 = lse[c];
-            const float l[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int k = 4 * c + e;
-              float x = __uint_as_float(a[k >> 5][k & 31]);
-              if constexpr (kExtra) {
-                x = score2(p, x, slope2, fabsf(static_cast<float>(at + k - key)), bend[k]) - l[e];
-              } else {
-                x = fmaf(x, scale2, -l[e]);
+          for (int c = 0; c < 32; ++c) {
+            const int k = 2 * c;
+            const ulonglong2 l2 = lse[c / 2];
+            const uint64_t l = c & 1 ? l2.y : l2.x;
+            float x = __uint_as_float(a[k >> 5][k & 31]), y = __uint_as_float(a[k >> 5][(k & 31) + 1]);
+            if constexpr (kForm != FORM_PLAIN) {
+              float lx, ly, bx, by;
+              unpair(l, lx, ly);
+              x = form.at<kForm>(x, slope2, fabsf(far + k), bx) + lx;
+              y = form.at<kForm>(y, slope2, fabsf(far + (k + 1)), by) + ly;
+              if constexpr (kForm == FORM_CAP) {
+                bend[k] = bx;
+                bend[k + 1] = by;
               }
-              pr[k] = fast_exp2(x);
+            } else {
+              unpair(fma_pair(pair(x, y), pair(form.scale2, form.scale2), l), x, y);
             }
+            x = fast_exp2(x);
+            y = fast_exp2(y);
+            if constexpr (decltype(is_masked)::value) {
+              x = k >= lo && k < hi ? x : 0.f;
+              y = k + 1 >= lo && k + 1 < hi ? y : 0.f;
+            }
+            pr[c] = pair(x, y);
+            w[c] = pack_bf16x2(x, y);
           }
-          if (masked) {
-#pragma unroll
-            for (int k = 0; k < 64; ++k) pr[k] = k >= lo && k < hi ? pr[k] : 0.f;
-          }
-          uint32_t w[32];
-#pragma unroll
-          for (int k = 0; k < 32; ++k) w[k] = pack_bf16x2(pr[2 * k], pr[2 * k + 1]);
           tmem_st_32x32b_x32(t_s + lanes + 64 * half, w);
-        }
+        };
+        if (masked)
+          weights(std::true_type{});
+        else
+          weights(std::false_type{});
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(A_PREADY));
         if (!(ok = mbar_wait_warp(bar(A_DPFULL), n_q & 1, ctl))) break;
         tc_fence_after();
-        {
+        const auto slopes = [&](auto is_masked) {
           uint32_t a[2][32], w[32];
           tmem_ld_32x32b_x32(t_dp + lanes + 64 * half, a[0]);
           tmem_ld_32x32b_x32(t_dp + lanes + 64 * half + 32, a[1]);
           tmem_ld_wait();
-          const float4* del = reinterpret_cast<const float4*>(vec + s * 256 + 128 + 64 * half);
+          const ulonglong2* del = reinterpret_cast<const ulonglong2*>(vec + s * 256 + 128 + 64 * half);
 #pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const float4 d4 = del[c];
-            const float d[4] = {d4.x, d4.y, d4.z, d4.w};
-            float x[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int k = 4 * c + e;
-              x[e] = pr[k] * (__uint_as_float(a[k >> 5][k & 31]) - d[e]);
-              if constexpr (kExtra) x[e] *= bend[k];
-              if (masked) x[e] = k >= lo && k < hi && !(alone && at + k == 0) ? x[e] : 0.f;
+          for (int c = 0; c < 32; ++c) {
+            const int k = 2 * c;
+            const ulonglong2 d2 = del[c / 2];
+            const uint64_t dp = pair(__uint_as_float(a[k >> 5][k & 31]), __uint_as_float(a[k >> 5][(k & 31) + 1]));
+            uint64_t ds = mul_pair(pr[c], add_pair(dp, c & 1 ? d2.y : d2.x));
+            if constexpr (kForm == FORM_CAP) ds = mul_pair(ds, pair(bend[k], bend[k + 1]));
+            float x, y;
+            unpair(ds, x, y);
+            if constexpr (decltype(is_masked)::value) {
+              x = k >= lo && k < hi && !(alone && at + k == 0) ? x : 0.f;
+              y = k + 1 >= lo && k + 1 < hi ? y : 0.f;
             }
-            w[2 * c] = pack_bf16x2(x[0], x[1]);
-            w[2 * c + 1] = pack_bf16x2(x[2], x[3]);
+            w[c] = pack_bf16x2(x, y);
           }
           tmem_st_32x32b_x32(t_dp + lanes + 64 * half, w);
-        }
+        };
+        if (masked)
+          slopes(std::true_type{});
+        else
+          slopes(std::false_type{});
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -446,20 +476,25 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // --------------------------------------------------------------------- dq ---
-// tensor memory: S, two of dP (then dS), dQ.  Order of the MMAs: dP_j, S_{j+1}, dQ_j.
-enum { C_QFULL = 0, C_QEMPTY, C_KVFULL, C_KVEMPTY = C_KVFULL + kStages, C_FIX = C_KVEMPTY + kStages,
-       C_SFULL = C_FIX + kStages, C_SEMPTY, C_DPFULL, C_DSREADY, C_OFULL, C_OEMPTY, C_DRAIN, C_COUNT };
-
-constexpr int dq_smem(int boxes) { return 1024 + (2 + 2 * kStages) * boxes * kBoxBytes + 8 * C_COUNT + 16; }
+// tensor memory: S, two of dP (then dS), dQ.  One warp issues S_j, another dP_{j+1} and
+// dQ_j: the products of a tile do not wait for the rows of the one before.
+constexpr int kK = 3, kV = 2;  // stages of key and value tiles
+enum { C_QFULL = 0, C_QEMPTY, C_KFULL, C_KEMPTY = C_KFULL + kK, C_KFIX = C_KEMPTY + kK, C_VFULL = C_KFIX + kK,
+       C_VEMPTY = C_VFULL + kV, C_SFULL = C_VEMPTY + kV, C_SEMPTY, C_DPFULL, C_DSREADY = C_DPFULL + 2, C_OFULL, C_OEMPTY,
+       C_DRAIN, C_RING = C_DRAIN + 2, C_COUNT = C_RING + kRingBars };
 
 struct QItem {
   Seq q;
   int head, q0, seen, tiles;
+  int end;
 };
-__device__ __forceinline__ bool q_item(const AttArgs& p, int64_t i, QItem& it) {
-  it.q = seq_of_slot<128>(p, static_cast<int>(i / p.Hq));
+constexpr int kQBars = (8 * C_COUNT + 15) / 16 * 16, kQMisc = 16 + static_cast<int>(sizeof(ItemRing<QItem>));
+constexpr int dq_smem(int boxes) { return 1024 + (2 + kK + kV) * boxes * kBoxBytes + kQBars + kQMisc; }
+__device__ __forceinline__ bool q_item(const AttArgs& p, int i, QItem& it) {
+  it.q = seq_of_slot<128>(p, i / p.Hq);
   if (it.q.tile < 0) return false;
-  it.head = static_cast<int>(i % p.Hq);
+  it.end = 0;
+  it.head = i % p.Hq;
   // the longest rows first
   it.q0 = 128 * (p.causal ? (it.q.n + 127) / 128 - 1 - it.q.tile : it.q.tile);
   it.seen = keys_seen(p, it.q, min(it.q0 + 128, it.q.n) - 1);
@@ -467,24 +502,27 @@ __device__ __forceinline__ bool q_item(const AttArgs& p, int64_t i, QItem& it) {
   return true;
 }
 
-template <int kBoxes, bool kExtra>
+template <int kBoxes, int kForm>
 __global__ void __launch_bounds__(kThreads, 1)
     att_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const AttArgs p,
-                  const float2* stats, int64_t items) {
+                  const float2* stats, int ask) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   constexpr uint32_t kTileBytes = kBoxes * kBoxBytes;
-  const uint32_t sq = base, sdo = sq + kTileBytes, sk = sdo + kTileBytes, sv = sk + kStages * kTileBytes;
-  const uint32_t bar0 = sv + kStages * kTileBytes;
-  uint8_t* misc = smem_raw + (bar0 - raw) + 8 * C_COUNT;
+  const uint32_t sq = base, sdo = sq + kTileBytes, sk = sdo + kTileBytes, sv = sk + kK * kTileBytes;
+  const uint32_t bar0 = sv + kV * kTileBytes;
+  uint8_t* misc = smem_raw + (bar0 - raw) + kQBars;
+  ItemRing<QItem>& ring = *reinterpret_cast<ItemRing<QItem>*>(misc + 16);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
   const auto bar = [&](int i) { return bar0 + 8u * i; };
+  const RingAt ring_at{bar(C_RING)};
   const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C_COUNT; ++i) mbar_init(bar(i), i == C_SEMPTY || i == C_DSREADY || i == C_OEMPTY ? kRowWarps : 1);
+    for (int i = 0; i < C_RING; ++i) mbar_init(bar(i), i == C_SEMPTY || i == C_DSREADY || i == C_OEMPTY ? kRowWarps : i == C_QEMPTY ? 2 : 1);
+    init_ring(ring_at, kReaders);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -498,8 +536,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_desc(&map_v);
     tma_prefetch_desc(&map_do);
   }
-  check_offsets(p);
-  zero_behind(p, const_cast<void*>(p.dq.x), p.dq.token_stride, p.dq.head_stride, p.Hq);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -513,10 +549,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
-      uint32_t n_q = 0, n_kv = 0;
+      uint32_t n_q = 0;
+      Turn k, v;
       bool ok = true;
-      for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-        if (!q_item(p, i, it)) continue;
+      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
         const int kv = it.head / (p.Hq / p.Hk);
         if (!(ok = mbar_wait_warp(bar(C_QEMPTY), (n_q++ & 1) ^ 1, ctl))) break;
         if (leader) {
@@ -524,100 +560,115 @@ __global__ void __launch_bounds__(kThreads, 1)
           load_tile(sq, &map_q, bar(C_QFULL), kBoxes, p.q.head_stride ? it.head : 0, it.q.start + it.q0);
           load_tile(sdo, &map_do, bar(C_QFULL), kBoxes, p.d_o.head_stride ? it.head : 0, it.q.start + it.q0);
         }
-        for (int j = 0; j < it.tiles; ++j, ++n_kv) {
-          const int s = n_kv % kStages;
-          if (!(ok = mbar_wait_warp(bar(C_KVEMPTY + s), (n_kv / kStages & 1) ^ 1, ctl))) break;
+        for (int j = 0; j < it.tiles; ++j, k.next(kK), v.next(kV)) {
+          if (!(ok = mbar_wait_warp(bar(C_KEMPTY + k.i), k.phase ^ 1, ctl))) break;
           if (leader) {
-            mbar_arrive_expect_tx(bar(C_KVFULL + s), 2 * kTileBytes);
-            load_tile(sk + s * kTileBytes, &map_k, bar(C_KVFULL + s), kBoxes, p.k.head_stride ? kv : 0, it.q.start + 128 * j);
-            load_tile(sv + s * kTileBytes, &map_v, bar(C_KVFULL + s), kBoxes, p.v.head_stride ? kv : 0, it.q.start + 128 * j);
+            mbar_arrive_expect_tx(bar(C_KFULL + k.i), kTileBytes);
+            load_tile(sk + k.i * kTileBytes, &map_k, bar(C_KFULL + k.i), kBoxes, p.k.head_stride ? kv : 0, it.q.start + 128 * j);
+          }
+          if (!(ok = mbar_wait_warp(bar(C_VEMPTY + v.i), v.phase ^ 1, ctl))) break;
+          if (leader) {
+            mbar_arrive_expect_tx(bar(C_VFULL + v.i), kTileBytes);
+            load_tile(sv + v.i * kTileBytes, &map_v, bar(C_VFULL + v.i), kBoxes, p.v.head_stride ? kv : 0, it.q.start + 128 * j);
           }
           const int rows = it.seen - 128 * j;
           if (rows < 128 && rows % 16 != 0) {
-            if (!(ok = mbar_wait_warp(bar(C_KVFULL + s), n_kv / kStages & 1, ctl))) break;
-            zero_rows(sk + s * kTileBytes, kBoxes, rows, up16(rows));
+            if (!(ok = mbar_wait_warp(bar(C_KFULL + k.i), k.phase, ctl))) break;
+            zero_rows(sk + k.i * kTileBytes, kBoxes, rows, up16(rows));
             fence_proxy_async_shared();
             __syncwarp();
-            if (leader) mbar_arrive(bar(C_FIX + s));
+            if (leader) mbar_arrive(bar(C_KFIX + k.i));
           }
         }
+        if (ok && leader) mbar_arrive(ring_at.issued());
       }
       if (!ok) let_copies_land();
       __syncwarp();
-    } else if (warp == kMmaWarp) {
+    } else if (warp < kItemWarp) {
       const bool leader = elect_one();
+      const bool first = warp == kMmaWarp;  // S; the other dP and dQ
       const int steps = (p.D + 15) / 16;
       const uint32_t id_out = idesc_bf16(128, 16 * steps, false, true);
-      uint32_t n_q = 0, n_kv = 0, fixed = 0;
+      uint32_t n_q = 0, n = 0, fixed = 0;  // items, tiles
+      Turn k, v;
       bool ok = true;
-      for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-        if (!q_item(p, i, it)) continue;
+      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok); ++n_q) {
         if (!(ok = mbar_wait_warp(bar(C_QFULL), n_q & 1, ctl))) break;
         const auto cols_of = [&](int j) { return up16(min(128, it.seen - 128 * j)); };
-        const auto scores = [&](int j) {
-          const uint32_t n = n_kv + j;
-          if (!mbar_wait_warp(bar(C_KVFULL + n % kStages), n / kStages & 1, ctl)) return false;
-          if (!mbar_wait_warp(bar(C_SEMPTY), (n & 1) ^ 1, ctl)) return false;
-          tc_fence_after();
-          const uint32_t id = idesc_bf16(128, cols_of(j), false, false);
-          if (leader) {
-            mma_rows(t_s, sq, sk + n % kStages * kTileBytes, id, steps);
-            umma_commit(bar(C_SFULL));
+        if (first) {
+          for (int j = 0; j < it.tiles; ++j, ++n, k.next(kK)) {
+            const Phase of[2] = {{bar(C_KFULL + k.i), k.phase}, {bar(C_SEMPTY), (n & 1) ^ 1}};
+            if (!(ok = mbar_wait_warp(of, ctl))) break;
+            tc_fence_after();
+            mma_rows(leader, t_s, sq, sk + k.i * kTileBytes, idesc_bf16(128, cols_of(j), false, false), steps);
+            if (leader) umma_commit(bar(C_SFULL));
           }
-          return true;
-        };
-        if (!(ok = scores(0))) break;
-        for (int j = 0; j < it.tiles; ++j) {
-          const uint32_t n = n_kv + j;
-          const int s = n % kStages, cols = cols_of(j);
-          if (leader) {
-            mma_rows(t_dp(n), sdo, sv + s * kTileBytes, idesc_bf16(128, cols, false, false), steps);
-            umma_commit(bar(C_DPFULL));
+        } else {
+          const auto products = [&](int j) {  // dP of a tile, into the accumulator that dQ of the one two before has read
+            mma_rows(leader, t_dp(n + j), sdo, sv + v.i * kTileBytes, idesc_bf16(128, cols_of(j), false, false), steps);
+            if (leader) {
+              umma_commit(bar(C_DPFULL + ((n + j) & 1)));
+              umma_commit(bar(C_VEMPTY + v.i));
+            }
+            v.next(kV);
+          };
+          for (int j = 0; j < min(2, it.tiles); ++j) {
+            if (!(ok = mbar_wait_warp(bar(C_VFULL + v.i), v.phase, ctl))) break;
+            tc_fence_after();
+            products(j);
           }
-          if (j + 1 < it.tiles && !(ok = scores(j + 1))) break;
-          const int rows = it.seen - 128 * j;
-          if (rows < 128 && rows % 16 != 0) {
-            if (!(ok = mbar_wait_warp(bar(C_FIX + s), fixed >> s & 1, ctl))) break;
-            fixed ^= 1u << s;
+          if (!ok) break;
+          for (int j = 0; j < it.tiles; ++j, k.next(kK)) {
+            const bool more = j + 2 < it.tiles;
+            const int rows = it.seen - 128 * j;
+            if (j == 0 && !(ok = mbar_wait_warp(bar(C_OEMPTY), (n_q & 1) ^ 1, ctl))) break;
+            const Phase dq_of[2] = {{bar(C_DSREADY), (n + j) & 1}, {bar(C_KFULL + k.i), k.phase}};
+            const Phase all_of[3] = {dq_of[0], dq_of[1], {bar(C_VFULL + v.i), v.phase}};
+            if (!(ok = more ? mbar_wait_warp(all_of, ctl) : mbar_wait_warp(dq_of, ctl))) break;
+            if (rows < 128 && rows % 16 != 0) {
+              if (!(ok = mbar_wait_warp(bar(C_KFIX + k.i), fixed >> k.i & 1, ctl))) break;
+              fixed ^= 1u << k.i;
+            }
+            tc_fence_after();
+            mma_cols(leader, t_dq, t_dp(n + j), 64, sk + k.i * kTileBytes, id_out, cols_of(j) / 16, j > 0);
+            if (leader) umma_commit(bar(C_KEMPTY + k.i));
+            if (more) products(j + 2);
           }
-          if (j == 0 && !(ok = mbar_wait_warp(bar(C_OEMPTY), (n_q & 1) ^ 1, ctl))) break;
-          if (!(ok = mbar_wait_warp(bar(C_DSREADY), n & 1, ctl))) break;
-          tc_fence_after();
-          if (leader) {
-            mma_cols(t_dq, t_dp(n), 64, sk + s * kTileBytes, id_out, cols / 16, j > 0);
-            umma_commit(bar(C_KVEMPTY + s));
-          }
+          n += it.tiles;
+          if (ok && leader) umma_commit(bar(C_OFULL));
         }
         if (!ok) break;
-        n_kv += it.tiles;
-        ++n_q;
-        if (leader) {
-          umma_commit(bar(C_OFULL));
-          umma_commit(bar(C_QEMPTY));
-        }
+        if (leader) umma_commit(bar(C_QEMPTY));
       }
-      drain_mmas(bar(C_DRAIN), leader, p.wait_limit_ns);
+      drain_mmas(bar(C_DRAIN + (first ? 0 : 1)), leader, p.wait_limit_ns);
+    } else if (warp == kItemWarp) {
+      hand_out(ring, ring_at, ask, ctl, [&](int i, QItem& item) { return q_item(p, i, item); },
+               [&](int i) {
+                 if (i == 0) check_offsets(p);
+                 const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
+                 if (i < parts) zero_behind(p, p.dq, p.Hq, i, parts);
+               });
     }
   } else {
     regs_inc<kRegsRows>();
     const int half = warp >> 2;  // of the tile's key columns
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const float scale2 = p.scale * kAttLog2e;
+    const ScoreForm form(p);
     uint32_t n_kv = 0, n_o = 0;
     bool ok = true;
-    for (int64_t i = blockIdx.x; ok && i < items; i += gridDim.x) {
-      if (!q_item(p, i, it)) continue;
+    for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
       const int pos = it.q0 + (warp & 3) * 32 + lane, real = min(pos, it.q.n - 1);
       const float2 st = stats[static_cast<int64_t>(it.head) * p.T + it.q.start + real];
       const int lim = keys_seen(p, it.q, real);
       const bool alone = pos == 0 && first_row_alone(p, it.q);
-      const float slope2 = kExtra && p.slopes ? p.slopes[it.head] * kAttLog2e : 0.f;
+      const float slope2 = kForm != FORM_PLAIN && p.slopes ? p.slopes[it.head] * kAttLog2e : 0.f;
       for (int j = 0; j < it.tiles; ++j, ++n_kv) {
         const int at = 128 * j + 64 * half, here = lim - at;
         const bool masked = __any_sync(0xffffffffu, here < 64);
+        [[maybe_unused]] const float far = static_cast<float>(pos - at);
         if (!(ok = mbar_wait_warp(bar(C_SFULL), n_kv & 1, ctl))) break;
         tc_fence_after();
-        float pr[64];
+        uint64_t pr[32];
         {
           uint32_t a[2][32];
           tmem_ld_32x32b_x32(t_s + lanes + 64 * half, a[0]);
@@ -627,37 +678,48 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C_SEMPTY));
 #pragma unroll
-          for (int k = 0; k < 64; ++k) {
-            float x = __uint_as_float(a[k >> 5][k & 31]);
-            if constexpr (kExtra) {
-              float bend;
-              x = score2(p, x, slope2, fabsf(static_cast<float>(pos - at - k)), bend) - st.x;
-              pr[k] = fast_exp2(x) * bend;  // (p itself is not needed here)
+          for (int c = 0; c < 32; ++c) {
+            const int k = 2 * c;
+            float x = __uint_as_float(a[k >> 5][k & 31]), y = __uint_as_float(a[k >> 5][(k & 31) + 1]);
+            if constexpr (kForm != FORM_PLAIN) {
+              float bx, by;
+              x = form.at<kForm>(x, slope2, fabsf(far - k), bx) - st.x;
+              y = form.at<kForm>(y, slope2, fabsf(far - (k + 1)), by) - st.x;
+              pr[c] = pair(fast_exp2(x), fast_exp2(y));
+              if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], pair(bx, by));  // (p itself is not needed here)
             } else {
-              pr[k] = fast_exp2(fmaf(x, scale2, -st.x));
+              unpair(fma_pair(pair(x, y), pair(form.scale2, form.scale2), pair(-st.x, -st.x)), x, y);
+              pr[c] = pair(fast_exp2(x), fast_exp2(y));
             }
           }
         }
-        if (!(ok = mbar_wait_warp(bar(C_DPFULL), n_kv & 1, ctl))) break;
+        if (!(ok = mbar_wait_warp(bar(C_DPFULL + (n_kv & 1)), n_kv >> 1 & 1, ctl))) break;
         tc_fence_after();
-        {
+        // (two copies of the loop: as one, the masks' instructions are issued for every tile)
+        const auto slopes = [&](auto is_masked) {
           uint32_t a[2][32], w[32];
           const uint32_t td = t_dp(n_kv) + lanes + 64 * half;
           tmem_ld_32x32b_x32(td, a[0]);
           tmem_ld_32x32b_x32(td + 32, a[1]);
           tmem_ld_wait();
 #pragma unroll
-          for (int k = 0; k < 64; k += 2) {
-            float x = pr[k] * (__uint_as_float(a[k >> 5][k & 31]) - st.y);
-            float y = pr[k + 1] * (__uint_as_float(a[k >> 5][(k & 31) + 1]) - st.y);
-            if (masked) {
+          for (int c = 0; c < 32; ++c) {
+            const int k = 2 * c;
+            const uint64_t dp = pair(__uint_as_float(a[k >> 5][k & 31]), __uint_as_float(a[k >> 5][(k & 31) + 1]));
+            float x, y;
+            unpair(mul_pair(pr[c], add_pair(dp, pair(-st.y, -st.y))), x, y);
+            if constexpr (decltype(is_masked)::value) {
               x = k < here && !alone ? x : 0.f;
               y = k + 1 < here && !alone ? y : 0.f;
             }
-            w[k / 2] = pack_bf16x2(x, y);
+            w[c] = pack_bf16x2(x, y);
           }
           tmem_st_32x32b_x32(td, w);
-        }
+        };
+        if (masked)
+          slopes(std::true_type{});
+        else
+          slopes(std::false_type{});
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -684,15 +746,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-template <int kBoxes, bool kExtra>
+template <int kBoxes, int kForm>
 olive_status run_bwd(const Ctx& c, const AttArgs& a) {
   CUtensorMap mq, mk, mv, mdo;
   if (!encode_heads(&mq, a.q, a.T, a.Hq, a.D) || !encode_heads(&mk, a.k, a.T, a.Hk, a.D) ||
       !encode_heads(&mv, a.v, a.T, a.Hk, a.D) || !encode_heads(&mdo, a.d_o, a.T, a.Hq, a.D))
     return OLIVE_ERR_CUDA;
   static std::atomic<int> done_kv[kMaxDevices], done_q[kMaxDevices];
-  const auto dkdv = att_dkdv_kernel<kBoxes, kExtra>;
-  const auto dq = att_dq_kernel<kBoxes, kExtra>;
+  const auto dkdv = att_dkdv_kernel<kBoxes, kForm>;
+  const auto dq = att_dq_kernel<kBoxes, kForm>;
   constexpr int kSmemKv = kv_smem(kBoxes), kSmemQ = dq_smem(kBoxes);
   static_assert(kSmemKv <= 227 * 1024 && kSmemQ <= 227 * 1024, "shared memory");
   if (!set_smem_once(reinterpret_cast<const void*>(dkdv), kSmemKv, c.device, done_kv) ||
@@ -700,16 +762,17 @@ olive_status run_bwd(const Ctx& c, const AttArgs& a) {
     return OLIVE_ERR_CUDA;
   float2* stats = static_cast<float2*>(a.ws);
   const int64_t slots = att_slots(a.T, a.S, 128);
-  const auto grid = [&](int64_t items) { return static_cast<unsigned>(std::min<int64_t>(items, c.num_sms)); };
+  const auto ask = [&](int64_t items) { return when_to_ask(items, c.num_sms, a.T, a.S); };
   att_delta_kernel<<<static_cast<unsigned>(slots * a.Hq), kDeltaThreads, 0, c.stream>>>(a, stats);
-  dkdv<<<grid(slots * a.Hk), kThreads, kSmemKv, c.stream>>>(mq, mk, mv, mdo, a, stats, slots * a.Hk);
-  dq<<<grid(slots * a.Hq), kThreads, kSmemQ, c.stream>>>(mq, mk, mv, mdo, a, stats, slots * a.Hq);
+  dkdv<<<static_cast<unsigned>(slots * a.Hk), kThreads, kSmemKv, c.stream>>>(mq, mk, mv, mdo, a, stats, ask(slots * a.Hk));
+  dq<<<static_cast<unsigned>(slots * a.Hq), kThreads, kSmemQ, c.stream>>>(mq, mk, mv, mdo, a, stats, ask(slots * a.Hq));
   return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
 }
 
 template <int kBoxes>
 olive_status by_form(const Ctx& c, const AttArgs& a) {
-  return a.cap > 0.f || a.slopes ? run_bwd<kBoxes, true>(c, a) : run_bwd<kBoxes, false>(c, a);
+  if (a.cap > 0.f) return run_bwd<kBoxes, FORM_CAP>(c, a);
+  return a.slopes ? run_bwd<kBoxes, FORM_BIAS>(c, a) : run_bwd<kBoxes, FORM_PLAIN>(c, a);
 }
 
 }  // namespace

@@ -126,6 +126,21 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, co
     }
   }
 }
+// The same for several phases together: where all are complete it takes as long as one.
+struct Phase {
+  uint32_t bar, parity;
+};
+template <int kN>
+__device__ __forceinline__ bool mbar_wait_warp(const Phase (&of)[kN], const WaitCtl& ctl) {
+  bool done = true;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) done &= mbar_try_wait(of[i].bar, of[i].parity);
+  if (__all_sync(0xffffffffu, done)) return true;
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    if (!mbar_wait_warp(of[i].bar, of[i].parity, ctl)) return false;
+  return true;
+}
 // One lane of a converged warp, the same at every call.
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
@@ -158,6 +173,31 @@ __device__ __forceinline__ void grid_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// ------------------------------------------------- cluster launch control ---
+// A running block takes over a block of its grid that has not started: the answer (16
+// bytes, 16-byte aligned shared memory) comes with 16 bytes on the mbarrier.  One thread
+// asks; after an answer that none was left it must not ask again.
+__device__ __forceinline__ void take_block(uint32_t answer, uint32_t bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                   answer),
+               "r"(bar)
+               : "memory");
+}
+// The x index of the block taken over, or -1.
+__device__ __forceinline__ int taken_block(uint32_t answer) {
+  int x;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\t.reg .b32 y, z, w;\n\t"
+      "ld.shared.b128 a, [%1];\n\t"
+      "mov.b32 %0, -1;\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, y, z, w}, a;\n\t}"
+      : "=r"(x)
+      : "r"(answer)
+      : "memory");
+  return x;
+}
 
 // ------------------------------------------------------------------- TMA ---
 // 2-D tiled bulk tensor load global -> shared, completion counted in bytes on
@@ -529,6 +569,31 @@ __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
