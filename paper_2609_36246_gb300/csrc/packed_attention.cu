@@ -19,6 +19,7 @@
 // follows its maximum only when that is more than 8 (in log2) above, as O has to be
 // scaled then; until there P and the sum are relative to the old one, exactly.
 #include <algorithm>
+#include <type_traits>
 
 #include "packed_attention.cuh"
 
@@ -26,14 +27,14 @@ namespace olive {
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kRegsLaunch = 168, kRegsSoft = 224, kRegsRest = 56;
+constexpr int kRegsLaunch = 168, kRegsSoft = 208, kRegsRest = 88;
 static_assert(2 * kRegsSoft + kRegsRest <= 3 * kRegsLaunch, "the block's registers");
 constexpr int kK = 3, kV = 2;  // stages of key and value tiles
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kItemWarp = 11;
+constexpr int kTmaWarp = 0, kMmaWarp = 1, kItemWarp = 3, kRestWarps = 4;
 constexpr int kReaders = 10;
 constexpr float kLag = 8.f;
 enum { B_QFULL = 0, B_QEMPTY = 2, B_KFULL = 4, B_KEMPTY = B_KFULL + kK, B_VFULL = B_KEMPTY + kK, B_VEMPTY = B_VFULL + kV,
-       B_VFIX = B_VEMPTY + kV, B_SFULL = B_VFIX + kV, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 2, B_OEMPTY = B_OFULL + 2,
+       B_VFIX = B_VEMPTY + kV, B_SFULL = B_VFIX + kV, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
        B_DRAIN = B_OEMPTY + 2, B_RING, B_COUNT = B_RING + kRingBars };
 
 // An item's slots: heads, first rows and key tiles.
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < B_RING; ++i) {
       const auto among = [&](int first, int n) { return i >= first && i < first + n; };
-      mbar_init(bar(i), among(B_PREADY, 2) || among(B_OEMPTY, 2) ? 4 : 1);
+      mbar_init(bar(i), among(B_PREADY, 4) || among(B_OEMPTY, 2) ? 4 : 1);
     }
     init_ring(ring_at, kReaders);
     *abort_flag = 0;
@@ -113,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const auto t_o = [&](int a) { return tmem + 256u + 128u * a; };
   Item it;
 
-  if (warp >= kTmaWarp) {
+  if (warp < kRestWarps) {
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
@@ -168,59 +169,95 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (uint32_t n = 0; ok && next_item(ring, ring_at, n, it, ctl, ok);) {
         const int tiles = max(it.tiles[0], it.tiles[1]), seen = max(it.seen[0], it.seen[1]);
-        // Slot 0's products of a round, the waits for slot 1's and for the next round's
-        // tiles while those run, slot 1's.  (A wait takes some 130 cycles where nothing is
-        // waited for, and what is queued lasts little longer: all of them ahead of a
-        // round, its period is 3430 cycles.)
-        const auto fix_rows = [&](int j) {  // whether tile j's last rows are mended
-          const int rows = seen - 128 * j;
-          return rows < 128 && rows % 16 != 0;
-        };
+        // A round: O += P V of the tile before and S of this one, slot 0, then slot 1.
+        // (A wait takes some 100 cycles where nothing is waited for, and what is queued
+        // for the tensor pipe lasts 300: so tiles are waited for together with the rows,
+        // and P's second half while the first one's products run.)
         if (!(ok = mbar_wait_warp(bar(B_KFULL + k.i), k.phase, ctl))) break;
+        // rounds in which both slots have whole tiles, the first one apart
+        const int whole = min(it.seen[0], it.seen[1]) / 128;
+        const auto whole_rounds = [&](auto s_steps, int& j) {
+          constexpr int kS = decltype(s_steps)::value;
+          constexpr uint32_t id_s = idesc_bf16(128, 128, false, false);
+          const uint64_t dq[2] = {sdesc_sw128(sq, 16, 1024), sdesc_sw128(sq + kTileBytes, 16, 1024)};
+          for (; j < whole; ++j) {
+            const uint64_t dk = sdesc_sw128(sk + k.i * kTileBytes, 16, 1024), dv = sdesc_sw128(sv + v.i * kTileBytes, kBoxBytes, 1024);
+            Turn next_k = k;
+            next_k.next(kK);
+            const uint32_t more = j > 1 ? 1u : 0u;
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+              const Phase of[2] = {{bar(B_PREADY + 2 * a), n_p[a] & 1},
+                                   a == 0 ? Phase{bar(B_VFULL + v.i), v.phase} : Phase{bar(B_KFULL + next_k.i), next_k.phase}};
+              if (a == 0 || j + 1 < tiles ? !mbar_wait_warp(of, ctl) : !mbar_wait_warp(of[0].bar, of[0].parity, ctl)) return false;
+              tc_fence_after();
+              mma_cols_of<8, 0, 4>(leader, t_o(a), t_s(a), dv, id_out, more);
+              if (!mbar_wait_warp(bar(B_PREADY + 2 * a + 1), n_p[a]++ & 1, ctl)) return false;
+              tc_fence_after();
+              mma_cols_of<8, 4, 8>(leader, t_o(a), t_s(a), dv, id_out, 1u);
+              mma_rows_of<kS>(leader, t_s(a), dq[a], dk, id_s);
+              umma_commit_by(leader, bar(B_SFULL + a));
+              if (j == it.tiles[a] - 1) umma_commit_by(leader, bar(B_QEMPTY + a));
+            }
+            umma_commit_by(leader, bar(B_VEMPTY + v.i));
+            umma_commit_by(leader, bar(B_KEMPTY + k.i));
+            v.next(kV);
+            k = next_k;
+          }
+          return true;
+        };
         for (int j = 0; ok && j <= tiles; ++j) {
-          // v: the tile before, of this round's second products; k: this round's
-          Turn k2 = k;
-          if (j < tiles) k2.next(kK);
+          if (j == 1 && whole > 1 && (steps == 8 || steps == 4)) {
+            if (!(ok = mbar_wait_warp(bar(B_OEMPTY), (n_o[0]++ & 1) ^ 1, ctl) && mbar_wait_warp(bar(B_OEMPTY + 1), (n_o[1]++ & 1) ^ 1, ctl))) break;
+            ok = steps == 8 ? whole_rounds(std::integral_constant<int, 8>{}, j) : whole_rounds(std::integral_constant<int, 4>{}, j);
+            if (!ok) break;
+          }
+          Turn next_k = k;
+          if (j < tiles) next_k.next(kK);
+          bool have_v = false, have_k = j + 1 >= tiles;
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
-            const bool add = j > 0 && j <= it.tiles[a];
-            if (add) {  // O += P V of the tile before
+            if (j > 0 && j <= it.tiles[a]) {
               if (j == 1 && !(ok = mbar_wait_warp(bar(B_OEMPTY + a), (n_o[a]++ & 1) ^ 1, ctl))) break;
-              if (!(ok = mbar_wait_warp(bar(B_PREADY + a), n_p[a]++ & 1, ctl))) break;
+              const Phase rows = {bar(B_PREADY + 2 * a), n_p[a] & 1};
+              if (!have_v) {
+                const Phase of[2] = {rows, {bar(B_VFULL + v.i), v.phase}};
+                if (!(ok = mbar_wait_warp(of, ctl))) break;
+                const int left = seen - 128 * (j - 1);
+                if (left < 128 && left % 16 != 0) {
+                  if (!(ok = mbar_wait_warp(bar(B_VFIX + v.i), fixed >> v.i & 1, ctl))) break;
+                  fixed ^= 1u << v.i;
+                }
+                have_v = true;
+              } else if (!have_k) {
+                const Phase of[2] = {rows, {bar(B_KFULL + next_k.i), next_k.phase}};
+                if (!(ok = mbar_wait_warp(of, ctl))) break;
+                have_k = true;
+              } else if (!(ok = mbar_wait_warp(rows.bar, rows.parity, ctl))) {
+                break;
+              }
               tc_fence_after();
               const int ks = up16(min(128, it.seen[a] - 128 * (j - 1))) / 16;
-              mma_cols(leader, t_o(a), t_s(a), 32, sv + v.i * kTileBytes, id_out, ks, j > 1);
-              if (leader && j == it.tiles[a]) umma_commit(bar(B_OFULL + a));
+              if (!(ok = mbar_wait_warp(bar(B_PREADY + 2 * a + 1), n_p[a]++ & 1, ctl))) break;
+              tc_fence_after();
+              mma_cols<8>(leader, t_o(a), t_s(a), sv + v.i * kTileBytes, id_out, ks, j > 1);
+              if (j == it.tiles[a]) umma_commit_by(leader, bar(B_OFULL + a));
             }
-            if (j < it.tiles[a]) {  // S of this one
+            if (j < it.tiles[a]) {
               if (j == 0 && !(ok = mbar_wait_warp(bar(B_QFULL + a), n_q[a]++ & 1, ctl))) break;
               tc_fence_after();
               const uint32_t id = idesc_bf16(128, up16(min(128, it.seen[a] - 128 * j)), false, false);
               mma_rows(leader, t_s(a), sq + a * kTileBytes, sk + k.i * kTileBytes, id, steps);
-              if (leader) {
-                umma_commit(bar(B_SFULL + a));
-                if (j == it.tiles[a] - 1) umma_commit(bar(B_QEMPTY + a));
-              }
-            }
-            if (a == 0 && j < tiles) {
-              // the next round's tiles: V of this one, K of the next
-              Turn v2 = v;
-              if (j > 0) v2.next(kV);
-              const Phase next[2] = {{bar(B_VFULL + v2.i), v2.phase},
-                                     {bar(B_KFULL + (j + 1 < tiles ? k2.i : k.i)), j + 1 < tiles ? k2.phase : k.phase}};
-              if (!(ok = mbar_wait_warp(next, ctl))) break;
-              if (fix_rows(j)) {
-                if (!(ok = mbar_wait_warp(bar(B_VFIX + v2.i), fixed >> v2.i & 1, ctl))) break;
-                fixed ^= 1u << v2.i;
-              }
+              umma_commit_by(leader, bar(B_SFULL + a));
+              if (j == it.tiles[a] - 1) umma_commit_by(leader, bar(B_QEMPTY + a));
             }
           }
-          if (ok && leader) {
-            if (j > 0) umma_commit(bar(B_VEMPTY + v.i));
-            if (j < tiles) umma_commit(bar(B_KEMPTY + k.i));
-          }
+          if (!ok) break;
+          if (j > 0) umma_commit_by(leader, bar(B_VEMPTY + v.i));
+          if (j < tiles) umma_commit_by(leader, bar(B_KEMPTY + k.i));
           if (j > 0) v.next(kV);
-          k = k2;
+          k = next_k;
+          if (!have_k && !(ok = mbar_wait_warp(bar(B_KFULL + k.i), k.phase, ctl))) break;
         }
       }
       drain_mmas(bar(B_DRAIN), leader, p.wait_limit_ns);
@@ -239,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     regs_inc<kRegsSoft>();
-    const int a = warp >> 2;
+    const int a = (warp - kRestWarps) >> 2;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const int row = (warp & 3) * 32 + lane;
     const uint32_t ts = t_s(a) + lanes, to = t_o(a) + lanes;
@@ -319,16 +356,16 @@ __global__ void __launch_bounds__(kThreads, 1)
             w[e] = pack_bf16x2(x, y);
           }
           tmem_st_32x32b_x32(ts + 32 * h, w);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_PREADY + 2 * a + h));
         }
         {
           float x, y;
           unpair(add_pair(part[0], part[1]), x, y);
           sum = x + y;
         }
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_PREADY + a));
       }
       if (!ok) break;
       if (!(ok = mbar_wait_warp(bar(B_OFULL + a), n_o++ & 1, ctl))) break;

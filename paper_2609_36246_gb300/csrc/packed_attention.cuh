@@ -2,6 +2,8 @@
 // sequences share: the work's tiles, the scores' forms and the operands in shared memory.
 #pragma once
 
+#include <type_traits>
+
 #include "internal.h"
 #include "sm103.cuh"
 
@@ -229,27 +231,51 @@ __device__ __forceinline__ void drain_mmas(uint32_t bar, bool leader, uint64_t l
 __device__ __forceinline__ int up16(int n) { return (n + 15) & ~15; }
 
 // The products of a whole warp, `leader` the lane that issues: with the loop and the
-// operands the warp's they stay in uniform registers (sm103.cuh, mbar_wait_warp).
+// operands the warp's they stay in uniform registers (sm103.cuh, mbar_wait_warp).  An MMA
+// takes some 33 cycles to issue and 65 to run; a bound that is looked at before each
+// doubles the first, so every number of K steps has its own copy.
+//
 // S = A B^T over a head's width: both operands tiles of rows (K-major).
-__device__ __forceinline__ void mma_rows(bool leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
-  const uint64_t da = sdesc_sw128(a, 16, 1024), db = sdesc_sw128(b, 16, 1024);
+template <int kSteps>
+__device__ __forceinline__ void mma_rows_of(bool leader, uint32_t d, uint64_t da, uint64_t db, uint32_t idesc) {
 #pragma unroll
-  for (int k = 0; k < kMaxAttDim / 16; ++k) {
-    if (k >= steps) break;
+  for (int k = 0; k < kSteps; ++k) {
     const uint32_t at = (k >> 2) * (kBoxBytes >> 4) + (k & 3) * 2;
-    if (leader) umma_bf16(d, da + at, db + at, idesc, k > 0 ? 1u : 0u);
+    umma_bf16_by(leader, d, da + at, db + at, idesc, k > 0 ? 1u : 0u);
   }
 }
-// D (+)= A B with A [128, rows of B] in tensor memory and B a tile of rows (MN-major);
-// A's second 64 columns lie `half` tensor memory columns behind its first.
-__device__ __forceinline__ void mma_cols(bool leader, uint32_t d, uint32_t a, int half, uint32_t b, uint32_t idesc, int steps, bool more) {
+// f of a number of K steps, 1 to 8, as a constant.
+template <class F>
+__device__ __forceinline__ void by_steps(int steps, F f) {
+  if (steps == 8) return f(std::integral_constant<int, 8>{});
+  switch (steps) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 3: return f(std::integral_constant<int, 3>{});
+    case 4: return f(std::integral_constant<int, 4>{});
+    case 5: return f(std::integral_constant<int, 5>{});
+    case 6: return f(std::integral_constant<int, 6>{});
+    case 7: return f(std::integral_constant<int, 7>{});
+  }
+}
+__device__ __forceinline__ void mma_rows(bool leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps) {
+  const uint64_t da = sdesc_sw128(a, 16, 1024), db = sdesc_sw128(b, 16, 1024);
+  by_steps(steps, [&](auto n) { mma_rows_of<decltype(n)::value>(leader, d, da, db, idesc); });
+}
+// D (+)= A B with A [128, rows of B] in tensor memory and B a tile of rows (MN-major).  kRun K steps of A are side by side, the next run 16 kRun columns on.
+template <int kRun>
+__device__ __forceinline__ uint32_t a_step(int k) { return (k / kRun) * (16 * kRun) + (k % kRun) * 8; }
+template <int kRun, int kFrom, int kTo>
+__device__ __forceinline__ void mma_cols_of(bool leader, uint32_t d, uint32_t a, uint64_t db, uint32_t idesc, uint32_t first) {
+#pragma unroll
+  for (int k = kFrom; k < kTo; ++k)
+    umma_bf16_ta_by(leader, d, a + a_step<kRun>(k), db + k * 128, idesc, k > 0 ? 1u : first);
+}
+template <int kRun>
+__device__ __forceinline__ void mma_cols(bool leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, int steps, bool more) {
   const uint64_t db = sdesc_sw128(b, kBoxBytes, 1024);
   const uint32_t first = more ? 1u : 0u;
-#pragma unroll
-  for (int k = 0; k < kAttTile / 16; ++k) {
-    if (k >= steps) break;
-    if (leader) umma_bf16_ta(d, a + (k >> 2) * half + (k & 3) * 8, db + k * 128, idesc, k > 0 ? 1u : first);
-  }
+  by_steps(steps, [&](auto n) { mma_cols_of<kRun, 0, decltype(n)::value>(leader, d, a, db, idesc, first); });
 }
 
 }  // namespace olive

@@ -18,12 +18,14 @@
 namespace olive {
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kRegsLaunch = 168, kRegsRows = 224, kRegsRest = 56;
-static_assert(2 * kRegsRows + kRegsRest <= 3 * kRegsLaunch, "the block's registers");
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kItemWarp = 11;  // (two warps issue MMAs)
-constexpr int kReaders = 11;
-constexpr int kRowWarps = 8;
+// Rows of a tile: 16 warps, four to a quarter of its columns.  (With eight, a half each,
+// their chain of waits, loads and stores is longer than the MMAs beside it.)
+constexpr int kRowWarps = 16, kCols = kAttTile / (kRowWarps / 4);
+constexpr int kTmaWarp = 0, kMmaWarp = 1, kItemWarp = 3, kRestWarps = 4;
+constexpr int kThreads = 32 * 20;
+constexpr int kReaders = kRowWarps + 2;
+constexpr int kRegsLaunch = 96, kRegsRows = 104, kRegsRest = 64;
+static_assert(4 * kRegsRows + kRegsRest <= 5 * kRegsLaunch, "the block's registers");
 
 // ------------------------------------------------------------------ delta ---
 // Rows that see up to this many keys have their delta from the keys themselves: <do, o>
@@ -115,13 +117,13 @@ __device__ __forceinline__ void store_cols(uint32_t taddr, __nv_bfloat16* row, b
 }
 
 // ----------------------------------------------------------------- dk, dv ---
-// tensor memory: S^T (then P^T), dP^T (then dS^T), dV, dK.  One warp issues S_t and dV_t,
-// another dP_t and dK_t: P_t is formed while dP_t runs, dS_t while dV_t and S_{t+1} do,
-// and no wait of one chain holds up the other.
+// tensor memory: S^T (then P^T), dP^T (then dS^T), dV, dK.  The MMAs run in the order
+// dV_t, S_{t+1}, dK_t, dP_{t+1}: P_{t+1} is formed while the last two run, dS_t while the
+// first two do.  (A warp for each pair mixes them: all four then end late.)
 constexpr int kQ = 3, kO = 2;  // stages of q and of do (whose rows' lse and delta come along)
 enum { A_KVFULL = 0, A_KVEMPTY, A_QFULL, A_QEMPTY = A_QFULL + kQ, A_QFIX = A_QEMPTY + kQ, A_DOFULL = A_QFIX + kQ,
        A_DOEMPTY = A_DOFULL + kO, A_DOFIX = A_DOEMPTY + kO, A_VECFULL = A_DOFIX + kO, A_VECEMPTY = A_VECFULL + kO,
-       A_SFULL = A_VECEMPTY + kO, A_PREADY, A_DPFULL, A_DSREADY, A_OFULL, A_OEMPTY, A_DRAIN, A_RING = A_DRAIN + 2,
+       A_SFULL = A_VECEMPTY + kO, A_PREADY, A_DPFULL, A_DSREADY, A_OFULL, A_OEMPTY, A_DRAIN, A_RING,
        A_COUNT = A_RING + kRingBars };
 
 struct KvItem {
@@ -180,8 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < A_RING; ++i) {
       const bool rows = i == A_PREADY || i == A_DSREADY || i == A_OEMPTY || (i >= A_VECEMPTY && i < A_VECEMPTY + kO);
-      const bool both = i == A_KVEMPTY || i == A_OFULL || (i >= A_DOEMPTY && i < A_DOEMPTY + kO);
-      mbar_init(bar(i), rows ? kRowWarps : both ? 2 : 1);
+      mbar_init(bar(i), rows ? kRowWarps : 1);
     }
     init_ring(ring_at, kReaders);
     *abort_flag = 0;
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const WaitCtl ctl{abort_flag, p.wait_limit_ns};
   KvItem it;
 
-  if (warp >= kTmaWarp) {
+  if (warp < kRestWarps) {
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
@@ -264,78 +265,65 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) let_copies_land();
       __syncwarp();
-    } else if (warp < kItemWarp) {
+    } else if (warp == kMmaWarp) {
       const bool leader = elect_one();
-      const bool first = warp == kMmaWarp;  // S and dV; the other dP and dK
       const int steps = (p.D + 15) / 16;
       const uint32_t id_out = idesc_bf16(128, 16 * steps, false, true);
-      uint32_t n_kv = 0, n = 0, fixed = 0;
-      Turn q, o;  // of the step whose second product is next
+      uint32_t n_kv = 0, n = 0, q_fixed = 0, o_fixed = 0;
+      Turn q, o;  // of the step whose second products are next
       bool ok = true;
       for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok); ++n_kv) {
-        if (!(ok = mbar_wait_warp(bar(A_KVFULL), n_kv & 1, ctl))) break;
         KvStep at(p, it);
-        // (a wait takes some 130 cycles where nothing is waited for: one a step, for its
-        // second product and the next step's first)
-        if (!(ok = mbar_wait_warp(first ? bar(A_QFULL + q.i) : bar(A_DOFULL + o.i), first ? q.phase : o.phase, ctl))) break;
-        tc_fence_after();
         int rows = min(128, it.q.n - at.q0);  // (a tile of a sequence's last rows is shorter)
         const auto scores = [&](const Turn& qs) {
           mma_rows(leader, t_s, sk, sq + qs.i * kTileBytes, idesc_bf16(128, up16(rows), false, false), steps);
-          if (leader) umma_commit(bar(A_SFULL));
+          umma_commit_by(leader, bar(A_SFULL));
         };
         const auto slopes = [&](const Turn& os) {
           mma_rows(leader, t_dp, sv, sdo + os.i * kTileBytes, idesc_bf16(128, up16(rows), false, false), steps);
-          if (leader) {
-            umma_commit(bar(A_DPFULL));
-            umma_commit(bar(A_DOEMPTY + os.i));
-          }
+          umma_commit_by(leader, bar(A_DPFULL));
         };
-        if (first)
-          scores(q);
-        else
-          slopes(o);
+        const Phase begin[3] = {{bar(A_KVFULL), n_kv & 1}, {bar(A_QFULL + q.i), q.phase}, {bar(A_DOFULL + o.i), o.phase}};
+        if (!(ok = mbar_wait_warp(begin, ctl))) break;
+        tc_fence_after();
+        scores(q);
+        slopes(o);
+        if (!(ok = mbar_wait_warp(bar(A_OEMPTY), (n_kv & 1) ^ 1, ctl))) break;
         for (int t = 0; t < it.steps; ++t, ++n) {
           const bool more = t + 1 < it.steps;
           Turn q2 = q, o2 = o;
           q2.next(kQ);
           o2.next(kO);
-          if (t == 0 && !(ok = mbar_wait_warp(bar(A_OEMPTY), (n_kv & 1) ^ 1, ctl))) break;
-          if (rows % 16 != 0) {
-            const int i = first ? o.i : q.i;
-            if (!(ok = mbar_wait_warp(bar((first ? A_DOFIX : A_QFIX) + i), fixed >> i & 1, ctl))) break;
-            fixed ^= 1u << i;
-          }
           const int ks = up16(rows) / 16;
+          if (rows % 16 != 0) {
+            const Phase fix[2] = {{bar(A_DOFIX + o.i), o_fixed >> o.i & 1}, {bar(A_QFIX + q.i), q_fixed >> q.i & 1}};
+            if (!(ok = mbar_wait_warp(fix, ctl))) break;
+            o_fixed ^= 1u << o.i;
+            q_fixed ^= 1u << q.i;
+          }
           at.next(it);
           rows = min(128, it.q.n - at.q0);
-          if (first) {
-            const Phase last[2] = {{bar(A_PREADY), n & 1}, {bar(A_DOFULL + o.i), o.phase}};
-            const Phase both[3] = {last[0], last[1], {bar(A_QFULL + q2.i), q2.phase}};
-            if (!(ok = more ? mbar_wait_warp(both, ctl) : mbar_wait_warp(last, ctl))) break;
-            tc_fence_after();
-            mma_cols(leader, t_dv, t_s, 64, sdo + o.i * kTileBytes, id_out, ks, t > 0);
-            if (leader) umma_commit(bar(A_DOEMPTY + o.i));
-            if (more) scores(q2);
-          } else {
-            const Phase last[2] = {{bar(A_DSREADY), n & 1}, {bar(A_QFULL + q.i), q.phase}};
-            const Phase both[3] = {last[0], last[1], {bar(A_DOFULL + o2.i), o2.phase}};
-            if (!(ok = more ? mbar_wait_warp(both, ctl) : mbar_wait_warp(last, ctl))) break;
-            tc_fence_after();
-            mma_cols(leader, t_dk, t_dp, 64, sq + q.i * kTileBytes, id_out, ks, t > 0);
-            if (leader) umma_commit(bar(A_QEMPTY + q.i));
-            if (more) slopes(o2);
-          }
+          // (one wait for what two products need: 100 cycles where nothing is waited for)
+          const Phase with_p[2] = {{bar(A_PREADY), n & 1}, {bar(A_QFULL + q2.i), q2.phase}};
+          if (!(ok = more ? mbar_wait_warp(with_p, ctl) : mbar_wait_warp(with_p[0].bar, with_p[0].parity, ctl))) break;
+          tc_fence_after();
+          mma_cols<2>(leader, t_dv, t_s, sdo + o.i * kTileBytes, id_out, ks, t > 0);
+          umma_commit_by(leader, bar(A_DOEMPTY + o.i));
+          if (more) scores(q2);
+          const Phase with_ds[2] = {{bar(A_DSREADY), n & 1}, {bar(A_DOFULL + o2.i), o2.phase}};
+          if (!(ok = more ? mbar_wait_warp(with_ds, ctl) : mbar_wait_warp(with_ds[0].bar, with_ds[0].parity, ctl))) break;
+          tc_fence_after();
+          mma_cols<2>(leader, t_dk, t_dp, sq + q.i * kTileBytes, id_out, ks, t > 0);
+          umma_commit_by(leader, bar(A_QEMPTY + q.i));
+          if (more) slopes(o2);
           q = q2;
           o = o2;
         }
         if (!ok) break;
-        if (leader) {
-          umma_commit(bar(A_OFULL));
-          umma_commit(bar(A_KVEMPTY));
-        }
+        umma_commit_by(leader, bar(A_OFULL));
+        umma_commit_by(leader, bar(A_KVEMPTY));
       }
-      drain_mmas(bar(A_DRAIN + (first ? 0 : 1)), leader, p.wait_limit_ns);
+      drain_mmas(bar(A_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
       hand_out(ring, ring_at, ask, ctl, [&](int i, KvItem& item) { return kv_item(p, i, item); },
                [&](int i) {
@@ -347,8 +335,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     regs_inc<kRegsRows>();
-    const int half = warp >> 2;  // of the tile's query columns
+    const int part = (warp - kRestWarps) >> 2;  // of the tile's query columns
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = t_s + lanes + kCols * part, td = t_dp + lanes + kCols * part;
     const ScoreForm form(p);
     uint32_t n_q = 0, n_o = 0;
     Turn o;
@@ -358,40 +347,35 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool alone = first_row_alone(p, it.q);
       KvStep step(p, it);
       for (int t = 0; t < it.steps; ++t, ++n_q, step.next(it), o.next(kO)) {
-        const int s = o.i, q0 = step.q0;
-        // columns [lo, hi) of this half see the key
-        const int at = q0 + 64 * half;
-        const int lo = key >= it.q.n ? 64 : p.causal && key >= it.q.prefix ? key - at : 0, hi = it.q.n - at;
-        const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < 64);
+        // columns [lo, hi) of this part see the key
+        const int at = step.q0 + kCols * part;
+        const int lo = key >= it.q.n ? kCols : p.causal && key >= it.q.prefix ? key - at : 0, hi = it.q.n - at;
+        const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < kCols);
         const float slope2 = kForm != FORM_PLAIN && p.slopes ? p.slopes[step.head] * kAttLog2e : 0.f;
-        if (!(ok = mbar_wait_warp(bar(A_VECFULL + s), o.phase, ctl))) break;
-        if (!(ok = mbar_wait_warp(bar(A_SFULL), n_q & 1, ctl))) break;
-        tc_fence_after();
-        uint64_t pr[32];  // pairs of columns
-        [[maybe_unused]] float bend[kForm == FORM_CAP ? 64 : 1];
         [[maybe_unused]] const float far = static_cast<float>(at - key);
+        const float* stage = vec + o.i * 256 + kCols * part;
+        const Phase of[2] = {{bar(A_VECFULL + o.i), o.phase}, {bar(A_SFULL), n_q & 1}};
+        if (!(ok = mbar_wait_warp(of, ctl))) break;
+        tc_fence_after();
+        uint64_t pr[kCols / 2];  // pairs of columns: p, times the cap's derivative
         // (two copies of the loops: as one, the masks' instructions are issued for every tile)
         const auto weights = [&](auto is_masked) {
-          uint32_t a[2][32], w[32];
-          tmem_ld_32x32b_x32(t_s + lanes + 64 * half, a[0]);
-          tmem_ld_32x32b_x32(t_s + lanes + 64 * half + 32, a[1]);
+          uint32_t a[32], w[16];
+          tmem_ld_32x32b_x32(ts, a);
           tmem_ld_wait();
-          const ulonglong2* lse = reinterpret_cast<const ulonglong2*>(vec + s * 256 + 64 * half);
+          const ulonglong2* lse = reinterpret_cast<const ulonglong2*>(stage);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
+          for (int c = 0; c < kCols / 2; ++c) {
             const int k = 2 * c;
             const ulonglong2 l2 = lse[c / 2];
             const uint64_t l = c & 1 ? l2.y : l2.x;
-            float x = __uint_as_float(a[k >> 5][k & 31]), y = __uint_as_float(a[k >> 5][(k & 31) + 1]);
+            float x = __uint_as_float(a[k]), y = __uint_as_float(a[k + 1]);
+            [[maybe_unused]] float bx, by;
             if constexpr (kForm != FORM_PLAIN) {
-              float lx, ly, bx, by;
+              float lx, ly;
               unpair(l, lx, ly);
               x = form.at<kForm>(x, slope2, fabsf(far + k), bx) + lx;
               y = form.at<kForm>(y, slope2, fabsf(far + (k + 1)), by) + ly;
-              if constexpr (kForm == FORM_CAP) {
-                bend[k] = bx;
-                bend[k + 1] = by;
-              }
             } else {
               unpair(fma_pair(pair(x, y), pair(form.scale2, form.scale2), l), x, y);
             }
@@ -402,9 +386,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               y = k + 1 >= lo && k + 1 < hi ? y : 0.f;
             }
             pr[c] = pair(x, y);
+            if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], pair(bx, by));
             w[c] = pack_bf16x2(x, y);
           }
-          tmem_st_32x32b_x32(t_s + lanes + 64 * half, w);
+          tmem_st_32x32b_x16(ts, w);
         };
         if (masked)
           weights(std::true_type{});
@@ -417,27 +402,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!(ok = mbar_wait_warp(bar(A_DPFULL), n_q & 1, ctl))) break;
         tc_fence_after();
         const auto slopes = [&](auto is_masked) {
-          uint32_t a[2][32], w[32];
-          tmem_ld_32x32b_x32(t_dp + lanes + 64 * half, a[0]);
-          tmem_ld_32x32b_x32(t_dp + lanes + 64 * half + 32, a[1]);
+          uint32_t a[32], w[16];
+          tmem_ld_32x32b_x32(td, a);
           tmem_ld_wait();
-          const ulonglong2* del = reinterpret_cast<const ulonglong2*>(vec + s * 256 + 128 + 64 * half);
+          const ulonglong2* del = reinterpret_cast<const ulonglong2*>(stage + 128);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
+          for (int c = 0; c < kCols / 2; ++c) {
             const int k = 2 * c;
             const ulonglong2 d2 = del[c / 2];
-            const uint64_t dp = pair(__uint_as_float(a[k >> 5][k & 31]), __uint_as_float(a[k >> 5][(k & 31) + 1]));
-            uint64_t ds = mul_pair(pr[c], add_pair(dp, c & 1 ? d2.y : d2.x));
-            if constexpr (kForm == FORM_CAP) ds = mul_pair(ds, pair(bend[k], bend[k + 1]));
             float x, y;
-            unpair(ds, x, y);
+            unpair(mul_pair(pr[c], add_pair(pair(__uint_as_float(a[k]), __uint_as_float(a[k + 1])), c & 1 ? d2.y : d2.x)), x, y);
             if constexpr (decltype(is_masked)::value) {
               x = k >= lo && k < hi && !(alone && at + k == 0) ? x : 0.f;
               y = k + 1 >= lo && k + 1 < hi ? y : 0.f;
             }
             w[c] = pack_bf16x2(x, y);
           }
-          tmem_st_32x32b_x32(t_dp + lanes + 64 * half, w);
+          tmem_st_32x32b_x16(td, w);
         };
         if (masked)
           slopes(std::true_type{});
@@ -448,18 +429,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(bar(A_DSREADY));
-          mbar_arrive(bar(A_VECEMPTY + s));
+          mbar_arrive(bar(A_VECEMPTY + o.i));
         }
       }
       if (!ok) break;
-      // dv by the first four warps, dk by the others
+      // dv by the first eight warps, dk by the others
       if (!(ok = mbar_wait_warp(bar(A_OFULL), n_o++ & 1, ctl))) break;
       tc_fence_after();
-      const HeadsView& dst = half ? p.dk : p.dv;
+      const bool is_k = part >= 2;
+      const HeadsView& dst = is_k ? p.dk : p.dv;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(const_cast<void*>(dst.x)) +
                            static_cast<int64_t>(it.q.start + key) * dst.token_stride + it.kv_head * dst.head_stride;
-      for (int c = 0; c < p.D; c += 32)
-        store_cols((half ? t_dk : t_dv) + lanes, out, key < it.q.n, c, p.D, half ? p.scale : 1.f);
+      for (int c = 32 * (part & 1); c < p.D; c += 64)
+        store_cols((is_k ? t_dk : t_dv) + lanes, out, key < it.q.n, c, p.D, is_k ? p.scale : 1.f);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(A_OEMPTY));
@@ -476,12 +458,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // --------------------------------------------------------------------- dq ---
-// tensor memory: S, two of dP (then dS), dQ.  One warp issues S_j, another dP_{j+1} and
+// tensor memory: S, two of dP (then dS), dQ.  The MMAs run in the order S_{j+1}, dP_{j+1},
 // dQ_j: the products of a tile do not wait for the rows of the one before.
 constexpr int kK = 3, kV = 2;  // stages of key and value tiles
 enum { C_QFULL = 0, C_QEMPTY, C_KFULL, C_KEMPTY = C_KFULL + kK, C_KFIX = C_KEMPTY + kK, C_VFULL = C_KFIX + kK,
        C_VEMPTY = C_VFULL + kV, C_SFULL = C_VEMPTY + kV, C_SEMPTY, C_DPFULL, C_DSREADY = C_DPFULL + 2, C_OFULL, C_OEMPTY,
-       C_DRAIN, C_RING = C_DRAIN + 2, C_COUNT = C_RING + kRingBars };
+       C_DRAIN, C_RING, C_COUNT = C_RING + kRingBars };
 
 struct QItem {
   Seq q;
@@ -521,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C_RING; ++i) mbar_init(bar(i), i == C_SEMPTY || i == C_DSREADY || i == C_OEMPTY ? kRowWarps : i == C_QEMPTY ? 2 : 1);
+    for (int i = 0; i < C_RING; ++i) mbar_init(bar(i), i == C_SEMPTY || i == C_DSREADY || i == C_OEMPTY ? kRowWarps : 1);
     init_ring(ring_at, kReaders);
     *abort_flag = 0;
     fence_mbar_init();
@@ -545,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const WaitCtl ctl{abort_flag, p.wait_limit_ns};
   QItem it;
 
-  if (warp >= kTmaWarp) {
+  if (warp < kRestWarps) {
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
@@ -584,63 +566,53 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (!ok) let_copies_land();
       __syncwarp();
-    } else if (warp < kItemWarp) {
+    } else if (warp == kMmaWarp) {
       const bool leader = elect_one();
-      const bool first = warp == kMmaWarp;  // S; the other dP and dQ
       const int steps = (p.D + 15) / 16;
       const uint32_t id_out = idesc_bf16(128, 16 * steps, false, true);
       uint32_t n_q = 0, n = 0, fixed = 0;  // items, tiles
-      Turn k, v;
+      Turn k, v;                           // of the tile whose S and dP are next
       bool ok = true;
       for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok); ++n_q) {
-        if (!(ok = mbar_wait_warp(bar(C_QFULL), n_q & 1, ctl))) break;
         const auto cols_of = [&](int j) { return up16(min(128, it.seen - 128 * j)); };
-        if (first) {
-          for (int j = 0; j < it.tiles; ++j, ++n, k.next(kK)) {
-            const Phase of[2] = {{bar(C_KFULL + k.i), k.phase}, {bar(C_SEMPTY), (n & 1) ^ 1}};
+        const Phase begin[2] = {{bar(C_QFULL), n_q & 1}, {bar(C_OEMPTY), (n_q & 1) ^ 1}};
+        if (!(ok = mbar_wait_warp(begin, ctl))) break;
+        int last_k = 0;  // the stage of the tile before
+        for (int j = 0; j <= it.tiles; ++j) {
+          const int stage = k.i;
+          if (j < it.tiles) {
+            const Phase of[3] = {{bar(C_SEMPTY), ((n + j) & 1) ^ 1}, {bar(C_KFULL + k.i), k.phase}, {bar(C_VFULL + v.i), v.phase}};
             if (!(ok = mbar_wait_warp(of, ctl))) break;
             tc_fence_after();
-            mma_rows(leader, t_s, sq, sk + k.i * kTileBytes, idesc_bf16(128, cols_of(j), false, false), steps);
-            if (leader) umma_commit(bar(C_SFULL));
-          }
-        } else {
-          const auto products = [&](int j) {  // dP of a tile, into the accumulator that dQ of the one two before has read
-            mma_rows(leader, t_dp(n + j), sdo, sv + v.i * kTileBytes, idesc_bf16(128, cols_of(j), false, false), steps);
-            if (leader) {
-              umma_commit(bar(C_DPFULL + ((n + j) & 1)));
-              umma_commit(bar(C_VEMPTY + v.i));
-            }
+            const uint32_t id = idesc_bf16(128, cols_of(j), false, false);
+            mma_rows(leader, t_s, sq, sk + k.i * kTileBytes, id, steps);
+            umma_commit_by(leader, bar(C_SFULL));
+            // (into the accumulator that dQ of the last tile but one has read)
+            mma_rows(leader, t_dp(n + j), sdo, sv + v.i * kTileBytes, id, steps);
+            umma_commit_by(leader, bar(C_DPFULL + ((n + j) & 1)));
+            umma_commit_by(leader, bar(C_VEMPTY + v.i));
+            k.next(kK);
             v.next(kV);
-          };
-          for (int j = 0; j < min(2, it.tiles); ++j) {
-            if (!(ok = mbar_wait_warp(bar(C_VFULL + v.i), v.phase, ctl))) break;
-            tc_fence_after();
-            products(j);
           }
-          if (!ok) break;
-          for (int j = 0; j < it.tiles; ++j, k.next(kK)) {
-            const bool more = j + 2 < it.tiles;
-            const int rows = it.seen - 128 * j;
-            if (j == 0 && !(ok = mbar_wait_warp(bar(C_OEMPTY), (n_q & 1) ^ 1, ctl))) break;
-            const Phase dq_of[2] = {{bar(C_DSREADY), (n + j) & 1}, {bar(C_KFULL + k.i), k.phase}};
-            const Phase all_of[3] = {dq_of[0], dq_of[1], {bar(C_VFULL + v.i), v.phase}};
-            if (!(ok = more ? mbar_wait_warp(all_of, ctl) : mbar_wait_warp(dq_of, ctl))) break;
+          if (j > 0) {
+            const int rows = it.seen - 128 * (j - 1);
             if (rows < 128 && rows % 16 != 0) {
-              if (!(ok = mbar_wait_warp(bar(C_KFIX + k.i), fixed >> k.i & 1, ctl))) break;
-              fixed ^= 1u << k.i;
+              if (!(ok = mbar_wait_warp(bar(C_KFIX + last_k), fixed >> last_k & 1, ctl))) break;
+              fixed ^= 1u << last_k;
             }
+            if (!(ok = mbar_wait_warp(bar(C_DSREADY), (n + j - 1) & 1, ctl))) break;
             tc_fence_after();
-            mma_cols(leader, t_dq, t_dp(n + j), 64, sk + k.i * kTileBytes, id_out, cols_of(j) / 16, j > 0);
-            if (leader) umma_commit(bar(C_KEMPTY + k.i));
-            if (more) products(j + 2);
+            mma_cols<2>(leader, t_dq, t_dp(n + j - 1), sk + last_k * kTileBytes, id_out, cols_of(j - 1) / 16, j > 1);
+            umma_commit_by(leader, bar(C_KEMPTY + last_k));
           }
-          n += it.tiles;
-          if (ok && leader) umma_commit(bar(C_OFULL));
+          last_k = stage;
         }
         if (!ok) break;
-        if (leader) umma_commit(bar(C_QEMPTY));
+        n += it.tiles;
+        umma_commit_by(leader, bar(C_OFULL));
+        umma_commit_by(leader, bar(C_QEMPTY));
       }
-      drain_mmas(bar(C_DRAIN + (first ? 0 : 1)), leader, p.wait_limit_ns);
+      drain_mmas(bar(C_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
       hand_out(ring, ring_at, ask, ctl, [&](int i, QItem& item) { return q_item(p, i, item); },
                [&](int i) {
@@ -651,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     regs_inc<kRegsRows>();
-    const int half = warp >> 2;  // of the tile's key columns
+    const int part = (warp - kRestWarps) >> 2;  // of the tile's key columns
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const ScoreForm form(p);
     uint32_t n_kv = 0, n_o = 0;
@@ -663,24 +635,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool alone = pos == 0 && first_row_alone(p, it.q);
       const float slope2 = kForm != FORM_PLAIN && p.slopes ? p.slopes[it.head] * kAttLog2e : 0.f;
       for (int j = 0; j < it.tiles; ++j, ++n_kv) {
-        const int at = 128 * j + 64 * half, here = lim - at;
-        const bool masked = __any_sync(0xffffffffu, here < 64);
+        const int at = 128 * j + kCols * part, here = lim - at;
+        const bool masked = __any_sync(0xffffffffu, here < kCols);
         [[maybe_unused]] const float far = static_cast<float>(pos - at);
         if (!(ok = mbar_wait_warp(bar(C_SFULL), n_kv & 1, ctl))) break;
         tc_fence_after();
-        uint64_t pr[32];
+        uint64_t pr[kCols / 2];
         {
-          uint32_t a[2][32];
-          tmem_ld_32x32b_x32(t_s + lanes + 64 * half, a[0]);
-          tmem_ld_32x32b_x32(t_s + lanes + 64 * half + 32, a[1]);
+          uint32_t a[32];
+          tmem_ld_32x32b_x32(t_s + lanes + kCols * part, a);
           tmem_ld_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C_SEMPTY));
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
+          for (int c = 0; c < kCols / 2; ++c) {
             const int k = 2 * c;
-            float x = __uint_as_float(a[k >> 5][k & 31]), y = __uint_as_float(a[k >> 5][(k & 31) + 1]);
+            float x = __uint_as_float(a[k]), y = __uint_as_float(a[k + 1]);
             if constexpr (kForm != FORM_PLAIN) {
               float bx, by;
               x = form.at<kForm>(x, slope2, fabsf(far - k), bx) - st.x;
@@ -697,24 +668,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         // (two copies of the loop: as one, the masks' instructions are issued for every tile)
         const auto slopes = [&](auto is_masked) {
-          uint32_t a[2][32], w[32];
-          const uint32_t td = t_dp(n_kv) + lanes + 64 * half;
-          tmem_ld_32x32b_x32(td, a[0]);
-          tmem_ld_32x32b_x32(td + 32, a[1]);
+          uint32_t a[32], w[16];
+          const uint32_t td = t_dp(n_kv) + lanes + kCols * part;
+          tmem_ld_32x32b_x32(td, a);
           tmem_ld_wait();
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
+          for (int c = 0; c < kCols / 2; ++c) {
             const int k = 2 * c;
-            const uint64_t dp = pair(__uint_as_float(a[k >> 5][k & 31]), __uint_as_float(a[k >> 5][(k & 31) + 1]));
             float x, y;
-            unpair(mul_pair(pr[c], add_pair(dp, pair(-st.y, -st.y))), x, y);
+            unpair(mul_pair(pr[c], add_pair(pair(__uint_as_float(a[k]), __uint_as_float(a[k + 1])), pair(-st.y, -st.y))), x, y);
             if constexpr (decltype(is_masked)::value) {
               x = k < here && !alone ? x : 0.f;
               y = k + 1 < here && !alone ? y : 0.f;
             }
             w[c] = pack_bf16x2(x, y);
           }
-          tmem_st_32x32b_x32(td, w);
+          tmem_st_32x32b_x16(td, w);
         };
         if (masked)
           slopes(std::true_type{});
@@ -730,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_after();
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(const_cast<void*>(p.dq.x)) +
                            static_cast<int64_t>(it.q.start + pos) * p.dq.token_stride + it.head * p.dq.head_stride;
-      for (int c = 32 * half; c < p.D; c += 64) store_cols(t_dq + lanes, out, pos < it.q.n, c, p.D, p.scale);
+      if (32 * part < p.D) store_cols(t_dq + lanes, out, pos < it.q.n, 32 * part, p.D, p.scale);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(C_OEMPTY));
