@@ -715,8 +715,8 @@ OLIVE_API olive_status olive_embedding_fwd(const void* W, const int32_t* ids, co
  * head's already: only rows that a token names are then read and written.  dW
  * [V, d] of grad_dtype, rounded once (with what it held in the same sum).
  * Tokens are sorted by id and summed in their order in fp32 (runs of more than 32
- * tokens, beyond 65536 tokens 128, in pieces of that size, added in fp64), so
- * results are the same bits from call to call.  Rows t >= *n_ids and ids outside
+ * tokens, beyond 65536 tokens 128, in pieces of that size, whose sums are added with
+ * a running compensation), so results are the same bits from call to call.  Rows t >= *n_ids and ids outside
  * [0, V) (OLIVE_ERR_TOKEN_RANGE) count nowhere.  T = 0: dW is zeroed, or left.
  * workspace: olive_workspace_size(OLIVE_OP_EMBEDDING_BWD, T, d, 0, V, 0, 0) bytes.
  */
@@ -750,8 +750,8 @@ OLIVE_API olive_status olive_row_norm_fwd(const void* x, const void* residual, c
  *   dx = r (a - mean(a) - n mean(a n)) + g_sum   (mean(a): OLIVE_NORM_LAYER only)
  *   dw = sum over rows of dy n,   db = sum over rows of dy    fp32 [d]
  * dx is the gradient of x and of the residual; it may be dy or g_sum.  db may be
- * NULL.  Sums over rows have a fixed order, in fp32 within a block of threads and
- * fp64 across.  T = 0: dw and db are zeroed.
+ * NULL.  Sums over rows are fp32 and have a fixed order (some tens of rows in turn,
+ * then a tree).  T = 0: dw and db are zeroed.
  * workspace: olive_workspace_size(OLIVE_OP_ROW_NORM_BWD, 1, d, 0, 1, 0, 0) bytes.
  */
 OLIVE_API olive_status olive_row_norm_bwd(const void* dy, const void* h, const void* w,

@@ -22,6 +22,7 @@ constexpr int kDigit = 9, kBins = 1 << kDigit;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kLookThreads = 256;
 constexpr int kSumThreads = 128, kSumCols = 8 * kSumThreads;  // columns of a block
+constexpr int kJoinThreads = 256;
 
 // Eight values.
 template <typename T>
@@ -60,26 +61,42 @@ __device__ __forceinline__ int ids_in_use(const EmbArgs& p) {
   return p.n_ids ? min(max(*p.n_ids, 0), p.T) : p.T;
 }
 
-// Forward: a thread copies vectors of eight.
+// Forward: a thread copies kLookVecs vectors of eight, a block's width apart.
+constexpr int kLookVecs = 4;
 template <typename T>
 __global__ void __launch_bounds__(kLookThreads) look_up_kernel(const EmbArgs p) {
   using V = Run<T>;
   using Raw = typename V::Raw;
   const int nv = p.d / 8;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kLookThreads + threadIdx.x;
-  if (i >= static_cast<int64_t>(p.T) * nv) return;
-  const int t = i >> 32 ? static_cast<int>(i / nv) : static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(nv));
-  const int at = static_cast<int>(i - static_cast<int64_t>(t) * nv);
-  float v[8] = {};
-  if (t < ids_in_use(p)) {
+  const int64_t all = static_cast<int64_t>(p.T) * nv;
+  const int64_t i0 = static_cast<int64_t>(blockIdx.x) * (kLookThreads * kLookVecs) + threadIdx.x;
+  const int n = ids_in_use(p);
+  Raw raw[kLookVecs];
+  int state[kLookVecs];  // 0: zeros, 1: a row, 2: none of that id
+#pragma unroll
+  for (int k = 0; k < kLookVecs; ++k) {
+    const int64_t i = i0 + k * kLookThreads;
+    state[k] = 0;
+    if (i >= all) continue;
+    const int t = i >> 32 ? static_cast<int>(i / nv) : static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(nv));
+    const int at = static_cast<int>(i - static_cast<int64_t>(t) * nv);
+    if (t >= n) continue;
     const int id = p.ids[t];
     const bool fine = id >= 0 && id < p.V;
-    if (fine) V::get(static_cast<const Raw*>(p.W)[static_cast<size_t>(id) * nv + at], v);
+    state[k] = fine ? 1 : 2;
+    if (fine) raw[k] = static_cast<const Raw*>(p.W)[static_cast<size_t>(id) * nv + at];
     if (!fine && at == 0 && p.dev_status) atomicOr(p.dev_status, kStatusToken);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = fine ? v[e] * p.scale : __uint_as_float(0x7fffffffu);
   }
-  static_cast<Raw*>(p.out)[static_cast<size_t>(t) * nv + at] = V::put(v);
+#pragma unroll
+  for (int k = 0; k < kLookVecs; ++k) {
+    const int64_t i = i0 + k * kLookThreads;
+    if (i >= all) continue;
+    float v[8] = {};
+    if (state[k] == 1) V::get(raw[k], v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = state[k] == 2 ? __uint_as_float(0x7fffffffu) : v[e] * p.scale;
+    static_cast<Raw*>(p.out)[i] = V::put(v);
+  }
 }
 
 // A token's sort key: its id, or V (behind all ids) where it has none.
@@ -110,6 +127,16 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const EmbArgs 
   }
   __syncthreads();
   if (threadIdx.x < kBins) s.table[static_cast<size_t>(blockIdx.x) * kBins + threadIdx.x] = count[threadIdx.x];
+}
+
+// Marks the rows of a warp's keys, one atomic a word of the bitmap.  (One a key: the words
+// of the frequent tokens took 8 us.)
+__device__ __forceinline__ void name_rows(const EmbArgs& p, const EmbSort& s, uint32_t key) {
+  const bool real = key < static_cast<uint32_t>(p.V);
+  const uint32_t word = real ? key >> 5 : 0xffffffffu;
+  const uint32_t same = __match_any_sync(0xffffffffu, word);
+  const uint32_t bits = __reduce_or_sync(same, 1u << (key & 31));
+  if (real && (same & ((1u << (threadIdx.x & 31)) - 1)) == 0) atomicOr(&s.named[word], bits);
 }
 
 // A block moves its tile: an entry goes behind all of lower digits, those of its digit
@@ -183,7 +210,96 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const EmbArgs p
     if (in) {
       keys_out[at] = key;
       pos_out[at] = kFirst ? static_cast<int32_t>(i) : pos[i];
-      if (kLast && key < static_cast<uint32_t>(p.V)) atomicOr(&s.named[key >> 5], 1u << (key & 31));
+    }
+    if (kLast) name_rows(p, s, in ? key : 0xffffffffu);
+  }
+}
+
+// Up to kOneBlock tokens: all passes in one block, keys and tokens in shared memory; a
+// thread takes its entries (a warp a run of the list, 32 at a time) into registers and
+// puts them where they belong.
+constexpr int kOneBlock = 4096;  // (9001 in one block: 26 us, in four launches 21)
+constexpr int kOneSmem = 8 * kOneBlock + 4 * kSortWarps * kBins;
+template <int kItems>
+__global__ void __launch_bounds__(kSortThreads) sort_one_kernel(const EmbArgs p, EmbSort s, int passes) {
+  extern __shared__ uint32_t one_smem[];
+  uint32_t* keys = one_smem;
+  int32_t* pos = reinterpret_cast<int32_t*>(one_smem + kItems * kSortThreads);
+  uint32_t* per_warp = one_smem + 2 * kItems * kSortThreads;  // [kSortWarps][kBins]
+  __shared__ uint32_t warp_total[kBins / 32];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int n = ids_in_use(p);
+  uint32_t key[kItems];
+  int32_t at[kItems];
+  const int first = warp * 32 * kItems + lane;
+  for (int w = threadIdx.x; w < (p.V + 31) / 32; w += kSortThreads) s.named[w] = 0;
+#pragma unroll
+  for (int r = 0; r < kItems; ++r) {
+    at[r] = first + 32 * r;
+    key[r] = at[r] < p.T ? first_key(p, n, at[r], true) : 0xffffffffu;  // (behind all: the last of every digit)
+  }
+  uint32_t* mine = per_warp + warp * kBins;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * kDigit;
+    for (int i = threadIdx.x; i < kSortWarps * kBins; i += kSortThreads) per_warp[i] = 0;
+    __syncthreads();
+    uint32_t rank[kItems];
+#pragma unroll
+    for (int r = 0; r < kItems; ++r) {
+      const uint32_t d = (key[r] >> shift) & (kBins - 1);
+      const uint32_t same = __match_any_sync(0xffffffffu, d);
+      rank[r] = mine[d] + __popc(same & ((1u << lane) - 1));
+      __syncwarp();
+      if ((same & ((1u << lane) - 1)) == 0) mine[d] += __popc(same);
+      __syncwarp();
+    }
+    __syncthreads();
+    // before each warp's entries of a digit: those of lower digits and of earlier warps
+    uint32_t sum = 0;
+    if (threadIdx.x < kBins) {
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) {
+        const uint32_t c = per_warp[w * kBins + threadIdx.x];
+        per_warp[w * kBins + threadIdx.x] = sum;
+        sum += c;
+      }
+      uint32_t up = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, up, o);
+        if (lane >= o) up += v;
+      }
+      if (lane == 31) warp_total[warp] = up;
+      sum = up - sum;
+    }
+    __syncthreads();
+    if (threadIdx.x < kBins) {
+      for (int w = 0; w < warp; ++w) sum += warp_total[w];
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) per_warp[w * kBins + threadIdx.x] += sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kItems; ++r) {
+      const uint32_t to = mine[(key[r] >> shift) & (kBins - 1)] + rank[r];
+      keys[to] = key[r];
+      pos[to] = at[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kItems; ++r) {
+      key[r] = keys[first + 32 * r];
+      at[r] = pos[first + 32 * r];
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kItems; ++r) {
+    const int i = first + 32 * r;
+    if (i >= p.T) continue;
+    s.buf_keys[0][i] = key[r];
+    s.buf_pos[0][i] = at[r];
+    if (i == 0 || keys[i - 1] != key[r]) {
+      if (key[r] < static_cast<uint32_t>(p.V)) atomicOr(&s.named[key[r] >> 5], 1u << (key[r] & 31));
     }
   }
 }
@@ -283,40 +399,54 @@ __global__ void __launch_bounds__(kSumThreads) sum_runs_kernel(const EmbArgs p, 
 }
 
 // Rows whose runs cross units: the unit that a run begins in adds up what it and the
-// units behind it stored.
+// units behind it stored, four columns a thread, with a running compensation (a run may
+// be all tokens).
 template <typename O>
-__global__ void __launch_bounds__(kSumThreads) join_runs_kernel(const EmbArgs p, EmbSort s, int unit, int units) {
-  const int u = static_cast<int>(blockIdx.x);
-  const int col = static_cast<int>(blockIdx.y) * kSumCols + 8 * static_cast<int>(threadIdx.x);
+__global__ void __launch_bounds__(kJoinThreads) join_runs_kernel(const EmbArgs p, EmbSort s, int unit, int units) {
+  const int u = static_cast<int>(blockIdx.x), lane = threadIdx.x % 32;
+  const int col = static_cast<int>(blockIdx.y) * (4 * kJoinThreads) + 4 * static_cast<int>(threadIdx.x);
   const int64_t begin = static_cast<int64_t>(u) * unit, end = begin + unit;
   if (end >= p.T) return;
-  const uint32_t run = s.keys[end - 1];
-  if (run == static_cast<uint32_t>(p.V) || s.keys[end] != run || (begin > 0 && s.keys[begin - 1] == run)) return;
-  // the run's end
-  int64_t lo = end, hi = p.T;  // keys[lo] == run, keys[hi] != run
+  const uint32_t run = s.keys[end - 1], behind = s.keys[end], ahead = begin > 0 ? s.keys[begin - 1] : ~run;
+  if (run == static_cast<uint32_t>(p.V) || behind != run || ahead == run) return;
+  // the last unit that begins with the run, a warp looking at 32 places at a time
+  int lo = u + 1, hi = units;  // unit lo begins with it, unit hi does not (or is none)
   while (hi - lo > 1) {
-    const int64_t mid = (lo + hi) / 2;
-    if (s.keys[mid] == run)
-      lo = mid;
-    else
-      hi = mid;
+    const int step = (hi - lo + 31) / 32, w = lo + step * lane;
+    const uint32_t got = __ballot_sync(0xffffffffu, w < hi && s.keys[static_cast<int64_t>(w) * unit] == run);
+    lo += step * (31 - __clz(got));
+    hi = min(hi, lo + step);
   }
-  const int last = static_cast<int>(lo / unit);
   if (col >= p.d) return;
-  double acc[8];
-  const auto add = [&](const float* at, bool first) {
-    const float4 a = reinterpret_cast<const float4*>(at)[0], b = reinterpret_cast<const float4*>(at)[1];
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = (first ? 0.0 : acc[e]) + static_cast<double>(v[e]);
+  float4 acc = *reinterpret_cast<const float4*>(s.part + (static_cast<size_t>(u) * 2 + 1) * p.d + col), low = make_float4(0.f, 0.f, 0.f, 0.f);
+  const auto add = [](float& a, float& c, float v) {
+    const float y = v - c, t = a + y;
+    c = (t - a) - y;
+    a = t;
   };
-  add(s.part + (static_cast<size_t>(u) * 2 + 1) * p.d + col, true);
-#pragma unroll 4
-  for (int w = u + 1; w <= last; ++w) add(s.part + static_cast<size_t>(w) * 2 * p.d + col, false);
-  float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(acc[e]);
-  put_row<O>(p, run, col, v);
+#pragma unroll 8
+  for (int w = u + 1; w <= lo; ++w) {
+    const float4 v = *reinterpret_cast<const float4*>(s.part + static_cast<size_t>(w) * 2 * p.d + col);
+    add(acc.x, low.x, v.x);
+    add(acc.y, low.y, v.y);
+    add(acc.z, low.z, v.z);
+    add(acc.w, low.w, v.w);
+  }
+  O* at = static_cast<O*>(p.dW) + static_cast<size_t>(run) * p.d + col;
+  const float v[4] = {acc.x, acc.y, acc.z, acc.w};
+  if constexpr (sizeof(O) == 4) {
+    float4 was = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (p.accumulate) was = *reinterpret_cast<const float4*>(at);
+    *reinterpret_cast<float4*>(at) = make_float4(fmaf(v[0], p.scale, was.x), fmaf(v[1], p.scale, was.y),
+                                                 fmaf(v[2], p.scale, was.z), fmaf(v[3], p.scale, was.w));
+  } else {
+    uint2 was = make_uint2(0, 0);
+    if (p.accumulate) was = *reinterpret_cast<const uint2*>(at);
+    const float w[4] = {__uint_as_float(was.x << 16), __uint_as_float(was.x & 0xffff0000u), __uint_as_float(was.y << 16),
+                        __uint_as_float(was.y & 0xffff0000u)};
+    *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16x2(fmaf(v[0], p.scale, w[0]), fmaf(v[1], p.scale, w[1])),
+                                               pack_bf16x2(fmaf(v[2], p.scale, w[2]), fmaf(v[3], p.scale, w[3])));
+  }
 }
 
 int sort_tile(int64_t T) { return T <= 65536 ? 2048 : 8192; }
@@ -329,7 +459,8 @@ void run_sums(const Ctx& c, const EmbArgs& a, const EmbSort& s) {
   const int64_t sums = static_cast<int64_t>(units) * cols;
   const int64_t blocks = sums + (a.accumulate ? 0 : ceil_div(a.V, 32));
   sum_runs_kernel<T, O><<<static_cast<unsigned>(blocks), kSumThreads, 0, c.stream>>>(a, s, unit, units, sums);
-  if (units > 1) join_runs_kernel<O><<<dim3(units, cols), kSumThreads, 0, c.stream>>>(a, s, unit, units);
+  if (units > 1)
+    join_runs_kernel<O><<<dim3(units, static_cast<unsigned>(ceil_div(a.d, 4 * kJoinThreads))), kJoinThreads, 0, c.stream>>>(a, s, unit, units);
 }
 
 }  // namespace
@@ -361,7 +492,7 @@ size_t emb_bwd_ws_bytes(int64_t T, int64_t d, int64_t V) {
 }
 
 olive_status launch_emb_fwd(const Ctx& c, const EmbArgs& a) {
-  const int64_t blocks = ceil_div(static_cast<int64_t>(a.T) * (a.d / 8), kLookThreads);
+  const int64_t blocks = ceil_div(static_cast<int64_t>(a.T) * (a.d / 8), kLookThreads * kLookVecs);
   if (a.dtype == OLIVE_DTYPE_BF16)
     look_up_kernel<__nv_bfloat16><<<static_cast<unsigned>(blocks), kLookThreads, 0, c.stream>>>(a);
   else
@@ -386,9 +517,16 @@ olive_status launch_emb_bwd(const Ctx& c, const EmbArgs& a, void* ws) {
   int bits = 1;
   while (bits < 32 && (static_cast<uint64_t>(a.V) >> bits) != 0) ++bits;
   const int passes = (bits + kDigit - 1) / kDigit;
-  const uint32_t* keys = nullptr;
-  const int32_t* pos = nullptr;
-  for (int i = 0; i < passes; ++i) {
+  const uint32_t* keys = s.buf_keys[0];
+  const int32_t* pos = s.buf_pos[0];
+  if (a.T <= kOneBlock) {
+    static std::atomic<int> done_one[2][kMaxDevices];
+    const bool few = a.T <= kSortThreads;
+    const auto one = few ? sort_one_kernel<1> : sort_one_kernel<kOneBlock / kSortThreads>;
+    if (!set_smem_once(reinterpret_cast<const void*>(one), kOneSmem, c.device, done_one[few])) return OLIVE_ERR_CUDA;
+    one<<<1, kSortThreads, kOneSmem, c.stream>>>(a, s, passes);
+  }
+  for (int i = 0; a.T > kOneBlock && i < passes; ++i) {
     const int shift = i * kDigit;
     uint32_t* ko = s.buf_keys[i & 1];
     int32_t* po = s.buf_pos[i & 1];
