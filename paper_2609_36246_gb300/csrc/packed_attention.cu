@@ -16,8 +16,9 @@
 //   warps 0-3, 4-7  the rows of slot 0 and 1, one a thread: the running maximum and
 //              sum, P = exp2(S - reference) in bf16 over S in tensor memory.
 // While one slot's rows are exponentiated the other's products run.  A row's reference
-// follows its maximum only when that is more than 8 (in log2) above, as O has to be
-// scaled then; until there P and the sum are relative to the old one, exactly.
+// follows its maximum only when that is more than 32 (in log2) above, as O has to be
+// scaled then; until there P and the sum are relative to the old one, exactly (bf16 and
+// fp32 hold 2^32 times a row's length), so a tile's exponentials do not wait for its maximum.
 #include <algorithm>
 #include <type_traits>
 
@@ -32,7 +33,7 @@ static_assert(2 * kRegsSoft + kRegsRest <= 3 * kRegsLaunch, "the block's registe
 constexpr int kK = 3, kV = 2;  // stages of key and value tiles
 constexpr int kTmaWarp = 0, kMmaWarp = 1, kItemWarp = 3, kRestWarps = 4;
 constexpr int kReaders = 10;
-constexpr float kLag = 8.f;
+constexpr float kLag = 32.f;
 enum { B_QFULL = 0, B_QEMPTY = 2, B_KFULL = 4, B_KEMPTY = B_KFULL + kK, B_VFULL = B_KEMPTY + kK, B_VEMPTY = B_VFULL + kV,
        B_VFIX = B_VEMPTY + kV, B_SFULL = B_VFIX + kV, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
        B_DRAIN = B_OEMPTY + 2, B_RING, B_COUNT = B_RING + kRingBars };
@@ -133,14 +134,19 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           return true;
         };
-        ok = query(0);
-        for (int j = 0; ok && j < tiles; ++j, k.next(kK), v.next(kV)) {
-          if (!(ok = mbar_wait_warp(bar(B_KEMPTY + k.i), k.phase ^ 1, ctl))) break;
+        const auto keys = [&](int j) {
+          if (!mbar_wait_warp(bar(B_KEMPTY + k.i), k.phase ^ 1, ctl)) return false;
           if (leader) {
             mbar_arrive_expect_tx(bar(B_KFULL + k.i), kTileBytes);
             load_tile(sk + k.i * kTileBytes, &map_k, bar(B_KFULL + k.i), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + 128 * j);
           }
-          if (j == 0 && !(ok = query(1))) break;
+          k.next(kK);
+          return true;
+        };
+        if (!(ok = query(0) && keys(0) && query(1))) break;
+        for (int j = 0; j < tiles; ++j, v.next(kV)) {
+          // (keys a tile ahead: V's stage is free only after the round before)
+          if (j + 1 < tiles && !(ok = keys(j + 1))) break;
           if (!(ok = mbar_wait_warp(bar(B_VEMPTY + v.i), v.phase ^ 1, ctl))) break;
           if (leader) {
             mbar_arrive_expect_tx(bar(B_VFULL + v.i), kTileBytes);
@@ -207,9 +213,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           return true;
         };
         for (int j = 0; ok && j <= tiles; ++j) {
-          if (j == 1 && whole > 1 && (steps == 8 || steps == 4)) {
+          if (j == 1 && whole > 1 && steps >= 4) {
             if (!(ok = mbar_wait_warp(bar(B_OEMPTY), (n_o[0]++ & 1) ^ 1, ctl) && mbar_wait_warp(bar(B_OEMPTY + 1), (n_o[1]++ & 1) ^ 1, ctl))) break;
-            ok = steps == 8 ? whole_rounds(std::integral_constant<int, 8>{}, j) : whole_rounds(std::integral_constant<int, 4>{}, j);
+            if constexpr (kBoxes == 1)
+              ok = whole_rounds(std::integral_constant<int, 4>{}, j);
+            else
+              ok = steps == 8   ? whole_rounds(std::integral_constant<int, 8>{}, j)
+                   : steps == 6 ? whole_rounds(std::integral_constant<int, 6>{}, j)
+                   : steps == 5 ? whole_rounds(std::integral_constant<int, 5>{}, j)
+                                : whole_rounds(std::integral_constant<int, 7>{}, j);
             if (!ok) break;
           }
           Turn next_k = k;
@@ -219,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int a = 0; a < 2; ++a) {
             if (j > 0 && j <= it.tiles[a]) {
               if (j == 1 && !(ok = mbar_wait_warp(bar(B_OEMPTY + a), (n_o[a]++ & 1) ^ 1, ctl))) break;
-              const Phase rows = {bar(B_PREADY + 2 * a), n_p[a] & 1};
+              const Phase rows = {bar(B_PREADY + 2 * a + 1), n_p[a]++ & 1};  // (P's second half: then the first is there too)
               if (!have_v) {
                 const Phase of[2] = {rows, {bar(B_VFULL + v.i), v.phase}};
                 if (!(ok = mbar_wait_warp(of, ctl))) break;
@@ -238,8 +250,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
               tc_fence_after();
               const int ks = up16(min(128, it.seen[a] - 128 * (j - 1))) / 16;
-              if (!(ok = mbar_wait_warp(bar(B_PREADY + 2 * a + 1), n_p[a]++ & 1, ctl))) break;
-              tc_fence_after();
               mma_cols<8>(leader, t_o(a), t_s(a), sv + v.i * kTileBytes, id_out, ks, j > 1);
               if (j == it.tiles[a]) umma_commit_by(leader, bar(B_OFULL + a));
             }
@@ -324,27 +334,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], __uint_as_float(s[c][e]));
         const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * mul;
-        if (j == 0) {
-          ref = m > -INFINITY ? m : 0.f;
-        } else if (__any_sync(0xffffffffu, m > ref + kLag)) {
-          const float now = m > ref + kLag ? m : ref;
-          const float f = fast_exp2(ref - now);
-          ref = now;
-          sum *= f;
-          for (int c = 0; c < p.D; c += 32) {
-            uint32_t o[32];
-            tmem_ld_32x32b_x32(to + c, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st_32x32b_x32(to + c, o);
-          }
-        }
-        uint64_t part[2] = {pair(sum, 0.f), pair(0.f, 0.f)};
-        const uint64_t mul2 = pair(mul, mul), off2 = pair(-ref, -ref);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
+        if (j == 0) ref = m > -INFINITY ? m : 0.f;
+        uint64_t part[2];
+        uint32_t w[2][32];
+        const auto weights = [&](int h) {  // of half the columns
+          const uint64_t mul2 = pair(mul, mul), off2 = pair(-ref, -ref);
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
             const int c = 2 * h + (e >> 4), k = 2 * (e & 15);
@@ -353,14 +347,38 @@ __global__ void __launch_bounds__(kThreads, 1)
             x = fast_exp2(x);
             y = fast_exp2(y);
             part[e & 1] = add_pair(part[e & 1], pair(x, y));
-            w[e] = pack_bf16x2(x, y);
+            w[h][e] = pack_bf16x2(x, y);
           }
-          tmem_st_32x32b_x32(ts + 32 * h, w);
+        };
+        const auto ready = [&](int h) {
+          tmem_st_32x32b_x32(ts + 32 * h, w[h]);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(B_PREADY + 2 * a + h));
+        };
+        part[0] = pair(sum, 0.f);
+        part[1] = pair(0.f, 0.f);
+        weights(0);
+        if (__any_sync(0xffffffffu, m > ref + kLag)) {
+          const float now = m > ref + kLag ? m : ref;
+          const float f = fast_exp2(ref - now);
+          ref = now;
+          for (int c = 0; c < p.D; c += 32) {
+            uint32_t o[32];
+            tmem_ld_32x32b_x32(to + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st_32x32b_x32(to + c, o);
+          }
+          part[0] = pair(sum * f, 0.f);
+          part[1] = pair(0.f, 0.f);
+          weights(0);
         }
+        ready(0);
+        weights(1);
+        ready(1);
         {
           float x, y;
           unpair(add_pair(part[0], part[1]), x, y);
