@@ -50,9 +50,9 @@ constexpr int smem_bytes(int boxes) {
 }
 // Two heads of a key head where their number is even, else two tiles of a head.
 template <bool kPairHeads>
-__device__ __forceinline__ bool item_at(const AttArgs& p, int i, int units, Item& it) {
+__device__ __forceinline__ bool item_at(const AttArgs& p, int i, int units, Item& it, int& near) {
   const int slot = i / units, u = i % units;
-  it.q = seq_of_slot<kPairHeads ? 128 : 256>(p, slot);
+  it.q = seq_of_slot<kPairHeads ? 128 : 256>(p, slot, near);
   if (it.q.tile < 0) return false;
   constexpr int R = kPairHeads ? 128 : 256;
   // the longest rows first
@@ -272,7 +272,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       drain_mmas(bar(B_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
-      hand_out(ring, ring_at, ask, ctl, [&](int i, Item& item) { return item_at<kPairHeads>(p, i, units, item); },
+      int near = 0;
+      hand_out(ring, ring_at, ask, ctl, [&](int i, Item& item) { return item_at<kPairHeads>(p, i, units, item, near); },
                [&](int i) {
                  if (i == 0) check_offsets(p);
                  const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
@@ -300,70 +301,29 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int pos = (a ? it.row0[1] : it.row0[0]) + row;
       const int lim = keys_seen(p, it.q, min(pos, it.q.n - 1));
       const float slope2 = kForm != FORM_PLAIN && p.slopes ? p.slopes[head] * kAttLog2e : 0.f;
+      const int my_seen = a ? it.seen[1] : it.seen[0];
+      // keys that all the warp's rows see; whether it has any
+      const int whole = warp_uniform(keys_seen(p, it.q, min(pos - lane, it.q.n - 1)));
+      const bool live = warp_uniform(static_cast<int>(pos - lane < it.q.n));
+      const float mul = kForm == FORM_PLAIN ? form.scale2 : 1.f;
       float ref = 0.f, sum = 0.f;
       for (int j = 0; j < tiles; ++j) {
         if (!(ok = mbar_wait_warp(bar(B_SFULL + a), n_s++ & 1, ctl))) break;
         tc_fence_after();
-        uint32_t s[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(ts + 32 * c, s[c]);
-        tmem_ld_wait();
-        float mul = form.scale2;
-        if constexpr (kForm != FORM_PLAIN) {
-          mul = 1.f;
-          const float far = static_cast<float>(pos - 128 * j);
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float bend;
-              s[c][e] = __float_as_uint(form.at<kForm>(__uint_as_float(s[c][e]), slope2, fabsf(far - (32 * c + e)), bend));
-            }
-        }
-        const int here = lim - 128 * j;
-        if (__any_sync(0xffffffffu, here < 128)) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (32 * c + e >= here) s[c][e] = 0xff800000u;
-        }
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], __uint_as_float(s[c][e]));
-        const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * mul;
-        if (j == 0) ref = m > -INFINITY ? m : 0.f;
-        uint64_t part[2];
-        uint32_t w[2][32];
-        const auto weights = [&](int h) {  // of half the columns
-          const uint64_t mul2 = pair(mul, mul), off2 = pair(-ref, -ref);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const int c = 2 * h + (e >> 4), k = 2 * (e & 15);
-            float x, y;
-            unpair(fma_pair(pair(__uint_as_float(s[c][k]), __uint_as_float(s[c][k + 1])), mul2, off2), x, y);
-            x = fast_exp2(x);
-            y = fast_exp2(y);
-            part[e & 1] = add_pair(part[e & 1], pair(x, y));
-            w[h][e] = pack_bf16x2(x, y);
-          }
-        };
-        const auto ready = [&](int h) {
-          tmem_st_32x32b_x32(ts + 32 * h, w[h]);
+        const auto arrive = [&](int h) {  // P's half h is there
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(B_PREADY + 2 * a + h));
         };
-        part[0] = pair(sum, 0.f);
-        part[1] = pair(0.f, 0.f);
-        weights(0);
-        if (__any_sync(0xffffffffu, m > ref + kLag)) {
+        const int here = lim - 128 * j;
+        const float far = static_cast<float>(pos - 128 * j);
+        // the reference follows the maximum m
+        const auto follow = [&](float m) {
           const float now = m > ref + kLag ? m : ref;
           const float f = fast_exp2(ref - now);
           ref = now;
+          sum *= f;
           for (int c = 0; c < p.D; c += 32) {
             uint32_t o[32];
             tmem_ld_32x32b_x32(to + c, o);
@@ -372,17 +332,114 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
             tmem_st_32x32b_x32(to + c, o);
           }
-          part[0] = pair(sum * f, 0.f);
-          part[1] = pair(0.f, 0.f);
-          weights(0);
-        }
-        ready(0);
-        weights(1);
-        ready(1);
-        {
+        };
+        if (!live) {  // (rows behind the sequence: nobody's)
+          arrive(0);
+          arrive(1);
+        } else if (128 * (j + 1) <= whole) {
+          uint32_t s[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(ts + 32 * c, s[c]);
+          tmem_ld_wait();
+          if constexpr (kForm != FORM_PLAIN) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                float bend;
+                s[c][e] = __float_as_uint(form.at<kForm>(__uint_as_float(s[c][e]), slope2, fabsf(far - (32 * c + e)), bend));
+              }
+          }
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], __uint_as_float(s[c][e]));
+          const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * mul;
+          if (j == 0) ref = m > -INFINITY ? m : 0.f;
+          uint64_t part[2];
+          uint32_t w[2][32];
+          const auto weights = [&](int h) {  // of half the columns
+            const uint64_t mul2 = pair(mul, mul), off2 = pair(-ref, -ref);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int c = 2 * h + (e >> 4), k = 2 * (e & 15);
+              float x, y;
+              unpair(fma_pair(pair(__uint_as_float(s[c][k]), __uint_as_float(s[c][k + 1])), mul2, off2), x, y);
+              x = fast_exp2(x);
+              y = fast_exp2(y);
+              part[e & 1] = add_pair(part[e & 1], pair(x, y));
+              w[h][e] = pack_bf16x2(x, y);
+            }
+          };
+          const auto begin = [&] {
+            part[0] = pair(sum, 0.f);
+            part[1] = pair(0.f, 0.f);
+            weights(0);
+          };
+          begin();
+          if (__any_sync(0xffffffffu, m > ref + kLag)) {
+            follow(m);
+            begin();
+          }
+          tmem_st_32x32b_x32(ts, w[0]);
+          arrive(0);
+          weights(1);
+          tmem_st_32x32b_x32(ts + 32, w[1]);
+          arrive(1);
           float x, y;
           unpair(add_pair(part[0], part[1]), x, y);
           sum = x + y;
+        } else {
+          // A tile that some row does not see whole, 32 columns at a time and only those
+          // that some row of the slot sees: scores as they are formed and masked go back
+          // to tensor memory, P follows them there.  (A loop: sequences of some forty
+          // tokens run this once an item, where unrolled code takes as long to fetch.)
+          const int chunks = min(4, (my_seen - 128 * j + 31) / 32);
+          float m = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < chunks; ++c) {
+            uint32_t s[32];
+            tmem_ld_32x32b_x32(ts + 32 * c, s);
+            tmem_ld_wait();
+            const int seen = here - 32 * c;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float x = __uint_as_float(s[e]), bend;
+              if constexpr (kForm != FORM_PLAIN) x = form.at<kForm>(x, slope2, fabsf(far - (32 * c + e)), bend);
+              x = e < seen ? x : -INFINITY;
+              m = fmaxf(m, x);
+              s[e] = __float_as_uint(x);
+            }
+            tmem_st_32x32b_x32(ts + 32 * c, s);
+          }
+          tmem_st_wait();
+          m *= mul;
+          if (j == 0) ref = m > -INFINITY ? m : 0.f;
+          if (__any_sync(0xffffffffu, m > ref + kLag)) follow(m);
+          const uint64_t mul2 = pair(mul, mul), off2 = pair(-ref, -ref);
+          uint64_t part = pair(sum, 0.f);
+#pragma unroll 1
+          for (int c = 0; c < chunks; ++c) {
+            uint32_t s[32], w[16];
+            tmem_ld_32x32b_x32(ts + 32 * c, s);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float x, y;
+              unpair(fma_pair(pair(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), mul2, off2), x, y);
+              x = fast_exp2(x);
+              y = fast_exp2(y);
+              part = add_pair(part, pair(x, y));
+              w[e] = pack_bf16x2(x, y);
+            }
+            tmem_st_32x32b_x16(ts + 16 * c, w);
+          }
+          float x, y;
+          unpair(part, x, y);
+          sum = x + y;
+          arrive(0);
+          arrive(1);
         }
       }
       if (!ok) break;

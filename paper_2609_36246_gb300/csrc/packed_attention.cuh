@@ -26,26 +26,40 @@ __device__ __forceinline__ int cu_at(const AttArgs& p, int s) { return min(max(p
 struct Seq {
   int start, n, prefix, tile;  // first token, tokens, those seen by all, tile in it
 };
+// `near`: a sequence at or before it, looked from first (items come in rising order), so
+// that one load, of 32 sequences' offsets, does for most.
 template <int R>
-__device__ __forceinline__ Seq seq_of_slot(const AttArgs& p, int slot) {
+__device__ __forceinline__ Seq seq_of_slot(const AttArgs& p, int slot, int& near) {
   const int lane = threadIdx.x & 31;
-  int lo = 0, hi = p.S;  // the last s in [lo, hi) whose slots begin at or before this one
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 31) / 32;
-    const int s = lo + step * lane;
-    const bool before = s < hi && cu_at(p, s) / R + s <= slot;
-    const uint32_t got = __ballot_sync(0xffffffffu, before);
-    // (offsets that fall set a status bit; the highest lane keeps the search going)
-    const int last = got ? 31 - __clz(got) : 0;
-    lo = lo + step * last;
-    hi = min(hi, lo + step);
+  int cu, first;
+  uint32_t got;
+  const auto look = [&](int from) {  // which of the 32 sequences from there on begin at or before the slot
+    first = from;
+    cu = cu_at(p, min(first + lane, p.S));
+    got = __ballot_sync(0xffffffffu, first + lane < p.S && cu / R + first + lane <= slot);
+  };
+  look(near);
+  if (got == 0 || (got >> 31) != 0) {
+    int lo = 0, hi = p.S;  // the last s in [lo, hi) whose slots begin at or before this one
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32;
+      const int s = lo + step * lane;
+      const uint32_t before = __ballot_sync(0xffffffffu, s < hi && cu_at(p, s) / R + s <= slot);
+      // (offsets that fall set a status bit; the highest lane keeps the search going)
+      lo = lo + step * (before ? 31 - __clz(before) : 0);
+      hi = min(hi, lo + step);
+    }
+    look(lo);
+    got = 1;
   }
+  const int last = 31 - __clz(got);
+  near = first + last;
   Seq q;
-  q.start = cu_at(p, lo);
-  const int end = max(q.start, cu_at(p, lo + 1));
+  q.start = __shfl_sync(0xffffffffu, cu, last);
+  const int end = max(q.start, __shfl_sync(0xffffffffu, cu, last + 1));
   q.n = end - q.start;
-  q.prefix = p.prefix_end ? min(max(p.prefix_end[lo] - q.start, 0), q.n) : 0;
-  q.tile = slot - (q.start / R + lo);
+  q.prefix = p.prefix_end ? min(max(p.prefix_end[near] - q.start, 0), q.n) : 0;
+  q.tile = slot - (q.start / R + near);
   if (q.tile < 0 || static_cast<int64_t>(q.tile) * R >= q.n) q.tile = -1;
   return q;
 }
@@ -116,35 +130,41 @@ __device__ __forceinline__ void hand_out(ItemRing<Item>& ring, const RingAt& at,
   const int lane = threadIdx.x & 31;
   const uint32_t answer = smem_u32(ring.answer);
   uint32_t n = 0, asked = 0;
-  bool ok = true;
-  int i = blockIdx.x;
-  while (i >= 0) {
-    Item it;
-    const bool there = find(i, it);
-    if (there) {
-      if (lane == 0) ring.item[n % kItems] = it;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(at.full(n));
-      ++n;
-    }
-    rest(i);
-    // (room for the next entry, be it the last)
-    if (!(ok = mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, ctl))) break;
-    if (ask == ASK_NEVER) break;
-    if (there && ask == ASK_LATE && !(ok = mbar_wait_warp(at.issued(), (n - 1) & 1, ctl))) break;
+  bool ok = true, pending = false;
+  const auto put_question = [&] {
     if (lane == 0) {
       fence_proxy_async_shared();
       mbar_arrive_expect_tx(at.taken(), 16);
       take_block(answer, at.taken());
     }
     __syncwarp();
-    if (!(ok = mbar_wait_warp(at.taken(), asked++ & 1, ctl))) {
-      let_copies_land();
-      break;
+    pending = true;
+  };
+  int i = blockIdx.x;
+  while (i >= 0) {
+    // (early: the next answer is on its way while this item's sequence is looked up)
+    if (ask == ASK_EARLY) put_question();
+    Item it;
+    const bool there = find(i, it);
+    if (there) {
+      if (!(ok = mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, ctl))) break;
+      if (lane == 0) ring.item[n % kItems] = it;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(at.full(n));
+      ++n;
     }
+    rest(i);
+    if (ask == ASK_NEVER) break;
+    if (ask == ASK_LATE) {
+      if (there && !(ok = mbar_wait_warp(at.issued(), (n - 1) & 1, ctl))) break;
+      put_question();
+    }
+    if (!(ok = mbar_wait_warp(at.taken(), asked++ & 1, ctl))) break;
+    pending = false;
     i = warp_uniform(taken_block(answer));
   }
-  if (ok && lane == 0) {
+  if (pending) let_copies_land();
+  if (ok && mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, ctl) && lane == 0) {
     ring.item[n % kItems].end = 1;
     mbar_arrive(at.full(n));
   }

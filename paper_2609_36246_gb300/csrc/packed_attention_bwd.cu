@@ -55,43 +55,64 @@ __device__ __forceinline__ const __nv_bfloat16* row_of(const HeadsView& x, int64
   return static_cast<const __nv_bfloat16*>(x.x) + t * x.token_stride + h * x.head_stride;
 }
 // stats: [Hq, T] of (lse in base 2, delta); a block works on a tile's rows of one head,
-// 16 lanes a row.
+// 16 lanes a row, four rows' loads in flight together.
 __global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttArgs p, float2* stats) {
-  const int head = static_cast<int>(blockIdx.x % p.Hq);
-  const Seq q = seq_of_slot<128>(p, static_cast<int>(blockIdx.x / p.Hq));
+  constexpr int kGroups = kDeltaThreads / 16, kAtOnce = 4;
+  const int head = static_cast<int>(blockIdx.x % p.Hq), slot = static_cast<int>(blockIdx.x / p.Hq);
+  int near = 0;
+  const Seq q = seq_of_slot<128>(p, slot, near);
   if (q.tile < 0) return;
   const int lane = threadIdx.x % 16, group = threadIdx.x / 16, kv = head / (p.Hq / p.Hk);
   const bool in = 8 * lane < p.D;
   const ScoreForm form(p);
   const float slope2 = p.slopes ? p.slopes[head] * kAttLog2e : 0.f;
+  const int row0 = q.tile * 128, rows = min(128, q.n - row0);
+  const float* lse = p.lse + static_cast<int64_t>(head) * p.T + q.start;
+  float2* out = stats + static_cast<int64_t>(head) * p.T + q.start;
 #pragma unroll 1
-  for (int r = group; r < 128; r += kDeltaThreads / 16) {
-    const int i = q.tile * 128 + r;
-    if (!__any_sync(0xffffffffu, i < q.n)) break;
-    const bool live = i < q.n;
-    const int64_t t = q.start + min(i, q.n - 1);
-    float a[8], b[8];
-    eight(row_of(p.d_o, t, head) + 8 * lane, in, a);
-    eight(row_of(p.o, t, head) + 8 * lane, in, b);
-    float delta = dot16(a, b);
-    const float lse2 = p.lse[static_cast<int64_t>(head) * p.T + t] * kAttLog2e;
-    const int keys = keys_seen(p, q, static_cast<int>(t) - q.start);
-    if (__any_sync(0xffffffffu, keys <= kFewKeys)) {
-      float qr[8], sum = 0.f;
-      eight(row_of(p.q, t, head) + 8 * lane, in, qr);
-      for (int j = 0; __any_sync(0xffffffffu, j < keys && keys <= kFewKeys); ++j) {
-        const int64_t tj = q.start + min(j, keys - 1);
-        eight(row_of(p.k, tj, kv) + 8 * lane, in, b);
-        float bend;
-        const float d = dot16(qr, b), far = fabsf(static_cast<float>(t - tj));
-        const float s = p.cap > 0.f ? form.at<FORM_CAP>(d, slope2, far, bend) : form.at<FORM_BIAS>(d, slope2, far, bend);
-        eight(row_of(p.v, tj, kv) + 8 * lane, in, b);
-        const float dp = dot16(a, b);
-        if (j < keys) sum = fmaf(fast_exp2(s - lse2), dp, sum);
-      }
-      if (keys <= kFewKeys) delta = sum;
+  for (int r = group; __any_sync(0xffffffffu, r < rows); r += kAtOnce * kGroups) {
+    float a[kAtOnce][8], b[kAtOnce][8], l[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t t = q.start + row0 + min(r + k * kGroups, rows - 1);
+      eight(row_of(p.d_o, t, head) + 8 * lane, in, a[k]);
+      eight(row_of(p.o, t, head) + 8 * lane, in, b[k]);
+      l[k] = lse[t - q.start];
     }
-    if (live && lane == 0) stats[static_cast<int64_t>(head) * p.T + t] = make_float2(lse2, delta);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (!__any_sync(0xffffffffu, r + k * kGroups < rows)) break;
+      const int i = row0 + min(r + k * kGroups, rows - 1);
+      const float lse2 = l[k] * kAttLog2e;
+      float delta = dot16(a[k], b[k]);
+      const int keys = keys_seen(p, q, i);
+      const bool few = keys <= kFewKeys && r + k * kGroups < rows;
+      if (__any_sync(0xffffffffu, few)) {
+        const int64_t t = q.start + i;
+        const int most = few ? keys : 0;
+        float qr[8], sum = 0.f;
+        eight(row_of(p.q, t, head) + 8 * lane, in, qr);
+        for (int j0 = 0; __any_sync(0xffffffffu, j0 < most); j0 += kAtOnce) {
+          float key[kAtOnce][8], value[kAtOnce][8];
+#pragma unroll
+          for (int e = 0; e < kAtOnce; ++e) {
+            const int64_t tj = q.start + min(j0 + e, keys - 1);
+            eight(row_of(p.k, tj, kv) + 8 * lane, in, key[e]);
+            eight(row_of(p.v, tj, kv) + 8 * lane, in, value[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < kAtOnce; ++e) {
+            float bend;
+            const float d = dot16(qr, key[e]), far = fabsf(static_cast<float>(i - min(j0 + e, keys - 1)));
+            const float s = p.cap > 0.f ? form.at<FORM_CAP>(d, slope2, far, bend) : form.at<FORM_BIAS>(d, slope2, far, bend);
+            const float dp = dot16(a[k], value[e]);
+            if (j0 + e < most) sum = fmaf(fast_exp2(s - lse2), dp, sum);
+          }
+        }
+        if (few) delta = sum;
+      }
+      if (r + k * kGroups < rows && lane == 0) out[i] = make_float2(lse2, delta);
+    }
   }
 }
 
@@ -133,8 +154,8 @@ struct KvItem {
 };
 constexpr int kKvBars = (8 * A_COUNT + 15) / 16 * 16, kKvMisc = 16 + static_cast<int>(sizeof(ItemRing<KvItem>));
 constexpr int kv_smem(int boxes) { return (2 + kQ + kO) * boxes * kBoxBytes + kO * 1024 + kKvBars + kKvMisc; }
-__device__ __forceinline__ bool kv_item(const AttArgs& p, int i, KvItem& it) {
-  it.q = seq_of_slot<128>(p, i / p.Hk);
+__device__ __forceinline__ bool kv_item(const AttArgs& p, int i, KvItem& it, int& near) {
+  it.q = seq_of_slot<128>(p, i / p.Hk, near);
   if (it.q.tile < 0) return false;
   it.end = 0;
   it.kv_head = i % p.Hk;
@@ -325,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       drain_mmas(bar(A_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
-      hand_out(ring, ring_at, ask, ctl, [&](int i, KvItem& item) { return kv_item(p, i, item); },
+      int near = 0;
+      hand_out(ring, ring_at, ask, ctl, [&](int i, KvItem& item) { return kv_item(p, i, item, near); },
                [&](int i) {
                  const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
                  if (i >= parts) return;
@@ -391,9 +413,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tmem_st_32x32b_x16(ts, w);
         };
-        if (masked)
+        // (not where all rows or all columns are behind the sequence: nothing reads them)
+        const bool some = it.k0 + (warp & 3) * 32 < it.q.n && hi > 0;
+        if (some && masked)
           weights(std::true_type{});
-        else
+        else if (some)
           weights(std::false_type{});
         tmem_st_wait();
         tc_fence_before();
@@ -420,9 +444,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tmem_st_32x32b_x16(td, w);
         };
-        if (masked)
+        if (some && masked)
           slopes(std::true_type{});
-        else
+        else if (some)
           slopes(std::false_type{});
         tmem_st_wait();
         tc_fence_before();
@@ -459,10 +483,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // --------------------------------------------------------------------- dq ---
 // tensor memory: S, two of dP (then dS), dQ.  The MMAs run in the order S_{j+1}, dP_{j+1},
-// dQ_j: the products of a tile do not wait for the rows of the one before.
+// dQ_j: the products of a tile do not wait for the rows of the one before.  So a warp may
+// be done with a tile that another has not begun: barriers of dP and dS by parity.
 constexpr int kK = 3, kV = 2;  // stages of key and value tiles
 enum { C_QFULL = 0, C_QEMPTY, C_KFULL, C_KEMPTY = C_KFULL + kK, C_KFIX = C_KEMPTY + kK, C_VFULL = C_KFIX + kK,
-       C_VEMPTY = C_VFULL + kV, C_SFULL = C_VEMPTY + kV, C_SEMPTY, C_DPFULL, C_DSREADY = C_DPFULL + 2, C_OFULL, C_OEMPTY,
+       C_VEMPTY = C_VFULL + kV, C_SFULL = C_VEMPTY + kV, C_SEMPTY, C_DPFULL, C_DSREADY = C_DPFULL + 2, C_OFULL = C_DSREADY + 2, C_OEMPTY,
        C_DRAIN, C_RING, C_COUNT = C_RING + kRingBars };
 
 struct QItem {
@@ -472,8 +497,8 @@ struct QItem {
 };
 constexpr int kQBars = (8 * C_COUNT + 15) / 16 * 16, kQMisc = 16 + static_cast<int>(sizeof(ItemRing<QItem>));
 constexpr int dq_smem(int boxes) { return 1024 + (2 + kK + kV) * boxes * kBoxBytes + kQBars + kQMisc; }
-__device__ __forceinline__ bool q_item(const AttArgs& p, int i, QItem& it) {
-  it.q = seq_of_slot<128>(p, i / p.Hq);
+__device__ __forceinline__ bool q_item(const AttArgs& p, int i, QItem& it, int& near) {
+  it.q = seq_of_slot<128>(p, i / p.Hq, near);
   if (it.q.tile < 0) return false;
   it.end = 0;
   it.head = i % p.Hq;
@@ -503,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = warp_uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < C_RING; ++i) mbar_init(bar(i), i == C_SEMPTY || i == C_DSREADY || i == C_OEMPTY ? kRowWarps : 1);
+    for (int i = 0; i < C_RING; ++i) mbar_init(bar(i), i == C_SEMPTY || i == C_DSREADY || i == C_DSREADY + 1 || i == C_OEMPTY ? kRowWarps : 1);
     init_ring(ring_at, kReaders);
     *abort_flag = 0;
     fence_mbar_init();
@@ -600,9 +625,10 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (!(ok = mbar_wait_warp(bar(C_KFIX + last_k), fixed >> last_k & 1, ctl))) break;
               fixed ^= 1u << last_k;
             }
-            if (!(ok = mbar_wait_warp(bar(C_DSREADY), (n + j - 1) & 1, ctl))) break;
+            const uint32_t before = n + j - 1;
+            if (!(ok = mbar_wait_warp(bar(C_DSREADY + (before & 1)), before >> 1 & 1, ctl))) break;
             tc_fence_after();
-            mma_cols<2>(leader, t_dq, t_dp(n + j - 1), sk + last_k * kTileBytes, id_out, cols_of(j - 1) / 16, j > 1);
+            mma_cols<2>(leader, t_dq, t_dp(before), sk + last_k * kTileBytes, id_out, cols_of(j - 1) / 16, j > 1);
             umma_commit_by(leader, bar(C_KEMPTY + last_k));
           }
           last_k = stage;
@@ -614,7 +640,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       drain_mmas(bar(C_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
-      hand_out(ring, ring_at, ask, ctl, [&](int i, QItem& item) { return q_item(p, i, item); },
+      int near = 0;
+      hand_out(ring, ring_at, ask, ctl, [&](int i, QItem& item) { return q_item(p, i, item, near); },
                [&](int i) {
                  if (i == 0) check_offsets(p);
                  const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
@@ -637,11 +664,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int j = 0; j < it.tiles; ++j, ++n_kv) {
         const int at = 128 * j + kCols * part, here = lim - at;
         const bool masked = __any_sync(0xffffffffu, here < kCols);
+        // (not where all rows or all columns are behind the sequence: nothing reads them)
+        const bool some = it.q0 + (warp & 3) * 32 < it.q.n && at < it.seen;
         [[maybe_unused]] const float far = static_cast<float>(pos - at);
         if (!(ok = mbar_wait_warp(bar(C_SFULL), n_kv & 1, ctl))) break;
         tc_fence_after();
         uint64_t pr[kCols / 2];
-        {
+        if (!some) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(C_SEMPTY));
+        } else {
           uint32_t a[32];
           tmem_ld_32x32b_x32(t_s + lanes + kCols * part, a);
           tmem_ld_wait();
@@ -685,14 +718,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tmem_st_32x32b_x16(td, w);
         };
-        if (masked)
+        if (some && masked)
           slopes(std::true_type{});
-        else
+        else if (some)
           slopes(std::false_type{});
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(C_DSREADY));
+        if (lane == 0) mbar_arrive(bar(C_DSREADY + (n_kv & 1)));
       }
       if (!ok) break;
       if (!(ok = mbar_wait_warp(bar(C_OFULL), n_o++ & 1, ctl))) break;
