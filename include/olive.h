@@ -168,7 +168,8 @@ OLIVE_API olive_status olive_status_clear(int32_t* dev_status, void* stream);
  *   op  OLIVE_OP_GRAD_CLIP: T = number of tensors; the rest ignored.
  *   op  OLIVE_OP_ROW_NORM_BWD: d = width; the rest ignored.
  *   op  OLIVE_OP_EMBEDDING_BWD: T, d = width, V; the rest ignored.
- *   op  OLIVE_OP_PACKED_ATTENTION_BWD: T, V = query heads; the rest ignored.
+ *   op  OLIVE_OP_PACKED_ATTENTION_BWD: T, d = head width, d_t = key heads, V = query
+ *       heads; the rest ignored.
  *   `grad` (bwd / divergence): non-zero when gradients are requested
  *   (OLIVE_OP_LOSS_BWD always computes them); `grad_dtype` is the dtype of
  *   d_W for OLIVE_OP_LOSS_BWD (bf16 output needs an fp32 accumulator).
@@ -803,7 +804,7 @@ OLIVE_API olive_status olive_packed_attention_fwd(
  * key head.  p and dz are rounded to bf16 as operands, sums are fp32 in a fixed order.
  * Rows behind the last sequence get 0.  All views bf16 with strides of their own, as in
  * the forward; the heads of dq, dk and dv must not share memory, nor those with the inputs.
- * workspace: olive_workspace_size(OLIVE_OP_PACKED_ATTENTION_BWD, T, 0, 0, Hq, 0, 0) bytes.
+ * workspace: olive_workspace_size(OLIVE_OP_PACKED_ATTENTION_BWD, T, D, Hk, Hq, 0, 0) bytes.
  */
 OLIVE_API olive_status olive_packed_attention_bwd(
     const void* d_o, int64_t d_o_token_stride, int64_t d_o_head_stride, const void* q,

@@ -679,8 +679,8 @@ def _need_given(cur, ws, dev_status):
 
 
 @functools.lru_cache(maxsize=4096)
-def _ws_bytes(op, T, d, V, grad, grad_dtype):
-    return int(lib().olive_workspace_size(op, T, d, 0, V, grad, grad_dtype))
+def _ws_bytes(op, T, d, V, grad, grad_dtype, d_t=0):
+    return int(lib().olive_workspace_size(op, T, d, d_t, V, grad, grad_dtype))
 
 
 def _bytes(n, dev):
@@ -1134,7 +1134,7 @@ def olive_packed_attention_bwd(d_o, q, k, v, o, lse, cu_seqlens, scale=None, cau
                                     ((dq, sq, "dq"), (dk, sk, "dk"), (dv, sk, "dv")))
     _need_given(cur, ws, dev_status)
     if ws is None:
-        ws = _bytes(_ws_bytes(16, sq[0], 0, sq[1], 0, 0), dev)
+        ws = _bytes(_ws_bytes(16, sq[0], sq[2], sq[1], 0, 0, sk[1]), dev)
     st = lib().olive_packed_attention_bwd(*vg, *vq, *vk, *vv, *vo, lse.data_ptr(), *common, *oq, *ok, *ov,
                                           ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream_of(cur))
     if st:

@@ -495,7 +495,7 @@ struct AttArgs {
   void* ws;
 };
 constexpr int kMaxAttDim = 128;
-size_t att_bwd_ws_bytes(int64_t T, int64_t Hq);
+size_t att_bwd_ws_bytes(int64_t T, int64_t Hq, int64_t Hk, int64_t D);
 olive_status launch_att_fwd(const Ctx& c, const AttArgs& a);
 olive_status launch_att_bwd(const Ctx& c, const AttArgs& a);
 // A 3-D bf16 tensor map of a view [T, heads, D] whose boxes are 128 tokens of one head's 64 values.

@@ -445,7 +445,9 @@ size_t olive_workspace_size(int op, int32_t T, int32_t d, int32_t d_t, int32_t V
                             int grad_dtype) {
   if (op == OLIVE_OP_SPLICE_MASKED) return T < 1 ? 0 : splice_masked_ws_bytes(T);
   if (op == OLIVE_OP_PACKED_ATTENTION_BWD)
-    return T < 1 || T > kMaxAttTokens || V < 1 || V > kMaxHeads ? 0 : att_bwd_ws_bytes(T, V);
+    return T < 1 || T > kMaxAttTokens || d_t < 1 || V < d_t || V > kMaxHeads || V % d_t != 0 || !width_ok(d) || d > kMaxAttDim
+               ? 0
+               : att_bwd_ws_bytes(T, V, d_t, d);
   if (op == OLIVE_OP_ROW_NORM_BWD) return width_ok(d) && d <= kMaxNormDim ? norm_bwd_ws_bytes(d) : 0;
   if (op == OLIVE_OP_QK_NORM_ROPE_BWD) return width_ok(d) && d <= kMaxHeadDim ? qk_bwd_ws_bytes(d) : 0;
   if (op == OLIVE_OP_GRAD_CLIP) return T < 1 ? 0 : grad_clip_ws_bytes(T);
@@ -1276,7 +1278,7 @@ olive_status olive_packed_attention_bwd(
       st = check_att_view(view, heads, a, written);
       if (st != OLIVE_OK) return st;
     }
-    st = check_ws(workspace, ws_bytes, att_bwd_ws_bytes(T, Hq));
+    st = check_ws(workspace, ws_bytes, att_bwd_ws_bytes(T, Hq, Hk, D));
     if (st != OLIVE_OK) return st;
   }
   Ctx c;

@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n_q[2] = {0, 0};
       Turn k, v;
       bool ok = true;
-      for (uint32_t n = 0; ok && next_item(ring, ring_at, n, it, ctl, ok);) {
+      for (uint32_t n = 0; ok && next_item<true>(ring, ring_at, n, it, ctl, ok);) {
         const int tiles = max(it.tiles[0], it.tiles[1]), seen = max(it.seen[0], it.seen[1]);
         const auto query = [&](int a) {
           if (it.tiles[a] == 0) return true;
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n_q[2] = {0, 0}, n_p[2] = {0, 0}, n_o[2] = {0, 0}, fixed = 0;
       Turn k, v;
       bool ok = true;
-      for (uint32_t n = 0; ok && next_item(ring, ring_at, n, it, ctl, ok);) {
+      for (uint32_t n = 0; ok && next_item<true>(ring, ring_at, n, it, ctl, ok);) {
         const int tiles = max(it.tiles[0], it.tiles[1]), seen = max(it.seen[0], it.seen[1]);
         // A round: O += P V of the tile before and S of this one, slot 0, then slot 1.
         // (A wait takes some 100 cycles where nothing is waited for, and what is queued
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const ScoreForm form(p);
     uint32_t n_s = 0, n_o = 0;
     bool ok = true;
-    for (uint32_t n = 0; ok && next_item(ring, ring_at, n, it, ctl, ok);) {
+    for (uint32_t n = 0; ok && next_item<false>(ring, ring_at, n, it, ctl, ok);) {
       const int tiles = a ? it.tiles[1] : it.tiles[0];
       if (tiles == 0) continue;
       const int head = a ? it.head[1] : it.head[0];

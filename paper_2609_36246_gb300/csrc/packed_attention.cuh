@@ -171,11 +171,16 @@ __device__ __forceinline__ void hand_out(ItemRing<Item>& ring, const RingAt& at,
   __syncwarp();
 }
 // A reader's next item; false: there is none (or the block gives up, ok = false).
-template <class Item>
+// kUniform: for a warp that issues copies or MMAs, whose operands follow from it.  (The
+// exchange by which the compiler learns that takes some 30 cycles a word.)
+template <bool kUniform, class Item>
 __device__ __forceinline__ bool next_item(const ItemRing<Item>& ring, const RingAt& at, uint32_t& n, Item& it,
                                           const WaitCtl& ctl, bool& ok) {
   if (!(ok = mbar_wait_warp(at.full(n), n / kItems & 1, ctl))) return false;
-  it = warp_uniform_copy(&ring.item[n % kItems]);
+  if constexpr (kUniform)
+    it = warp_uniform_copy(&ring.item[n % kItems]);
+  else
+    it = ring.item[n % kItems];
   __syncwarp();
   if ((threadIdx.x & 31) == 0) mbar_arrive(at.empty(n));
   ++n;

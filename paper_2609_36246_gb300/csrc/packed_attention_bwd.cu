@@ -55,9 +55,9 @@ __device__ __forceinline__ const __nv_bfloat16* row_of(const HeadsView& x, int64
   return static_cast<const __nv_bfloat16*>(x.x) + t * x.token_stride + h * x.head_stride;
 }
 // stats: [Hq, T] of (lse in base 2, delta); a block works on a tile's rows of one head,
-// 16 lanes a row, four rows' loads in flight together.
-__global__ void __launch_bounds__(kDeltaThreads) att_delta_kernel(const AttArgs p, float2* stats) {
-  constexpr int kGroups = kDeltaThreads / 16, kAtOnce = 4;
+// 16 lanes a row, two rows' loads in flight together.
+__global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttArgs p, float2* stats) {
+  constexpr int kGroups = kDeltaThreads / 16, kAtOnce = 2;
   const int head = static_cast<int>(blockIdx.x % p.Hq), slot = static_cast<int>(blockIdx.x / p.Hq);
   int near = 0;
   const Seq q = seq_of_slot<128>(p, slot, near);
@@ -137,6 +137,44 @@ __device__ __forceinline__ void store_cols(uint32_t taddr, __nv_bfloat16* row, b
   }
 }
 
+// The same as they are, in fp32, and where: [dv, dk][part][T, Hk, D].
+__device__ __forceinline__ void store_sums(uint32_t taddr, float* row, bool store, int col, int D) {
+  uint32_t o[32];
+  tmem_ld_32x32b_x32(taddr + col, o);
+  tmem_ld_wait();
+#pragma unroll
+  for (int v = 0; v < 8; ++v)
+    if (store && col + 4 * v < D) reinterpret_cast<uint4*>(row + col)[v] = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+}
+__device__ __forceinline__ int64_t sums_at(const AttArgs& p, bool is_k, int parts, int part, int64_t token, int kv_head) {
+  return (((static_cast<int64_t>(is_k) * parts + part) * p.T + token) * p.Hk + kv_head) * p.D;
+}
+// dv and dk of the query heads' parts added, in their order.
+__global__ void __launch_bounds__(256) att_join_kernel(const AttArgs p, const float* sums, int parts) {
+  const int vecs = p.D / 8;
+  const int64_t n = static_cast<int64_t>(cu_at(p, p.S)) * p.Hk * vecs;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < 2 * n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const bool is_k = i >= n;
+    const int64_t row = (is_k ? i - n : i) / vecs;
+    const int col = 8 * static_cast<int>((is_k ? i - n : i) % vecs);
+    const int64_t token = row / p.Hk;
+    const int head = static_cast<int>(row % p.Hk);
+    float f[8] = {};
+#pragma unroll 4
+    for (int g = 0; g < parts; ++g) {
+      const float4* at = reinterpret_cast<const float4*>(sums + sums_at(p, is_k, parts, g, token, head) + col);
+      const float4 a = at[0], b = at[1];
+      f[0] += a.x, f[1] += a.y, f[2] += a.z, f[3] += a.w, f[4] += b.x, f[5] += b.y, f[6] += b.z, f[7] += b.w;
+    }
+    const float by = is_k ? p.scale : 1.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= by;
+    const HeadsView& dst = is_k ? p.dk : p.dv;
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(const_cast<void*>(dst.x)) + token * dst.token_stride + head * dst.head_stride + col;
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+  }
+}
+
 // ----------------------------------------------------------------- dk, dv ---
 // tensor memory: S^T (then P^T), dP^T (then dS^T), dV, dK.  The MMAs run in the order
 // dV_t, S_{t+1}, dK_t, dP_{t+1}: P_{t+1} is formed while the last two run, dS_t while the
@@ -149,27 +187,31 @@ enum { A_KVFULL = 0, A_KVEMPTY, A_QFULL, A_QEMPTY = A_QFULL + kQ, A_QFIX = A_QEM
 
 struct KvItem {
   Seq q;
-  int kv_head, k0, first, tiles, steps;  // first query tile, query tiles of a head, of all heads
+  int kv_head, part, heads;        // which part of the key head's query heads, how many
+  int k0, first, tiles, steps;     // first query tile, query tiles of a head, of all heads
   int end;
 };
 constexpr int kKvBars = (8 * A_COUNT + 15) / 16 * 16, kKvMisc = 16 + static_cast<int>(sizeof(ItemRing<KvItem>));
 constexpr int kv_smem(int boxes) { return (2 + kQ + kO) * boxes * kBoxBytes + kO * 1024 + kKvBars + kKvMisc; }
-__device__ __forceinline__ bool kv_item(const AttArgs& p, int i, KvItem& it, int& near) {
-  it.q = seq_of_slot<128>(p, i / p.Hk, near);
+__device__ __forceinline__ bool kv_item(const AttArgs& p, int i, int parts, KvItem& it, int& near) {
+  const int units = p.Hk * parts, u = i % units;
+  it.q = seq_of_slot<128>(p, i / units, near);
   if (it.q.tile < 0) return false;
   it.end = 0;
-  it.kv_head = i % p.Hk;
+  it.kv_head = u / parts;
+  it.part = u % parts;
+  it.heads = p.Hq / p.Hk / parts;
   it.k0 = 128 * it.q.tile;
   it.first = p.causal && it.k0 >= it.q.prefix ? it.q.tile : 0;
   it.tiles = (it.q.n + 127) / 128 - it.first;
-  it.steps = it.tiles * (p.Hq / p.Hk);
+  it.steps = it.tiles * it.heads;
   return true;
 }
 // An item's steps: a query head and the first row of a query tile.
 struct KvStep {
   int head, q0, left;
   __device__ __forceinline__ KvStep(const AttArgs& p, const KvItem& it)
-      : head(it.kv_head * (p.Hq / p.Hk)), q0(128 * it.first), left(it.tiles) {}
+      : head(it.kv_head * (p.Hq / p.Hk) + it.part * it.heads), q0(128 * it.first), left(it.tiles) {}
   __device__ __forceinline__ void next(const KvItem& it) {
     q0 += 128;
     if (--left == 0) {
@@ -184,7 +226,7 @@ template <int kBoxes, int kForm>
 __global__ void __launch_bounds__(kThreads, 1)
     att_dkdv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do, const AttArgs p,
-                    const float2* stats, int ask) {
+                    const float2* stats, float* sums, int parts, int ask) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);  // (of 1024 bytes' alignment: there is no room to move up)
   constexpr uint32_t kTileBytes = kBoxes * kBoxBytes;
@@ -234,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n_kv = 0;
       Turn q, o;
       bool ok = true;
-      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
+      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok);) {
         if (!(ok = mbar_wait_warp(bar(A_KVEMPTY), (n_kv++ & 1) ^ 1, ctl))) break;
         if (leader) {
           mbar_arrive_expect_tx(bar(A_KVFULL), 2 * kTileBytes);
@@ -293,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n_kv = 0, n = 0, q_fixed = 0, o_fixed = 0;
       Turn q, o;  // of the step whose second products are next
       bool ok = true;
-      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok); ++n_kv) {
+      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok); ++n_kv) {
         KvStep at(p, it);
         int rows = min(128, it.q.n - at.q0);  // (a tile of a sequence's last rows is shorter)
         const auto scores = [&](const Turn& qs) {
@@ -347,12 +389,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain_mmas(bar(A_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
       int near = 0;
-      hand_out(ring, ring_at, ask, ctl, [&](int i, KvItem& item) { return kv_item(p, i, item, near); },
+      hand_out(ring, ring_at, ask, ctl, [&](int i, KvItem& item) { return kv_item(p, i, parts, item, near); },
                [&](int i) {
-                 const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
-                 if (i >= parts) return;
-                 zero_behind(p, p.dk, p.Hk, i, parts);
-                 zero_behind(p, p.dv, p.Hk, i, parts);
+                 const int64_t shares = min(static_cast<int64_t>(gridDim.x), kParts);
+                 if (i >= shares) return;
+                 zero_behind(p, p.dk, p.Hk, i, shares);
+                 zero_behind(p, p.dv, p.Hk, i, shares);
                });
     }
   } else {
@@ -364,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t n_q = 0, n_o = 0;
     Turn o;
     bool ok = true;
-    for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
+    for (uint32_t ni = 0; ok && next_item<false>(ring, ring_at, ni, it, ctl, ok);) {
       const int key = it.k0 + (warp & 3) * 32 + lane;
       const bool alone = first_row_alone(p, it.q);
       KvStep step(p, it);
@@ -464,8 +506,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const HeadsView& dst = is_k ? p.dk : p.dv;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(const_cast<void*>(dst.x)) +
                            static_cast<int64_t>(it.q.start + key) * dst.token_stride + it.kv_head * dst.head_stride;
-      for (int c = 32 * (part & 1); c < p.D; c += 64)
-        store_cols((is_k ? t_dk : t_dv) + lanes, out, key < it.q.n, c, p.D, is_k ? p.scale : 1.f);
+      for (int c = 32 * (part & 1); c < p.D; c += 64) {
+        const uint32_t from = (is_k ? t_dk : t_dv) + lanes;
+        if (parts == 1)
+          store_cols(from, out, key < it.q.n, c, p.D, is_k ? p.scale : 1.f);
+        else
+          store_sums(from, sums + sums_at(p, is_k, parts, it.part, it.q.start + key, it.kv_head), key < it.q.n, c, p.D);
+      }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(A_OEMPTY));
@@ -559,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n_q = 0;
       Turn k, v;
       bool ok = true;
-      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
+      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok);) {
         const int kv = it.head / (p.Hq / p.Hk);
         if (!(ok = mbar_wait_warp(bar(C_QEMPTY), (n_q++ & 1) ^ 1, ctl))) break;
         if (leader) {
@@ -598,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t n_q = 0, n = 0, fixed = 0;  // items, tiles
       Turn k, v;                           // of the tile whose S and dP are next
       bool ok = true;
-      for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok); ++n_q) {
+      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok); ++n_q) {
         const auto cols_of = [&](int j) { return up16(min(128, it.seen - 128 * j)); };
         const Phase begin[2] = {{bar(C_QFULL), n_q & 1}, {bar(C_OEMPTY), (n_q & 1) ^ 1}};
         if (!(ok = mbar_wait_warp(begin, ctl))) break;
@@ -655,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const ScoreForm form(p);
     uint32_t n_kv = 0, n_o = 0;
     bool ok = true;
-    for (uint32_t ni = 0; ok && next_item(ring, ring_at, ni, it, ctl, ok);) {
+    for (uint32_t ni = 0; ok && next_item<false>(ring, ring_at, ni, it, ctl, ok);) {
       const int pos = it.q0 + (warp & 3) * 32 + lane, real = min(pos, it.q.n - 1);
       const float2 st = stats[static_cast<int64_t>(it.head) * p.T + it.q.start + real];
       const int lim = keys_seen(p, it.q, real);
@@ -748,6 +795,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
+size_t stats_bytes(int64_t T, int64_t Hq) { return align_up(8ull * T * Hq, kWsAlign); }
+// Parts that the query heads of a key head are cut into for dk and dv: all of them where
+// the key tiles do not fill the SMs (152), as the first tiles of a causal sequence take
+// longest.  (5003 tokens of 15 + 3 heads: 215 us in one part.  Below four tiles a launch
+// more costs what it saves.)
+int head_parts(int64_t T, int64_t Hq, int64_t Hk) {
+  const int64_t tiles = ceil_div(T, 128);
+  return tiles >= 4 && tiles * Hk <= 152 ? static_cast<int>(Hq / Hk) : 1;
+}
+
 template <int kBoxes, int kForm>
 olive_status run_bwd(const Ctx& c, const AttArgs& a) {
   CUtensorMap mq, mk, mv, mdo;
@@ -766,7 +823,14 @@ olive_status run_bwd(const Ctx& c, const AttArgs& a) {
   const int64_t slots = att_slots(a.T, a.S, 128);
   const auto ask = [&](int64_t items) { return when_to_ask(items, c.num_sms, a.T, a.S); };
   att_delta_kernel<<<static_cast<unsigned>(slots * a.Hq), kDeltaThreads, 0, c.stream>>>(a, stats);
-  dkdv<<<static_cast<unsigned>(slots * a.Hk), kThreads, kSmemKv, c.stream>>>(mq, mk, mv, mdo, a, stats, ask(slots * a.Hk));
+  const int parts = head_parts(a.T, a.Hq, a.Hk);
+  float* sums = reinterpret_cast<float*>(static_cast<char*>(a.ws) + stats_bytes(a.T, a.Hq));
+  dkdv<<<static_cast<unsigned>(slots * a.Hk * parts), kThreads, kSmemKv, c.stream>>>(mq, mk, mv, mdo, a, stats, sums, parts,
+                                                                                    ask(slots * a.Hk * parts));
+  if (parts > 1) {
+    const int64_t blocks = ceil_div(2ll * a.T * a.Hk * (a.D / 8), 256);
+    att_join_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, 16 * c.num_sms)), 256, 0, c.stream>>>(a, sums, parts);
+  }
   dq<<<static_cast<unsigned>(slots * a.Hq), kThreads, kSmemQ, c.stream>>>(mq, mk, mv, mdo, a, stats, ask(slots * a.Hq));
   return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
 }
@@ -779,7 +843,10 @@ olive_status by_form(const Ctx& c, const AttArgs& a) {
 
 }  // namespace
 
-size_t att_bwd_ws_bytes(int64_t T, int64_t Hq) { return align_up(8ull * T * Hq, kWsAlign); }
+size_t att_bwd_ws_bytes(int64_t T, int64_t Hq, int64_t Hk, int64_t D) {
+  const int parts = head_parts(T, Hq, Hk);
+  return stats_bytes(T, Hq) + (parts > 1 ? align_up(8ull * parts * T * Hk * D, kWsAlign) : 0);
+}
 
 olive_status launch_att_bwd(const Ctx& c, const AttArgs& a) {
   return a.D <= 64 ? by_form<1>(c, a) : by_form<2>(c, a);
