@@ -7,9 +7,10 @@ its own sequence (olive_packed_positions), and a step runs
   -> gated feed-forward block with the residual -> norm -> masked continuation loss
 
 backwards through all of it, clips the gradients by their global norm and takes a plain gradient
-step.  Embedding, the rows' norms, the projections and the attention are ordinary torch; the rest is
-the library.  `python examples/student_layer_step.py` prints the loss and the gradients' norm of some
-steps on drawn ids.
+step.  The attention's projections are ordinary torch; the rest is the library.  (layer() also runs
+in elementary torch operations, in any precision, where its parts are given so.)
+`python examples/student_layer_step.py` prints the loss and the gradients' norm of some steps on
+drawn ids.
 """
 
 from __future__ import annotations
@@ -51,20 +52,37 @@ def _rows_norm(x, w):
     return (f * (f.square().mean(-1, keepdim=True) + EPS).rsqrt() * w.float()).to(x.dtype)
 
 
-def layer(p, ids, positions, sequence, tables, heads, kv_heads, qk_norm_rope=B.qk_norm_rope, gated_mlp=B.gated_mlp):
-    """Hidden rows [T, d] of packed ids; `sequence` [T] numbers the tokens' sequences."""
+def _attend(q, k, v, sequence):
+    """Attention of every token to those of its sequence up to itself; `sequence` [T] numbers them."""
+    at = torch.arange(q.shape[0], device=q.device)
+    seen = (sequence[:, None] == sequence[None]) & (at[None] <= at[:, None])
+    per_head = lambda t: t.transpose(0, 1).repeat_interleave(q.shape[1] // t.shape[1], 0)[None]
+    o = torch.nn.functional.scaled_dot_product_attention(per_head(q), per_head(k), per_head(v), attn_mask=seen)
+    return o[0].transpose(0, 1)
+
+
+def layer(p, ids, positions, sequence, tables, heads, kv_heads, qk_norm_rope=B.qk_norm_rope, gated_mlp=B.gated_mlp,
+          embedding=None, row_norm=None, attention=None):
+    """Hidden rows [T, d] of packed ids.  `embedding`, `row_norm` and `attention` are the library's, or
+    None for elementary operations; only those of the attention need `sequence`."""
     T, d, D = ids.numel(), p["W"].shape[1], p["w_q"].numel()
-    x = p["W"][ids.long()] * d ** 0.5
-    qkv = (_rows_norm(x, p["w_in"]) @ p["W_qkv"].t()).view(T, heads + 2 * kv_heads, D)
+
+    def normed(x, w, residual=None):
+        """The rows' norm, and the rows (with the residual added)."""
+        if row_norm is None:
+            x = x if residual is None else x + residual
+            return _rows_norm(x, w), x
+        return (row_norm(x, w, eps=EPS), x) if residual is None else row_norm(x, w, residual=residual, eps=EPS)
+
+    x = p["W"][ids.long()] * d ** 0.5 if embedding is None else embedding(p["W"], ids, d ** 0.5)
+    n, x = normed(x, p["w_in"])
+    qkv = (n @ p["W_qkv"].t()).view(T, heads + 2 * kv_heads, D)
     q, k = qk_norm_rope(qkv[:, :heads], qkv[:, heads:heads + kv_heads], p["w_q"], p["w_k"], *tables, positions, EPS)
     v = qkv[:, heads + kv_heads:]
-    at = torch.arange(T, device=ids.device)
-    seen = (sequence[:, None] == sequence[None]) & (at[None] <= at[:, None])
-    per_head = lambda t: t.transpose(0, 1).repeat_interleave(heads // t.shape[1], 0)[None]
-    o = torch.nn.functional.scaled_dot_product_attention(per_head(q), per_head(k), per_head(v), attn_mask=seen)
-    x = x + o[0].transpose(0, 1).reshape(T, heads * D) @ p["W_o"].t()
-    x = gated_mlp(_rows_norm(x, p["w_mid"]), p["W_gate"], p["W_up"], p["W_down"], x)
-    return _rows_norm(x, p["w_out"]).contiguous()
+    o = _attend(q, k, v, sequence) if attention is None else attention(q, k, v)
+    n, x = normed(o.reshape(T, heads * D) @ p["W_o"].t(), p["w_mid"], x)
+    x = gated_mlp(n, p["W_gate"], p["W_up"], p["W_down"], x)
+    return normed(x, p["w_out"])[0].contiguous()
 
 
 def step(p, batch, V, T, heads, kv_heads, tables, lr=0.0, max_norm=1.0, dev_status=None):
@@ -74,9 +92,10 @@ def step(p, batch, V, T, heads, kv_heads, tables, lr=0.0, max_norm=1.0, dev_stat
     st = B.new_status() if dev_status is None else dev_status
     pk = B.olive_splice_pack(*batch, V, T, dev_status=st)
     positions = B.olive_packed_positions(pk["cu_seqlens"], T)
-    sequence = (torch.arange(T, device="cuda")[:, None] >= pk["cu_seqlens"][None, 1:]).sum(1)
-    hidden = layer(p, pk["ids"], positions, sequence, tables, heads, kv_heads,
-                   functools.partial(B.qk_norm_rope, dev_status=st), functools.partial(B.gated_mlp, dev_status=st))
+    with_status = lambda f, **kw: functools.partial(f, dev_status=st, **kw)
+    hidden = layer(p, pk["ids"], positions, None, tables, heads, kv_heads, with_status(B.qk_norm_rope),
+                   with_status(B.gated_mlp), with_status(B.embedding, n_ids=pk["cu_seqlens"][-1:]), B.row_norm,
+                   with_status(B.packed_attention, cu_seqlens=pk["cu_seqlens"]))
     loss = B.fused_lmhead_ce(hidden, p["W"], pk["targets"], pk["rows"], pk["n_rows"], reduction="mean", dev_status=st)
     loss.backward()
     norm = B.clip_grad_norm_(p.values(), max_norm)
