@@ -336,19 +336,22 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!live) {  // (rows behind the sequence: nobody's)
           arrive(0);
           arrive(1);
-        } else if (128 * (j + 1) <= whole) {
-          uint32_t s[4][32];
+          continue;
+        }
+        uint32_t s[4][32];
+        bool at_once = 128 * (j + 1) <= whole;
+        if (at_once) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(ts + 32 * c, s[c]);
           tmem_ld_wait();
+          if constexpr (kForm == FORM_CAP)
+            at_once = all_small(form, fmaxf(fmaxf(largest(s[0]), largest(s[1])), fmaxf(largest(s[2]), largest(s[3]))));
+        }
+        if (at_once) {
           if constexpr (kForm != FORM_PLAIN) {
+            uint64_t none[1];
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                float bend;
-                s[c][e] = __float_as_uint(form.at<kForm>(__uint_as_float(s[c][e]), slope2, fabsf(far - (32 * c + e)), bend));
-              }
+            for (int c = 0; c < 4; ++c) form_scores<kForm, false, true>(form, s[c], slope2, far - 32 * c, none);
           }
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -391,8 +394,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           unpair(add_pair(part[0], part[1]), x, y);
           sum = x + y;
         } else {
-          // A tile that some row does not see whole, 32 columns at a time and only those
-          // that some row of the slot sees: scores as they are formed and masked go back
+          // A tile that some row does not see whole (or some score is near its cap), 32
+          // columns at a time and only those that some row of the slot sees: scores as they are formed and masked go back
           // to tensor memory, P follows them there.  (A loop: sequences of some forty
           // tokens run this once an item, where unrolled code takes as long to fetch.)
           const int chunks = min(4, (my_seen - 128 * j + 31) / 32);
@@ -403,11 +406,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_ld_32x32b_x32(ts + 32 * c, s);
             tmem_ld_wait();
             const int seen = here - 32 * c;
+            uint64_t none[1];
+            if constexpr (kForm != FORM_PLAIN) form_scores<kForm, false>(form, s, slope2, far - 32 * c, none);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              float x = __uint_as_float(s[e]), bend;
-              if constexpr (kForm != FORM_PLAIN) x = form.at<kForm>(x, slope2, fabsf(far - (32 * c + e)), bend);
-              x = e < seen ? x : -INFINITY;
+              const float x = e < seen ? __uint_as_float(s[e]) : -INFINITY;
               m = fmaxf(m, x);
               s[e] = __float_as_uint(x);
             }

@@ -197,25 +197,76 @@ __device__ __forceinline__ float tanh_of(float x2) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + fast_exp2(x2)));
   return fmaf(-2.f, r, 1.f);
 }
+// Two at once for |x| <= 0.7: x times a polynomial in x^2, fitted to tanh(x) / x at
+// Chebyshev nodes of [0, 0.5] (off by 2^-25 of it at most, before rounding).  A score as
+// most are takes half the time: the exact form's three special functions an element, four
+// cycles each, are what bounds a capped tile.
+__device__ __forceinline__ uint64_t small_tanh_pair(uint64_t x) {
+  const uint64_t y = mul_pair(x, x);
+  const auto k = [](float v) { return pair(v, v); };
+  uint64_t r = fma_pair(y, k(-0.005041549913585186f), k(0.019973110407590866f));
+  r = fma_pair(y, r, k(-0.05350660905241966f));
+  r = fma_pair(y, r, k(0.13328121602535248f));
+  r = fma_pair(y, r, k(-0.3333311676979065f));
+  return mul_pair(x, fma_pair(y, r, k(1.f)));
+}
 // How scores are formed from products: as they are, lowered with the distance, or
 // capped (and lowered, by a slope that may be 0).  In base 2.
 enum { FORM_PLAIN = 0, FORM_BIAS = 1, FORM_CAP = 2 };
 struct ScoreForm {
-  float scale2, to_cap, cap2;
+  float scale2, in_cap, cap2;
   __device__ __forceinline__ explicit ScoreForm(const AttArgs& p)
-      : scale2(p.scale * kAttLog2e), to_cap(p.cap > 0.f ? 2.f * kAttLog2e * p.scale / p.cap : 0.f), cap2(p.cap * kAttLog2e) {}
-  // The score of a product at a distance, and the derivative of its cap.
-  template <int kForm>
-  __device__ __forceinline__ float at(float s, float slope2, float dist, float& bend) const {
-    if constexpr (kForm == FORM_CAP) {
-      const float t = tanh_of(s * to_cap);
-      bend = fmaf(-t, t, 1.f);
-      return fmaf(-slope2, dist, cap2 * t);
-    }
-    bend = 1.f;
-    return fmaf(-slope2, dist, s * scale2);
+      : scale2(p.scale * kAttLog2e), in_cap(p.cap > 0.f ? p.scale / p.cap : 0.f), cap2(p.cap * kAttLog2e) {}
+  // One score of a product at a distance.
+  __device__ __forceinline__ float at(float s, float slope2, float dist) const {
+    const float x = in_cap > 0.f ? cap2 * tanh_of(s * (2.f * kAttLog2e * in_cap)) : s * scale2;
+    return fmaf(-slope2, dist, x);
   }
 };
+// 32 products to scores, column e at the distance |far - e|; with kBend the derivatives of
+// the cap, in pairs.  (A whole warp, which takes the small or the exact form together.)
+__device__ __forceinline__ float largest(const uint32_t (&s)[32]) {
+  float top = 0.f;
+#pragma unroll
+  for (int e = 0; e < 32; ++e) top = fmaxf(top, fabsf(__uint_as_float(s[e])));
+  return top;
+}
+// Whether a warp's products, none larger than `top`, take the small form.
+__device__ __forceinline__ bool all_small(const ScoreForm& f, float top) { return __all_sync(0xffffffffu, top * f.in_cap <= 0.7f); }
+// kSmall: known to (then the exact form, of as much code, is not there).
+template <int kForm, bool kBend, bool kSmall = false>
+__device__ __forceinline__ void form_scores(const ScoreForm& f, uint32_t (&s)[32], float slope2, float far, uint64_t (&bend)[kBend ? 16 : 1]) {
+  if constexpr (kForm == FORM_CAP) {
+    if (kSmall || all_small(f, largest(s))) {
+      const uint64_t in = pair(f.in_cap, f.in_cap), out = pair(f.cap2, f.cap2), one = pair(1.f, 1.f), minus = pair(-1.f, -1.f);
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) {
+        const uint64_t t = small_tanh_pair(mul_pair(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), in));
+        if constexpr (kBend) bend[e / 2] = fma_pair(mul_pair(t, minus), t, one);
+        float x, y;
+        unpair(mul_pair(t, out), x, y);
+        s[e] = __float_as_uint(x);
+        s[e + 1] = __float_as_uint(y);
+      }
+    } else {
+      const float in = 2.f * kAttLog2e * f.in_cap;
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) {
+        const float t = tanh_of(__uint_as_float(s[e]) * in), u = tanh_of(__uint_as_float(s[e + 1]) * in);
+        if constexpr (kBend) bend[e / 2] = pair(fmaf(-t, t, 1.f), fmaf(-u, u, 1.f));
+        s[e] = __float_as_uint(f.cap2 * t);
+        s[e + 1] = __float_as_uint(f.cap2 * u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f.scale2);
+  }
+  if (slope2 != 0.f) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(fmaf(-slope2, fabsf(far - e), __uint_as_float(s[e])));
+  }
+}
 
 // A tile of up to 128 columns into shared memory: boxes of 64 columns.
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int boxes, int head, int token) {

@@ -102,9 +102,7 @@ __global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttAr
           }
 #pragma unroll
           for (int e = 0; e < kAtOnce; ++e) {
-            float bend;
-            const float d = dot16(qr, key[e]), far = fabsf(static_cast<float>(i - min(j0 + e, keys - 1)));
-            const float s = p.cap > 0.f ? form.at<FORM_CAP>(d, slope2, far, bend) : form.at<FORM_BIAS>(d, slope2, far, bend);
+            const float s = form.at(dot16(qr, key[e]), slope2, fabsf(static_cast<float>(i - min(j0 + e, keys - 1))));
             const float dp = dot16(a[k], value[e]);
             if (j0 + e < most) sum = fmaf(fast_exp2(s - lse2), dp, sum);
           }
@@ -416,33 +414,34 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int lo = key >= it.q.n ? kCols : p.causal && key >= it.q.prefix ? key - at : 0, hi = it.q.n - at;
         const bool masked = __any_sync(0xffffffffu, lo > 0 || hi < kCols);
         const float slope2 = kForm != FORM_PLAIN && p.slopes ? p.slopes[step.head] * kAttLog2e : 0.f;
-        [[maybe_unused]] const float far = static_cast<float>(at - key);
+        [[maybe_unused]] const float far = static_cast<float>(key - at);
         const float* stage = vec + o.i * 256 + kCols * part;
         const Phase of[2] = {{bar(A_VECFULL + o.i), o.phase}, {bar(A_SFULL), n_q & 1}};
         if (!(ok = mbar_wait_warp(of, ctl))) break;
         tc_fence_after();
+        // (not where all rows or all columns are behind the sequence: nothing reads them)
+        const bool some = it.k0 + (warp & 3) * 32 < it.q.n && hi > 0;
         uint64_t pr[kCols / 2];  // pairs of columns: p, times the cap's derivative
-        // (two copies of the loops: as one, the masks' instructions are issued for every tile)
-        const auto weights = [&](auto is_masked) {
-          uint32_t a[32], w[16];
+        uint32_t a[32];
+        [[maybe_unused]] uint64_t bend[kForm == FORM_CAP ? 16 : 1];
+        if (some) {
           tmem_ld_32x32b_x32(ts, a);
           tmem_ld_wait();
+          if constexpr (kForm != FORM_PLAIN) form_scores<kForm, kForm == FORM_CAP>(form, a, slope2, far, bend);
+        }
+        // (two copies of the loops: as one, the masks' instructions are issued for every tile)
+        const auto weights = [&](auto is_masked) {
+          uint32_t w[16];
           const ulonglong2* lse = reinterpret_cast<const ulonglong2*>(stage);
+          constexpr bool kFormed = kForm != FORM_PLAIN;
+          const uint64_t mul = pair(kFormed ? 1.f : form.scale2, kFormed ? 1.f : form.scale2);
 #pragma unroll
           for (int c = 0; c < kCols / 2; ++c) {
             const int k = 2 * c;
             const ulonglong2 l2 = lse[c / 2];
-            const uint64_t l = c & 1 ? l2.y : l2.x;
-            float x = __uint_as_float(a[k]), y = __uint_as_float(a[k + 1]);
-            [[maybe_unused]] float bx, by;
-            if constexpr (kForm != FORM_PLAIN) {
-              float lx, ly;
-              unpair(l, lx, ly);
-              x = form.at<kForm>(x, slope2, fabsf(far + k), bx) + lx;
-              y = form.at<kForm>(y, slope2, fabsf(far + (k + 1)), by) + ly;
-            } else {
-              unpair(fma_pair(pair(x, y), pair(form.scale2, form.scale2), l), x, y);
-            }
+            const uint64_t l = c & 1 ? l2.y : l2.x, s2 = pair(__uint_as_float(a[k]), __uint_as_float(a[k + 1]));
+            float x, y;
+            unpair(kFormed ? add_pair(s2, l) : fma_pair(s2, mul, l), x, y);
             x = fast_exp2(x);
             y = fast_exp2(y);
             if constexpr (decltype(is_masked)::value) {
@@ -450,13 +449,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               y = k + 1 >= lo && k + 1 < hi ? y : 0.f;
             }
             pr[c] = pair(x, y);
-            if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], pair(bx, by));
+            if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], bend[c]);
             w[c] = pack_bf16x2(x, y);
           }
           tmem_st_32x32b_x16(ts, w);
         };
-        // (not where all rows or all columns are behind the sequence: nothing reads them)
-        const bool some = it.k0 + (warp & 3) * 32 < it.q.n && hi > 0;
         if (some && masked)
           weights(std::true_type{});
         else if (some)
@@ -728,20 +725,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C_SEMPTY));
+          [[maybe_unused]] uint64_t bend[kForm == FORM_CAP ? 16 : 1];
+          if constexpr (kForm != FORM_PLAIN) form_scores<kForm, kForm == FORM_CAP>(form, a, slope2, far, bend);
 #pragma unroll
           for (int c = 0; c < kCols / 2; ++c) {
-            const int k = 2 * c;
-            float x = __uint_as_float(a[k]), y = __uint_as_float(a[k + 1]);
-            if constexpr (kForm != FORM_PLAIN) {
-              float bx, by;
-              x = form.at<kForm>(x, slope2, fabsf(far - k), bx) - st.x;
-              y = form.at<kForm>(y, slope2, fabsf(far - (k + 1)), by) - st.x;
-              pr[c] = pair(fast_exp2(x), fast_exp2(y));
-              if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], pair(bx, by));  // (p itself is not needed here)
-            } else {
-              unpair(fma_pair(pair(x, y), pair(form.scale2, form.scale2), pair(-st.x, -st.x)), x, y);
-              pr[c] = pair(fast_exp2(x), fast_exp2(y));
-            }
+            const uint64_t s2 = pair(__uint_as_float(a[2 * c]), __uint_as_float(a[2 * c + 1])), l = pair(-st.x, -st.x);
+            float x, y;
+            unpair(kForm != FORM_PLAIN ? add_pair(s2, l) : fma_pair(s2, pair(form.scale2, form.scale2), l), x, y);
+            pr[c] = pair(fast_exp2(x), fast_exp2(y));
+            if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], bend[c]);  // (p itself is not needed here)
           }
         }
         if (!(ok = mbar_wait_warp(bar(C_DPFULL + (n_kv & 1)), n_kv >> 1 & 1, ctl))) break;
