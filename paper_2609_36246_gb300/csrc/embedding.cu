@@ -112,7 +112,9 @@ __device__ __forceinline__ uint32_t first_key(const EmbArgs& p, int n, int t, bo
 template <bool kFirst>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const EmbArgs p, EmbSort s, const uint32_t* keys, int shift, int tile) {
   __shared__ uint32_t count[kBins];
+  grid_launch_dependents();
   if (threadIdx.x < kBins) count[threadIdx.x] = 0;
+  if (!kFirst) grid_wait();
   if constexpr (kFirst) {
     const int words = (p.V + 31) / 32;
     for (int w = blockIdx.x * kSortThreads + threadIdx.x; w < words; w += gridDim.x * kSortThreads) s.named[w] = 0;
@@ -148,7 +150,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const EmbArgs p
   __shared__ uint32_t base[kBins];
   __shared__ uint32_t warp_total[kBins / 32];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  grid_launch_dependents();
   for (int i = threadIdx.x; i < kSortWarps * kBins; i += kSortThreads) per_warp[i] = 0;
+  grid_wait();
   uint32_t total = 0, before = 0;
   if (threadIdx.x < kBins) {
 #pragma unroll 4
@@ -228,6 +232,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_one_kernel(const EmbArgs p,
   uint32_t* per_warp = one_smem + 2 * kItems * kSortThreads;  // [kSortWarps][kBins]
   __shared__ uint32_t warp_total[kBins / 32];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  grid_launch_dependents();
   const int n = ids_in_use(p);
   uint32_t key[kItems];
   int32_t at[kItems];
@@ -329,6 +334,8 @@ __global__ void __launch_bounds__(kSumThreads) sum_runs_kernel(const EmbArgs p, 
   using V = Run<T>;
   using Raw = typename V::Raw;
   const int64_t block = blockIdx.x;
+  grid_launch_dependents();
+  grid_wait();
   if (block >= sums) {
     const int word = static_cast<int>(block - sums);
     const uint32_t named = s.named[word];
@@ -407,6 +414,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_runs_kernel(const EmbArgs p
   const int col = static_cast<int>(blockIdx.y) * (4 * kJoinThreads) + 4 * static_cast<int>(threadIdx.x);
   const int64_t begin = static_cast<int64_t>(u) * unit, end = begin + unit;
   if (end >= p.T) return;
+  grid_wait();
   const uint32_t run = s.keys[end - 1], behind = s.keys[end], ahead = begin > 0 ? s.keys[begin - 1] : ~run;
   if (run == static_cast<uint32_t>(p.V) || behind != run || ahead == run) return;
   // the last unit that begins with the run, a warp looking at 32 places at a time
@@ -449,6 +457,23 @@ __global__ void __launch_bounds__(kJoinThreads) join_runs_kernel(const EmbArgs p
   }
 }
 
+// Launches a kernel that waits for the one ahead by itself (grid_wait, before it touches
+// what that one reads or writes), so that it is on the SMs when that ends.
+template <class... K, class... A>
+void launch_after(const Ctx& c, void (*kernel)(K...), dim3 grid, int threads, size_t smem, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...);
+}
+
 int sort_tile(int64_t T) { return T <= 65536 ? 2048 : 8192; }
 int sum_unit(int64_t T) { return T <= 65536 ? 32 : 128; }
 
@@ -458,9 +483,9 @@ void run_sums(const Ctx& c, const EmbArgs& a, const EmbSort& s) {
   const int cols = static_cast<int>(ceil_div(a.d, kSumCols));
   const int64_t sums = static_cast<int64_t>(units) * cols;
   const int64_t blocks = sums + (a.accumulate ? 0 : ceil_div(a.V, 32));
-  sum_runs_kernel<T, O><<<static_cast<unsigned>(blocks), kSumThreads, 0, c.stream>>>(a, s, unit, units, sums);
+  launch_after(c, sum_runs_kernel<T, O>, dim3(static_cast<unsigned>(blocks)), kSumThreads, 0, a, s, unit, units, sums);
   if (units > 1)
-    join_runs_kernel<O><<<dim3(units, static_cast<unsigned>(ceil_div(a.d, 4 * kJoinThreads))), kJoinThreads, 0, c.stream>>>(a, s, unit, units);
+    launch_after(c, join_runs_kernel<O>, dim3(units, static_cast<unsigned>(ceil_div(a.d, 4 * kJoinThreads))), kJoinThreads, 0, a, s, unit, units);
 }
 
 }  // namespace
@@ -534,10 +559,10 @@ olive_status launch_emb_bwd(const Ctx& c, const EmbArgs& a, void* ws) {
     if (i == 0)
       sort_count_kernel<true><<<blocks, kSortThreads, 0, c.stream>>>(a, s, keys, shift, tile);
     else
-      sort_count_kernel<false><<<blocks, kSortThreads, 0, c.stream>>>(a, s, keys, shift, tile);
+      launch_after(c, sort_count_kernel<false>, dim3(blocks), kSortThreads, 0, a, s, keys, shift, tile);
     const auto move = i == 0 ? (last ? sort_move_kernel<true, true> : sort_move_kernel<true, false>)
                              : (last ? sort_move_kernel<false, true> : sort_move_kernel<false, false>);
-    move<<<blocks, kSortThreads, kSmem, c.stream>>>(a, s, keys, pos, ko, po, shift, tile);
+    launch_after(c, move, dim3(blocks), kSortThreads, kSmem, a, s, keys, pos, ko, po, shift, tile);
     keys = ko;
     pos = po;
   }

@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(ts + 32 * c, s[c]);
           tmem_ld_wait();
           if constexpr (kForm == FORM_CAP)
-            at_once = all_small(form, fmaxf(fmaxf(largest(s[0]), largest(s[1])), fmaxf(largest(s[2]), largest(s[3]))));
+            at_once = all_small(form, pos < it.q.n ? fmaxf(fmaxf(largest(s[0]), largest(s[1])), fmaxf(largest(s[2]), largest(s[3]))) : 0.f);
         }
         if (at_once) {
           if constexpr (kForm != FORM_PLAIN) {
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_ld_wait();
             const int seen = here - 32 * c;
             uint64_t none[1];
-            if constexpr (kForm != FORM_PLAIN) form_scores<kForm, false>(form, s, slope2, far - 32 * c, none);
+            if constexpr (kForm != FORM_PLAIN) form_scores<kForm, false, false>(form, s, slope2, far - 32 * c, none);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const float x = e < seen ? __uint_as_float(s[e]) : -INFINITY;

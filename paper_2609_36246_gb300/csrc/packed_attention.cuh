@@ -223,21 +223,22 @@ struct ScoreForm {
     return fmaf(-slope2, dist, x);
   }
 };
-// 32 products to scores, column e at the distance |far - e|; with kBend the derivatives of
-// the cap, in pairs.  (A whole warp, which takes the small or the exact form together.)
 __device__ __forceinline__ float largest(const uint32_t (&s)[32]) {
   float top = 0.f;
 #pragma unroll
   for (int e = 0; e < 32; ++e) top = fmaxf(top, fabsf(__uint_as_float(s[e])));
   return top;
 }
-// Whether a warp's products, none larger than `top`, take the small form.
+// Whether a warp's products, none larger than `top`, take the small form.  Asked of whole
+// tiles and of a sequence's own rows alone: what lies behind it must not decide in which
+// form, so with which rounding, its scores are formed.
 __device__ __forceinline__ bool all_small(const ScoreForm& f, float top) { return __all_sync(0xffffffffu, top * f.in_cap <= 0.7f); }
-// kSmall: known to (then the exact form, of as much code, is not there).
-template <int kForm, bool kBend, bool kSmall = false>
+// 32 products to scores, column e at the distance |far - e|; with kBend the derivatives of
+// the cap, in pairs.
+template <int kForm, bool kBend, bool kSmall>
 __device__ __forceinline__ void form_scores(const ScoreForm& f, uint32_t (&s)[32], float slope2, float far, uint64_t (&bend)[kBend ? 16 : 1]) {
   if constexpr (kForm == FORM_CAP) {
-    if (kSmall || all_small(f, largest(s))) {
+    if constexpr (kSmall) {
       const uint64_t in = pair(f.in_cap, f.in_cap), out = pair(f.cap2, f.cap2), one = pair(1.f, 1.f), minus = pair(-1.f, -1.f);
 #pragma unroll
       for (int e = 0; e < 32; e += 2) {

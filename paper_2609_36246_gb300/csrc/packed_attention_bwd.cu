@@ -427,7 +427,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (some) {
           tmem_ld_32x32b_x32(ts, a);
           tmem_ld_wait();
-          if constexpr (kForm != FORM_PLAIN) form_scores<kForm, kForm == FORM_CAP>(form, a, slope2, far, bend);
+          if constexpr (kForm != FORM_PLAIN) {
+            if (!masked && all_small(form, largest(a)))
+              form_scores<kForm, kForm == FORM_CAP, true>(form, a, slope2, far, bend);
+            else
+              form_scores<kForm, kForm == FORM_CAP, false>(form, a, slope2, far, bend);
+          }
         }
         // (two copies of the loops: as one, the masks' instructions are issued for every tile)
         const auto weights = [&](auto is_masked) {
@@ -726,7 +731,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C_SEMPTY));
           [[maybe_unused]] uint64_t bend[kForm == FORM_CAP ? 16 : 1];
-          if constexpr (kForm != FORM_PLAIN) form_scores<kForm, kForm == FORM_CAP>(form, a, slope2, far, bend);
+          if constexpr (kForm != FORM_PLAIN) {
+            if (!masked && all_small(form, pos < it.q.n ? largest(a) : 0.f))
+              form_scores<kForm, kForm == FORM_CAP, true>(form, a, slope2, far, bend);
+            else
+              form_scores<kForm, kForm == FORM_CAP, false>(form, a, slope2, far, bend);
+          }
 #pragma unroll
           for (int c = 0; c < kCols / 2; ++c) {
             const uint64_t s2 = pair(__uint_as_float(a[2 * c]), __uint_as_float(a[2 * c + 1])), l = pair(-st.x, -st.x);

@@ -193,9 +193,11 @@ def test_largest_scores_late():
     _check(s)
 
 
-def test_what_is_not_finite():
-    """A bad token behind a sequence's end, or in another one, does not show; its own sequence's does."""
-    s = _case([100, 77, 60], 4, 2, 64, pad=20)
+@pytest.mark.parametrize("form", [dict(), dict(cap=6.0), dict(cap=3.0, bias=True, prefix=20), dict(causal=False)], ids=str)
+def test_what_is_not_finite(form):
+    """A bad token behind a sequence's end, or in another one, does not show, not in a bit; its own
+    sequence's does."""
+    s = _case([100, 77, 60], 4, 2, 64, pad=20, **form)
     good = _check(s)
     for n in ("q", "k", "v", "do"):
         s[n][100 + 77:] = float("nan")  # the last sequence, and nobody's rows
@@ -203,6 +205,18 @@ def test_what_is_not_finite():
     assert torch.equal(o[:177], good[0][:177]) and torch.equal(lse[:, :177], good[1][:, :177])
     for g, want in zip((o, *_backward(s, o, lse)), (good[0], *good[2:])):
         assert torch.equal(g[:177], want[:177]) and torch.isnan(g[177:237]).all() and not g[237:].any()
+
+
+@pytest.mark.parametrize("form", [dict(cap=20.0), dict(cap=5.0, bias=True), dict(prefix=900), dict(causal=False, cap=20.0)], ids=str)
+def test_the_same_bits_whatever_ran_before(form):
+    """What earlier launches left in shared and tensor memory decides nothing."""
+    s = _case([2000, 45, 130], 5, 1, 128, **form)
+    other = _case([700] * 3, 5, 1, 128, sharp=8.0, seed=1)
+    run = lambda: (lambda o, lse: (o, lse, *_backward(s, o, lse)))(*_forward(s))
+    want = run()
+    for _ in range(8):
+        _backward(other, *_forward(other))
+        assert all(torch.equal(a, b) for a, b in zip(run(), want))
 
 
 def test_layouts():
