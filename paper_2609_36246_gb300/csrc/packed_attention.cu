@@ -340,6 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         uint32_t s[4][32];
         bool at_once = 128 * (j + 1) <= whole;
+        if constexpr (kForm == FORM_BIAS) at_once = at_once && one_side(far, 128);
         if (at_once) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(ts + 32 * c, s[c]);

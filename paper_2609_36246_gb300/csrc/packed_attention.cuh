@@ -233,12 +233,18 @@ __device__ __forceinline__ float largest(const uint32_t (&s)[32]) {
 // tiles and of a sequence's own rows alone: what lies behind it must not decide in which
 // form, so with which rounding, its scores are formed.
 __device__ __forceinline__ bool all_small(const ScoreForm& f, float top) { return __all_sync(0xffffffffu, top * f.in_cap <= 0.7f); }
-// 32 products to scores, column e at the distance |far - e|; with kBend the derivatives of
-// the cap, in pairs.
-template <int kForm, bool kBend, bool kSmall>
+// Whether each of a warp's rows has `cols` columns on one side of its own, before it or
+// behind: then the distance is linear in the column, one instruction a score in place of
+// two and half of one.
+__device__ __forceinline__ bool one_side(float far, int cols) {
+  return __all_sync(0xffffffffu, far <= 0.f || far >= static_cast<float>(cols - 1));
+}
+// 32 products to scores, column e at the distance |far - e| (kEven: all on one side); with
+// kBend the derivatives of the cap, in pairs.
+template <int kForm, bool kBend, bool kEven>
 __device__ __forceinline__ void form_scores(const ScoreForm& f, uint32_t (&s)[32], float slope2, float far, uint64_t (&bend)[kBend ? 16 : 1]) {
   if constexpr (kForm == FORM_CAP) {
-    if constexpr (kSmall) {
+    if constexpr (kEven) {
       const uint64_t in = pair(f.in_cap, f.in_cap), out = pair(f.cap2, f.cap2), one = pair(1.f, 1.f), minus = pair(-1.f, -1.f);
 #pragma unroll
       for (int e = 0; e < 32; e += 2) {
@@ -259,11 +265,22 @@ __device__ __forceinline__ void form_scores(const ScoreForm& f, uint32_t (&s)[32
         s[e + 1] = __float_as_uint(f.cap2 * u);
       }
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * f.scale2);
   }
-  if (slope2 != 0.f) {
+  // (a bias is there in FORM_BIAS: scaled and lowered in one instruction)
+  if constexpr (kForm == FORM_BIAS && kEven) {
+    const float per = far > 0.f ? slope2 : -slope2, first = -per * far;
+    const uint64_t scale = pair(f.scale2, f.scale2);
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+      float x, y;
+      unpair(fma_pair(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale, pair(fmaf(per, e, first), fmaf(per, e + 1, first))), x, y);
+      s[e] = __float_as_uint(x);
+      s[e + 1] = __float_as_uint(y);
+    }
+  } else if constexpr (kForm == FORM_BIAS) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(fmaf(-slope2, fabsf(far - e), __uint_as_float(s[e]) * f.scale2));
+  } else if (slope2 != 0.f) {
 #pragma unroll
     for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(fmaf(-slope2, fabsf(far - e), __uint_as_float(s[e])));
   }

@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld_32x32b_x32(ts, a);
           tmem_ld_wait();
           if constexpr (kForm != FORM_PLAIN) {
-            if (!masked && all_small(form, largest(a)))
+            if (!masked && (kForm == FORM_CAP ? all_small(form, largest(a)) : one_side(far, kCols)))
               form_scores<kForm, kForm == FORM_CAP, true>(form, a, slope2, far, bend);
             else
               form_scores<kForm, kForm == FORM_CAP, false>(form, a, slope2, far, bend);
@@ -732,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane == 0) mbar_arrive(bar(C_SEMPTY));
           [[maybe_unused]] uint64_t bend[kForm == FORM_CAP ? 16 : 1];
           if constexpr (kForm != FORM_PLAIN) {
-            if (!masked && all_small(form, pos < it.q.n ? largest(a) : 0.f))
+            if (!masked && (kForm == FORM_CAP ? all_small(form, pos < it.q.n ? largest(a) : 0.f) : one_side(far, kCols)))
               form_scores<kForm, kForm == FORM_CAP, true>(form, a, slope2, far, bend);
             else
               form_scores<kForm, kForm == FORM_CAP, false>(form, a, slope2, far, bend);
