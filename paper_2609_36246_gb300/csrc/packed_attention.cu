@@ -7,7 +7,9 @@
 // or the sequence's end), so a mask is one number a row.
 //
 // A CTA works on two slots of 128 query rows with the same keys (two heads of a key
-// head, or two tiles of a head) and walks the key tiles:
+// head, or two tiles of a head) and walks the key tiles from the last that a row sees to
+// the first (scores that a bias lowers with the distance are largest at its beginning, so
+// a row's reference stays):
 //   warp 8     TMA: query tiles, then key and value tiles into rings of three and two
 //   warp 9     MMA: S = Q K^T into tensor memory, O += P V with P read from there, the
 //              slots in turn (a warp for each: their products mix, both slots' rows then
@@ -134,11 +136,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           return true;
         };
+        const auto first_key = [&](int j) { return 128 * (tiles - 1 - j); };
         const auto keys = [&](int j) {
           if (!mbar_wait_warp(bar(B_KEMPTY + k.i), k.phase ^ 1, ctl)) return false;
           if (leader) {
             mbar_arrive_expect_tx(bar(B_KFULL + k.i), kTileBytes);
-            load_tile(sk + k.i * kTileBytes, &map_k, bar(B_KFULL + k.i), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + 128 * j);
+            load_tile(sk + k.i * kTileBytes, &map_k, bar(B_KFULL + k.i), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + first_key(j));
           }
           k.next(kK);
           return true;
@@ -150,13 +153,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!(ok = mbar_wait_warp(bar(B_VEMPTY + v.i), v.phase ^ 1, ctl))) break;
           if (leader) {
             mbar_arrive_expect_tx(bar(B_VFULL + v.i), kTileBytes);
-            load_tile(sv + v.i * kTileBytes, &map_v, bar(B_VFULL + v.i), kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + 128 * j);
+            load_tile(sv + v.i * kTileBytes, &map_v, bar(B_VFULL + v.i), kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + first_key(j));
           }
           // the sequence's last rows: what follows them up to whole K steps is zeroed
-          const int rows = seen - 128 * j;
+          const int rows = seen - first_key(j);
           if (rows < 128 && rows % 16 != 0) {
             if (!(ok = mbar_wait_warp(bar(B_VFULL + v.i), v.phase, ctl))) break;
-            if (it.q.n - 128 * j < 128) zero_rows(sv + v.i * kTileBytes, kBoxes, rows, up16(rows));
+            if (it.q.n - first_key(j) < 128) zero_rows(sv + v.i * kTileBytes, kBoxes, rows, up16(rows));
             fence_proxy_async_shared();
             __syncwarp();
             if (leader) mbar_arrive(bar(B_VFIX + v.i));
@@ -180,19 +183,20 @@ __global__ void __launch_bounds__(kThreads, 1)
         // for the tensor pipe lasts 300: so tiles are waited for together with the rows,
         // and P's second half while the first one's products run.)
         if (!(ok = mbar_wait_warp(bar(B_KFULL + k.i), k.phase, ctl))) break;
-        // rounds in which both slots have whole tiles, the first one apart
-        const int whole = min(it.seen[0], it.seen[1]) / 128;
+        // a slot's first round; those from `even` on: both slots have whole tiles
+        const int begin[2] = {tiles - it.tiles[0], tiles - it.tiles[1]}, even = tiles - min(it.seen[0], it.seen[1]) / 128;
+        const auto keys_of = [&](int a, int j) { return up16(min(128, it.seen[a] - 128 * (tiles - 1 - j))); };
         const auto whole_rounds = [&](auto s_steps, int& j) {
           constexpr int kS = decltype(s_steps)::value;
           constexpr uint32_t id_s = idesc_bf16(128, 128, false, false);
           const uint64_t dq[2] = {sdesc_sw128(sq, 16, 1024), sdesc_sw128(sq + kTileBytes, 16, 1024)};
-          for (; j < whole; ++j) {
+          for (; j < tiles; ++j) {
             const uint64_t dk = sdesc_sw128(sk + k.i * kTileBytes, 16, 1024), dv = sdesc_sw128(sv + v.i * kTileBytes, kBoxBytes, 1024);
             Turn next_k = k;
             next_k.next(kK);
-            const uint32_t more = j > 1 ? 1u : 0u;
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
+              const uint32_t more = j - 1 > begin[a] ? 1u : 0u;
               const Phase of[2] = {{bar(B_PREADY + 2 * a), n_p[a] & 1},
                                    a == 0 ? Phase{bar(B_VFULL + v.i), v.phase} : Phase{bar(B_KFULL + next_k.i), next_k.phase}};
               if (a == 0 || j + 1 < tiles ? !mbar_wait_warp(of, ctl) : !mbar_wait_warp(of[0].bar, of[0].parity, ctl)) return false;
@@ -203,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               mma_cols_of<8, 4, 8>(leader, t_o(a), t_s(a), dv, id_out, 1u);
               mma_rows_of<kS>(leader, t_s(a), dq[a], dk, id_s);
               umma_commit_by(leader, bar(B_SFULL + a));
-              if (j == it.tiles[a] - 1) umma_commit_by(leader, bar(B_QEMPTY + a));
+              if (j == tiles - 1) umma_commit_by(leader, bar(B_QEMPTY + a));
             }
             umma_commit_by(leader, bar(B_VEMPTY + v.i));
             umma_commit_by(leader, bar(B_KEMPTY + k.i));
@@ -213,8 +217,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           return true;
         };
         for (int j = 0; ok && j <= tiles; ++j) {
-          if (j == 1 && whole > 1 && steps >= 4) {
-            if (!(ok = mbar_wait_warp(bar(B_OEMPTY), (n_o[0]++ & 1) ^ 1, ctl) && mbar_wait_warp(bar(B_OEMPTY + 1), (n_o[1]++ & 1) ^ 1, ctl))) break;
+          if (j > even && j < tiles && steps >= 4) {
+#pragma unroll
+            for (int a = 0; ok && a < 2; ++a)
+              if (j - 1 == begin[a]) ok = mbar_wait_warp(bar(B_OEMPTY + a), (n_o[a]++ & 1) ^ 1, ctl);
+            if (!ok) break;
             if constexpr (kBoxes == 1)
               ok = whole_rounds(std::integral_constant<int, 4>{}, j);
             else
@@ -229,13 +236,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           bool have_v = false, have_k = j + 1 >= tiles;
 #pragma unroll
           for (int a = 0; a < 2; ++a) {
-            if (j > 0 && j <= it.tiles[a]) {
-              if (j == 1 && !(ok = mbar_wait_warp(bar(B_OEMPTY + a), (n_o[a]++ & 1) ^ 1, ctl))) break;
+            if (j > begin[a]) {
+              if (j - 1 == begin[a] && !(ok = mbar_wait_warp(bar(B_OEMPTY + a), (n_o[a]++ & 1) ^ 1, ctl))) break;
               const Phase rows = {bar(B_PREADY + 2 * a + 1), n_p[a]++ & 1};  // (P's second half: then the first is there too)
               if (!have_v) {
                 const Phase of[2] = {rows, {bar(B_VFULL + v.i), v.phase}};
                 if (!(ok = mbar_wait_warp(of, ctl))) break;
-                const int left = seen - 128 * (j - 1);
+                const int left = seen - 128 * (tiles - j);
                 if (left < 128 && left % 16 != 0) {
                   if (!(ok = mbar_wait_warp(bar(B_VFIX + v.i), fixed >> v.i & 1, ctl))) break;
                   fixed ^= 1u << v.i;
@@ -249,17 +256,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 break;
               }
               tc_fence_after();
-              const int ks = up16(min(128, it.seen[a] - 128 * (j - 1))) / 16;
-              mma_cols<8>(leader, t_o(a), t_s(a), sv + v.i * kTileBytes, id_out, ks, j > 1);
-              if (j == it.tiles[a]) umma_commit_by(leader, bar(B_OFULL + a));
+              mma_cols<8>(leader, t_o(a), t_s(a), sv + v.i * kTileBytes, id_out, keys_of(a, j - 1) / 16, j - 1 > begin[a]);
+              if (j == tiles) umma_commit_by(leader, bar(B_OFULL + a));
             }
-            if (j < it.tiles[a]) {
-              if (j == 0 && !(ok = mbar_wait_warp(bar(B_QFULL + a), n_q[a]++ & 1, ctl))) break;
+            if (j >= begin[a] && j < tiles) {
+              if (j == begin[a] && !(ok = mbar_wait_warp(bar(B_QFULL + a), n_q[a]++ & 1, ctl))) break;
               tc_fence_after();
-              const uint32_t id = idesc_bf16(128, up16(min(128, it.seen[a] - 128 * j)), false, false);
+              const uint32_t id = idesc_bf16(128, keys_of(a, j), false, false);
               mma_rows(leader, t_s(a), sq + a * kTileBytes, sk + k.i * kTileBytes, id, steps);
               umma_commit_by(leader, bar(B_SFULL + a));
-              if (j == it.tiles[a] - 1) umma_commit_by(leader, bar(B_QEMPTY + a));
+              if (j == tiles - 1) umma_commit_by(leader, bar(B_QEMPTY + a));
             }
           }
           if (!ok) break;
@@ -307,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool live = warp_uniform(static_cast<int>(pos - lane < it.q.n));
       const float mul = kForm == FORM_PLAIN ? form.scale2 : 1.f;
       float ref = 0.f, sum = 0.f;
-      for (int j = 0; j < tiles; ++j) {
+      for (int j = tiles - 1; j >= 0; --j) {
         if (!(ok = mbar_wait_warp(bar(B_SFULL + a), n_s++ & 1, ctl))) break;
         tc_fence_after();
         const auto arrive = [&](int h) {  // P's half h is there
@@ -360,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int c = 0; c < 4; ++c) top[c] = fmaxf(top[c], __uint_as_float(s[c][e]));
           const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * mul;
-          if (j == 0) ref = m > -INFINITY ? m : 0.f;
+          if (j == tiles - 1) ref = m > -INFINITY ? m : 0.f;
           uint64_t part[2];
           uint32_t w[2][32];
           const auto weights = [&](int h) {  // of half the columns
@@ -419,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           tmem_st_wait();
           m *= mul;
-          if (j == 0) ref = m > -INFINITY ? m : 0.f;
+          if (j == tiles - 1) ref = m > -INFINITY ? m : 0.f;
           if (__any_sync(0xffffffffu, m > ref + kLag)) follow(m);
           const uint64_t mul2 = pair(mul, mul), off2 = pair(-ref, -ref);
           uint64_t part = pair(sum, 0.f);
