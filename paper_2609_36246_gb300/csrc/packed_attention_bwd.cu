@@ -178,7 +178,9 @@ __global__ void __launch_bounds__(256) att_join_kernel(const AttArgs p, const fl
 // dV_t, S_{t+1}, dK_t, dP_{t+1}: P_{t+1} is formed while the last two run, dS_t while the
 // first two do.  (A warp for each pair mixes them: all four then end late.)
 constexpr int kQ = 3, kO = 2;  // stages of q and of do (whose rows' lse and delta come along)
-enum { A_KVFULL = 0, A_KVEMPTY, A_QFULL, A_QEMPTY = A_QFULL + kQ, A_QFIX = A_QEMPTY + kQ, A_DOFULL = A_QFIX + kQ,
+// An item's own tiles: narrow heads have room for the next one's.
+constexpr int own_stages(int boxes) { return boxes == 1 ? 2 : 1; }
+enum { A_KVFULL = 0, A_KVEMPTY = 2, A_QFULL = 4, A_QEMPTY = A_QFULL + kQ, A_QFIX = A_QEMPTY + kQ, A_DOFULL = A_QFIX + kQ,
        A_DOEMPTY = A_DOFULL + kO, A_DOFIX = A_DOEMPTY + kO, A_VECFULL = A_DOFIX + kO, A_VECEMPTY = A_VECFULL + kO,
        A_SFULL = A_VECEMPTY + kO, A_PREADY, A_DPFULL, A_DSREADY, A_OFULL, A_OEMPTY, A_DRAIN, A_RING,
        A_COUNT = A_RING + kRingBars };
@@ -190,7 +192,7 @@ struct KvItem {
   int end;
 };
 constexpr int kKvBars = (8 * A_COUNT + 15) / 16 * 16, kKvMisc = 16 + static_cast<int>(sizeof(ItemRing<KvItem>));
-constexpr int kv_smem(int boxes) { return (2 + kQ + kO) * boxes * kBoxBytes + kO * 1024 + kKvBars + kKvMisc; }
+constexpr int kv_smem(int boxes) { return (2 * own_stages(boxes) + kQ + kO) * boxes * kBoxBytes + kO * 1024 + kKvBars + kKvMisc; }
 __device__ __forceinline__ bool kv_item(const AttArgs& p, int i, int parts, KvItem& it, int& near) {
   const int units = p.Hk * parts, u = i % units;
   it.q = seq_of_slot<128>(p, i / units, near);
@@ -228,7 +230,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);  // (of 1024 bytes' alignment: there is no room to move up)
   constexpr uint32_t kTileBytes = kBoxes * kBoxBytes;
-  const uint32_t sk = raw, sv = sk + kTileBytes, sq = sv + kTileBytes, sdo = sq + kQ * kTileBytes;
+  constexpr int kOwn = own_stages(kBoxes);
+  const uint32_t skv = raw, sq = skv + 2 * kOwn * kTileBytes, sdo = sq + kQ * kTileBytes;
   const uint32_t vec0 = sdo + kO * kTileBytes;  // a stage's [2][128]: -lse, -delta
   float* vec = reinterpret_cast<float*>(smem_raw + (vec0 - raw));
   const uint32_t bar0 = vec0 + kO * 1024;
@@ -271,16 +274,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
-      uint32_t n_kv = 0;
-      Turn q, o;
+      Turn kv, q, o;
       bool ok = true;
       for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok);) {
-        if (!(ok = mbar_wait_warp(bar(A_KVEMPTY), (n_kv++ & 1) ^ 1, ctl))) break;
+        if (!(ok = mbar_wait_warp(bar(A_KVEMPTY + kv.i), kv.phase ^ 1, ctl))) break;
         if (leader) {
-          mbar_arrive_expect_tx(bar(A_KVFULL), 2 * kTileBytes);
-          load_tile(sk, &map_k, bar(A_KVFULL), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + it.k0);
-          load_tile(sv, &map_v, bar(A_KVFULL), kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + it.k0);
+          const uint32_t full = bar(A_KVFULL + kv.i), sk = skv + 2 * kv.i * kTileBytes;
+          mbar_arrive_expect_tx(full, 2 * kTileBytes);
+          load_tile(sk, &map_k, full, kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + it.k0);
+          load_tile(sk + kTileBytes, &map_v, full, kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + it.k0);
         }
+        kv.next(kOwn);
         KvStep at(p, it);
         for (int t = 0; t < it.steps; ++t, at.next(it), q.next(kQ), o.next(kO)) {
           float2 got[4];  // the rows' lse and delta, on their way while the stages are waited for
@@ -330,12 +334,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool leader = elect_one();
       const int steps = (p.D + 15) / 16;
       const uint32_t id_out = idesc_bf16(128, 16 * steps, false, true);
-      uint32_t n_kv = 0, n = 0, q_fixed = 0, o_fixed = 0;
-      Turn q, o;  // of the step whose second products are next
+      uint32_t n_o = 0, n = 0, q_fixed = 0, o_fixed = 0;
+      Turn kv, q, o;  // of the step whose second products are next
       bool ok = true;
-      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok); ++n_kv) {
+      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok); ++n_o, kv.next(kOwn)) {
         KvStep at(p, it);
         int rows = min(128, it.q.n - at.q0);  // (a tile of a sequence's last rows is shorter)
+        const uint32_t sk = skv + 2 * kv.i * kTileBytes, sv = sk + kTileBytes;
         const auto scores = [&](const Turn& qs) {
           mma_rows(leader, t_s, sk, sq + qs.i * kTileBytes, idesc_bf16(128, up16(rows), false, false), steps);
           umma_commit_by(leader, bar(A_SFULL));
@@ -344,12 +349,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           mma_rows(leader, t_dp, sv, sdo + os.i * kTileBytes, idesc_bf16(128, up16(rows), false, false), steps);
           umma_commit_by(leader, bar(A_DPFULL));
         };
-        const Phase begin[3] = {{bar(A_KVFULL), n_kv & 1}, {bar(A_QFULL + q.i), q.phase}, {bar(A_DOFULL + o.i), o.phase}};
+        const Phase begin[3] = {{bar(A_KVFULL + kv.i), kv.phase}, {bar(A_QFULL + q.i), q.phase}, {bar(A_DOFULL + o.i), o.phase}};
         if (!(ok = mbar_wait_warp(begin, ctl))) break;
         tc_fence_after();
         scores(q);
         slopes(o);
-        if (!(ok = mbar_wait_warp(bar(A_OEMPTY), (n_kv & 1) ^ 1, ctl))) break;
+        if (!(ok = mbar_wait_warp(bar(A_OEMPTY), (n_o & 1) ^ 1, ctl))) break;
         for (int t = 0; t < it.steps; ++t, ++n) {
           const bool more = t + 1 < it.steps;
           Turn q2 = q, o2 = o;
@@ -382,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!ok) break;
         umma_commit_by(leader, bar(A_OFULL));
-        umma_commit_by(leader, bar(A_KVEMPTY));
+        umma_commit_by(leader, bar(A_KVEMPTY + kv.i));
       }
       drain_mmas(bar(A_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
@@ -535,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // dQ_j: the products of a tile do not wait for the rows of the one before.  So a warp may
 // be done with a tile that another has not begun: barriers of dP and dS by parity.
 constexpr int kK = 3, kV = 2;  // stages of key and value tiles
-enum { C_QFULL = 0, C_QEMPTY, C_KFULL, C_KEMPTY = C_KFULL + kK, C_KFIX = C_KEMPTY + kK, C_VFULL = C_KFIX + kK,
+enum { C_QFULL = 0, C_QEMPTY = 2, C_KFULL = 4, C_KEMPTY = C_KFULL + kK, C_KFIX = C_KEMPTY + kK, C_VFULL = C_KFIX + kK,
        C_VEMPTY = C_VFULL + kV, C_SFULL = C_VEMPTY + kV, C_SEMPTY, C_DPFULL, C_DSREADY = C_DPFULL + 2, C_OFULL = C_DSREADY + 2, C_OEMPTY,
        C_DRAIN, C_RING, C_COUNT = C_RING + kRingBars };
 
@@ -545,7 +550,7 @@ struct QItem {
   int end;
 };
 constexpr int kQBars = (8 * C_COUNT + 15) / 16 * 16, kQMisc = 16 + static_cast<int>(sizeof(ItemRing<QItem>));
-constexpr int dq_smem(int boxes) { return 1024 + (2 + kK + kV) * boxes * kBoxBytes + kQBars + kQMisc; }
+constexpr int dq_smem(int boxes) { return 1024 + (2 * own_stages(boxes) + kK + kV) * boxes * kBoxBytes + kQBars + kQMisc; }
 __device__ __forceinline__ bool q_item(const AttArgs& p, int i, QItem& it, int& near) {
   it.q = seq_of_slot<128>(p, i / p.Hq, near);
   if (it.q.tile < 0) return false;
@@ -566,7 +571,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   constexpr uint32_t kTileBytes = kBoxes * kBoxBytes;
-  const uint32_t sq = base, sdo = sq + kTileBytes, sk = sdo + kTileBytes, sv = sk + kK * kTileBytes;
+  constexpr int kOwn = own_stages(kBoxes);
+  const uint32_t sqdo = base, sk = sqdo + 2 * kOwn * kTileBytes, sv = sk + kK * kTileBytes;
   const uint32_t bar0 = sv + kV * kTileBytes;
   uint8_t* misc = smem_raw + (bar0 - raw) + kQBars;
   ItemRing<QItem>& ring = *reinterpret_cast<ItemRing<QItem>*>(misc + 16);
@@ -605,17 +611,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     regs_dec<kRegsRest>();
     if (warp == kTmaWarp) {
       const bool leader = elect_one();
-      uint32_t n_q = 0;
-      Turn k, v;
+      Turn q, k, v;
       bool ok = true;
       for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok);) {
         const int kv = it.head / (p.Hq / p.Hk);
-        if (!(ok = mbar_wait_warp(bar(C_QEMPTY), (n_q++ & 1) ^ 1, ctl))) break;
+        if (!(ok = mbar_wait_warp(bar(C_QEMPTY + q.i), q.phase ^ 1, ctl))) break;
         if (leader) {
-          mbar_arrive_expect_tx(bar(C_QFULL), 2 * kTileBytes);
-          load_tile(sq, &map_q, bar(C_QFULL), kBoxes, p.q.head_stride ? it.head : 0, it.q.start + it.q0);
-          load_tile(sdo, &map_do, bar(C_QFULL), kBoxes, p.d_o.head_stride ? it.head : 0, it.q.start + it.q0);
+          const uint32_t full = bar(C_QFULL + q.i), sq = sqdo + 2 * q.i * kTileBytes;
+          mbar_arrive_expect_tx(full, 2 * kTileBytes);
+          load_tile(sq, &map_q, full, kBoxes, p.q.head_stride ? it.head : 0, it.q.start + it.q0);
+          load_tile(sq + kTileBytes, &map_do, full, kBoxes, p.d_o.head_stride ? it.head : 0, it.q.start + it.q0);
         }
+        q.next(kOwn);
         for (int j = 0; j < it.tiles; ++j, k.next(kK), v.next(kV)) {
           if (!(ok = mbar_wait_warp(bar(C_KEMPTY + k.i), k.phase ^ 1, ctl))) break;
           if (leader) {
@@ -644,12 +651,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool leader = elect_one();
       const int steps = (p.D + 15) / 16;
       const uint32_t id_out = idesc_bf16(128, 16 * steps, false, true);
-      uint32_t n_q = 0, n = 0, fixed = 0;  // items, tiles
-      Turn k, v;                           // of the tile whose S and dP are next
+      uint32_t n_o = 0, n = 0, fixed = 0;  // items, tiles
+      Turn q, k, v;                        // k, v: of the tile whose S and dP are next
       bool ok = true;
-      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok); ++n_q) {
+      for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok); ++n_o, q.next(kOwn)) {
         const auto cols_of = [&](int j) { return up16(min(128, it.seen - 128 * j)); };
-        const Phase begin[2] = {{bar(C_QFULL), n_q & 1}, {bar(C_OEMPTY), (n_q & 1) ^ 1}};
+        const uint32_t sq = sqdo + 2 * q.i * kTileBytes, sdo = sq + kTileBytes;
+        const Phase begin[2] = {{bar(C_QFULL + q.i), q.phase}, {bar(C_OEMPTY), (n_o & 1) ^ 1}};
         if (!(ok = mbar_wait_warp(begin, ctl))) break;
         int last_k = 0;  // the stage of the tile before
         for (int j = 0; j <= it.tiles; ++j) {
@@ -685,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         n += it.tiles;
         umma_commit_by(leader, bar(C_OFULL));
-        umma_commit_by(leader, bar(C_QEMPTY));
+        umma_commit_by(leader, bar(C_QEMPTY + q.i));
       }
       drain_mmas(bar(C_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
