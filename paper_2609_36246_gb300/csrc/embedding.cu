@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const EmbArgs 
   if (threadIdx.x < kBins) count[threadIdx.x] = 0;
   if (!kFirst) grid_wait();
   if constexpr (kFirst) {
-    const int words = (p.V + 31) / 32;
+    const int words = (p.V - 1) / 32 + 1;
     for (int w = blockIdx.x * kSortThreads + threadIdx.x; w < words; w += gridDim.x * kSortThreads) s.named[w] = 0;
   }
   const int n = kFirst ? ids_in_use(p) : 0;
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_one_kernel(const EmbArgs p,
   uint32_t key[kItems];
   int32_t at[kItems];
   const int first = warp * 32 * kItems + lane;
-  for (int w = threadIdx.x; w < (p.V + 31) / 32; w += kSortThreads) s.named[w] = 0;
+  for (int w = threadIdx.x; w < (p.V - 1) / 32 + 1; w += kSortThreads) s.named[w] = 0;
 #pragma unroll
   for (int r = 0; r < kItems; ++r) {
     at[r] = first + 32 * r;

@@ -172,3 +172,18 @@ def test_rows_beyond_32_bits():
     dW = B.olive_embedding_bwd(rows, ids, T, grad_dtype=BF16, out=torch.full_like(x, 7))
     assert torch.equal(dW[T - 1], (2 * rows[0].float()).to(BF16)) and torch.equal(dW[T - 2], rows[2])
     assert torch.equal(dW[0], rows[1]) and not dW[1:T - 2].any()
+
+
+def test_embedding_of_the_largest_vocabulary():
+    """Every row of 2^31 - 1 is written, whatever the workspace held."""
+    V, d = 2**31 - 1, 8
+    ids = torch.tensor([V - 1, 0, 1 << 30, V - 1, 63], dtype=torch.int32, device="cuda")
+    dy = torch.arange(1, 41, device="cuda").reshape(5, d).to(BF16)
+    ws = torch.full((B.olive_workspace_size("embedding_bwd", 5, d, V),), 255, dtype=torch.uint8, device="cuda")
+    dW = torch.empty((V, d), dtype=BF16, device="cuda").fill_(7)
+    B.olive_embedding_bwd(dy, ids, V, ws=ws, out=dW)
+    for row, tokens in ((V - 1, [0, 3]), (0, [1]), (1 << 30, [2]), (63, [4])):
+        assert torch.equal(dW[row], dy[tokens].float().sum(0).to(BF16))
+        dW[row] = 0
+    for rows in dW.split(1 << 27):
+        assert not rows.any()
