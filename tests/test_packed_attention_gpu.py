@@ -18,6 +18,8 @@ pytestmark = pytest.mark.gpu
 
 BF16 = torch.bfloat16
 STEP = 2.0 ** -8 * 1.01
+# A weight (of a row whose largest is near 1) or a product below the smallest normal number may count as 0.
+FLUSH = 2.0 ** -126
 
 
 def _case(lens, hq, hk, D, pad=0, prefix=None, cap=0.0, bias=False, causal=True, seed=0, sharp=1.0, scale=None):
@@ -79,14 +81,17 @@ def _reference(s, grads=False):
             err = err + 2.0 ** -20 * m["cap"]
         if m["slopes"] is not None:
             z = z - m["slopes"][h].double() * far
-            err = err + 2.0 ** -22 * m["slopes"][h].double() * far
+            # log2 e (half a step), times the slope, times the distance, to the tile's column, to the
+            # score, less the reference: 5.5 of 2^-24
+            err = err + 2.0 ** -21 * m["slopes"][h].double().abs() * far
         err = (err * seen).amax(-1, keepdim=True) + 2.0 ** -20
         z = z.masked_fill(~seen, -math.inf)
         lse = torch.logsumexp(z, -1)
         p = torch.where(seen, (z - lse[:, None]).exp(), 0.0)
         o = p @ V
         out["o"][:, h], out["lse"][h] = o, lse
-        out["tol_o"][:, h] = (STEP + 2 * err) * (p @ V.abs()) + STEP * o.abs()
+        lost = FLUSH * seen.double()
+        out["tol_o"][:, h] = (STEP + 2 * err) * (p @ V.abs()) + STEP * o.abs() + lost @ V.abs()
         out["tol_lse"][h] = err[:, 0] + 2.0 ** -21 * (1 + torch.where(seen.any(-1), lse.abs(), 0.0))
         if not grads:
             continue
@@ -99,7 +104,8 @@ def _reference(s, grads=False):
         e_dp = 2.0 ** -16 * (dO.abs() @ V.abs().t())
         e_delta = (STEP + 2 * err) * (dO.abs() * (p @ V.abs())).sum(-1, keepdim=True) + STEP * (dO.abs() * o.abs()).sum(-1, keepdim=True)
         e_ds = p * (e_dp + e_delta) + (2 * err + STEP + 2.0 ** -20) * p * (dp.abs() + delta.abs()) + STEP * ds.abs()
-        e_p = (STEP + 2 * err) * p
+        e_ds = e_ds + lost * (1 + dp.abs() + delta.abs())
+        e_p = (STEP + 2 * err) * p + lost
         out["dq"][:, h] = scale * ds @ K
         out["tol_dq"][:, h] = scale * e_ds @ K.abs() + STEP * out["dq"][:, h].abs()
         out["dk"][:, h // per] += scale * ds.t() @ Q
@@ -190,6 +196,24 @@ def test_largest_scores_late():
     by = torch.linspace(0.2, 12, 700, device="cuda")[:, None, None]
     s["k"].copy_((s["q"][:, :1].float().mean(0, keepdim=True) * 0 + 1) * by.to(BF16))
     s["q"].copy_(s["q"].abs())
+    _check(s)
+
+
+def test_largest_scores_early():
+    """The same the other way round."""
+    s = _case([700], 2, 1, 64)
+    by = torch.linspace(12, 0.2, 700, device="cuda")[:, None, None]
+    s["k"].copy_(torch.ones_like(s["k"]) * by.to(BF16))
+    s["q"].copy_(s["q"].abs())
+    _check(s)
+
+
+@pytest.mark.parametrize("slope", [-0.5, -0.03, 0.03, 0.5, 4.0])
+@pytest.mark.parametrize("form", [dict(), dict(prefix=300), dict(causal=False), dict(cap=5.0)], ids=str)
+def test_slopes(form, slope):
+    """Scores that fall, or rise, with the distance by up to 500 a tile."""
+    s = _case([700, 129, 1], 2, 1, 64, bias=True, **form)
+    s["more"]["slopes"] = torch.tensor([slope, slope / 3], device="cuda")
     _check(s)
 
 
