@@ -6,8 +6,8 @@
 // What a row sees is always its sequence's first keys (up to itself, its prompt's end
 // or the sequence's end), so a mask is one number a row.
 //
-// A CTA works on two slots of 128 query rows with the same keys (two heads of a key
-// head, or two tiles of a head) and walks the key tiles from the last that a row sees to
+// A CTA works on two slots of 128 query rows, two heads of a key head or two tiles of a
+// head (or two heads each with its own keys, where sequences are short), and walks the key tiles from the last that a row sees to
 // the first (scores that a bias lowers with the distance are largest at its beginning, so
 // a row's reference stays):
 //   warp 8     TMA: query tiles, then key and value tiles into rings of three and two
@@ -40,39 +40,43 @@ enum { B_QFULL = 0, B_QEMPTY = 2, B_KFULL = 4, B_KEMPTY = B_KFULL + kK, B_VFULL 
        B_VFIX = B_VEMPTY + kV, B_SFULL = B_VFIX + kV, B_PREADY = B_SFULL + 2, B_OFULL = B_PREADY + 4, B_OEMPTY = B_OFULL + 2,
        B_DRAIN = B_OEMPTY + 2, B_RING, B_COUNT = B_RING + kRingBars };
 
+// What an item's two slots are: two tiles of a head, two heads of a key head, or two heads
+// whose keys and values are loaded apart.
+enum { PAIR_TILES = 0, PAIR_HEADS = 1, PAIR_APART = 2 };
+constexpr int rows_of(int pair) { return pair == PAIR_TILES ? 256 : 128; }
 // An item's slots: heads, first rows and key tiles.
 struct Item {
   Seq q;
-  int kv_head, head[2], row0[2], tiles[2], seen[2];  // seen: keys that the slot's last row sees
+  int kv_head[2], head[2], row0[2], tiles[2], seen[2];  // seen: keys that the slot's last row sees
   int end;
 };
 constexpr int kMisc = 16 + static_cast<int>(sizeof(ItemRing<Item>));
 constexpr int smem_bytes(int boxes) {
   return 1024 + (2 + kK + kV) * boxes * kBoxBytes + (8 * B_COUNT + 15) / 16 * 16 + kMisc;
 }
-// Two heads of a key head where their number is even, else two tiles of a head.
-template <bool kPairHeads>
+template <int kPair>
 __device__ __forceinline__ bool item_at(const AttArgs& p, int i, int units, Item& it, int& near) {
   const int slot = i / units, u = i % units;
-  it.q = seq_of_slot<kPairHeads ? 128 : 256>(p, slot, near);
+  constexpr int R = rows_of(kPair);
+  it.q = seq_of_slot<R>(p, slot, near);
   if (it.q.tile < 0) return false;
-  constexpr int R = kPairHeads ? 128 : 256;
   // the longest rows first
   const int tile = p.causal ? (it.q.n + R - 1) / R - 1 - it.q.tile : it.q.tile;
   const int per = p.Hq / p.Hk;
 #pragma unroll
   for (int a = 0; a < 2; ++a) {
-    it.head[a] = kPairHeads ? 2 * u + a : u;
-    it.row0[a] = kPairHeads ? tile * 128 : tile * 256 + a * 128;
-    it.seen[a] = it.row0[a] < it.q.n ? keys_seen(p, it.q, min(it.row0[a] + 128, it.q.n) - 1) : 0;
+    it.head[a] = kPair == PAIR_TILES ? u : 2 * u + a;
+    it.row0[a] = kPair == PAIR_TILES ? tile * 256 + a * 128 : tile * 128;
+    const bool there = it.row0[a] < it.q.n && (kPair != PAIR_APART || it.head[a] < p.Hq);
+    it.seen[a] = there ? keys_seen(p, it.q, min(it.row0[a] + 128, it.q.n) - 1) : 0;
     it.tiles[a] = (it.seen[a] + 127) / 128;
+    it.kv_head[a] = it.head[a] / per;
   }
-  it.kv_head = it.head[0] / per;
   it.end = 0;
   return true;
 }
 
-template <int kBoxes, bool kPairHeads, int kForm>
+template <int kBoxes, int kPair, int kForm>
 __global__ void __launch_bounds__(kThreads, 1)
     att_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const AttArgs p, int units, int ask) {
@@ -137,32 +141,52 @@ __global__ void __launch_bounds__(kThreads, 1)
           return true;
         };
         const auto first_key = [&](int j) { return 128 * (tiles - 1 - j); };
-        const auto keys = [&](int j) {
+        const auto keys = [&](int j, int a) {
           if (!mbar_wait_warp(bar(B_KEMPTY + k.i), k.phase ^ 1, ctl)) return false;
           if (leader) {
             mbar_arrive_expect_tx(bar(B_KFULL + k.i), kTileBytes);
-            load_tile(sk + k.i * kTileBytes, &map_k, bar(B_KFULL + k.i), kBoxes, p.k.head_stride ? it.kv_head : 0, it.q.start + first_key(j));
+            load_tile(sk + k.i * kTileBytes, &map_k, bar(B_KFULL + k.i), kBoxes, p.k.head_stride ? it.kv_head[a] : 0, it.q.start + first_key(j));
           }
           k.next(kK);
           return true;
         };
-        if (!(ok = query(0) && keys(0) && query(1))) break;
-        for (int j = 0; j < tiles; ++j, v.next(kV)) {
-          // (keys a tile ahead: V's stage is free only after the round before)
-          if (j + 1 < tiles && !(ok = keys(j + 1))) break;
-          if (!(ok = mbar_wait_warp(bar(B_VEMPTY + v.i), v.phase ^ 1, ctl))) break;
+        const auto values = [&](const Turn& to, int j, int a) {
+          if (!mbar_wait_warp(bar(B_VEMPTY + to.i), to.phase ^ 1, ctl)) return false;
           if (leader) {
-            mbar_arrive_expect_tx(bar(B_VFULL + v.i), kTileBytes);
-            load_tile(sv + v.i * kTileBytes, &map_v, bar(B_VFULL + v.i), kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + first_key(j));
+            mbar_arrive_expect_tx(bar(B_VFULL + to.i), kTileBytes);
+            load_tile(sv + to.i * kTileBytes, &map_v, bar(B_VFULL + to.i), kBoxes, p.v.head_stride ? it.kv_head[a] : 0, it.q.start + first_key(j));
           }
-          // the sequence's last rows: what follows them up to whole K steps is zeroed
+          return true;
+        };
+        // the sequence's last rows: what follows them up to whole K steps is zeroed
+        const auto last_values = [&](const Turn& at, int j) {
           const int rows = seen - first_key(j);
           if (rows < 128 && rows % 16 != 0) {
-            if (!(ok = mbar_wait_warp(bar(B_VFULL + v.i), v.phase, ctl))) break;
-            if (it.q.n - first_key(j) < 128) zero_rows(sv + v.i * kTileBytes, kBoxes, rows, up16(rows));
+            if (!mbar_wait_warp(bar(B_VFULL + at.i), at.phase, ctl)) return false;
+            if (it.q.n - first_key(j) < 128) zero_rows(sv + at.i * kTileBytes, kBoxes, rows, up16(rows));
             fence_proxy_async_shared();
             __syncwarp();
-            if (leader) mbar_arrive(bar(B_VFIX + v.i));
+            if (leader) mbar_arrive(bar(B_VFIX + at.i));
+          }
+          return true;
+        };
+        if constexpr (kPair == PAIR_APART) {
+          const bool two = it.tiles[1] > 0;
+          if (!(ok = query(0) && keys(0, 0) && (!two || (query(1) && keys(0, 1))))) break;
+          for (int j = 0; j < tiles; ++j) {
+            if (j + 1 < tiles && !(ok = keys(j + 1, 0) && (!two || keys(j + 1, 1)))) break;
+            const Turn v0 = v;
+            v.next(kV);
+            const Turn v1 = v;
+            if (two) v.next(kV);
+            if (!(ok = values(v0, j, 0) && (!two || values(v1, j, 1)) && last_values(v0, j) && (!two || last_values(v1, j)))) break;
+          }
+        } else {
+          if (!(ok = query(0) && keys(0, 0) && query(1))) break;
+          for (int j = 0; j < tiles; ++j, v.next(kV)) {
+            // (keys a tile ahead: V's stage is free only after the round before)
+            if (j + 1 < tiles && !(ok = keys(j + 1, 0))) break;
+            if (!(ok = values(v, j, 0) && last_values(v, j))) break;
           }
         }
         if (ok && leader) mbar_arrive(ring_at.issued());
@@ -178,6 +202,41 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool ok = true;
       for (uint32_t n = 0; ok && next_item<true>(ring, ring_at, n, it, ctl, ok);) {
         const int tiles = max(it.tiles[0], it.tiles[1]), seen = max(it.seen[0], it.seen[1]);
+        if constexpr (kPair == PAIR_APART) {  // (short sequences: most have one tile)
+          const int left = up16(min(128, seen - 128 * (tiles - 1)));  // of the first round's tile, the sequence's last
+          for (int j = 0; ok && j <= tiles; ++j) {
+            const auto keys_at = [&](int i) { return i == 0 ? left : 128; };
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+              if (it.tiles[a] == 0) continue;
+              if (j > 0) {
+                if (j == 1 && !(ok = mbar_wait_warp(bar(B_OEMPTY + a), (n_o[a]++ & 1) ^ 1, ctl))) break;
+                const Phase of[2] = {{bar(B_PREADY + 2 * a + 1), n_p[a]++ & 1}, {bar(B_VFULL + v.i), v.phase}};
+                if (!(ok = mbar_wait_warp(of, ctl))) break;
+                if (j == 1 && seen % 16 != 0) {
+                  if (!(ok = mbar_wait_warp(bar(B_VFIX + v.i), fixed >> v.i & 1, ctl))) break;
+                  fixed ^= 1u << v.i;
+                }
+                tc_fence_after();
+                mma_cols<8>(leader, t_o(a), t_s(a), sv + v.i * kTileBytes, id_out, keys_at(j - 1) / 16, j > 1);
+                umma_commit_by(leader, bar(B_VEMPTY + v.i));
+                v.next(kV);
+                if (j == tiles) umma_commit_by(leader, bar(B_OFULL + a));
+              }
+              if (j < tiles) {
+                if (j == 0 && !(ok = mbar_wait_warp(bar(B_QFULL + a), n_q[a]++ & 1, ctl))) break;
+                if (!(ok = mbar_wait_warp(bar(B_KFULL + k.i), k.phase, ctl))) break;
+                tc_fence_after();
+                mma_rows(leader, t_s(a), sq + a * kTileBytes, sk + k.i * kTileBytes, idesc_bf16(128, keys_at(j), false, false), steps);
+                umma_commit_by(leader, bar(B_SFULL + a));
+                umma_commit_by(leader, bar(B_KEMPTY + k.i));
+                k.next(kK);
+                if (j == tiles - 1) umma_commit_by(leader, bar(B_QEMPTY + a));
+              }
+            }
+          }
+          continue;
+        }
         // A round: O += P V of the tile before and S of this one, slot 0, then slot 1.
         // (A wait takes some 100 cycles where nothing is waited for, and what is queued
         // for the tensor pipe lasts 300: so tiles are waited for together with the rows,
@@ -279,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       drain_mmas(bar(B_DRAIN), leader, p.wait_limit_ns);
     } else if (warp == kItemWarp) {
       int near = 0;
-      hand_out(ring, ring_at, ask, ctl, [&](int i, Item& item) { return item_at<kPairHeads>(p, i, units, item, near); },
+      hand_out(ring, ring_at, ask, ctl, [&](int i, Item& item) { return item_at<kPair>(p, i, units, item, near); },
                [&](int i) {
                  if (i == 0) check_offsets(p);
                  const int64_t parts = min(static_cast<int64_t>(gridDim.x), kParts);
@@ -489,31 +548,39 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-template <int kBoxes, bool kPairHeads, int kForm>
+template <int kBoxes, int kPair, int kForm>
 olive_status run_fwd(const Ctx& c, const AttArgs& a) {
   CUtensorMap mq, mk, mv;
   if (!encode_heads(&mq, a.q, a.T, a.Hq, a.D) || !encode_heads(&mk, a.k, a.T, a.Hk, a.D) || !encode_heads(&mv, a.v, a.T, a.Hk, a.D))
     return OLIVE_ERR_CUDA;
   static std::atomic<int> done[kMaxDevices];
-  const auto kernel = att_fwd_kernel<kBoxes, kPairHeads, kForm>;
+  const auto kernel = att_fwd_kernel<kBoxes, kPair, kForm>;
   constexpr int kSmem = smem_bytes(kBoxes);
   if (!set_smem_once(reinterpret_cast<const void*>(kernel), kSmem, c.device, done)) return OLIVE_ERR_CUDA;
-  const int units = kPairHeads ? a.Hq / 2 : a.Hq;
-  const int64_t items = att_slots(a.T, a.S, kPairHeads ? 128 : 256) * units;
+  const int units = kPair == PAIR_TILES ? a.Hq : (a.Hq + 1) / 2;
+  const int64_t items = att_slots(a.T, a.S, rows_of(kPair)) * units;
   kernel<<<static_cast<unsigned>(items), kThreads, kSmem, c.stream>>>(mq, mk, mv, a, units,
                                                                      when_to_ask(items, c.num_sms, a.T, a.S));
   return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
 }
 
-template <int kBoxes, bool kPairHeads>
+template <int kBoxes, int kPair>
 olive_status by_form(const Ctx& c, const AttArgs& a) {
-  if (a.cap > 0.f) return run_fwd<kBoxes, kPairHeads, FORM_CAP>(c, a);
-  return a.slopes ? run_fwd<kBoxes, kPairHeads, FORM_BIAS>(c, a) : run_fwd<kBoxes, kPairHeads, FORM_PLAIN>(c, a);
+  if (a.cap > 0.f) return run_fwd<kBoxes, kPair, FORM_CAP>(c, a);
+  return a.slopes ? run_fwd<kBoxes, kPair, FORM_BIAS>(c, a) : run_fwd<kBoxes, kPair, FORM_PLAIN>(c, a);
 }
 
+// Two heads of a key head where their number is even: K and V are loaded once for both.
+// Else two tiles of a head, or two heads apart where sequences are so short that the second
+// tile is mostly empty, or causal and so short that items of 256 rows end too unevenly.
+// (8192 tokens, two tiles and apart, us.  16 + 16 heads of 64 in sequences of 41: 59 and 45;
+// of 128 in 128 that see all: 49 and 53, 1024: 77 and 86; causal 256: 64 and 53, 384: 57 and
+// 49, 1024: 66 and 67.)
+bool heads_apart(const AttArgs& a) { return a.Hq > 1 && a.T / a.S < (a.causal ? 512 : 128); }
 template <int kBoxes>
 olive_status by_heads(const Ctx& c, const AttArgs& a) {
-  return a.Hq / a.Hk % 2 == 0 ? by_form<kBoxes, true>(c, a) : by_form<kBoxes, false>(c, a);
+  if (a.Hq / a.Hk % 2 == 0) return by_form<kBoxes, PAIR_HEADS>(c, a);
+  return heads_apart(a) ? by_form<kBoxes, PAIR_APART>(c, a) : by_form<kBoxes, PAIR_TILES>(c, a);
 }
 
 }  // namespace
