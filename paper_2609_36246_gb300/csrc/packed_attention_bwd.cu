@@ -59,6 +59,7 @@ __device__ __forceinline__ const __nv_bfloat16* row_of(const HeadsView& x, int64
 __global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttArgs p, float2* stats) {
   constexpr int kGroups = kDeltaThreads / 16, kAtOnce = 2;
   const int head = static_cast<int>(blockIdx.x % p.Hq), slot = static_cast<int>(blockIdx.x / p.Hq);
+  grid_launch_dependents();
   int near = 0;
   const Seq q = seq_of_slot<128>(p, slot, near);
   if (q.tile < 0) return;
@@ -149,6 +150,8 @@ __device__ __forceinline__ int64_t sums_at(const AttArgs& p, bool is_k, int part
 }
 // dv and dk of the query heads' parts added, in their order.
 __global__ void __launch_bounds__(256) att_join_kernel(const AttArgs p, const float* sums, int parts) {
+  grid_launch_dependents();
+  grid_wait();
   const int vecs = p.D / 8;
   const int64_t n = static_cast<int64_t>(cu_at(p, p.S)) * p.Hk * vecs;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < 2 * n; i += static_cast<int64_t>(gridDim.x) * 256) {
@@ -265,6 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  grid_launch_dependents();
+  grid_wait();
   const uint32_t tmem = warp_uniform(*tmem_slot);
   const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 384;
   const WaitCtl ctl{abort_flag, p.wait_limit_ns};
@@ -601,6 +606,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  grid_launch_dependents();
+  grid_wait();
   const uint32_t tmem = warp_uniform(*tmem_slot);
   const auto t_dp = [&](uint32_t n) { return tmem + 128u + 128u * (n & 1); };
   const uint32_t t_s = tmem, t_dq = tmem + 384;
@@ -815,6 +822,23 @@ int head_parts(int64_t T, int64_t Hq, int64_t Hk) {
   return tiles >= 4 && tiles * Hk <= 152 ? static_cast<int>(Hq / Hk) : 1;
 }
 
+// Launches a kernel that waits for the one ahead by itself, once it has set itself up: it
+// starts on SMs that the one ahead leaves idle at its end.
+template <class... K, class... A>
+void launch_after(const Ctx& c, void (*kernel)(K...), int64_t blocks, int threads, size_t smem, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = c.stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...);
+}
+
 template <int kBoxes, int kForm>
 olive_status run_bwd(const Ctx& c, const AttArgs& a) {
   CUtensorMap mq, mk, mv, mdo;
@@ -835,13 +859,12 @@ olive_status run_bwd(const Ctx& c, const AttArgs& a) {
   att_delta_kernel<<<static_cast<unsigned>(slots * a.Hq), kDeltaThreads, 0, c.stream>>>(a, stats);
   const int parts = head_parts(a.T, a.Hq, a.Hk);
   float* sums = reinterpret_cast<float*>(static_cast<char*>(a.ws) + stats_bytes(a.T, a.Hq));
-  dkdv<<<static_cast<unsigned>(slots * a.Hk * parts), kThreads, kSmemKv, c.stream>>>(mq, mk, mv, mdo, a, stats, sums, parts,
-                                                                                    ask(slots * a.Hk * parts));
+  launch_after(c, dkdv, slots * a.Hk * parts, kThreads, kSmemKv, mq, mk, mv, mdo, a, stats, sums, parts, ask(slots * a.Hk * parts));
   if (parts > 1) {
     const int64_t blocks = ceil_div(2ll * a.T * a.Hk * (a.D / 8), 256);
-    att_join_kernel<<<static_cast<unsigned>(std::min<int64_t>(blocks, 16 * c.num_sms)), 256, 0, c.stream>>>(a, sums, parts);
+    launch_after(c, att_join_kernel, std::min<int64_t>(blocks, 16 * c.num_sms), 256, 0, a, sums, parts);
   }
-  dq<<<static_cast<unsigned>(slots * a.Hq), kThreads, kSmemQ, c.stream>>>(mq, mk, mv, mdo, a, stats, ask(slots * a.Hq));
+  launch_after(c, dq, slots * a.Hq, kThreads, kSmemQ, mq, mk, mv, mdo, a, stats, ask(slots * a.Hq));
   return cudaGetLastError() == cudaSuccess ? OLIVE_OK : OLIVE_ERR_CUDA;
 }
 
