@@ -775,8 +775,8 @@ OLIVE_API olive_status olive_row_norm_bwd(const void* dy, const void* h, const v
  * bf16, D values of a head contiguous; token and head strides as in
  * olive_qk_norm_rope_fwd, so q, k, v may be views of one projection (the token stride is
  * not 0 where T > 1).  lse may be NULL.  Scores, maxima and sums are fp32; the weights
- * exp(s - reference) are rounded to bf16 as operands of the second product (2^-9
- * relative each).  A value that is not finite in a row of k or v reaches rows of its own
+ * exp(s - reference) are rounded to bf16 as operands of the second product (2^-8
+ * relative each at most).  A value that is not finite in a row of k or v reaches rows of its own
  * sequence only (it may reach earlier ones of its 128-row tile).
  *   D a multiple of 8, 8 <= D <= 128; Hq a multiple of Hk, 1 <= Hk <= Hq <= 4096;
  *   S >= 1; 0 <= T <= 2^30; scale > 0; cap >= 0; strides multiples of 8, base pointers
@@ -802,7 +802,8 @@ OLIVE_API olive_status olive_packed_attention_fwd(
  *   dq_i = scale sum dz_ij k_j,   dk_j = scale sum dz_ij q_i
  * t_ij = tanh(z_ij / cap), 0 without a cap; dk and dv summed over the query heads of a
  * key head.  p and dz are rounded to bf16 as operands, sums are fp32 in a fixed order.
- * Rows behind the last sequence get 0.  All views bf16 with strides of their own, as in
+ * Rows behind the last sequence get 0.  What is not finite in a row reaches its own
+ * sequence only.  All views bf16 with strides of their own, as in
  * the forward; the heads of dq, dk and dv must not share memory, nor those with the inputs.
  * workspace: olive_workspace_size(OLIVE_OP_PACKED_ATTENTION_BWD, T, D, Hk, Hq, 0, 0) bytes.
  */
