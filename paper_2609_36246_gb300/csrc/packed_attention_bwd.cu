@@ -35,88 +35,140 @@ static_assert(4 * kRegsRows + kRegsRest <= 5 * kRegsLaunch, "the block's registe
 // ------------------------------------------------------------------ delta ---
 // Rows that see up to this many keys have their delta from the keys themselves: <do, o>
 // carries o's rounding, which is large beside dp - delta where one key has all the weight.
+// They are among the first so many of a sequence.
 constexpr int kFewKeys = 16;
 constexpr int kDeltaThreads = 128;
 
-__device__ __forceinline__ void eight(const __nv_bfloat16* at, bool in, float (&v)[8]) {
-  const uint4 r = in ? *reinterpret_cast<const uint4*>(at) : make_uint4(0, 0, 0, 0);
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-// Sum over the 16 lanes of a row.
-__device__ __forceinline__ float dot16(const float (&a)[8], const float (&b)[8]) {
-  float s = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s = fmaf(a[e], b[e], s);
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return s;
-}
 __device__ __forceinline__ const __nv_bfloat16* row_of(const HeadsView& x, int64_t t, int h) {
   return static_cast<const __nv_bfloat16*>(x.x) + t * x.token_stride + h * x.head_stride;
 }
-// stats: [Hq, T] of (lse in base 2, delta); a block works on a tile's rows of one head,
-// 16 lanes a row, two rows' loads in flight together.
-__global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttArgs p, float2* stats) {
-  constexpr int kGroups = kDeltaThreads / 16, kAtOnce = 2;
-  const int head = static_cast<int>(blockIdx.x % p.Hq), slot = static_cast<int>(blockIdx.x / p.Hq);
-  grid_launch_dependents();
-  int near = 0;
-  const Seq q = seq_of_slot<128>(p, slot, near);
-  if (q.tile < 0) return;
-  const int lane = threadIdx.x % 16, group = threadIdx.x / 16, kv = head / (p.Hq / p.Hk);
-  const bool in = 8 * lane < p.D;
+// s + <a, b>, even and odd entries apart.
+__device__ __forceinline__ uint64_t dot8(const uint4& a, const uint4& b, uint64_t s) {
+  const auto two = [](uint32_t w) { return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); };
+  s = fma_pair(two(a.x), two(b.x), s);
+  s = fma_pair(two(a.y), two(b.y), s);
+  s = fma_pair(two(a.z), two(b.z), s);
+  return fma_pair(two(a.w), two(b.w), s);
+}
+// 16 x 8 += 16 x 16 times 16 x 8 of a warp's registers.
+__device__ __forceinline__ void mma_16x8(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+// A warp: stats of a sequence's first 16 rows that see up to 16 keys, for one head.  Two
+// products of 16 x 16 (a lane a key of its own takes as long to load as the whole launch).
+__device__ __forceinline__ void few_keys(const AttArgs& p, float2* stats, int s, int head) {
+  const int lane = threadIdx.x & 31;
+  Seq q;
+  q.start = cu_at(p, s);
+  q.n = max(q.start, cu_at(p, s + 1)) - q.start;
+  q.prefix = p.prefix_end ? min(max(p.prefix_end[s] - q.start, 0), q.n) : 0;
+  if (q.n == 0 || keys_seen(p, q, 0) > kFewKeys) return;
+  const int kv = head / (p.Hq / p.Hk), r = lane / 4, last = q.n - 1;
+  const __nv_bfloat16 *q0 = row_of(p.q, q.start + min(r, last), head), *q1 = row_of(p.q, q.start + min(r + 8, last), head);
+  const __nv_bfloat16 *d0 = row_of(p.d_o, q.start + min(r, last), head), *d1 = row_of(p.d_o, q.start + min(r + 8, last), head);
+  const __nv_bfloat16 *k0 = row_of(p.k, q.start + min(r, last), kv), *k1 = row_of(p.k, q.start + min(r + 8, last), kv);
+  const __nv_bfloat16 *v0 = row_of(p.v, q.start + min(r, last), kv), *v1 = row_of(p.v, q.start + min(r + 8, last), kv);
+  float z[2][4] = {}, dp[2][4] = {};
+#pragma unroll 4
+  for (int c = 2 * (lane % 4); c < p.D; c += 16) {  // (D is a multiple of 8: only the second half may be behind it)
+    const bool both = c + 8 < p.D;
+    const auto low = [&](const __nv_bfloat16* x) { return *reinterpret_cast<const uint32_t*>(x + c); };
+    const auto high = [&](const __nv_bfloat16* x) { return both ? *reinterpret_cast<const uint32_t*>(x + c + 8) : 0u; };
+    const uint32_t aq[4] = {low(q0), low(q1), high(q0), high(q1)}, ad[4] = {low(d0), low(d1), high(d0), high(d1)};
+    const uint32_t bk[2][2] = {{low(k0), high(k0)}, {low(k1), high(k1)}}, bv[2][2] = {{low(v0), high(v0)}, {low(v1), high(v1)}};
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      mma_16x8(z[t], aq, bk[t]);
+      mma_16x8(dp[t], ad, bv[t]);
+    }
+  }
   const ScoreForm form(p);
   const float slope2 = p.slopes ? p.slopes[head] * kAttLog2e : 0.f;
-  const int row0 = q.tile * 128, rows = min(128, q.n - row0);
-  const float* lse = p.lse + static_cast<int64_t>(head) * p.T + q.start;
-  float2* out = stats + static_cast<int64_t>(head) * p.T + q.start;
-#pragma unroll 1
-  for (int r = group; __any_sync(0xffffffffu, r < rows); r += kAtOnce * kGroups) {
-    float a[kAtOnce][8], b[kAtOnce][8], l[kAtOnce];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = r + 8 * h, keys = i < q.n ? keys_seen(p, q, i) : 0;
+    const bool few = keys > 0 && keys <= kFewKeys;
+    const int64_t at = static_cast<int64_t>(head) * p.T + q.start + i;
+    const float lse2 = few ? p.lse[at] * kAttLog2e : 0.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int t = e / 2, x = e % 2, j = 8 * t + 2 * (lane % 4) + x;
+      const float w = fast_exp2(form.at(z[t][2 * h + x], slope2, fabsf(static_cast<float>(i - j))) - lse2);
+      if (few && j < keys) sum = fmaf(w, dp[t][2 * h + x], sum);
+    }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    if (few && lane % 4 == 0) stats[at] = make_float2(lse2, sum);
+  }
+}
+// The last sequence that begins at or before token t (a warp; the first where none does).
+__device__ __forceinline__ int seq_of_token(const AttArgs& p, int t) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = p.S;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, s = lo + step * lane;
+    const uint32_t before = __ballot_sync(0xffffffffu, s < hi && cu_at(p, s) <= t);
+    lo += step * (before ? 31 - __clz(before) : 0);
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+// stats: [Hq, T] of (lse in base 2, delta).  The first blocks: few_keys, a warp a sequence
+// and head.  The others: L = 8 or 16 lanes work on four tokens of a head, whose rows are on
+// their way while the sequence is looked up.
+template <int L>
+__global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttArgs p, float2* stats, int64_t few_blocks) {
+  constexpr int kGroups = kDeltaThreads / L, kAtOnce = 4;
+  grid_launch_dependents();
+  if (blockIdx.x < few_blocks) {
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kDeltaThreads / 32) + threadIdx.x / 32;
+    const int s = static_cast<int>(unit / p.Hq);
+    if (s < p.S) few_keys(p, stats, s, static_cast<int>(unit % p.Hq));
+    return;
+  }
+  const int lane = threadIdx.x % L;
+  const bool in = 8 * lane < p.D;
+  const int64_t units = (static_cast<int64_t>(p.T) + kAtOnce - 1) / kAtOnce * p.Hq;
+  const int64_t first = (blockIdx.x - few_blocks) * kGroups + threadIdx.x / 32 * (32 / L);  // the warp's
+  for (int64_t u0 = first; u0 < units; u0 += (gridDim.x - few_blocks) * kGroups) {
+    const int64_t unit = min(u0 + (threadIdx.x % 32) / L, units - 1);  // (the last one more than once, to the same bits)
+    const int quad = unit >> 32 ? static_cast<int>(unit / p.Hq) : static_cast<int>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(p.Hq));
+    const int head = static_cast<int>(unit - static_cast<int64_t>(quad) * p.Hq), t0 = quad * kAtOnce;
+    const int64_t at = static_cast<int64_t>(head) * p.T;
+    uint4 a[kAtOnce] = {}, b[kAtOnce] = {};
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      const int64_t t = q.start + row0 + min(r + k * kGroups, rows - 1);
-      eight(row_of(p.d_o, t, head) + 8 * lane, in, a[k]);
-      eight(row_of(p.o, t, head) + 8 * lane, in, b[k]);
-      l[k] = lse[t - q.start];
+      const int t = min(t0 + k, p.T - 1);
+      if (in) a[k] = reinterpret_cast<const uint4*>(row_of(p.d_o, t, head))[lane];
+      if (in) b[k] = reinterpret_cast<const uint4*>(row_of(p.o, t, head))[lane];
     }
+    // lane k of a group writes token k's
+    const int t = t0 + lane;
+    const bool mine = lane < kAtOnce && t < p.T;
+    const float lse2 = mine ? p.lse[at + t] * kAttLog2e : 0.f;
+    int s = seq_of_token(p, __shfl_sync(0xffffffffu, t0, 0));
+    while (mine && s + 1 < p.S && cu_at(p, s + 1) <= t) ++s;
+    Seq q;
+    q.start = cu_at(p, s);
+    q.n = max(q.start, cu_at(p, s + 1)) - q.start;
+    q.prefix = p.prefix_end ? min(max(p.prefix_end[s] - q.start, 0), q.n) : 0;
+    const int i = t - q.start;
+    const bool live = mine && i >= 0 && i < q.n && keys_seen(p, q, i) > kFewKeys;
+    __syncwarp();
+    float delta = 0.f;
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
-      if (!__any_sync(0xffffffffu, r + k * kGroups < rows)) break;
-      const int i = row0 + min(r + k * kGroups, rows - 1);
-      const float lse2 = l[k] * kAttLog2e;
-      float delta = dot16(a[k], b[k]);
-      const int keys = keys_seen(p, q, i);
-      const bool few = keys <= kFewKeys && r + k * kGroups < rows;
-      if (__any_sync(0xffffffffu, few)) {
-        const int64_t t = q.start + i;
-        const int most = few ? keys : 0;
-        float qr[8], sum = 0.f;
-        eight(row_of(p.q, t, head) + 8 * lane, in, qr);
-        for (int j0 = 0; __any_sync(0xffffffffu, j0 < most); j0 += kAtOnce) {
-          float key[kAtOnce][8], value[kAtOnce][8];
+      float x, y;
+      unpair(dot8(a[k], b[k], 0), x, y);
+      x += y;
 #pragma unroll
-          for (int e = 0; e < kAtOnce; ++e) {
-            const int64_t tj = q.start + min(j0 + e, keys - 1);
-            eight(row_of(p.k, tj, kv) + 8 * lane, in, key[e]);
-            eight(row_of(p.v, tj, kv) + 8 * lane, in, value[e]);
-          }
-#pragma unroll
-          for (int e = 0; e < kAtOnce; ++e) {
-            const float s = form.at(dot16(qr, key[e]), slope2, fabsf(static_cast<float>(i - min(j0 + e, keys - 1))));
-            const float dp = dot16(a[k], value[e]);
-            if (j0 + e < most) sum = fmaf(fast_exp2(s - lse2), dp, sum);
-          }
-        }
-        if (few) delta = sum;
-      }
-      if (r + k * kGroups < rows && lane == 0) out[i] = make_float2(lse2, delta);
+      for (int o = L / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+      if (lane == k) delta = x;
     }
+    if (live) stats[at + t] = make_float2(lse2, delta);
   }
 }
 
@@ -861,7 +913,10 @@ olive_status run_bwd(const Ctx& c, const AttArgs& a) {
   float2* stats = static_cast<float2*>(a.ws);
   const int64_t slots = att_slots(a.T, a.S, 128);
   const auto ask = [&](int64_t items) { return when_to_ask(items, c.num_sms, a.T, a.S); };
-  att_delta_kernel<<<static_cast<unsigned>(slots * a.Hq), kDeltaThreads, 0, c.stream>>>(a, stats);
+  constexpr int kLanes = kBoxes == 1 ? 8 : 16;
+  const int64_t few = ceil_div(static_cast<int64_t>(a.S) * a.Hq, kDeltaThreads / 32);
+  const int64_t rest = std::min<int64_t>(ceil_div(ceil_div(a.T, 4) * a.Hq, kDeltaThreads / kLanes), 1 << 30);
+  att_delta_kernel<kLanes><<<static_cast<unsigned>(few + rest), kDeltaThreads, 0, c.stream>>>(a, stats, few);
   const int parts = head_parts(a.T, a.Hq, a.Hk);
   float* sums = reinterpret_cast<float*>(static_cast<char*>(a.ws) + stats_bytes(a.T, a.Hq));
   launch_after(c, dkdv, slots * a.Hk * parts, kThreads, kSmemKv, mq, mk, mv, mdo, a, stats, sums, parts, ask(slots * a.Hk * parts));
