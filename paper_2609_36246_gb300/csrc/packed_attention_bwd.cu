@@ -11,10 +11,11 @@
 // added up in memory, results are the same bits from call to call, and no fp32 copy of
 // dq exists.
 //
-// 8 sequences of 4096, 32 + 8 heads of 128, causal: 107, 1230 and 1110 us; the seven products
+// 8 sequences of 4096, 32 + 8 heads of 128, causal: 88, 1235 and 1110 us; the seven products
 // run at 1.57 PFLOP/s (tensor pipe active 74 and 62 % of a shorter launch's cycles), near what
-// the power cap leaves.  200 sequences of some 41 tokens, 16 + 16 heads of 64: 29, 91 and 48
-// us, an item's chain of waits.
+// the power cap leaves.  200 sequences of some 41 tokens, 16 + 16 heads of 64: 9, 91 and 48
+// us, an item's chain of waits.  Each launch starts under the one ahead (225 us forward and
+// backward at that step, 236 without).
 #include <algorithm>
 #include <type_traits>
 
@@ -35,7 +36,8 @@ static_assert(4 * kRegsRows + kRegsRest <= 5 * kRegsLaunch, "the block's registe
 // ------------------------------------------------------------------ delta ---
 // Rows that see up to this many keys have their delta from the keys themselves: <do, o>
 // carries o's rounding, which is large beside dp - delta where one key has all the weight.
-// They are among the first so many of a sequence.
+// They are among the first so many of a sequence.  (Up to 128 keys: the error of short
+// sequences' dq and dk 2.6e-3 -> 2.4e-3 of their norm, this launch 9 -> 49 us.)
 constexpr int kFewKeys = 16;
 constexpr int kDeltaThreads = 128;
 
@@ -56,8 +58,9 @@ __device__ __forceinline__ void mma_16x8(float (&d)[4], const uint32_t (&a)[4], 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// A warp: stats of a sequence's first 16 rows that see up to 16 keys, for one head.  Two
-// products of 16 x 16 (a lane a key of its own takes as long to load as the whole launch).
+// A warp: stats of a sequence's first 16 rows that see up to 16 keys, for one head: two
+// products of 16 x 16, too small for tensor memory.  (By dot products of 16 lanes the 200
+// sequences' launch took 29 us, of which 18 for these.)
 __device__ __forceinline__ void few_keys(const AttArgs& p, float2* stats, int s, int head) {
   const int lane = threadIdx.x & 31;
   Seq q;
@@ -118,7 +121,8 @@ __device__ __forceinline__ int seq_of_token(const AttArgs& p, int t) {
 }
 // stats: [Hq, T] of (lse in base 2, delta).  The first blocks: few_keys, a warp a sequence
 // and head.  The others: L = 8 or 16 lanes work on four tokens of a head, whose rows are on
-// their way while the sequence is looked up.
+// their way while the sequence is looked up.  Bound by memory: 32768 tokens of 32 heads of
+// 128, 537 MB, 88 us (6.1 TB/s; 107 by tiles of 128 rows of a head).
 template <int L>
 __global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttArgs p, float2* stats, int64_t few_blocks) {
   constexpr int kGroups = kDeltaThreads / L, kAtOnce = 4;

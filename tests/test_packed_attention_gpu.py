@@ -354,6 +354,36 @@ def test_offsets_that_do_not_describe_the_batch(cu):
     assert B.status_bits(st) == ["OLIVE_ERR_OFFSETS"]
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_sequences_without_tokens(causal):
+    """All of them: every row is behind the last one, whatever it holds."""
+    s = _case([0, 0, 0], 3, 1, 64, pad=300, causal=causal)
+    for n in ("q", "k", "v", "do"):
+        s[n].fill_(float("nan"))
+    o, lse = _forward(s)
+    assert not o.any() and bool((lse == -math.inf).all())
+    assert not any(g.any() for g in _backward(s, o, lse))
+
+
+@pytest.mark.parametrize("n", [15, 16, 17, 18, 33])
+@pytest.mark.parametrize("form", [dict(), dict(prefix=16), dict(prefix=17), dict(causal=False), dict(cap=4.0, bias=True)], ids=str)
+@pytest.mark.parametrize("D", [8, 24, 128])
+def test_rows_of_few_keys(n, form, D):
+    """Around the number of keys up to which a row's delta comes from the keys."""
+    _check(_case([n, 1, n - 1, 2], 6, 2, D, sharp=2.0, pad=3, **form))
+
+
+def test_outputs_beside_others():
+    """Gradients written into views of one array leave what lies between them."""
+    s = _case([100, 60], 4, 2, 64, pad=7)
+    o, lse = _forward(s)
+    want = _backward(s, o, lse)
+    wide = torch.full((167, 4 + 2 + 2 + 3, 64), 7.0, dtype=BF16, device="cuda")
+    got = _backward(s, o, lse, out=(wide[:, :4], wide[:, 5:7], wide[:, 8:10]))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert bool((wide[:, [4, 7, 10]] == 7).all())
+
+
 def test_no_tokens():
     s = _case([1], 2, 1, 64)
     o, lse = B.olive_packed_attention_fwd(s["q"][:0], s["k"][:0], s["v"][:0], torch.zeros(2, dtype=torch.int32, device="cuda"))
