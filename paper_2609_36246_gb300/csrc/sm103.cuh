@@ -220,13 +220,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
       : "memory");
 }
-// Untiled bulk copy global -> shared (both addresses 16-byte aligned, size a multiple of
-// 16), completion counted in bytes on the mbarrier.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
-               : "memory");
-}
 
 // Untiled bulk copy shared -> global (both addresses 16-byte aligned, size a
 // multiple of 16), part of this thread's current bulk group.
@@ -294,17 +287,6 @@ __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t adesc, uint6
       : "memory");
 }
 
-// The same with A in tensor memory: lane = row, a 32-bit column = two values along K.
-__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
-                                             uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-
 // The same for a converged warp, of which the lane with `leader` issues: predicated, not
 // branched to, so that nothing diverges between one MMA and the next.
 __device__ __forceinline__ void umma_bf16_by(bool leader, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
@@ -317,6 +299,7 @@ __device__ __forceinline__ void umma_bf16_by(bool leader, uint32_t d_tmem, uint6
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(static_cast<uint32_t>(leader))
       : "memory");
 }
+// A in tensor memory: lane = row, a 32-bit column = two values along K.
 __device__ __forceinline__ void umma_bf16_ta_by(bool leader, uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
                                                 uint32_t idesc, uint32_t accumulate) {
   asm volatile(
