@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(ts + 32 * c, s[c]);
           tmem_ld_wait();
-          if constexpr (kForm == FORM_CAP)
+          if constexpr (is_capped(kForm))
             at_once = all_small(form, pos < it.q.n ? fmaxf(fmaxf(largest(s[0]), largest(s[1])), fmaxf(largest(s[2]), largest(s[3]))) : 0.f);
         }
         if (at_once) {
@@ -480,7 +480,16 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_ld_wait();
             const int seen = here - 32 * c;
             uint64_t none[1];
-            if constexpr (kForm != FORM_PLAIN) form_scores<kForm, false, false>(form, s, slope2, far - 32 * c, none);
+            bool small = false;
+            if constexpr (kForm == FORM_WIDE) {
+              float top = 0.f;
+#pragma unroll
+              for (int e = 0; e < 32; ++e) top = fmaxf(top, e < seen ? fabsf(__uint_as_float(s[e])) : 0.f);
+              small = all_small(form, pos < it.q.n ? top : 0.f);
+              if (small) form_scores<kForm, false, true>(form, s, slope2, far - 32 * c, none);
+            }
+            if constexpr (kForm != FORM_PLAIN)
+              if (!small) form_scores<kForm, false, false>(form, s, slope2, far - 32 * c, none);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               const float x = e < seen ? __uint_as_float(s[e]) : -INFINITY;
@@ -573,7 +582,7 @@ olive_status run_fwd(const Ctx& c, const AttArgs& a) {
 
 template <int kBoxes, int kPair>
 olive_status by_form(const Ctx& c, const AttArgs& a) {
-  if (a.cap > 0.f) return run_fwd<kBoxes, kPair, FORM_CAP>(c, a);
+  if (a.cap > 0.f) return a.cap > kWideCap ? run_fwd<kBoxes, kPair, FORM_WIDE>(c, a) : run_fwd<kBoxes, kPair, FORM_CAP>(c, a);
   return a.slopes ? run_fwd<kBoxes, kPair, FORM_BIAS>(c, a) : run_fwd<kBoxes, kPair, FORM_PLAIN>(c, a);
 }
 

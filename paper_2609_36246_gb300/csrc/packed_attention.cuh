@@ -191,16 +191,18 @@ inline int when_to_ask(int64_t items, int sms, int64_t T, int64_t S) {
 }
 
 // tanh(x) = 1 - 2 / (1 + e^2x), x in units of ln 2 / 2: off by some 2^-23, which is
-// times the cap in a score.
+// times the cap in a score: up to kWideCap no more than a product's own fp32 sum.
+constexpr float kWideCap = 64.f;
 __device__ __forceinline__ float tanh_of(float x2) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + fast_exp2(x2)));
   return fmaf(-2.f, r, 1.f);
 }
-// Two at once for |x| <= 0.7: x times a polynomial in x^2, fitted to tanh(x) / x at
+// Two at once for |x| <= kSmallTanh: x times a polynomial in x^2, fitted to tanh(x) / x at
 // Chebyshev nodes of [0, 0.5] (off by 2^-25 of it at most, before rounding).  A score as
 // most are takes half the time: the exact form's three special functions an element, four
 // cycles each, are what bounds a capped tile.
+constexpr float kSmallTanh = 0.7f;
 __device__ __forceinline__ uint64_t small_tanh_pair(uint64_t x) {
   const uint64_t y = mul_pair(x, x);
   const auto k = [](float v) { return pair(v, v); };
@@ -210,16 +212,47 @@ __device__ __forceinline__ uint64_t small_tanh_pair(uint64_t x) {
   r = fma_pair(y, r, k(-0.3333311676979065f));
   return mul_pair(x, fma_pair(y, r, k(1.f)));
 }
+// Two for wide caps, each by its own size: off by a part of itself, however small it is.
+// (Both forms are computed and one is selected: as a condition it became a branch an
+// element, a tenth slower where most scores are near the cap.  With the exact form for
+// small ones too a cap of 1e6 was off by 0.09 in the tiles that it took, one of 1e9 by the
+// score.)
+__device__ __forceinline__ float select_above(float size, float than, float yes, float no) {
+  float r;
+  asm("{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %1, %2;\n\tselp.f32 %0, %3, %4, p;\n\t}" : "=f"(r) : "f"(size), "f"(than), "f"(yes), "f"(no));
+  return r;
+}
+__device__ __forceinline__ uint64_t wide_tanh_pair(uint64_t x) {
+  float a, b, s, t;
+  unpair(x, a, b);
+  unpair(small_tanh_pair(x), s, t);
+  return pair(select_above(fabsf(a), kSmallTanh, tanh_of(a * (2.f * kAttLog2e)), s),
+              select_above(fabsf(b), kSmallTanh, tanh_of(b * (2.f * kAttLog2e)), t));
+}
 // How scores are formed from products: as they are, lowered with the distance, or
-// capped (and lowered, by a slope that may be 0).  In base 2.
-enum { FORM_PLAIN = 0, FORM_BIAS = 1, FORM_CAP = 2 };
+// capped (and lowered, by a slope that may be 0), by a cap up to kWideCap or a wider one.
+// In base 2.  (The wide caps' form in place of the other, forward, us.  A cap of 1, 8
+// sequences of 4096, 32 + 8 heads of 128: 3235 and 1812.  All scores small: these 1392 and
+// 1338; 200 sequences of 41, 16 + 16 heads of 64: 63 and 55.)
+enum { FORM_PLAIN = 0, FORM_BIAS = 1, FORM_CAP = 2, FORM_WIDE = 3 };
+constexpr bool is_capped(int form) { return form == FORM_CAP || form == FORM_WIDE; }
 struct ScoreForm {
   float scale2, in_cap, cap2;
+  // (a cap above 1e30 bends no score that one of 1e30 does not, but its reciprocal loses
+  // bits; that of one near 0 must not be infinite, as 0 times it is a NaN)
   __device__ __forceinline__ explicit ScoreForm(const AttArgs& p)
-      : scale2(p.scale * kAttLog2e), in_cap(p.cap > 0.f ? p.scale / p.cap : 0.f), cap2(p.cap * kAttLog2e) {}
+      : scale2(p.scale * kAttLog2e), in_cap(p.cap > 0.f ? fminf(p.scale / fminf(p.cap, 1e30f), 1e37f) : 0.f),
+        cap2(fminf(p.cap, 1e30f) * kAttLog2e) {}
   // One score of a product at a distance.
   __device__ __forceinline__ float at(float s, float slope2, float dist) const {
-    const float x = in_cap > 0.f ? cap2 * tanh_of(s * (2.f * kAttLog2e * in_cap)) : s * scale2;
+    float x = s * scale2;
+    if (cap2 > kWideCap * kAttLog2e) {
+      float t, same;
+      unpair(wide_tanh_pair(pair(s * in_cap, s * in_cap)), t, same);
+      x = cap2 * t;
+    } else if (cap2 > 0.f) {
+      x = cap2 * tanh_of(s * (2.f * kAttLog2e * in_cap));
+    }
     return fmaf(-slope2, dist, x);
   }
 };
@@ -231,24 +264,26 @@ __device__ __forceinline__ float largest(const uint32_t (&s)[32]) {
 }
 // Whether a warp's products, none larger than `top`, take the small form.  Asked of whole
 // tiles and of a sequence's own rows alone: what lies behind it must not decide in which
-// form, so with which rounding, its scores are formed.
-__device__ __forceinline__ bool all_small(const ScoreForm& f, float top) { return __all_sync(0xffffffffu, top * f.in_cap <= 0.7f); }
+// form, so with which rounding, its scores are formed.  (With a wide cap a score's form is
+// its own, and this only a shorter way to the same bits.)
+__device__ __forceinline__ bool all_small(const ScoreForm& f, float top) { return __all_sync(0xffffffffu, top * f.in_cap <= kSmallTanh); }
 // Whether each of a warp's rows has `cols` columns on one side of its own, before it or
 // behind: then the distance is linear in the column, one instruction a score in place of
 // two and half of one.
 __device__ __forceinline__ bool one_side(float far, int cols) {
   return __all_sync(0xffffffffu, far <= 0.f || far >= static_cast<float>(cols - 1));
 }
-// 32 products to scores, column e at the distance |far - e| (kEven: all on one side); with
-// kBend the derivatives of the cap, in pairs.
+// 32 products to scores, column e at the distance |far - e| (kEven: all on one side, or all
+// capped ones small); with kBend the derivatives of the cap, in pairs.
 template <int kForm, bool kBend, bool kEven>
 __device__ __forceinline__ void form_scores(const ScoreForm& f, uint32_t (&s)[32], float slope2, float far, uint64_t (&bend)[kBend ? 16 : 1]) {
-  if constexpr (kForm == FORM_CAP) {
-    if constexpr (kEven) {
+  if constexpr (is_capped(kForm)) {
+    if constexpr (kEven || kForm == FORM_WIDE) {
       const uint64_t in = pair(f.in_cap, f.in_cap), out = pair(f.cap2, f.cap2), one = pair(1.f, 1.f), minus = pair(-1.f, -1.f);
 #pragma unroll
       for (int e = 0; e < 32; e += 2) {
-        const uint64_t t = small_tanh_pair(mul_pair(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), in));
+        const uint64_t x2 = mul_pair(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), in);
+        const uint64_t t = kEven ? small_tanh_pair(x2) : wide_tanh_pair(x2);
         if constexpr (kBend) bend[e / 2] = fma_pair(mul_pair(t, minus), t, one);
         float x, y;
         unpair(mul_pair(t, out), x, y);

@@ -494,15 +494,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool some = it.k0 + (warp & 3) * 32 < it.q.n && hi > 0;
         uint64_t pr[kCols / 2];  // pairs of columns: p, times the cap's derivative
         uint32_t a[32];
-        [[maybe_unused]] uint64_t bend[kForm == FORM_CAP ? 16 : 1];
+        [[maybe_unused]] uint64_t bend[is_capped(kForm) ? 16 : 1];
         if (some) {
           tmem_ld_32x32b_x32(ts, a);
           tmem_ld_wait();
           if constexpr (kForm != FORM_PLAIN) {
-            if (!masked && (kForm == FORM_CAP ? all_small(form, largest(a)) : one_side(far, kCols)))
-              form_scores<kForm, kForm == FORM_CAP, true>(form, a, slope2, far, bend);
+            bool even = !masked || kForm == FORM_WIDE;
+            if (even) even = is_capped(kForm) ? all_small(form, key < it.q.n ? largest(a) : 0.f) : one_side(far, kCols);
+            if (even)
+              form_scores<kForm, is_capped(kForm), true>(form, a, slope2, far, bend);
             else
-              form_scores<kForm, kForm == FORM_CAP, false>(form, a, slope2, far, bend);
+              form_scores<kForm, is_capped(kForm), false>(form, a, slope2, far, bend);
           }
         }
         // (two copies of the loops: as one, the masks' instructions are issued for every tile)
@@ -525,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               y = k + 1 >= lo && k + 1 < hi ? y : 0.f;
             }
             pr[c] = pair(x, y);
-            if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], bend[c]);
+            if constexpr (is_capped(kForm)) pr[c] = mul_pair(pr[c], bend[c]);
             w[c] = pack_bf16x2(x, y);
           }
           tmem_st_32x32b_x16(ts, w);
@@ -806,12 +808,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(C_SEMPTY));
-          [[maybe_unused]] uint64_t bend[kForm == FORM_CAP ? 16 : 1];
+          [[maybe_unused]] uint64_t bend[is_capped(kForm) ? 16 : 1];
           if constexpr (kForm != FORM_PLAIN) {
-            if (!masked && (kForm == FORM_CAP ? all_small(form, pos < it.q.n ? largest(a) : 0.f) : one_side(far, kCols)))
-              form_scores<kForm, kForm == FORM_CAP, true>(form, a, slope2, far, bend);
+            bool even = !masked || kForm == FORM_WIDE;
+            if (even) even = is_capped(kForm) ? all_small(form, pos < it.q.n ? largest(a) : 0.f) : one_side(far, kCols);
+            if (even)
+              form_scores<kForm, is_capped(kForm), true>(form, a, slope2, far, bend);
             else
-              form_scores<kForm, kForm == FORM_CAP, false>(form, a, slope2, far, bend);
+              form_scores<kForm, is_capped(kForm), false>(form, a, slope2, far, bend);
           }
 #pragma unroll
           for (int c = 0; c < kCols / 2; ++c) {
@@ -819,7 +823,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             float x, y;
             unpair(kForm != FORM_PLAIN ? add_pair(s2, l) : fma_pair(s2, pair(form.scale2, form.scale2), l), x, y);
             pr[c] = pair(fast_exp2(x), fast_exp2(y));
-            if constexpr (kForm == FORM_CAP) pr[c] = mul_pair(pr[c], bend[c]);  // (p itself is not needed here)
+            if constexpr (is_capped(kForm)) pr[c] = mul_pair(pr[c], bend[c]);  // (p itself is not needed here)
           }
         }
         if (!(ok = mbar_wait_warp(bar(C_DPFULL + (n_kv & 1)), n_kv >> 1 & 1, ctl))) break;
@@ -934,7 +938,7 @@ olive_status run_bwd(const Ctx& c, const AttArgs& a) {
 
 template <int kBoxes>
 olive_status by_form(const Ctx& c, const AttArgs& a) {
-  if (a.cap > 0.f) return run_bwd<kBoxes, FORM_CAP>(c, a);
+  if (a.cap > 0.f) return a.cap > kWideCap ? run_bwd<kBoxes, FORM_WIDE>(c, a) : run_bwd<kBoxes, FORM_CAP>(c, a);
   return a.slopes ? run_bwd<kBoxes, FORM_BIAS>(c, a) : run_bwd<kBoxes, FORM_PLAIN>(c, a);
 }
 
