@@ -766,7 +766,8 @@ OLIVE_API olive_status olive_row_norm_bwd(const void* dy, const void* h, const v
  * sequence.  Token cu_seqlens[s] + i is row i of sequence s (n_s rows); query head h
  * goes with key head h / (Hq / Hk).  Row i sees key j < n_s where not `causal` or
  * j <= i or j < prefix_end[s] - cu_seqlens[s] (int32 [S], e.g. olive_splice_pack's
- * cut_offsets: prompt and prefix are then seen by all rows; NULL: no such keys):
+ * cut_offsets: prompt and prefix are then seen by all rows; an end before the sequence
+ * counts as its beginning, one behind it as its end; NULL: no such keys):
  *   s_ij = z_ij, or cap tanh(z_ij / cap) if cap > 0,  with z_ij = scale <q_i, k_j>
  *          - slopes[h] |i - j|                 (slopes fp32 [Hq], NULL: none)
  *   lse_i = log sum over seen j of exp(s_ij)                      fp32 [Hq, T]

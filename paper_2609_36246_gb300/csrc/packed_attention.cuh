@@ -26,6 +26,11 @@ __device__ __forceinline__ int cu_at(const AttArgs& p, int s) { return min(max(p
 struct Seq {
   int start, n, prefix, tile;  // first token, tokens, those seen by all, tile in it
 };
+// Keys of a sequence that all its rows see: none where the end given is before it, all where
+// it is behind.  (Compared before it is subtracted from: an end near -2^31 must not wrap.)
+__device__ __forceinline__ int prefix_of(const AttArgs& p, int s, const Seq& q) {
+  return p.prefix_end ? min(max(p.prefix_end[s], q.start) - q.start, q.n) : 0;
+}
 // `near`: a sequence at or before it, looked from first (items come in rising order), so
 // that one load, of 32 sequences' offsets, does for most.
 template <int R>
@@ -58,7 +63,7 @@ __device__ __forceinline__ Seq seq_of_slot(const AttArgs& p, int slot, int& near
   q.start = __shfl_sync(0xffffffffu, cu, last);
   const int end = max(q.start, __shfl_sync(0xffffffffu, cu, last + 1));
   q.n = end - q.start;
-  q.prefix = p.prefix_end ? min(max(p.prefix_end[near] - q.start, 0), q.n) : 0;
+  q.prefix = prefix_of(p, near, q);
   q.tile = slot - (q.start / R + near);
   if (q.tile < 0 || static_cast<int64_t>(q.tile) * R >= q.n) q.tile = -1;
   return q;

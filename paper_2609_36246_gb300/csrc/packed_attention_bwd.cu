@@ -66,7 +66,7 @@ __device__ __forceinline__ void few_keys(const AttArgs& p, float2* stats, int s,
   Seq q;
   q.start = cu_at(p, s);
   q.n = max(q.start, cu_at(p, s + 1)) - q.start;
-  q.prefix = p.prefix_end ? min(max(p.prefix_end[s] - q.start, 0), q.n) : 0;
+  q.prefix = prefix_of(p, s, q);
   if (q.n == 0 || keys_seen(p, q, 0) > kFewKeys) return;
   const int kv = head / (p.Hq / p.Hk), r = lane / 4, last = q.n - 1;
   const __nv_bfloat16 *q0 = row_of(p.q, q.start + min(r, last), head), *q1 = row_of(p.q, q.start + min(r + 8, last), head);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttAr
     Seq q;
     q.start = cu_at(p, s);
     q.n = max(q.start, cu_at(p, s + 1)) - q.start;
-    q.prefix = p.prefix_end ? min(max(p.prefix_end[s] - q.start, 0), q.n) : 0;
+    q.prefix = prefix_of(p, s, q);
     const int i = t - q.start;
     const bool live = mine && i >= 0 && i < q.n && keys_seen(p, q, i) > kFewKeys;
     __syncwarp();
