@@ -56,6 +56,7 @@ struct Item {
   Seq q;
   int kv_head[2], head[2], row0[2], tiles[2], seen[2];  // seen: keys that the slot's last row sees
   int end;
+  __device__ __forceinline__ int length() const { return max(tiles[0], tiles[1]); }
 };
 constexpr int kMisc = 16 + static_cast<int>(sizeof(ItemRing<Item>));
 constexpr int smem_bytes(int boxes) {
@@ -368,7 +369,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (uint32_t n = 0; ok && next_item<false>(ring, ring_at, n, it, ctl, ok);) {
       const int tiles = a ? it.tiles[1] : it.tiles[0];
-      if (tiles == 0) continue;
+      if (tiles == 0) {  // (the other slot's rows are worked on: all of them, before the next item is out)
+        ok = mbar_wait_warp(ring_at.full(n), n / kItems & 1, for_steps(ctl, it.length()));
+        continue;
+      }
       const int head = a ? it.head[1] : it.head[0];
       const int pos = (a ? it.row0[1] : it.row0[0]) + row;
       const int lim = keys_seen(p, it.q, min(pos, it.q.n - 1));

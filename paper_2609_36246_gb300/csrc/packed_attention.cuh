@@ -128,6 +128,10 @@ __device__ __forceinline__ void init_ring(const RingAt& r, int readers) {
     mbar_init(r.empty(i), readers);
   }
 }
+// A wait's limit is that of a tile, a microsecond or two of work: who waits for an item of
+// `steps` tiles as a whole has as many.  (Where the work itself is stuck, those who do it
+// give up after one, and everybody sees their flag.)
+__device__ __forceinline__ WaitCtl for_steps(const WaitCtl& ctl, int steps) { return {ctl.abort, ctl.limit_ns * (1 + static_cast<uint64_t>(steps))}; }
 // The warp that hands out items.  find(i, item) says whether item i exists; rest(i) is
 // what else is done for every i, after the item is out.
 template <class Item, class Find, class Rest>
@@ -135,6 +139,7 @@ __device__ __forceinline__ void hand_out(ItemRing<Item>& ring, const RingAt& at,
   const int lane = threadIdx.x & 31;
   const uint32_t answer = smem_u32(ring.answer);
   uint32_t n = 0, asked = 0;
+  int most = 0;  // steps of an item so far
   bool ok = true, pending = false;
   const auto put_question = [&] {
     if (lane == 0) {
@@ -152,7 +157,8 @@ __device__ __forceinline__ void hand_out(ItemRing<Item>& ring, const RingAt& at,
     Item it;
     const bool there = find(i, it);
     if (there) {
-      if (!(ok = mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, ctl))) break;
+      if (!(ok = mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, for_steps(ctl, most)))) break;
+      most = max(most, it.length());
       if (lane == 0) ring.item[n % kItems] = it;
       __syncwarp();
       if (lane == 0) mbar_arrive(at.full(n));
@@ -161,7 +167,7 @@ __device__ __forceinline__ void hand_out(ItemRing<Item>& ring, const RingAt& at,
     rest(i);
     if (ask == ASK_NEVER) break;
     if (ask == ASK_LATE) {
-      if (there && !(ok = mbar_wait_warp(at.issued(), (n - 1) & 1, ctl))) break;
+      if (there && !(ok = mbar_wait_warp(at.issued(), (n - 1) & 1, for_steps(ctl, most)))) break;
       put_question();
     }
     if (!(ok = mbar_wait_warp(at.taken(), asked++ & 1, ctl))) break;
@@ -169,7 +175,7 @@ __device__ __forceinline__ void hand_out(ItemRing<Item>& ring, const RingAt& at,
     i = warp_uniform(taken_block(answer));
   }
   if (pending) let_copies_land();
-  if (ok && mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, ctl) && lane == 0) {
+  if (ok && mbar_wait_warp(at.empty(n), (n / kItems & 1) ^ 1, for_steps(ctl, most)) && lane == 0) {
     ring.item[n % kItems].end = 1;
     mbar_arrive(at.full(n));
   }

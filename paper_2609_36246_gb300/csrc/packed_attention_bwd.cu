@@ -254,6 +254,7 @@ struct KvItem {
   int kv_head, part, heads;        // which part of the key head's query heads, how many
   int k0, first, tiles, steps;     // first query tile, query tiles of a head, of all heads
   int end;
+  __device__ __forceinline__ int length() const { return steps; }
 };
 constexpr int kKvBars = (8 * A_COUNT + 15) / 16 * 16, kKvMisc = 16 + static_cast<int>(sizeof(ItemRing<KvItem>));
 constexpr int kv_smem(int boxes) { return (2 * own_stages(boxes) + kQ + kO) * boxes * kBoxBytes + kO * 1024 + kKvBars + kKvMisc; }
@@ -616,6 +617,7 @@ struct QItem {
   Seq q;
   int head, q0, seen, tiles;
   int end;
+  __device__ __forceinline__ int length() const { return tiles; }
 };
 constexpr int kQBars = (8 * C_COUNT + 15) / 16 * 16, kQMisc = 16 + static_cast<int>(sizeof(ItemRing<QItem>));
 constexpr int dq_smem(int boxes) { return 1024 + (2 * own_stages(boxes) + kK + kV) * boxes * kBoxBytes + kQBars + kQMisc; }

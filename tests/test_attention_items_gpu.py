@@ -3,6 +3,8 @@ than SMs, of long sequences (a block asks when its last copies are issued) and o
 ahead), heads wider than 64 and narrower, two heads, two tiles and heads apart in a block, dk and dv in
 one part and in several.  Tolerances as for the other lengths."""
 
+import os
+
 import pytest
 import torch
 
@@ -31,6 +33,36 @@ def test_short_sequences(form, hq, hk, D):
 def test_parts_of_the_query_heads(lens, hq, hk):
     """Numbers of key tiles, from the fewest on, that give dk and dv different parts of the heads."""
     base._check(base._case(lens, hq, hk, 32, prefix=100))
+
+
+def _as(limit_ms, run):
+    old = os.environ.get("OLIVE_WAIT_LIMIT_MS")
+    os.environ["OLIVE_WAIT_LIMIT_MS"] = str(limit_ms)
+    try:
+        out = run()
+        torch.cuda.synchronize()
+        return out
+    finally:
+        del os.environ["OLIVE_WAIT_LIMIT_MS"]
+        if old is not None:
+            os.environ["OLIVE_WAIT_LIMIT_MS"] = old
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_an_item_longer_than_the_limit_of_a_wait(causal):
+    """The limit is that of a wait for the next tile, not of an item: a row's 260000 keys take some
+    milliseconds, and no wait among them one.  (The last item has one tile of rows, so half of its block
+    waits for the other half.)"""
+    n = 262144 - 200
+    s = base._case([n], 1, 1, 64, causal=causal)
+
+    def run():
+        o, lse = base._forward(s)
+        return (o, lse, *base._backward(s, o, lse))
+
+    want = _as(1000, run)
+    got = _as(1, run)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_prefix_ends_outside_the_sequence():
