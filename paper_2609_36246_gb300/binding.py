@@ -16,6 +16,7 @@ import os
 import re
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -1262,10 +1263,20 @@ class GatedMLP(torch.autograd.Function):
                                    need_dW=ctx.need_dW, dev_status=ctx.dev_status)
 
 
+def _values_only(*tensors):
+    """Whether a call is one for its values: autograd is off, and no tensor has a tangent
+    (forward mode works where autograd is off; the Functions have none and say so)."""
+    if torch.is_grad_enabled():
+        return False
+    # (asked of the tensors only where there is a level for tangents: 0.5 us each)
+    return getattr(forward_ad, "_current_level", 0) < 0 or all(
+        t is None or forward_ad.unpack_dual(t).tangent is None for t in tensors)
+
+
 def gated_mlp(x, W_gate, W_up, W_down, residual=None, act="silu", dev_status=None):
     # (asked here: inside a Function autograd is off anyway, and a Parameter "needs" its
     # gradient under no_grad too; what is saved is 4 T f bytes)
-    if not torch.is_grad_enabled():
+    if _values_only(x, W_gate, W_up, W_down, residual):
         return olive_gated_mlp_fwd(x, W_gate, W_up, W_down, residual, act, dev_status=dev_status)[0]
     return GatedMLP.apply(x, W_gate, W_up, W_down, residual, act, dev_status)
 
@@ -1326,7 +1337,7 @@ class RowNorm(torch.autograd.Function):
 
 def row_norm(x, w, b=None, residual=None, eps=1e-6, kind="rms"):
     # (nothing is kept for a backward where autograd is off)
-    if not torch.is_grad_enabled():
+    if _values_only(x, w, b, residual):
         y, h, _ = olive_row_norm_fwd(x, w, b, residual, eps, kind)
         return y if residual is None else (y, h)
     return RowNorm.apply(x, w, b, residual, eps, kind)
