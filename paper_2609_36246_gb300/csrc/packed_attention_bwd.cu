@@ -251,7 +251,7 @@ enum { A_KVFULL = 0, A_KVEMPTY = 2, A_QFULL = 4, A_QEMPTY = A_QFULL + kQ, A_QFIX
 
 struct KvItem {
   Seq q;
-  int kv_head, part, heads;        // which part of the key head's query heads, how many
+  int kv_head, part, head;         // which part of the key head's query heads, the first of them
   int k0, first, tiles, steps;     // first query tile, query tiles of a head, of all heads
   int end;
   __device__ __forceinline__ int length() const { return steps; }
@@ -265,18 +265,18 @@ __device__ __forceinline__ bool kv_item(const AttArgs& p, int i, int parts, KvIt
   it.end = 0;
   it.kv_head = u / parts;
   it.part = u % parts;
-  it.heads = p.Hq / p.Hk / parts;
+  const int per = p.Hq / p.Hk, each = (per + parts - 1) / parts;  // (the last part may be smaller)
+  it.head = it.kv_head * per + it.part * each;
   it.k0 = 128 * it.q.tile;
   it.first = p.causal && it.k0 >= it.q.prefix ? it.q.tile : 0;
   it.tiles = (it.q.n + 127) / 128 - it.first;
-  it.steps = it.tiles * it.heads;
+  it.steps = it.tiles * min(each, per - it.part * each);
   return true;
 }
 // An item's steps: a query head and the first row of a query tile.
 struct KvStep {
   int head, q0, left;
-  __device__ __forceinline__ KvStep(const AttArgs& p, const KvItem& it)
-      : head(it.kv_head * (p.Hq / p.Hk) + it.part * it.heads), q0(128 * it.first), left(it.tiles) {}
+  __device__ __forceinline__ explicit KvStep(const KvItem& it) : head(it.head), q0(128 * it.first), left(it.tiles) {}
   __device__ __forceinline__ void next(const KvItem& it) {
     q0 += 128;
     if (--left == 0) {
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           load_tile(sk + kTileBytes, &map_v, full, kBoxes, p.v.head_stride ? it.kv_head : 0, it.q.start + it.k0);
         }
         kv.next(kOwn);
-        KvStep at(p, it);
+        KvStep at(it);
         for (int t = 0; t < it.steps; ++t, at.next(it), q.next(kQ), o.next(kO)) {
           float2 got[4];  // the rows' lse and delta, on their way while the stages are waited for
 #pragma unroll
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       Turn kv, q, o;  // of the step whose second products are next
       bool ok = true;
       for (uint32_t ni = 0; ok && next_item<true>(ring, ring_at, ni, it, ctl, ok); ++n_o, kv.next(kOwn)) {
-        KvStep at(p, it);
+        KvStep at(it);
         int rows = min(128, it.q.n - at.q0);  // (a tile of a sequence's last rows is shorter)
         const uint32_t sk = skv + 2 * kv.i * kTileBytes, sv = sk + kTileBytes;
         const auto scores = [&](const Turn& qs) {
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (uint32_t ni = 0; ok && next_item<false>(ring, ring_at, ni, it, ctl, ok);) {
       const int key = it.k0 + (warp & 3) * 32 + lane;
       const bool alone = first_row_alone(p, it.q);
-      KvStep step(p, it);
+      KvStep step(it);
       for (int t = 0; t < it.steps; ++t, ++n_q, step.next(it), o.next(kO)) {
         // columns [lo, hi) of this part see the key
         const int at = step.q0 + kCols * part;
@@ -880,13 +880,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 size_t stats_bytes(int64_t T, int64_t Hq) { return align_up(8ull * T * Hq, kWsAlign); }
-// Parts that the query heads of a key head are cut into for dk and dv: all of them where
-// the key tiles do not fill the SMs (152), as the first tiles of a causal sequence take
-// longest.  (5003 tokens of 15 + 3 heads: 215 us in one part, 112 in five with their join.
-// Below four tiles a launch more costs what it saves.)
+// Parts that the query heads of a key head are cut into for dk and dv: where the key tiles
+// do not fill the SMs (152), as the first tiles of a causal sequence take longest, as many
+// as give some four items an SM, with as few heads in the largest as these allow.  Their
+// sums, 1024 D bytes of a key head's tile and part, are so at most 100 MB whatever the
+// heads' number.  (dk, dv and join, us.  5003 tokens of 15 + 3 heads of 96: 112 in five
+// parts, 215 in one; 16384 of 64 + 1 heads of 128: 4770 + 130 in five, 5290 + 205 and 1.1 GB
+// in 64; 4096 of 32 + 4: 181 + 24 in four, 215 + 42 in eight.  Three items an SM in place of
+// four: 16384 of 64 + 1 heads 5010 + 460, 2048 of 32 + 1 71 + 22 for 89 + 32.  Below four
+// tiles a launch more costs what it saves.)
 int head_parts(int64_t T, int64_t Hq, int64_t Hk) {
-  const int64_t tiles = ceil_div(T, 128);
-  return tiles >= 4 && tiles * Hk <= 152 ? static_cast<int>(Hq / Hk) : 1;
+  const int64_t items = ceil_div(T, 128) * Hk, per = Hq / Hk;
+  if (items < 4 * Hk || items > 152) return 1;
+  const int64_t each = ceil_div(per, std::min(per, ceil_div(4 * 152, items)));
+  return static_cast<int>(ceil_div(per, each));
 }
 
 // Launches a kernel that waits for the one ahead by itself, once it has set itself up: it
