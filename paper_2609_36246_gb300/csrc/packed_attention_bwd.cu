@@ -154,7 +154,15 @@ __global__ void __launch_bounds__(kDeltaThreads, 8) att_delta_kernel(const AttAr
     const bool mine = lane < kAtOnce && t < p.T;
     const float lse2 = mine ? p.lse[at + t] * kAttLog2e : 0.f;
     int s = seq_of_token(p, __shfl_sync(0xffffffffu, t0, 0));
-    while (mine && s + 1 < p.S && cu_at(p, s + 1) <= t) ++s;
+    // (mostly that sequence or the next; with any number of empty ones between: one after the
+    // other, 4096 of them took 290 us)
+    if (mine) {
+      const auto begun = [&](int later) { return s + later < p.S && cu_at(p, s + later) <= t; };
+      int step = 1;
+      for (; begun(step); step *= 2) s += step;
+      while ((step /= 2) > 0)
+        if (begun(step)) s += step;
+    }
     Seq q;
     q.start = cu_at(p, s);
     q.n = max(q.start, cu_at(p, s + 1)) - q.start;

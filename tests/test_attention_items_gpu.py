@@ -35,6 +35,33 @@ def test_parts_of_the_query_heads(lens, hq, hk):
     base._check(base._case(lens, hq, hk, 32, prefix=100))
 
 
+@pytest.mark.parametrize("at", [0, 1, 2])
+def test_runs_of_empty_sequences(at):
+    """Thousands, before, between and behind sequences that do not begin at a multiple of four."""
+    lens = [[5, 130], [17, 1]]
+    lens.insert(at, [0] * 5000)
+    base._check(base._case(sum(lens, []), 2, 1, 64, pad=7, prefix=3))
+
+
+def test_empty_sequences_between_tokens_cost_no_more_than_before_them():
+    """The same items either way: a token's sequence is not looked for by counting."""
+    best = []
+    for lens in ([0] * 30000 + [4001, 4000], [4001] + [0] * 30000 + [4000]):
+        s = base._case(lens, 4, 4, 64)
+        o, lse = base._forward(s)
+        base._backward(s, o, lse)
+        times = []
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            base._backward(s, o, lse)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        best.append(min(times))
+    assert best[1] < 1.5 * best[0]
+
+
 def _as(limit_ms, run):
     old = os.environ.get("OLIVE_WAIT_LIMIT_MS")
     os.environ["OLIVE_WAIT_LIMIT_MS"] = str(limit_ms)
