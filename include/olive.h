@@ -751,8 +751,9 @@ OLIVE_API olive_status olive_row_norm_fwd(const void* x, const void* residual, c
  *   dx = r (a - mean(a) - n mean(a n)) + g_sum   (mean(a): OLIVE_NORM_LAYER only)
  *   dw = sum over rows of dy n,   db = sum over rows of dy    fp32 [d]
  * dx is the gradient of x and of the residual; it may be dy or g_sum.  db may be
- * NULL.  Sums over rows are fp32 and have a fixed order (some tens of rows in turn,
- * then a tree).  T = 0: dw and db are zeroed.
+ * NULL.  Sums over rows are fp32 and have a fixed order: T / groups rows in turn by each
+ * of up to 1024 groups (widths above 4096: one an SM), up to 32 groups' sums in turn, then
+ * a tree.  T = 0: dw and db are zeroed.
  * workspace: olive_workspace_size(OLIVE_OP_ROW_NORM_BWD, 1, d, 0, 1, 0, 0) bytes.
  */
 OLIVE_API olive_status olive_row_norm_bwd(const void* dy, const void* h, const void* w,

@@ -8,8 +8,9 @@
 // a n) then come from one exchange.
 //
 // Backward: a block takes every so-manieth row, so that a thread keeps the weights'
-// gradients of its columns in registers from beginning to end; the blocks' sums are
-// stored and added in a second launch, in a fixed order.
+// gradients of its columns in registers from beginning to end, in fp32: T / groups rows in
+// turn (at most 1024 groups, 152 above a width of 4096); the blocks' sums are stored and
+// added in a second launch, in a fixed order.
 //
 // Bound by memory.  32768 rows of 4096, bf16, with a residual and its gradient: forward 152
 // us (7.1 TB/s), backward 179 (6.0) and 6 for the weights'.  3001 rows of 2040 in fp32: 10,
