@@ -13,7 +13,7 @@
 // Bound by memory.  32768 tokens of a vocabulary of 151936, rows of 4096 in bf16: look-up 64
 // us, gradient 262 us (5.8 TB/s over dy and dW), of which the sort is some 25 (its launches,
 // and the counts that every block reads) and the joins 10 to 20.  9001 tokens, 4097 rows of
-// 1000 in fp32: 13 and 39 us, five launches in a chain, each starting under the one ahead
+// 1000 in fp32: 13 and 39 us, six launches in a chain, each starting under the one ahead
 // (51 us where each waits for the last one's end).
 #include <algorithm>
 
@@ -480,7 +480,14 @@ void launch_after(const Ctx& c, void (*kernel)(K...), dim3 grid, int threads, si
   cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...);
 }
 
-int sort_tile(int64_t T) { return T <= 65536 ? 2048 : 8192; }
+// Tokens of a sort's block: every block reads all blocks' counts, so larger ones where there
+// are many.  (The last of the sort's launches, us, tiles of 2048, 4096 and 8192, rows of
+// 4096: 65537 tokens 23, 33, 57; 131072 30, 35, 58.  The call, rows of 64: 2^18 tokens 145,
+// 139, 150; 2^20 555, 481, 489; 2^21 1200, 918, 861.  The order is the same with all.)
+int sort_tile(int64_t T) { return T <= 131072 ? 2048 : T <= 1 << 20 ? 4096 : 8192; }
+// Tokens of a unit: short ones spread frequent ids over more blocks, but their joins and the
+// workspace grow with the units' number.  (Sums and joins, us, units of 32 and 128, rows of
+// 4096: 65537 tokens 278 + 63, 295 + 41; 131072 371 + 102, 380 + 49.)
 int sum_unit(int64_t T) { return T <= 65536 ? 32 : 128; }
 
 template <typename T, typename O>
