@@ -1012,7 +1012,8 @@ def _like(cur, t, x, name):
 def olive_row_norm_fwd(x, w, b=None, residual=None, eps: float = 1e-6, kind: str = "layer",
                        save: bool = False, out=None, sum_out=None):
     """Norm of the rows of h = x (+ residual), [T, d] bf16 or fp32: kind "layer"
-    (centred) or "rms", weights w and bias b [d].  Returns (y, h, stats): h is x
+    (centred; the default here and in olive_row_norm_bwd) or "rms" (row_norm's, the
+    autograd form's), weights w and bias b [d].  Returns (y, h, stats): h is x
     itself where there is no residual, stats (save=True) what olive_row_norm_bwd
     takes, else None."""
     T, d, dtype, cur = _norm_args(x, w, "x")
@@ -1039,8 +1040,8 @@ def olive_row_norm_fwd(x, w, b=None, residual=None, eps: float = 1e-6, kind: str
 
 def olive_row_norm_bwd(dy, h, w, stats, g_h=None, kind: str = "layer", need_db: bool = True, ws=None,
                        out=None):
-    """Gradients of olive_row_norm_fwd for the rows h that it normed: (dx, dw, db),
-    dx that of x and of the residual, dw and db fp32 [d] (db None where it is not
+    """Gradients of olive_row_norm_fwd for the rows h that it normed and the kind it was
+    given ("layer" by default, as there): (dx, dw, db), dx that of x and of the residual, dw and db fp32 [d] (db None where it is not
     needed).  g_h, the gradient of h by other ways, is added to dx."""
     T, d, dtype, cur = _norm_args(h, w, "h")
     dev = h.device
@@ -1311,7 +1312,8 @@ def embedding(W, ids, scale=1.0, n_ids=None, dev_status=None):
 
 class RowNorm(torch.autograd.Function):
     """Rows' norm as an autograd op (weights' gradients in the weights' type; first
-    derivatives only): y, or with a residual (y, h) with h the sum."""
+    derivatives only): y, or with a residual (y, h) with h the sum.  Its kind is "rms"
+    unless given, that of the direct calls "layer"."""
 
     @staticmethod
     def forward(ctx, x, w, b=None, residual=None, eps=1e-6, kind="rms"):
@@ -1336,6 +1338,7 @@ class RowNorm(torch.autograd.Function):
 
 
 def row_norm(x, w, b=None, residual=None, eps=1e-6, kind="rms"):
+    """RowNorm's form as a function: note its kind where none is given, "rms"."""
     # (nothing is kept for a backward where autograd is off)
     if _values_only(x, w, b, residual):
         y, h, _ = olive_row_norm_fwd(x, w, b, residual, eps, kind)
