@@ -27,7 +27,10 @@
 // of a shorter launch's cycles).  One sequence of 20011, 8 + 2 heads, with a bias: 575 us,
 // 1.43 PFLOP/s (704 from the first key tile to the last, where every tile raises the
 // reference; 770 with two and a half instructions more a score).  200 sequences of some 41
-// tokens: 45 us, latency.
+// tokens, 16 + 16 heads of 64: 51 us, latency, and two thirds of a tile's rows nobody's.
+// 5003 tokens in 7 sequences, 15 + 3 heads of 96, capped: 73 us, 47 without the cap: tiles
+// that some row does not see whole go through tensor memory once more, and capped scores
+// there take three special functions each.
 #include <algorithm>
 #include <type_traits>
 

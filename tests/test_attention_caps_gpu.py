@@ -57,3 +57,14 @@ def test_scores_of_every_size_in_a_tile(cap):
     s["q"][1::2] *= 64
     s["q"][2::4] *= 2.0 ** -10
     _compare(s, {})
+
+
+@pytest.mark.parametrize("form", [dict(cap=100.0), dict(cap=65.0, bias=True, prefix=20), dict(cap=1e5, causal=False)], ids=str)
+def test_what_is_not_finite_with_a_wide_cap(form):
+    """As with a small one: a bad token behind a sequence's end, or in another one, does not show in a bit."""
+    base.test_what_is_not_finite({**form, "sharp": 4.0})
+
+
+@pytest.mark.parametrize("form", [dict(cap=100.0), dict(cap=70.0, bias=True), dict(prefix=900, cap=100.0)], ids=str)
+def test_the_same_bits_whatever_ran_before_with_a_wide_cap(form):
+    base.test_the_same_bits_whatever_ran_before({**form, "sharp": 4.0})
