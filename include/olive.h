@@ -778,9 +778,10 @@ OLIVE_API olive_status olive_row_norm_bwd(const void* dy, const void* h, const v
  * olive_qk_norm_rope_fwd, so q, k, v may be views of one projection (the token stride is
  * not 0 where T > 1).  lse may be NULL.  Scores, maxima and sums are fp32; the weights
  * exp(s - reference) are rounded to bf16 as operands of the second product (2^-8
- * relative each at most).  What the cap itself adds to a score's error is below 2^-16 up
- * to a cap of 64, and 2^-20 of the score above.  A value that is not finite in a row of k or v reaches rows of its own
- * sequence only (it may reach earlier ones of its 128-row tile).
+ * relative each at most).  What the cap itself adds to a score's error is at most 2^-15
+ * up to a cap of 64, and 2^-20 of the score above.  A value that is not finite in a row of
+ * k or v reaches rows of its own sequence only (it may reach earlier ones of its 128-row
+ * tile).
  *   D a multiple of 8, 8 <= D <= 128; Hq a multiple of Hk, 1 <= Hk <= Hq <= 4096;
  *   S >= 1; 0 <= T <= 2^30; scale > 0; cap >= 0; strides multiples of 8, base pointers
  *   16-byte aligned; the heads of o must not share memory, nor with q, k, v.

@@ -1041,8 +1041,9 @@ def olive_row_norm_fwd(x, w, b=None, residual=None, eps: float = 1e-6, kind: str
 def olive_row_norm_bwd(dy, h, w, stats, g_h=None, kind: str = "layer", need_db: bool = True, ws=None,
                        out=None):
     """Gradients of olive_row_norm_fwd for the rows h that it normed and the kind it was
-    given ("layer" by default, as there): (dx, dw, db), dx that of x and of the residual, dw and db fp32 [d] (db None where it is not
-    needed).  g_h, the gradient of h by other ways, is added to dx."""
+    given ("layer" by default, as there): (dx, dw, db), dx that of x and of the residual,
+    dw and db fp32 [d] (db None where it is not needed).  g_h, the gradient of h by other
+    ways, is added to dx."""
     T, d, dtype, cur = _norm_args(h, w, "h")
     dev = h.device
     _like(cur, dy, h, "dy")

@@ -131,7 +131,10 @@ __device__ __forceinline__ void init_ring(const RingAt& r, int readers) {
 // A wait's limit is that of a tile, a microsecond or two of work: who waits for an item of
 // `steps` tiles as a whole has as many.  (Where the work itself is stuck, those who do it
 // give up after one, and everybody sees their flag.)
-__device__ __forceinline__ WaitCtl for_steps(const WaitCtl& ctl, int steps) { return {ctl.abort, ctl.limit_ns * (1 + static_cast<uint64_t>(steps))}; }
+__device__ __forceinline__ WaitCtl for_steps(const WaitCtl& ctl, int steps) {
+  const uint64_t n = 1 + static_cast<uint64_t>(steps);
+  return {ctl.abort, __umul64hi(ctl.limit_ns, n) == 0 ? ctl.limit_ns * n : ~0ull};  // (a limit that means none stays one)
+}
 // The warp that hands out items.  find(i, item) says whether item i exists; rest(i) is
 // what else is done for every i, after the item is out.
 template <class Item, class Find, class Rest>
@@ -201,8 +204,9 @@ inline int when_to_ask(int64_t items, int sms, int64_t T, int64_t S) {
   return items <= sms ? ASK_NEVER : T / S <= 256 ? ASK_EARLY : ASK_LATE;
 }
 
-// tanh(x) = 1 - 2 / (1 + e^2x), x in units of ln 2 / 2: off by some 2^-23, which is
-// times the cap in a score: up to kWideCap no more than a product's own fp32 sum.
+// tanh(x) = 1 - 2 / (1 + e^2x), x in units of ln 2 / 2: off by some 2^-23 (2^-21 at
+// most), which is times the cap in a score: up to kWideCap as little as a product's own
+// fp32 sum.
 constexpr float kWideCap = 64.f;
 __device__ __forceinline__ float tanh_of(float x2) {
   float r;

@@ -14,8 +14,8 @@
 // 8 sequences of 4096, 32 + 8 heads of 128, causal: 88, 1235 and 1130 us; the seven products
 // run at 1.55 PFLOP/s (tensor pipe active 74 and 62 % of a shorter launch's cycles), near what
 // the power cap leaves.  200 sequences of some 41 tokens, 16 + 16 heads of 64: 9, 95 and 59
-// us (with what each waits for the one ahead), an item's chain of waits.  Each launch starts under the one ahead (225 us forward and
-// backward at that step, 236 without).
+// us (with what each waits for the one ahead), an item's chain of waits.  Each launch starts
+// under the one ahead (225 us forward and backward at that step, 236 without).
 #include <algorithm>
 #include <type_traits>
 

@@ -92,6 +92,18 @@ def test_an_item_longer_than_the_limit_of_a_wait(causal):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_a_limit_that_means_none():
+    """2^50 ms are 15625 2^56 ns: times the 256 that an item of 255 tiles has, they must not become 0."""
+    s = base._case([255 * 128], 2, 2, 64)
+
+    def run():
+        o, lse = base._forward(s)
+        return (o, lse, *base._backward(s, o, lse))
+
+    want = _as(1000, run)
+    assert all(torch.equal(a, b) for a, b in zip(_as(2 ** 50, run), want))
+
+
 def test_prefix_ends_outside_the_sequence():
     """Before its beginning: no key is seen by all rows; behind its end: all are.  However far outside."""
     s = base._case([50, 200, 3], 4, 2, 64, prefix=0)
